@@ -298,6 +298,105 @@ void boa_free_index(boa_index *idx);
 
 const char *boa_last_error(void);
 
+/*
+ * Operators of a query tower: what turns an encoder's output into query
+ * vectors, fits them to the points of an index, and serves them.
+ *
+ * Conventions, beside those above:
+ *   - Every pointer is DEVICE memory. Matrices are row-major with the last
+ *     dimension contiguous; strides are in elements, from row to row.
+ *   - Calls are asynchronous on `stream`: they return once the kernels are
+ *     queued, allocate nothing and can be captured into a graph. Work memory
+ *     is the caller's (16-byte aligned, at least as large as the matching
+ *     _workspace function says) and must not serve two calls at once.
+ *   - Sums, statistics and logits are float32 whatever the element type, and
+ *     results are rounded to it once. There are no atomics: the same inputs
+ *     give the same bits.
+ */
+enum { BOA_T_F32 = 0, BOA_T_BF16 = 1, BOA_T_F16 = 2 };
+
+#define BOA_MAX_NORM_D (1 << 20)
+/*
+ * Layer norm of `rows` rows of d values: y = (x - mean) * rstd * weight + bias,
+ * rstd = 1 / sqrt(mean((x - mean)^2) + eps). weight and bias may be NULL (1, 0);
+ * param_dtype is theirs, dtype or BOA_T_F32. y is dense (rows x d, dtype). mean
+ * and rstd (float32, one per row) are what the backward pass needs, or NULL.
+ * Errors: BOA_EINVAL, BOA_EHIP. */
+int boa_layer_norm(const void *x, int64_t rows, int32_t d, int64_t x_stride, int32_t dtype, const void *weight,
+                   const void *bias, int32_t param_dtype, float eps, void *y, float *mean, float *rstd, void *stream);
+
+/* Work memory of boa_layer_norm_backward in bytes. */
+int64_t boa_layer_norm_backward_workspace(int64_t rows, int32_t d);
+
+/* Gradients of boa_layer_norm: dx (rows x d, dtype), dweight and dbias (d,
+ * param_dtype; zeros without rows). Each may be NULL; the workspace is needed
+ * for dweight or dbias only. */
+int boa_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int64_t rows, int32_t d,
+                            int32_t dtype, const void *weight, int32_t param_dtype, const float *mean,
+                            const float *rstd, void *dx, void *dweight, void *dbias, void *workspace,
+                            int64_t workspace_bytes, void *stream);
+
+#define BOA_MAX_XENT_D 4096
+enum { BOA_REDUCE_NONE = 0, BOA_REDUCE_SUM = 1, BOA_REDUCE_MEAN = 2 };
+/*
+ * Softmax cross entropy of B queries over V points as classes:
+ *   logit[b][v] = scale * (h[b] . points[v]) + bias[v]
+ *   loss[b] = log(sum_v exp(logit[b][v])) - logit[b][labels[b]]
+ * The logits are formed in tiles and never stored.
+ */
+typedef struct {
+    int32_t dtype;          /* of h, points, dh and dpoints: BOA_T_F32 or BOA_T_BF16 */
+    int32_t d;              /* 1 .. BOA_MAX_XENT_D */
+    int64_t B, V;           /* queries (B >= 0), points (V >= 1); both below 2^31 - 2^16 */
+    const void *h;          /* B x d */
+    int64_t h_stride;
+    const void *points;     /* V x d */
+    int64_t points_stride;
+    const int64_t *labels;  /* B: the point each query belongs to. A negative label leaves its
+                               query out (loss 0, gradients 0, not counted by the mean); one of V
+                               or more gives loss NaN and gradients 0 */
+    const float *bias;      /* V, or NULL. -inf leaves a point out; with every point left out a
+                               query's loss is +inf and its gradients are 0. For squared L2 in
+                               place of the inner product: scale = 2 t, bias[v] = -t |points[v]|^2 */
+    float scale;
+    int32_t reduction;      /* of the loss. BOA_REDUCE_MEAN divides by the queries not left out
+                               (0 where there is none) */
+    float *loss;            /* B floats (BOA_REDUCE_NONE) or one */
+    float *lse;             /* B: log of the sum of exponentials, or NULL */
+    /* gradients (boa_softmax_xent_grad only) */
+    const float *dloss;     /* gradient of `loss`, shaped like it; NULL: 1 */
+    void *dh;               /* B x d, dense, or NULL */
+    void *dpoints;          /* V x d, dense, or NULL */
+    float *dbias;           /* V, or NULL */
+} boa_xent;
+
+/* Work memory in bytes of one call with these arguments (grad: of
+ * boa_softmax_xent_grad); a negative BOA_E* code for invalid sizes. */
+int64_t boa_softmax_xent_workspace(const boa_xent *x, int32_t grad);
+
+/* The losses. Errors: BOA_EINVAL, BOA_EUNSUPPORTED (float16: probabilities of
+ * many points fall below its range), BOA_EHIP. */
+int boa_softmax_xent(const boa_xent *x, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* The losses and their gradients in one call. */
+int boa_softmax_xent_grad(const boa_xent *x, void *workspace, int64_t workspace_bytes, void *stream);
+
+#define BOA_MAX_MATVEC_M 65535
+#define BOA_MAX_MATVEC_K (1 << 20)
+/*
+ * Products of M vectors of K values with rows of 4-bit codes:
+ *   y[m][n] = sum_k x[m][k] * w[n][k],
+ *   w[n][k] = scales[n][k / group] * q + offsets[n][k / group],
+ * or scales * (q - 8) where offsets is NULL. codes: rows x (K + 1) / 2 bytes,
+ * byte j holds the code of k = 2j in its low nibble and of 2j + 1 in its high
+ * nibble (as in boa_set_pq), codes_stride bytes from row to row. scales and
+ * offsets share scale_dtype and scale_stride. x and y have `dtype`, any of the
+ * three. A non-finite x makes its vector's results NaN or infinite.
+ * Errors: BOA_EINVAL, BOA_EHIP. */
+int boa_matvec_fourbit(const void *x, int64_t M, int64_t x_stride, int32_t dtype, const uint8_t *codes, int64_t rows,
+                       int32_t K, int64_t codes_stride, const void *scales, const void *offsets, int64_t scale_stride,
+                       int32_t scale_dtype, int32_t group, void *y, int64_t y_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

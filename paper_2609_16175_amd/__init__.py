@@ -272,3 +272,15 @@ class Index:
 
     def reset_counters(self):
         _check(lib().boa_reset_counters(self._h))
+
+
+# The query-tower operators (ops.py), loaded on first use: they import torch.
+_OPS = ("layer_norm", "layer_norm_forward", "layer_norm_backward", "softmax_xent", "softmax_xent_grad", "XentResult",
+        "matvec_4bit")
+
+
+def __getattr__(name):
+    if name in _OPS:
+        from . import ops
+        return getattr(ops, name)
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

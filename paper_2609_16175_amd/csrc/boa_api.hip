@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "boa_internal.h"
+#include "boa_ops.h"
 
 using namespace boa;
 
@@ -158,6 +159,8 @@ struct boa_index {
     };
     mutable Occupancy occ[256] = {};
 };
+
+int boa::set_error(int code, const char *msg) { return fail(code, msg); }
 
 extern "C" {
 

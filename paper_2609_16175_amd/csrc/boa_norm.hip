@@ -1,0 +1,495 @@
+// Layer norm of rows and its gradient.
+//
+// Forward, per row x of d values: mu = mean(x), v = mean((x - mu)^2),
+// r = 1 / sqrt(v + eps), y = (x - mu) r w + b. Backward, with xh = (x - mu) r
+// and g = dy w: dx = r (g - mean(g) - xh mean(g xh)); dw = sum over rows of
+// dy xh, db = sum over rows of dy.
+//
+// Both are bound by memory: a row is read once into registers (TPR threads,
+// NV loads of VEC values each), its sums are taken in float32 over the values
+// held (the variance from x - mu, so that a large mean costs no digits), and
+// the result is written from the same registers. The backward pass keeps each
+// thread's columns of dw and db in registers over all rows of its block and
+// leaves one partial row per block, which a second kernel adds in block order:
+// no atomics, so results do not depend on the schedule.
+#include <algorithm>
+
+#include "boa_ops.h"
+
+using namespace boa;
+
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int64_t MAX_BLOCKS = 1024;   // of the backward pass: 4 per CU, each with one partial row of dw and db
+
+struct NormArgs {
+    const void *x, *dy, *w, *b;
+    void *y;                     // forward: y; backward: dx
+    float *mean, *rstd;
+    float *partial;              // backward: blocks x 2 x d
+    int64_t rows, x_stride, dy_stride;
+    int32_t d;
+    float eps;
+};
+
+// Sum of a value over the TPR threads of a row (a wave, or the block).
+template <int TPR>
+__device__ inline float row_sum(float v, float *red)
+{
+    v = wave_sum(v);
+    if constexpr (TPR > 64) {
+        const int wave = threadIdx.x >> 6;
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) red[wave] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < TPR / 64; ++i) v += red[i];
+    }
+    return v;
+}
+
+// Two sums at once.
+template <int TPR>
+__device__ inline void row_sum2(float &a, float &b, float *red)
+{
+    a = wave_sum(a);
+    b = wave_sum(b);
+    if constexpr (TPR > 64) {
+        const int wave = threadIdx.x >> 6;
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+            red[wave] = a;
+            red[4 + wave] = b;
+        }
+        __syncthreads();
+        a = b = 0.0f;
+#pragma unroll
+        for (int i = 0; i < TPR / 64; ++i) {
+            a += red[i];
+            b += red[4 + i];
+        }
+    }
+}
+
+template <class T, class P, int VEC, int NV, int TPR>
+__global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a)
+{
+    __shared__ float red[8];
+    const int lane = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
+    if (row >= a.rows) return;   // a whole wave (TPR 64) or block (TPR 256) leaves
+    const int32_t d = a.d;
+    const T *x = (const T *)a.x + row * a.x_stride;
+    float v[NV][VEC];
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + lane) * VEC;
+        if (c < d) {
+            load_f32<VEC, T>(v[i], x + c);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) v[i][j] = 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) s += v[i][j];
+    }
+    const float mu = row_sum<TPR>(s, red) / (float)d;
+    float q = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + lane) * VEC;
+        if (c < d) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                v[i][j] -= mu;
+                q = fmaf(v[i][j], v[i][j], q);
+            }
+        }
+    }
+    const float r = 1.0f / sqrtf(row_sum<TPR>(q, red) / (float)d + a.eps);
+    if (lane == 0) {
+        if (a.mean) a.mean[row] = mu;
+        if (a.rstd) a.rstd[row] = r;
+    }
+    T *y = (T *)a.y + row * (int64_t)d;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + lane) * VEC;
+        if (c >= d) continue;
+        float o[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) o[j] = v[i][j] * r;
+        if (a.w) {
+            float w[VEC];
+            load_f32<VEC, P>(w, (const P *)a.w + c);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) o[j] *= w[j];
+        }
+        if (a.b) {
+            float b[VEC];
+            load_f32<VEC, P>(b, (const P *)a.b + c);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) o[j] += b[j];
+        }
+        store_f32<VEC, T>(y + c, o);
+    }
+}
+
+// Rows wider than the registers: a block per row, read three times (the
+// second and third time from the caches).
+template <class T, class P>
+__global__ __launch_bounds__(THREADS) void norm_wide_kernel(NormArgs a)
+{
+    __shared__ float red[8];
+    const int64_t row = blockIdx.x;
+    const int32_t d = a.d;
+    const T *x = (const T *)a.x + row * a.x_stride;
+    T *y = (T *)a.y + row * (int64_t)d;
+    float s = 0.0f;
+    for (int c = threadIdx.x; c < d; c += THREADS) s += (float)x[c];
+    const float mu = row_sum<THREADS>(s, red) / (float)d;
+    float q = 0.0f;
+    for (int c = threadIdx.x; c < d; c += THREADS) {
+        const float t = (float)x[c] - mu;
+        q = fmaf(t, t, q);
+    }
+    const float r = 1.0f / sqrtf(row_sum<THREADS>(q, red) / (float)d + a.eps);
+    if (threadIdx.x == 0) {
+        if (a.mean) a.mean[row] = mu;
+        if (a.rstd) a.rstd[row] = r;
+    }
+    for (int c = threadIdx.x; c < d; c += THREADS) {
+        float o = ((float)x[c] - mu) * r;
+        if (a.w) o *= (float)((const P *)a.w)[c];
+        if (a.b) o += (float)((const P *)a.b)[c];
+        y[c] = (T)o;
+    }
+}
+
+// DX: dx is wanted; DP: dw and db are.
+template <class T, class P, int VEC, int NV, int TPR, bool DP>
+__global__ __launch_bounds__(THREADS) void norm_back_kernel(NormArgs a)
+{
+    __shared__ float red[8];
+    extern __shared__ float cols[];   // 2 x d, where several rows share a block
+    constexpr int GROUPS = THREADS / TPR;
+    const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const int32_t d = a.d;
+    float w[NV][VEC], dw[NV][VEC], db[NV][VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + lane) * VEC;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            w[i][j] = c < d ? 1.0f : 0.0f;
+            dw[i][j] = db[i][j] = 0.0f;
+        }
+        if (a.w && c < d) load_f32<VEC, P>(w[i], (const P *)a.w + c);
+    }
+    for (int64_t row = (int64_t)blockIdx.x * GROUPS + group; row < a.rows; row += (int64_t)gridDim.x * GROUPS) {
+        const T *x = (const T *)a.x + row * a.x_stride;
+        const T *dy = (const T *)a.dy + row * a.dy_stride;
+        const float mu = a.mean[row], r = a.rstd[row];
+        float xh[NV][VEC], g[NV][VEC];
+        float c1 = 0.0f, c2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + lane) * VEC;
+            if (c < d) {
+                load_f32<VEC, T>(xh[i], x + c);
+                load_f32<VEC, T>(g[i], dy + c);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    xh[i][j] = mu;
+                    g[i][j] = 0.0f;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                xh[i][j] = (xh[i][j] - mu) * r;
+                if (DP) {
+                    dw[i][j] = fmaf(g[i][j], xh[i][j], dw[i][j]);
+                    db[i][j] += g[i][j];
+                }
+                g[i][j] *= w[i][j];
+                c1 += g[i][j];
+                c2 = fmaf(g[i][j], xh[i][j], c2);
+            }
+        }
+        if (a.y) {
+            row_sum2<TPR>(c1, c2, red);
+            c1 /= (float)d;
+            c2 /= (float)d;
+            T *dx = (T *)a.y + row * (int64_t)d;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * TPR + lane) * VEC;
+                if (c >= d) continue;
+                float o[VEC];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) o[j] = r * (g[i][j] - c1 - xh[i][j] * c2);
+                store_f32<VEC, T>(dx + c, o);
+            }
+        }
+    }
+    if constexpr (DP) {
+        float *out = a.partial + (int64_t)blockIdx.x * 2 * d;
+        if constexpr (GROUPS == 1) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * TPR + lane) * VEC;
+                if (c >= d) continue;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    out[c + j] = dw[i][j];
+                    out[d + c + j] = db[i][j];
+                }
+            }
+        } else {
+            for (int k = 0; k < GROUPS; ++k) {   // the block's rows of waves added in wave order
+                if (group == k) {
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) {
+                        const int c = (i * TPR + lane) * VEC;
+                        if (c >= d) continue;
+#pragma unroll
+                        for (int j = 0; j < VEC; ++j) {
+                            cols[c + j] = k ? cols[c + j] + dw[i][j] : dw[i][j];
+                            cols[d + c + j] = k ? cols[d + c + j] + db[i][j] : db[i][j];
+                        }
+                    }
+                }
+                __syncthreads();
+            }
+            for (int c = threadIdx.x; c < 2 * d; c += THREADS) out[c] = cols[c];
+        }
+    }
+}
+
+// Rows wider than the registers: dx by a block per row ...
+template <class T, class P>
+__global__ __launch_bounds__(THREADS) void norm_back_wide_kernel(NormArgs a)
+{
+    __shared__ float red[8];
+    const int64_t row = blockIdx.x;
+    const int32_t d = a.d;
+    const T *x = (const T *)a.x + row * a.x_stride;
+    const T *dy = (const T *)a.dy + row * a.dy_stride;
+    const float mu = a.mean[row], r = a.rstd[row];
+    float c1 = 0.0f, c2 = 0.0f;
+    for (int c = threadIdx.x; c < d; c += THREADS) {
+        const float g = (float)dy[c] * (a.w ? (float)((const P *)a.w)[c] : 1.0f);
+        c1 += g;
+        c2 = fmaf(g, ((float)x[c] - mu) * r, c2);
+    }
+    row_sum2<THREADS>(c1, c2, red);
+    c1 /= (float)d;
+    c2 /= (float)d;
+    T *dx = (T *)a.y + row * (int64_t)d;
+    for (int c = threadIdx.x; c < d; c += THREADS) {
+        const float g = (float)dy[c] * (a.w ? (float)((const P *)a.w)[c] : 1.0f);
+        dx[c] = (T)(r * (g - c1 - ((float)x[c] - mu) * r * c2));
+    }
+}
+
+// ... and dw, db by a block per 256 columns and stripe of rows.
+template <class T>
+__global__ __launch_bounds__(THREADS) void norm_cols_kernel(NormArgs a)
+{
+    const int c = blockIdx.y * THREADS + threadIdx.x;
+    const int32_t d = a.d;
+    if (c >= d) return;
+    float dw = 0.0f, db = 0.0f;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const float g = (float)((const T *)a.dy)[row * a.dy_stride + c];
+        const float xh = ((float)((const T *)a.x)[row * a.x_stride + c] - a.mean[row]) * a.rstd[row];
+        dw = fmaf(g, xh, dw);
+        db += g;
+    }
+    a.partial[(int64_t)blockIdx.x * 2 * d + c] = dw;
+    a.partial[(int64_t)blockIdx.x * 2 * d + d + c] = db;
+}
+
+// Adds the blocks' partial rows: 64 columns of dw | db per block, 16 slices
+// of the partial rows, then the slices in order.
+template <class P>
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float *partial, int32_t blocks, int32_t d, P *dw, P *db)
+{
+    __shared__ float part[16][64];
+    const int col = threadIdx.x & 63, slice = threadIdx.x >> 6;
+    const int c = blockIdx.x * 64 + col;
+    float s = 0.0f;
+    if (c < 2 * d)
+        for (int i = slice; i < blocks; i += 16) s += partial[(int64_t)i * 2 * d + c];
+    part[slice][col] = s;
+    __syncthreads();
+    if (slice == 0 && c < 2 * d) {
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += part[i][col];
+        if (c < d) {
+            if (dw) dw[c] = (P)s;
+        } else if (db) {
+            db[c - d] = (P)s;
+        }
+    }
+}
+
+// Calls f(T{}, P{}) for an element type and a parameter type: the parameters
+// have the rows' type or are float32.
+template <class F>
+int with_types(int32_t dtype, int32_t param, F f)
+{
+    if (dtype == BOA_T_F32) return f(0.0f, 0.0f);
+    if (dtype == BOA_T_BF16) return param == BOA_T_F32 ? f(bf16_t{}, 0.0f) : f(bf16_t{}, bf16_t{});
+    return param == BOA_T_F32 ? f(f16_t{}, 0.0f) : f(f16_t{}, f16_t{});
+}
+
+// The registers a row takes: f(VEC, NV, TPR) as compile-time constants.
+// Vector loads where every row allows them. A wave per row up to 4 loads a
+// lane, then a block per row; false where a row does not fit.
+template <int V>
+struct Int {
+    static constexpr int value = V;
+};
+
+template <int VECMAX, class F>
+bool with_shape(int32_t d, bool vec, F f)
+{
+    if (vec) {
+        const int64_t n = ceil_div(d, VECMAX);
+        if (n <= 64) f(Int<VECMAX>{}, Int<1>{}, Int<64>{});
+        else if (n <= 128) f(Int<VECMAX>{}, Int<2>{}, Int<64>{});
+        else if (n <= 192) f(Int<VECMAX>{}, Int<3>{}, Int<64>{});
+        else if (n <= 256) f(Int<VECMAX>{}, Int<4>{}, Int<64>{});
+        else if (n <= 512) f(Int<VECMAX>{}, Int<2>{}, Int<256>{});
+        else if (n <= 1024) f(Int<VECMAX>{}, Int<4>{}, Int<256>{});
+        else return false;
+        return true;
+    }
+    if (d <= 128) f(Int<1>{}, Int<2>{}, Int<64>{});
+    else if (d <= 256) f(Int<1>{}, Int<4>{}, Int<64>{});
+    else if (d <= 512) f(Int<1>{}, Int<8>{}, Int<64>{});
+    else if (d <= 1024) f(Int<1>{}, Int<16>{}, Int<64>{});
+    else if (d <= 4096) f(Int<1>{}, Int<16>{}, Int<256>{});
+    else return false;
+    return true;
+}
+
+bool rows_allow(const void *p, int64_t stride, int64_t esize)
+{
+    return aligned(p, 16) && (stride * esize) % 16 == 0;
+}
+
+int check_norm(const char *what, const void *x, int64_t rows, int32_t d, int64_t x_stride, int32_t dtype, int32_t param,
+               bool has_param)
+{
+    char msg[160];
+    const char *why = nullptr;
+    if (!dtype_known(dtype)) why = "unknown dtype";
+    else if (has_param && param != dtype && param != BOA_T_F32) why = "parameters must have the rows' type or be float32";
+    else if (rows < 0 || rows >= (int64_t)1 << 31) why = "rows out of range [0, 2^31)";
+    else if (d < 1 || d > BOA_MAX_NORM_D) why = "d out of range [1, 2^20]";
+    else if (rows > 1 && x_stride < d) why = "row stride smaller than d";
+    else if (rows && !x) why = "NULL rows";
+    if (!why) return BOA_OK;
+    __builtin_snprintf(msg, sizeof(msg), "%s: %s", what, why);
+    return set_error(BOA_EINVAL, msg);
+}
+
+int64_t back_blocks(int64_t rows, int32_t d)
+{
+    // as many partial rows as blocks: at most 4 per CU, fewer where the partial
+    // rows would outweigh the input
+    return std::max<int64_t>(1, std::min<int64_t>(MAX_BLOCKS, ceil_div(rows, 8)));
+}
+
+}  // namespace
+
+extern "C" {
+
+int boa_layer_norm(const void *x, int64_t rows, int32_t d, int64_t x_stride, int32_t dtype, const void *weight,
+                   const void *bias, int32_t param_dtype, float eps, void *y, float *mean, float *rstd, void *stream)
+{
+    if (int rc = check_norm("layer_norm", x, rows, d, x_stride, dtype, param_dtype, weight || bias)) return rc;
+    if (!(eps >= 0.0f)) return set_error(BOA_EINVAL, "layer_norm: eps must not be negative");
+    if (rows && !y) return set_error(BOA_EINVAL, "layer_norm: NULL output");
+    if (rows == 0) return BOA_OK;
+    NormArgs a{};
+    a.x = x, a.w = weight, a.b = bias, a.y = y, a.mean = mean, a.rstd = rstd;
+    a.rows = rows, a.x_stride = x_stride, a.d = d, a.eps = eps;
+    hipStream_t st = (hipStream_t)stream;
+    return with_types(dtype, (weight || bias) ? param_dtype : dtype, [&](auto t, auto p) {
+        using T = decltype(t);
+        using P = decltype(p);
+        constexpr int VMAX = 16 / sizeof(T);
+        const bool vec = d % VMAX == 0 && rows_allow(x, x_stride, sizeof(T)) && aligned(y, 16) && aligned(weight, 16)
+                         && aligned(bias, 16);
+        const bool fits = with_shape<VMAX>(d, vec, [&](auto ve, auto nv, auto tpr) {
+            constexpr int VEC = decltype(ve)::value, NV = decltype(nv)::value, TPR = decltype(tpr)::value;
+            const int64_t blocks = ceil_div(rows, THREADS / TPR);
+            norm_kernel<T, P, VEC, NV, TPR><<<dim3((uint32_t)blocks), THREADS, 0, st>>>(a);
+        });
+        if (!fits) norm_wide_kernel<T, P><<<dim3((uint32_t)rows), THREADS, 0, st>>>(a);
+        return launch_status("layer_norm");
+    });
+}
+
+int64_t boa_layer_norm_backward_workspace(int64_t rows, int32_t d)
+{
+    if (rows < 0 || d < 1) return 0;
+    return back_blocks(rows, d) * 2 * d * (int64_t)sizeof(float);
+}
+
+int boa_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int64_t rows, int32_t d,
+                            int32_t dtype, const void *weight, int32_t param_dtype, const float *mean,
+                            const float *rstd, void *dx, void *dweight, void *dbias, void *workspace,
+                            int64_t workspace_bytes, void *stream)
+{
+    const bool params = dweight || dbias;
+    if (int rc = check_norm("layer_norm_backward", x, rows, d, x_stride, dtype, param_dtype, weight || params)) return rc;
+    if (rows && (!dy || !mean || !rstd)) return set_error(BOA_EINVAL, "layer_norm_backward: NULL input");
+    if (rows > 1 && dy_stride < d) return set_error(BOA_EINVAL, "layer_norm_backward: row stride smaller than d");
+    if (params && (!workspace || !aligned(workspace, 16)
+                   || workspace_bytes < boa_layer_norm_backward_workspace(rows, d)))
+        return set_error(BOA_EINVAL, "layer_norm_backward: workspace missing, unaligned or too small");
+    if (!params && (!dx || rows == 0)) return BOA_OK;
+    NormArgs a{};
+    a.x = x, a.dy = dy, a.w = weight, a.y = dx, a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
+    a.rows = rows, a.x_stride = x_stride, a.dy_stride = dy_stride, a.d = d, a.partial = (float *)workspace;
+    hipStream_t st = (hipStream_t)stream;
+    return with_types(dtype, (weight || params) ? param_dtype : dtype, [&](auto t, auto p) {
+        using T = decltype(t);
+        using P = decltype(p);
+        constexpr int VMAX = 16 / sizeof(T);
+        const bool vec = d % VMAX == 0 && rows_allow(x, x_stride, sizeof(T)) && rows_allow(dy, dy_stride, sizeof(T))
+                         && aligned(dx, 16) && aligned(weight, 16);
+        const int64_t blocks = back_blocks(rows, d);
+        const bool fits = with_shape<VMAX>(d, vec, [&](auto ve, auto nv, auto tpr) {
+            constexpr int VEC = decltype(ve)::value, NV = decltype(nv)::value, TPR = decltype(tpr)::value;
+            const size_t lds = TPR < THREADS ? (size_t)2 * d * sizeof(float) : 0;
+            if (params)
+                norm_back_kernel<T, P, VEC, NV, TPR, true><<<dim3((uint32_t)blocks), THREADS, lds, st>>>(a);
+            else
+                norm_back_kernel<T, P, VEC, NV, TPR, false><<<dim3((uint32_t)blocks), THREADS, 0, st>>>(a);
+        });
+        if (!fits) {
+            if (dx && rows) norm_back_wide_kernel<T, P><<<dim3((uint32_t)rows), THREADS, 0, st>>>(a);
+            if (params)
+                norm_cols_kernel<T><<<dim3((uint32_t)blocks, (uint32_t)ceil_div(d, THREADS)), THREADS, 0, st>>>(a);
+        }
+        if (params)
+            norm_join_kernel<P><<<dim3((uint32_t)ceil_div(2 * (int64_t)d, 64)), 1024, 0, st>>>(
+                (const float *)workspace, (int32_t)blocks, d, (P *)dweight, (P *)dbias);
+        return launch_status("layer_norm_backward");
+    });
+}
+
+}  // extern "C"

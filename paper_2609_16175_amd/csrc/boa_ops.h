@@ -1,0 +1,69 @@
+// Shared by the query-tower operators (boa_norm.hip, boa_xent.hip,
+// boa_matvec.hip): element types, wave reductions, error reporting.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "boa.h"
+
+namespace boa {
+
+// boa_api.hip: records the thread's error message and returns the code
+int set_error(int code, const char *msg);
+
+typedef __bf16 bf16_t;
+typedef _Float16 f16_t;
+
+inline int64_t dtype_bytes(int32_t t) { return t == BOA_T_F32 ? 4 : 2; }
+inline bool dtype_known(int32_t t) { return t == BOA_T_F32 || t == BOA_T_BF16 || t == BOA_T_F16; }
+inline bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// the error a launch left, as a return code of the C interface
+inline int launch_status(const char *what)
+{
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return BOA_OK;
+    char msg[256];
+    __builtin_snprintf(msg, sizeof(msg), "%s: %s", what, hipGetErrorString(e));
+    return set_error(BOA_EHIP, msg);
+}
+
+template <int N, class T>
+struct alignas(N * sizeof(T)) Pack {
+    T v[N];
+};
+
+template <int N, class T>
+__device__ inline void load_f32(float (&to)[N], const T *p)
+{
+    const Pack<N, T> a = *reinterpret_cast<const Pack<N, T> *>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) to[i] = (float)a.v[i];
+}
+
+template <int N, class T>
+__device__ inline void store_f32(T *p, const float (&from)[N])
+{
+    Pack<N, T> a;
+#pragma unroll
+    for (int i = 0; i < N; ++i) a.v[i] = (T)from[i];
+    *reinterpret_cast<Pack<N, T> *>(p) = a;
+}
+
+__device__ inline float wave_sum(float v)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+__device__ inline float wave_max(float v)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+
+}  // namespace boa

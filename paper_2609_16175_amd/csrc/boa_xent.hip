@@ -1,0 +1,1047 @@
+// Softmax cross entropy of B queries over V points as classes, with its
+// gradients, in pieces of the points and without keeping the logits.
+//
+//   l_bv = scale h_b . c_v + bias_v     lse_b = log sum_v exp l_bv
+//   loss_b = lse_b - l_b,y(b)           q_bv  = g_b (exp(l_bv - lse_b) - [v = y_b])
+//   dh_b = scale sum_v q_bv c_v         dc_v  = scale sum_b q_bv h_b      dbias_v = sum_b q_bv
+//
+// Every product runs on the bf16 matrix instructions with float32 sums, one
+// tile routine for all of them (tile_product). float32 inputs are split into
+// three bf16 parts whose sum is the value (8 + 8 + 8 bits), and the six
+// products of parts above 2^-24 of the result are added: float32's precision
+// at six bf16 products, against sixteen times the cost of the float32
+// instructions' one.
+//
+// The losses take one pass over the points: a block keeps, per query, the
+// running maximum and sum of exponentials of its share of the points; the
+// shares are joined afterwards. The gradients take a second pass over pieces
+// of the points: probabilities of a piece from the logits formed again (two
+// more bits of work per logit than storing them would cost in memory
+// traffic), rounded to the products' type, then the two products. The label's
+// own entry is left out of the rounded probabilities and added in float32, so
+// that a query whose point has nearly all the probability keeps its digits.
+#include <algorithm>
+#include <cmath>
+
+#include "boa_ops.h"
+
+using namespace boa;
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+// running maximum of nothing: exp2(-inf - NO_MAX) is 0 and not NaN, and logits at the type's lowest value still count
+constexpr float NO_MAX = -__FLT_MAX__;
+constexpr int BK = 64;               // values of k per stage: 128 bytes of a row
+constexpr int MAX_SEG = 6;
+
+// One operand: `rows` rows of bf16, `ld` values apart. Rows past the end are
+// read as the last one (their results are dropped).
+struct Operand {
+    const bf16_t *p;
+    int64_t ld;
+    int32_t rows;
+};
+
+// A product over segments of k: K values (a multiple of 16) of the parts
+// seg_a[i] and seg_b[i] (offsets in values), i < segs.
+struct Product {
+    Operand a, b;
+    int32_t K, segs;
+    int64_t seg_a[MAX_SEG], seg_b[MAX_SEG];
+};
+
+template <int WM_, int WN_, int TM_, int TN_>
+struct Shape {
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_;
+    static constexpr int BM = WM * TM * 32, BN = WN * TN * 32, THREADS = 64 * WM * WN;
+    static constexpr int STAGE = (BM + BN) * BK;   // bf16 values of one stage
+};
+
+// acc += A[row0a ..][k] * B[row0b ..][k], k in [from_k, from_k + K), over all
+// segments. Two stages of
+// BK values of k: the loads of the next stage go straight to LDS while the
+// matrix instructions work on this one. A stage holds rows of 128 bytes whose
+// 16-byte chunks are stored in the order chunk ^ (row & 7), so that the 32
+// rows a fragment reads at one k spread over the banks; the permutation is
+// applied to the addresses loaded from, since a load to LDS writes its lanes
+// in order.
+template <class S>
+__device__ inline void tile_product(const Product &pr, int32_t row0a, int32_t row0b, bf16_t *lds,
+                                    f32x16 (&acc)[S::TM][S::TN], int32_t from_k, int32_t K)
+{
+    constexpr int NA = (S::BM * 8 + S::THREADS - 1) / S::THREADS, NB = (S::BN * 8 + S::THREADS - 1) / S::THREADS;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int wm = wave % S::WM, wn = wave / S::WM;
+    const int chunk = (t & 7) ^ ((t >> 3) & 7);
+    const bf16_t *pa[NA], *pb[NB];
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+        pa[i] = pr.a.p + (int64_t)min(row0a + i * (S::THREADS / 8) + (t >> 3), pr.a.rows - 1) * pr.a.ld + from_k;
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+        pb[i] = pr.b.p + (int64_t)min(row0b + i * (S::THREADS / 8) + (t >> 3), pr.b.rows - 1) * pr.b.ld + from_k;
+    const int per_seg = (K + BK - 1) / BK, total = per_seg * pr.segs;
+
+    auto load = [&](int stage, int seg, int k0) {
+        bf16_t *to = lds + stage * S::STAGE;
+        // chunks past K are not multiplied: read the row's first instead
+        const int k = k0 + chunk * 8 < K ? k0 + chunk * 8 : 0;
+        const int64_t oa = pr.seg_a[seg] + k, ob = pr.seg_b[seg] + k;
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if ((i * S::THREADS + wave * 64) < S::BM * 8)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(pa[i] + oa),
+                                                 (__attribute__((address_space(3))) void *)(to + (i * S::THREADS + wave * 64) * 8),
+                                                 16, 0, 0);
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+            if ((i * S::THREADS + wave * 64) < S::BN * 8)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(pb[i] + ob),
+                                                 (__attribute__((address_space(3))) void *)(to + S::BM * BK + (i * S::THREADS + wave * 64) * 8),
+                                                 16, 0, 0);
+    };
+
+    const int r = lane & 31, half = lane >> 5;
+    const int at_a = (wm * S::TM * 32 + r) * BK, at_b = S::BM * BK + (wn * S::TN * 32 + r) * BK;
+    load(0, 0, 0);
+    __syncthreads();
+    int seg = 0, k0 = 0;
+    for (int it = 0; it < total; ++it) {
+        const int steps = min(BK, K - k0) >> 4;
+        k0 += BK;
+        if (k0 >= K) {
+            k0 = 0;
+            ++seg;
+        }
+        if (it + 1 < total) load((it + 1) & 1, seg, k0);
+        const bf16_t *from = lds + (it & 1) * S::STAGE;
+#pragma unroll
+        for (int s = 0; s < BK / 16; ++s) {
+            if (s < steps) {
+                const int c = ((s * 2 + half) ^ (r & 7)) * 8;
+                bf16x8 fa[S::TM], fb[S::TN];
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i) fa[i] = *(const bf16x8 *)(from + at_a + i * 32 * BK + c);
+#pragma unroll
+                for (int j = 0; j < S::TN; ++j) fb[j] = *(const bf16x8 *)(from + at_b + j * 32 * BK + c);
+#pragma unroll
+                for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::TN; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Row of a 32 x 32 tile that a lane's value i stands for (the column is lane & 31).
+__device__ inline int tile_row(int i, int half) { return (i >> 2) * 8 + half * 4 + (i & 3); }
+
+// Work item of a block: `minor` blocks that share operand rows run on one XCD
+// (blocks go to the 8 XCDs in turn). False: nothing to do.
+__device__ inline bool split_block(int32_t majors, int32_t minors, int32_t *major, int32_t *minor)
+{
+    const int32_t id = (int32_t)blockIdx.x, local = id >> 3;
+    *major = (id & 7) + 8 * (local / minors);
+    *minor = local % minors;
+    return *major < majors;
+}
+inline uint32_t split_grid(int64_t majors, int64_t minors) { return (uint32_t)(ceil_div(majors, 8) * 8 * minors); }
+
+template <class S>
+__device__ inline void clear(f32x16 (&acc)[S::TM][S::TN])
+{
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+}
+
+// ---------------------------------------------------------------------------
+// operands
+
+// Copies a block of 64 rows x 64 columns of `src` (R x C) as bf16 parts:
+// `plain` [part][rows_pad][cols_pad] and `across` [part][cols][across_ld],
+// zeros past the end. Either may be null.
+template <class T>
+__global__ __launch_bounds__(256) void parts_kernel(const T *src, int64_t stride, int32_t R, int32_t C, bf16_t *plain,
+                                                    int64_t plain_ld, int64_t plain_part, int32_t rows_pad,
+                                                    bf16_t *across, int64_t across_ld, int64_t across_part,
+                                                    int32_t across_rows)
+{
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+    __shared__ bf16_t tile[PARTS][64][66];
+    const int32_t r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+    const int c = threadIdx.x & 63;
+    for (int r = threadIdx.x >> 6; r < 64; r += 4) {
+        float v = 0.0f;
+        if (r0 + r < R && c0 + c < C) v = (float)src[(int64_t)(r0 + r) * stride + c0 + c];
+        if constexpr (PARTS == 1) {
+            tile[0][r][c] = (bf16_t)v;
+        } else {
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                const float part = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
+                tile[p][r][c] = (bf16_t)part;
+                v = fabsf(part) < INFINITY ? v - part : 0.0f;   // an infinity or NaN is its first part alone
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+        if (plain)
+            for (int r = threadIdx.x >> 6; r < 64; r += 4)
+                if (r0 + r < rows_pad && c0 + c < plain_ld)
+                    plain[p * plain_part + (int64_t)(r0 + r) * plain_ld + c0 + c] = tile[p][r][c];
+        if (across)
+            for (int k = threadIdx.x >> 6; k < 64; k += 4)
+                if (c0 + k < across_rows && r0 + c < across_ld)
+                    across[p * across_part + (int64_t)(c0 + k) * across_ld + r0 + c] = tile[p][c][k];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// losses
+
+struct RowState {
+    float m, s;   // running maximum (base 2) and sum of exponentials
+};
+
+// A point's bias in base 2. Finite ones stay finite, masks of the type's lowest
+// value among them.
+__device__ inline float base2(float bias)
+{
+    return fabsf(bias) < INFINITY ? fmaxf(-__FLT_MAX__, fminf(__FLT_MAX__, bias * LOG2E)) : bias;
+}
+
+struct StatsArgs {
+    Product pr;              // a: points, b: queries
+    const float *bias;
+    RowState *part;          // splits x B
+    float scale2;            // scale * log2(e)
+    int32_t B, V, tiles_v, tiles_b, splits;
+};
+
+__device__ inline void join(RowState &a, float m, float s)
+{
+    const float top = fmaxf(a.m, m);
+    a.s = a.s * __builtin_amdgcn_exp2f(a.m - top) + s * __builtin_amdgcn_exp2f(m - top);
+    a.m = top;
+}
+
+// A block takes every splits-th tile of points for one tile of queries. A
+// lane's values belong to TN queries (the columns of its tiles), so the
+// running states stay in its registers until the end.
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void stats_kernel(StatsArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) bf16_t lds[];
+    int32_t split, tb;
+    if (!split_block(a.splits, a.tiles_b, &split, &tb)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int wm = wave % S::WM, wn = wave / S::WM;
+    RowState st[S::TN];
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) st[j] = RowState{NO_MAX, 0.0f};
+    for (int32_t tv = split; tv < a.tiles_v; tv += a.splits) {
+        f32x16 acc[S::TM][S::TN];
+        clear<S>(acc);
+        tile_product<S>(a.pr, tv * S::BM, tb * S::BN, lds, acc, 0, a.pr.K);
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i) {
+            const int32_t v0 = tv * S::BM + (wm * S::TM + i) * 32;
+            float off[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int32_t v = v0 + tile_row(e, half);
+                off[e] = v >= a.V ? -INFINITY : a.bias ? base2(a.bias[v]) : 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) {
+                float top = st[j].m;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    acc[i][j][e] = fmaf(acc[i][j][e], a.scale2, off[e]);
+                    top = fmaxf(top, acc[i][j][e]);
+                }
+                float s = st[j].s * __builtin_amdgcn_exp2f(st[j].m - top);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(acc[i][j][e] - top);
+                st[j] = RowState{top, s};
+            }
+        }
+    }
+    RowState *red = (RowState *)lds;   // WM x BN; the product has passed its last barrier
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+        const float m = __shfl_xor(st[j].m, 32), s = __shfl_xor(st[j].s, 32);
+        join(st[j], m, s);
+        if (half == 0) red[wm * S::BN + (wn * S::TN + j) * 32 + lane] = st[j];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < S::BN; c += S::THREADS) {
+        const int32_t b = tb * S::BN + c;
+        if (b >= a.B) continue;
+        RowState one = red[c];
+        for (int w = 1; w < S::WM; ++w) join(one, red[w * S::BN + c].m, red[w * S::BN + c].s);
+        a.part[(int64_t)split * a.B + b] = one;
+    }
+}
+
+struct RowArgs {
+    const void *h, *points;
+    int64_t h_stride, points_stride;
+    const int64_t *labels;
+    const float *bias, *dloss;
+    const RowState *part;
+    float *loss;             // per query (the caller's, or scratch where the loss is reduced)
+    float *lse;              // the caller's, or null
+    float *top;              // rows_pad: the largest logit, base 2
+    float *rowf;             // rows_pad: g / sum of 2^(l - top), 0 for a query without gradient
+    float *coef;             // B: g * (p_label - 1)
+    int32_t *label;          // rows_pad: the label, or -1 where it has no entry
+    float scale;
+    int32_t B, V, d, splits, reduction, rows_pad;
+};
+
+// A wave per query: joins the splits, forms the label's logit in float32.
+template <class T>
+__global__ __launch_bounds__(256) void row_kernel(RowArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const int32_t b = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (b >= a.rows_pad) return;
+    if (b >= a.B) {
+        if (lane == 0) {
+            a.top[b] = 0.0f;
+            a.rowf[b] = 0.0f;
+            a.label[b] = -1;
+        }
+        return;
+    }
+    RowState st{NO_MAX, 0.0f};
+    for (int i = lane; i < a.splits; i += 64) {
+        const RowState o = a.part[(int64_t)i * a.B + b];
+        join(st, o.m, o.s);
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        const float m = __shfl_xor(st.m, o), s = __shfl_xor(st.s, o);
+        join(st, m, s);
+    }
+    const int64_t y = a.labels[b];
+    const bool in = y >= 0 && y < a.V;
+    float dot = 0.0f;
+    if (in) {
+        const T *h = (const T *)a.h + (int64_t)b * a.h_stride, *c = (const T *)a.points + y * a.points_stride;
+        for (int k = lane; k < a.d; k += 64) dot = fmaf((float)h[k], (float)c[k], dot);
+        dot = wave_sum(dot);
+    }
+    if (lane) return;
+    const bool none = st.s == 0.0f;   // every point left out
+    const float log_s = __builtin_amdgcn_logf(st.s);
+    const float l2 = in ? fmaf(dot, a.scale * LOG2E, a.bias ? base2(a.bias[y]) : 0.0f) : 0.0f;
+    float loss = 0.0f;
+    if (y >= a.V) loss = NAN;
+    else if (in) loss = none ? INFINITY : ((st.m - l2) + log_s) * LN2;
+    a.loss[b] = loss;
+    if (a.lse) a.lse[b] = none ? -INFINITY : (st.m + log_s) * LN2;
+    const float g = !in || none ? 0.0f : a.reduction == BOA_REDUCE_NONE && a.dloss ? a.dloss[b] : 1.0f;
+    a.top[b] = none ? 0.0f : st.m;
+    a.rowf[b] = g == 0.0f ? 0.0f : g / st.s;
+    a.label[b] = in && !none ? (int32_t)y : -1;
+    if (a.coef) a.coef[b] = in && !none ? g * (__builtin_amdgcn_exp2f(l2 - st.m) / st.s - 1.0f) : 0.0f;
+}
+
+// One block: the reduced loss, and the factor every gradient gets.
+__global__ __launch_bounds__(1024) void total_kernel(const float *row_loss, const int64_t *labels, int32_t B,
+                                                     int32_t reduction, const float *dloss, float *loss, float *factor)
+{
+    __shared__ float ls[16], ns[16];
+    float s = 0.0f, n = 0.0f;
+    for (int32_t b = threadIdx.x; b < B; b += 1024) {
+        s += row_loss[b];
+        n += labels[b] >= 0 ? 1.0f : 0.0f;
+    }
+    s = wave_sum(s);
+    n = wave_sum(n);
+    if ((threadIdx.x & 63) == 0) {
+        ls[threadIdx.x >> 6] = s;
+        ns[threadIdx.x >> 6] = n;
+    }
+    __syncthreads();
+    if (threadIdx.x) return;
+    s = n = 0.0f;
+    for (int i = 0; i < 16; ++i) {
+        s += ls[i];
+        n += ns[i];
+    }
+    const float by = reduction == BOA_REDUCE_MEAN ? fmaxf(n, 1.0f) : 1.0f;
+    if (loss) *loss = s / by;
+    if (factor) *factor = (dloss && reduction != BOA_REDUCE_NONE ? *dloss : 1.0f) / by;
+}
+
+// ---------------------------------------------------------------------------
+// gradients
+
+struct ProbArgs {
+    Product pr;              // a: queries, b: points of the piece
+    const float *bias;       // of the piece
+    const float *top, *rowf;
+    const int32_t *label;
+    bf16_t *p, *pt;          // [part][rows_pad][cols_pad], [part][cols_pad][rows_pad], or null
+    float *col;              // tiles_b x cols_pad: sums over the tile's queries, or null
+    float scale2;
+    int32_t B, V, v0;        // v0: the piece's first point
+    int32_t n, cols_pad, rows_pad, tiles_b, tiles_v;
+};
+
+// bf16 part `part` of PARTS of a value (see parts_kernel); one part rounds.
+template <int PARTS>
+__device__ inline bf16_t part_of(float v, int part)
+{
+    if constexpr (PARTS == 1) return (bf16_t)v;
+    float top = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
+#pragma unroll
+    for (int i = 0; i < PARTS - 1; ++i)
+        if (i < part) {
+            v -= top;
+            top = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
+        }
+    return (bf16_t)top;
+}
+
+// Probabilities of a tile of queries and points of the piece, without the
+// labels' own entries, written through LDS as rows of queries (p) and rows of
+// points (pt).
+template <class S, int PARTS>
+__global__ __launch_bounds__(S::THREADS) void prob_kernel(ProbArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) bf16_t lds[];
+    int32_t tv, tb;
+    if (!split_block(a.tiles_v, a.tiles_b, &tv, &tb)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, r = lane & 31;
+    const int wm = wave % S::WM, wn = wave / S::WM;
+    f32x16 acc[S::TM][S::TN];
+    clear<S>(acc);
+    tile_product<S>(a.pr, tb * S::BM, tv * S::BN, lds, acc, 0, a.pr.K);
+    float off[S::TN];
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+        const int32_t v = tv * S::BN + (wn * S::TN + j) * 32 + r;
+        off[j] = v >= a.n ? -INFINITY : a.bias ? base2(a.bias[v]) : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) {
+        const int32_t b0 = tb * S::BM + (wm * S::TM + i) * 32;
+        const int32_t mine = a.label[b0 + r] - a.v0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int32_t b = b0 + tile_row(e, half);
+            const float top = a.top[b], f = a.rowf[b];
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) {
+                const float l = fmaf(acc[i][j][e], a.scale2, off[j]);
+                acc[i][j][e] = f == 0.0f ? 0.0f : f * __builtin_amdgcn_exp2f(l - top);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+            const int32_t c0 = tv * S::BN + (wn * S::TN + j) * 32;
+            if (__any(mine >= c0 && mine < c0 + 32)) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (__shfl(mine, tile_row(e, half)) == c0 + r) acc[i][j][e] = 0.0f;
+            }
+        }
+    }
+    if (a.col) {
+        float *red = (float *)lds;   // WM x BN
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s += acc[i][j][e];
+            s += __shfl_xor(s, 32);
+            if (half == 0) red[wm * S::BN + (wn * S::TN + j) * 32 + r] = s;
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < S::BN; c += S::THREADS) {
+            float s = 0.0f;
+            for (int w = 0; w < S::WM; ++w) s += red[w * S::BN + c];
+            a.col[(int64_t)tb * a.cols_pad + tv * S::BN + c] = s;
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+        if (a.p) {
+            constexpr int LD = S::BN + 8;
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        lds[((wm * S::TM + i) * 32 + tile_row(e, half)) * LD + (wn * S::TN + j) * 32 + r]
+                            = part_of<PARTS>(acc[i][j][e], part);
+            __syncthreads();
+            bf16_t *to = a.p + ((int64_t)part * a.rows_pad + tb * S::BM) * a.cols_pad + tv * S::BN;
+            for (int c = threadIdx.x; c < S::BM * (S::BN / 8); c += S::THREADS) {
+                const int row = c / (S::BN / 8), col = c % (S::BN / 8) * 8;
+                *(bf16x8 *)(to + (int64_t)row * a.cols_pad + col) = *(const bf16x8 *)(lds + row * LD + col);
+            }
+            __syncthreads();
+        }
+        if (a.pt) {
+            constexpr int LD = S::BM + 8;
+#pragma unroll
+            for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        bf16x4 four;
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) four[f] = part_of<PARTS>(acc[i][j][e + f], part);
+                        *(bf16x4 *)(lds + ((wn * S::TN + j) * 32 + r) * LD + (wm * S::TM + i) * 32 + tile_row(e, half)) = four;
+                    }
+            __syncthreads();
+            bf16_t *to = a.pt + ((int64_t)part * a.cols_pad + tv * S::BN) * a.rows_pad + tb * S::BM;
+            for (int c = threadIdx.x; c < S::BN * (S::BM / 8); c += S::THREADS) {
+                const int row = c / (S::BM / 8), col = c % (S::BM / 8) * 8;
+                *(bf16x8 *)(to + (int64_t)row * a.rows_pad + col) = *(const bf16x8 *)(lds + row * LD + col);
+            }
+            __syncthreads();
+        }
+    }
+}
+
+struct DhArgs {
+    Product pr;              // a: probabilities, b: the piece's points across
+    float *part;             // splits x rows_pad x d
+    int32_t d, rows_pad, tiles_b, tiles_d, splits, k_split, first;
+};
+
+// A split's share of sum_v p_bv c_v over the piece, added to what earlier
+// pieces left.
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void dh_kernel(DhArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) bf16_t lds[];
+    int32_t split, tile;
+    if (!split_block(a.splits, a.tiles_b * a.tiles_d, &split, &tile)) return;
+    const int32_t tb = tile / a.tiles_d, td = tile % a.tiles_d;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, r = lane & 31;
+    const int wm = wave % S::WM, wn = wave / S::WM;
+    const int32_t k0 = split * a.k_split, K = min(a.k_split, a.pr.K - k0);
+    f32x16 acc[S::TM][S::TN];
+    clear<S>(acc);
+    if (K > 0) tile_product<S>(a.pr, tb * S::BM, td * S::BN, lds, acc, k0, K);
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+            const int32_t c = td * S::BN + (wn * S::TN + j) * 32 + r;
+            if (c >= a.d) continue;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int32_t b = tb * S::BM + (wm * S::TM + i) * 32 + tile_row(e, half);
+                float *to = a.part + ((int64_t)split * a.rows_pad + b) * a.d + c;
+                *to = a.first ? acc[i][j][e] : *to + acc[i][j][e];
+            }
+        }
+}
+
+struct DcArgs {
+    Product pr;              // a: probabilities across, b: the queries across
+    void *out;               // of the piece
+    const int32_t *first;    // V: the first query of a point, or -1
+    const float *own;        // B x d: the labels' own terms, by first query
+    const float *factor;
+    float scale;
+    int32_t n, d, v0, tiles_v, tiles_d;
+};
+
+template <class S, class T>
+__global__ __launch_bounds__(S::THREADS) void dc_kernel(DcArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) bf16_t lds[];
+    int32_t tv, td;
+    if (!split_block(a.tiles_v, a.tiles_d, &tv, &td)) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, r = lane & 31;
+    const int wm = wave % S::WM, wn = wave / S::WM;
+    f32x16 acc[S::TM][S::TN];
+    clear<S>(acc);
+    tile_product<S>(a.pr, tv * S::BM, td * S::BN, lds, acc, 0, a.pr.K);
+    const float by = a.scale * *a.factor;
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int32_t v = tv * S::BM + (wm * S::TM + i) * 32 + tile_row(e, half);
+            if (v >= a.n) continue;
+            const int32_t first = a.first[a.v0 + v];
+#pragma unroll
+            for (int j = 0; j < S::TN; ++j) {
+                const int32_t c = td * S::BN + (wn * S::TN + j) * 32 + r;
+                if (c >= a.d) continue;
+                float x = acc[i][j][e];
+                if (first >= 0) x += a.own[(int64_t)first * a.d + c];
+                ((T *)a.out)[(int64_t)v * a.d + c] = (T)(by * x);
+            }
+        }
+}
+
+// A block per query b that is its point's first: own[b] = sum over the point's
+// queries, in order, of coef * h; first[point] = b; own_bias[b] likewise.
+template <class T>
+__global__ __launch_bounds__(256) void own_kernel(const T *h, int64_t h_stride, int32_t B, int32_t d,
+                                                  const int32_t *label, const float *coef, int32_t *first, float *own,
+                                                  float *own_bias)
+{
+    __shared__ int earlier;
+    __shared__ int32_t list[256];
+    __shared__ int count;
+    const int32_t b = blockIdx.x, y = label[b];
+    if (y < 0) return;
+    if (threadIdx.x == 0) earlier = 0;
+    __syncthreads();
+    for (int32_t i = threadIdx.x; i < b; i += 256)
+        if (label[i] == y) earlier = 1;
+    __syncthreads();
+    if (earlier) return;
+    float sb = 0.0f;
+    float acc[BOA_MAX_XENT_D / 256];
+#pragma unroll
+    for (int k = 0; k < BOA_MAX_XENT_D / 256; ++k) acc[k] = 0.0f;
+    for (int32_t i0 = b; i0 < B; i0 += 256) {
+        // the queries of this stretch that share the label, in order
+        __syncthreads();
+        if (threadIdx.x == 0) count = 0;
+        __syncthreads();
+        const int32_t i = i0 + threadIdx.x;
+        const bool hit = i < B && label[i] == y;
+        const uint64_t in_wave = __ballot(hit);
+        for (int w = 0; w < 4; ++w) {
+            if ((threadIdx.x >> 6) == w && in_wave) {
+                const int at = count + __popcll(in_wave & ((1ull << (threadIdx.x & 63)) - 1));
+                if (hit) list[at] = i;
+                __builtin_amdgcn_wave_barrier();
+                if ((threadIdx.x & 63) == 0) count += __popcll(in_wave);
+            }
+            __syncthreads();
+        }
+        for (int j = 0; j < count; ++j) {
+            const int32_t q = list[j];
+            const float c = coef[q];
+            sb += c;
+#pragma unroll
+            for (int k = 0; k < BOA_MAX_XENT_D / 256; ++k)
+                if (k * 256 + (int)threadIdx.x < d)
+                    acc[k] = fmaf(c, (float)h[(int64_t)q * h_stride + k * 256 + threadIdx.x], acc[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < BOA_MAX_XENT_D / 256; ++k)
+        if (k * 256 + (int)threadIdx.x < d && own) own[(int64_t)b * d + k * 256 + threadIdx.x] = acc[k];
+    if (threadIdx.x == 0) {
+        first[y] = b;
+        own_bias[b] = sb;
+    }
+}
+
+__global__ __launch_bounds__(256) void fill_kernel(int32_t *p, int64_t n, int32_t v)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = v;
+}
+
+__global__ __launch_bounds__(256) void dbias_kernel(const float *col, int32_t tiles_b, int32_t cols_pad, int32_t n,
+                                                    int32_t v0, const int32_t *first, const float *own_bias,
+                                                    const float *factor, float *out)
+{
+    const int32_t v = blockIdx.x * 256 + threadIdx.x;
+    if (v >= n) return;
+    float s = 0.0f;
+    for (int32_t t = 0; t < tiles_b; ++t) s += col[(int64_t)t * cols_pad + v];
+    const int32_t f = first[v0 + v];
+    if (f >= 0) s += own_bias[f];
+    out[v] = s * *factor;
+}
+
+// dh = scale factor (sum of the splits + coef c_label)
+template <class T>
+__global__ __launch_bounds__(256) void dh_join_kernel(const float *part, int32_t splits, int32_t rows_pad, int32_t B,
+                                                      int32_t d, const T *points, int64_t points_stride,
+                                                      const int32_t *label, const float *coef, const float *factor,
+                                                      float scale, T *dh)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)B * d) return;
+    const int32_t b = (int32_t)(i / d), c = (int32_t)(i % d);
+    float s = 0.0f;
+    for (int32_t k = 0; k < splits; ++k) s += part[((int64_t)k * rows_pad + b) * d + c];
+    const int32_t y = label[b];
+    if (y >= 0) s = fmaf(coef[b], (float)points[(int64_t)y * points_stride + c], s);
+    dh[i] = (T)(scale * *factor * s);
+}
+
+// ---------------------------------------------------------------------------
+// host side
+
+int64_t round_up(int64_t a, int64_t to) { return ceil_div(a, to) * to; }
+
+// Where everything lies in the workspace, for one call's sizes.
+struct Plan {
+    int32_t parts, Kp, tile_b, rows_pad, tiles_b;
+    bool direct;               // the points are read where they are
+    int32_t splits;            // of the statistics
+    int64_t Vc, cols_pad;      // points per piece, and its padded size
+    int32_t dh_splits, dh_k;
+    int64_t off_h, off_ht, off_c, off_ct, off_part, off_loss, off_top, off_rowf, off_coef, off_label, off_factor;
+    int64_t off_p, off_pt, off_col, off_dh, off_first, off_own, off_ownb, total;
+};
+
+bool points_direct(const boa_xent *x)
+{
+    return x->dtype == BOA_T_BF16 && x->d % 16 == 0 && aligned(x->points, 16) && x->points_stride % 8 == 0;
+}
+
+Plan make_plan(const boa_xent *x, bool grad)
+{
+    Plan p{};
+    p.parts = x->dtype == BOA_T_F32 ? 3 : 1;
+    p.direct = points_direct(x);
+    p.Kp = (int32_t)round_up(x->d, 16);
+    p.tile_b = x->B <= 32 ? 32 : x->B <= 128 ? 128 : 256;
+    p.tiles_b = (int32_t)ceil_div(x->B, p.tile_b);
+    p.rows_pad = p.tiles_b * p.tile_b;
+    const int64_t tiles_v = ceil_div(x->V, 256);
+    // the losses' splits: a block per CU (its stages fill LDS), and no more than there are tiles
+    p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles_v, 256 / p.tiles_b));
+    // a piece's probabilities: 128 MB in each order, half of the last-level cache
+    const int64_t per = (int64_t)p.rows_pad * 2 * p.parts;
+    int64_t vc = std::max<int64_t>(1024, ((int64_t)128 << 20) / per / 1024 * 1024);
+    if (!p.direct)   // and its copied points
+        vc = std::min(vc, std::max<int64_t>(1024, ((int64_t)128 << 20) / ((int64_t)p.Kp * 2 * p.parts) / 1024 * 1024));
+    p.Vc = std::min(vc, round_up(x->V, 256));
+    p.cols_pad = round_up(p.Vc, 256);
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t o = at;
+        at += round_up(std::max<int64_t>(bytes, 16), 256);
+        return o;
+    };
+    p.off_h = take((int64_t)p.parts * p.rows_pad * p.Kp * 2);
+    if (!p.direct) p.off_c = take((int64_t)p.parts * p.cols_pad * p.Kp * 2);
+    // a piece's tiles are split like all of them where there are several pieces
+    p.off_part = take((int64_t)p.splits * ceil_div(x->V, p.Vc) * x->B * sizeof(RowState));
+    p.off_loss = take(x->B * 4);
+    p.off_top = take(p.rows_pad * 4);
+    p.off_rowf = take(p.rows_pad * 4);
+    p.off_label = take(p.rows_pad * 4);
+    p.off_factor = take(16);
+    if (grad) {
+        p.off_coef = take(x->B * 4);
+        if (x->dh) {
+            const int32_t tile_d = x->d <= 32 ? 32 : x->d <= 128 ? 128 : 256;
+            const int64_t tiles = p.tiles_b * ceil_div(x->d, tile_d);
+            const int64_t want = std::max<int64_t>(1, 512 / tiles);
+            p.dh_k = (int32_t)round_up(ceil_div(p.cols_pad, std::min(want, ceil_div(p.cols_pad, 256))), 64);
+            p.dh_splits = (int32_t)ceil_div(p.cols_pad, p.dh_k);
+            p.off_p = take(per * p.cols_pad);
+            p.off_ct = take((int64_t)p.parts * x->d * p.cols_pad * 2);
+            p.off_dh = take((int64_t)p.dh_splits * p.rows_pad * x->d * 4);
+        }
+        if (x->dpoints) {
+            p.off_pt = take(per * p.cols_pad);
+            p.off_ht = take((int64_t)p.parts * x->d * p.rows_pad * 2);
+            p.off_own = take(x->B * (int64_t)x->d * 4);
+        }
+        if (x->dbias) p.off_col = take((int64_t)p.tiles_b * p.cols_pad * 4);
+        if (x->dpoints || x->dbias) {
+            p.off_first = take(x->V * 4);
+            p.off_ownb = take(x->B * 4);
+        }
+    }
+    p.total = at;
+    return p;
+}
+
+// The part products of one operand pair: of the nine products of three parts
+// each, the six above 2^-24 of the result, smallest first.
+void set_segments(Product &pr, int32_t parts, int64_t part_a, int64_t part_b)
+{
+    if (parts == 1) {
+        pr.segs = 1;
+        pr.seg_a[0] = pr.seg_b[0] = 0;
+        return;
+    }
+    static const int ia[6] = {2, 1, 0, 1, 0, 0}, ib[6] = {0, 1, 2, 0, 1, 0};
+    pr.segs = 6;
+    for (int i = 0; i < 6; ++i) {
+        pr.seg_a[i] = ia[i] * part_a;
+        pr.seg_b[i] = ib[i] * part_b;
+    }
+}
+
+template <class S>
+constexpr size_t stage_bytes()
+{
+    return 2 * S::STAGE * sizeof(bf16_t);
+}
+
+template <class K, class A>
+void run(K kernel, uint32_t grid, uint32_t threads, size_t lds, hipStream_t st, const A &args)
+{
+    // LDS above 64 KB has to be asked for
+    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    kernel<<<dim3(grid), threads, lds, st>>>(args);
+}
+
+template <class F>
+void with_tile(int32_t n, F f)   // 32, 128 or 256 rows of the smaller side
+{
+    if (n <= 32) f(std::integral_constant<int, 32>{});
+    else if (n <= 128) f(std::integral_constant<int, 128>{});
+    else f(std::integral_constant<int, 256>{});
+}
+
+template <int BM, int BN>
+struct Pick;
+template <> struct Pick<256, 256> { using S = Shape<2, 4, 4, 2>; };
+template <> struct Pick<256, 128> { using S = Shape<4, 2, 2, 2>; };
+template <> struct Pick<128, 256> { using S = Shape<2, 4, 2, 2>; };
+template <> struct Pick<128, 128> { using S = Shape<2, 4, 2, 1>; };
+template <> struct Pick<256, 32> { using S = Shape<8, 1, 1, 1>; };
+template <> struct Pick<32, 256> { using S = Shape<1, 8, 1, 1>; };
+template <> struct Pick<128, 32> { using S = Shape<4, 1, 1, 1>; };
+template <> struct Pick<32, 128> { using S = Shape<1, 4, 1, 1>; };
+template <> struct Pick<32, 32> { using S = Shape<1, 1, 1, 1>; };
+
+int check(const boa_xent *x, bool grad)
+{
+    auto bad = [](const char *why) { return set_error(BOA_EINVAL, why); };
+    if (!x) return bad("softmax_xent: NULL arguments");
+    if (x->dtype == BOA_T_F16)
+        return set_error(BOA_EUNSUPPORTED, "softmax_xent: float16 does not hold the probabilities of many points; use bfloat16 or float32");
+    if (x->dtype != BOA_T_F32 && x->dtype != BOA_T_BF16) return bad("softmax_xent: unknown dtype");
+    if (x->d < 1 || x->d > BOA_MAX_XENT_D) return bad("softmax_xent: d out of range [1, 4096]");
+    if (x->B < 0 || x->B > ((int64_t)1 << 31) - (1 << 16)) return bad("softmax_xent: B out of range");
+    if (x->V < 1 || x->V > ((int64_t)1 << 31) - (1 << 16)) return bad("softmax_xent: V out of range");
+    if (x->reduction < BOA_REDUCE_NONE || x->reduction > BOA_REDUCE_MEAN) return bad("softmax_xent: unknown reduction");
+    if ((x->B > 1 && x->h_stride < x->d) || (x->V > 1 && x->points_stride < x->d))
+        return bad("softmax_xent: row stride smaller than d");
+    if (!std::isfinite(x->scale)) return bad("softmax_xent: scale must be finite");
+    if (grad && x->dbias && !x->bias) return bad("softmax_xent: a gradient of bias without a bias");
+    return BOA_OK;
+}
+
+template <class T>
+int run_xent(const boa_xent *x, bool grad, uint8_t *ws, hipStream_t st)
+{
+    const Plan p = make_plan(x, grad);
+    const int32_t B = (int32_t)x->B, V = (int32_t)x->V, d = x->d;
+    const bool reduced = x->reduction != BOA_REDUCE_NONE;
+    bf16_t *hp = (bf16_t *)(ws + p.off_h), *ht = grad && x->dpoints ? (bf16_t *)(ws + p.off_ht) : nullptr;
+    float *row_loss = reduced ? (float *)(ws + p.off_loss) : x->loss;
+    float *factor = (float *)(ws + p.off_factor);
+    const int64_t h_part = (int64_t)p.rows_pad * p.Kp, ht_part = (int64_t)d * p.rows_pad;
+
+    parts_kernel<T><<<dim3((uint32_t)ceil_div(p.rows_pad, 64), (uint32_t)ceil_div(p.Kp, 64)), 256, 0, st>>>(
+        (const T *)x->h, x->h_stride, B, d, hp, p.Kp, h_part, p.rows_pad, ht, p.rows_pad, ht_part, d);
+
+    const int32_t pieces = (int32_t)ceil_div(V, p.Vc);
+    auto points_of = [&](int64_t v0, int32_t n, bool across) {
+        Operand o{};
+        bf16_t *cp = p.direct ? nullptr : (bf16_t *)(ws + p.off_c);
+        bf16_t *ct = across ? (bf16_t *)(ws + p.off_ct) : nullptr;
+        if (cp || ct)
+            parts_kernel<T><<<dim3((uint32_t)(p.cols_pad / 64), (uint32_t)ceil_div(p.Kp, 64)), 256, 0, st>>>(
+                (const T *)x->points + v0 * x->points_stride, x->points_stride, n, d, cp, p.Kp,
+                p.cols_pad * p.Kp, (int32_t)p.cols_pad, ct, p.cols_pad, (int64_t)d * p.cols_pad, d);
+        o.p = cp ? cp : (const bf16_t *)x->points + v0 * x->points_stride;
+        o.ld = cp ? p.Kp : x->points_stride;
+        o.rows = cp ? (int32_t)p.cols_pad : n;
+        return o;
+    };
+
+    // losses: all points at once where they are read in place, else by pieces
+    {
+        const int32_t step = p.direct ? V : (int32_t)p.Vc;
+        int32_t used = 0;
+        for (int64_t v0 = 0; v0 < V; v0 += step) {
+            const int32_t n = (int32_t)std::min<int64_t>(step, V - v0);
+            StatsArgs a{};
+            a.pr.a = points_of(v0, n, false);
+            a.pr.b = Operand{hp, p.Kp, p.rows_pad};
+            a.pr.K = p.Kp;
+            set_segments(a.pr, p.parts, p.cols_pad * p.Kp, h_part);
+            a.bias = x->bias ? x->bias + v0 : nullptr;
+            a.scale2 = x->scale * LOG2E;
+            a.B = B, a.V = n, a.tiles_b = p.tiles_b;
+            a.tiles_v = (int32_t)ceil_div(n, 256);
+            a.splits = std::min(p.splits, a.tiles_v);
+            a.part = (RowState *)(ws + p.off_part) + (int64_t)used * B;
+            used += a.splits;
+            with_tile(p.tile_b, [&](auto bn) {
+                using S = typename Pick<256, decltype(bn)::value>::S;
+                run(stats_kernel<S>, split_grid(a.splits, a.tiles_b), S::THREADS, stage_bytes<S>(), st, a);
+            });
+        }
+        RowArgs r{};
+        r.h = x->h, r.points = x->points, r.h_stride = x->h_stride, r.points_stride = x->points_stride;
+        r.labels = x->labels, r.bias = x->bias, r.dloss = grad ? x->dloss : nullptr;
+        r.part = (RowState *)(ws + p.off_part), r.loss = row_loss, r.lse = x->lse;
+        r.top = (float *)(ws + p.off_top), r.rowf = (float *)(ws + p.off_rowf);
+        r.coef = grad ? (float *)(ws + p.off_coef) : nullptr, r.label = (int32_t *)(ws + p.off_label);
+        r.scale = x->scale, r.B = B, r.V = V, r.d = d, r.splits = used, r.reduction = x->reduction, r.rows_pad = p.rows_pad;
+        row_kernel<T><<<dim3((uint32_t)ceil_div(p.rows_pad, 4)), 256, 0, st>>>(r);
+        if (reduced || grad)
+            total_kernel<<<1, 1024, 0, st>>>(row_loss, x->labels, B, x->reduction, grad ? x->dloss : nullptr,
+                                             reduced ? x->loss : nullptr, grad ? factor : nullptr);
+    }
+    if (!grad || !(x->dh || x->dpoints || x->dbias)) return launch_status("softmax_xent");
+
+    const int32_t *label = (const int32_t *)(ws + p.off_label);
+    const float *coef = (const float *)(ws + p.off_coef);
+    int32_t *first = nullptr;
+    float *own = nullptr, *own_bias = nullptr;
+    if (x->dpoints || x->dbias) {
+        first = (int32_t *)(ws + p.off_first);
+        own_bias = (float *)(ws + p.off_ownb);
+        own = x->dpoints ? (float *)(ws + p.off_own) : nullptr;
+        fill_kernel<<<dim3((uint32_t)std::min<int64_t>(1024, ceil_div(V, 256))), 256, 0, st>>>(first, V, -1);
+        own_kernel<T><<<dim3((uint32_t)B), 256, 0, st>>>((const T *)x->h, x->h_stride, B, d, label, coef, first, own, own_bias);
+    }
+    const int64_t p_part = (int64_t)p.rows_pad * p.cols_pad;
+    for (int32_t i = 0; i < pieces; ++i) {
+        const int32_t v0 = (int32_t)(i * p.Vc), n = (int32_t)std::min<int64_t>(p.Vc, V - v0);
+        const int32_t tiles_v = (int32_t)ceil_div(n, 256);
+        ProbArgs a{};
+        a.pr.a = Operand{hp, p.Kp, p.rows_pad};
+        a.pr.b = points_of(v0, n, x->dh != nullptr);
+        a.pr.K = p.Kp;
+        set_segments(a.pr, p.parts, h_part, p.cols_pad * p.Kp);
+        a.bias = x->bias ? x->bias + v0 : nullptr;
+        a.top = (const float *)(ws + p.off_top), a.rowf = (const float *)(ws + p.off_rowf), a.label = label;
+        a.p = x->dh ? (bf16_t *)(ws + p.off_p) : nullptr;
+        a.pt = x->dpoints ? (bf16_t *)(ws + p.off_pt) : nullptr;
+        a.col = x->dbias ? (float *)(ws + p.off_col) : nullptr;
+        a.scale2 = x->scale * LOG2E;
+        a.B = B, a.V = V, a.v0 = v0, a.n = n, a.cols_pad = (int32_t)p.cols_pad, a.rows_pad = p.rows_pad;
+        a.tiles_b = p.tiles_b, a.tiles_v = tiles_v;
+        with_tile(p.tile_b, [&](auto bm) {
+            using S = typename Pick<decltype(bm)::value, 256>::S;
+            const size_t lds = std::max(stage_bytes<S>(), sizeof(bf16_t) * std::max<size_t>(S::BM * (S::BN + 8), S::BN * (S::BM + 8)));
+            if (p.parts == 1) run(prob_kernel<S, 1>, split_grid(tiles_v, p.tiles_b), S::THREADS, lds, st, a);
+            else run(prob_kernel<S, 3>, split_grid(tiles_v, p.tiles_b), S::THREADS, lds, st, a);
+        });
+        if (x->dbias)
+            dbias_kernel<<<dim3((uint32_t)ceil_div(n, 256)), 256, 0, st>>>(a.col, p.tiles_b, (int32_t)p.cols_pad, n, v0, first,
+                                                                          own_bias, factor, x->dbias + v0);
+        if (x->dh) {
+            DhArgs g{};
+            g.pr.a = Operand{a.p, p.cols_pad, p.rows_pad};
+            g.pr.b = Operand{(const bf16_t *)(ws + p.off_ct), p.cols_pad, d};
+            g.pr.K = tiles_v * 256;
+            set_segments(g.pr, p.parts, p_part, (int64_t)d * p.cols_pad);
+            g.part = (float *)(ws + p.off_dh);
+            g.d = d, g.rows_pad = p.rows_pad, g.tiles_b = p.tiles_b, g.splits = p.dh_splits, g.k_split = p.dh_k, g.first = i == 0;
+            with_tile(p.tile_b, [&](auto bm) {
+                with_tile(d, [&](auto bn) {
+                    using S = typename Pick<decltype(bm)::value, decltype(bn)::value>::S;
+                    g.tiles_d = (int32_t)ceil_div(d, S::BN);
+                    run(dh_kernel<S>, split_grid(g.splits, g.tiles_b * g.tiles_d), S::THREADS, stage_bytes<S>(), st, g);
+                });
+            });
+        }
+        if (x->dpoints) {
+            DcArgs g{};
+            g.pr.a = Operand{a.pt, p.rows_pad, (int32_t)p.cols_pad};
+            g.pr.b = Operand{ht, p.rows_pad, d};
+            g.pr.K = p.rows_pad;
+            set_segments(g.pr, p.parts, p_part, ht_part);
+            g.out = (T *)x->dpoints + (int64_t)v0 * d;
+            g.first = first, g.own = own, g.factor = factor, g.scale = x->scale;
+            g.n = n, g.d = d, g.v0 = v0, g.tiles_v = tiles_v;
+            with_tile(d, [&](auto bn) {
+                using S = typename Pick<256, decltype(bn)::value>::S;
+                g.tiles_d = (int32_t)ceil_div(d, S::BN);
+                run(dc_kernel<S, T>, split_grid(tiles_v, g.tiles_d), S::THREADS, stage_bytes<S>(), st, g);
+            });
+        }
+    }
+    if (x->dh)
+        dh_join_kernel<T><<<dim3((uint32_t)ceil_div((int64_t)B * d, 256)), 256, 0, st>>>(
+            (const float *)(ws + p.off_dh), p.dh_splits, p.rows_pad, B, d, (const T *)x->points, x->points_stride, label,
+            coef, factor, x->scale, (T *)x->dh);
+    return launch_status("softmax_xent_grad");
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void zero_kernel(T *p, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = (T)0.0f;
+}
+
+template <class T>
+void zero(T *p, int64_t n, hipStream_t st)
+{
+    if (p && n) zero_kernel<<<dim3((uint32_t)std::min<int64_t>(4096, ceil_div(n, 256))), 256, 0, st>>>(p, n);
+}
+
+int xent(const boa_xent *x, bool grad, void *ws, int64_t ws_bytes, void *stream)
+{
+    if (int rc = check(x, grad)) return rc;
+    auto bad = [](const char *why) { return set_error(BOA_EINVAL, why); };
+    if (!x->points || (x->B && (!x->h || !x->labels))) return bad("softmax_xent: NULL input");
+    if (!x->loss && (x->B || x->reduction != BOA_REDUCE_NONE)) return bad("softmax_xent: NULL loss");
+    hipStream_t st = (hipStream_t)stream;
+    if (x->B == 0) {   // nothing to learn from: a loss of 0, gradients of 0
+        if (x->reduction != BOA_REDUCE_NONE) zero(x->loss, 1, st);
+        if (grad) {
+            if (x->dtype == BOA_T_F32) zero((float *)x->dpoints, x->V * x->d, st);
+            else zero((bf16_t *)x->dpoints, x->V * x->d, st);
+            zero(x->dbias, x->V, st);
+        }
+        return launch_status("softmax_xent");
+    }
+    if (!ws || !aligned(ws, 16) || ws_bytes < make_plan(x, grad).total)
+        return bad("softmax_xent: workspace missing, unaligned or too small");
+    return x->dtype == BOA_T_F32 ? run_xent<float>(x, grad, (uint8_t *)ws, st) : run_xent<bf16_t>(x, grad, (uint8_t *)ws, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t boa_softmax_xent_workspace(const boa_xent *x, int32_t grad)
+{
+    if (int rc = check(x, grad != 0)) return rc;
+    return x->B ? make_plan(x, grad != 0).total : 0;
+}
+
+int boa_softmax_xent(const boa_xent *x, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    return xent(x, false, workspace, workspace_bytes, stream);
+}
+
+int boa_softmax_xent_grad(const boa_xent *x, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    return xent(x, true, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"
