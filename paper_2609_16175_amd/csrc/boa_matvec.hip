@@ -2,6 +2,7 @@
 //   y[m][n] = sum_k x[m][k] w[n][k],  w = s q + o  or, without offsets, s (q - 8),
 // one scale (and offset) per row and group of consecutive k.
 #include <algorithm>
+#include <type_traits>
 
 #include "boa_ops.h"
 
@@ -62,9 +63,283 @@ __global__ __launch_bounds__(256) void rows4_any_kernel(VecArgs a)
     }
 }
 
+// ---------------------------------------------------------------------------
+// Rows of whole 16-byte chunks (32 codes), groups of whole chunks.
+//
+// Bound by reading the codes: at half a byte per weight even the few steps
+// that turn a code into a number count, so the products run on the 16x16x32
+// bf16 matrix instruction and a code becomes a bf16 number in one step: its
+// four bits under the exponent of 16 are 16 + q. x is held exactly as
+// bf16 parts (1 of bfloat16, 2 of float16, 3 of float32), each a column of its
+// own, and sum (16 + q) x has 24 (or 16) times sum x taken off by starting
+// there, which leaves sum (q - 8) x (or sum q x).
+//
+// A lane holds one row's chunk: lane l has row l & 15 and chunk l >> 4 of four
+// in a step of 128 k, so a wave reads 64 bytes of 16 rows at once. Lanes of
+// different chunks may need different scales, so their sums must stay apart:
+// columns are laid out as 4 chunks x 4 slots, x being zero except in the slots
+// of the lane's own chunk. Result row 4 c + s of the matrix instruction is
+// then chunk c's sum for slot s, and it lies in the lanes that hold chunk c
+// and its scale. The zeros cost matrix time only, which is idle here.
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int FAST_WAVES = 8;               // per block
+constexpr int ROWS_W = 32;                  // rows of a wave: two tiles of 16
+constexpr size_t FAST_LDS = 64 << 10;       // x of one stretch of k, at most
+
+template <class T>
+constexpr int parts_v = sizeof(T) == 4 ? 3 : std::is_same<T, bf16_t>::value ? 1 : 2;
+
+// bytes of x in LDS per step of 128 k: 4 chunks x (4 pieces of 8 k x 4 slots x 16 bytes, and 4 sums) per column set
+constexpr int step_bytes(int nc) { return nc * (1024 + 64); }
+
+struct FastArgs {
+    VecArgs v;
+    int32_t m0, vectors;       // the vectors of this launch
+    int32_t split_k;           // waves of a block that share rows, each taking every split_k-th step
+    int32_t steps, stretch;    // steps of 128 k in a row; of them held in LDS at a time
+    uint32_t group_inv;        // 2^32 / (chunks per group), rounded up; 0: one chunk per group
+};
+
+template <class SC>
+__device__ inline float scale_at(const void *p, int64_t i) { return (float)((const SC *)p)[i]; }
+
+// value[0..VALS) of both tiles, summed over the four chunks' lanes; afterwards
+// quarter q of the wave holds values 2u + (q & 1) of tile q >> 1 in out[u].
+template <int VALS>
+__device__ inline void join_chunks(const float (&a)[2][VALS], float (&out)[(VALS + 1) / 2])
+{
+    float half[VALS + 1];
+#pragma unroll
+    for (int i = 0; i < VALS; ++i) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a[0][i]), __float_as_uint(a[1][i]), false, false);
+        half[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    half[VALS] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < (VALS + 1) / 2; ++u) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(half[2 * u]), __float_as_uint(half[2 * u + 1]), false, false);
+        out[u] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+}
+
+// NC column sets of 4 slots; a vector takes parts_v<T> slots in a row.
+template <class T, class SC, int NC, bool OFFSETS>
+__global__ __launch_bounds__(64 * FAST_WAVES) void rows4_kernel(FastArgs f)
+{
+    constexpr int PARTS = parts_v<T>, VALS = NC * 4 / PARTS;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const VecArgs &a = f.v;
+    // x: [step][piece j of 4][set][chunk][slot][8 k] bf16; sums: [step][set][chunk][slot]; then 16 zero bytes
+    bf16x8 *xs = (bf16x8 *)lds;
+    f32x4 *sums = (f32x4 *)(lds + (size_t)f.stretch * NC * 1024);
+    const int zero_at = f.stretch * NC * 68;   // in units of 16 bytes: past x and the sums
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunk = lane >> 4, r = lane & 15;
+    const int split = wave % f.split_k, per_block = FAST_WAVES / f.split_k;
+    const int64_t tiles = (a.rows + ROWS_W - 1) / ROWS_W;
+
+    auto fill = [&](int step0) {   // x of steps [step0, step0 + stretch)
+        for (int i = threadIdx.x; i < f.stretch * NC * 16; i += 64 * FAST_WAVES) {
+            const int slot = i & 3, c = (i >> 2) & 3, set = (i >> 4) % NC, step = i / (16 * NC);
+            const int col = set * 4 + slot, m = col / PARTS, part = col % PARTS;
+            const int k0 = (step0 + step) * 128 + c * 32;
+            const bool live = col < VALS * PARTS && m < f.vectors && k0 < a.K;
+            const T *x = (const T *)a.x + (int64_t)(f.m0 + m) * a.x_stride + k0;
+            float sum = 0.0f;
+            for (int j = 0; j < 4; ++j) {
+                bf16x8 to;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    // codes k and k + 4 of a word share a register
+                    const float v = live ? (float)x[j * 8 + (k >> 1) + (k & 1) * 4] : 0.0f;
+                    float rest = v, top = 0.0f;
+#pragma unroll
+                    for (int p = 0; p < PARTS; ++p) {
+                        top = PARTS == 1 ? rest : __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u);
+                        if (p == part) break;
+                        rest = fabsf(rest) < INFINITY ? rest - top : 0.0f;
+                    }
+                    to[k] = (bf16_t)top;
+                    sum += top;
+                }
+                xs[((step * 4 + j) * NC + set) * 16 + c * 4 + slot] = to;
+            }
+            ((float *)sums)[((step * NC + set) * 4 + c) * 4 + slot] = sum;
+        }
+        if (threadIdx.x == 0) ((u32x4 *)lds)[zero_at] = u32x4{0, 0, 0, 0};
+    };
+
+    const bool once = f.steps <= f.stretch;
+    const int x_at = (r >> 2) == chunk ? chunk * 4 + (r & 3) : -1;   // where this lane's x lies; else the zeros
+    if (once) {
+        fill(0);
+        __syncthreads();
+    }
+    for (int64_t t0 = (int64_t)blockIdx.x * per_block; t0 < tiles; t0 += (int64_t)gridDim.x * per_block) {
+        const int64_t tile = t0 + wave / f.split_k;
+        const int64_t row0 = tile * ROWS_W;
+        const uint8_t *codes[2];
+        int64_t sc[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int64_t row = min(row0 + t * 16 + r, a.rows - 1);
+            codes[t] = a.codes + row * a.codes_stride;
+            sc[t] = row * a.scale_stride;
+        }
+        float y[2][NC * 4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < NC * 4; ++i) y[t][i] = 0.0f;
+        for (int step0 = 0; step0 < f.steps; step0 += f.stretch) {
+            if (!once) {
+                __syncthreads();
+                fill(step0);
+                __syncthreads();
+            }
+            const int end = min(f.steps, step0 + f.stretch);
+#pragma unroll 2
+            for (int step = step0 + split; step < end; step += f.split_k) {
+                const int c = step * 4 + chunk;
+                const bool in = c * 32 < a.K;   // the last step may have fewer than four chunks
+                const int cc = in ? c : 0;
+                u32x4 w[2];
+                float s[2], o[2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    w[t] = *(const u32x4 *)(codes[t] + cc * 16);
+                    const int64_t at = sc[t] + (f.group_inv ? (int)__umulhi((uint32_t)cc, f.group_inv) : cc);
+                    s[t] = scale_at<SC>(a.scales, at);
+                    o[t] = OFFSETS ? scale_at<SC>(a.offsets, at) : 0.0f;
+                    if (!in) s[t] = o[t] = 0.0f;
+                }
+                f32x4 acc[2][NC], xsum[NC];
+#pragma unroll
+                for (int n = 0; n < NC; ++n) {
+                    xsum[n] = sums[((step - step0) * NC + n) * 4 + chunk];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[t][n][i] = (OFFSETS ? -16.0f : -24.0f) * xsum[n][i];
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    bf16x8 b[2];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const uint32_t q = w[t][j];
+                        u32x4 e;
+                        e[0] = ((q << 3) & 0x00780078u) | 0x41804180u;
+                        e[1] = ((q >> 1) & 0x00780078u) | 0x41804180u;
+                        e[2] = ((q >> 5) & 0x00780078u) | 0x41804180u;
+                        e[3] = ((q >> 9) & 0x00780078u) | 0x41804180u;
+                        b[t] = __builtin_bit_cast(bf16x8, e);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NC; ++n) {
+                        const bf16x8 x = xs[x_at >= 0 ? (((step - step0) * 4 + j) * NC + n) * 16 + x_at : zero_at];
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+                            acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, b[t], acc[t][n], 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int n = 0; n < NC; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            y[t][n * 4 + i] = fmaf(s[t], acc[t][n][i], y[t][n * 4 + i]);
+                            if (OFFSETS) y[t][n * 4 + i] = fmaf(o[t], xsum[n][i], y[t][n * 4 + i]);
+                        }
+            }
+        }
+        float v[2][VALS], out[(VALS + 1) / 2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < VALS; ++i) {
+                v[t][i] = y[t][i * PARTS];
+#pragma unroll
+                for (int p = 1; p < PARTS; ++p) v[t][i] += y[t][i * PARTS + p];
+            }
+        join_chunks<VALS>(v, out);
+        if (f.split_k > 1) {   // the waves of a tile, in order; x is no longer needed in this tile
+            __syncthreads();
+            float *red = (float *)lds;
+#pragma unroll
+            for (int u = 0; u < (VALS + 1) / 2; ++u) red[(wave * ((VALS + 1) / 2) + u) * 64 + lane] = out[u];
+            __syncthreads();
+            if (split == 0)
+                for (int k = 1; k < f.split_k; ++k)
+#pragma unroll
+                    for (int u = 0; u < (VALS + 1) / 2; ++u) out[u] += red[((wave + k) * ((VALS + 1) / 2) + u) * 64 + lane];
+        }
+        if (split == 0) {
+            const int64_t row = row0 + (chunk >> 1) * 16 + r;
+            if (row < a.rows)
+#pragma unroll
+                for (int u = 0; u < (VALS + 1) / 2; ++u) {
+                    const int m = 2 * u + (chunk & 1);
+                    if (m < VALS && m < f.vectors) ((T *)a.y)[(int64_t)(f.m0 + m) * a.y_stride + row] = (T)out[u];
+                }
+        }
+        if (f.split_k > 1 && once && t0 + (int64_t)gridDim.x * per_block < tiles) {   // the sums overwrote x
+            __syncthreads();
+            fill(0);
+            __syncthreads();
+        }
+    }
+}
+
+template <class T, class SC, int NC>
+void launch_fast(FastArgs f, hipStream_t st)
+{
+    const VecArgs &a = f.v;
+    f.steps = (int32_t)ceil_div(a.K, 128);
+    f.stretch = (int32_t)std::min<int64_t>(f.steps, (FAST_LDS - 16) / step_bytes(NC));
+    // exact for the at most 2^15 chunks of a row
+    const int32_t per_group = a.group / 32;
+    f.group_inv = per_group == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + per_group - 1) / per_group);
+    const int64_t tiles = ceil_div(a.rows, ROWS_W);
+    // waves share a tile's steps while there are too few tiles to give every
+    // CU two blocks of them
+    f.split_k = 1;
+    while (f.split_k < FAST_WAVES && f.split_k * 2 <= f.steps && tiles * f.split_k < 512 * FAST_WAVES) f.split_k *= 2;
+    const int64_t blocks = std::min<int64_t>(ceil_div(tiles, FAST_WAVES / f.split_k), f.split_k > 1 ? 4096 : 512);
+    size_t lds = (size_t)f.stretch * step_bytes(NC) + 16;
+    if (f.split_k > 1) lds = std::max(lds, (size_t)FAST_WAVES * NC * 2 * 64 * sizeof(float));
+    if (a.offsets) rows4_kernel<T, SC, NC, true><<<dim3((uint32_t)blocks), 64 * FAST_WAVES, lds, st>>>(f);
+    else rows4_kernel<T, SC, NC, false><<<dim3((uint32_t)blocks), 64 * FAST_WAVES, lds, st>>>(f);
+}
+
+template <class T, class SC>
+void launch_sets(const VecArgs &a, hipStream_t st)
+{
+    constexpr int PARTS = parts_v<T>, MOST = 16 / PARTS;
+    for (int32_t m0 = 0; m0 < a.M; m0 += MOST) {
+        FastArgs f{};
+        f.v = a, f.m0 = m0, f.vectors = std::min(MOST, a.M - m0);
+        const int cols = f.vectors * PARTS;
+        if (cols <= 4) launch_fast<T, SC, 1>(f, st);
+        else if (cols <= 8) launch_fast<T, SC, 2>(f, st);
+        else launch_fast<T, SC, 4>(f, st);
+    }
+}
+
 template <class T>
 int launch_rows4(const VecArgs &a, hipStream_t st)
 {
+    const bool chunks = a.K % 32 == 0 && a.group % 32 == 0 && aligned(a.codes, 16) && a.codes_stride % 16 == 0;
+    if (chunks) {
+        if (a.scale_dtype == BOA_T_F32) launch_sets<T, float>(a, st);
+        else if (a.scale_dtype == BOA_T_BF16) launch_sets<T, bf16_t>(a, st);
+        else launch_sets<T, f16_t>(a, st);
+        return launch_status("matvec_fourbit");
+    }
     const dim3 grid((uint32_t)ceil_div(a.rows, 4));
     if (a.M == 1)
         rows4_any_kernel<T, 1><<<grid, 256, 0, st>>>(a);
