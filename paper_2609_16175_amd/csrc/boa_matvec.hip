@@ -87,6 +87,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int FAST_WAVES = 8;               // per block
+constexpr int AHEAD = 2;                    // units of loads a wave keeps in flight
 constexpr int ROWS_W = 32;                  // rows of a wave: two tiles of 16
 constexpr size_t FAST_LDS = 64 << 10;       // x of one stretch of k, at most
 
@@ -103,9 +104,6 @@ struct FastArgs {
     int32_t steps, stretch;    // steps of 128 k in a row; of them held in LDS at a time
     uint32_t group_inv;        // 2^32 / (chunks per group), rounded up; 0: one chunk per group
 };
-
-template <class SC>
-__device__ inline float scale_at(const void *p, int64_t i) { return (float)((const SC *)p)[i]; }
 
 // value[0..VALS) of both tiles, summed over the four chunks' lanes; afterwards
 // quarter q of the wave holds values 2u + (q & 1) of tile q >> 1 in out[u].
@@ -141,123 +139,128 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void rows4_kernel(FastArgs f)
     const int split = wave % f.split_k, per_block = FAST_WAVES / f.split_k;
     const int64_t tiles = (a.rows + ROWS_W - 1) / ROWS_W;
 
-    auto fill = [&](int step0) {   // x of steps [step0, step0 + stretch)
-        for (int i = threadIdx.x; i < f.stretch * NC * 16; i += 64 * FAST_WAVES) {
-            const int slot = i & 3, c = (i >> 2) & 3, set = (i >> 4) % NC, step = i / (16 * NC);
+    // x of steps [step0, step0 + stretch): the parts, then their sums
+    auto fill = [&](int step0) {
+        for (int i = threadIdx.x; i < f.stretch * NC * 64; i += 64 * FAST_WAVES) {
+            const int slot = i & 3, c = (i >> 2) & 3, j = (i >> 4) & 3, set = (i >> 6) % NC, step = i / (64 * NC);
             const int col = set * 4 + slot, m = col / PARTS, part = col % PARTS;
-            const int k0 = (step0 + step) * 128 + c * 32;
+            const int k0 = (step0 + step) * 128 + c * 32 + j * 8;
             const bool live = col < VALS * PARTS && m < f.vectors && k0 < a.K;
             const T *x = (const T *)a.x + (int64_t)(f.m0 + m) * a.x_stride + k0;
-            float sum = 0.0f;
-            for (int j = 0; j < 4; ++j) {
-                bf16x8 to;
+            bf16x8 to;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    // codes k and k + 4 of a word share a register
-                    const float v = live ? (float)x[j * 8 + (k >> 1) + (k & 1) * 4] : 0.0f;
-                    float rest = v, top = 0.0f;
+            for (int k = 0; k < 8; ++k) {
+                // codes k and k + 4 of a word share a register
+                float rest = live ? (float)x[(k >> 1) + (k & 1) * 4] : 0.0f, top = rest;
+                if constexpr (PARTS > 1) {
 #pragma unroll
                     for (int p = 0; p < PARTS; ++p) {
-                        top = PARTS == 1 ? rest : __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u);
-                        if (p == part) break;
-                        rest = fabsf(rest) < INFINITY ? rest - top : 0.0f;
+                        const float cut = __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u);
+                        if (p == part) top = cut;
+                        rest = fabsf(rest) < INFINITY ? rest - cut : 0.0f;
                     }
-                    to[k] = (bf16_t)top;
-                    sum += top;
                 }
-                xs[((step * 4 + j) * NC + set) * 16 + c * 4 + slot] = to;
+                to[k] = (bf16_t)top;
             }
-            ((float *)sums)[((step * NC + set) * 4 + c) * 4 + slot] = sum;
+            xs[((step * 4 + j) * NC + set) * 16 + c * 4 + slot] = to;
         }
         if (threadIdx.x == 0) ((u32x4 *)lds)[zero_at] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+        for (int i = threadIdx.x; i < f.stretch * NC * 16; i += 64 * FAST_WAVES) {
+            const int at = i & 15, set = (i >> 4) % NC, step = i / (16 * NC);
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bf16x8 v = xs[((step * 4 + j) * NC + set) * 16 + at];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum += (float)v[k];
+            }
+            ((float *)sums)[(step * NC + set) * 16 + at] = sum;
+        }
+        __syncthreads();
     };
 
-    const bool once = f.steps <= f.stretch;
-    const int x_at = (r >> 2) == chunk ? chunk * 4 + (r & 3) : -1;   // where this lane's x lies; else the zeros
-    if (once) {
-        fill(0);
-        __syncthreads();
-    }
-    for (int64_t t0 = (int64_t)blockIdx.x * per_block; t0 < tiles; t0 += (int64_t)gridDim.x * per_block) {
-        const int64_t tile = t0 + wave / f.split_k;
-        const int64_t row0 = tile * ROWS_W;
+    // this lane's rows of a tile
+    struct Rows {
         const uint8_t *codes[2];
         int64_t sc[2];
+    };
+    auto rows_of = [&](Rows &to, int64_t tile) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int64_t row = min(row0 + t * 16 + r, a.rows - 1);
-            codes[t] = a.codes + row * a.codes_stride;
-            sc[t] = row * a.scale_stride;
+            const int64_t row = min(tile * ROWS_W + t * 16 + r, a.rows - 1);
+            to.codes[t] = a.codes + row * a.codes_stride;
+            to.sc[t] = row * a.scale_stride;
         }
-        float y[2][NC * 4];
+    };
+    // one step of a tile's codes and scales, for this lane's rows and chunk
+    struct Loaded {
+        u32x4 w[2];
+        SC s[2], o[2];
+    };
+    auto load = [&](Loaded &to, const Rows &rows, int step) {
+        const int c = step * 4 + chunk;
+        const int cc = c * 32 < a.K ? c : 0;   // the last step may have fewer than four chunks; x is 0 there
+        const int g = f.group_inv ? (int)__umulhi((uint32_t)cc, f.group_inv) : cc;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            to.w[t] = *(const u32x4 *)(rows.codes[t] + cc * 16);
+            to.s[t] = ((const SC *)a.scales)[rows.sc[t] + g];
+            if (OFFSETS) to.o[t] = ((const SC *)a.offsets)[rows.sc[t] + g];
+        }
+    };
+    const int x_at = (r >> 2) == chunk ? chunk * 4 + (r & 3) : -1;   // where this lane's x lies; else the zeros
+    float y[2][NC * 4];
+    auto multiply = [&](const Loaded &from, int at) {   // at: the step's place in LDS
+        f32x4 acc[2][NC], xsum[NC];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            xsum[n] = sums[(at * NC + n) * 4 + chunk];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[t][n][i] = (OFFSETS ? -16.0f : -24.0f) * xsum[n][i];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            bf16x8 b[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const uint32_t q = from.w[t][j];
+                u32x4 e;
+                e[0] = ((q << 3) & 0x00780078u) | 0x41804180u;
+                e[1] = ((q >> 1) & 0x00780078u) | 0x41804180u;
+                e[2] = ((q >> 5) & 0x00780078u) | 0x41804180u;
+                e[3] = ((q >> 9) & 0x00780078u) | 0x41804180u;
+                b[t] = __builtin_bit_cast(bf16x8, e);
+            }
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                const bf16x8 x = xs[x_at >= 0 ? ((at * 4 + j) * NC + n) * 16 + x_at : zero_at];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, b[t], acc[t][n], 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int n = 0; n < NC; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    y[t][n * 4 + i] = fmaf((float)from.s[t], acc[t][n][i], y[t][n * 4 + i]);
+                    if (OFFSETS) y[t][n * 4 + i] = fmaf((float)from.o[t], xsum[n][i], y[t][n * 4 + i]);
+                }
+    };
+    auto clear = [&] {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < NC * 4; ++i) y[t][i] = 0.0f;
-        for (int step0 = 0; step0 < f.steps; step0 += f.stretch) {
-            if (!once) {
-                __syncthreads();
-                fill(step0);
-                __syncthreads();
-            }
-            const int end = min(f.steps, step0 + f.stretch);
-#pragma unroll 2
-            for (int step = step0 + split; step < end; step += f.split_k) {
-                const int c = step * 4 + chunk;
-                const bool in = c * 32 < a.K;   // the last step may have fewer than four chunks
-                const int cc = in ? c : 0;
-                u32x4 w[2];
-                float s[2], o[2];
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    w[t] = *(const u32x4 *)(codes[t] + cc * 16);
-                    const int64_t at = sc[t] + (f.group_inv ? (int)__umulhi((uint32_t)cc, f.group_inv) : cc);
-                    s[t] = scale_at<SC>(a.scales, at);
-                    o[t] = OFFSETS ? scale_at<SC>(a.offsets, at) : 0.0f;
-                    if (!in) s[t] = o[t] = 0.0f;
-                }
-                f32x4 acc[2][NC], xsum[NC];
-#pragma unroll
-                for (int n = 0; n < NC; ++n) {
-                    xsum[n] = sums[((step - step0) * NC + n) * 4 + chunk];
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[t][n][i] = (OFFSETS ? -16.0f : -24.0f) * xsum[n][i];
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    bf16x8 b[2];
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        const uint32_t q = w[t][j];
-                        u32x4 e;
-                        e[0] = ((q << 3) & 0x00780078u) | 0x41804180u;
-                        e[1] = ((q >> 1) & 0x00780078u) | 0x41804180u;
-                        e[2] = ((q >> 5) & 0x00780078u) | 0x41804180u;
-                        e[3] = ((q >> 9) & 0x00780078u) | 0x41804180u;
-                        b[t] = __builtin_bit_cast(bf16x8, e);
-                    }
-#pragma unroll
-                    for (int n = 0; n < NC; ++n) {
-                        const bf16x8 x = xs[x_at >= 0 ? (((step - step0) * 4 + j) * NC + n) * 16 + x_at : zero_at];
-#pragma unroll
-                        for (int t = 0; t < 2; ++t)
-                            acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, b[t], acc[t][n], 0, 0, 0);
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int n = 0; n < NC; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            y[t][n * 4 + i] = fmaf(s[t], acc[t][n][i], y[t][n * 4 + i]);
-                            if (OFFSETS) y[t][n * 4 + i] = fmaf(o[t], xsum[n][i], y[t][n * 4 + i]);
-                        }
-            }
-        }
-        float v[2][VALS], out[(VALS + 1) / 2];
+    };
+    constexpr int OUT = (VALS + 1) / 2;
+    auto totals = [&](float (&out)[OUT]) {   // the parts of a value, then the chunks
+        float v[2][VALS];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -267,31 +270,98 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void rows4_kernel(FastArgs f)
                 for (int p = 1; p < PARTS; ++p) v[t][i] += y[t][i * PARTS + p];
             }
         join_chunks<VALS>(v, out);
-        if (f.split_k > 1) {   // the waves of a tile, in order; x is no longer needed in this tile
-            __syncthreads();
+    };
+    auto write = [&](const float (&out)[OUT], int64_t tile) {
+        const int64_t row = tile * ROWS_W + (chunk >> 1) * 16 + r;
+        if (row >= a.rows) return;
+#pragma unroll
+        for (int u = 0; u < OUT; ++u) {
+            const int m = 2 * u + (chunk & 1);
+            if (m < VALS && m < f.vectors) ((T *)a.y)[(int64_t)(f.m0 + m) * a.y_stride + row] = (T)out[u];
+        }
+    };
+
+    if (f.split_k == 1 && f.steps <= f.stretch) {
+        // A wave walks through its tiles' steps as one sequence with AHEAD units
+        // of loads in flight. A unit is two steps, so that the two halves of a
+        // row's 128-byte lines are asked for together.
+        const int64_t stride = (int64_t)gridDim.x * FAST_WAVES;
+        int64_t tile = (int64_t)blockIdx.x * FAST_WAVES + wave, next = tile;
+        int step = 0, next_step = 0;
+        Loaded buf[AHEAD][2];
+        Rows rows;
+        auto fetch = [&](Loaded (&to)[2]) {
+            if (next < tiles) {
+                if (next_step == 0) rows_of(rows, next);
+                load(to[0], rows, next_step);
+                if (next_step + 1 < f.steps) load(to[1], rows, next_step + 1);
+            }
+            next_step += 2;
+            if (next_step >= f.steps) {
+                next_step = 0;
+                next += stride;
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) fetch(buf[i]);
+        fill(0);
+        clear();
+        while (tile < tiles) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                if (tile < tiles) {
+                    multiply(buf[i][0], step);
+                    if (step + 1 < f.steps) multiply(buf[i][1], step + 1);
+                    fetch(buf[i]);
+                    step += 2;
+                    if (step >= f.steps) {
+                        float out[OUT];
+                        totals(out);
+                        write(out, tile);
+                        clear();
+                        step = 0;
+                        tile += stride;
+                    }
+                }
+            }
+        }
+        return;
+    }
+    // Few tiles, or rows longer than LDS holds of x: the waves of a tile take
+    // its steps in turn and add their sums in order.
+    for (int64_t t0 = (int64_t)blockIdx.x * per_block; t0 < tiles; t0 += (int64_t)gridDim.x * per_block) {
+        const int64_t tile = t0 + wave / f.split_k;
+        clear();
+        Rows rows;
+        rows_of(rows, tile);
+        for (int step0 = 0; step0 < f.steps; step0 += f.stretch) {
+            const int end = min(f.steps, step0 + f.stretch);
+            int step = step0 + split;
+            Loaded cur;
+            if (step < end) load(cur, rows, step);
+            if (t0 != (int64_t)blockIdx.x * per_block || step0) __syncthreads();
+            fill(step0);
+            for (; step < end; step += f.split_k) {
+                Loaded nxt;
+                if (step + f.split_k < end) load(nxt, rows, step + f.split_k);
+                multiply(cur, step - step0);
+                cur = nxt;
+            }
+        }
+        float out[OUT];
+        totals(out);
+        if (f.split_k > 1) {
+            __syncthreads();   // x has been read
             float *red = (float *)lds;
 #pragma unroll
-            for (int u = 0; u < (VALS + 1) / 2; ++u) red[(wave * ((VALS + 1) / 2) + u) * 64 + lane] = out[u];
+            for (int u = 0; u < OUT; ++u) red[(wave * OUT + u) * 64 + lane] = out[u];
             __syncthreads();
             if (split == 0)
                 for (int k = 1; k < f.split_k; ++k)
 #pragma unroll
-                    for (int u = 0; u < (VALS + 1) / 2; ++u) out[u] += red[((wave + k) * ((VALS + 1) / 2) + u) * 64 + lane];
+                    for (int u = 0; u < OUT; ++u) out[u] += red[((wave + k) * OUT + u) * 64 + lane];
         }
-        if (split == 0) {
-            const int64_t row = row0 + (chunk >> 1) * 16 + r;
-            if (row < a.rows)
-#pragma unroll
-                for (int u = 0; u < (VALS + 1) / 2; ++u) {
-                    const int m = 2 * u + (chunk & 1);
-                    if (m < VALS && m < f.vectors) ((T *)a.y)[(int64_t)(f.m0 + m) * a.y_stride + row] = (T)out[u];
-                }
-        }
-        if (f.split_k > 1 && once && t0 + (int64_t)gridDim.x * per_block < tiles) {   // the sums overwrote x
-            __syncthreads();
-            fill(0);
-            __syncthreads();
-        }
+        if (split == 0) write(out, tile);
     }
 }
 
