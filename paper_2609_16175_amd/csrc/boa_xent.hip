@@ -32,6 +32,9 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+__device__ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
@@ -169,27 +172,46 @@ __device__ inline void clear(f32x16 (&acc)[S::TM][S::TN])
 // ---------------------------------------------------------------------------
 // operands
 
-// Copies a block of 64 rows x 64 columns of `src` (R x C) as bf16 parts:
-// `plain` [part][rows_pad][cols_pad] and `across` [part][cols][across_ld],
-// zeros past the end. Either may be null.
+// Copies rows (R x C) as bf16 parts, zeros past the end: `plain`
+// [part][rows_pad][plain_ld], `kept` the same without the rows that are left
+// out (whatever they hold, zeros take their place), `across` [part][C][across_ld]
+// likewise without. Any of them may be null. Of queries it also gives the
+// labels: -1 where a query has none, past the last one too.
+struct PartsArgs {
+    const void *src;
+    int64_t stride, plain_ld, plain_part, across_ld, across_part;
+    int32_t R, C, rows_pad;
+    bf16_t *plain, *kept, *across;
+    const int64_t *labels;   // of queries, or null
+    int32_t V;
+    int32_t *label;          // rows_pad
+};
+
 template <class T>
-__global__ __launch_bounds__(256) void parts_kernel(const T *src, int64_t stride, int32_t R, int32_t C, bf16_t *plain,
-                                                    int64_t plain_ld, int64_t plain_part, int32_t rows_pad,
-                                                    bf16_t *across, int64_t across_ld, int64_t across_part,
-                                                    int32_t across_rows)
+__global__ __launch_bounds__(256) void parts_kernel(PartsArgs a)
 {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
     __shared__ bf16_t tile[PARTS][64][66];
+    __shared__ int32_t live[64];
     const int32_t r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
     const int c = threadIdx.x & 63;
+    if (threadIdx.x < 64) {
+        const int32_t b = r0 + c;
+        int32_t y = 0;
+        if (a.labels) {
+            y = b < a.R && a.labels[b] >= 0 && a.labels[b] < a.V ? (int32_t)a.labels[b] : -1;
+            if (blockIdx.y == 0 && b < a.rows_pad) a.label[b] = y;
+        }
+        live[c] = y >= 0;
+    }
     for (int r = threadIdx.x >> 6; r < 64; r += 4) {
         float v = 0.0f;
-        if (r0 + r < R && c0 + c < C) v = (float)src[(int64_t)(r0 + r) * stride + c0 + c];
-        if constexpr (PARTS == 1) {
-            tile[0][r][c] = (bf16_t)v;
-        } else {
+        if (r0 + r < a.R && c0 + c < a.C) v = (float)((const T *)a.src)[(int64_t)(r0 + r) * a.stride + c0 + c];
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
+        for (int p = 0; p < PARTS; ++p) {
+            if constexpr (PARTS == 1) {
+                tile[0][r][c] = (bf16_t)v;
+            } else {
                 const float part = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
                 tile[p][r][c] = (bf16_t)part;
                 v = fabsf(part) < INFINITY ? v - part : 0.0f;   // an infinity or NaN is its first part alone
@@ -197,16 +219,19 @@ __global__ __launch_bounds__(256) void parts_kernel(const T *src, int64_t stride
         }
     }
     __syncthreads();
+    const bf16_t nil = (bf16_t)0.0f;
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
-        if (plain)
-            for (int r = threadIdx.x >> 6; r < 64; r += 4)
-                if (r0 + r < rows_pad && c0 + c < plain_ld)
-                    plain[p * plain_part + (int64_t)(r0 + r) * plain_ld + c0 + c] = tile[p][r][c];
-        if (across)
+        for (int r = threadIdx.x >> 6; r < 64; r += 4)
+            if (r0 + r < a.rows_pad && c0 + c < a.plain_ld) {
+                const int64_t at = p * a.plain_part + (int64_t)(r0 + r) * a.plain_ld + c0 + c;
+                if (a.plain) a.plain[at] = tile[p][r][c];
+                if (a.kept) a.kept[at] = live[r] ? tile[p][r][c] : nil;
+            }
+        if (a.across)
             for (int k = threadIdx.x >> 6; k < 64; k += 4)
-                if (c0 + k < across_rows && r0 + c < across_ld)
-                    across[p * across_part + (int64_t)(c0 + k) * across_ld + r0 + c] = tile[p][c][k];
+                if (c0 + k < a.C && r0 + c < a.across_ld)
+                    a.across[p * a.across_part + (int64_t)(c0 + k) * a.across_ld + r0 + c] = live[c] ? tile[p][c][k] : nil;
     }
 }
 
@@ -228,8 +253,10 @@ struct StatsArgs {
     Product pr;              // a: points, b: queries
     const float *bias;
     RowState *part;          // splits x B
+    const int32_t *label;    // of the queries, padded
+    float *pick;             // B: the label's logit, base 2
     float scale2;            // scale * log2(e)
-    int32_t B, V, tiles_v, tiles_b, splits;
+    int32_t B, V, v0, tiles_v, tiles_b, splits;   // v0: the first point among all
 };
 
 __device__ inline void join(RowState &a, float m, float s)
@@ -251,8 +278,12 @@ __global__ __launch_bounds__(S::THREADS) void stats_kernel(StatsArgs a)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     const int wm = wave % S::WM, wn = wave / S::WM;
     RowState st[S::TN];
+    int32_t lab[S::TN];
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j) st[j] = RowState{NO_MAX, 0.0f};
+    for (int j = 0; j < S::TN; ++j) {
+        st[j] = RowState{NO_MAX, 0.0f};
+        lab[j] = a.label[tb * S::BN + (wn * S::TN + j) * 32 + (lane & 31)] - a.v0;
+    }
     for (int32_t tv = split; tv < a.tiles_v; tv += a.splits) {
         f32x16 acc[S::TM][S::TN];
         clear<S>(acc);
@@ -274,6 +305,11 @@ __global__ __launch_bounds__(S::THREADS) void stats_kernel(StatsArgs a)
                     acc[i][j][e] = fmaf(acc[i][j][e], a.scale2, off[e]);
                     top = fmaxf(top, acc[i][j][e]);
                 }
+                const int32_t rel = lab[j] - v0;
+                if (__any((uint32_t)rel < 32u))   // a query's own point is among these
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (rel == tile_row(e, half)) a.pick[tb * S::BN + (wn * S::TN + j) * 32 + (lane & 31)] = acc[i][j][e];
                 float s = st[j].s * __builtin_amdgcn_exp2f(st[j].m - top);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(acc[i][j][e] - top);
@@ -299,23 +335,19 @@ __global__ __launch_bounds__(S::THREADS) void stats_kernel(StatsArgs a)
 }
 
 struct RowArgs {
-    const void *h, *points;
-    int64_t h_stride, points_stride;
     const int64_t *labels;
-    const float *bias, *dloss;
+    const float *dloss, *pick;
     const RowState *part;
     float *loss;             // per query (the caller's, or scratch where the loss is reduced)
     float *lse;              // the caller's, or null
-    float *top;              // rows_pad: the largest logit, base 2
+    float *top;              // rows_pad: what the sum is relative to, base 2
     float *rowf;             // rows_pad: g / sum of 2^(l - top), 0 for a query without gradient
     float *coef;             // B: g * (p_label - 1)
     int32_t *label;          // rows_pad: the label, or -1 where it has no entry
-    float scale;
-    int32_t B, V, d, splits, reduction, rows_pad;
+    int32_t B, V, shares, reduction, rows_pad;
 };
 
-// A wave per query: joins the splits, forms the label's logit in float32.
-template <class T>
+// A wave per query: joins the shares of its statistics.
 __global__ __launch_bounds__(256) void row_kernel(RowArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -323,14 +355,13 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a)
     if (b >= a.rows_pad) return;
     if (b >= a.B) {
         if (lane == 0) {
-            a.top[b] = 0.0f;
+            a.top[b] = INFINITY;   // probabilities of 0 whatever the bias
             a.rowf[b] = 0.0f;
-            a.label[b] = -1;
         }
         return;
     }
     RowState st{NO_MAX, 0.0f};
-    for (int i = lane; i < a.splits; i += 64) {
+    for (int i = lane; i < a.shares; i += 64) {
         const RowState o = a.part[(int64_t)i * a.B + b];
         join(st, o.m, o.s);
     }
@@ -339,27 +370,21 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a)
         const float m = __shfl_xor(st.m, o), s = __shfl_xor(st.s, o);
         join(st, m, s);
     }
+    if (lane) return;
     const int64_t y = a.labels[b];
     const bool in = y >= 0 && y < a.V;
-    float dot = 0.0f;
-    if (in) {
-        const T *h = (const T *)a.h + (int64_t)b * a.h_stride, *c = (const T *)a.points + y * a.points_stride;
-        for (int k = lane; k < a.d; k += 64) dot = fmaf((float)h[k], (float)c[k], dot);
-        dot = wave_sum(dot);
-    }
-    if (lane) return;
     const bool none = st.s == 0.0f;   // every point left out
     const float log_s = __builtin_amdgcn_logf(st.s);
-    const float l2 = in ? fmaf(dot, a.scale * LOG2E, a.bias ? base2(a.bias[y]) : 0.0f) : 0.0f;
+    const float l2 = in ? a.pick[b] : 0.0f;
     float loss = 0.0f;
     if (y >= a.V) loss = NAN;
     else if (in) loss = none ? INFINITY : ((st.m - l2) + log_s) * LN2;
     a.loss[b] = loss;
     if (a.lse) a.lse[b] = none ? -INFINITY : (st.m + log_s) * LN2;
     const float g = !in || none ? 0.0f : a.reduction == BOA_REDUCE_NONE && a.dloss ? a.dloss[b] : 1.0f;
-    a.top[b] = none ? 0.0f : st.m;
+    a.top[b] = none || !in ? INFINITY : st.m;
     a.rowf[b] = g == 0.0f ? 0.0f : g / st.s;
-    a.label[b] = in && !none ? (int32_t)y : -1;
+    if (none || !in) a.label[b] = -1;
     if (a.coef) a.coef[b] = in && !none ? g * (__builtin_amdgcn_exp2f(l2 - st.m) / st.s - 1.0f) : 0.0f;
 }
 
@@ -699,6 +724,523 @@ __global__ __launch_bounds__(256) void dh_join_kernel(const float *part, int32_t
 }
 
 // ---------------------------------------------------------------------------
+// Rows of at most 128 values: one kernel for each pass, which forms a tile of
+// logits, turns it into probabilities in registers and multiplies them on at
+// once, so that they never leave the wave.
+//
+// A wave keeps TN tiles of 32 rows of one side (N) in registers and streams
+// the other side (M) through LDS, 32 rows at a time. The logits are formed as
+// M x N tiles: a lane then has 16 M values of one N row, its softmax
+// statistics are its own, and the probabilities, rounded, are in place as the
+// operand of the second product
+//   out^T (values x N) += stream^T (values x M) * p (M x N),
+// whose other operand is the same LDS tile read transposed. A lane's 16 values
+// are rows 8 (i / 4) + 4 half + i % 4 of the tile; the second product takes
+// its 32 k in that order on both sides, which is what two transposed reads of
+// four rows give.
+//   SWEEP_LOSS: N = queries, M = points: running maximum and sum
+//   SWEEP_H:    the same and sum_v p c_v, relative to the running maximum
+//   SWEEP_C:    N = points, M = queries: sum_b p h_b and sum_b p, p from the
+//               first pass's statistics
+// The maximum a column is taken relative to moves only when a logit exceeds it
+// by 2^8: the sums have room for that, and the output is scaled rarely.
+enum { SWEEP_LOSS = 0, SWEEP_H = 1, SWEEP_C = 2 };
+constexpr float SLACK = 8.0f;
+constexpr int SWEEP_THREADS = 256;
+
+template <int DT_, int PARTS_, int MODE_, int TN_, int WN_>
+struct Sweep {
+    static constexpr int DT = DT_, PARTS = PARTS_, MODE = MODE_, TN = TN_, WN = WN_;
+    static constexpr int WS = 4 / WN;                        // waves that share N rows and take M rows in turn
+    static constexpr int NB = WN * TN * 32;                  // N rows of a block
+    static constexpr int SR = WS > 1 ? 32 * WS : PARTS == 1 ? 64 : 32;   // M rows of a stage
+    static constexpr int SUBS = SR / 32 / WS;                // tiles of a stage per wave
+    static constexpr int CH = DT == 1 ? 4 : DT == 2 ? 8 : 16;            // 16-byte chunks of an LDS row
+    static constexpr int ROWB = CH * 16, PLANE = SR * ROWB;
+    static constexpr int SIDES = MODE == SWEEP_C ? 3 : 1;    // float arrays along M: bias, or top, factor and label
+    static constexpr int STAGE = PARTS * PLANE + SIDES * SR * 4;
+    static constexpr bool STAGED = PARTS == 3 && MODE != SWEEP_C;        // float32 points: split on the way to LDS
+    static constexpr int OUT_LD = DT * 32 + 4;               // floats of a row of the output in LDS
+    static constexpr size_t lds()
+    {
+        return std::max<size_t>(2 * STAGE, MODE == SWEEP_C ? 4 * 32 * OUT_LD * 4 : 0);
+    }
+};
+
+struct SweepArgs {
+    const bf16_t *n, *m;      // bf16 rows of each side (parts n_part, m_part values apart)
+    const float *nf, *mf;     // float32 points in their place
+    int64_t n_ld, m_ld, n_part, m_part;
+    int32_t N, M;             // rows of each side
+    int32_t d, Kp;            // values of a row, and of it present in the bf16 rows (a multiple of 16)
+    int32_t vec;              // float32 rows may be read 16 bytes at a time
+    int32_t tiles_n, stages, splits, per_split;
+    float scale2;
+    const float *bias;        // padded: base 2, -inf past the last point
+    const float *top, *rowf;  // padded (SWEEP_C)
+    const int32_t *label;     // of the queries, padded
+    float *pick;              // the label's logit, base 2
+    RowState *part;           // (splits * WS) x N
+    float *out;               // (splits * WS) x N x DT * 32 partial outputs
+    float *col;               // splits x N partial sums of p, or null
+    // SWEEP_C in one split: the results themselves
+    void *dc;
+    float *dbias;
+    const int32_t *first;
+    const float *own, *own_bias, *factor;
+    float scale;
+};
+
+template <class S>
+__global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
+{
+    constexpr int DT = S::DT, PARTS = S::PARTS, TN = S::TN, KS = 2 * DT;
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    int32_t split, tn0;
+    if (S::MODE == SWEEP_C ? !split_block(a.tiles_n, a.splits, &tn0, &split)
+                           : !split_block(a.splits, a.tiles_n, &split, &tn0))
+        return;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, half = lane >> 5, r = lane & 31;
+    const int wn = wave % S::WN, ws = wave / S::WN;
+    const int32_t n0 = tn0 * S::NB + wn * TN * 32;
+    const int32_t s_begin = split * a.per_split, s_end = min(a.stages, s_begin + a.per_split);
+
+    // the kept side
+    bf16x8 fn[PARTS][KS][TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int64_t row = min(n0 + j * 32 + r, a.N - 1);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const int at = k * 16 + half * 8;
+            if constexpr (PARTS == 3 && S::MODE == SWEEP_C) {
+                float v[8];
+                const float *from = a.nf + row * a.n_ld + at;
+                if (a.vec && at + 8 <= a.d) {
+                    load_f32<4, float>(*(float(*)[4])v, from);
+                    load_f32<4, float>(*(float(*)[4])(v + 4), from + 4);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = at + e < a.d ? from[e] : 0.0f;
+                }
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float top = __uint_as_float(__float_as_uint(v[e]) & 0xFFFF0000u);
+                        fn[p][k][j][e] = (bf16_t)top;
+                        v[e] = fabsf(top) < INFINITY ? v[e] - top : 0.0f;
+                    }
+            } else {
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    if (at < a.Kp) {
+                        fn[p][k][j] = *(const bf16x8 *)(a.n + p * a.n_part + row * a.n_ld + at);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) fn[p][k][j][e] = (bf16_t)0.0f;
+                    }
+                }
+            }
+        }
+    }
+
+    // streamed rows: thread t's slots are rows t / CH + i * (256 / CH), stored chunk t % CH
+    constexpr int PER = SWEEP_THREADS / S::CH, ITS = (S::SR + PER - 1) / PER;
+    const int slot_row = t / S::CH, slot_chunk = (t % S::CH) ^ (slot_row & (S::CH - 1));
+    // a chunk past the values present meets zeros on the other side: any finite value of the row will do
+    const int slot_at = slot_chunk * 8 < a.Kp ? slot_chunk * 8 : 0;
+    auto dma = [&](int buf, int32_t stage) {
+        uint8_t *to = smem + buf * S::STAGE;
+        if constexpr (!S::STAGED) {
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                for (int i = 0; i < ITS; ++i) {
+                    if (S::SR % PER && wave * 64 >= S::SR * S::CH) continue;
+                    const int64_t row = min(stage * S::SR + i * PER + slot_row, a.M - 1);
+                    __builtin_amdgcn_global_load_lds(
+                        (const __attribute__((address_space(1))) void *)(a.m + p * a.m_part + row * a.m_ld + slot_at),
+                        (__attribute__((address_space(3))) void *)(to + p * S::PLANE + (i * SWEEP_THREADS + wave * 64) * 16),
+                        16, 0, 0);
+                }
+        }
+#pragma unroll
+        for (int k = 0; k < S::SIDES; ++k) {
+            const void *side = S::MODE != SWEEP_C ? (const void *)a.bias
+                             : k == 0 ? (const void *)a.top : k == 1 ? (const void *)a.rowf : (const void *)a.label;
+            if (wave * 64 < S::SR && t < S::SR)
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void *)((const float *)side + stage * S::SR + t),
+                    (__attribute__((address_space(3))) void *)(to + PARTS * S::PLANE + k * S::SR * 4 + wave * 256), 4, 0, 0);
+        }
+    };
+    // float32 points: 8 threads a row, DT * 4 values each, split into parts on the way
+    float held[S::STAGED ? DT : 1][4];
+    auto fetch = [&](int32_t stage) {
+        if constexpr (S::STAGED) {
+            const float *from = a.mf + (int64_t)min(stage * S::SR + (t >> 3), a.M - 1) * a.m_ld;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+                const int at = ((t & 7) + 8 * i) * 4;
+                if (a.vec && at < a.d) {
+                    load_f32<4, float>(held[i], from + at);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) held[i][e] = at + e < a.d ? from[at + e] : 0.0f;
+                }
+            }
+        }
+    };
+    auto put = [&](int buf) {
+        if constexpr (S::STAGED) {
+            const int row = t >> 3;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+                const int q = (t & 7) + 8 * i;
+                uint8_t *to = smem + buf * S::STAGE + row * S::ROWB + (((q >> 1) ^ (row & (S::CH - 1))) * 16) + (q & 1) * 8;
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    bf16x4 four;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float top = __uint_as_float(__float_as_uint(held[i][e]) & 0xFFFF0000u);
+                        four[e] = (bf16_t)top;
+                        held[i][e] = fabsf(top) < INFINITY ? held[i][e] - top : 0.0f;
+                    }
+                    *(bf16x4 *)(to + p * S::PLANE) = four;
+                }
+            }
+        }
+    };
+
+    f32x16 out[S::MODE == SWEEP_LOSS ? 1 : DT][TN];
+    float mx[TN], sum[TN], off[TN];
+    int32_t lab[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+#pragma unroll
+        for (int i = 0; i < (S::MODE == SWEEP_LOSS ? 1 : DT); ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) out[i][j][e] = 0.0f;
+        mx[j] = NO_MAX;
+        sum[j] = 0.0f;
+        const int32_t n = n0 + j * 32 + r;
+        off[j] = S::MODE == SWEEP_C ? a.bias[min(n, a.N - 1)] : 0.0f;
+        lab[j] = S::MODE != SWEEP_C && n < a.N ? a.label[n] : -1;
+    }
+
+    // lane's place in transposed reads: group g of 16 lanes takes values 16 (g & 1).. of rows 4 half..
+    const int tr_row = ((lane & 15) >> 2) + 4 * half, tr_chunk = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
+    const int tr_at = (lane & 1) * 8;
+
+    if (s_begin < s_end) {
+        dma(0, s_begin);
+        fetch(s_begin);
+        put(0);
+    }
+    __syncthreads();
+    for (int32_t stage = s_begin; stage < s_end; ++stage) {
+        const int buf = (stage - s_begin) & 1;
+        if (stage + 1 < s_end) {
+            dma(buf ^ 1, stage + 1);
+            fetch(stage + 1);
+        }
+        const uint8_t *from = smem + buf * S::STAGE;
+        const float *side = (const float *)(from + PARTS * S::PLANE);
+#pragma unroll 1
+        for (int sub = 0; sub < S::SUBS; ++sub) {   // not unrolled: the registers are full
+            const int row0 = (sub * S::WS + ws) * 32;   // of the stage
+            f32x16 acc[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[j][e] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const uint8_t *at = from + (row0 + r) * S::ROWB + (((2 * k + half) ^ (r & (S::CH - 1))) * 16);
+                bf16x8 fm[PARTS];
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) fm[p] = *(const bf16x8 *)(at + p * S::PLANE);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    if constexpr (PARTS == 3) {
+                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[2], fn[0][k][j], acc[j], 0, 0, 0);
+                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[1], fn[1][k][j], acc[j], 0, 0, 0);
+                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fn[2][k][j], acc[j], 0, 0, 0);
+                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[1], fn[0][k][j], acc[j], 0, 0, 0);
+                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fn[1][k][j], acc[j], 0, 0, 0);
+                    }
+                    acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fn[0][k][j], acc[j], 0, 0, 0);
+                }
+            }
+            // logits to probabilities
+            if constexpr (S::MODE != SWEEP_C) {
+                float bias[16];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) load_f32<4, float>(*(float(*)[4])(bias + 4 * q), side + row0 + 8 * q + 4 * half);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    float top = NO_MAX;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        acc[j][e] = fmaf(acc[j][e], a.scale2, bias[e]);
+                        top = fmaxf(top, acc[j][e]);
+                    }
+                    if (__any(top > mx[j] + SLACK)) {
+                        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+                        top = fmaxf(fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])), mx[j]);
+                        const float by = __builtin_amdgcn_exp2f(mx[j] - top);
+                        sum[j] *= by;
+                        if constexpr (S::MODE == SWEEP_H)
+#pragma unroll
+                            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) out[i][j][e] *= by;
+                        mx[j] = top;
+                    }
+                    const int32_t rel = lab[j] - (stage * S::SR + row0);
+                    const bool mine = (uint32_t)rel < 32u;
+                    if (__any(mine)) {   // a column's own point is among these rows
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const bool here = rel == tile_row(e, half);
+                            if (here) a.pick[n0 + j * 32 + r] = acc[j][e];
+                            acc[j][e] = __builtin_amdgcn_exp2f(acc[j][e] - mx[j]);
+                            sum[j] += acc[j][e];
+                            if (here) acc[j][e] = 0.0f;
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            acc[j][e] = __builtin_amdgcn_exp2f(acc[j][e] - mx[j]);
+                            sum[j] += acc[j][e];
+                        }
+                    }
+                }
+            } else {
+                const int32_t own = ((const int32_t *)side)[2 * S::SR + row0 + r];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float top[4], f[4];
+                    load_f32<4, float>(top, side + row0 + 8 * q + 4 * half);
+                    load_f32<4, float>(f, side + S::SR + row0 + 8 * q + 4 * half);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            acc[j][4 * q + e] = f[e] * __builtin_amdgcn_exp2f(fmaf(acc[j][4 * q + e], a.scale2, off[j]) - top[e]);
+                }
+                if (__any((uint32_t)(own - n0) < (uint32_t)(32 * TN))) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int32_t y = __shfl(own, tile_row(e, half));
+#pragma unroll
+                        for (int j = 0; j < TN; ++j)
+                            if (y == n0 + j * 32 + r) acc[j][e] = 0.0f;
+                    }
+                }
+                if (a.col || a.dbias)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) sum[j] += acc[j][e];
+            }
+            // the second product
+            if constexpr (S::MODE != SWEEP_LOSS) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    bf16x8 fp[PARTS][TN];
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+#pragma unroll
+                            for (int p = 0; p < PARTS; ++p) fp[p][j][e] = part_of<PARTS>(acc[j][8 * kb + e], p);
+#pragma unroll
+                    for (int i = 0; i < DT; ++i) {
+                        bf16x8 fm[PARTS];
+#pragma unroll
+                        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                            for (int jj = 0; jj < 2; ++jj) {
+                                const int row = row0 + 16 * kb + 8 * jj + tr_row;
+                                const uint8_t *at = from + p * S::PLANE + row * S::ROWB
+                                                    + (((i * 4 + tr_chunk) ^ (row & (S::CH - 1))) * 16) + tr_at;
+                                const short4v four = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                    (__attribute__((address_space(3))) short4v *)at);
+                                const bf16x4 v = __builtin_bit_cast(bf16x4, four);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) fm[p][4 * jj + e] = v[e];
+                            }
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) {
+                            if constexpr (PARTS == 3) {
+                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[2], fp[0][j], out[i][j], 0, 0, 0);
+                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[1], fp[1][j], out[i][j], 0, 0, 0);
+                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fp[2][j], out[i][j], 0, 0, 0);
+                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[1], fp[0][j], out[i][j], 0, 0, 0);
+                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fp[1][j], out[i][j], 0, 0, 0);
+                            }
+                            out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fp[0][j], out[i][j], 0, 0, 0);
+                        }
+                    }
+                }
+            }
+        }
+        if (stage + 1 < s_end) put(buf ^ 1);
+        __syncthreads();
+    }
+
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sum[j] += __shfl_xor(sum[j], 32);
+    const int64_t share = (int64_t)split * S::WS + ws;
+    if constexpr (S::MODE != SWEEP_C) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int32_t n = n0 + j * 32 + r;
+            if (n >= a.N) continue;
+            // the halves move their maximum together, except where one never saw a logit above the start
+            const float other = __shfl_xor(mx[j], 32);
+            if (half == 0) a.part[share * a.N + n] = RowState{fmaxf(mx[j], other), sum[j]};
+            if constexpr (S::MODE == SWEEP_H)
+#pragma unroll
+                for (int i = 0; i < DT; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float four[4] = {out[i][j][4 * q], out[i][j][4 * q + 1], out[i][j][4 * q + 2], out[i][j][4 * q + 3]};
+                        store_f32<4, float>(a.out + (share * a.N + n) * (DT * 32) + i * 32 + 8 * q + 4 * half, four);
+                    }
+        }
+    } else {
+        float *mine = (float *)smem + wave * 32 * S::OUT_LD;
+        const bool whole = a.splits == 1;
+        const float factor = whole ? *a.factor : 1.0f;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int32_t base = n0 + j * 32;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float four[4] = {out[i][j][4 * q], out[i][j][4 * q + 1], out[i][j][4 * q + 2], out[i][j][4 * q + 3]};
+                    store_f32<4, float>(mine + r * S::OUT_LD + i * 32 + 8 * q + 4 * half, four);
+                }
+            __syncthreads();
+            if (half == 0 && base + r < a.N) {
+                if (!whole && a.col) a.col[(int64_t)split * a.N + base + r] = sum[j];
+                if (whole && a.dbias) {
+                    const int32_t f = a.first[base + r];
+                    a.dbias[base + r] = factor * (f >= 0 ? sum[j] + a.own_bias[f] : sum[j]);
+                }
+            }
+            constexpr int CHUNKS = DT * 4, ROWS = 64 / CHUNKS > 0 ? 64 / CHUNKS : 1;   // chunks of 8 values, rows at once
+            for (int row = lane / CHUNKS; row < 32; row += ROWS) {
+                const int32_t n = base + row;
+                const int at = (lane % CHUNKS) * 8;
+                if (n >= a.N || lane >= ROWS * CHUNKS || at >= a.d) continue;
+                float v[8];
+                load_f32<4, float>(*(float(*)[4])v, mine + row * S::OUT_LD + at);
+                load_f32<4, float>(*(float(*)[4])(v + 4), mine + row * S::OUT_LD + at + 4);
+                if (!whole) {
+                    float *to = a.out + ((int64_t)split * a.N + n) * (DT * 32) + at;
+                    store_f32<4, float>(to, *(float(*)[4])v);
+                    store_f32<4, float>(to + 4, *(float(*)[4])(v + 4));
+                    continue;
+                }
+                const int32_t f = a.first[n];
+                const float by = a.scale * factor;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (f >= 0 && at + e < a.d) v[e] += a.own[(int64_t)f * a.d + at + e];
+                    v[e] *= by;
+                }
+                using T = typename std::conditional<PARTS == 3, float, bf16_t>::type;
+                T *to = (T *)a.dc + (int64_t)n * a.d + at;
+                if (a.d % 8 == 0 && aligned16(a.dc)) {
+                    constexpr int V = 16 / sizeof(T);
+#pragma unroll
+                    for (int e = 0; e < 8; e += V) store_f32<V, T>(to + e, *(float(*)[V])(v + e));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (at + e < a.d) to[e] = (T)v[e];
+                }
+            }
+        }
+    }
+}
+
+// The splits of SWEEP_C added in order, and what a single split writes itself.
+template <class T>
+__global__ __launch_bounds__(256) void dc_join_kernel(const float *out, const float *col, int32_t splits, int32_t N, int32_t d,
+                                                      int32_t ld, const int32_t *first, const float *own,
+                                                      const float *own_bias, const float *factor, float scale, T *dc,
+                                                      float *dbias)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (dc && i < (int64_t)N * d) {
+        const int64_t n = i / d;
+        const int c = (int)(i % d);
+        float s = 0.0f;
+        for (int k = 0; k < splits; ++k) s += out[((int64_t)k * N + n) * ld + c];
+        const int32_t f = first[n];
+        if (f >= 0) s += own[(int64_t)f * d + c];
+        dc[i] = (T)(scale * *factor * s);
+    }
+    if (dbias && i < N) {
+        float s = 0.0f;
+        for (int k = 0; k < splits; ++k) s += col[(int64_t)k * N + i];
+        const int32_t f = first[i];
+        if (f >= 0) s += own_bias[f];
+        dbias[i] = *factor * s;
+    }
+}
+
+// The shares of SWEEP_H, brought to the common maximum:
+// dh = scale factor (g / sum  sum_shares 2^(m - top) out + coef c_label)
+template <class T>
+__global__ __launch_bounds__(256) void dh_shares_kernel(const float *out, const RowState *part, int32_t shares, int32_t B,
+                                                        int32_t d, int32_t ld, const float *top, const float *rowf,
+                                                        const T *points, int64_t points_stride, const int32_t *label,
+                                                        const float *coef, const float *factor, float scale, T *dh)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)B * d) return;
+    const int32_t b = (int32_t)(i / d), c = (int32_t)(i % d);
+    const float f = rowf[b], m = top[b];
+    float s = 0.0f;
+    if (f != 0.0f) {
+        for (int32_t k = 0; k < shares; ++k) {
+            const int64_t at = (int64_t)k * B + b;
+            s = fmaf(__builtin_amdgcn_exp2f(part[at].m - m), out[at * ld + c], s);
+        }
+        s *= f;
+    }
+    const int32_t y = label[b];
+    if (y >= 0) s = fmaf(coef[b], (float)points[(int64_t)y * points_stride + c], s);
+    dh[i] = (T)(scale * *factor * s);
+}
+
+// Biases in base 2 as SWEEP_LOSS and SWEEP_H read them, and the points' first
+// queries cleared.
+__global__ __launch_bounds__(256) void points_kernel(const float *bias, int32_t V, int32_t padded, float *to, int32_t *first)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < padded; i += (int64_t)gridDim.x * 256) {
+        to[i] = i >= V ? -INFINITY : bias ? base2(bias[i]) : 0.0f;
+        if (first && i < V) first[i] = -1;
+    }
+}
+
+// Labels as the sweeps read them: -1 where a query has none, past the last one too.
+__global__ __launch_bounds__(256) void labels_kernel(const int64_t *labels, int32_t B, int32_t V, int32_t padded, int32_t *to)
+{
+    const int32_t b = blockIdx.x * 256 + threadIdx.x;
+    if (b < padded) to[b] = b < B && labels[b] >= 0 && labels[b] < V ? (int32_t)labels[b] : -1;
+}
+
+// ---------------------------------------------------------------------------
 // host side
 
 int64_t round_up(int64_t a, int64_t to) { return ceil_div(a, to) * to; }
@@ -707,13 +1249,18 @@ int64_t round_up(int64_t a, int64_t to) { return ceil_div(a, to) * to; }
 struct Plan {
     int32_t parts, Kp, tile_b, rows_pad, tiles_b;
     bool direct;               // the points are read where they are
-    int32_t splits;            // of the statistics
+    bool sweep;                // rows of at most 128 values: sweep_kernel
+    int32_t ld;                // sweep: values of a padded row
+    int32_t splits, shares, per_split;               // of the statistics
+    int32_t c_splits, c_per_split, c_tiles;          // sweep: of the points' gradient
     int64_t Vc, cols_pad;      // points per piece, and its padded size
     int32_t dh_splits, dh_k;
-    int64_t off_h, off_ht, off_c, off_ct, off_part, off_loss, off_top, off_rowf, off_coef, off_label, off_factor;
-    int64_t off_p, off_pt, off_col, off_dh, off_first, off_own, off_ownb, total;
+    int64_t off_h, off_ht, off_c, off_ct, off_part, off_loss, off_top, off_rowf, off_coef, off_label, off_pick, off_factor;
+    int64_t off_p, off_pt, off_col, off_dh, off_first, off_own, off_ownb, off_bias, off_hz, off_dc, total;
 };
 
+// Whether the tiles can be read where the points are: bfloat16 rows of whole
+// 16-byte chunks, an even number of them.
 bool points_direct(const boa_xent *x)
 {
     return x->dtype == BOA_T_BF16 && x->d % 16 == 0 && aligned(x->points, 16) && x->points_stride % 8 == 0;
@@ -724,38 +1271,66 @@ Plan make_plan(const boa_xent *x, bool grad)
     Plan p{};
     p.parts = x->dtype == BOA_T_F32 ? 3 : 1;
     p.direct = points_direct(x);
-    p.Kp = (int32_t)round_up(x->d, 16);
-    p.tile_b = x->B <= 32 ? 32 : x->B <= 128 ? 128 : 256;
-    p.tiles_b = (int32_t)ceil_div(x->B, p.tile_b);
-    p.rows_pad = p.tiles_b * p.tile_b;
-    const int64_t tiles_v = ceil_div(x->V, 256);
-    // the losses' splits: a block per CU (its stages fill LDS), and no more than there are tiles
-    p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles_v, 256 / p.tiles_b));
-    // a piece's probabilities: 128 MB in each order, half of the last-level cache
-    const int64_t per = (int64_t)p.rows_pad * 2 * p.parts;
-    int64_t vc = std::max<int64_t>(1024, ((int64_t)128 << 20) / per / 1024 * 1024);
-    if (!p.direct)   // and its copied points
-        vc = std::min(vc, std::max<int64_t>(1024, ((int64_t)128 << 20) / ((int64_t)p.Kp * 2 * p.parts) / 1024 * 1024));
-    p.Vc = std::min(vc, round_up(x->V, 256));
-    p.cols_pad = round_up(p.Vc, 256);
+    p.sweep = x->d <= 128;
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t o = at;
         at += round_up(std::max<int64_t>(bytes, 16), 256);
         return o;
     };
-    p.off_h = take((int64_t)p.parts * p.rows_pad * p.Kp * 2);
-    if (!p.direct) p.off_c = take((int64_t)p.parts * p.cols_pad * p.Kp * 2);
-    // a piece's tiles are split like all of them where there are several pieces
-    p.off_part = take((int64_t)p.splits * ceil_div(x->V, p.Vc) * x->B * sizeof(RowState));
-    p.off_loss = take(x->B * 4);
-    p.off_top = take(p.rows_pad * 4);
-    p.off_rowf = take(p.rows_pad * 4);
-    p.off_label = take(p.rows_pad * 4);
-    p.off_factor = take(16);
-    if (grad) {
-        p.off_coef = take(x->B * 4);
-        if (x->dh) {
+    const bool dh = grad && x->dh, dc = grad && x->dpoints, db = grad && x->dbias;
+    if (p.sweep) {
+        p.ld = (int32_t)round_up(x->d, 32);
+        // up to 32 queries the waves of a block share them and part the points
+        p.tile_b = p.parts == 1 ? (x->B <= 32 ? 32 : x->B <= 128 ? 128 : 256) : 128;
+        const int32_t ws = p.tile_b == 32 ? 4 : 1, rows = p.tile_b == 32 ? 128 : p.parts == 1 ? 64 : 32;
+        p.tiles_b = (int32_t)ceil_div(x->B, p.tile_b);
+        p.rows_pad = (int32_t)round_up(x->B, 256);
+        const int64_t stages = ceil_div(x->V, rows);
+        // two blocks per CU; whole multiples of the 8 XCDs, so that none gets a block more
+        int64_t splits = std::max<int64_t>(1, 512 / p.tiles_b);
+        if (splits > 8) splits = splits / 8 * 8;
+        splits = std::min(splits, stages);
+        p.per_split = (int32_t)ceil_div(stages, splits);
+        p.splits = (int32_t)ceil_div(stages, p.per_split);
+        p.shares = p.splits * ws;
+        p.off_bias = take(round_up(x->V, 128) * 4);
+        p.off_h = take((int64_t)p.parts * p.rows_pad * p.ld * 2);
+        if (x->dtype == BOA_T_BF16 && !p.direct) p.off_c = take(x->V * (int64_t)p.ld * 2);
+        if (dh) p.off_dh = take((int64_t)p.shares * x->B * p.ld * 4);
+        if (dc || db) {
+            p.off_hz = take((int64_t)p.parts * p.rows_pad * p.ld * 2);
+            const int64_t c_stages = ceil_div(x->B, p.parts == 1 ? 64 : 32);
+            p.c_tiles = (int32_t)ceil_div(x->V, p.parts == 1 ? 256 : 128);
+            // few points: the queries are parted, and the parts joined
+            const int64_t c_splits = std::min(c_stages, std::max<int64_t>(1, p.c_tiles < 256 ? 512 / p.c_tiles : 1));
+            p.c_per_split = (int32_t)ceil_div(c_stages, c_splits);
+            p.c_splits = (int32_t)ceil_div(c_stages, p.c_per_split);
+            if (p.c_splits > 1) {
+                p.off_dc = take((int64_t)p.c_splits * x->V * p.ld * 4);
+                p.off_col = take((int64_t)p.c_splits * x->V * 4);
+            }
+        }
+    } else {
+        p.Kp = (int32_t)round_up(x->d, 16);
+        p.tile_b = x->B <= 32 ? 32 : x->B <= 128 ? 128 : 256;
+        p.tiles_b = (int32_t)ceil_div(x->B, p.tile_b);
+        p.rows_pad = p.tiles_b * p.tile_b;
+        const int64_t tiles_v = ceil_div(x->V, 256);
+        // the losses' splits: a block per CU (its stages fill LDS), and no more than there are tiles
+        p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles_v, 256 / p.tiles_b));
+        // a piece's probabilities: 128 MB in each order, half of the last-level cache
+        const int64_t per = (int64_t)p.rows_pad * 2 * p.parts;
+        int64_t vc = std::max<int64_t>(1024, ((int64_t)128 << 20) / per / 1024 * 1024);
+        if (!p.direct)   // and its copied points
+            vc = std::min(vc, std::max<int64_t>(1024, ((int64_t)128 << 20) / ((int64_t)p.Kp * 2 * p.parts) / 1024 * 1024));
+        p.Vc = std::min(vc, round_up(x->V, 256));
+        p.cols_pad = round_up(p.Vc, 256);
+        // a piece's tiles are split like all of them where there are several pieces
+        p.shares = p.splits * (int32_t)ceil_div(x->V, p.Vc);
+        p.off_h = take((int64_t)p.parts * p.rows_pad * p.Kp * 2);
+        if (!p.direct) p.off_c = take((int64_t)p.parts * p.cols_pad * p.Kp * 2);
+        if (dh) {
             const int32_t tile_d = x->d <= 32 ? 32 : x->d <= 128 ? 128 : 256;
             const int64_t tiles = p.tiles_b * ceil_div(x->d, tile_d);
             const int64_t want = std::max<int64_t>(1, 512 / tiles);
@@ -765,16 +1340,24 @@ Plan make_plan(const boa_xent *x, bool grad)
             p.off_ct = take((int64_t)p.parts * x->d * p.cols_pad * 2);
             p.off_dh = take((int64_t)p.dh_splits * p.rows_pad * x->d * 4);
         }
-        if (x->dpoints) {
+        if (dc) {
             p.off_pt = take(per * p.cols_pad);
             p.off_ht = take((int64_t)p.parts * x->d * p.rows_pad * 2);
-            p.off_own = take(x->B * (int64_t)x->d * 4);
         }
-        if (x->dbias) p.off_col = take((int64_t)p.tiles_b * p.cols_pad * 4);
-        if (x->dpoints || x->dbias) {
-            p.off_first = take(x->V * 4);
-            p.off_ownb = take(x->B * 4);
-        }
+        if (db) p.off_col = take((int64_t)p.tiles_b * p.cols_pad * 4);
+    }
+    p.off_part = take((int64_t)p.shares * x->B * sizeof(RowState));
+    p.off_loss = take(x->B * 4);
+    p.off_pick = take(x->B * 4);
+    p.off_top = take((int64_t)p.rows_pad * 4);
+    p.off_rowf = take((int64_t)p.rows_pad * 4);
+    p.off_label = take((int64_t)p.rows_pad * 4);
+    p.off_factor = take(16);
+    if (grad) p.off_coef = take(x->B * 4);
+    if (dc || db) {
+        p.off_first = take(x->V * 4);
+        p.off_ownb = take(x->B * 4);
+        if (dc) p.off_own = take(x->B * (int64_t)x->d * 4);
     }
     p.total = at;
     return p;
@@ -849,29 +1432,185 @@ int check(const boa_xent *x, bool grad)
     return BOA_OK;
 }
 
+// What one call's steps share.
 template <class T>
-int run_xent(const boa_xent *x, bool grad, uint8_t *ws, hipStream_t st)
+struct Work {
+    const boa_xent *x;
+    bool grad;
+    Plan p;
+    uint8_t *ws;
+    hipStream_t st;
+
+    template <class P>
+    P *at(int64_t off) const { return (P *)(ws + off); }
+    float *row_loss() const { return x->reduction == BOA_REDUCE_NONE ? x->loss : at<float>(p.off_loss); }
+    bool want_c() const { return grad && (x->dpoints || x->dbias); }
+
+    // queries as parts, and their labels
+    void queries(int32_t ld, bf16_t *kept, bf16_t *across) const
+    {
+        PartsArgs a{};
+        a.src = x->h, a.stride = x->h_stride, a.R = (int32_t)x->B, a.C = x->d, a.rows_pad = p.rows_pad;
+        a.plain = at<bf16_t>(p.off_h), a.plain_ld = ld, a.plain_part = (int64_t)p.rows_pad * ld, a.kept = kept;
+        a.across = across, a.across_ld = p.rows_pad, a.across_part = (int64_t)x->d * p.rows_pad;
+        a.labels = x->labels, a.V = (int32_t)x->V, a.label = at<int32_t>(p.off_label);
+        parts_kernel<T><<<dim3((uint32_t)ceil_div(p.rows_pad, 64), (uint32_t)ceil_div(ld, 64)), 256, 0, st>>>(a);
+    }
+
+    // after the statistics: losses, and what the gradients need of each query
+    void rows(int32_t shares) const
+    {
+        const bool reduced = x->reduction != BOA_REDUCE_NONE;
+        RowArgs r{};
+        r.labels = x->labels, r.dloss = grad ? x->dloss : nullptr, r.pick = at<float>(p.off_pick);
+        r.part = at<RowState>(p.off_part), r.loss = row_loss(), r.lse = x->lse;
+        r.top = at<float>(p.off_top), r.rowf = at<float>(p.off_rowf), r.label = at<int32_t>(p.off_label);
+        r.coef = grad ? at<float>(p.off_coef) : nullptr;
+        r.B = (int32_t)x->B, r.V = (int32_t)x->V, r.shares = shares, r.reduction = x->reduction, r.rows_pad = p.rows_pad;
+        row_kernel<<<dim3((uint32_t)ceil_div(p.rows_pad, 4)), 256, 0, st>>>(r);
+        if (reduced || grad)
+            total_kernel<<<1, 1024, 0, st>>>(row_loss(), x->labels, r.B, x->reduction, r.dloss, reduced ? x->loss : nullptr,
+                                             grad ? at<float>(p.off_factor) : nullptr);
+    }
+
+    void own() const
+    {
+        own_kernel<T><<<dim3((uint32_t)x->B), 256, 0, st>>>(
+            (const T *)x->h, x->h_stride, (int32_t)x->B, x->d, at<int32_t>(p.off_label), at<float>(p.off_coef),
+            at<int32_t>(p.off_first), x->dpoints ? at<float>(p.off_own) : nullptr, at<float>(p.off_ownb));
+    }
+};
+
+template <class S>
+void launch_sweep(const SweepArgs &a, hipStream_t st)
 {
-    const Plan p = make_plan(x, grad);
+    const uint32_t grid = S::MODE == SWEEP_C ? split_grid(a.tiles_n, a.splits) : split_grid(a.splits, a.tiles_n);
+    run(sweep_kernel<S>, grid, SWEEP_THREADS, S::lds(), st, a);
+}
+
+template <int DT, int MODE, class T>
+void sweep(const SweepArgs &a, int32_t tile, hipStream_t st)
+{
+    if constexpr (sizeof(T) == 4) {
+        launch_sweep<Sweep<DT, 3, MODE, 1, 4>>(a, st);
+    } else if constexpr (MODE == SWEEP_C) {
+        launch_sweep<Sweep<DT, 1, MODE, 2, 4>>(a, st);
+    } else {
+        if (tile == 32) launch_sweep<Sweep<DT, 1, MODE, 1, 1>>(a, st);
+        else if (tile == 128) launch_sweep<Sweep<DT, 1, MODE, 1, 4>>(a, st);
+        else launch_sweep<Sweep<DT, 1, MODE, 2, 4>>(a, st);
+    }
+}
+
+template <int MODE, class T>
+void sweep(const SweepArgs &a, int32_t tile, int32_t ld, hipStream_t st)
+{
+    if (ld == 32) sweep<1, MODE, T>(a, tile, st);
+    else if (ld == 64) sweep<2, MODE, T>(a, tile, st);
+    else if (ld == 96) sweep<3, MODE, T>(a, tile, st);
+    else sweep<4, MODE, T>(a, tile, st);
+}
+
+template <class T>
+int run_sweeps(const Work<T> &w)
+{
+    const boa_xent *x = w.x;
+    const Plan &p = w.p;
     const int32_t B = (int32_t)x->B, V = (int32_t)x->V, d = x->d;
-    const bool reduced = x->reduction != BOA_REDUCE_NONE;
+    hipStream_t st = w.st;
+    bf16_t *h = w.template at<bf16_t>(p.off_h), *hz = w.want_c() ? w.template at<bf16_t>(p.off_hz) : nullptr;
+    int32_t *first = w.want_c() ? w.template at<int32_t>(p.off_first) : nullptr;
+    float *bias = w.template at<float>(p.off_bias);
+    const int32_t v_pad = (int32_t)round_up(V, 128);
+
+    w.queries(p.ld, hz, nullptr);
+    points_kernel<<<dim3((uint32_t)std::min<int64_t>(1024, ceil_div(v_pad, 256))), 256, 0, st>>>(x->bias, V, v_pad, bias, first);
+    SweepArgs c{};   // the points' side of the arguments
+    if constexpr (sizeof(T) == 4) {
+        c.mf = (const float *)x->points, c.m_ld = x->points_stride;
+        c.vec = d % 4 == 0 && x->points_stride % 4 == 0 && aligned(x->points, 16);
+        c.Kp = p.ld;
+    } else if (p.direct) {
+        c.m = (const bf16_t *)x->points, c.m_ld = x->points_stride, c.Kp = d;
+    } else {
+        PartsArgs a{};
+        a.src = x->points, a.stride = x->points_stride, a.R = V, a.C = d, a.rows_pad = V;
+        a.plain = w.template at<bf16_t>(p.off_c), a.plain_ld = p.ld;
+        parts_kernel<T><<<dim3((uint32_t)ceil_div(V, 64), (uint32_t)ceil_div(p.ld, 64)), 256, 0, st>>>(a);
+        c.m = a.plain, c.m_ld = p.ld, c.Kp = p.ld;
+    }
+    SweepArgs a = c;
+    a.n = h, a.n_ld = p.ld, a.n_part = (int64_t)p.rows_pad * p.ld, a.N = B, a.M = V, a.d = d;
+    a.Kp = p.ld;
+    if (p.direct) a.Kp = d;   // h has zeros there, the points other values
+    a.tiles_n = p.tiles_b, a.splits = p.splits, a.per_split = p.per_split;
+    a.stages = (int32_t)ceil_div(V, p.tile_b == 32 ? 128 : p.parts == 1 ? 64 : 32);
+    a.scale2 = x->scale * LOG2E, a.bias = bias, a.label = w.template at<int32_t>(p.off_label);
+    a.pick = w.template at<float>(p.off_pick), a.part = w.template at<RowState>(p.off_part);
+    const bool dh = w.grad && x->dh;
+    if (dh) {
+        a.out = w.template at<float>(p.off_dh);
+        sweep<SWEEP_H, T>(a, p.tile_b, p.ld, st);
+    } else {
+        sweep<SWEEP_LOSS, T>(a, p.tile_b, p.ld, st);
+    }
+    w.rows(p.shares);
+    if (!w.grad) return launch_status("softmax_xent");
+    const float *factor = w.template at<float>(p.off_factor), *coef = w.template at<float>(p.off_coef);
+    if (dh)
+        dh_shares_kernel<T><<<dim3((uint32_t)ceil_div((int64_t)B * d, 256)), 256, 0, st>>>(
+            a.out, a.part, p.shares, B, d, p.ld, w.template at<float>(p.off_top), w.template at<float>(p.off_rowf),
+            (const T *)x->points, x->points_stride, a.label, coef, factor, x->scale, (T *)x->dh);
+    if (w.want_c()) {
+        w.own();
+        SweepArgs g = c;
+        g.n = c.m, g.nf = c.mf, g.n_ld = c.m_ld, g.N = V, g.M = B, g.d = d;
+        g.m = hz, g.mf = nullptr, g.m_ld = p.ld, g.m_part = (int64_t)p.rows_pad * p.ld;
+        g.tiles_n = p.c_tiles, g.splits = p.c_splits, g.per_split = p.c_per_split;
+        g.stages = (int32_t)ceil_div(B, p.parts == 1 ? 64 : 32);
+        g.scale2 = a.scale2, g.bias = bias, g.label = a.label;
+        g.top = w.template at<float>(p.off_top), g.rowf = w.template at<float>(p.off_rowf);
+        g.first = first, g.factor = factor, g.scale = x->scale;
+        g.own = x->dpoints ? w.template at<float>(p.off_own) : nullptr, g.own_bias = w.template at<float>(p.off_ownb);
+        g.dc = x->dpoints, g.dbias = x->dbias;
+        if (p.c_splits > 1) {
+            g.out = w.template at<float>(p.off_dc);
+            g.col = x->dbias ? w.template at<float>(p.off_col) : nullptr;
+        }
+        sweep<SWEEP_C, T>(g, 0, p.ld, st);
+        if (p.c_splits > 1)
+            dc_join_kernel<T><<<dim3((uint32_t)ceil_div((int64_t)V * (x->dpoints ? d : 1), 256)), 256, 0, st>>>(
+                g.out, g.col, p.c_splits, V, d, p.ld, first, g.own, g.own_bias, factor, x->scale, (T *)x->dpoints, x->dbias);
+    }
+    return launch_status("softmax_xent_grad");
+}
+
+template <class T>
+int run_tiles(const Work<T> &w)
+{
+    const boa_xent *x = w.x;
+    const Plan &p = w.p;
+    const bool grad = w.grad;
+    uint8_t *ws = w.ws;
+    hipStream_t st = w.st;
+    const int32_t B = (int32_t)x->B, V = (int32_t)x->V, d = x->d;
     bf16_t *hp = (bf16_t *)(ws + p.off_h), *ht = grad && x->dpoints ? (bf16_t *)(ws + p.off_ht) : nullptr;
-    float *row_loss = reduced ? (float *)(ws + p.off_loss) : x->loss;
     float *factor = (float *)(ws + p.off_factor);
     const int64_t h_part = (int64_t)p.rows_pad * p.Kp, ht_part = (int64_t)d * p.rows_pad;
-
-    parts_kernel<T><<<dim3((uint32_t)ceil_div(p.rows_pad, 64), (uint32_t)ceil_div(p.Kp, 64)), 256, 0, st>>>(
-        (const T *)x->h, x->h_stride, B, d, hp, p.Kp, h_part, p.rows_pad, ht, p.rows_pad, ht_part, d);
+    w.queries(p.Kp, nullptr, ht);
 
     const int32_t pieces = (int32_t)ceil_div(V, p.Vc);
     auto points_of = [&](int64_t v0, int32_t n, bool across) {
         Operand o{};
         bf16_t *cp = p.direct ? nullptr : (bf16_t *)(ws + p.off_c);
         bf16_t *ct = across ? (bf16_t *)(ws + p.off_ct) : nullptr;
-        if (cp || ct)
-            parts_kernel<T><<<dim3((uint32_t)(p.cols_pad / 64), (uint32_t)ceil_div(p.Kp, 64)), 256, 0, st>>>(
-                (const T *)x->points + v0 * x->points_stride, x->points_stride, n, d, cp, p.Kp,
-                p.cols_pad * p.Kp, (int32_t)p.cols_pad, ct, p.cols_pad, (int64_t)d * p.cols_pad, d);
+        if (cp || ct) {
+            PartsArgs a{};
+            a.src = (const T *)x->points + v0 * x->points_stride, a.stride = x->points_stride;
+            a.R = n, a.C = d, a.rows_pad = (int32_t)p.cols_pad, a.plain = cp, a.plain_ld = p.Kp, a.plain_part = p.cols_pad * p.Kp;
+            a.across = ct, a.across_ld = p.cols_pad, a.across_part = (int64_t)d * p.cols_pad;
+            parts_kernel<T><<<dim3((uint32_t)(p.cols_pad / 64), (uint32_t)ceil_div(p.Kp, 64)), 256, 0, st>>>(a);
+        }
         o.p = cp ? cp : (const bf16_t *)x->points + v0 * x->points_stride;
         o.ld = cp ? p.Kp : x->points_stride;
         o.rows = cp ? (int32_t)p.cols_pad : n;
@@ -891,7 +1630,8 @@ int run_xent(const boa_xent *x, bool grad, uint8_t *ws, hipStream_t st)
             set_segments(a.pr, p.parts, p.cols_pad * p.Kp, h_part);
             a.bias = x->bias ? x->bias + v0 : nullptr;
             a.scale2 = x->scale * LOG2E;
-            a.B = B, a.V = n, a.tiles_b = p.tiles_b;
+            a.label = (const int32_t *)(ws + p.off_label), a.pick = (float *)(ws + p.off_pick);
+            a.B = B, a.V = n, a.v0 = (int32_t)v0, a.tiles_b = p.tiles_b;
             a.tiles_v = (int32_t)ceil_div(n, 256);
             a.splits = std::min(p.splits, a.tiles_v);
             a.part = (RowState *)(ws + p.off_part) + (int64_t)used * B;
@@ -901,17 +1641,7 @@ int run_xent(const boa_xent *x, bool grad, uint8_t *ws, hipStream_t st)
                 run(stats_kernel<S>, split_grid(a.splits, a.tiles_b), S::THREADS, stage_bytes<S>(), st, a);
             });
         }
-        RowArgs r{};
-        r.h = x->h, r.points = x->points, r.h_stride = x->h_stride, r.points_stride = x->points_stride;
-        r.labels = x->labels, r.bias = x->bias, r.dloss = grad ? x->dloss : nullptr;
-        r.part = (RowState *)(ws + p.off_part), r.loss = row_loss, r.lse = x->lse;
-        r.top = (float *)(ws + p.off_top), r.rowf = (float *)(ws + p.off_rowf);
-        r.coef = grad ? (float *)(ws + p.off_coef) : nullptr, r.label = (int32_t *)(ws + p.off_label);
-        r.scale = x->scale, r.B = B, r.V = V, r.d = d, r.splits = used, r.reduction = x->reduction, r.rows_pad = p.rows_pad;
-        row_kernel<T><<<dim3((uint32_t)ceil_div(p.rows_pad, 4)), 256, 0, st>>>(r);
-        if (reduced || grad)
-            total_kernel<<<1, 1024, 0, st>>>(row_loss, x->labels, B, x->reduction, grad ? x->dloss : nullptr,
-                                             reduced ? x->loss : nullptr, grad ? factor : nullptr);
+        w.rows(used);
     }
     if (!grad || !(x->dh || x->dpoints || x->dbias)) return launch_status("softmax_xent");
 
@@ -924,7 +1654,7 @@ int run_xent(const boa_xent *x, bool grad, uint8_t *ws, hipStream_t st)
         own_bias = (float *)(ws + p.off_ownb);
         own = x->dpoints ? (float *)(ws + p.off_own) : nullptr;
         fill_kernel<<<dim3((uint32_t)std::min<int64_t>(1024, ceil_div(V, 256))), 256, 0, st>>>(first, V, -1);
-        own_kernel<T><<<dim3((uint32_t)B), 256, 0, st>>>((const T *)x->h, x->h_stride, B, d, label, coef, first, own, own_bias);
+        w.own();
     }
     const int64_t p_part = (int64_t)p.rows_pad * p.cols_pad;
     for (int32_t i = 0; i < pieces; ++i) {
@@ -1021,7 +1751,12 @@ int xent(const boa_xent *x, bool grad, void *ws, int64_t ws_bytes, void *stream)
     }
     if (!ws || !aligned(ws, 16) || ws_bytes < make_plan(x, grad).total)
         return bad("softmax_xent: workspace missing, unaligned or too small");
-    return x->dtype == BOA_T_F32 ? run_xent<float>(x, grad, (uint8_t *)ws, st) : run_xent<bf16_t>(x, grad, (uint8_t *)ws, st);
+    if (x->dtype == BOA_T_F32) {
+        const Work<float> w{x, grad, make_plan(x, grad), (uint8_t *)ws, st};
+        return w.p.sweep ? run_sweeps(w) : run_tiles(w);
+    }
+    const Work<bf16_t> w{x, grad, make_plan(x, grad), (uint8_t *)ws, st};
+    return w.p.sweep ? run_sweeps(w) : run_tiles(w);
 }
 
 }  // namespace
