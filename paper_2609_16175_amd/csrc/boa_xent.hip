@@ -758,7 +758,7 @@ struct Sweep {
     static constexpr int CH = DT == 1 ? 4 : DT == 2 ? 8 : 16;            // 16-byte chunks of an LDS row
     static constexpr int ROWB = CH * 16, PLANE = SR * ROWB;
     static constexpr int SIDES = MODE == SWEEP_C ? 3 : 1;    // float arrays along M: bias, or top, factor and label
-    static constexpr int STAGE = PARTS * PLANE + SIDES * SR * 4;
+    static constexpr int STAGE = (PARTS * PLANE + SIDES * SR * 4 + 255) / 256 * 256;
     static constexpr bool STAGED = PARTS == 3 && MODE != SWEEP_C;        // float32 points: split on the way to LDS
     static constexpr int OUT_LD = DT * 32 + 4;               // floats of a row of the output in LDS
     static constexpr size_t lds()
@@ -791,11 +791,14 @@ struct SweepArgs {
     float scale;
 };
 
+typedef __attribute__((address_space(3))) bf16x8 LdsRow;
+typedef __attribute__((address_space(3))) short4v LdsFour;
+
 template <class S>
 __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
 {
     constexpr int DT = S::DT, PARTS = S::PARTS, TN = S::TN, KS = 2 * DT;
-    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    extern __shared__ __attribute__((aligned(256))) uint8_t smem[];
     int32_t split, tn0;
     if (S::MODE == SWEEP_C ? !split_block(a.tiles_n, a.splits, &tn0, &split)
                            : !split_block(a.splits, a.tiles_n, &split, &tn0))
@@ -932,7 +935,9 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
 
     // lane's place in transposed reads: group g of 16 lanes takes values 16 (g & 1).. of rows 4 half..
     const int tr_row = ((lane & 15) >> 2) + 4 * half, tr_chunk = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
-    const int tr_at = (lane & 1) * 8;
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
+    const uint32_t s_lane = r * S::ROWB + ((half ^ (r & (S::CH - 1))) * 16);
+    const uint32_t t_lane = tr_row * S::ROWB + ((tr_chunk ^ (tr_row & (S::CH - 1))) * 16) + (lane & 1) * 8;
 
     if (s_begin < s_end) {
         dma(0, s_begin);
@@ -951,6 +956,10 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
 #pragma unroll 1
         for (int sub = 0; sub < S::SUBS; ++sub) {   // not unrolled: the registers are full
             const int row0 = (sub * S::WS + ws) * 32;   // of the stage
+            // Both reads' addresses: the chunk's permutation is an exclusive or on
+            // bits that rows and stages leave alone.
+            const uint32_t s_at = base + buf * S::STAGE + row0 * S::ROWB + s_lane;
+            const uint32_t t_at = base + buf * S::STAGE + row0 * S::ROWB + t_lane;
             f32x16 acc[TN];
 #pragma unroll
             for (int j = 0; j < TN; ++j)
@@ -958,10 +967,10 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                 for (int e = 0; e < 16; ++e) acc[j][e] = 0.0f;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const uint8_t *at = from + (row0 + r) * S::ROWB + (((2 * k + half) ^ (r & (S::CH - 1))) * 16);
+                if (S::TN * S::DT >= 8 && k && k % 2 == 0) __builtin_amdgcn_sched_barrier(0);
                 bf16x8 fm[PARTS];
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p) fm[p] = *(const bf16x8 *)(at + p * S::PLANE);
+                for (int p = 0; p < PARTS; ++p) fm[p] = *(const LdsRow *)(uintptr_t)((s_at ^ (k * 32)) + p * S::PLANE);
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
                     if constexpr (PARTS == 3) {
@@ -974,30 +983,37 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                     acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fn[0][k][j], acc[j], 0, 0, 0);
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);   // the registers are full: the phases stay apart
             // logits to probabilities
             if constexpr (S::MODE != SWEEP_C) {
-                float bias[16];
+                float top[TN];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) load_f32<4, float>(*(float(*)[4])(bias + 4 * q), side + row0 + 8 * q + 4 * half);
+                for (int j = 0; j < TN; ++j) top[j] = NO_MAX;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float bias[4];
+                    load_f32<4, float>(bias, side + row0 + 8 * q + 4 * half);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            acc[j][4 * q + e] = fmaf(acc[j][4 * q + e], a.scale2, bias[e]);
+                            top[j] = fmaxf(top[j], acc[j][4 * q + e]);
+                        }
+                }
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
-                    float top = NO_MAX;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        acc[j][e] = fmaf(acc[j][e], a.scale2, bias[e]);
-                        top = fmaxf(top, acc[j][e]);
-                    }
-                    if (__any(top > mx[j] + SLACK)) {
-                        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-                        top = fmaxf(fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])), mx[j]);
-                        const float by = __builtin_amdgcn_exp2f(mx[j] - top);
+                    if (__any(top[j] > mx[j] + SLACK)) {
+                        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[j]), __float_as_uint(top[j]), false, false);
+                        const float now = fmaxf(fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])), mx[j]);
+                        const float by = __builtin_amdgcn_exp2f(mx[j] - now);
                         sum[j] *= by;
                         if constexpr (S::MODE == SWEEP_H)
 #pragma unroll
                             for (int i = 0; i < DT; ++i)
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) out[i][j][e] *= by;
-                        mx[j] = top;
+                        mx[j] = now;
                     }
                     const int32_t rel = lab[j] - (stage * S::SR + row0);
                     const bool mine = (uint32_t)rel < 32u;
@@ -1006,9 +1022,9 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                         for (int e = 0; e < 16; ++e) {
                             const bool here = rel == tile_row(e, half);
                             if (here) a.pick[n0 + j * 32 + r] = acc[j][e];
-                            acc[j][e] = __builtin_amdgcn_exp2f(acc[j][e] - mx[j]);
-                            sum[j] += acc[j][e];
-                            if (here) acc[j][e] = 0.0f;
+                            const float p = __builtin_amdgcn_exp2f(acc[j][e] - mx[j]);
+                            sum[j] += p;
+                            acc[j][e] = here ? 0.0f : p;
                         }
                     } else {
 #pragma unroll
@@ -1019,7 +1035,6 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                     }
                 }
             } else {
-                const int32_t own = ((const int32_t *)side)[2 * S::SR + row0 + r];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     float top[4], f[4];
@@ -1031,6 +1046,7 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                         for (int e = 0; e < 4; ++e)
                             acc[j][4 * q + e] = f[e] * __builtin_amdgcn_exp2f(fmaf(acc[j][4 * q + e], a.scale2, off[j]) - top[e]);
                 }
+                const int32_t own = ((const int32_t *)side)[2 * S::SR + row0 + r];
                 if (__any((uint32_t)(own - n0) < (uint32_t)(32 * TN))) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
@@ -1048,15 +1064,16 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
             }
             // the second product
             if constexpr (S::MODE != SWEEP_LOSS) {
+                bf16x8 fp[2][PARTS][TN];
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+#pragma unroll
+                        for (int p = 0; p < PARTS; ++p) fp[e >> 3][p][j][e & 7] = part_of<PARTS>(acc[j][e], p);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) {
-                    bf16x8 fp[PARTS][TN];
-#pragma unroll
-                    for (int j = 0; j < TN; ++j)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-#pragma unroll
-                            for (int p = 0; p < PARTS; ++p) fp[p][j][e] = part_of<PARTS>(acc[j][8 * kb + e], p);
 #pragma unroll
                     for (int i = 0; i < DT; ++i) {
                         bf16x8 fm[PARTS];
@@ -1064,11 +1081,10 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                         for (int p = 0; p < PARTS; ++p)
 #pragma unroll
                             for (int jj = 0; jj < 2; ++jj) {
-                                const int row = row0 + 16 * kb + 8 * jj + tr_row;
-                                const uint8_t *at = from + p * S::PLANE + row * S::ROWB
-                                                    + (((i * 4 + tr_chunk) ^ (row & (S::CH - 1))) * 16) + tr_at;
-                                const short4v four = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                    (__attribute__((address_space(3))) short4v *)at);
+                                // of chunk i * 4 + tr_chunk of row 16 kb + 8 jj + tr_row
+                                const uint32_t at = (t_at ^ ((i * 64) ^ (jj * 128 & (S::CH - 1) * 16)))
+                                                    + p * S::PLANE + (16 * kb + 8 * jj) * S::ROWB;
+                                const short4v four = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsFour *)(uintptr_t)at);
                                 const bf16x4 v = __builtin_bit_cast(bf16x4, four);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) fm[p][4 * jj + e] = v[e];
@@ -1076,13 +1092,13 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
 #pragma unroll
                         for (int j = 0; j < TN; ++j) {
                             if constexpr (PARTS == 3) {
-                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[2], fp[0][j], out[i][j], 0, 0, 0);
-                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[1], fp[1][j], out[i][j], 0, 0, 0);
-                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fp[2][j], out[i][j], 0, 0, 0);
-                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[1], fp[0][j], out[i][j], 0, 0, 0);
-                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fp[1][j], out[i][j], 0, 0, 0);
+                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[2], fp[kb][0][j], out[i][j], 0, 0, 0);
+                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[1], fp[kb][1][j], out[i][j], 0, 0, 0);
+                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fp[kb][2][j], out[i][j], 0, 0, 0);
+                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[1], fp[kb][0][j], out[i][j], 0, 0, 0);
+                                out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fp[kb][1][j], out[i][j], 0, 0, 0);
                             }
-                            out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fp[0][j], out[i][j], 0, 0, 0);
+                            out[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fp[kb][0][j], out[i][j], 0, 0, 0);
                         }
                     }
                 }
