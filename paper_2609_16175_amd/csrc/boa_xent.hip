@@ -40,15 +40,18 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 // running maximum of nothing: exp2(-inf - NO_MAX) is 0 and not NaN, and logits at the type's lowest value still count
 constexpr float NO_MAX = -__FLT_MAX__;
-constexpr int BK = 64;               // values of k per stage: 128 bytes of a row
+constexpr int BK = 32;               // values of k per stage of tile_product
+constexpr int STAGES = 4;            // of them in LDS
 constexpr int MAX_SEG = 6;
 
-// One operand: `rows` rows of bf16, `ld` values apart. Rows past the end are
-// read as the last one (their results are dropped).
+// One operand of a product: bf16 rows `ld` values apart, which run along k or,
+// `across`, along the operand's own dimension (a row is then one k). Rows past
+// the end are read as the last one, 16-byte chunks past `cols` as the row's
+// first; what they give is dropped, or meets zeros on the other side.
 struct Operand {
     const bf16_t *p;
     int64_t ld;
-    int32_t rows;
+    int32_t rows, cols;
 };
 
 // A product over segments of k: K values (a multiple of 16) of the parts
@@ -64,75 +67,134 @@ struct Shape {
     static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_;
     static constexpr int BM = WM * TM * 32, BN = WN * TN * 32, THREADS = 64 * WM * WN;
     static constexpr int STAGE = (BM + BN) * BK;   // bf16 values of one stage
+    static constexpr int NA = BM * 4 / THREADS, NB = BN * 4 / THREADS;   // 16-byte loads of a thread and stage
+    static_assert(NA * THREADS == BM * 4 && NB * THREADS == BN * 4, "every wave loads the same");
+};
+
+// Waits until at most `left` of this wave's loads are on their way and its LDS
+// reads are done, then for the other waves.
+template <int LEFT>
+__device__ inline void wait_and_meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
+// One operand's side of tile_product: where this thread's loads come from and
+// where its fragments lie. ROWS of the operand's own dimension.
+//
+// Along k, a stage holds ROWS rows of 64 bytes whose 16-byte chunks are stored
+// in the order chunk ^ (row / 4 & 3); across, 32 rows of ROWS values in the
+// order chunk ^ (row & 3) * 4, and fragments are read transposed, 64 bytes of
+// four rows by half a wave. Either way what lanes read together spreads over
+// the banks.
+// The permutation is applied to the addresses loaded from, since a load to LDS
+// writes its lanes in order.
+template <class S, int ROWS, bool ACROSS>
+struct Side {
+    static constexpr int N = ROWS * 4 / S::THREADS;
+    static constexpr int PER = ACROSS ? S::THREADS / (ROWS / 8) : S::THREADS / 4;   // LDS rows of one load of all threads
+    const bf16_t *p;
+    int64_t ld;
+    int32_t row, last, at;   // this thread's first row, the last there is, value within a row (across: of the tile's first)
+    int32_t cols;
+    static_assert(!ACROSS || ROWS >= 128, "the permutation takes 16 chunks");
+
+    __device__ Side(const Operand &o, int32_t row0, int32_t from_k)
+    {
+        const int t = threadIdx.x;
+        ld = o.ld, last = o.rows - 1, cols = o.cols;
+        if constexpr (ACROSS) {
+            row = from_k + t / (ROWS / 8);
+            at = row0;
+            p = o.p;
+        } else {
+            row = row0 + (t >> 2);
+            at = ((t & 3) ^ ((t >> 4) & 3)) * 8;
+            p = o.p + from_k;
+        }
+    }
+    // loads k [k0, k0 + BK) of a part; K: end of k
+    __device__ void load(bf16_t *to, int64_t part, int32_t k0, int32_t K) const
+    {
+        const int wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bf16_t *from;
+            if constexpr (ACROSS) {
+                const int t = threadIdx.x, chunk = (t % (ROWS / 8)) ^ (((t / (ROWS / 8) + i * PER) & 3) * 4);
+                from = p + part + (int64_t)min(row + k0 + i * PER, last) * ld + (at + chunk * 8 < cols ? at + chunk * 8 : 0);
+            } else
+                from = p + part + (int64_t)min(row + i * PER, last) * ld + (k0 + at < K ? k0 + at : 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                             (__attribute__((address_space(3))) void *)(to + (i * S::THREADS + wave * 64) * 8),
+                                             16, 0, 0);
+        }
+    }
+    // the fragment of 32 rows from row0 (of the tile) and k step s
+    __device__ static bf16x8 fragment(const bf16_t *from, int row0, int s)
+    {
+        const int lane = threadIdx.x & 63, half = lane >> 5, r = lane & 31;
+        if constexpr (ACROSS) {
+            bf16x8 f;
+            const int k = 8 * half + ((lane & 15) >> 2), chunk = row0 / 8 + ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
+#pragma unroll
+            for (int jj = 0; jj < 2; ++jj) {
+                const int row = 16 * s + k + 4 * jj;
+                const bf16_t *a = from + row * ROWS + (chunk ^ ((row & 3) * 4)) * 8 + (lane & 1) * 4;
+                const bf16x4 v = __builtin_bit_cast(
+                    bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v *)a));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[4 * jj + e] = v[e];
+            }
+            return f;
+        } else {
+            return *(const bf16x8 *)(from + (row0 + r) * BK + ((s * 2 + half) ^ ((r >> 2) & 3)) * 8);
+        }
+    }
 };
 
 // acc += A[row0a ..][k] * B[row0b ..][k], k in [from_k, from_k + K), over all
-// segments. Two stages of
-// BK values of k: the loads of the next stage go straight to LDS while the
-// matrix instructions work on this one. A stage holds rows of 128 bytes whose
-// 16-byte chunks are stored in the order chunk ^ (row & 7), so that the 32
-// rows a fragment reads at one k spread over the banks; the permutation is
-// applied to the addresses loaded from, since a load to LDS writes its lanes
-// in order.
-template <class S>
+// segments. Four stages of 32 k in LDS, loads three stages ahead of the matrix
+// instructions: a stage is about 1000 cycles of them, and memory answers
+// within three. ACROSS_A, ACROSS_B: the operand's rows are k.
+template <class S, bool ACROSS_A, bool ACROSS_B>
 __device__ inline void tile_product(const Product &pr, int32_t row0a, int32_t row0b, bf16_t *lds,
                                     f32x16 (&acc)[S::TM][S::TN], int32_t from_k, int32_t K)
 {
-    constexpr int NA = (S::BM * 8 + S::THREADS - 1) / S::THREADS, NB = (S::BN * 8 + S::THREADS - 1) / S::THREADS;
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int wm = wave % S::WM, wn = wave / S::WM;
-    const int chunk = (t & 7) ^ ((t >> 3) & 7);
-    const bf16_t *pa[NA], *pb[NB];
-#pragma unroll
-    for (int i = 0; i < NA; ++i)
-        pa[i] = pr.a.p + (int64_t)min(row0a + i * (S::THREADS / 8) + (t >> 3), pr.a.rows - 1) * pr.a.ld + from_k;
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-        pb[i] = pr.b.p + (int64_t)min(row0b + i * (S::THREADS / 8) + (t >> 3), pr.b.rows - 1) * pr.b.ld + from_k;
+    const int wave = threadIdx.x >> 6, wm = wave % S::WM, wn = wave / S::WM;
+    const Side<S, S::BM, ACROSS_A> a(pr.a, row0a, from_k);
+    const Side<S, S::BN, ACROSS_B> b(pr.b, row0b, from_k);
     const int per_seg = (K + BK - 1) / BK, total = per_seg * pr.segs;
-
-    auto load = [&](int stage, int seg, int k0) {
+    int seg = 0, k_load = 0;
+    auto load = [&](int stage) {   // past the end, what is loaded is not used
         bf16_t *to = lds + stage * S::STAGE;
-        // chunks past K are not multiplied: read the row's first instead
-        const int k = k0 + chunk * 8 < K ? k0 + chunk * 8 : 0;
-        const int64_t oa = pr.seg_a[seg] + k, ob = pr.seg_b[seg] + k;
-#pragma unroll
-        for (int i = 0; i < NA; ++i)
-            if ((i * S::THREADS + wave * 64) < S::BM * 8)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(pa[i] + oa),
-                                                 (__attribute__((address_space(3))) void *)(to + (i * S::THREADS + wave * 64) * 8),
-                                                 16, 0, 0);
-#pragma unroll
-        for (int i = 0; i < NB; ++i)
-            if ((i * S::THREADS + wave * 64) < S::BN * 8)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(pb[i] + ob),
-                                                 (__attribute__((address_space(3))) void *)(to + S::BM * BK + (i * S::THREADS + wave * 64) * 8),
-                                                 16, 0, 0);
-    };
-
-    const int r = lane & 31, half = lane >> 5;
-    const int at_a = (wm * S::TM * 32 + r) * BK, at_b = S::BM * BK + (wn * S::TN * 32 + r) * BK;
-    load(0, 0, 0);
-    __syncthreads();
-    int seg = 0, k0 = 0;
-    for (int it = 0; it < total; ++it) {
-        const int steps = min(BK, K - k0) >> 4;
-        k0 += BK;
-        if (k0 >= K) {
-            k0 = 0;
+        a.load(to, pr.seg_a[seg], k_load, K);
+        b.load(to + S::BM * BK, pr.seg_b[seg], k_load, K);
+        k_load += BK;
+        if (k_load >= K && seg + 1 < pr.segs) {
+            k_load = 0;
             ++seg;
+        } else if (k_load >= K) {
+            k_load -= BK;
         }
-        if (it + 1 < total) load((it + 1) & 1, seg, k0);
-        const bf16_t *from = lds + (it & 1) * S::STAGE;
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) load(i);
+    int k0 = 0;
+    for (int it = 0; it < total; ++it) {
+        wait_and_meet<(STAGES - 2) * (S::NA + S::NB)>();
+        load((it + STAGES - 1) % STAGES);
+        const int steps = min(BK, K - k0) >> 4;
+        k0 = k0 + BK < K ? k0 + BK : 0;
+        const bf16_t *from = lds + (it % STAGES) * S::STAGE;
 #pragma unroll
         for (int s = 0; s < BK / 16; ++s) {
             if (s < steps) {
-                const int c = ((s * 2 + half) ^ (r & 7)) * 8;
                 bf16x8 fa[S::TM], fb[S::TN];
 #pragma unroll
-                for (int i = 0; i < S::TM; ++i) fa[i] = *(const bf16x8 *)(from + at_a + i * 32 * BK + c);
+                for (int i = 0; i < S::TM; ++i) fa[i] = a.fragment(from, (wm * S::TM + i) * 32, s);
 #pragma unroll
-                for (int j = 0; j < S::TN; ++j) fb[j] = *(const bf16x8 *)(from + at_b + j * 32 * BK + c);
+                for (int j = 0; j < S::TN; ++j) fb[j] = b.fragment(from + S::BM * BK, (wn * S::TN + j) * 32, s);
 #pragma unroll
                 for (int i = 0; i < S::TM; ++i)
 #pragma unroll
@@ -140,8 +202,8 @@ __device__ inline void tile_product(const Product &pr, int32_t row0a, int32_t ro
                         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
             }
         }
-        __syncthreads();
     }
+    wait_and_meet<0>();
 }
 
 // Row of a 32 x 32 tile that a lane's value i stands for (the column is lane & 31).
@@ -173,66 +235,70 @@ __device__ inline void clear(f32x16 (&acc)[S::TM][S::TN])
 // operands
 
 // Copies rows (R x C) as bf16 parts, zeros past the end: `plain`
-// [part][rows_pad][plain_ld], `kept` the same without the rows that are left
-// out (whatever they hold, zeros take their place), `across` [part][C][across_ld]
-// likewise without. Any of them may be null. Of queries it also gives the
-// labels: -1 where a query has none, past the last one too.
+// [part][rows_pad][plain_ld], and `kept` the same without the rows that are left
+// out (whatever they hold, zeros take their place). Either may be null. Of
+// queries it also gives the labels: -1 where a query has none, past the last
+// one too.
 struct PartsArgs {
     const void *src;
-    int64_t stride, plain_ld, plain_part, across_ld, across_part;
+    int64_t stride, plain_ld, plain_part;
     int32_t R, C, rows_pad;
-    bf16_t *plain, *kept, *across;
+    bf16_t *plain, *kept;
     const int64_t *labels;   // of queries, or null
     int32_t V;
     int32_t *label;          // rows_pad
 };
 
+// A thread makes 8 values of a row (plain_ld is a multiple of 16).
 template <class T>
 __global__ __launch_bounds__(256) void parts_kernel(PartsArgs a)
 {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    __shared__ bf16_t tile[PARTS][64][66];
-    __shared__ int32_t live[64];
-    const int32_t r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
-    const int c = threadIdx.x & 63;
-    if (threadIdx.x < 64) {
-        const int32_t b = r0 + c;
-        int32_t y = 0;
-        if (a.labels) {
-            y = b < a.R && a.labels[b] >= 0 && a.labels[b] < a.V ? (int32_t)a.labels[b] : -1;
-            if (blockIdx.y == 0 && b < a.rows_pad) a.label[b] = y;
-        }
-        live[c] = y >= 0;
+    const int64_t chunks = a.plain_ld / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t r = i / chunks;
+    const int32_t c = (int32_t)(i % chunks) * 8;
+    if (r >= a.rows_pad) return;
+    bool live = true;
+    if (a.labels) {
+        const int64_t y = r < a.R ? a.labels[r] : -1;
+        live = y >= 0 && y < a.V;
+        if (c == 0) a.label[r] = live ? (int32_t)y : -1;
     }
-    for (int r = threadIdx.x >> 6; r < 64; r += 4) {
-        float v = 0.0f;
-        if (r0 + r < a.R && c0 + c < a.C) v = (float)((const T *)a.src)[(int64_t)(r0 + r) * a.stride + c0 + c];
+    float v[8];
+    const T *from = (const T *)a.src + r * a.stride + c;
+    if (r < a.R && c + 8 <= a.C && aligned16(from)) {
+        constexpr int N = 16 / sizeof(T);
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-            if constexpr (PARTS == 1) {
-                tile[0][r][c] = (bf16_t)v;
-            } else {
-                const float part = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
-                tile[p][r][c] = (bf16_t)part;
-                v = fabsf(part) < INFINITY ? v - part : 0.0f;   // an infinity or NaN is its first part alone
-            }
-        }
+        for (int e = 0; e < 8; e += N) load_f32<N, T>(*(float(*)[N])(v + e), from + e);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = r < a.R && c + e < a.C ? (float)from[e] : 0.0f;
     }
-    __syncthreads();
-    const bf16_t nil = (bf16_t)0.0f;
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
-        for (int r = threadIdx.x >> 6; r < 64; r += 4)
-            if (r0 + r < a.rows_pad && c0 + c < a.plain_ld) {
-                const int64_t at = p * a.plain_part + (int64_t)(r0 + r) * a.plain_ld + c0 + c;
-                if (a.plain) a.plain[at] = tile[p][r][c];
-                if (a.kept) a.kept[at] = live[r] ? tile[p][r][c] : nil;
+        bf16x8 part, nil;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            nil[e] = (bf16_t)0.0f;
+            if constexpr (PARTS == 1) {
+                part[e] = (bf16_t)v[e];
+            } else {
+                const float top = __uint_as_float(__float_as_uint(v[e]) & 0xFFFF0000u);
+                part[e] = (bf16_t)top;
+                v[e] = fabsf(top) < INFINITY ? v[e] - top : 0.0f;   // an infinity or NaN is its first part alone
             }
-        if (a.across)
-            for (int k = threadIdx.x >> 6; k < 64; k += 4)
-                if (c0 + k < a.C && r0 + c < a.across_ld)
-                    a.across[p * a.across_part + (int64_t)(c0 + k) * a.across_ld + r0 + c] = live[c] ? tile[p][c][k] : nil;
+        }
+        const int64_t at = p * a.plain_part + r * a.plain_ld + c;
+        if (a.plain) *(bf16x8 *)(a.plain + at) = part;
+        if (a.kept) *(bf16x8 *)(a.kept + at) = live ? part : nil;
     }
+}
+
+template <class T>
+void launch_parts(const PartsArgs &a, hipStream_t st)
+{
+    const int64_t n = (int64_t)a.rows_pad * (a.plain_ld / 8);
+    parts_kernel<T><<<dim3((uint32_t)((n + 255) / 256)), 256, 0, st>>>(a);
 }
 
 // ---------------------------------------------------------------------------
@@ -287,7 +353,7 @@ __global__ __launch_bounds__(S::THREADS) void stats_kernel(StatsArgs a)
     for (int32_t tv = split; tv < a.tiles_v; tv += a.splits) {
         f32x16 acc[S::TM][S::TN];
         clear<S>(acc);
-        tile_product<S>(a.pr, tv * S::BM, tb * S::BN, lds, acc, 0, a.pr.K);
+        tile_product<S, false, false>(a.pr, tv * S::BM, tb * S::BN, lds, acc, 0, a.pr.K);
 #pragma unroll
         for (int i = 0; i < S::TM; ++i) {
             const int32_t v0 = tv * S::BM + (wm * S::TM + i) * 32;
@@ -424,7 +490,7 @@ struct ProbArgs {
     const float *bias;       // of the piece
     const float *top, *rowf;
     const int32_t *label;
-    bf16_t *p, *pt;          // [part][rows_pad][cols_pad], [part][cols_pad][rows_pad], or null
+    bf16_t *p;               // [part][rows_pad][cols_pad], or null
     float *col;              // tiles_b x cols_pad: sums over the tile's queries, or null
     float scale2;
     int32_t B, V, v0;        // v0: the piece's first point
@@ -447,8 +513,7 @@ __device__ inline bf16_t part_of(float v, int part)
 }
 
 // Probabilities of a tile of queries and points of the piece, without the
-// labels' own entries, written through LDS as rows of queries (p) and rows of
-// points (pt).
+// labels' own entries, written through LDS as rows of queries.
 template <class S, int PARTS>
 __global__ __launch_bounds__(S::THREADS) void prob_kernel(ProbArgs a)
 {
@@ -459,7 +524,7 @@ __global__ __launch_bounds__(S::THREADS) void prob_kernel(ProbArgs a)
     const int wm = wave % S::WM, wn = wave / S::WM;
     f32x16 acc[S::TM][S::TN];
     clear<S>(acc);
-    tile_product<S>(a.pr, tb * S::BM, tv * S::BN, lds, acc, 0, a.pr.K);
+    tile_product<S, false, false>(a.pr, tb * S::BM, tv * S::BN, lds, acc, 0, a.pr.K);
     float off[S::TN];
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) {
@@ -530,32 +595,11 @@ __global__ __launch_bounds__(S::THREADS) void prob_kernel(ProbArgs a)
             }
             __syncthreads();
         }
-        if (a.pt) {
-            constexpr int LD = S::BM + 8;
-#pragma unroll
-            for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-                for (int j = 0; j < S::TN; ++j)
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        bf16x4 four;
-#pragma unroll
-                        for (int f = 0; f < 4; ++f) four[f] = part_of<PARTS>(acc[i][j][e + f], part);
-                        *(bf16x4 *)(lds + ((wn * S::TN + j) * 32 + r) * LD + (wm * S::TM + i) * 32 + tile_row(e, half)) = four;
-                    }
-            __syncthreads();
-            bf16_t *to = a.pt + ((int64_t)part * a.cols_pad + tv * S::BN) * a.rows_pad + tb * S::BM;
-            for (int c = threadIdx.x; c < S::BN * (S::BM / 8); c += S::THREADS) {
-                const int row = c / (S::BM / 8), col = c % (S::BM / 8) * 8;
-                *(bf16x8 *)(to + (int64_t)row * a.rows_pad + col) = *(const bf16x8 *)(lds + row * LD + col);
-            }
-            __syncthreads();
-        }
     }
 }
 
 struct DhArgs {
-    Product pr;              // a: probabilities, b: the piece's points across
+    Product pr;              // a: probabilities, b: the piece's points, across
     float *part;             // splits x rows_pad x d
     int32_t d, rows_pad, tiles_b, tiles_d, splits, k_split, first;
 };
@@ -574,7 +618,7 @@ __global__ __launch_bounds__(S::THREADS) void dh_kernel(DhArgs a)
     const int32_t k0 = split * a.k_split, K = min(a.k_split, a.pr.K - k0);
     f32x16 acc[S::TM][S::TN];
     clear<S>(acc);
-    if (K > 0) tile_product<S>(a.pr, tb * S::BM, td * S::BN, lds, acc, k0, K);
+    if (K > 0) tile_product<S, false, true>(a.pr, tb * S::BM, td * S::BN, lds, acc, k0, K);
 #pragma unroll
     for (int i = 0; i < S::TM; ++i)
 #pragma unroll
@@ -591,7 +635,7 @@ __global__ __launch_bounds__(S::THREADS) void dh_kernel(DhArgs a)
 }
 
 struct DcArgs {
-    Product pr;              // a: probabilities across, b: the queries across
+    Product pr;              // a: probabilities, b: the queries, both across
     void *out;               // of the piece
     const int32_t *first;    // V: the first query of a point, or -1
     const float *own;        // B x d: the labels' own terms, by first query
@@ -610,7 +654,7 @@ __global__ __launch_bounds__(S::THREADS) void dc_kernel(DcArgs a)
     const int wm = wave % S::WM, wn = wave / S::WM;
     f32x16 acc[S::TM][S::TN];
     clear<S>(acc);
-    tile_product<S>(a.pr, tv * S::BM, td * S::BN, lds, acc, 0, a.pr.K);
+    tile_product<S, true, true>(a.pr, tv * S::BM, td * S::BN, lds, acc, 0, a.pr.K);
     const float by = a.scale * *a.factor;
 #pragma unroll
     for (int i = 0; i < S::TM; ++i)
@@ -791,6 +835,15 @@ struct SweepArgs {
     float scale;
 };
 
+// The order of a row's chunks in LDS is chunk ^ sweep_swap(row): eight rows at
+// one chunk (the first product) and four chunks of four rows (the second's
+// transposed reads) both spread over all banks.
+template <int CH>
+__device__ constexpr int sweep_swap(int row)
+{
+    return CH == 16 ? ((row & 3) << 2) | ((row >> 2) & 3) : CH == 8 ? (row >> 1 & 1) << 2 | ((row >> 2) & 3) : (row >> 2) & 3;
+}
+
 typedef __attribute__((address_space(3))) bf16x8 LdsRow;
 typedef __attribute__((address_space(3))) short4v LdsFour;
 
@@ -850,7 +903,7 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
 
     // streamed rows: thread t's slots are rows t / CH + i * (256 / CH), stored chunk t % CH
     constexpr int PER = SWEEP_THREADS / S::CH, ITS = (S::SR + PER - 1) / PER;
-    const int slot_row = t / S::CH, slot_chunk = (t % S::CH) ^ (slot_row & (S::CH - 1));
+    const int slot_row = t / S::CH, slot_chunk = (t % S::CH) ^ sweep_swap<S::CH>(slot_row);
     // a chunk past the values present meets zeros on the other side: any finite value of the row will do
     const int slot_at = slot_chunk * 8 < a.Kp ? slot_chunk * 8 : 0;
     auto dma = [&](int buf, int32_t stage) {
@@ -901,7 +954,7 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
 #pragma unroll
             for (int i = 0; i < DT; ++i) {
                 const int q = (t & 7) + 8 * i;
-                uint8_t *to = smem + buf * S::STAGE + row * S::ROWB + (((q >> 1) ^ (row & (S::CH - 1))) * 16) + (q & 1) * 8;
+                uint8_t *to = smem + buf * S::STAGE + row * S::ROWB + (((q >> 1) ^ sweep_swap<S::CH>(row)) * 16) + (q & 1) * 8;
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p) {
                     bf16x4 four;
@@ -936,8 +989,8 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
     // lane's place in transposed reads: group g of 16 lanes takes values 16 (g & 1).. of rows 4 half..
     const int tr_row = ((lane & 15) >> 2) + 4 * half, tr_chunk = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
-    const uint32_t s_lane = r * S::ROWB + ((half ^ (r & (S::CH - 1))) * 16);
-    const uint32_t t_lane = tr_row * S::ROWB + ((tr_chunk ^ (tr_row & (S::CH - 1))) * 16) + (lane & 1) * 8;
+    const uint32_t s_lane = r * S::ROWB + ((half ^ sweep_swap<S::CH>(r)) * 16);
+    const uint32_t t_lane = tr_row * S::ROWB + ((tr_chunk ^ sweep_swap<S::CH>(tr_row)) * 16) + (lane & 1) * 8;
 
     if (s_begin < s_end) {
         dma(0, s_begin);
@@ -1082,7 +1135,7 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
 #pragma unroll
                             for (int jj = 0; jj < 2; ++jj) {
                                 // of chunk i * 4 + tr_chunk of row 16 kb + 8 jj + tr_row
-                                const uint32_t at = (t_at ^ ((i * 64) ^ (jj * 128 & (S::CH - 1) * 16)))
+                                const uint32_t at = (t_at ^ ((i * 64) ^ (jj * 32)))
                                                     + p * S::PLANE + (16 * kb + 8 * jj) * S::ROWB;
                                 const short4v four = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsFour *)(uintptr_t)at);
                                 const bf16x4 v = __builtin_bit_cast(bf16x4, four);
@@ -1270,9 +1323,10 @@ struct Plan {
     int32_t splits, shares, per_split;               // of the statistics
     int32_t c_splits, c_per_split, c_tiles;          // sweep: of the points' gradient
     int64_t Vc, cols_pad;      // points per piece, and its padded size
-    int32_t dh_splits, dh_k;
-    int64_t off_h, off_ht, off_c, off_ct, off_part, off_loss, off_top, off_rowf, off_coef, off_label, off_pick, off_factor;
-    int64_t off_p, off_pt, off_col, off_dh, off_first, off_own, off_ownb, off_bias, off_hz, off_dc, total;
+    int64_t copied;            // points that are held as parts at a time
+    int32_t dh_splits, dh_k, tile_d, tiles_d;
+    int64_t off_h, off_c, off_part, off_loss, off_top, off_rowf, off_coef, off_label, off_pick, off_factor;
+    int64_t off_p, off_col, off_dh, off_first, off_own, off_ownb, off_bias, off_hz, off_dc, total;
 };
 
 // Whether the tiles can be read where the points are: bfloat16 rows of whole
@@ -1335,31 +1389,32 @@ Plan make_plan(const boa_xent *x, bool grad)
         const int64_t tiles_v = ceil_div(x->V, 256);
         // the losses' splits: a block per CU (its stages fill LDS), and no more than there are tiles
         p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles_v, 256 / p.tiles_b));
-        // a piece's probabilities: 128 MB in each order, half of the last-level cache
+        // a piece's probabilities: 128 MB, half of the last-level cache
         const int64_t per = (int64_t)p.rows_pad * 2 * p.parts;
-        int64_t vc = std::max<int64_t>(1024, ((int64_t)128 << 20) / per / 1024 * 1024);
-        if (!p.direct)   // and its copied points
-            vc = std::min(vc, std::max<int64_t>(1024, ((int64_t)128 << 20) / ((int64_t)p.Kp * 2 * p.parts) / 1024 * 1024));
+        const int64_t vc = std::max<int64_t>(1024, ((int64_t)128 << 20) / per / 1024 * 1024);
         p.Vc = std::min(vc, round_up(x->V, 256));
-        p.cols_pad = round_up(p.Vc, 256);
-        // a piece's tiles are split like all of them where there are several pieces
-        p.shares = p.splits * (int32_t)ceil_div(x->V, p.Vc);
+        p.cols_pad = p.Vc;
+        // points as parts: all of them up to 2 GB, so that one copy serves both
+        // passes, else a piece at a time
+        const int64_t point = (int64_t)p.Kp * 2 * p.parts;
+        p.copied = x->V * point <= (int64_t)2 << 30 ? x->V : p.Vc;
+        if (p.direct) p.copied = 0;
+        const int64_t pieces = p.direct || p.copied >= x->V ? 1 : ceil_div(x->V, p.Vc);
+        p.shares = p.splits * (int32_t)pieces;   // a piece's tiles are split like all of them
         p.off_h = take((int64_t)p.parts * p.rows_pad * p.Kp * 2);
-        if (!p.direct) p.off_c = take((int64_t)p.parts * p.cols_pad * p.Kp * 2);
+        p.off_c = take(p.copied * point);
+        // columns of the gradients' products: 256, or 128 where that leaves 15% less past the end
+        p.tile_d = round_up(x->d, 256) * 100 > round_up(x->d, 128) * 115 ? 128 : 256;
+        p.tiles_d = (int32_t)ceil_div(x->d, p.tile_d);
         if (dh) {
-            const int32_t tile_d = x->d <= 32 ? 32 : x->d <= 128 ? 128 : 256;
-            const int64_t tiles = p.tiles_b * ceil_div(x->d, tile_d);
+            const int64_t tiles = (int64_t)p.tiles_b * p.tiles_d;
             const int64_t want = std::max<int64_t>(1, 512 / tiles);
             p.dh_k = (int32_t)round_up(ceil_div(p.cols_pad, std::min(want, ceil_div(p.cols_pad, 256))), 64);
             p.dh_splits = (int32_t)ceil_div(p.cols_pad, p.dh_k);
-            p.off_p = take(per * p.cols_pad);
-            p.off_ct = take((int64_t)p.parts * x->d * p.cols_pad * 2);
             p.off_dh = take((int64_t)p.dh_splits * p.rows_pad * x->d * 4);
         }
-        if (dc) {
-            p.off_pt = take(per * p.cols_pad);
-            p.off_ht = take((int64_t)p.parts * x->d * p.rows_pad * 2);
-        }
+        if (dh || dc) p.off_p = take(per * p.cols_pad);
+        if (dc || db) p.off_hz = take((int64_t)p.parts * p.rows_pad * p.Kp * 2);
         if (db) p.off_col = take((int64_t)p.tiles_b * p.cols_pad * 4);
     }
     p.off_part = take((int64_t)p.shares * x->B * sizeof(RowState));
@@ -1399,7 +1454,7 @@ void set_segments(Product &pr, int32_t parts, int64_t part_a, int64_t part_b)
 template <class S>
 constexpr size_t stage_bytes()
 {
-    return 2 * S::STAGE * sizeof(bf16_t);
+    return STAGES * S::STAGE * sizeof(bf16_t);
 }
 
 template <class K, class A>
@@ -1424,11 +1479,9 @@ template <> struct Pick<256, 256> { using S = Shape<2, 4, 4, 2>; };
 template <> struct Pick<256, 128> { using S = Shape<4, 2, 2, 2>; };
 template <> struct Pick<128, 256> { using S = Shape<2, 4, 2, 2>; };
 template <> struct Pick<128, 128> { using S = Shape<2, 4, 2, 1>; };
-template <> struct Pick<256, 32> { using S = Shape<8, 1, 1, 1>; };
-template <> struct Pick<32, 256> { using S = Shape<1, 8, 1, 1>; };
-template <> struct Pick<128, 32> { using S = Shape<4, 1, 1, 1>; };
-template <> struct Pick<32, 128> { using S = Shape<1, 4, 1, 1>; };
-template <> struct Pick<32, 32> { using S = Shape<1, 1, 1, 1>; };
+template <> struct Pick<256, 32> { using S = Shape<2, 1, 4, 1>; };
+template <> struct Pick<32, 256> { using S = Shape<1, 2, 1, 4>; };
+template <> struct Pick<32, 128> { using S = Shape<1, 2, 1, 2>; };
 
 int check(const boa_xent *x, bool grad)
 {
@@ -1463,14 +1516,13 @@ struct Work {
     bool want_c() const { return grad && (x->dpoints || x->dbias); }
 
     // queries as parts, and their labels
-    void queries(int32_t ld, bf16_t *kept, bf16_t *across) const
+    void queries(int32_t ld, bf16_t *kept) const
     {
         PartsArgs a{};
         a.src = x->h, a.stride = x->h_stride, a.R = (int32_t)x->B, a.C = x->d, a.rows_pad = p.rows_pad;
         a.plain = at<bf16_t>(p.off_h), a.plain_ld = ld, a.plain_part = (int64_t)p.rows_pad * ld, a.kept = kept;
-        a.across = across, a.across_ld = p.rows_pad, a.across_part = (int64_t)x->d * p.rows_pad;
         a.labels = x->labels, a.V = (int32_t)x->V, a.label = at<int32_t>(p.off_label);
-        parts_kernel<T><<<dim3((uint32_t)ceil_div(p.rows_pad, 64), (uint32_t)ceil_div(ld, 64)), 256, 0, st>>>(a);
+        launch_parts<T>(a, st);
     }
 
     // after the statistics: losses, and what the gradients need of each query
@@ -1539,7 +1591,7 @@ int run_sweeps(const Work<T> &w)
     float *bias = w.template at<float>(p.off_bias);
     const int32_t v_pad = (int32_t)round_up(V, 128);
 
-    w.queries(p.ld, hz, nullptr);
+    w.queries(p.ld, hz);
     points_kernel<<<dim3((uint32_t)std::min<int64_t>(1024, ceil_div(v_pad, 256))), 256, 0, st>>>(x->bias, V, v_pad, bias, first);
     SweepArgs c{};   // the points' side of the arguments
     if constexpr (sizeof(T) == 4) {
@@ -1552,7 +1604,7 @@ int run_sweeps(const Work<T> &w)
         PartsArgs a{};
         a.src = x->points, a.stride = x->points_stride, a.R = V, a.C = d, a.rows_pad = V;
         a.plain = w.template at<bf16_t>(p.off_c), a.plain_ld = p.ld;
-        parts_kernel<T><<<dim3((uint32_t)ceil_div(V, 64), (uint32_t)ceil_div(p.ld, 64)), 256, 0, st>>>(a);
+        launch_parts<T>(a, st);
         c.m = a.plain, c.m_ld = p.ld, c.Kp = p.ld;
     }
     SweepArgs a = c;
@@ -1610,40 +1662,38 @@ int run_tiles(const Work<T> &w)
     uint8_t *ws = w.ws;
     hipStream_t st = w.st;
     const int32_t B = (int32_t)x->B, V = (int32_t)x->V, d = x->d;
-    bf16_t *hp = (bf16_t *)(ws + p.off_h), *ht = grad && x->dpoints ? (bf16_t *)(ws + p.off_ht) : nullptr;
+    bf16_t *hp = (bf16_t *)(ws + p.off_h), *hz = w.want_c() ? (bf16_t *)(ws + p.off_hz) : nullptr;
     float *factor = (float *)(ws + p.off_factor);
-    const int64_t h_part = (int64_t)p.rows_pad * p.Kp, ht_part = (int64_t)d * p.rows_pad;
-    w.queries(p.Kp, nullptr, ht);
+    const int64_t h_part = (int64_t)p.rows_pad * p.Kp, c_part = p.copied * p.Kp;
+    w.queries(p.Kp, hz);
 
     const int32_t pieces = (int32_t)ceil_div(V, p.Vc);
-    auto points_of = [&](int64_t v0, int32_t n, bool across) {
-        Operand o{};
-        bf16_t *cp = p.direct ? nullptr : (bf16_t *)(ws + p.off_c);
-        bf16_t *ct = across ? (bf16_t *)(ws + p.off_ct) : nullptr;
-        if (cp || ct) {
+    const bool whole = p.copied >= V;   // the points' copy serves both passes
+    auto points_of = [&](int64_t v0, int32_t n, bool again) {
+        if (p.direct)
+            return Operand{(const bf16_t *)x->points + v0 * x->points_stride, x->points_stride, n, p.Kp};
+        bf16_t *copy = (bf16_t *)(ws + p.off_c);
+        if (!(whole && again)) {
             PartsArgs a{};
             a.src = (const T *)x->points + v0 * x->points_stride, a.stride = x->points_stride;
-            a.R = n, a.C = d, a.rows_pad = (int32_t)p.cols_pad, a.plain = cp, a.plain_ld = p.Kp, a.plain_part = p.cols_pad * p.Kp;
-            a.across = ct, a.across_ld = p.cols_pad, a.across_part = (int64_t)d * p.cols_pad;
-            parts_kernel<T><<<dim3((uint32_t)(p.cols_pad / 64), (uint32_t)ceil_div(p.Kp, 64)), 256, 0, st>>>(a);
+            a.R = a.rows_pad = n, a.C = d, a.plain_ld = p.Kp, a.plain_part = c_part;
+            a.plain = copy + (whole ? v0 * p.Kp : 0);
+            launch_parts<T>(a, st);
         }
-        o.p = cp ? cp : (const bf16_t *)x->points + v0 * x->points_stride;
-        o.ld = cp ? p.Kp : x->points_stride;
-        o.rows = cp ? (int32_t)p.cols_pad : n;
-        return o;
+        return Operand{copy + (whole ? v0 * p.Kp : 0), p.Kp, n, p.Kp};
     };
 
     // losses: all points at once where they are read in place, else by pieces
     {
-        const int32_t step = p.direct ? V : (int32_t)p.Vc;
+        const int32_t step = p.direct || whole ? V : (int32_t)p.Vc;
         int32_t used = 0;
         for (int64_t v0 = 0; v0 < V; v0 += step) {
             const int32_t n = (int32_t)std::min<int64_t>(step, V - v0);
             StatsArgs a{};
             a.pr.a = points_of(v0, n, false);
-            a.pr.b = Operand{hp, p.Kp, p.rows_pad};
+            a.pr.b = Operand{hp, p.Kp, p.rows_pad, p.Kp};
             a.pr.K = p.Kp;
-            set_segments(a.pr, p.parts, p.cols_pad * p.Kp, h_part);
+            set_segments(a.pr, p.parts, c_part, h_part);
             a.bias = x->bias ? x->bias + v0 : nullptr;
             a.scale2 = x->scale * LOG2E;
             a.label = (const int32_t *)(ws + p.off_label), a.pick = (float *)(ws + p.off_pick);
@@ -1677,21 +1727,20 @@ int run_tiles(const Work<T> &w)
         const int32_t v0 = (int32_t)(i * p.Vc), n = (int32_t)std::min<int64_t>(p.Vc, V - v0);
         const int32_t tiles_v = (int32_t)ceil_div(n, 256);
         ProbArgs a{};
-        a.pr.a = Operand{hp, p.Kp, p.rows_pad};
-        a.pr.b = points_of(v0, n, x->dh != nullptr);
+        a.pr.a = Operand{hp, p.Kp, p.rows_pad, p.Kp};
+        a.pr.b = points_of(v0, n, true);
         a.pr.K = p.Kp;
-        set_segments(a.pr, p.parts, h_part, p.cols_pad * p.Kp);
+        set_segments(a.pr, p.parts, h_part, c_part);
         a.bias = x->bias ? x->bias + v0 : nullptr;
         a.top = (const float *)(ws + p.off_top), a.rowf = (const float *)(ws + p.off_rowf), a.label = label;
-        a.p = x->dh ? (bf16_t *)(ws + p.off_p) : nullptr;
-        a.pt = x->dpoints ? (bf16_t *)(ws + p.off_pt) : nullptr;
+        a.p = x->dh || x->dpoints ? (bf16_t *)(ws + p.off_p) : nullptr;
         a.col = x->dbias ? (float *)(ws + p.off_col) : nullptr;
         a.scale2 = x->scale * LOG2E;
         a.B = B, a.V = V, a.v0 = v0, a.n = n, a.cols_pad = (int32_t)p.cols_pad, a.rows_pad = p.rows_pad;
         a.tiles_b = p.tiles_b, a.tiles_v = tiles_v;
         with_tile(p.tile_b, [&](auto bm) {
             using S = typename Pick<decltype(bm)::value, 256>::S;
-            const size_t lds = std::max(stage_bytes<S>(), sizeof(bf16_t) * std::max<size_t>(S::BM * (S::BN + 8), S::BN * (S::BM + 8)));
+            const size_t lds = std::max(stage_bytes<S>(), sizeof(bf16_t) * (size_t)S::BM * (S::BN + 8));
             if (p.parts == 1) run(prob_kernel<S, 1>, split_grid(tiles_v, p.tiles_b), S::THREADS, lds, st, a);
             else run(prob_kernel<S, 3>, split_grid(tiles_v, p.tiles_b), S::THREADS, lds, st, a);
         });
@@ -1700,34 +1749,42 @@ int run_tiles(const Work<T> &w)
                                                                           own_bias, factor, x->dbias + v0);
         if (x->dh) {
             DhArgs g{};
-            g.pr.a = Operand{a.p, p.cols_pad, p.rows_pad};
-            g.pr.b = Operand{(const bf16_t *)(ws + p.off_ct), p.cols_pad, d};
+            g.pr.a = Operand{a.p, p.cols_pad, p.rows_pad, (int32_t)p.cols_pad};
+            g.pr.b = a.pr.b;
             g.pr.K = tiles_v * 256;
-            set_segments(g.pr, p.parts, p_part, (int64_t)d * p.cols_pad);
+            set_segments(g.pr, p.parts, p_part, c_part);
             g.part = (float *)(ws + p.off_dh);
             g.d = d, g.rows_pad = p.rows_pad, g.tiles_b = p.tiles_b, g.splits = p.dh_splits, g.k_split = p.dh_k, g.first = i == 0;
+            g.tiles_d = p.tiles_d;
             with_tile(p.tile_b, [&](auto bm) {
-                with_tile(d, [&](auto bn) {
-                    using S = typename Pick<decltype(bm)::value, decltype(bn)::value>::S;
-                    g.tiles_d = (int32_t)ceil_div(d, S::BN);
-                    run(dh_kernel<S>, split_grid(g.splits, g.tiles_b * g.tiles_d), S::THREADS, stage_bytes<S>(), st, g);
-                });
+                constexpr int BM = decltype(bm)::value;
+                const uint32_t grid = split_grid(g.splits, g.tiles_b * g.tiles_d);
+                if (p.tile_d == 128) {
+                    using S = typename Pick<BM, 128>::S;
+                    run(dh_kernel<S>, grid, S::THREADS, stage_bytes<S>(), st, g);
+                } else {
+                    using S = typename Pick<BM, 256>::S;
+                    run(dh_kernel<S>, grid, S::THREADS, stage_bytes<S>(), st, g);
+                }
             });
         }
         if (x->dpoints) {
             DcArgs g{};
-            g.pr.a = Operand{a.pt, p.rows_pad, (int32_t)p.cols_pad};
-            g.pr.b = Operand{ht, p.rows_pad, d};
+            g.pr.a = Operand{a.p, p.cols_pad, p.rows_pad, (int32_t)p.cols_pad};
+            g.pr.b = Operand{hz, p.Kp, p.rows_pad, p.Kp};
             g.pr.K = p.rows_pad;
-            set_segments(g.pr, p.parts, p_part, ht_part);
+            set_segments(g.pr, p.parts, p_part, h_part);
             g.out = (T *)x->dpoints + (int64_t)v0 * d;
             g.first = first, g.own = own, g.factor = factor, g.scale = x->scale;
-            g.n = n, g.d = d, g.v0 = v0, g.tiles_v = tiles_v;
-            with_tile(d, [&](auto bn) {
-                using S = typename Pick<256, decltype(bn)::value>::S;
-                g.tiles_d = (int32_t)ceil_div(d, S::BN);
-                run(dc_kernel<S, T>, split_grid(tiles_v, g.tiles_d), S::THREADS, stage_bytes<S>(), st, g);
-            });
+            g.n = n, g.d = d, g.v0 = v0, g.tiles_v = tiles_v, g.tiles_d = p.tiles_d;
+            const uint32_t grid = split_grid(tiles_v, g.tiles_d);
+            if (p.tile_d == 128) {
+                using S = Pick<256, 128>::S;
+                run(dc_kernel<S, T>, grid, S::THREADS, stage_bytes<S>(), st, g);
+            } else {
+                using S = Pick<256, 256>::S;
+                run(dc_kernel<S, T>, grid, S::THREADS, stage_bytes<S>(), st, g);
+            }
         }
     }
     if (x->dh)
