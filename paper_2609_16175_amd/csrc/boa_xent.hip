@@ -33,6 +33,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short short4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) bf16x8 LdsRow;
+typedef __attribute__((address_space(3))) short4v LdsFour;
 
 __device__ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -40,9 +42,6 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 // running maximum of nothing: exp2(-inf - NO_MAX) is 0 and not NaN, and logits at the type's lowest value still count
 constexpr float NO_MAX = -__FLT_MAX__;
-constexpr int BK = 32;               // values of k per stage of tile_product
-constexpr int STAGES = 4;            // of them in LDS
-constexpr int MAX_SEG = 6;
 
 // One operand of a product: bf16 rows `ld` values apart, which run along k or,
 // `across`, along the operand's own dimension (a row is then one k). Rows past
@@ -54,21 +53,28 @@ struct Operand {
     int32_t rows, cols;
 };
 
-// A product over segments of k: K values (a multiple of 16) of the parts
-// seg_a[i] and seg_b[i] (offsets in values), i < segs.
+// A product of K values (a multiple of 16). With parts, the operands' parts
+// are part_a and part_b values apart.
 struct Product {
     Operand a, b;
-    int32_t K, segs;
-    int64_t seg_a[MAX_SEG], seg_b[MAX_SEG];
+    int32_t K;
+    int64_t part_a, part_b;
 };
 
-template <int WM_, int WN_, int TM_, int TN_>
+// A block's tile: WM x WN waves of TM x TN tiles of 32 x 32. A stage of k in
+// LDS is 32 values of k, or 16 of each of three parts. Blocks of four waves or
+// fewer leave room for a second one on the CU.
+template <int WM_, int WN_, int TM_, int TN_, int PARTS_>
 struct Shape {
-    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_;
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, PARTS = PARTS_;
     static constexpr int BM = WM * TM * 32, BN = WN * TN * 32, THREADS = 64 * WM * WN;
-    static constexpr int STAGE = (BM + BN) * BK;   // bf16 values of one stage
-    static constexpr int NA = BM * 4 / THREADS, NB = BN * 4 / THREADS;   // 16-byte loads of a thread and stage
-    static_assert(NA * THREADS == BM * 4 && NB * THREADS == BN * 4, "every wave loads the same");
+    static constexpr int BK = PARTS == 1 ? 32 : 16;
+    static constexpr int STAGE = (BM + BN) * BK * PARTS;   // bf16 values
+    static constexpr int ROOM = (THREADS == 512 ? 150 : 75) * 1024 / (STAGE * 2);
+    static constexpr int STAGES = ROOM > 4 ? 4 : ROOM;
+    static constexpr int LOADS = (BM + BN) * (BK / 8) / THREADS * PARTS;   // 16-byte loads of a thread and stage
+    static_assert(BM * (BK / 8) % THREADS == 0 && BN * (BK / 8) % THREADS == 0, "every wave loads the same");
+    static_assert(STAGES >= 2, "two stages at least");
 };
 
 // Waits until at most `left` of this wave's loads are on their way and its LDS
@@ -82,127 +88,158 @@ __device__ inline void wait_and_meet()
 // One operand's side of tile_product: where this thread's loads come from and
 // where its fragments lie. ROWS of the operand's own dimension.
 //
-// Along k, a stage holds ROWS rows of 64 bytes whose 16-byte chunks are stored
-// in the order chunk ^ (row / 4 & 3); across, 32 rows of ROWS values in the
-// order chunk ^ (row & 3) * 4, and fragments are read transposed, 64 bytes of
-// four rows by half a wave. Either way what lanes read together spreads over
-// the banks.
-// The permutation is applied to the addresses loaded from, since a load to LDS
-// writes its lanes in order.
+// Along k, a stage holds ROWS rows of BK values whose 16-byte chunks are
+// stored in the order chunk ^ (row / 4 & 3), or of two chunks chunk ^ (row / 8
+// & 1); across, BK rows of ROWS values in the order chunk ^ (row & 3) * 4, and
+// fragments are read transposed, 64 bytes of four rows by half a wave. Either
+// way what lanes read together spreads over the banks. The permutation is
+// applied to the addresses loaded from, since a load to LDS writes its lanes
+// in order.
 template <class S, int ROWS, bool ACROSS>
 struct Side {
-    static constexpr int N = ROWS * 4 / S::THREADS;
-    static constexpr int PER = ACROSS ? S::THREADS / (ROWS / 8) : S::THREADS / 4;   // LDS rows of one load of all threads
+    static constexpr int CHUNKS = ACROSS ? ROWS / 8 : S::BK / 8;      // of an LDS row
+    static constexpr int N = ROWS * (S::BK / 8) / S::THREADS;         // loads of a part
+    static constexpr int PER = S::THREADS / CHUNKS;                   // LDS rows of one load of all threads
+    static constexpr int PART = ROWS * S::BK;                         // values of a part's stage
     const bf16_t *p;
-    int64_t ld;
+    int64_t ld, part;
     int32_t row, last, at;   // this thread's first row, the last there is, value within a row (across: of the tile's first)
     int32_t cols;
     static_assert(!ACROSS || ROWS >= 128, "the permutation takes 16 chunks");
 
-    __device__ Side(const Operand &o, int32_t row0, int32_t from_k)
+    __device__ static int swap(int row) { return ACROSS ? (row & 3) * 4 : CHUNKS == 4 ? (row >> 2) & 3 : (row >> 3) & 1; }
+
+    __device__ Side(const Operand &o, int64_t part_, int32_t row0, int32_t from_k)
     {
         const int t = threadIdx.x;
-        ld = o.ld, last = o.rows - 1, cols = o.cols;
+        ld = o.ld, part = part_, last = o.rows - 1, cols = o.cols;
         if constexpr (ACROSS) {
-            row = from_k + t / (ROWS / 8);
+            row = from_k + t / CHUNKS;
             at = row0;
             p = o.p;
         } else {
-            row = row0 + (t >> 2);
-            at = ((t & 3) ^ ((t >> 4) & 3)) * 8;
+            static_assert(PER % 16 == 0 || ACROSS, "one permutation for all of a thread's loads");
+            row = row0 + t / CHUNKS;
+            at = (t % CHUNKS ^ swap(t / CHUNKS)) * 8;
             p = o.p + from_k;
         }
     }
-    // loads k [k0, k0 + BK) of a part; K: end of k
-    __device__ void load(bf16_t *to, int64_t part, int32_t k0, int32_t K) const
+    // loads k [k0, k0 + BK); K: end of k
+    __device__ void load(bf16_t *to, int32_t k0, int32_t K) const
     {
-        const int wave = threadIdx.x >> 6;
+        const int t = threadIdx.x, wave = t >> 6;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const bf16_t *from;
             if constexpr (ACROSS) {
-                const int t = threadIdx.x, chunk = (t % (ROWS / 8)) ^ (((t / (ROWS / 8) + i * PER) & 3) * 4);
-                from = p + part + (int64_t)min(row + k0 + i * PER, last) * ld + (at + chunk * 8 < cols ? at + chunk * 8 : 0);
-            } else
-                from = p + part + (int64_t)min(row + i * PER, last) * ld + (k0 + at < K ? k0 + at : 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                             (__attribute__((address_space(3))) void *)(to + (i * S::THREADS + wave * 64) * 8),
-                                             16, 0, 0);
+                const int c = at + (t % CHUNKS ^ swap(t / CHUNKS + i * PER)) * 8;
+                from = p + (int64_t)min(row + k0 + i * PER, last) * ld + (c < cols ? c : 0);
+            } else {
+                from = p + (int64_t)min(row + i * PER, last) * ld + (k0 + at < K ? k0 + at : 0);
+            }
+#pragma unroll
+            for (int q = 0; q < S::PARTS; ++q)
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void *)(from + q * part),
+                    (__attribute__((address_space(3))) void *)(to + q * PART + (i * S::THREADS + wave * 64) * 8), 16, 0, 0);
         }
     }
-    // the fragment of 32 rows from row0 (of the tile) and k step s
-    __device__ static bf16x8 fragment(const bf16_t *from, int row0, int s)
+    // where this lane's fragments begin in a stage, in bytes; row0: the wave's first row of the tile
+    __device__ static uint32_t lane_at(int row0)
     {
         const int lane = threadIdx.x & 63, half = lane >> 5, r = lane & 31;
         if constexpr (ACROSS) {
+            const int row = 8 * half + ((lane & 15) >> 2), chunk = row0 / 8 + ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
+            return row * ROWS * 2 + (chunk ^ swap(row)) * 16 + (lane & 1) * 8;
+        } else {
+            return (row0 + r) * S::BK * 2 + (half ^ swap(r)) * 16;
+        }
+    }
+    // The fragment of the wave's tile i, k step s and part q. `at`: lane_at plus
+    // the stage; tiles and steps are exclusive ors on bits that nothing carries
+    // into, so one address serves them all.
+    __device__ static bf16x8 fragment(uint32_t at, int i, int s, int q)
+    {
+        if constexpr (ACROSS) {
             bf16x8 f;
-            const int k = 8 * half + ((lane & 15) >> 2), chunk = row0 / 8 + ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
 #pragma unroll
             for (int jj = 0; jj < 2; ++jj) {
-                const int row = 16 * s + k + 4 * jj;
-                const bf16_t *a = from + row * ROWS + (chunk ^ ((row & 3) * 4)) * 8 + (lane & 1) * 4;
-                const bf16x4 v = __builtin_bit_cast(
-                    bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v *)a));
+                const uint32_t a = (at ^ (i * 64)) + q * PART * 2 + (16 * s + 4 * jj) * ROWS * 2;
+                const bf16x4 v = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsFour *)(uintptr_t)a));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) f[4 * jj + e] = v[e];
             }
             return f;
         } else {
-            return *(const bf16x8 *)(from + (row0 + r) * BK + ((s * 2 + half) ^ ((r >> 2) & 3)) * 8);
+            return *(const LdsRow *)(uintptr_t)((at ^ (s * 32)) + q * PART * 2 + i * 32 * S::BK * 2);
         }
     }
 };
 
-// acc += A[row0a ..][k] * B[row0b ..][k], k in [from_k, from_k + K), over all
-// segments. Four stages of 32 k in LDS, loads three stages ahead of the matrix
-// instructions: a stage is about 1000 cycles of them, and memory answers
-// within three. ACROSS_A, ACROSS_B: the operand's rows are k.
+// acc += A[row0a ..][k] * B[row0b ..][k], k in [from_k, from_k + K). Loads run
+// STAGES - 1 stages ahead of the matrix instructions (a stage of 256 x 256 is
+// 1000 cycles of them, 3000 with parts). Of parts, the six products above
+// 2^-24 of the result are added, smallest first. ACROSS_A, ACROSS_B: the
+// operand's rows are k.
 template <class S, bool ACROSS_A, bool ACROSS_B>
 __device__ inline void tile_product(const Product &pr, int32_t row0a, int32_t row0b, bf16_t *lds,
                                     f32x16 (&acc)[S::TM][S::TN], int32_t from_k, int32_t K)
 {
+    constexpr int STAGES = S::STAGES, BK = S::BK;
     const int wave = threadIdx.x >> 6, wm = wave % S::WM, wn = wave / S::WM;
-    const Side<S, S::BM, ACROSS_A> a(pr.a, row0a, from_k);
-    const Side<S, S::BN, ACROSS_B> b(pr.b, row0b, from_k);
-    const int per_seg = (K + BK - 1) / BK, total = per_seg * pr.segs;
-    int seg = 0, k_load = 0;
-    auto load = [&](int stage) {   // past the end, what is loaded is not used
-        bf16_t *to = lds + stage * S::STAGE;
-        a.load(to, pr.seg_a[seg], k_load, K);
-        b.load(to + S::BM * BK, pr.seg_b[seg], k_load, K);
-        k_load += BK;
-        if (k_load >= K && seg + 1 < pr.segs) {
-            k_load = 0;
-            ++seg;
-        } else if (k_load >= K) {
-            k_load -= BK;
-        }
+    using A = Side<S, S::BM, ACROSS_A>;
+    using B = Side<S, S::BN, ACROSS_B>;
+    const A a(pr.a, pr.part_a, row0a, from_k);
+    const B b(pr.b, pr.part_b, row0b, from_k);
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) bf16_t *)lds;
+    const uint32_t lane_a = A::lane_at(wm * S::TM * 32), lane_b = B::lane_at(wn * S::TN * 32);
+    const int total = (K + BK - 1) / BK;
+    auto load = [&](int it) {   // past the end, the last stage again: it is not used
+        bf16_t *to = lds + it % STAGES * S::STAGE;
+        const int k0 = min(it, total - 1) * BK;
+        a.load(to, k0, K);
+        b.load(to + S::BM * BK * S::PARTS, k0, K);
     };
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) load(i);
-    int k0 = 0;
-    for (int it = 0; it < total; ++it) {
-        wait_and_meet<(STAGES - 2) * (S::NA + S::NB)>();
-        load((it + STAGES - 1) % STAGES);
-        const int steps = min(BK, K - k0) >> 4;
-        k0 = k0 + BK < K ? k0 + BK : 0;
-        const bf16_t *from = lds + (it % STAGES) * S::STAGE;
+    auto step = [&](int it, auto steps) {
+        wait_and_meet<(STAGES - 2) * S::LOADS>();
+        load(it + STAGES - 1);
+        const uint32_t stage = base + it % STAGES * S::STAGE * 2;
+        const uint32_t at_a = stage + lane_a, at_b = stage + S::BM * BK * S::PARTS * 2 + lane_b;
 #pragma unroll
-        for (int s = 0; s < BK / 16; ++s) {
-            if (s < steps) {
-                bf16x8 fa[S::TM], fb[S::TN];
+        for (int s = 0; s < decltype(steps)::value; ++s) {
+            constexpr int PAIRS = S::PARTS == 1 ? 1 : 6, QA = S::PARTS - 1;
+            constexpr int qa[6] = {QA, QA / 2, 0, QA / 2, 0, 0}, qb[6] = {0, 1, 2, 0, 1, 0};
+            // with parts, a row of tiles at a time: all fragments at once do not fit the registers
+            constexpr int ROW = S::PARTS == 1 ? S::TM : S::TM > 2 ? 2 : 1;
+            bf16x8 fb[S::PARTS][S::TN];
 #pragma unroll
-                for (int i = 0; i < S::TM; ++i) fa[i] = a.fragment(from, (wm * S::TM + i) * 32, s);
+            for (int q = 0; q < S::PARTS; ++q)
 #pragma unroll
-                for (int j = 0; j < S::TN; ++j) fb[j] = b.fragment(from + S::BM * BK, (wn * S::TN + j) * 32, s);
+                for (int j = 0; j < S::TN; ++j) fb[q][j] = B::fragment(at_b, j, s, q);
 #pragma unroll
-                for (int i = 0; i < S::TM; ++i)
+            for (int i0 = 0; i0 < S::TM; i0 += ROW) {
+                bf16x8 fa[S::PARTS][ROW];
 #pragma unroll
-                    for (int j = 0; j < S::TN; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+                for (int q = 0; q < S::PARTS; ++q)
+#pragma unroll
+                    for (int i = 0; i < ROW; ++i)
+                        fa[q][i] = A::fragment(at_a, i0 + i, s, q);
+#pragma unroll
+                for (int q = 0; q < PAIRS; ++q)
+#pragma unroll
+                    for (int i = 0; i < ROW; ++i)
+#pragma unroll
+                        for (int j = 0; j < S::TN; ++j)
+                            acc[i0 + i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[qa[q]][i], fb[qb[q]][j],
+                                                                                     acc[i0 + i][j], 0, 0, 0);
+                if (S::PARTS > 1) __builtin_amdgcn_sched_barrier(0);
             }
         }
-    }
+    };
+    for (int it = 0; it < K / BK; ++it) step(it, std::integral_constant<int, BK / 16>{});
+    if (K % BK) step(total - 1, std::integral_constant<int, 1>{});
     wait_and_meet<0>();
 }
 
@@ -336,9 +373,9 @@ __device__ inline void join(RowState &a, float m, float s)
 // lane's values belong to TN queries (the columns of its tiles), so the
 // running states stay in its registers until the end.
 template <class S>
-__global__ __launch_bounds__(S::THREADS) void stats_kernel(StatsArgs a)
+__global__ __launch_bounds__(S::THREADS, 2) void stats_kernel(StatsArgs a)
 {
-    extern __shared__ __attribute__((aligned(16))) bf16_t lds[];
+    extern __shared__ __attribute__((aligned(256))) bf16_t lds[];
     int32_t split, tb;
     if (!split_block(a.splits, a.tiles_b, &split, &tb)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
@@ -514,10 +551,11 @@ __device__ inline bf16_t part_of(float v, int part)
 
 // Probabilities of a tile of queries and points of the piece, without the
 // labels' own entries, written through LDS as rows of queries.
-template <class S, int PARTS>
-__global__ __launch_bounds__(S::THREADS) void prob_kernel(ProbArgs a)
+template <class S>
+__global__ __launch_bounds__(S::THREADS, 2) void prob_kernel(ProbArgs a)
 {
-    extern __shared__ __attribute__((aligned(16))) bf16_t lds[];
+    constexpr int PARTS = S::PARTS;
+    extern __shared__ __attribute__((aligned(256))) bf16_t lds[];
     int32_t tv, tb;
     if (!split_block(a.tiles_v, a.tiles_b, &tv, &tb)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, r = lane & 31;
@@ -575,26 +613,33 @@ __global__ __launch_bounds__(S::THREADS) void prob_kernel(ProbArgs a)
         }
         __syncthreads();
     }
-#pragma unroll
+    if (!a.p) return;
+    constexpr int LD = S::BN + 8;
+#pragma unroll 1
     for (int part = 0; part < PARTS; ++part) {
-        if (a.p) {
-            constexpr int LD = S::BN + 8;
 #pragma unroll
-            for (int i = 0; i < S::TM; ++i)
+        for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-                for (int j = 0; j < S::TN; ++j)
+            for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        lds[((wm * S::TM + i) * 32 + tile_row(e, half)) * LD + (wn * S::TN + j) * 32 + r]
-                            = part_of<PARTS>(acc[i][j][e], part);
-            __syncthreads();
-            bf16_t *to = a.p + ((int64_t)part * a.rows_pad + tb * S::BM) * a.cols_pad + tv * S::BN;
-            for (int c = threadIdx.x; c < S::BM * (S::BN / 8); c += S::THREADS) {
-                const int row = c / (S::BN / 8), col = c % (S::BN / 8) * 8;
-                *(bf16x8 *)(to + (int64_t)row * a.cols_pad + col) = *(const bf16x8 *)(lds + row * LD + col);
-            }
-            __syncthreads();
+                for (int e = 0; e < 16; ++e) {
+                    bf16_t one;
+                    if constexpr (PARTS == 1) {
+                        one = (bf16_t)acc[i][j][e];
+                    } else {   // the parts one after the other: what is left stays in acc
+                        const float top = __uint_as_float(__float_as_uint(acc[i][j][e]) & 0xFFFF0000u);
+                        one = (bf16_t)top;
+                        acc[i][j][e] -= top;
+                    }
+                    lds[((wm * S::TM + i) * 32 + tile_row(e, half)) * LD + (wn * S::TN + j) * 32 + r] = one;
+                }
+        __syncthreads();
+        bf16_t *to = a.p + ((int64_t)part * a.rows_pad + tb * S::BM) * a.cols_pad + tv * S::BN;
+        for (int c = threadIdx.x; c < S::BM * (S::BN / 8); c += S::THREADS) {
+            const int row = c / (S::BN / 8), col = c % (S::BN / 8) * 8;
+            *(bf16x8 *)(to + (int64_t)row * a.cols_pad + col) = *(const bf16x8 *)(lds + row * LD + col);
         }
+        __syncthreads();
     }
 }
 
@@ -607,9 +652,9 @@ struct DhArgs {
 // A split's share of sum_v p_bv c_v over the piece, added to what earlier
 // pieces left.
 template <class S>
-__global__ __launch_bounds__(S::THREADS) void dh_kernel(DhArgs a)
+__global__ __launch_bounds__(S::THREADS, 2) void dh_kernel(DhArgs a)
 {
-    extern __shared__ __attribute__((aligned(16))) bf16_t lds[];
+    extern __shared__ __attribute__((aligned(256))) bf16_t lds[];
     int32_t split, tile;
     if (!split_block(a.splits, a.tiles_b * a.tiles_d, &split, &tile)) return;
     const int32_t tb = tile / a.tiles_d, td = tile % a.tiles_d;
@@ -645,9 +690,9 @@ struct DcArgs {
 };
 
 template <class S, class T>
-__global__ __launch_bounds__(S::THREADS) void dc_kernel(DcArgs a)
+__global__ __launch_bounds__(S::THREADS, 2) void dc_kernel(DcArgs a)
 {
-    extern __shared__ __attribute__((aligned(16))) bf16_t lds[];
+    extern __shared__ __attribute__((aligned(256))) bf16_t lds[];
     int32_t tv, td;
     if (!split_block(a.tiles_v, a.tiles_d, &tv, &td)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, r = lane & 31;
@@ -843,9 +888,6 @@ __device__ constexpr int sweep_swap(int row)
 {
     return CH == 16 ? ((row & 3) << 2) | ((row >> 2) & 3) : CH == 8 ? (row >> 1 & 1) << 2 | ((row >> 2) & 3) : (row >> 2) & 3;
 }
-
-typedef __attribute__((address_space(3))) bf16x8 LdsRow;
-typedef __attribute__((address_space(3))) short4v LdsFour;
 
 template <class S>
 __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
@@ -1383,16 +1425,34 @@ Plan make_plan(const boa_xent *x, bool grad)
         }
     } else {
         p.Kp = (int32_t)round_up(x->d, 16);
-        p.tile_b = x->B <= 32 ? 32 : x->B <= 128 ? 128 : 256;
+        // rows of queries in a tile: 256, or 128 where that leaves 10% less past the end
+        p.tile_b = x->B <= 32 ? 32 : round_up(x->B, 256) * 10 > round_up(x->B, 128) * 11 ? 128 : 256;
         p.tiles_b = (int32_t)ceil_div(x->B, p.tile_b);
         p.rows_pad = p.tiles_b * p.tile_b;
         const int64_t tiles_v = ceil_div(x->V, 256);
         // the losses' splits: a block per CU (its stages fill LDS), and no more than there are tiles
-        p.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles_v, 256 / p.tiles_b));
-        // a piece's probabilities: 128 MB, half of the last-level cache
+        const int64_t resident = p.tile_b == 256 ? 256 : 512;   // blocks
+        int64_t splits = std::max<int64_t>(1, resident / p.tiles_b);
+        if (splits > 8) splits = splits / 8 * 8;   // none of the 8 XCDs with a block more
+        p.splits = (int32_t)std::min(tiles_v, splits);
+        // columns of the gradients' products: 256, or 128 where that leaves 15% less past the end
+        p.tile_d = round_up(x->d, 256) * 100 > round_up(x->d, 128) * 115 ? 128 : 256;
+        p.tiles_d = (int32_t)ceil_div(x->d, p.tile_d);
+        // A piece's probabilities take up to 256 MB. Of the numbers of pieces
+        // that do, the one whose launches fill the GPU best: each launch takes
+        // whole rounds of resident blocks.
         const int64_t per = (int64_t)p.rows_pad * 2 * p.parts;
-        const int64_t vc = std::max<int64_t>(1024, ((int64_t)128 << 20) / per / 1024 * 1024);
-        p.Vc = std::min(vc, round_up(x->V, 256));
+        const int64_t most = std::max<int64_t>(4, ((int64_t)256 << 20) / per / 256);   // tiles of points
+        const int64_t least = ceil_div(tiles_v, most);
+        int64_t best = -1, best_cost = 0;
+        for (int64_t n = least; n < least + 6; ++n) {
+            const int64_t tv = ceil_div(tiles_v, n), c_resident = p.tile_d == 256 ? 256 : 512;
+            // rounds, each worth the work of its blocks
+            const int64_t cost = n * (ceil_div(tv * p.tiles_b, resident) * resident * p.tile_b * x->d
+                                      + ceil_div(tv * p.tiles_d, c_resident) * c_resident * p.tile_d * p.rows_pad);
+            if (best < 0 || cost < best_cost) best = tv, best_cost = cost;
+        }
+        p.Vc = best * 256;
         p.cols_pad = p.Vc;
         // points as parts: all of them up to 2 GB, so that one copy serves both
         // passes, else a piece at a time
@@ -1403,12 +1463,9 @@ Plan make_plan(const boa_xent *x, bool grad)
         p.shares = p.splits * (int32_t)pieces;   // a piece's tiles are split like all of them
         p.off_h = take((int64_t)p.parts * p.rows_pad * p.Kp * 2);
         p.off_c = take(p.copied * point);
-        // columns of the gradients' products: 256, or 128 where that leaves 15% less past the end
-        p.tile_d = round_up(x->d, 256) * 100 > round_up(x->d, 128) * 115 ? 128 : 256;
-        p.tiles_d = (int32_t)ceil_div(x->d, p.tile_d);
         if (dh) {
             const int64_t tiles = (int64_t)p.tiles_b * p.tiles_d;
-            const int64_t want = std::max<int64_t>(1, 512 / tiles);
+            const int64_t want = std::max<int64_t>(1, (p.tile_b == 256 && p.tile_d == 256 ? 256 : 512) / tiles);
             p.dh_k = (int32_t)round_up(ceil_div(p.cols_pad, std::min(want, ceil_div(p.cols_pad, 256))), 64);
             p.dh_splits = (int32_t)ceil_div(p.cols_pad, p.dh_k);
             p.off_dh = take((int64_t)p.dh_splits * p.rows_pad * x->d * 4);
@@ -1434,27 +1491,10 @@ Plan make_plan(const boa_xent *x, bool grad)
     return p;
 }
 
-// The part products of one operand pair: of the nine products of three parts
-// each, the six above 2^-24 of the result, smallest first.
-void set_segments(Product &pr, int32_t parts, int64_t part_a, int64_t part_b)
-{
-    if (parts == 1) {
-        pr.segs = 1;
-        pr.seg_a[0] = pr.seg_b[0] = 0;
-        return;
-    }
-    static const int ia[6] = {2, 1, 0, 1, 0, 0}, ib[6] = {0, 1, 2, 0, 1, 0};
-    pr.segs = 6;
-    for (int i = 0; i < 6; ++i) {
-        pr.seg_a[i] = ia[i] * part_a;
-        pr.seg_b[i] = ib[i] * part_b;
-    }
-}
-
 template <class S>
 constexpr size_t stage_bytes()
 {
-    return STAGES * S::STAGE * sizeof(bf16_t);
+    return S::STAGES * S::STAGE * sizeof(bf16_t);
 }
 
 template <class K, class A>
@@ -1473,15 +1513,20 @@ void with_tile(int32_t n, F f)   // 32, 128 or 256 rows of the smaller side
     else f(std::integral_constant<int, 256>{});
 }
 
-template <int BM, int BN>
+// Waves of 128 x 64 (or 64 x 128) where a tile has room: 6 fragments for 8
+// matrix instructions, which LDS delivers in half their time.
+template <int BM, int BN, int PARTS>
 struct Pick;
-template <> struct Pick<256, 256> { using S = Shape<2, 4, 4, 2>; };
-template <> struct Pick<256, 128> { using S = Shape<4, 2, 2, 2>; };
-template <> struct Pick<128, 256> { using S = Shape<2, 4, 2, 2>; };
-template <> struct Pick<128, 128> { using S = Shape<2, 4, 2, 1>; };
-template <> struct Pick<256, 32> { using S = Shape<2, 1, 4, 1>; };
-template <> struct Pick<32, 256> { using S = Shape<1, 2, 1, 4>; };
-template <> struct Pick<32, 128> { using S = Shape<1, 2, 1, 2>; };
+template <int P> struct Pick<256, 256, P> { using S = Shape<2, 4, 4, 2, P>; };
+template <int P> struct Pick<256, 128, P> { using S = Shape<2, 2, 4, 2, P>; };
+template <int P> struct Pick<128, 256, P> { using S = Shape<2, 2, 2, 4, P>; };
+template <int P> struct Pick<128, 128, P> { using S = Shape<2, 2, 2, 2, P>; };
+template <> struct Pick<256, 32, 1> { using S = Shape<2, 1, 4, 1, 1>; };
+template <> struct Pick<32, 256, 1> { using S = Shape<1, 2, 1, 4, 1>; };
+template <> struct Pick<32, 128, 1> { using S = Shape<1, 2, 1, 2, 1>; };
+template <> struct Pick<256, 32, 3> { using S = Shape<1, 1, 8, 1, 3>; };
+template <> struct Pick<32, 256, 3> { using S = Shape<1, 1, 1, 8, 3>; };
+template <> struct Pick<32, 128, 3> { using S = Shape<1, 1, 1, 4, 3>; };
 
 int check(const boa_xent *x, bool grad)
 {
@@ -1656,6 +1701,7 @@ int run_sweeps(const Work<T> &w)
 template <class T>
 int run_tiles(const Work<T> &w)
 {
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
     const boa_xent *x = w.x;
     const Plan &p = w.p;
     const bool grad = w.grad;
@@ -1693,7 +1739,7 @@ int run_tiles(const Work<T> &w)
             a.pr.a = points_of(v0, n, false);
             a.pr.b = Operand{hp, p.Kp, p.rows_pad, p.Kp};
             a.pr.K = p.Kp;
-            set_segments(a.pr, p.parts, c_part, h_part);
+            a.pr.part_a = c_part, a.pr.part_b = h_part;
             a.bias = x->bias ? x->bias + v0 : nullptr;
             a.scale2 = x->scale * LOG2E;
             a.label = (const int32_t *)(ws + p.off_label), a.pick = (float *)(ws + p.off_pick);
@@ -1703,7 +1749,7 @@ int run_tiles(const Work<T> &w)
             a.part = (RowState *)(ws + p.off_part) + (int64_t)used * B;
             used += a.splits;
             with_tile(p.tile_b, [&](auto bn) {
-                using S = typename Pick<256, decltype(bn)::value>::S;
+                using S = typename Pick<256, decltype(bn)::value, PARTS>::S;
                 run(stats_kernel<S>, split_grid(a.splits, a.tiles_b), S::THREADS, stage_bytes<S>(), st, a);
             });
         }
@@ -1730,7 +1776,7 @@ int run_tiles(const Work<T> &w)
         a.pr.a = Operand{hp, p.Kp, p.rows_pad, p.Kp};
         a.pr.b = points_of(v0, n, true);
         a.pr.K = p.Kp;
-        set_segments(a.pr, p.parts, h_part, c_part);
+        a.pr.part_a = h_part, a.pr.part_b = c_part;
         a.bias = x->bias ? x->bias + v0 : nullptr;
         a.top = (const float *)(ws + p.off_top), a.rowf = (const float *)(ws + p.off_rowf), a.label = label;
         a.p = x->dh || x->dpoints ? (bf16_t *)(ws + p.off_p) : nullptr;
@@ -1739,10 +1785,9 @@ int run_tiles(const Work<T> &w)
         a.B = B, a.V = V, a.v0 = v0, a.n = n, a.cols_pad = (int32_t)p.cols_pad, a.rows_pad = p.rows_pad;
         a.tiles_b = p.tiles_b, a.tiles_v = tiles_v;
         with_tile(p.tile_b, [&](auto bm) {
-            using S = typename Pick<decltype(bm)::value, 256>::S;
+            using S = typename Pick<decltype(bm)::value, 256, PARTS>::S;
             const size_t lds = std::max(stage_bytes<S>(), sizeof(bf16_t) * (size_t)S::BM * (S::BN + 8));
-            if (p.parts == 1) run(prob_kernel<S, 1>, split_grid(tiles_v, p.tiles_b), S::THREADS, lds, st, a);
-            else run(prob_kernel<S, 3>, split_grid(tiles_v, p.tiles_b), S::THREADS, lds, st, a);
+            run(prob_kernel<S>, split_grid(tiles_v, p.tiles_b), S::THREADS, lds, st, a);
         });
         if (x->dbias)
             dbias_kernel<<<dim3((uint32_t)ceil_div(n, 256)), 256, 0, st>>>(a.col, p.tiles_b, (int32_t)p.cols_pad, n, v0, first,
@@ -1752,7 +1797,7 @@ int run_tiles(const Work<T> &w)
             g.pr.a = Operand{a.p, p.cols_pad, p.rows_pad, (int32_t)p.cols_pad};
             g.pr.b = a.pr.b;
             g.pr.K = tiles_v * 256;
-            set_segments(g.pr, p.parts, p_part, c_part);
+            g.pr.part_a = p_part, g.pr.part_b = c_part;
             g.part = (float *)(ws + p.off_dh);
             g.d = d, g.rows_pad = p.rows_pad, g.tiles_b = p.tiles_b, g.splits = p.dh_splits, g.k_split = p.dh_k, g.first = i == 0;
             g.tiles_d = p.tiles_d;
@@ -1760,10 +1805,10 @@ int run_tiles(const Work<T> &w)
                 constexpr int BM = decltype(bm)::value;
                 const uint32_t grid = split_grid(g.splits, g.tiles_b * g.tiles_d);
                 if (p.tile_d == 128) {
-                    using S = typename Pick<BM, 128>::S;
+                    using S = typename Pick<BM, 128, PARTS>::S;
                     run(dh_kernel<S>, grid, S::THREADS, stage_bytes<S>(), st, g);
                 } else {
-                    using S = typename Pick<BM, 256>::S;
+                    using S = typename Pick<BM, 256, PARTS>::S;
                     run(dh_kernel<S>, grid, S::THREADS, stage_bytes<S>(), st, g);
                 }
             });
@@ -1773,16 +1818,16 @@ int run_tiles(const Work<T> &w)
             g.pr.a = Operand{a.p, p.cols_pad, p.rows_pad, (int32_t)p.cols_pad};
             g.pr.b = Operand{hz, p.Kp, p.rows_pad, p.Kp};
             g.pr.K = p.rows_pad;
-            set_segments(g.pr, p.parts, p_part, h_part);
+            g.pr.part_a = p_part, g.pr.part_b = h_part;
             g.out = (T *)x->dpoints + (int64_t)v0 * d;
             g.first = first, g.own = own, g.factor = factor, g.scale = x->scale;
             g.n = n, g.d = d, g.v0 = v0, g.tiles_v = tiles_v, g.tiles_d = p.tiles_d;
             const uint32_t grid = split_grid(tiles_v, g.tiles_d);
             if (p.tile_d == 128) {
-                using S = Pick<256, 128>::S;
+                using S = typename Pick<256, 128, PARTS>::S;
                 run(dc_kernel<S, T>, grid, S::THREADS, stage_bytes<S>(), st, g);
             } else {
-                using S = Pick<256, 256>::S;
+                using S = typename Pick<256, 256, PARTS>::S;
                 run(dc_kernel<S, T>, grid, S::THREADS, stage_bytes<S>(), st, g);
             }
         }
