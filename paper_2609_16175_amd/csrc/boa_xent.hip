@@ -345,6 +345,16 @@ struct RowState {
     float m, s;   // running maximum (base 2) and sum of exponentials
 };
 
+// sum += x with what rounding loses kept in `lost` and brought in by the next
+// addition: thousands of small exponentials would vanish one by one beside a
+// large sum.
+__device__ inline void add_kept(float &sum, float &lost, float x)
+{
+    const float y = x - lost, t = sum + y;
+    lost = (t - sum) - y;
+    sum = t;
+}
+
 // A point's bias in base 2. Finite ones stay finite, masks of the type's lowest
 // value among them.
 __device__ inline float base2(float bias)
@@ -381,10 +391,12 @@ __global__ __launch_bounds__(S::THREADS, 2) void stats_kernel(StatsArgs a)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     const int wm = wave % S::WM, wn = wave / S::WM;
     RowState st[S::TN];
+    float lost[S::TN];
     int32_t lab[S::TN];
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) {
         st[j] = RowState{NO_MAX, 0.0f};
+        lost[j] = 0.0f;
         lab[j] = a.label[tb * S::BN + (wn * S::TN + j) * 32 + (lane & 31)] - a.v0;
     }
     for (int32_t tv = split; tv < a.tiles_v; tv += a.splits) {
@@ -413,10 +425,14 @@ __global__ __launch_bounds__(S::THREADS, 2) void stats_kernel(StatsArgs a)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
                         if (rel == tile_row(e, half)) a.pick[tb * S::BN + (wn * S::TN + j) * 32 + (lane & 31)] = acc[i][j][e];
-                float s = st[j].s * __builtin_amdgcn_exp2f(st[j].m - top);
+                const float by = __builtin_amdgcn_exp2f(st[j].m - top);
+                float s = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(acc[i][j][e] - top);
-                st[j] = RowState{top, s};
+                st[j].m = top;
+                st[j].s *= by;
+                lost[j] *= by;
+                add_kept(st[j].s, lost[j], s);
             }
         }
     }
@@ -850,9 +866,13 @@ struct Sweep {
     static constexpr int STAGE = (PARTS * PLANE + SIDES * SR * 4 + 255) / 256 * 256;
     static constexpr bool STAGED = PARTS == 3 && MODE != SWEEP_C;        // float32 points: split on the way to LDS
     static constexpr int OUT_LD = DT * 32 + 4;               // floats of a row of the output in LDS
+    // The kept rows' last k steps lie in LDS where the registers do not hold
+    // them all: a spilled one would be waited for together with the loads on
+    // their way to the next stage.
+    static constexpr int KS = 2 * DT, SHED = MODE != SWEEP_LOSS && PARTS * TN * DT >= 8 ? (MODE == SWEEP_H ? 2 : 1) : 0;
     static constexpr size_t lds()
     {
-        return std::max<size_t>(2 * STAGE, MODE == SWEEP_C ? 4 * 32 * OUT_LD * 4 : 0);
+        return std::max<size_t>(2 * STAGE + SHED * TN * PARTS * SWEEP_THREADS * 16, MODE == SWEEP_C ? 4 * 32 * OUT_LD * 4 : 0);
     }
 };
 
@@ -892,7 +912,7 @@ __device__ constexpr int sweep_swap(int row)
 template <class S>
 __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
 {
-    constexpr int DT = S::DT, PARTS = S::PARTS, TN = S::TN, KS = 2 * DT;
+    constexpr int DT = S::DT, PARTS = S::PARTS, TN = S::TN, KS = S::KS, KEEP = KS - S::SHED;
     extern __shared__ __attribute__((aligned(256))) uint8_t smem[];
     int32_t split, tn0;
     if (S::MODE == SWEEP_C ? !split_block(a.tiles_n, a.splits, &tn0, &split)
@@ -904,13 +924,14 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
     const int32_t s_begin = split * a.per_split, s_end = min(a.stages, s_begin + a.per_split);
 
     // the kept side
-    bf16x8 fn[PARTS][KS][TN];
+    bf16x8 fn[PARTS][KEEP][TN], *shed = (bf16x8 *)(smem + 2 * S::STAGE) + t;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const int64_t row = min(n0 + j * 32 + r, a.N - 1);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             const int at = k * 16 + half * 8;
+            bf16x8 f[PARTS];
             if constexpr (PARTS == 3 && S::MODE == SWEEP_C) {
                 float v[8];
                 const float *from = a.nf + row * a.n_ld + at;
@@ -926,19 +947,24 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float top = __uint_as_float(__float_as_uint(v[e]) & 0xFFFF0000u);
-                        fn[p][k][j][e] = (bf16_t)top;
+                        f[p][e] = (bf16_t)top;
                         v[e] = fabsf(top) < INFINITY ? v[e] - top : 0.0f;
                     }
             } else {
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p) {
                     if (at < a.Kp) {
-                        fn[p][k][j] = *(const bf16x8 *)(a.n + p * a.n_part + row * a.n_ld + at);
+                        f[p] = *(const bf16x8 *)(a.n + p * a.n_part + row * a.n_ld + at);
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) fn[p][k][j][e] = (bf16_t)0.0f;
+                        for (int e = 0; e < 8; ++e) f[p][e] = (bf16_t)0.0f;
                     }
                 }
+            }
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                if (k < KEEP) fn[p][k < KEEP ? k : 0][j] = f[p];
+                else shed[(((k - KEEP) * TN + j) * PARTS + p) * SWEEP_THREADS] = f[p];
             }
         }
     }
@@ -950,27 +976,35 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
     const int slot_at = slot_chunk * 8 < a.Kp ? slot_chunk * 8 : 0;
     auto dma = [&](int buf, int32_t stage) {
         uint8_t *to = smem + buf * S::STAGE;
-        if constexpr (!S::STAGED) {
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-                for (int i = 0; i < ITS; ++i) {
-                    if (S::SR % PER && wave * 64 >= S::SR * S::CH) continue;
-                    const int64_t row = min(stage * S::SR + i * PER + slot_row, a.M - 1);
-                    __builtin_amdgcn_global_load_lds(
-                        (const __attribute__((address_space(1))) void *)(a.m + p * a.m_part + row * a.m_ld + slot_at),
-                        (__attribute__((address_space(3))) void *)(to + p * S::PLANE + (i * SWEEP_THREADS + wave * 64) * 16),
-                        16, 0, 0);
-                }
-        }
+        uint32_t side_at = t * 4;
+        asm volatile("" : "+v"(side_at));
 #pragma unroll
         for (int k = 0; k < S::SIDES; ++k) {
             const void *side = S::MODE != SWEEP_C ? (const void *)a.bias
                              : k == 0 ? (const void *)a.top : k == 1 ? (const void *)a.rowf : (const void *)a.label;
             if (wave * 64 < S::SR && t < S::SR)
                 __builtin_amdgcn_global_load_lds(
-                    (const __attribute__((address_space(1))) void *)((const float *)side + stage * S::SR + t),
+                    (const __attribute__((address_space(1))) void *)((const uint8_t *)side + (int64_t)stage * S::SR * 4 + side_at),
                     (__attribute__((address_space(3))) void *)(to + PARTS * S::PLANE + k * S::SR * 4 + wave * 256), 4, 0, 0);
+        }
+        if constexpr (!S::STAGED) {
+            // a stage's rows lie within 32 bits of its first one (a.m_ld is below 2^24):
+            // one address for the wave and an offset per lane, made anew each time to save registers
+            const uint8_t *first = (const uint8_t *)(a.m + (int64_t)stage * S::SR * a.m_ld);
+            int32_t row0 = slot_row;
+            asm volatile("" : "+v"(row0));
+            const int32_t last = a.M - 1 - stage * S::SR;
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                for (int i = 0; i < ITS; ++i) {
+                    if (S::SR % PER && wave * 64 >= S::SR * S::CH) continue;
+                    const uint32_t at = ((uint32_t)min(i * PER + row0, last) * (uint32_t)a.m_ld + slot_at) * 2;
+                    __builtin_amdgcn_global_load_lds(
+                        (const __attribute__((address_space(1))) void *)(first + p * a.m_part * 2 + at),
+                        (__attribute__((address_space(3))) void *)(to + p * S::PLANE + (i * SWEEP_THREADS + wave * 64) * 16),
+                        16, 0, 0);
+                }
         }
     };
     // float32 points: 8 threads a row, DT * 4 values each, split into parts on the way
@@ -1013,7 +1047,7 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
     };
 
     f32x16 out[S::MODE == SWEEP_LOSS ? 1 : DT][TN];
-    float mx[TN], sum[TN], off[TN];
+    float mx[TN], sum[TN], lost[TN], off[TN];
     int32_t lab[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
@@ -1022,7 +1056,7 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
 #pragma unroll
             for (int e = 0; e < 16; ++e) out[i][j][e] = 0.0f;
         mx[j] = NO_MAX;
-        sum[j] = 0.0f;
+        sum[j] = lost[j] = 0.0f;
         const int32_t n = n0 + j * 32 + r;
         off[j] = S::MODE == SWEEP_C ? a.bias[min(n, a.N - 1)] : 0.0f;
         lab[j] = S::MODE != SWEEP_C && n < a.N ? a.label[n] : -1;
@@ -1068,14 +1102,18 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                 for (int p = 0; p < PARTS; ++p) fm[p] = *(const LdsRow *)(uintptr_t)((s_at ^ (k * 32)) + p * S::PLANE);
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
+                    bf16x8 f[PARTS];   // a thread reads back what it put there itself
+#pragma unroll
+                    for (int p = 0; p < PARTS; ++p)
+                        f[p] = k < KEEP ? fn[p][k < KEEP ? k : 0][j] : shed[(((k - KEEP) * TN + j) * PARTS + p) * SWEEP_THREADS];
                     if constexpr (PARTS == 3) {
-                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[2], fn[0][k][j], acc[j], 0, 0, 0);
-                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[1], fn[1][k][j], acc[j], 0, 0, 0);
-                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fn[2][k][j], acc[j], 0, 0, 0);
-                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[1], fn[0][k][j], acc[j], 0, 0, 0);
-                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fn[1][k][j], acc[j], 0, 0, 0);
+                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[2], f[0], acc[j], 0, 0, 0);
+                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[1], f[1], acc[j], 0, 0, 0);
+                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], f[2], acc[j], 0, 0, 0);
+                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[1], f[0], acc[j], 0, 0, 0);
+                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], f[1], acc[j], 0, 0, 0);
                     }
-                    acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], fn[0][k][j], acc[j], 0, 0, 0);
+                    acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fm[0], f[0], acc[j], 0, 0, 0);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);   // the registers are full: the phases stay apart
@@ -1103,6 +1141,7 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                         const float now = fmaxf(fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])), mx[j]);
                         const float by = __builtin_amdgcn_exp2f(mx[j] - now);
                         sum[j] *= by;
+                        lost[j] *= by;
                         if constexpr (S::MODE == SWEEP_H)
 #pragma unroll
                             for (int i = 0; i < DT; ++i)
@@ -1112,22 +1151,24 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                     }
                     const int32_t rel = lab[j] - (stage * S::SR + row0);
                     const bool mine = (uint32_t)rel < 32u;
+                    float s = 0.0f;
                     if (__any(mine)) {   // a column's own point is among these rows
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const bool here = rel == tile_row(e, half);
                             if (here) a.pick[n0 + j * 32 + r] = acc[j][e];
                             const float p = __builtin_amdgcn_exp2f(acc[j][e] - mx[j]);
-                            sum[j] += p;
+                            s += p;
                             acc[j][e] = here ? 0.0f : p;
                         }
                     } else {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             acc[j][e] = __builtin_amdgcn_exp2f(acc[j][e] - mx[j]);
-                            sum[j] += acc[j][e];
+                            s += acc[j][e];
                         }
                     }
+                    add_kept(sum[j], lost[j], s);
                 }
             } else {
 #pragma unroll
@@ -1153,9 +1194,12 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                 }
                 if (a.col || a.dbias)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j)
+                    for (int j = 0; j < TN; ++j) {
+                        float s = 0.0f;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) sum[j] += acc[j][e];
+                        for (int e = 0; e < 16; ++e) s += acc[j][e];
+                        add_kept(sum[j], lost[j], s);
+                    }
             }
             // the second product
             if constexpr (S::MODE != SWEEP_LOSS) {
@@ -1375,7 +1419,8 @@ struct Plan {
 // 16-byte chunks, an even number of them.
 bool points_direct(const boa_xent *x)
 {
-    return x->dtype == BOA_T_BF16 && x->d % 16 == 0 && aligned(x->points, 16) && x->points_stride % 8 == 0;
+    return x->dtype == BOA_T_BF16 && x->d % 16 == 0 && aligned(x->points, 16) && x->points_stride % 8 == 0
+           && x->points_stride < (1 << 24);
 }
 
 Plan make_plan(const boa_xent *x, bool grad)
