@@ -310,8 +310,8 @@ const char *boa_last_error(void);
  *     is the caller's (16-byte aligned, at least as large as the matching
  *     _workspace function says) and must not serve two calls at once.
  *   - Sums, statistics and logits are float32 whatever the element type, and
- *     results are rounded to it once. There are no atomics: the same inputs
- *     give the same bits.
+ *     results are rounded to it once. Nothing is added in an order that depends
+ *     on the schedule: the same inputs give the same bits.
  */
 enum { BOA_T_F32 = 0, BOA_T_BF16 = 1, BOA_T_F16 = 2 };
 

@@ -288,10 +288,10 @@ struct PartsArgs {
 
 // A thread makes 8 values of a row (plain_ld is a multiple of 16).
 template <class T>
-__global__ __launch_bounds__(256) void parts_kernel(PartsArgs a)
+__device__ inline void make_parts(const PartsArgs &a, int64_t i)
 {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    const int64_t chunks = a.plain_ld / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t chunks = a.plain_ld / 8;
     const int64_t r = i / chunks;
     const int32_t c = (int32_t)(i % chunks) * 8;
     if (r >= a.rows_pad) return;
@@ -332,10 +332,46 @@ __global__ __launch_bounds__(256) void parts_kernel(PartsArgs a)
 }
 
 template <class T>
-void launch_parts(const PartsArgs &a, hipStream_t st)
+__global__ __launch_bounds__(256) void parts_kernel(PartsArgs a)
 {
-    const int64_t n = (int64_t)a.rows_pad * (a.plain_ld / 8);
-    parts_kernel<T><<<dim3((uint32_t)((n + 255) / 256)), 256, 0, st>>>(a);
+    make_parts<T>(a, (int64_t)blockIdx.x * 256 + threadIdx.x);
+}
+
+inline int64_t parts_blocks(const PartsArgs &a) { return ceil_div((int64_t)a.rows_pad * (a.plain_ld / 8), 256); }
+
+// A point's bias in base 2. Finite ones stay finite, masks of the type's lowest
+// value among them.
+__device__ inline float base2(float bias)
+{
+    return fabsf(bias) < INFINITY ? fmaxf(-__FLT_MAX__, fminf(__FLT_MAX__, bias * LOG2E)) : bias;
+}
+
+// What a call begins with, in one launch: the queries as parts; the points'
+// biases in base 2, -inf past the last point (`to`, or null); the points' first
+// queries (or null) and the blocks that are done cleared.
+struct PrepArgs {
+    PartsArgs queries;
+    int32_t query_blocks, point_blocks;
+    const float *bias;
+    float *to;
+    int32_t V, padded;
+    int32_t *first;
+    uint32_t *done;
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void prep_kernel(PrepArgs a)
+{
+    if (blockIdx.x < (uint32_t)a.query_blocks) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
+        make_parts<T>(a.queries, (int64_t)blockIdx.x * 256 + threadIdx.x);
+        return;
+    }
+    const int64_t step = (int64_t)a.point_blocks * 256;
+    for (int64_t i = (int64_t)(blockIdx.x - a.query_blocks) * 256 + threadIdx.x; i < a.padded; i += step) {
+        if (a.to) a.to[i] = i >= a.V ? -INFINITY : a.bias ? base2(a.bias[i]) : 0.0f;
+        if (a.first && i < a.V) a.first[i] = -1;
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -353,13 +389,6 @@ __device__ inline void add_kept(float &sum, float &lost, float x)
     const float y = x - lost, t = sum + y;
     lost = (t - sum) - y;
     sum = t;
-}
-
-// A point's bias in base 2. Finite ones stay finite, masks of the type's lowest
-// value among them.
-__device__ inline float base2(float bias)
-{
-    return fabsf(bias) < INFINITY ? fmaxf(-__FLT_MAX__, fminf(__FLT_MAX__, bias * LOG2E)) : bias;
 }
 
 struct StatsArgs {
@@ -464,75 +493,79 @@ struct RowArgs {
     float *coef;             // B: g * (p_label - 1)
     int32_t *label;          // rows_pad: the label, or -1 where it has no entry
     int32_t B, V, shares, reduction, rows_pad;
+    uint32_t *done;          // blocks that are done, 0 at the start
+    float *total, *factor;   // the reduced loss and the factor every gradient gets, or null
 };
 
-// A wave per query: joins the shares of its statistics.
+// A wave per query: joins the shares of its statistics. The last block to end
+// adds the losses, in order whichever it is.
 __global__ __launch_bounds__(256) void row_kernel(RowArgs a)
 {
     const int lane = threadIdx.x & 63;
     const int32_t b = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (b >= a.rows_pad) return;
     if (b >= a.B) {
-        if (lane == 0) {
+        if (lane == 0 && b < a.rows_pad) {
             a.top[b] = INFINITY;   // probabilities of 0 whatever the bias
             a.rowf[b] = 0.0f;
         }
-        return;
-    }
-    RowState st{NO_MAX, 0.0f};
-    for (int i = lane; i < a.shares; i += 64) {
-        const RowState o = a.part[(int64_t)i * a.B + b];
-        join(st, o.m, o.s);
-    }
+    } else {
+        RowState st{NO_MAX, 0.0f};
+        for (int i = lane; i < a.shares; i += 64) {
+            const RowState o = a.part[(int64_t)i * a.B + b];
+            join(st, o.m, o.s);
+        }
 #pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        const float m = __shfl_xor(st.m, o), s = __shfl_xor(st.s, o);
-        join(st, m, s);
+        for (int o = 32; o; o >>= 1) {
+            const float m = __shfl_xor(st.m, o), s = __shfl_xor(st.s, o);
+            join(st, m, s);
+        }
+        if (lane == 0) {
+            const int64_t y = a.labels[b];
+            const bool in = y >= 0 && y < a.V;
+            const bool none = st.s == 0.0f;   // every point left out
+            const float log_s = __builtin_amdgcn_logf(st.s);
+            const float l2 = in ? a.pick[b] : 0.0f;
+            float loss = 0.0f;
+            if (y >= a.V) loss = NAN;
+            else if (in) loss = none ? INFINITY : ((st.m - l2) + log_s) * LN2;
+            a.loss[b] = loss;
+            if (a.lse) a.lse[b] = none ? -INFINITY : (st.m + log_s) * LN2;
+            const float g = !in || none ? 0.0f : a.reduction == BOA_REDUCE_NONE && a.dloss ? a.dloss[b] : 1.0f;
+            a.top[b] = none || !in ? INFINITY : st.m;
+            a.rowf[b] = g == 0.0f ? 0.0f : g / st.s;
+            if (none || !in) a.label[b] = -1;
+            if (a.coef) a.coef[b] = in && !none ? g * (__builtin_amdgcn_exp2f(l2 - st.m) / st.s - 1.0f) : 0.0f;
+        }
     }
-    if (lane) return;
-    const int64_t y = a.labels[b];
-    const bool in = y >= 0 && y < a.V;
-    const bool none = st.s == 0.0f;   // every point left out
-    const float log_s = __builtin_amdgcn_logf(st.s);
-    const float l2 = in ? a.pick[b] : 0.0f;
-    float loss = 0.0f;
-    if (y >= a.V) loss = NAN;
-    else if (in) loss = none ? INFINITY : ((st.m - l2) + log_s) * LN2;
-    a.loss[b] = loss;
-    if (a.lse) a.lse[b] = none ? -INFINITY : (st.m + log_s) * LN2;
-    const float g = !in || none ? 0.0f : a.reduction == BOA_REDUCE_NONE && a.dloss ? a.dloss[b] : 1.0f;
-    a.top[b] = none || !in ? INFINITY : st.m;
-    a.rowf[b] = g == 0.0f ? 0.0f : g / st.s;
-    if (none || !in) a.label[b] = -1;
-    if (a.coef) a.coef[b] = in && !none ? g * (__builtin_amdgcn_exp2f(l2 - st.m) / st.s - 1.0f) : 0.0f;
-}
-
-// One block: the reduced loss, and the factor every gradient gets.
-__global__ __launch_bounds__(1024) void total_kernel(const float *row_loss, const int64_t *labels, int32_t B,
-                                                     int32_t reduction, const float *dloss, float *loss, float *factor)
-{
-    __shared__ float ls[16], ns[16];
+    if (!a.total && !a.factor) return;
+    __shared__ bool last;
+    __shared__ float ls[4], ns[4];
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicAdd(a.done, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
     float s = 0.0f, n = 0.0f;
-    for (int32_t b = threadIdx.x; b < B; b += 1024) {
-        s += row_loss[b];
-        n += labels[b] >= 0 ? 1.0f : 0.0f;
+    for (int32_t i = threadIdx.x; i < a.B; i += 256) {
+        s += __builtin_nontemporal_load(a.loss + i);
+        n += a.labels[i] >= 0 ? 1.0f : 0.0f;
     }
     s = wave_sum(s);
     n = wave_sum(n);
-    if ((threadIdx.x & 63) == 0) {
+    if (lane == 0) {
         ls[threadIdx.x >> 6] = s;
         ns[threadIdx.x >> 6] = n;
     }
     __syncthreads();
     if (threadIdx.x) return;
-    s = n = 0.0f;
-    for (int i = 0; i < 16; ++i) {
-        s += ls[i];
-        n += ns[i];
-    }
-    const float by = reduction == BOA_REDUCE_MEAN ? fmaxf(n, 1.0f) : 1.0f;
-    if (loss) *loss = s / by;
-    if (factor) *factor = (dloss && reduction != BOA_REDUCE_NONE ? *dloss : 1.0f) / by;
+    s = ls[0] + ls[1] + ls[2] + ls[3];
+    n = ns[0] + ns[1] + ns[2] + ns[3];
+    const float by = a.reduction == BOA_REDUCE_MEAN ? fmaxf(n, 1.0f) : 1.0f;
+    if (a.total) *a.total = s / by;
+    if (a.factor) *a.factor = (a.dloss && a.reduction != BOA_REDUCE_NONE ? *a.dloss : 1.0f) / by;
 }
 
 // ---------------------------------------------------------------------------
@@ -737,15 +770,29 @@ __global__ __launch_bounds__(S::THREADS, 2) void dc_kernel(DcArgs a)
 
 // A block per query b that is its point's first: own[b] = sum over the point's
 // queries, in order, of coef * h; first[point] = b; own_bias[b] likewise.
+struct OwnArgs {
+    const void *h;
+    int64_t h_stride;
+    int32_t B, d;
+    const int32_t *label;
+    const float *coef;
+    int32_t *first;
+    float *own, *own_bias;   // own may be null
+};
+
 template <class T>
-__global__ __launch_bounds__(256) void own_kernel(const T *h, int64_t h_stride, int32_t B, int32_t d,
-                                                  const int32_t *label, const float *coef, int32_t *first, float *own,
-                                                  float *own_bias)
+__device__ inline void own_terms(const OwnArgs &a, int32_t b)
 {
+    const T *h = (const T *)a.h;
+    const int64_t h_stride = a.h_stride;
+    const int32_t B = a.B, d = a.d, *label = a.label;
+    const float *coef = a.coef;
+    int32_t *first = a.first;
+    float *own = a.own, *own_bias = a.own_bias;
     __shared__ int earlier;
     __shared__ int32_t list[256];
     __shared__ int count;
-    const int32_t b = blockIdx.x, y = label[b];
+    const int32_t y = label[b];
     if (y < 0) return;
     if (threadIdx.x == 0) earlier = 0;
     __syncthreads();
@@ -793,9 +840,10 @@ __global__ __launch_bounds__(256) void own_kernel(const T *h, int64_t h_stride, 
     }
 }
 
-__global__ __launch_bounds__(256) void fill_kernel(int32_t *p, int64_t n, int32_t v)
+template <class T>
+__global__ __launch_bounds__(256) void own_kernel(OwnArgs a)
 {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = v;
+    own_terms<T>(a, blockIdx.x);
 }
 
 __global__ __launch_bounds__(256) void dbias_kernel(const float *col, int32_t tiles_b, int32_t cols_pad, int32_t n,
@@ -1355,44 +1403,54 @@ __global__ __launch_bounds__(256) void dc_join_kernel(const float *out, const fl
 
 // The shares of SWEEP_H, brought to the common maximum:
 // dh = scale factor (g / sum  sum_shares 2^(m - top) out + coef c_label)
+struct DhShares {
+    const float *out;        // shares x B x ld
+    const RowState *part;
+    int32_t shares, ld;
+    const float *top, *rowf, *factor;
+    const void *points;
+    int64_t points_stride;
+    float scale;
+    void *dh;
+};
+
+// A block per query: ld / 4 threads take four values each, and as many times as
+// they fit the block they part the shares, whose sums are then added in order.
 template <class T>
-__global__ __launch_bounds__(256) void dh_shares_kernel(const float *out, const RowState *part, int32_t shares, int32_t B,
-                                                        int32_t d, int32_t ld, const float *top, const float *rowf,
-                                                        const T *points, int64_t points_stride, const int32_t *label,
-                                                        const float *coef, const float *factor, float scale, T *dh)
+__device__ inline void dh_of_shares(const DhShares &a, const OwnArgs &o, int32_t b)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (int64_t)B * d) return;
-    const int32_t b = (int32_t)(i / d), c = (int32_t)(i % d);
-    const float f = rowf[b], m = top[b];
-    float s = 0.0f;
-    if (f != 0.0f) {
-        for (int32_t k = 0; k < shares; ++k) {
-            const int64_t at = (int64_t)k * B + b;
-            s = fmaf(__builtin_amdgcn_exp2f(part[at].m - m), out[at * ld + c], s);
+    __shared__ float part[256 * 4];
+    const int cols = a.ld / 4, slices = 256 / cols, col = threadIdx.x % cols, slice = threadIdx.x / cols;
+    const float f = a.rowf[b], m = a.top[b];
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (f != 0.0f && slice < slices)
+        for (int32_t k = slice; k < a.shares; k += slices) {
+            const int64_t at = (int64_t)k * o.B + b;
+            float v[4];
+            load_f32<4, float>(v, a.out + at * a.ld + col * 4);
+            const float by = __builtin_amdgcn_exp2f(a.part[at].m - m);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] = fmaf(by, v[e], s[e]);
         }
-        s *= f;
-    }
-    const int32_t y = label[b];
-    if (y >= 0) s = fmaf(coef[b], (float)points[(int64_t)y * points_stride + c], s);
-    dh[i] = (T)(scale * *factor * s);
+    store_f32<4, float>(part + threadIdx.x * 4, s);
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c >= o.d) return;
+    float sum = 0.0f;
+    for (int k = 0; k < slices; ++k) sum += part[(k * cols) * 4 + c];
+    sum *= f;
+    const int32_t y = o.label[b];
+    if (y >= 0) sum = fmaf(o.coef[b], (float)((const T *)a.points)[(int64_t)y * a.points_stride + c], sum);
+    ((T *)a.dh)[(int64_t)b * o.d + c] = (T)(a.scale * *a.factor * sum);
 }
 
-// Biases in base 2 as SWEEP_LOSS and SWEEP_H read them, and the points' first
-// queries cleared.
-__global__ __launch_bounds__(256) void points_kernel(const float *bias, int32_t V, int32_t padded, float *to, int32_t *first)
+// Between the sweeps: a block per query and task.
+template <class T>
+__global__ __launch_bounds__(256) void between_kernel(OwnArgs o, DhShares s)
 {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < padded; i += (int64_t)gridDim.x * 256) {
-        to[i] = i >= V ? -INFINITY : bias ? base2(bias[i]) : 0.0f;
-        if (first && i < V) first[i] = -1;
-    }
-}
-
-// Labels as the sweeps read them: -1 where a query has none, past the last one too.
-__global__ __launch_bounds__(256) void labels_kernel(const int64_t *labels, int32_t B, int32_t V, int32_t padded, int32_t *to)
-{
-    const int32_t b = blockIdx.x * 256 + threadIdx.x;
-    if (b < padded) to[b] = b < B && labels[b] >= 0 && labels[b] < V ? (int32_t)labels[b] : -1;
+    const int32_t b = (int32_t)blockIdx.x >= o.B ? blockIdx.x - o.B : blockIdx.x;
+    if (s.dh && (int32_t)blockIdx.x < o.B) dh_of_shares<T>(s, o, b);
+    else if (o.first) own_terms<T>(o, b);
 }
 
 // ---------------------------------------------------------------------------
@@ -1411,7 +1469,7 @@ struct Plan {
     int64_t Vc, cols_pad;      // points per piece, and its padded size
     int64_t copied;            // points that are held as parts at a time
     int32_t dh_splits, dh_k, tile_d, tiles_d;
-    int64_t off_h, off_c, off_part, off_loss, off_top, off_rowf, off_coef, off_label, off_pick, off_factor;
+    int64_t off_h, off_c, off_part, off_loss, off_top, off_rowf, off_coef, off_label, off_pick, off_factor, off_done;
     int64_t off_p, off_col, off_dh, off_first, off_own, off_ownb, off_bias, off_hz, off_dc, total;
 };
 
@@ -1526,6 +1584,7 @@ Plan make_plan(const boa_xent *x, bool grad)
     p.off_rowf = take((int64_t)p.rows_pad * 4);
     p.off_label = take((int64_t)p.rows_pad * 4);
     p.off_factor = take(16);
+    p.off_done = take(16);
     if (grad) p.off_coef = take(x->B * 4);
     if (dc || db) {
         p.off_first = take(x->V * 4);
@@ -1545,8 +1604,8 @@ constexpr size_t stage_bytes()
 template <class K, class A>
 void run(K kernel, uint32_t grid, uint32_t threads, size_t lds, hipStream_t st, const A &args)
 {
-    // LDS above 64 KB has to be asked for
-    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (lds > 64 << 10)   // has to be asked for
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     kernel<<<dim3(grid), threads, lds, st>>>(args);
 }
 
@@ -1605,37 +1664,46 @@ struct Work {
     float *row_loss() const { return x->reduction == BOA_REDUCE_NONE ? x->loss : at<float>(p.off_loss); }
     bool want_c() const { return grad && (x->dpoints || x->dbias); }
 
-    // queries as parts, and their labels
-    void queries(int32_t ld, bf16_t *kept) const
+    // queries as parts and their labels, and the points' side of it
+    void prep(int32_t ld, bf16_t *kept, float *bias, int32_t padded) const
     {
-        PartsArgs a{};
-        a.src = x->h, a.stride = x->h_stride, a.R = (int32_t)x->B, a.C = x->d, a.rows_pad = p.rows_pad;
-        a.plain = at<bf16_t>(p.off_h), a.plain_ld = ld, a.plain_part = (int64_t)p.rows_pad * ld, a.kept = kept;
-        a.labels = x->labels, a.V = (int32_t)x->V, a.label = at<int32_t>(p.off_label);
-        launch_parts<T>(a, st);
+        PrepArgs a{};
+        PartsArgs &q = a.queries;
+        q.src = x->h, q.stride = x->h_stride, q.R = (int32_t)x->B, q.C = x->d, q.rows_pad = p.rows_pad;
+        q.plain = at<bf16_t>(p.off_h), q.plain_ld = ld, q.plain_part = (int64_t)p.rows_pad * ld, q.kept = kept;
+        q.labels = x->labels, q.V = (int32_t)x->V, q.label = at<int32_t>(p.off_label);
+        a.query_blocks = (int32_t)parts_blocks(q);
+        a.bias = x->bias, a.to = bias, a.V = (int32_t)x->V, a.padded = padded;
+        a.first = want_c() ? at<int32_t>(p.off_first) : nullptr;
+        a.point_blocks = a.to || a.first ? (int32_t)std::min<int64_t>(1024, ceil_div(padded, 256)) : 0;
+        a.done = at<uint32_t>(p.off_done);
+        prep_kernel<T><<<dim3((uint32_t)(a.query_blocks + a.point_blocks)), 256, 0, st>>>(a);
     }
 
     // after the statistics: losses, and what the gradients need of each query
     void rows(int32_t shares) const
     {
-        const bool reduced = x->reduction != BOA_REDUCE_NONE;
         RowArgs r{};
         r.labels = x->labels, r.dloss = grad ? x->dloss : nullptr, r.pick = at<float>(p.off_pick);
         r.part = at<RowState>(p.off_part), r.loss = row_loss(), r.lse = x->lse;
         r.top = at<float>(p.off_top), r.rowf = at<float>(p.off_rowf), r.label = at<int32_t>(p.off_label);
         r.coef = grad ? at<float>(p.off_coef) : nullptr;
         r.B = (int32_t)x->B, r.V = (int32_t)x->V, r.shares = shares, r.reduction = x->reduction, r.rows_pad = p.rows_pad;
+        r.done = at<uint32_t>(p.off_done);
+        r.total = x->reduction != BOA_REDUCE_NONE ? x->loss : nullptr, r.factor = grad ? at<float>(p.off_factor) : nullptr;
         row_kernel<<<dim3((uint32_t)ceil_div(p.rows_pad, 4)), 256, 0, st>>>(r);
-        if (reduced || grad)
-            total_kernel<<<1, 1024, 0, st>>>(row_loss(), x->labels, r.B, x->reduction, r.dloss, reduced ? x->loss : nullptr,
-                                             grad ? at<float>(p.off_factor) : nullptr);
     }
 
-    void own() const
+    OwnArgs own() const
     {
-        own_kernel<T><<<dim3((uint32_t)x->B), 256, 0, st>>>(
-            (const T *)x->h, x->h_stride, (int32_t)x->B, x->d, at<int32_t>(p.off_label), at<float>(p.off_coef),
-            at<int32_t>(p.off_first), x->dpoints ? at<float>(p.off_own) : nullptr, at<float>(p.off_ownb));
+        OwnArgs o{};
+        o.h = x->h, o.h_stride = x->h_stride, o.B = (int32_t)x->B, o.d = x->d;
+        o.label = at<int32_t>(p.off_label), o.coef = at<float>(p.off_coef);
+        if (want_c()) {
+            o.first = at<int32_t>(p.off_first), o.own_bias = at<float>(p.off_ownb);
+            o.own = x->dpoints ? at<float>(p.off_own) : nullptr;
+        }
+        return o;
     }
 };
 
@@ -1681,8 +1749,7 @@ int run_sweeps(const Work<T> &w)
     float *bias = w.template at<float>(p.off_bias);
     const int32_t v_pad = (int32_t)round_up(V, 128);
 
-    w.queries(p.ld, hz);
-    points_kernel<<<dim3((uint32_t)std::min<int64_t>(1024, ceil_div(v_pad, 256))), 256, 0, st>>>(x->bias, V, v_pad, bias, first);
+    w.prep(p.ld, hz, bias, v_pad);
     SweepArgs c{};   // the points' side of the arguments
     if constexpr (sizeof(T) == 4) {
         c.mf = (const float *)x->points, c.m_ld = x->points_stride;
@@ -1694,7 +1761,7 @@ int run_sweeps(const Work<T> &w)
         PartsArgs a{};
         a.src = x->points, a.stride = x->points_stride, a.R = V, a.C = d, a.rows_pad = V;
         a.plain = w.template at<bf16_t>(p.off_c), a.plain_ld = p.ld;
-        launch_parts<T>(a, st);
+        parts_kernel<T><<<dim3((uint32_t)parts_blocks(a)), 256, 0, st>>>(a);
         c.m = a.plain, c.m_ld = p.ld, c.Kp = p.ld;
     }
     SweepArgs a = c;
@@ -1714,13 +1781,18 @@ int run_sweeps(const Work<T> &w)
     }
     w.rows(p.shares);
     if (!w.grad) return launch_status("softmax_xent");
-    const float *factor = w.template at<float>(p.off_factor), *coef = w.template at<float>(p.off_coef);
-    if (dh)
-        dh_shares_kernel<T><<<dim3((uint32_t)ceil_div((int64_t)B * d, 256)), 256, 0, st>>>(
-            a.out, a.part, p.shares, B, d, p.ld, w.template at<float>(p.off_top), w.template at<float>(p.off_rowf),
-            (const T *)x->points, x->points_stride, a.label, coef, factor, x->scale, (T *)x->dh);
+    const float *factor = w.template at<float>(p.off_factor);
+    const OwnArgs own = w.own();
+    DhShares shares{};
+    if (dh) {
+        shares.out = a.out, shares.part = a.part, shares.shares = p.shares, shares.ld = p.ld;
+        shares.top = w.template at<float>(p.off_top), shares.rowf = w.template at<float>(p.off_rowf);
+        shares.factor = factor, shares.points = x->points, shares.points_stride = x->points_stride;
+        shares.scale = x->scale, shares.dh = x->dh;
+    }
+    if (dh || w.want_c())
+        between_kernel<T><<<dim3((uint32_t)(dh && w.want_c() ? 2 * B : B)), 256, 0, st>>>(own, shares);
     if (w.want_c()) {
-        w.own();
         SweepArgs g = c;
         g.n = c.m, g.nf = c.mf, g.n_ld = c.m_ld, g.N = V, g.M = B, g.d = d;
         g.m = hz, g.mf = nullptr, g.m_ld = p.ld, g.m_part = (int64_t)p.rows_pad * p.ld;
@@ -1729,7 +1801,7 @@ int run_sweeps(const Work<T> &w)
         g.scale2 = a.scale2, g.bias = bias, g.label = a.label;
         g.top = w.template at<float>(p.off_top), g.rowf = w.template at<float>(p.off_rowf);
         g.first = first, g.factor = factor, g.scale = x->scale;
-        g.own = x->dpoints ? w.template at<float>(p.off_own) : nullptr, g.own_bias = w.template at<float>(p.off_ownb);
+        g.own = own.own, g.own_bias = own.own_bias;
         g.dc = x->dpoints, g.dbias = x->dbias;
         if (p.c_splits > 1) {
             g.out = w.template at<float>(p.off_dc);
@@ -1756,7 +1828,7 @@ int run_tiles(const Work<T> &w)
     bf16_t *hp = (bf16_t *)(ws + p.off_h), *hz = w.want_c() ? (bf16_t *)(ws + p.off_hz) : nullptr;
     float *factor = (float *)(ws + p.off_factor);
     const int64_t h_part = (int64_t)p.rows_pad * p.Kp, c_part = p.copied * p.Kp;
-    w.queries(p.Kp, hz);
+    w.prep(p.Kp, hz, nullptr, V);
 
     const int32_t pieces = (int32_t)ceil_div(V, p.Vc);
     const bool whole = p.copied >= V;   // the points' copy serves both passes
@@ -1769,7 +1841,7 @@ int run_tiles(const Work<T> &w)
             a.src = (const T *)x->points + v0 * x->points_stride, a.stride = x->points_stride;
             a.R = a.rows_pad = n, a.C = d, a.plain_ld = p.Kp, a.plain_part = c_part;
             a.plain = copy + (whole ? v0 * p.Kp : 0);
-            launch_parts<T>(a, st);
+            parts_kernel<T><<<dim3((uint32_t)parts_blocks(a)), 256, 0, st>>>(a);
         }
         return Operand{copy + (whole ? v0 * p.Kp : 0), p.Kp, n, p.Kp};
     };
@@ -1804,15 +1876,10 @@ int run_tiles(const Work<T> &w)
 
     const int32_t *label = (const int32_t *)(ws + p.off_label);
     const float *coef = (const float *)(ws + p.off_coef);
-    int32_t *first = nullptr;
-    float *own = nullptr, *own_bias = nullptr;
-    if (x->dpoints || x->dbias) {
-        first = (int32_t *)(ws + p.off_first);
-        own_bias = (float *)(ws + p.off_ownb);
-        own = x->dpoints ? (float *)(ws + p.off_own) : nullptr;
-        fill_kernel<<<dim3((uint32_t)std::min<int64_t>(1024, ceil_div(V, 256))), 256, 0, st>>>(first, V, -1);
-        w.own();
-    }
+    const OwnArgs oa = w.own();
+    const int32_t *first = oa.first;
+    const float *own = oa.own, *own_bias = oa.own_bias;
+    if (w.want_c()) own_kernel<T><<<dim3((uint32_t)B), 256, 0, st>>>(oa);
     const int64_t p_part = (int64_t)p.rows_pad * p.cols_pad;
     for (int32_t i = 0; i < pieces; ++i) {
         const int32_t v0 = (int32_t)(i * p.Vc), n = (int32_t)std::min<int64_t>(p.Vc, V - v0);

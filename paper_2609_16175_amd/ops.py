@@ -3,9 +3,9 @@ entropy over the points of an index, products with 4-bit rows.
 
 Argument marshalling for libboa.so (include/boa.h); every computation runs in
 the library's HIP kernels. Tensors live on one GPU; calls are queued on its
-current stream (or `stream`) and return without waiting. Where `stream` is
-given, tensors made here are recorded on it, and ordering it after the
-inputs' own stream is the caller's.
+current stream, or on `stream`, and return without waiting. With `stream`,
+results belong to it, and its order after whatever makes the inputs is the
+caller's.
 """
 from __future__ import annotations
 
@@ -50,42 +50,28 @@ def _lib():
     return _ready
 
 
-class _Call:
-    """The device and stream of one call: what it allocates belongs to the
-    stream that the kernels run on."""
+# The current device and stream as plain numbers: a call on one row is a few
+# microseconds of kernel, and torch's stream objects cost as much again.
+_current_device = torch._C._cuda_getDevice
+_current_stream = torch._C._cuda_getCurrentRawStream
 
-    def __init__(self, tensor, stream):
-        self.dev = tensor.device
-        self.current = torch.cuda.current_stream(self.dev)
-        self.stream = stream if stream is not None else self.current
-        self.guard = None
-        if torch.cuda.current_device() != self.dev.index:
-            self.guard = torch.cuda.device(self.dev)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self
+def _at(x, stream, *inputs):
+    """None where the call can go on: x lies on the current GPU and `stream` is
+    its current stream. Else the context in which to make the call again, with
+    the inputs kept for the other stream: what the call allocates and copies
+    then belongs to it too."""
+    dev = x.get_device()
+    if stream is not None and stream.cuda_stream != _current_stream(dev):
+        for t in inputs:
+            if t is not None:
+                t.record_stream(stream)
+        return torch.cuda.stream(stream)
+    return torch.cuda.device(dev) if dev != _current_device() else None
 
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
 
-    def empty(self, shape, dtype):
-        t = torch.empty(shape, dtype=dtype, device=self.dev)
-        if self.stream != self.current:
-            t.record_stream(self.stream)
-        return t
-
-    def workspace(self, nbytes):
-        return self.empty((max(16, int(nbytes)),), torch.uint8)
-
-    def used(self, *tensors):
-        """Inputs may be freed by their owner while the call still runs."""
-        if self.stream != self.current:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
+def _workspace(x, nbytes):
+    return torch.empty((max(16, int(nbytes)),), dtype=torch.uint8, device=x.device)
 
 
 def _ptr(t):
@@ -97,11 +83,12 @@ def _device(name, *tensors):
     for t in tensors:
         if t is None:
             continue
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        at = t.get_device() if isinstance(t, torch.Tensor) and t.is_cuda else -1
+        if at < 0:
             raise ValueError(f"{name}: arguments must be device tensors")
-        if dev is not None and t.device != dev:
+        if dev is not None and at != dev:
             raise ValueError(f"{name}: tensors on different devices")
-        dev = t.device
+        dev = at
 
 
 def _dtype(name, t, of=tuple(_DTYPES)):
@@ -113,7 +100,9 @@ def _dtype(name, t, of=tuple(_DTYPES)):
 def _rows(x):
     """x as a matrix whose last dimension is contiguous, without a copy where
     its strides allow."""
-    m = x if x.dim() == 2 else x.reshape(-1, x.shape[-1]) if x.shape[-1] else x.new_empty((0, 0))
+    if x.is_contiguous() and x.dim() == 2:
+        return x
+    m = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
     if m.shape[1] > 1 and m.stride(1) != 1 or m.shape[0] > 1 and m.stride(0) < m.shape[1]:
         m = m.contiguous()
     return m
@@ -127,17 +116,23 @@ def _stride(m):
 # layer norm
 
 def _norm_params(name, x, weight, bias):
-    if x.dim() < 1 or x.shape[-1] < 1:
+    last = x.shape[-1:]
+    if not last or last[0] < 1:
         raise ValueError(f"{name}: x needs a last dimension of at least 1")
+    dtype = None
     for p in (weight, bias):
         if p is None:
             continue
-        if p.dtype not in (x.dtype, torch.float32) or tuple(p.shape) != (x.shape[-1],):
-            raise ValueError(f"{name}: weight and bias must be ({x.shape[-1]},) of x's type or float32")
-    if weight is not None and bias is not None and weight.dtype != bias.dtype:
-        raise ValueError(f"{name}: weight and bias must have one type")
-    p = weight if weight is not None else bias
-    return _DTYPES[p.dtype] if p is not None else _DTYPES[x.dtype]
+        if p.shape != last or p.dtype != x.dtype and p.dtype != torch.float32:
+            raise ValueError(f"{name}: weight and bias must be ({last[0]},) of x's type or float32")
+        if dtype is not None and p.dtype != dtype:
+            raise ValueError(f"{name}: weight and bias must have one type")
+        dtype = p.dtype
+    return _DTYPES[x.dtype if dtype is None else dtype]
+
+
+def _dense(t):
+    return t if t is None or t.is_contiguous() else t.contiguous()
 
 
 def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, stream=None):
@@ -149,17 +144,18 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, stream=None):
     _device("layer_norm", x, weight, bias)
     dt = _dtype("layer_norm", x)
     pd = _norm_params("layer_norm", x, weight, bias)
-    w = None if weight is None else weight.contiguous()
-    b = None if bias is None else bias.contiguous()
+    w, b = _dense(weight), _dense(bias)
+    other = _at(x, stream, x, weight, bias)
+    if other is not None:
+        with other:
+            return layer_norm_forward(x, weight, bias, eps)
     m = _rows(x)
     rows, d = m.shape
-    with _Call(x, stream) as call:
-        y = call.empty(x.shape, x.dtype)
-        stats = call.empty((2, rows), torch.float32)
-        call.used(m, w, b)
-        _check(_lib().boa_layer_norm(m.data_ptr(), rows, d, _stride(m), dt, _ptr(w), _ptr(b), pd, eps, y.data_ptr(),
-                                     stats[0].data_ptr(), stats[1].data_ptr(), call.stream.cuda_stream))
-    return y, stats[0], stats[1]
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
+    _check(_lib().boa_layer_norm(m.data_ptr(), rows, d, _stride(m), dt, _ptr(w), _ptr(b), pd, eps, y.data_ptr(),
+                                 mean.data_ptr(), rstd.data_ptr(), _current_stream(x.get_device())))
+    return y, mean, rstd
 
 
 def layer_norm_backward(dy, x, weight, mean, rstd, need=(True, True, True), stream=None):
@@ -175,18 +171,25 @@ def layer_norm_backward(dy, x, weight, mean, rstd, need=(True, True, True), stre
     for s in (mean, rstd):
         if s.dtype != torch.float32 or s.numel() != rows or not s.is_contiguous():
             raise ValueError("layer_norm_backward: mean and rstd must be the float32 tensors of the forward pass")
-    w = None if weight is None else weight.contiguous()
+    other = _at(x, stream, dy, x, weight, mean, rstd)
+    if other is not None:
+        with other:
+            return layer_norm_backward(dy, x, weight, mean, rstd, need)
+    w = _dense(weight)
     ptype = x.dtype if weight is None else weight.dtype
-    with _Call(x, stream) as call:
-        dx = call.empty(x.shape, x.dtype) if need[0] else None
-        dw = call.empty((d,), ptype) if need[1] else None
-        db = call.empty((d,), ptype) if need[2] else None
-        nbytes = _lib().boa_layer_norm_backward_workspace(rows, d) if need[1] or need[2] else 0
-        ws = call.workspace(nbytes)
-        call.used(m, g, w, mean, rstd)
-        _check(_lib().boa_layer_norm_backward(g.data_ptr(), _stride(g), m.data_ptr(), _stride(m), rows, d, dt, _ptr(w), pd,
-                                              mean.data_ptr(), rstd.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db),
-                                              ws.data_ptr(), ws.numel(), call.stream.cuda_stream))
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need[0] else None
+    dw = db = None
+    if need[1] and need[2]:
+        dw, db = torch.empty((2, d), dtype=ptype, device=x.device).unbind(0)
+    elif need[1]:
+        dw = torch.empty((d,), dtype=ptype, device=x.device)
+    elif need[2]:
+        db = torch.empty((d,), dtype=ptype, device=x.device)
+    ws = _workspace(x, _lib().boa_layer_norm_backward_workspace(rows, d)) if need[1] or need[2] else None
+    _check(_lib().boa_layer_norm_backward(g.data_ptr(), _stride(g), m.data_ptr(), _stride(m), rows, d, dt, _ptr(w), pd,
+                                          mean.data_ptr(), rstd.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db), _ptr(ws),
+                                          0 if ws is None else ws.numel(),
+                                          _current_stream(x.get_device())))
     return dx, dw, db
 
 
@@ -241,26 +244,28 @@ def _xent(name, h, rows, labels, bias, scale, reduction, stream, grad, dloss=Non
     shape = (B,) if reduction == "none" else ()
     if dloss is not None and (dloss.dtype != torch.float32 or tuple(dloss.shape) != shape):
         raise ValueError(f"{name}: dloss must be float32 of the loss's shape")
-    hm, rm, lab = _rows(h), _rows(rows), labels.contiguous()
-    bm = None if bias is None else bias.contiguous()
-    gm = None if dloss is None else dloss.contiguous()
-    with _Call(h, stream) as call:
-        r = XentResult(call.empty(shape, torch.float32), call.empty((B,), torch.float32))
-        if h_grad:
-            r.dh = call.empty((B, d), h.dtype)
-        if rows_grad:
-            r.drows = call.empty((V, d), rows.dtype)
-        if bias_grad:
-            r.dbias = call.empty((V,), torch.float32)
-        a = Xent(dt, d, B, V, hm.data_ptr(), _stride(hm), rm.data_ptr(), _stride(rm), lab.data_ptr(), _ptr(bm), scale,
-                 _REDUCE[reduction], r.loss.data_ptr(), r.lse.data_ptr(), _ptr(gm), _ptr(r.dh), _ptr(r.drows), _ptr(r.dbias))
-        nbytes = _lib().boa_softmax_xent_workspace(C.byref(a), int(grad))
-        if nbytes < 0:
-            _check(nbytes)
-        ws = call.workspace(nbytes)
-        call.used(hm, rm, lab, bm, gm)
-        fn = _lib().boa_softmax_xent_grad if grad else _lib().boa_softmax_xent
-        _check(fn(C.byref(a), ws.data_ptr(), ws.numel(), call.stream.cuda_stream))
+    other = _at(h, stream, h, rows, labels, bias, dloss)
+    if other is not None:
+        with other:
+            return _xent(name, h, rows, labels, bias, scale, reduction, None, grad, dloss, h_grad, rows_grad, bias_grad)
+    dev = h.device
+    hm, rm, lab, bm, gm = _rows(h), _rows(rows), _dense(labels), _dense(bias), _dense(dloss)
+    r = XentResult(torch.empty(shape, dtype=torch.float32, device=dev), torch.empty((B,), dtype=torch.float32, device=dev))
+    if h_grad:
+        r.dh = torch.empty((B, d), dtype=h.dtype, device=dev)
+    if rows_grad:
+        r.drows = torch.empty((V, d), dtype=rows.dtype, device=dev)
+    if bias_grad:
+        r.dbias = torch.empty((V,), dtype=torch.float32, device=dev)
+    a = Xent(dt, d, B, V, hm.data_ptr(), _stride(hm), rm.data_ptr(), _stride(rm), lab.data_ptr(), _ptr(bm), scale,
+             _REDUCE[reduction], r.loss.data_ptr(), r.lse.data_ptr(), _ptr(gm), _ptr(r.dh), _ptr(r.drows), _ptr(r.dbias))
+    nbytes = _lib().boa_softmax_xent_workspace(C.byref(a), int(grad))
+    if nbytes < 0:
+        _check(nbytes)
+    ws = _workspace(h, nbytes)
+    fn = _lib().boa_softmax_xent_grad if grad else _lib().boa_softmax_xent
+    _check(fn(C.byref(a), ws.data_ptr(), ws.numel(),
+              _current_stream(h.get_device())))
     return r
 
 
@@ -347,13 +352,15 @@ def matvec_4bit(x, codes, scales, offsets=None, group=None, stream=None):
         raise ValueError(f"matvec_4bit: {G} groups of {group} do not cover K = {K}")
     if offsets is not None and (offsets.shape != scales.shape or offsets.dtype != scales.dtype):
         raise ValueError("matvec_4bit: offsets must have the scales' shape and type")
+    other = _at(x, stream, x, codes, scales, offsets)
+    if other is not None:
+        with other:
+            return matvec_4bit(x, codes, scales, offsets, group)
     c, s = _rows(codes), _rows(scales)
     o = None if offsets is None else _rows(offsets)
     if o is not None and _stride(o) != _stride(s):
         s, o = s.contiguous(), o.contiguous()
-    with _Call(x, stream) as call:
-        y = call.empty((M, N), x.dtype)
-        call.used(m, c, s, o)
-        _check(_lib().boa_matvec_fourbit(m.data_ptr(), M, _stride(m), dt, c.data_ptr(), N, K, _stride(c), s.data_ptr(),
-                                         _ptr(o), _stride(s), sd, group, y.data_ptr(), N, call.stream.cuda_stream))
+    y = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    _check(_lib().boa_matvec_fourbit(m.data_ptr(), M, _stride(m), dt, c.data_ptr(), N, K, _stride(c), s.data_ptr(), _ptr(o),
+                                     _stride(s), sd, group, y.data_ptr(), N, _current_stream(x.get_device())))
     return y if x.dim() == 2 else y[0]
