@@ -33,6 +33,25 @@ struct NormArgs {
     float eps;
 };
 
+// A thread's columns of load i of a row: [c, c + VEC), moved back to end with
+// the row where they would pass its end; the first `skip` of them are then
+// another thread's too, or all (skip >= VEC). Every load is whole and within the
+// row, with no branch around it. WHOLE: rows of whole loads, where skip is 0
+// or at least VEC.
+template <int VEC, int TPR>
+struct Cols {
+    int c, skip;
+    __device__ Cols(int i, int lane, int32_t d)
+    {
+        const int c0 = (i * TPR + lane) * VEC;
+        c = min(c0, d - VEC);
+        skip = c0 - c;
+    }
+    __device__ bool any() const { return skip < VEC; }
+    template <bool WHOLE>
+    __device__ bool mine(int j) const { return WHOLE ? skip == 0 : j >= skip; }
+};
+
 // Sum of a value over the TPR threads of a row (a wave, or the block).
 template <int TPR>
 __device__ inline float row_sum(float v, float *red)
@@ -73,9 +92,10 @@ __device__ inline void row_sum2(float &a, float &b, float *red)
     }
 }
 
-template <class T, class P, int VEC, int NV, int TPR>
+template <class T, class P, int NV, int TPR, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a)
 {
+    constexpr int VEC = 16 / sizeof(T);
     __shared__ float red[8];
     const int lane = threadIdx.x % TPR;
     const int64_t row = (int64_t)blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
@@ -85,28 +105,23 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a)
     float v[NV][VEC];
     float s = 0.0f;
 #pragma unroll
+    for (int i = 0; i < NV; ++i) load_loose<VEC, T>(v[i], x + Cols<VEC, TPR>(i, lane, d).c);
+#pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * TPR + lane) * VEC;
-        if (c < d) {
-            load_f32<VEC, T>(v[i], x + c);
-        } else {
+        const Cols<VEC, TPR> at(i, lane, d);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) v[i][j] = 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) s += v[i][j];
+        for (int j = 0; j < VEC; ++j) s += at.template mine<WHOLE>(j) ? v[i][j] : 0.0f;
     }
     const float mu = row_sum<TPR>(s, red) / (float)d;
     float q = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * TPR + lane) * VEC;
-        if (c < d) {
+        const Cols<VEC, TPR> at(i, lane, d);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                v[i][j] -= mu;
-                q = fmaf(v[i][j], v[i][j], q);
-            }
+        for (int j = 0; j < VEC; ++j) {
+            v[i][j] -= mu;
+            const float t = at.template mine<WHOLE>(j) ? v[i][j] : 0.0f;
+            q = fmaf(t, t, q);
         }
     }
     const float r = 1.0f / sqrtf(row_sum<TPR>(q, red) / (float)d + a.eps);
@@ -117,24 +132,24 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a)
     T *y = (T *)a.y + row * (int64_t)d;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * TPR + lane) * VEC;
-        if (c >= d) continue;
+        const Cols<VEC, TPR> at(i, lane, d);
         float o[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) o[j] = v[i][j] * r;
         if (a.w) {
             float w[VEC];
-            load_f32<VEC, P>(w, (const P *)a.w + c);
+            load_loose<VEC, P>(w, (const P *)a.w + at.c);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) o[j] *= w[j];
         }
         if (a.b) {
             float b[VEC];
-            load_f32<VEC, P>(b, (const P *)a.b + c);
+            load_loose<VEC, P>(b, (const P *)a.b + at.c);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) o[j] += b[j];
         }
-        store_f32<VEC, T>(y + c, o);
+        // two threads' common columns hold the same values
+        if (at.any()) store_loose<VEC, T>(y + at.c, o);
     }
 }
 
@@ -169,10 +184,11 @@ __global__ __launch_bounds__(THREADS) void norm_wide_kernel(NormArgs a)
     }
 }
 
-// DX: dx is wanted; DP: dw and db are.
-template <class T, class P, int VEC, int NV, int TPR, bool DP>
+// DP: dw and db are wanted.
+template <class T, class P, int NV, int TPR, bool WHOLE, bool DP>
 __global__ __launch_bounds__(THREADS) void norm_back_kernel(NormArgs a)
 {
+    constexpr int VEC = 16 / sizeof(T);
     __shared__ float red[8];
     extern __shared__ float cols[];   // 2 x d, where several rows share a block
     constexpr int GROUPS = THREADS / TPR;
@@ -181,13 +197,14 @@ __global__ __launch_bounds__(THREADS) void norm_back_kernel(NormArgs a)
     float w[NV][VEC], dw[NV][VEC], db[NV][VEC];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * TPR + lane) * VEC;
+        const Cols<VEC, TPR> at(i, lane, d);
+        if (a.w) load_loose<VEC, P>(w[i], (const P *)a.w + at.c);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            w[i][j] = c < d ? 1.0f : 0.0f;
+            // columns that are not this thread's count for nothing in the row's sums
+            w[i][j] = !at.template mine<WHOLE>(j) ? 0.0f : a.w ? w[i][j] : 1.0f;
             dw[i][j] = db[i][j] = 0.0f;
         }
-        if (a.w && c < d) load_f32<VEC, P>(w[i], (const P *)a.w + c);
     }
     for (int64_t row = (int64_t)blockIdx.x * GROUPS + group; row < a.rows; row += (int64_t)gridDim.x * GROUPS) {
         const T *x = (const T *)a.x + row * a.x_stride;
@@ -197,17 +214,9 @@ __global__ __launch_bounds__(THREADS) void norm_back_kernel(NormArgs a)
         float c1 = 0.0f, c2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * TPR + lane) * VEC;
-            if (c < d) {
-                load_f32<VEC, T>(xh[i], x + c);
-                load_f32<VEC, T>(g[i], dy + c);
-            } else {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    xh[i][j] = mu;
-                    g[i][j] = 0.0f;
-                }
-            }
+            const int c = Cols<VEC, TPR>(i, lane, d).c;
+            load_loose<VEC, T>(xh[i], x + c);
+            load_loose<VEC, T>(g[i], dy + c);
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -230,46 +239,40 @@ __global__ __launch_bounds__(THREADS) void norm_back_kernel(NormArgs a)
             T *dx = (T *)a.y + row * (int64_t)d;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int c = (i * TPR + lane) * VEC;
-                if (c >= d) continue;
+                const Cols<VEC, TPR> at(i, lane, d);
                 float o[VEC];
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) o[j] = r * (g[i][j] - c1 - xh[i][j] * c2);
-                store_f32<VEC, T>(dx + c, o);
+                if (WHOLE ? at.any() : at.skip == 0) {
+                    store_loose<VEC, T>(dx + at.c, o);
+                } else if (at.any()) {   // the first columns are the thread's before, whose g is here 0
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j)
+                        if (at.template mine<WHOLE>(j)) dx[at.c + j] = (T)o[j];
+                }
             }
         }
     }
     if constexpr (DP) {
         float *out = a.partial + (int64_t)blockIdx.x * 2 * d;
-        if constexpr (GROUPS == 1) {
+        for (int k = 0; k < GROUPS; ++k) {   // the block's waves with a row each, added in order
+            if (group == k) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = (i * TPR + lane) * VEC;
-                if (c >= d) continue;
+                for (int i = 0; i < NV; ++i) {
+                    const Cols<VEC, TPR> at(i, lane, d);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    out[c + j] = dw[i][j];
-                    out[d + c + j] = db[i][j];
-                }
-            }
-        } else {
-            for (int k = 0; k < GROUPS; ++k) {   // the block's rows of waves added in wave order
-                if (group == k) {
-#pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        const int c = (i * TPR + lane) * VEC;
-                        if (c >= d) continue;
-#pragma unroll
-                        for (int j = 0; j < VEC; ++j) {
-                            cols[c + j] = k ? cols[c + j] + dw[i][j] : dw[i][j];
-                            cols[d + c + j] = k ? cols[d + c + j] + db[i][j] : db[i][j];
-                        }
+                    for (int j = 0; j < VEC; ++j) {
+                        if (!at.template mine<WHOLE>(j)) continue;
+                        float *tw = (GROUPS == 1 ? out : cols) + at.c + j, *tb = tw + d;
+                        *tw = k ? *tw + dw[i][j] : dw[i][j];
+                        *tb = k ? *tb + db[i][j] : db[i][j];
                     }
                 }
-                __syncthreads();
             }
-            for (int c = threadIdx.x; c < 2 * d; c += THREADS) out[c] = cols[c];
+            if (GROUPS > 1) __syncthreads();
         }
+        if (GROUPS > 1)
+            for (int c = threadIdx.x; c < 2 * d; c += THREADS) out[c] = cols[c];
     }
 }
 
@@ -358,40 +361,27 @@ int with_types(int32_t dtype, int32_t param, F f)
     return param == BOA_T_F32 ? f(f16_t{}, 0.0f) : f(f16_t{}, f16_t{});
 }
 
-// The registers a row takes: f(VEC, NV, TPR) as compile-time constants.
-// Vector loads where every row allows them. A wave per row up to 4 loads a
-// lane, then a block per row; false where a row does not fit.
+// The registers a row takes: f(NV, TPR, WHOLE) as compile-time constants. A
+// wave per row up to 4 loads a lane, then a block per row; false where a row
+// does not fit, or is shorter than a load.
 template <int V>
 struct Int {
     static constexpr int value = V;
 };
 
-template <int VECMAX, class F>
-bool with_shape(int32_t d, bool vec, F f)
+template <int VEC, class F>
+bool with_shape(int32_t d, F f)
 {
-    if (vec) {
-        const int64_t n = ceil_div(d, VECMAX);
-        if (n <= 64) f(Int<VECMAX>{}, Int<1>{}, Int<64>{});
-        else if (n <= 128) f(Int<VECMAX>{}, Int<2>{}, Int<64>{});
-        else if (n <= 192) f(Int<VECMAX>{}, Int<3>{}, Int<64>{});
-        else if (n <= 256) f(Int<VECMAX>{}, Int<4>{}, Int<64>{});
-        else if (n <= 512) f(Int<VECMAX>{}, Int<2>{}, Int<256>{});
-        else if (n <= 1024) f(Int<VECMAX>{}, Int<4>{}, Int<256>{});
-        else return false;
-        return true;
-    }
-    if (d <= 128) f(Int<1>{}, Int<2>{}, Int<64>{});
-    else if (d <= 256) f(Int<1>{}, Int<4>{}, Int<64>{});
-    else if (d <= 512) f(Int<1>{}, Int<8>{}, Int<64>{});
-    else if (d <= 1024) f(Int<1>{}, Int<16>{}, Int<64>{});
-    else if (d <= 4096) f(Int<1>{}, Int<16>{}, Int<256>{});
-    else return false;
+    const int64_t n = ceil_div(d, VEC);
+    if (d < VEC || n > 1024) return false;
+    auto whole = [&](auto nv, auto tpr) { d % VEC ? f(nv, tpr, Int<0>{}) : f(nv, tpr, Int<1>{}); };
+    if (n <= 64) whole(Int<1>{}, Int<64>{});
+    else if (n <= 128) whole(Int<2>{}, Int<64>{});
+    else if (n <= 192) whole(Int<3>{}, Int<64>{});
+    else if (n <= 256) whole(Int<4>{}, Int<64>{});
+    else if (n <= 512) whole(Int<2>{}, Int<256>{});
+    else whole(Int<4>{}, Int<256>{});
     return true;
-}
-
-bool rows_allow(const void *p, int64_t stride, int64_t esize)
-{
-    return aligned(p, 16) && (stride * esize) % 16 == 0;
 }
 
 int check_norm(const char *what, const void *x, int64_t rows, int32_t d, int64_t x_stride, int32_t dtype, int32_t param,
@@ -435,13 +425,12 @@ int boa_layer_norm(const void *x, int64_t rows, int32_t d, int64_t x_stride, int
     return with_types(dtype, (weight || bias) ? param_dtype : dtype, [&](auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
-        constexpr int VMAX = 16 / sizeof(T);
-        const bool vec = d % VMAX == 0 && rows_allow(x, x_stride, sizeof(T)) && aligned(y, 16) && aligned(weight, 16)
-                         && aligned(bias, 16);
-        const bool fits = with_shape<VMAX>(d, vec, [&](auto ve, auto nv, auto tpr) {
-            constexpr int VEC = decltype(ve)::value, NV = decltype(nv)::value, TPR = decltype(tpr)::value;
+        constexpr int VEC = 16 / sizeof(T);
+        const bool fits = with_shape<VEC>(d, [&](auto nv, auto tpr, auto whole) {
+            constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value;
+            constexpr bool WHOLE = decltype(whole)::value;
             const int64_t blocks = ceil_div(rows, THREADS / TPR);
-            norm_kernel<T, P, VEC, NV, TPR><<<dim3((uint32_t)blocks), THREADS, 0, st>>>(a);
+            norm_kernel<T, P, NV, TPR, WHOLE><<<dim3((uint32_t)blocks), THREADS, 0, st>>>(a);
         });
         if (!fits) norm_wide_kernel<T, P><<<dim3((uint32_t)rows), THREADS, 0, st>>>(a);
         return launch_status("layer_norm");
@@ -474,17 +463,16 @@ int boa_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, in
     return with_types(dtype, (weight || params) ? param_dtype : dtype, [&](auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
-        constexpr int VMAX = 16 / sizeof(T);
-        const bool vec = d % VMAX == 0 && rows_allow(x, x_stride, sizeof(T)) && rows_allow(dy, dy_stride, sizeof(T))
-                         && aligned(dx, 16) && aligned(weight, 16);
+        constexpr int VEC = 16 / sizeof(T);
         const int64_t blocks = back_blocks(rows, d);
-        const bool fits = with_shape<VMAX>(d, vec, [&](auto ve, auto nv, auto tpr) {
-            constexpr int VEC = decltype(ve)::value, NV = decltype(nv)::value, TPR = decltype(tpr)::value;
+        const bool fits = with_shape<VEC>(d, [&](auto nv, auto tpr, auto whole) {
+            constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value;
+            constexpr bool WHOLE = decltype(whole)::value;
             const size_t lds = TPR < THREADS ? (size_t)2 * d * sizeof(float) : 0;
             if (params)
-                norm_back_kernel<T, P, VEC, NV, TPR, true><<<dim3((uint32_t)blocks), THREADS, lds, st>>>(a);
+                norm_back_kernel<T, P, NV, TPR, WHOLE, true><<<dim3((uint32_t)blocks), THREADS, lds, st>>>(a);
             else
-                norm_back_kernel<T, P, VEC, NV, TPR, false><<<dim3((uint32_t)blocks), THREADS, 0, st>>>(a);
+                norm_back_kernel<T, P, NV, TPR, WHOLE, false><<<dim3((uint32_t)blocks), THREADS, 0, st>>>(a);
         });
         if (!fits) {
             if (dx && rows) norm_back_wide_kernel<T, P><<<dim3((uint32_t)rows), THREADS, 0, st>>>(a);

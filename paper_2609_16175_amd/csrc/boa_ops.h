@@ -52,6 +52,35 @@ __device__ inline void store_f32(T *p, const float (&from)[N])
     *reinterpret_cast<Pack<N, T> *>(p) = a;
 }
 
+// The same at any element's address: 16-byte loads and stores need no alignment
+// above two bytes.
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+typedef words4 loose4 __attribute__((aligned(2)));
+
+template <int N, class T>
+__device__ inline void load_loose(float (&to)[N], const T *p)
+{
+    constexpr int V = 16 / sizeof(T);
+    static_assert(N % V == 0, "whole 16-byte loads");
+#pragma unroll
+    for (int k = 0; k < N; k += V) {
+        const words4 w = *reinterpret_cast<const loose4 *>(p + k);
+        const Pack<V, T> a = __builtin_bit_cast(Pack<V, T>, w);
+#pragma unroll
+        for (int i = 0; i < V; ++i) to[k + i] = (float)a.v[i];
+    }
+}
+
+template <int N, class T>
+__device__ inline void store_loose(T *p, const float (&from)[N])
+{
+    static_assert(N * sizeof(T) == 16, "one 16-byte store");
+    Pack<N, T> a;
+#pragma unroll
+    for (int i = 0; i < N; ++i) a.v[i] = (T)from[i];
+    *reinterpret_cast<loose4 *>(p) = __builtin_bit_cast(words4, a);
+}
+
 __device__ inline float wave_sum(float v)
 {
 #pragma unroll
