@@ -613,3 +613,21 @@ def test_binding_refuses():
             bad()
     with pytest.raises(TypeError):
         boa.layer_norm(x.double())
+
+
+# ---------------------------------------------------------------------------
+# the operators together
+
+def test_query_tower_example():
+    from examples import query_tower
+    from workloads import rows4
+    r = query_tower.main(["--steps", "60", "--points", "3000"])
+    assert r["last"] < 0.5 * r["first"] and r["found"] > 0.8 and r["found_4bit"] > 0.7
+    # the served vectors are the tower's with the weights that the codes stand for
+    w4 = rows4.dequantize(*rows4.quantize(r["W"], group=32)).double()
+    w, b = (t.detach().double() for t in r["norm"])
+    x = r["x"].double()
+    c = x - x.mean(1, keepdim=True)
+    y = c / torch.sqrt((c * c).mean(1, keepdim=True) + 1e-5) * w + b
+    err = (r["served"].double() - y @ w4.t()).abs()
+    assert (err <= 1e-5 * (y.abs() @ w4.abs().t()) + 1e-5).all()
