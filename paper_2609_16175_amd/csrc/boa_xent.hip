@@ -694,8 +694,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void prob_kernel(ProbArgs a)
 
 struct DhArgs {
     Product pr;              // a: probabilities, b: the piece's points, across
-    float *part;             // splits x rows_pad x d
-    int32_t d, rows_pad, tiles_b, tiles_d, splits, k_split, first;
+    float *part;             // splits x rows_pad x ld
+    int32_t d, ld, rows_pad, tiles_b, tiles_d, splits, k_split, first;
 };
 
 // A split's share of sum_v p_bv c_v over the piece, added to what earlier
@@ -722,7 +722,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void dh_kernel(DhArgs a)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int32_t b = tb * S::BM + (wm * S::TM + i) * 32 + tile_row(e, half);
-                float *to = a.part + ((int64_t)split * a.rows_pad + b) * a.d + c;
+                float *to = a.part + ((int64_t)split * a.rows_pad + b) * a.ld + c;
                 *to = a.first ? acc[i][j][e] : *to + acc[i][j][e];
             }
         }
@@ -749,27 +749,46 @@ __global__ __launch_bounds__(S::THREADS, 2) void dc_kernel(DcArgs a)
     f32x16 acc[S::TM][S::TN];
     clear<S>(acc);
     tile_product<S, true, true>(a.pr, tv * S::BM, td * S::BN, lds, acc, 0, a.pr.K);
+    // out by way of LDS, a row of the waves' tiles at a time, so that rows are
+    // written 16 bytes a lane (with single values the launch took twice as long
+    // at 384 queries)
     const float by = a.scale * *a.factor;
+    constexpr int LD = S::BN + 4, ROWS = S::WM * 32, V = 16 / sizeof(T);
+    float *rows = (float *)lds;   // ROWS x LD
+    const bool whole = a.d % V == 0 && aligned16(a.out);
 #pragma unroll
-    for (int i = 0; i < S::TM; ++i)
+    for (int i = 0; i < S::TM; ++i) {
+        if (i) __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int32_t v = tv * S::BM + (wm * S::TM + i) * 32 + tile_row(e, half);
-            if (v >= a.n) continue;
+        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) rows[(wm * 32 + tile_row(e, half)) * LD + (wn * S::TN + j) * 32 + r] = acc[i][j][e];
+        __syncthreads();
+        for (int at = threadIdx.x; at < ROWS * (S::BN / V); at += S::THREADS) {
+            const int row = at / (S::BN / V), col = at % (S::BN / V) * V;
+            const int32_t v = tv * S::BM + (row / 32 * S::TM + i) * 32 + row % 32, c = td * S::BN + col;
+            if (v >= a.n || c >= a.d) continue;
+            float x[V];
+#pragma unroll
+            for (int k = 0; k < V; k += 4) load_f32<4, float>(*(float(*)[4])(x + k), rows + row * LD + col + k);
             const int32_t first = a.first[a.v0 + v];
 #pragma unroll
-            for (int j = 0; j < S::TN; ++j) {
-                const int32_t c = td * S::BN + (wn * S::TN + j) * 32 + r;
-                if (c >= a.d) continue;
-                float x = acc[i][j][e];
-                if (first >= 0) x += a.own[(int64_t)first * a.d + c];
-                ((T *)a.out)[(int64_t)v * a.d + c] = (T)(by * x);
+            for (int k = 0; k < V; ++k) {
+                if (first >= 0 && c + k < a.d) x[k] += a.own[(int64_t)first * a.d + c + k];
+                x[k] *= by;
+            }
+            T *to = (T *)a.out + (int64_t)v * a.d + c;
+            if (whole) {
+                store_f32<V, T>(to, x);
+            } else {
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    if (c + k < a.d) to[k] = (T)x[k];
             }
         }
+    }
 }
 
-// A block per query b that is its point's first: own[b] = sum over the point's
-// queries, in order, of coef * h; first[point] = b; own_bias[b] likewise.
 struct OwnArgs {
     const void *h;
     int64_t h_stride;
@@ -780,7 +799,7 @@ struct OwnArgs {
     float *own, *own_bias;   // own may be null
 };
 
-template <class T>
+template <class T, int TH>
 __device__ inline void own_terms(const OwnArgs &a, int32_t b)
 {
     const T *h = (const T *)a.h;
@@ -790,21 +809,21 @@ __device__ inline void own_terms(const OwnArgs &a, int32_t b)
     int32_t *first = a.first;
     float *own = a.own, *own_bias = a.own_bias;
     __shared__ int earlier;
-    __shared__ int32_t list[256];
+    __shared__ int32_t list[TH];
     __shared__ int count;
     const int32_t y = label[b];
     if (y < 0) return;
     if (threadIdx.x == 0) earlier = 0;
     __syncthreads();
-    for (int32_t i = threadIdx.x; i < b; i += 256)
+    for (int32_t i = threadIdx.x; i < b; i += TH)
         if (label[i] == y) earlier = 1;
     __syncthreads();
     if (earlier) return;
     float sb = 0.0f;
-    float acc[BOA_MAX_XENT_D / 256];
+    float acc[BOA_MAX_XENT_D / TH];
 #pragma unroll
-    for (int k = 0; k < BOA_MAX_XENT_D / 256; ++k) acc[k] = 0.0f;
-    for (int32_t i0 = b; i0 < B; i0 += 256) {
+    for (int k = 0; k < BOA_MAX_XENT_D / TH; ++k) acc[k] = 0.0f;
+    for (int32_t i0 = b; i0 < B; i0 += TH) {
         // the queries of this stretch that share the label, in order
         __syncthreads();
         if (threadIdx.x == 0) count = 0;
@@ -812,7 +831,7 @@ __device__ inline void own_terms(const OwnArgs &a, int32_t b)
         const int32_t i = i0 + threadIdx.x;
         const bool hit = i < B && label[i] == y;
         const uint64_t in_wave = __ballot(hit);
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < TH / 64; ++w) {
             if ((threadIdx.x >> 6) == w && in_wave) {
                 const int at = count + __popcll(in_wave & ((1ull << (threadIdx.x & 63)) - 1));
                 if (hit) list[at] = i;
@@ -826,14 +845,14 @@ __device__ inline void own_terms(const OwnArgs &a, int32_t b)
             const float c = coef[q];
             sb += c;
 #pragma unroll
-            for (int k = 0; k < BOA_MAX_XENT_D / 256; ++k)
-                if (k * 256 + (int)threadIdx.x < d)
-                    acc[k] = fmaf(c, (float)h[(int64_t)q * h_stride + k * 256 + threadIdx.x], acc[k]);
+            for (int k = 0; k < BOA_MAX_XENT_D / TH; ++k)
+                if (k * TH + (int)threadIdx.x < d)
+                    acc[k] = fmaf(c, (float)h[(int64_t)q * h_stride + k * TH + threadIdx.x], acc[k]);
         }
     }
 #pragma unroll
-    for (int k = 0; k < BOA_MAX_XENT_D / 256; ++k)
-        if (k * 256 + (int)threadIdx.x < d && own) own[(int64_t)b * d + k * 256 + threadIdx.x] = acc[k];
+    for (int k = 0; k < BOA_MAX_XENT_D / TH; ++k)
+        if (k * TH + (int)threadIdx.x < d && own) own[(int64_t)b * d + k * TH + threadIdx.x] = acc[k];
     if (threadIdx.x == 0) {
         first[y] = b;
         own_bias[b] = sb;
@@ -843,7 +862,7 @@ __device__ inline void own_terms(const OwnArgs &a, int32_t b)
 template <class T>
 __global__ __launch_bounds__(256) void own_kernel(OwnArgs a)
 {
-    own_terms<T>(a, blockIdx.x);
+    own_terms<T, 256>(a, blockIdx.x);
 }
 
 __global__ __launch_bounds__(256) void dbias_kernel(const float *col, int32_t tiles_b, int32_t cols_pad, int32_t n,
@@ -859,21 +878,33 @@ __global__ __launch_bounds__(256) void dbias_kernel(const float *col, int32_t ti
     out[v] = s * *factor;
 }
 
-// dh = scale factor (sum of the splits + coef c_label)
+// dh = scale factor (sum of the splits + coef c_label), four values a thread
+// (ld, a multiple of 4, is the splits' row)
 template <class T>
 __global__ __launch_bounds__(256) void dh_join_kernel(const float *part, int32_t splits, int32_t rows_pad, int32_t B,
-                                                      int32_t d, const T *points, int64_t points_stride,
+                                                      int32_t d, int32_t ld, const T *points, int64_t points_stride,
                                                       const int32_t *label, const float *coef, const float *factor,
                                                       float scale, T *dh)
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (int64_t)B * d) return;
-    const int32_t b = (int32_t)(i / d), c = (int32_t)(i % d);
-    float s = 0.0f;
-    for (int32_t k = 0; k < splits; ++k) s += part[((int64_t)k * rows_pad + b) * d + c];
+    if (i >= (int64_t)B * (ld / 4)) return;
+    const int32_t b = (int32_t)(i / (ld / 4)), c = (int32_t)(i % (ld / 4)) * 4;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int32_t k = 0; k < splits; ++k) {
+        float v[4];
+        load_f32<4, float>(v, part + ((int64_t)k * rows_pad + b) * ld + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += v[e];
+    }
     const int32_t y = label[b];
-    if (y >= 0) s = fmaf(coef[b], (float)points[(int64_t)y * points_stride + c], s);
-    dh[i] = (T)(scale * *factor * s);
+    const float by = scale * *factor;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (c + e >= d) break;
+        if (y >= 0) s[e] = fmaf(coef[b], (float)points[(int64_t)y * points_stride + c + e], s[e]);
+        dh[(int64_t)b * d + c + e] = (T)(by * s[e]);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -920,7 +951,8 @@ struct Sweep {
     static constexpr int KS = 2 * DT, SHED = MODE != SWEEP_LOSS && PARTS * TN * DT >= 8 ? (MODE == SWEEP_H ? 2 : 1) : 0;
     static constexpr size_t lds()
     {
-        return std::max<size_t>(2 * STAGE + SHED * TN * PARTS * SWEEP_THREADS * 16, MODE == SWEEP_C ? 4 * 32 * OUT_LD * 4 : 0);
+        return std::max<size_t>(2 * STAGE + SHED * TN * PARTS * SWEEP_THREADS * 16,
+                                MODE == SWEEP_C ? 4 * 32 * OUT_LD * 4 : WS > 1 ? WS * 32 * (OUT_LD + 2) * 4 : 0);
     }
 };
 
@@ -937,8 +969,8 @@ struct SweepArgs {
     const float *top, *rowf;  // padded (SWEEP_C)
     const int32_t *label;     // of the queries, padded
     float *pick;              // the label's logit, base 2
-    RowState *part;           // (splits * WS) x N
-    float *out;               // (splits * WS) x N x DT * 32 partial outputs
+    RowState *part;           // splits x N
+    float *out;               // splits x N x DT * 32 partial outputs
     float *col;               // splits x N partial sums of p, or null
     // SWEEP_C in one split: the results themselves
     void *dc;
@@ -1297,7 +1329,41 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
 
 #pragma unroll
     for (int j = 0; j < TN; ++j) sum[j] += __shfl_xor(sum[j], 32);
-    const int64_t share = (int64_t)split * S::WS + ws;
+    if constexpr (S::WS > 1) {   // the waves that share these rows: brought to one maximum and added, in order
+        constexpr int ROW = DT * 32 + 4;
+        float *mine = (float *)smem + ws * 32 * (ROW + 2) + r * (ROW + 2);   // out, then maximum and sum; TN is 1
+        if constexpr (S::MODE == SWEEP_H)
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) mine[i * 32 + tile_row(e, half)] = out[i][0][e];
+        if (half == 0) {
+            mine[ROW] = mx[0];
+            mine[ROW + 1] = sum[0];
+        }
+        __syncthreads();
+        if (ws) return;
+        float by[S::WS], top = mx[0];
+#pragma unroll
+        for (int w = 1; w < S::WS; ++w) top = fmaxf(top, mine[w * 32 * (ROW + 2) + ROW]);
+#pragma unroll
+        for (int w = 0; w < S::WS; ++w) by[w] = __builtin_amdgcn_exp2f(mine[w * 32 * (ROW + 2) + ROW] - top);
+        mx[0] = top;
+        sum[0] *= by[0];
+#pragma unroll
+        for (int w = 1; w < S::WS; ++w) sum[0] = fmaf(by[w], mine[w * 32 * (ROW + 2) + ROW + 1], sum[0]);
+        if constexpr (S::MODE == SWEEP_H)
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    out[i][0][e] *= by[0];
+#pragma unroll
+                    for (int w = 1; w < S::WS; ++w)
+                        out[i][0][e] = fmaf(by[w], mine[w * 32 * (ROW + 2) + i * 32 + tile_row(e, half)], out[i][0][e]);
+                }
+    }
+    const int64_t share = split;
     if constexpr (S::MODE != SWEEP_C) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -1416,14 +1482,15 @@ struct DhShares {
 
 // A block per query: ld / 4 threads take four values each, and as many times as
 // they fit the block they part the shares, whose sums are then added in order.
-template <class T>
+template <class T, int TH>
 __device__ inline void dh_of_shares(const DhShares &a, const OwnArgs &o, int32_t b)
 {
-    __shared__ float part[256 * 4];
-    const int cols = a.ld / 4, slices = 256 / cols, col = threadIdx.x % cols, slice = threadIdx.x / cols;
+    __shared__ float part[TH * 4];
+    const int cols = a.ld / 4, slices = TH / cols, col = threadIdx.x % cols, slice = threadIdx.x / cols;
     const float f = a.rowf[b], m = a.top[b];
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (f != 0.0f && slice < slices)
+#pragma unroll 4
         for (int32_t k = slice; k < a.shares; k += slices) {
             const int64_t at = (int64_t)k * o.B + b;
             float v[4];
@@ -1444,13 +1511,14 @@ __device__ inline void dh_of_shares(const DhShares &a, const OwnArgs &o, int32_t
     ((T *)a.dh)[(int64_t)b * o.d + c] = (T)(a.scale * *a.factor * sum);
 }
 
-// Between the sweeps: a block per query and task.
-template <class T>
-__global__ __launch_bounds__(256) void between_kernel(OwnArgs o, DhShares s)
+// Between the sweeps: a block per query and task. TH: 1024 threads where there
+// are many shares to add, which are many where there are few queries.
+template <class T, int TH>
+__global__ __launch_bounds__(TH) void between_kernel(OwnArgs o, DhShares s)
 {
     const int32_t b = (int32_t)blockIdx.x >= o.B ? blockIdx.x - o.B : blockIdx.x;
-    if (s.dh && (int32_t)blockIdx.x < o.B) dh_of_shares<T>(s, o, b);
-    else if (o.first) own_terms<T>(o, b);
+    if (s.dh && (int32_t)blockIdx.x < o.B) dh_of_shares<T, TH>(s, o, b);
+    else if (o.first) own_terms<T, TH>(o, b);
 }
 
 // ---------------------------------------------------------------------------
@@ -1498,7 +1566,7 @@ Plan make_plan(const boa_xent *x, bool grad)
         p.ld = (int32_t)round_up(x->d, 32);
         // up to 32 queries the waves of a block share them and part the points
         p.tile_b = p.parts == 1 ? (x->B <= 32 ? 32 : x->B <= 128 ? 128 : 256) : 128;
-        const int32_t ws = p.tile_b == 32 ? 4 : 1, rows = p.tile_b == 32 ? 128 : p.parts == 1 ? 64 : 32;
+        const int32_t rows = p.tile_b == 32 ? 128 : p.parts == 1 ? 64 : 32;
         p.tiles_b = (int32_t)ceil_div(x->B, p.tile_b);
         p.rows_pad = (int32_t)round_up(x->B, 256);
         const int64_t stages = ceil_div(x->V, rows);
@@ -1508,7 +1576,7 @@ Plan make_plan(const boa_xent *x, bool grad)
         splits = std::min(splits, stages);
         p.per_split = (int32_t)ceil_div(stages, splits);
         p.splits = (int32_t)ceil_div(stages, p.per_split);
-        p.shares = p.splits * ws;
+        p.shares = p.splits;
         p.off_bias = take(round_up(x->V, 128) * 4);
         p.off_h = take((int64_t)p.parts * p.rows_pad * p.ld * 2);
         if (x->dtype == BOA_T_BF16 && !p.direct) p.off_c = take(x->V * (int64_t)p.ld * 2);
@@ -1571,7 +1639,7 @@ Plan make_plan(const boa_xent *x, bool grad)
             const int64_t want = std::max<int64_t>(1, (p.tile_b == 256 && p.tile_d == 256 ? 256 : 512) / tiles);
             p.dh_k = (int32_t)round_up(ceil_div(p.cols_pad, std::min(want, ceil_div(p.cols_pad, 256))), 64);
             p.dh_splits = (int32_t)ceil_div(p.cols_pad, p.dh_k);
-            p.off_dh = take((int64_t)p.dh_splits * p.rows_pad * x->d * 4);
+            p.off_dh = take((int64_t)p.dh_splits * p.rows_pad * p.Kp * 4);
         }
         if (dh || dc) p.off_p = take(per * p.cols_pad);
         if (dc || db) p.off_hz = take((int64_t)p.parts * p.rows_pad * p.Kp * 2);
@@ -1791,7 +1859,11 @@ int run_sweeps(const Work<T> &w)
         shares.scale = x->scale, shares.dh = x->dh;
     }
     if (dh || w.want_c())
-        between_kernel<T><<<dim3((uint32_t)(dh && w.want_c() ? 2 * B : B)), 256, 0, st>>>(own, shares);
+    {
+        const dim3 grid((uint32_t)(dh && w.want_c() ? 2 * B : B));
+        if (p.shares > 64) between_kernel<T, 1024><<<grid, 1024, 0, st>>>(own, shares);
+        else between_kernel<T, 256><<<grid, 256, 0, st>>>(own, shares);
+    }
     if (w.want_c()) {
         SweepArgs g = c;
         g.n = c.m, g.nf = c.mf, g.n_ld = c.m_ld, g.N = V, g.M = B, g.d = d;
@@ -1911,7 +1983,7 @@ int run_tiles(const Work<T> &w)
             g.pr.K = tiles_v * 256;
             g.pr.part_a = p_part, g.pr.part_b = c_part;
             g.part = (float *)(ws + p.off_dh);
-            g.d = d, g.rows_pad = p.rows_pad, g.tiles_b = p.tiles_b, g.splits = p.dh_splits, g.k_split = p.dh_k, g.first = i == 0;
+            g.d = d, g.ld = p.Kp, g.rows_pad = p.rows_pad, g.tiles_b = p.tiles_b, g.splits = p.dh_splits, g.k_split = p.dh_k, g.first = i == 0;
             g.tiles_d = p.tiles_d;
             with_tile(p.tile_b, [&](auto bm) {
                 constexpr int BM = decltype(bm)::value;
@@ -1945,8 +2017,8 @@ int run_tiles(const Work<T> &w)
         }
     }
     if (x->dh)
-        dh_join_kernel<T><<<dim3((uint32_t)ceil_div((int64_t)B * d, 256)), 256, 0, st>>>(
-            (const float *)(ws + p.off_dh), p.dh_splits, p.rows_pad, B, d, (const T *)x->points, x->points_stride, label,
+        dh_join_kernel<T><<<dim3((uint32_t)ceil_div((int64_t)B * (p.Kp / 4), 256)), 256, 0, st>>>(
+            (const float *)(ws + p.off_dh), p.dh_splits, p.rows_pad, B, d, p.Kp, (const T *)x->points, x->points_stride, label,
             coef, factor, x->scale, (T *)x->dh);
     return launch_status("softmax_xent_grad");
 }
