@@ -131,10 +131,10 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void rows4_kernel(FastArgs f)
     constexpr int PARTS = parts_v<T>, VALS = NC * 4 / PARTS;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const VecArgs &a = f.v;
-    // x: [step][piece j of 4][set][chunk][slot][8 k] bf16; sums: [step][set][chunk][slot]; then 16 zero bytes
+    // x: [step][piece j of 4][set][chunk][slot][8 k] bf16; sums: [step][set][chunk][slot]; then a step of zeros
     bf16x8 *xs = (bf16x8 *)lds;
     f32x4 *sums = (f32x4 *)(lds + (size_t)f.stretch * NC * 1024);
-    const int zero_at = f.stretch * NC * 68;   // in units of 16 bytes: past x and the sums
+    const int zero_at = f.stretch * NC * 68;   // in units of 16 bytes: past x and the sums, NC * 64 of them
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunk = lane >> 4, r = lane & 15;
     const int split = wave % f.split_k, per_block = FAST_WAVES / f.split_k;
     const int64_t tiles = (a.rows + ROWS_W - 1) / ROWS_W;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void rows4_kernel(FastArgs f)
             }
             xs[((step * 4 + j) * NC + set) * 16 + c * 4 + slot] = to;
         }
-        if (threadIdx.x == 0) ((u32x4 *)lds)[zero_at] = u32x4{0, 0, 0, 0};
+        for (int i = threadIdx.x; i < NC * 64; i += 64 * FAST_WAVES) ((u32x4 *)lds)[zero_at + i] = u32x4{0, 0, 0, 0};
         __syncthreads();
         for (int i = threadIdx.x; i < f.stretch * NC * 16; i += 64 * FAST_WAVES) {
             const int at = i & 15, set = (i >> 4) % NC, step = i / (16 * NC);
@@ -209,7 +209,13 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void rows4_kernel(FastArgs f)
             if (OFFSETS) to.o[t] = ((const SC *)a.offsets)[rows.sc[t] + g];
         }
     };
-    const int x_at = (r >> 2) == chunk ? chunk * 4 + (r & 3) : -1;   // where this lane's x lies; else the zeros
+    // where this lane's x lies in a step: in its own chunk's slots, else among the zeros, which all steps share
+    const bool mine = (r >> 2) == chunk;
+    const int x_at = mine ? chunk * 4 + (r & 3) : zero_at, x_step = mine ? NC * 64 : 0;
+    // in registers, so that masking and setting the exponent are one instruction
+    uint32_t four_bits = 0x00780078u, sixteen = 0x41804180u;
+    asm volatile("" : "+v"(four_bits));
+    asm volatile("" : "+s"(sixteen));
     float y[2][NC * 4];
     auto multiply = [&](const Loaded &from, int at) {   // at: the step's place in LDS
         f32x4 acc[2][NC], xsum[NC];
@@ -228,15 +234,15 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void rows4_kernel(FastArgs f)
             for (int t = 0; t < 2; ++t) {
                 const uint32_t q = from.w[t][j];
                 u32x4 e;
-                e[0] = ((q << 3) & 0x00780078u) | 0x41804180u;
-                e[1] = ((q >> 1) & 0x00780078u) | 0x41804180u;
-                e[2] = ((q >> 5) & 0x00780078u) | 0x41804180u;
-                e[3] = ((q >> 9) & 0x00780078u) | 0x41804180u;
+                e[0] = ((q << 3) & four_bits) | sixteen;
+                e[1] = ((q >> 1) & four_bits) | sixteen;
+                e[2] = ((q >> 5) & four_bits) | sixteen;
+                e[3] = ((q >> 9) & four_bits) | sixteen;
                 b[t] = __builtin_bit_cast(bf16x8, e);
             }
 #pragma unroll
             for (int n = 0; n < NC; ++n) {
-                const bf16x8 x = xs[x_at >= 0 ? ((at * 4 + j) * NC + n) * 16 + x_at : zero_at];
+                const bf16x8 x = xs[x_at + at * x_step + (j * NC + n) * 16];
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
                     acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, b[t], acc[t][n], 0, 0, 0);
@@ -370,7 +376,7 @@ void launch_fast(FastArgs f, hipStream_t st)
 {
     const VecArgs &a = f.v;
     f.steps = (int32_t)ceil_div(a.K, 128);
-    f.stretch = (int32_t)std::min<int64_t>(f.steps, (FAST_LDS - 16) / step_bytes(NC));
+    f.stretch = (int32_t)std::min<int64_t>(f.steps, (FAST_LDS - NC * 1024) / step_bytes(NC));
     // exact for the at most 2^15 chunks of a row
     const int32_t per_group = a.group / 32;
     f.group_inv = per_group == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + per_group - 1) / per_group);
@@ -380,7 +386,7 @@ void launch_fast(FastArgs f, hipStream_t st)
     f.split_k = 1;
     while (f.split_k < FAST_WAVES && f.split_k * 2 <= f.steps && tiles * f.split_k < 512 * FAST_WAVES) f.split_k *= 2;
     const int64_t blocks = std::min<int64_t>(ceil_div(tiles, FAST_WAVES / f.split_k), f.split_k > 1 ? 4096 : 512);
-    size_t lds = (size_t)f.stretch * step_bytes(NC) + 16;
+    size_t lds = (size_t)f.stretch * step_bytes(NC) + NC * 1024;
     if (f.split_k > 1) lds = std::max(lds, (size_t)FAST_WAVES * NC * 2 * 64 * sizeof(float));
     if (a.offsets) rows4_kernel<T, SC, NC, true><<<dim3((uint32_t)blocks), 64 * FAST_WAVES, lds, st>>>(f);
     else rows4_kernel<T, SC, NC, false><<<dim3((uint32_t)blocks), 64 * FAST_WAVES, lds, st>>>(f);
