@@ -13,7 +13,6 @@
 #include <vector>
 
 #include "boa_internal.h"
-#include "boa_ops.h"
 
 using namespace boa;
 
@@ -159,8 +158,6 @@ struct boa_index {
     };
     mutable Occupancy occ[256] = {};
 };
-
-int boa::set_error(int code, const char *msg) { return fail(code, msg); }
 
 extern "C" {
 

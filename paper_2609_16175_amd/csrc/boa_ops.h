@@ -9,8 +9,14 @@
 
 namespace boa {
 
-// boa_api.hip: records the thread's error message and returns the code
-int set_error(int code, const char *msg);
+// Records the thread's error message and returns the code. boa_last_error()
+// gives the thread's buffer (boa_api.hip's g_err, 512 characters); nobody else
+// holds it while a call of this thread runs.
+inline int set_error(int code, const char *msg)
+{
+    __builtin_snprintf(const_cast<char *>(boa_last_error()), 512, "%s", msg);
+    return code;
+}
 
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
