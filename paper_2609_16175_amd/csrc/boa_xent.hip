@@ -1717,7 +1717,7 @@ int check(const boa_xent *x, bool grad)
         return set_error(BOA_EUNSUPPORTED, "softmax_xent: float16 does not hold the probabilities of many points; use bfloat16 or float32");
     if (x->dtype != BOA_T_F32 && x->dtype != BOA_T_BF16) return bad("softmax_xent: unknown dtype");
     if (x->d < 1 || x->d > BOA_MAX_XENT_D) return bad("softmax_xent: d out of range [1, 4096]");
-    if (x->B < 0 || x->B > ((int64_t)1 << 31) - (1 << 16)) return bad("softmax_xent: B out of range");
+    if (x->B < 0 || x->B > (1 << 24)) return bad("softmax_xent: B out of range [0, 2^24]");
     if (x->V < 1 || x->V > ((int64_t)1 << 31) - (1 << 16)) return bad("softmax_xent: V out of range");
     if (x->reduction < BOA_REDUCE_NONE || x->reduction > BOA_REDUCE_MEAN) return bad("softmax_xent: unknown reduction");
     if ((x->B > 1 && x->h_stride < x->d) || (x->V > 1 && x->points_stride < x->d))
