@@ -51,6 +51,8 @@ struct Operand {
     const bf16_t *p;
     int64_t ld;
     int32_t rows, cols;
+    const float *f;   // float32 rows in place of p, split into parts on the way to LDS: `cols` values
+    int32_t vec;      // and whether 16 bytes of them may be read at a time
 };
 
 // A product of K values (a multiple of 16). With parts, the operands' parts
@@ -71,10 +73,14 @@ struct Shape {
     static constexpr int BK = PARTS == 1 ? 32 : 16;
     static constexpr int STAGE = (BM + BN) * BK * PARTS;   // bf16 values
     static constexpr int ROOM = (THREADS == 512 ? 150 : 75) * 1024 / (STAGE * 2);
-    static constexpr int STAGES = ROOM > 4 ? 4 : ROOM;
-    static constexpr int LOADS = (BM + BN) * (BK / 8) / THREADS * PARTS;   // 16-byte loads of a thread and stage
-    static_assert(BM * (BK / 8) % THREADS == 0 && BN * (BK / 8) % THREADS == 0, "every wave loads the same");
-    static_assert(STAGES >= 2, "two stages at least");
+    static constexpr bool EVEN = BM * (BK / 8) % THREADS == 0 && BN * (BK / 8) % THREADS == 0;   // every wave loads the same
+    static constexpr int STAGES = !EVEN ? 2 : ROOM > 4 ? 4 : ROOM;
+    static_assert(ROOM >= 2, "two stages at least");
+    // Up to 32 queries, float32 points are split into parts on the way to LDS:
+    // reading them is the work. With more, the splitting would be done over for
+    // every tile of queries, and a copy in parts serves them all (777 queries,
+    // 100,003 x 768: 4.00 ms in place of 3.55).
+    static constexpr bool SPLIT = PARTS == 3 && (BM == 32 || BN == 32);
 };
 
 // Waits until at most `left` of this wave's loads are on their way and its LDS
@@ -95,12 +101,18 @@ __device__ inline void wait_and_meet()
 // way what lanes read together spreads over the banks. The permutation is
 // applied to the addresses loaded from, since a load to LDS writes its lanes
 // in order.
-template <class S, int ROWS, bool ACROSS>
+template <class S, int ROWS, bool ACROSS, bool F32>
 struct Side {
     static constexpr int CHUNKS = ACROSS ? ROWS / 8 : S::BK / 8;      // of an LDS row
-    static constexpr int N = ROWS * (S::BK / 8) / S::THREADS;         // loads of a part
+    static constexpr int N = (ROWS * (S::BK / 8) + S::THREADS - 1) / S::THREADS;   // loads of a part
     static constexpr int PER = S::THREADS / CHUNKS;                   // LDS rows of one load of all threads
     static constexpr int PART = ROWS * S::BK;                         // values of a part's stage
+    // float32: four values a load
+    static constexpr int QUADS = (ACROSS ? ROWS : S::BK) / 4, NF = ROWS * S::BK / 4 / S::THREADS, PERF = S::THREADS / QUADS;
+    static_assert(!F32 || (S::PARTS == 3 && NF * S::THREADS * 4 == ROWS * S::BK), "float32 has parts");
+    float held[F32 ? NF : 1][4];
+    const float *f;
+    int32_t vec, k_from;
     const bf16_t *p;
     int64_t ld, part;
     int32_t row, last, at;   // this thread's first row, the last there is, value within a row (across: of the tile's first)
@@ -113,12 +125,17 @@ struct Side {
     {
         const int t = threadIdx.x;
         ld = o.ld, part = part_, last = o.rows - 1, cols = o.cols;
-        if constexpr (ACROSS) {
+        f = o.f, vec = o.vec, k_from = from_k;
+        if constexpr (F32) {
+            row = row0;
+            at = 0;
+            p = nullptr;
+        } else if constexpr (ACROSS) {
             row = from_k + t / CHUNKS;
             at = row0;
             p = o.p;
         } else {
-            static_assert(PER % 16 == 0 || ACROSS, "one permutation for all of a thread's loads");
+            static_assert(PER % 16 == 0 || N == 1, "one permutation for all of a thread's loads");
             row = row0 + t / CHUNKS;
             at = (t % CHUNKS ^ swap(t / CHUNKS)) * 8;
             p = o.p + from_k;
@@ -130,6 +147,7 @@ struct Side {
         const int t = threadIdx.x, wave = t >> 6;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
+            if (!S::EVEN && i * S::THREADS + wave * 64 >= ROWS * (S::BK / 8)) continue;
             const bf16_t *from;
             if constexpr (ACROSS) {
                 const int c = at + (t % CHUNKS ^ swap(t / CHUNKS + i * PER)) * 8;
@@ -142,6 +160,43 @@ struct Side {
                 __builtin_amdgcn_global_load_lds(
                     (const __attribute__((address_space(1))) void *)(from + q * part),
                     (__attribute__((address_space(3))) void *)(to + q * PART + (i * S::THREADS + wave * 64) * 8), 16, 0, 0);
+        }
+    }
+    // float32: k [k0, k0 + BK) into registers, and from there as parts to LDS
+    __device__ void fetch(int32_t k0)
+    {
+        const int t = threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < NF; ++i) {
+            const int r = t / QUADS + i * PERF, q = t % QUADS * 4;
+            const int32_t c = ACROSS ? row + q : k_from + k0 + q;   // value within a row
+            const float *from = f + (int64_t)min((ACROSS ? k_from + k0 : row) + r, last) * ld + c;
+            if (vec && c < cols) {
+                load_f32<4, float>(held[i], from);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) held[i][e] = c + e < cols ? from[e] : 0.0f;
+            }
+        }
+    }
+    __device__ void put(bf16_t *to)
+    {
+        const int t = threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < NF; ++i) {
+            const int r = t / QUADS + i * PERF, q = t % QUADS;
+            bf16_t *at_row = to + r * CHUNKS * 8 + ((q >> 1) ^ swap(r)) * 8 + (q & 1) * 4;
+#pragma unroll
+            for (int part_i = 0; part_i < S::PARTS; ++part_i) {
+                bf16x4 four;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float top = __uint_as_float(__float_as_uint(held[i][e]) & 0xFFFF0000u);
+                    four[e] = (bf16_t)top;
+                    held[i][e] = fabsf(top) < INFINITY ? held[i][e] - top : 0.0f;
+                }
+                *(bf16x4 *)(at_row + part_i * PART) = four;
+            }
         }
     }
     // where this lane's fragments begin in a stage, in bytes; row0: the wave's first row of the tile
@@ -180,30 +235,42 @@ struct Side {
 // STAGES - 1 stages ahead of the matrix instructions (a stage of 256 x 256 is
 // 1000 cycles of them, 3000 with parts). Of parts, the six products above
 // 2^-24 of the result are added, smallest first. ACROSS_A, ACROSS_B: the
-// operand's rows are k.
-template <class S, bool ACROSS_A, bool ACROSS_B>
+// operand's rows are k; F32_A, F32_B: it is float32 in memory.
+template <class S, bool ACROSS_A, bool ACROSS_B, bool F32_A = false, bool F32_B = false>
 __device__ inline void tile_product(const Product &pr, int32_t row0a, int32_t row0b, bf16_t *lds,
                                     f32x16 (&acc)[S::TM][S::TN], int32_t from_k, int32_t K)
 {
     constexpr int STAGES = S::STAGES, BK = S::BK;
     const int wave = threadIdx.x >> 6, wm = wave % S::WM, wn = wave / S::WM;
-    using A = Side<S, S::BM, ACROSS_A>;
-    using B = Side<S, S::BN, ACROSS_B>;
-    const A a(pr.a, pr.part_a, row0a, from_k);
-    const B b(pr.b, pr.part_b, row0b, from_k);
+    using A = Side<S, S::BM, ACROSS_A, F32_A>;
+    using B = Side<S, S::BN, ACROSS_B, F32_B>;
+    A a(pr.a, pr.part_a, row0a, from_k);
+    B b(pr.b, pr.part_b, row0b, from_k);
+    // loads to LDS that may be on their way when a stage is waited for
+    constexpr int COUNTED = (STAGES - 2) * S::PARTS * ((F32_A ? 0 : A::N) + (F32_B ? 0 : B::N));
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) bf16_t *)lds;
     const uint32_t lane_a = A::lane_at(wm * S::TM * 32), lane_b = B::lane_at(wn * S::TN * 32);
     const int total = (K + BK - 1) / BK;
     auto load = [&](int it) {   // past the end, the last stage again: it is not used
         bf16_t *to = lds + it % STAGES * S::STAGE;
         const int k0 = min(it, total - 1) * BK;
-        a.load(to, k0, K);
-        b.load(to + S::BM * BK * S::PARTS, k0, K);
+        if constexpr (F32_A) a.fetch(k0);
+        if constexpr (F32_B) b.fetch(k0);
+        if constexpr (!F32_A) a.load(to, k0, K);
+        if constexpr (!F32_B) b.load(to + S::BM * BK * S::PARTS, k0, K);
+    };
+    auto put = [&](int it) {
+        bf16_t *to = lds + it % STAGES * S::STAGE;
+        if constexpr (F32_A) a.put(to);
+        if constexpr (F32_B) b.put(to + S::BM * BK * S::PARTS);
     };
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) load(i);
+    for (int i = 0; i < STAGES - 1; ++i) {
+        load(i);
+        put(i);
+    }
     auto step = [&](int it, auto steps) {
-        wait_and_meet<(STAGES - 2) * S::LOADS>();
+        wait_and_meet<COUNTED>();
         load(it + STAGES - 1);
         const uint32_t stage = base + it % STAGES * S::STAGE * 2;
         const uint32_t at_a = stage + lane_a, at_b = stage + S::BM * BK * S::PARTS * 2 + lane_b;
@@ -237,6 +304,7 @@ __device__ inline void tile_product(const Product &pr, int32_t row0a, int32_t ro
                 if (S::PARTS > 1) __builtin_amdgcn_sched_barrier(0);
             }
         }
+        put(it + STAGES - 1);
     };
     for (int it = 0; it < K / BK; ++it) step(it, std::integral_constant<int, BK / 16>{});
     if (K % BK) step(total - 1, std::integral_constant<int, 1>{});
@@ -431,7 +499,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void stats_kernel(StatsArgs a)
     for (int32_t tv = split; tv < a.tiles_v; tv += a.splits) {
         f32x16 acc[S::TM][S::TN];
         clear<S>(acc);
-        tile_product<S, false, false>(a.pr, tv * S::BM, tb * S::BN, lds, acc, 0, a.pr.K);
+        tile_product<S, false, false, S::SPLIT, false>(a.pr, tv * S::BM, tb * S::BN, lds, acc, 0, a.pr.K);
 #pragma unroll
         for (int i = 0; i < S::TM; ++i) {
             const int32_t v0 = tv * S::BM + (wm * S::TM + i) * 32;
@@ -611,7 +679,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void prob_kernel(ProbArgs a)
     const int wm = wave % S::WM, wn = wave / S::WM;
     f32x16 acc[S::TM][S::TN];
     clear<S>(acc);
-    tile_product<S, false, false>(a.pr, tb * S::BM, tv * S::BN, lds, acc, 0, a.pr.K);
+    tile_product<S, false, false, false, S::SPLIT>(a.pr, tb * S::BM, tv * S::BN, lds, acc, 0, a.pr.K);
     float off[S::TN];
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) {
@@ -712,7 +780,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void dh_kernel(DhArgs a)
     const int32_t k0 = split * a.k_split, K = min(a.k_split, a.pr.K - k0);
     f32x16 acc[S::TM][S::TN];
     clear<S>(acc);
-    if (K > 0) tile_product<S, false, true>(a.pr, tb * S::BM, td * S::BN, lds, acc, k0, K);
+    if (K > 0) tile_product<S, false, true, false, S::SPLIT>(a.pr, tb * S::BM, td * S::BN, lds, acc, k0, K);
 #pragma unroll
     for (int i = 0; i < S::TM; ++i)
 #pragma unroll
@@ -1535,7 +1603,7 @@ struct Plan {
     int32_t splits, shares, per_split;               // of the statistics
     int32_t c_splits, c_per_split, c_tiles;          // sweep: of the points' gradient
     int64_t Vc, cols_pad;      // points per piece, and its padded size
-    int64_t copied;            // points that are held as parts at a time
+    int64_t copied;            // points that are held as a copy at a time
     int32_t dh_splits, dh_k, tile_d, tiles_d;
     int64_t off_h, off_c, off_part, off_loss, off_top, off_rowf, off_coef, off_label, off_pick, off_factor, off_done;
     int64_t off_p, off_col, off_dh, off_first, off_own, off_ownb, off_bias, off_hz, off_dc, total;
@@ -1625,11 +1693,11 @@ Plan make_plan(const boa_xent *x, bool grad)
         }
         p.Vc = best * 256;
         p.cols_pad = p.Vc;
-        // points as parts: all of them up to 2 GB, so that one copy serves both
-        // passes, else a piece at a time
+        // Points that cannot be read where they are get a copy: of all of them up
+        // to 2 GB, so that it serves both passes, else a piece at a time.
+        if (p.parts == 3) p.direct = p.tile_b == 32;   // Shape::SPLIT
         const int64_t point = (int64_t)p.Kp * 2 * p.parts;
-        p.copied = x->V * point <= (int64_t)2 << 30 ? x->V : p.Vc;
-        if (p.direct) p.copied = 0;
+        p.copied = p.direct ? 0 : x->V * point <= (int64_t)2 << 30 ? x->V : p.Vc;
         const int64_t pieces = p.direct || p.copied >= x->V ? 1 : ceil_div(x->V, p.Vc);
         p.shares = p.splits * (int32_t)pieces;   // a piece's tiles are split like all of them
         p.off_h = take((int64_t)p.parts * p.rows_pad * p.Kp * 2);
@@ -1639,10 +1707,10 @@ Plan make_plan(const boa_xent *x, bool grad)
             // tiles of a split run on one XCD, so splits come in eights; a block
             // pays for reading and adding to its share of the sums as for `over`
             // values of k (26 us and 32 cycles each, six times less with parts).
-            const int64_t tiles = (int64_t)p.tiles_b * p.tiles_d, over = p.parts == 1 ? 2000 : 330;
+            const int64_t tiles = (int64_t)p.tiles_b * p.tiles_d, over = (p.parts == 1 ? 2000 : 330) * p.tile_b / 256;
             const int64_t room = p.tile_b == 256 && p.tile_d == 256 ? 32 : 64;   // blocks an XCD holds
             int64_t splits = 1, split_cost = 0;
-            for (int64_t n = 1; n <= 64 && n * 256 <= p.cols_pad; n += n < 8 ? n : 8) {
+            for (int64_t n = 1; n <= 512 && n * 256 <= p.cols_pad; n += n < 8 ? n : 8) {
                 const int64_t cost = ceil_div(ceil_div(n, 8) * tiles, room) * (ceil_div(p.cols_pad, n) + over);
                 if (n == 1 || cost < split_cost) splits = n, split_cost = cost;
             }
@@ -1705,9 +1773,9 @@ template <int P> struct Pick<128, 128, P> { using S = Shape<2, 2, 2, 2, P>; };
 template <> struct Pick<256, 32, 1> { using S = Shape<2, 1, 4, 1, 1>; };
 template <> struct Pick<32, 256, 1> { using S = Shape<1, 2, 1, 4, 1>; };
 template <> struct Pick<32, 128, 1> { using S = Shape<1, 2, 1, 2, 1>; };
-template <> struct Pick<256, 32, 3> { using S = Shape<1, 1, 8, 1, 3>; };
-template <> struct Pick<32, 256, 3> { using S = Shape<1, 1, 1, 8, 3>; };
-template <> struct Pick<32, 128, 3> { using S = Shape<1, 1, 1, 4, 3>; };
+template <> struct Pick<256, 32, 3> { using S = Shape<4, 1, 2, 1, 3>; };
+template <> struct Pick<32, 256, 3> { using S = Shape<1, 4, 1, 2, 3>; };
+template <> struct Pick<32, 128, 3> { using S = Shape<1, 4, 1, 1, 3>; };
 
 int check(const boa_xent *x, bool grad)
 {
@@ -1914,17 +1982,26 @@ int run_tiles(const Work<T> &w)
     const int32_t pieces = (int32_t)ceil_div(V, p.Vc);
     const bool whole = p.copied >= V;   // the points' copy serves both passes
     auto points_of = [&](int64_t v0, int32_t n, bool again) {
-        if (p.direct)
-            return Operand{(const bf16_t *)x->points + v0 * x->points_stride, x->points_stride, n, p.Kp};
-        bf16_t *copy = (bf16_t *)(ws + p.off_c);
+        Operand o{};
+        o.rows = n, o.ld = x->points_stride;
+        if (p.direct) {
+            if constexpr (PARTS == 3) {
+                o.f = (const float *)x->points + v0 * x->points_stride, o.cols = d;
+                o.vec = d % 4 == 0 && x->points_stride % 4 == 0 && aligned(x->points, 16);
+            } else {
+                o.p = (const bf16_t *)x->points + v0 * x->points_stride, o.cols = p.Kp;
+            }
+            return o;
+        }
+        bf16_t *copy = (bf16_t *)(ws + p.off_c) + (whole ? v0 * p.Kp : 0);
+        o.p = copy, o.ld = o.cols = p.Kp;
         if (!(whole && again)) {
             PartsArgs a{};
             a.src = (const T *)x->points + v0 * x->points_stride, a.stride = x->points_stride;
-            a.R = a.rows_pad = n, a.C = d, a.plain_ld = p.Kp, a.plain_part = c_part;
-            a.plain = copy + (whole ? v0 * p.Kp : 0);
+            a.R = a.rows_pad = n, a.C = d, a.plain_ld = p.Kp, a.plain_part = c_part, a.plain = copy;
             parts_kernel<T><<<dim3((uint32_t)parts_blocks(a)), 256, 0, st>>>(a);
         }
-        return Operand{copy + (whole ? v0 * p.Kp : 0), p.Kp, n, p.Kp};
+        return o;
     };
 
     // losses: all points at once where they are read in place, else by pieces
