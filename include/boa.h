@@ -337,6 +337,7 @@ int boa_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, in
                             int64_t workspace_bytes, void *stream);
 
 #define BOA_MAX_XENT_D 4096
+#define BOA_MAX_XENT_B (1 << 21)
 enum { BOA_REDUCE_NONE = 0, BOA_REDUCE_SUM = 1, BOA_REDUCE_MEAN = 2 };
 /*
  * Softmax cross entropy of B queries over V points as classes:
@@ -347,7 +348,7 @@ enum { BOA_REDUCE_NONE = 0, BOA_REDUCE_SUM = 1, BOA_REDUCE_MEAN = 2 };
 typedef struct {
     int32_t dtype;          /* of h, points, dh and dpoints: BOA_T_F32 or BOA_T_BF16 */
     int32_t d;              /* 1 .. BOA_MAX_XENT_D */
-    int64_t B, V;           /* queries, 0 .. 2^24; points, 1 .. 2^31 - 2^16 */
+    int64_t B, V;           /* queries, 0 .. BOA_MAX_XENT_B; points, 1 .. 2^31 - 2^16 */
     const void *h;          /* B x d */
     int64_t h_stride;
     const void *points;     /* V x d */

@@ -420,11 +420,20 @@ int launch_rows4(const VecArgs &a, hipStream_t st)
         else launch_sets<T, f16_t>(a, st);
         return launch_status("matvec_fourbit");
     }
-    const dim3 grid((uint32_t)ceil_div(a.rows, 4));
-    if (a.M == 1)
-        rows4_any_kernel<T, 1><<<grid, 256, 0, st>>>(a);
-    else
-        rows4_any_kernel<T, 8><<<grid, 256, 0, st>>>(a);
+    for (int64_t row = 0; row < a.rows; row += LAUNCH_ROWS) {
+        VecArgs n = a;
+        const int64_t scale = row * a.scale_stride * dtype_bytes(a.scale_dtype);
+        n.codes += row * a.codes_stride;
+        n.scales = (const uint8_t *)a.scales + scale;
+        if (a.offsets) n.offsets = (const uint8_t *)a.offsets + scale;
+        n.y = (T *)a.y + row;
+        n.rows = std::min(LAUNCH_ROWS, a.rows - row);
+        const dim3 grid((uint32_t)ceil_div(n.rows, 4));
+        if (a.M == 1)
+            rows4_any_kernel<T, 1><<<grid, 256, 0, st>>>(n);
+        else
+            rows4_any_kernel<T, 8><<<grid, 256, 0, st>>>(n);
+    }
     return launch_status("matvec_fourbit");
 }
 

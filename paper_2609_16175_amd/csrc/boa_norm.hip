@@ -35,6 +35,19 @@ struct NormArgs {
     float eps;
 };
 
+// The arguments of the rows from `row` on that one launch takes.
+template <class T>
+NormArgs rows_from(NormArgs a, int64_t row)
+{
+    a.x = (const T *)a.x + row * a.x_stride;
+    if (a.dy) a.dy = (const T *)a.dy + row * a.dy_stride;
+    a.y = (T *)a.y + row * a.d;
+    if (a.mean) a.mean += row;
+    if (a.rstd) a.rstd += row;
+    a.rows = std::min(LAUNCH_ROWS, a.rows - row);
+    return a;
+}
+
 // A thread's columns of load i of a row: [c, c + VEC), moved back to end with
 // the row where they would pass its end; the first `skip` of them are then
 // another thread's too, or all (skip >= VEC). Every load is whole and within the
@@ -428,13 +441,16 @@ int boa_layer_norm(const void *x, int64_t rows, int32_t d, int64_t x_stride, int
         using T = decltype(t);
         using P = decltype(p);
         constexpr int VEC = 16 / sizeof(T);
-        const bool fits = with_shape<VEC>(d, [&](auto nv, auto tpr, auto whole) {
-            constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value;
-            constexpr bool WHOLE = decltype(whole)::value;
-            const int64_t blocks = ceil_div(rows, THREADS / TPR);
-            norm_kernel<T, P, NV, TPR, WHOLE><<<dim3((uint32_t)blocks), THREADS, 0, st>>>(a);
-        });
-        if (!fits) norm_wide_kernel<T, P><<<dim3((uint32_t)rows), THREADS, 0, st>>>(a);
+        for (int64_t row = 0; row < rows; row += LAUNCH_ROWS) {
+            const NormArgs n = rows_from<T>(a, row);
+            const bool fits = with_shape<VEC>(d, [&](auto nv, auto tpr, auto whole) {
+                constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value;
+                constexpr bool WHOLE = decltype(whole)::value;
+                const int64_t blocks = ceil_div(n.rows, THREADS / TPR);
+                norm_kernel<T, P, NV, TPR, WHOLE><<<dim3((uint32_t)blocks), THREADS, 0, st>>>(n);
+            });
+            if (!fits) norm_wide_kernel<T, P><<<dim3((uint32_t)n.rows), THREADS, 0, st>>>(n);
+        }
         return launch_status("layer_norm");
     });
 }
@@ -477,7 +493,10 @@ int boa_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, in
                 norm_back_kernel<T, P, NV, TPR, WHOLE, false><<<dim3((uint32_t)blocks), THREADS, 0, st>>>(a);
         });
         if (!fits) {
-            if (dx && rows) norm_back_wide_kernel<T, P><<<dim3((uint32_t)rows), THREADS, 0, st>>>(a);
+            for (int64_t row = 0; dx && row < rows; row += LAUNCH_ROWS) {
+                const NormArgs n = rows_from<T>(a, row);
+                norm_back_wide_kernel<T, P><<<dim3((uint32_t)n.rows), THREADS, 0, st>>>(n);
+            }
             if (params)
                 norm_cols_kernel<T><<<dim3((uint32_t)blocks, (uint32_t)ceil_div(d, THREADS)), THREADS, 0, st>>>(a);
         }

@@ -22,6 +22,10 @@ typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
 
 inline int64_t dtype_bytes(int32_t t) { return t == BOA_T_F32 ? 4 : 2; }
+// Rows that one launch takes at up to 256 threads a row: a launch may not have
+// 2^32 threads. More rows take several launches.
+constexpr int64_t LAUNCH_ROWS = (int64_t)1 << 23;
+
 inline bool dtype_known(int32_t t) { return t == BOA_T_F32 || t == BOA_T_BF16 || t == BOA_T_F16; }
 inline bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

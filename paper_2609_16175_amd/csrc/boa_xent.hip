@@ -1794,7 +1794,8 @@ int check(const boa_xent *x, bool grad)
         return set_error(BOA_EUNSUPPORTED, "softmax_xent: float16 does not hold the probabilities of many points; use bfloat16 or float32");
     if (x->dtype != BOA_T_F32 && x->dtype != BOA_T_BF16) return bad("softmax_xent: unknown dtype");
     if (x->d < 1 || x->d > BOA_MAX_XENT_D) return bad("softmax_xent: d out of range [1, 4096]");
-    if (x->B < 0 || x->B > (1 << 24)) return bad("softmax_xent: B out of range [0, 2^24]");
+    // two blocks per query, or a thread per four values of them, stay below a launch's 2^32 threads
+    if (x->B < 0 || x->B > BOA_MAX_XENT_B) return bad("softmax_xent: B out of range [0, 2^21]");
     if (x->V < 1 || x->V > ((int64_t)1 << 31) - (1 << 16)) return bad("softmax_xent: V out of range");
     if (x->reduction < BOA_REDUCE_NONE || x->reduction > BOA_REDUCE_MEAN) return bad("softmax_xent: unknown reduction");
     if ((x->B > 1 && x->h_stride < x->d) || (x->V > 1 && x->points_stride < x->d))
@@ -1912,11 +1913,15 @@ int run_sweeps(const Work<T> &w)
     } else if (p.direct) {
         c.m = (const bf16_t *)x->points, c.m_ld = x->points_stride, c.Kp = d;
     } else {
-        PartsArgs a{};
-        a.src = x->points, a.stride = x->points_stride, a.R = V, a.C = d, a.rows_pad = V;
-        a.plain = w.template at<bf16_t>(p.off_c), a.plain_ld = p.ld;
-        parts_kernel<T><<<dim3((uint32_t)parts_blocks(a)), 256, 0, st>>>(a);
-        c.m = a.plain, c.m_ld = p.ld, c.Kp = p.ld;
+        bf16_t *copy = w.template at<bf16_t>(p.off_c);
+        for (int64_t v0 = 0; v0 < V; v0 += LAUNCH_ROWS) {
+            PartsArgs a{};
+            a.src = (const T *)x->points + v0 * x->points_stride, a.stride = x->points_stride;
+            a.R = a.rows_pad = (int32_t)std::min<int64_t>(LAUNCH_ROWS, V - v0), a.C = d;
+            a.plain = copy + v0 * p.ld, a.plain_ld = p.ld;
+            parts_kernel<T><<<dim3((uint32_t)parts_blocks(a)), 256, 0, st>>>(a);
+        }
+        c.m = copy, c.m_ld = p.ld, c.Kp = p.ld;
     }
     SweepArgs a = c;
     a.n = h, a.n_ld = p.ld, a.n_part = (int64_t)p.rows_pad * p.ld, a.N = B, a.M = V, a.d = d;

@@ -1,0 +1,69 @@
+"""Query-tower operators on the GPU: more rows than one launch takes, and what
+autograd may ask of them. Rows of a long call have to equal a short call's bit
+for bit: the kernels treat each row alike, and the short calls are tested
+against float64 in test_gpu_ops.py."""
+import pytest
+import torch
+
+import paper_2609_16175_amd as boa
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+LAUNCH = 1 << 23   # rows that one launch takes
+
+
+def normal(*shape, seed=0, dt=F32):
+    return torch.empty(*shape, dtype=dt, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(seed))
+
+
+def around(*edges):
+    return [(e - 20, e + 20) for e in edges]
+
+
+@pytest.mark.parametrize("d", [4, 8])   # a block per row, a wave per row
+def test_layer_norm_more_rows_than_a_launch(d):
+    rows = 2 * LAUNCH + 21
+    x, dy = normal(rows, d, dt=BF16), normal(rows, d, seed=1, dt=BF16)
+    w, b = normal(d, seed=2), normal(d, seed=3)
+    y, mean, rstd = boa.layer_norm_forward(x, w, b)
+    dx, _, _ = boa.layer_norm_backward(dy, x, w, mean, rstd)
+    for lo, hi in [(0, 40), *around(LAUNCH, 2 * LAUNCH), (rows - 40, rows)]:
+        few = boa.layer_norm_forward(x[lo:hi], w, b)
+        assert all(torch.equal(a[lo:hi], c) for a, c in zip((y, mean, rstd), few)), lo
+        assert torch.equal(dx[lo:hi], boa.layer_norm_backward(dy[lo:hi], x[lo:hi], w, few[1], few[2])[0]), lo
+
+
+@pytest.mark.parametrize("offsets", [False, True])
+def test_matvec_4bit_more_rows_than_a_launch(offsets):
+    N = LAUNCH + 33
+    codes = torch.randint(256, (N, 2), dtype=torch.uint8, device="cuda", generator=torch.Generator("cuda").manual_seed(4))
+    s = normal(N, 2, seed=5, dt=BF16)
+    o = normal(N, 2, seed=6, dt=BF16) if offsets else None
+    x = normal(2, 3, seed=7)
+    y = boa.matvec_4bit(x, codes, s, o, group=2)
+    for lo, hi in [(0, 40), *around(LAUNCH), (N - 40, N)]:
+        few = boa.matvec_4bit(x, codes[lo:hi], s[lo:hi], None if o is None else o[lo:hi], group=2)
+        assert torch.equal(y[:, lo:hi], few), lo
+
+
+def test_softmax_xent_more_copied_points_than_a_launch():
+    # rows of 3 values are copied before they are read
+    V, d, B = LAUNCH + 37, 3, 3
+    pts, h = normal(V, d, seed=8, dt=BF16), normal(B, d, seed=9, dt=BF16)
+    labels = torch.tensor([V - 1, LAUNCH, 5], device="cuda")
+    r = boa.softmax_xent_grad(h, pts, labels, reduction="none")
+    H, P = h.double(), pts.double()
+    l = torch.mm(H, P.t().contiguous())
+    lse = torch.logsumexp(l, 1)
+    assert (r.loss.double() - (lse - l[torch.arange(B, device="cuda"), labels])).abs().max() < 1e-4
+    p = torch.exp(l - lse[:, None])
+    want = torch.mm(p, P) - P[labels]
+    # probabilities rounded to bfloat16, the result once more, and 1e-4 of the exponentials
+    bound = 2.0 ** -8 * (torch.mm(p, P.abs()) + want.abs()) + 1e-4
+    assert ((r.dh.double() - want).abs() <= bound).all()
+    for v in (V - 1, V - 2, LAUNCH, LAUNCH - 1, 5):
+        q = p[:, v] - (labels == v).double()
+        row = q @ H
+        bound = (p[:, v] * 2.0 ** -8 + 1e-4) @ H.abs() + 2.0 ** -8 * row.abs()
+        assert ((r.drows[v].double() - row).abs() <= bound).all(), v

@@ -73,6 +73,11 @@ def test_softmax_xent_refuses(over, code, needle):
     assert _xent(**over) == code and needle in _err()
 
 
+def test_softmax_xent_refuses_more_queries_than_its_launches_take():
+    assert _xent(B=(1 << 21) + 1) == EINVAL and "B out of range" in _err()
+    assert _xent(B=1 << 21, n=16) == EINVAL and "workspace" in _err()
+
+
 def test_xent_null_struct():
     assert ops._lib().boa_softmax_xent(None, P, 1 << 30, None) == EINVAL
     assert ops._lib().boa_softmax_xent_workspace(None, 1) == EINVAL
