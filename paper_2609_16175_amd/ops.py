@@ -13,6 +13,7 @@ import ctypes as C
 from dataclasses import dataclass
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import _check, lib
 
@@ -158,12 +159,17 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, stream=None):
     return y, mean, rstd
 
 
-def layer_norm_backward(dy, x, weight, mean, rstd, need=(True, True, True), stream=None):
-    """(dx, dweight, dbias) of layer_norm_forward; weight may be None (then
-    dweight and dbias have x's type). need: which of the three to compute."""
+def layer_norm_backward(dy, x, weight, mean, rstd, need=(True, True, True), stream=None, param_dtype=None):
+    """(dx, dweight, dbias) of layer_norm_forward; weight may be None. dweight
+    and dbias have weight's type; without one, param_dtype (x's, the default,
+    or float32). need: which of the three to compute."""
     _device("layer_norm_backward", dy, x, weight, mean, rstd)
     dt = _dtype("layer_norm_backward", x)
     pd = _norm_params("layer_norm_backward", x, weight, None)
+    ptype = weight.dtype if weight is not None else x.dtype if param_dtype is None else param_dtype
+    if param_dtype not in (None, ptype) or ptype not in (x.dtype, torch.float32):
+        raise ValueError("layer_norm_backward: param_dtype must be weight's type, or without one x's or float32")
+    pd = _DTYPES[ptype]
     if dy.shape != x.shape or dy.dtype != x.dtype:
         raise ValueError("layer_norm_backward: dy must have x's shape and type")
     m, g = _rows(x), _rows(dy)
@@ -174,9 +180,8 @@ def layer_norm_backward(dy, x, weight, mean, rstd, need=(True, True, True), stre
     other = _at(x, stream, dy, x, weight, mean, rstd)
     if other is not None:
         with other:
-            return layer_norm_backward(dy, x, weight, mean, rstd, need)
+            return layer_norm_backward(dy, x, weight, mean, rstd, need, param_dtype=param_dtype)
     w = _dense(weight)
-    ptype = x.dtype if weight is None else weight.dtype
     dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need[0] else None
     dw = db = None
     if need[1] and need[2]:
@@ -202,10 +207,10 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
-        dx, dw, db = layer_norm_backward(dy, x, weight, mean, rstd, need=ctx.needs_input_grad[:3])
-        return dx, dw, db if db is None else db.to(ctx.bias_type), None
+        return *layer_norm_backward(dy, x, weight, mean, rstd, ctx.needs_input_grad[:3], param_dtype=ctx.bias_type), None
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
@@ -300,6 +305,7 @@ class _SoftmaxXent(torch.autograd.Function):
         return r.loss
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dloss):
         scale, reduction = ctx.args
         need = ctx.needs_input_grad

@@ -67,3 +67,30 @@ def test_softmax_xent_more_copied_points_than_a_launch():
         row = q @ H
         bound = (p[:, v] * 2.0 ** -8 + 1e-4) @ H.abs() + 2.0 ** -8 * row.abs()
         assert ((r.drows[v].double() - row).abs() <= bound).all(), v
+
+
+def test_layer_norm_float32_bias_without_weight():
+    # its gradient is rounded once, to float32
+    x, b = normal(300, 64, seed=10, dt=BF16), normal(64, seed=11).requires_grad_()
+    dy = normal(300, 64, seed=12, dt=BF16)
+    boa.layer_norm(x, None, b).backward(dy)
+    want = dy.double().sum(0)
+    assert b.grad.dtype == F32
+    assert ((b.grad.double() - want).abs() <= 300 * 2.0 ** -24 * dy.double().abs().sum(0)).all()
+    y, mean, rstd = boa.layer_norm_forward(x)
+    with pytest.raises(ValueError, match="param_dtype"):
+        boa.layer_norm_backward(dy, x, None, mean, rstd, param_dtype=torch.float16)
+    with pytest.raises(ValueError, match="param_dtype"):
+        boa.layer_norm_backward(dy, x, b.detach(), mean, rstd, param_dtype=BF16)
+
+
+@pytest.mark.parametrize("reduction", ["none", "mean"])
+def test_second_derivatives_are_refused(reduction):
+    x = normal(4, 32, seed=13).requires_grad_()
+    g, = torch.autograd.grad((boa.layer_norm(x) ** 2).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.sum().backward()
+    loss = boa.softmax_xent(x, normal(50, 32, seed=14), torch.arange(4, device="cuda"), reduction=reduction)
+    g, = torch.autograd.grad((loss ** 2).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.sum().backward()
