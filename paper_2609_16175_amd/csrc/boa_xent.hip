@@ -1481,6 +1481,7 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                     a.dbias[base + r] = factor * (f >= 0 ? sum[j] + a.own_bias[f] : sum[j]);
                 }
             }
+            if (whole && !a.dc) continue;   // the biases' gradient alone
             constexpr int CHUNKS = DT * 4, ROWS = 64 / CHUNKS > 0 ? 64 / CHUNKS : 1;   // chunks of 8 values, rows at once
             for (int row = lane / CHUNKS; row < 32; row += ROWS) {
                 const int32_t n = base + row;
