@@ -17,8 +17,11 @@
 // shares are joined afterwards. The gradients take a second pass over pieces
 // of the points: probabilities of a piece from the logits formed again,
 // rounded to the products' type, then the two products. The label's
-// own entry is left out of the rounded probabilities and added in float32, so
-// that a query whose point has nearly all the probability keeps its digits.
+// own entry is left out of the rounded probabilities, and out of the sums of
+// exponentials until the shares are joined: with r the others' sum and e the
+// label's term, its entry is -g r / (r + e), added in float32, and the loss of a
+// query whose point has most of the probability log(1 + r / e). Neither is the
+// small difference of larger numbers, whatever 1 - p is.
 #include <algorithm>
 #include <cmath>
 
@@ -447,7 +450,7 @@ __global__ __launch_bounds__(256) void prep_kernel(PrepArgs a)
 // losses
 
 struct RowState {
-    float m, s;   // running maximum (base 2) and sum of exponentials
+    float m, s;   // running maximum (base 2) and sum of exponentials, the label's own left out
 };
 
 // sum += x with what rounding loses kept in `lost` and brought in by the next
@@ -519,14 +522,19 @@ __global__ __launch_bounds__(S::THREADS, 2) void stats_kernel(StatsArgs a)
                     top = fmaxf(top, acc[i][j][e]);
                 }
                 const int32_t rel = lab[j] - v0;
-                if (__any((uint32_t)rel < 32u))   // a query's own point is among these
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (rel == tile_row(e, half)) a.pick[tb * S::BN + (wn * S::TN + j) * 32 + (lane & 31)] = acc[i][j][e];
                 const float by = __builtin_amdgcn_exp2f(st[j].m - top);
                 float s = 0.0f;
+                if (__any((uint32_t)rel < 32u)) {   // a query's own point is among these: it is joined later
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(acc[i][j][e] - top);
+                    for (int e = 0; e < 16; ++e) {
+                        const bool here = rel == tile_row(e, half);
+                        if (here) a.pick[tb * S::BN + (wn * S::TN + j) * 32 + (lane & 31)] = acc[i][j][e];
+                        s += here ? 0.0f : __builtin_amdgcn_exp2f(acc[i][j][e] - top);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(acc[i][j][e] - top);
+                }
                 st[j].m = top;
                 st[j].s *= by;
                 lost[j] *= by;
@@ -558,8 +566,8 @@ struct RowArgs {
     float *loss;             // per query (the caller's, or scratch where the loss is reduced)
     float *lse;              // the caller's, or null
     float *top;              // rows_pad: what the sum is relative to, base 2
-    float *rowf;             // rows_pad: g / sum of 2^(l - top), 0 for a query without gradient
-    float *coef;             // B: g * (p_label - 1)
+    float *rowf;             // rows_pad: g / sum of 2^(l - top) over all points, 0 for a query without gradient
+    float *coef;             // B: g * (p_label - 1), by way of the others' sum
     int32_t *label;          // rows_pad: the label, or -1 where it has no entry
     int32_t B, V, shares, reduction, rows_pad;
     uint32_t *done;          // blocks that are done, 0 at the start
@@ -591,19 +599,20 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a)
         if (lane == 0) {
             const int64_t y = a.labels[b];
             const bool in = y >= 0 && y < a.V;
-            const bool none = st.s == 0.0f;   // every point left out
-            const float log_s = __builtin_amdgcn_logf(st.s);
             const float l2 = in ? a.pick[b] : 0.0f;
+            const float mine = in ? __builtin_amdgcn_exp2f(l2 - st.m) : 0.0f, all = st.s + mine;
+            const bool none = all == 0.0f;   // every point left out
+            const float log_s = __builtin_amdgcn_logf(all);
             float loss = 0.0f;
             if (y >= a.V) loss = NAN;
-            else if (in) loss = none ? INFINITY : ((st.m - l2) + log_s) * LN2;
+            else if (in) loss = none ? INFINITY : mine > st.s ? log1pf(st.s / mine) : ((st.m - l2) + log_s) * LN2;
             a.loss[b] = loss;
             if (a.lse) a.lse[b] = none ? -INFINITY : (st.m + log_s) * LN2;
             const float g = !in || none ? 0.0f : a.reduction == BOA_REDUCE_NONE && a.dloss ? a.dloss[b] : 1.0f;
             a.top[b] = none || !in ? INFINITY : st.m;
-            a.rowf[b] = g == 0.0f ? 0.0f : g / st.s;
+            a.rowf[b] = g == 0.0f ? 0.0f : g / all;
             if (none || !in) a.label[b] = -1;
-            if (a.coef) a.coef[b] = in && !none ? g * (__builtin_amdgcn_exp2f(l2 - st.m) / st.s - 1.0f) : 0.0f;
+            if (a.coef) a.coef[b] = in && !none ? -g * (st.s / all) : 0.0f;
         }
     }
     if (!a.total && !a.factor) return;
@@ -1308,22 +1317,19 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                     }
                     const int32_t rel = lab[j] - (stage * S::SR + row0);
                     const bool mine = (uint32_t)rel < 32u;
-                    float s = 0.0f;
-                    if (__any(mine)) {   // a column's own point is among these rows
+                    if (__any(mine)) {   // a column's own point is among these rows: it is joined later
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const bool here = rel == tile_row(e, half);
                             if (here) a.pick[n0 + j * 32 + r] = acc[j][e];
-                            const float p = __builtin_amdgcn_exp2f(acc[j][e] - mx[j]);
-                            s += p;
-                            acc[j][e] = here ? 0.0f : p;
+                            acc[j][e] = here ? -INFINITY : acc[j][e];
                         }
-                    } else {
+                    }
+                    float s = 0.0f;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            acc[j][e] = __builtin_amdgcn_exp2f(acc[j][e] - mx[j]);
-                            s += acc[j][e];
-                        }
+                    for (int e = 0; e < 16; ++e) {
+                        acc[j][e] = __builtin_amdgcn_exp2f(acc[j][e] - mx[j]);
+                        s += acc[j][e];
                     }
                     add_kept(sum[j], lost[j], s);
                 }
