@@ -1696,8 +1696,15 @@ Plan make_plan(const boa_xent *x, bool grad)
         // A piece's probabilities take up to 256 MB. Of the numbers of pieces
         // that do, the one whose launches fill the GPU best: each launch takes
         // whole rounds of resident blocks.
+        // Points that cannot be read where they are get a copy: of all of them up
+        // to 2 GB, so that it serves both passes, else a piece at a time, which
+        // then is no larger than that either.
+        if (p.parts == 3) p.direct = p.tile_b == 32;   // Shape::SPLIT
         const int64_t per = (int64_t)p.rows_pad * 2 * p.parts;
-        const int64_t most = std::max<int64_t>(4, ((int64_t)256 << 20) / per / 256);   // tiles of points
+        const int64_t point = (int64_t)p.Kp * 2 * p.parts, copy = (int64_t)2 << 30;
+        const bool by_pieces = !p.direct && x->V * point > copy;
+        int64_t most = std::max<int64_t>(4, ((int64_t)256 << 20) / per / 256);   // tiles of points
+        if (by_pieces) most = std::min(most, copy / point / 256);   // at least 341 tiles
         const int64_t least = ceil_div(tiles_v, most);
         int64_t best = -1, best_cost = 0;
         for (int64_t n = least; n < least + 6; ++n) {
@@ -1709,12 +1716,8 @@ Plan make_plan(const boa_xent *x, bool grad)
         }
         p.Vc = best * 256;
         p.cols_pad = p.Vc;
-        // Points that cannot be read where they are get a copy: of all of them up
-        // to 2 GB, so that it serves both passes, else a piece at a time.
-        if (p.parts == 3) p.direct = p.tile_b == 32;   // Shape::SPLIT
-        const int64_t point = (int64_t)p.Kp * 2 * p.parts;
-        p.copied = p.direct ? 0 : x->V * point <= (int64_t)2 << 30 ? x->V : p.Vc;
-        const int64_t pieces = p.direct || p.copied >= x->V ? 1 : ceil_div(x->V, p.Vc);
+        p.copied = p.direct ? 0 : by_pieces ? p.Vc : x->V;
+        const int64_t pieces = by_pieces ? ceil_div(x->V, p.Vc) : 1;
         p.shares = p.splits * (int32_t)pieces;   // a piece's tiles are split like all of them
         p.off_h = take((int64_t)p.parts * p.rows_pad * p.Kp * 2);
         p.off_c = take(p.copied * point);

@@ -71,3 +71,46 @@ def test_softmax_xent_probabilities_next_to_one(B, d, dt):
     near(r.dh, q @ C, e_q @ C.abs() + u * (q @ C).abs())
     near(r.drows, q.t() @ H, e_q.t() @ H.abs() + u * (q.t() @ H).abs() + 1e-42)
     near(r.dbias, q.sum(0), (q.abs() * e_p).sum(0) + sums(B) * q.abs().sum(0) + 1e-42)
+
+
+@pytest.mark.parametrize("dt,B,V,d", [(F32, 33, 480_000, 768), (F32, 40, 150_000, 4096), (BF16, 3, 1_300_000, 1001)])
+def test_softmax_xent_points_copied_in_pieces(dt, B, V, d):
+    # more than 2 GB of copied points: each pass copies them piece by piece
+    dev = "cuda"
+    gn = torch.Generator(dev).manual_seed(d)
+    pts = torch.empty(V, d, dtype=dt, device=dev).normal_(generator=gn)
+    labels = torch.randint(V, (B,), device=dev, generator=gn)
+    labels[:3] = torch.tensor([V - 1, 0, V // 2], device=dev)
+    h = (pts[labels].float() + torch.randn(B, d, device=dev, generator=gn)).to(dt)
+    bias = 0.5 * torch.randn(V, device=dev, generator=gn)
+    bias[17::101] = -math.inf
+    bias[labels] = 0.25
+    scale = 4.0 / d
+    r = boa.softmax_xent_grad(h, pts, labels, bias, scale, bias_grad=True)
+    H, rows = h.double(), torch.arange(B, device=dev)
+    l = torch.cat([torch.mm(H, c.double().t().contiguous()) for c in pts.split(50_000)], 1) * scale + bias.double()
+    mag = scale * float(H.norm(dim=1).max()) * max(float(c.double().norm(dim=1).max()) for c in pts.split(50_000))
+    lse = torch.logsumexp(l, 1)
+    want = (lse - l[rows, labels]).mean()
+    e_lse = sums(6 * d) * mag + 8 * EPS * float(l[torch.isfinite(l)].abs().max()) + sums(V) + 16 * EPS
+    assert abs(float(r.loss) - float(want)) <= 2 * e_lse + sums(B) * float(want)
+    p = torch.exp(l - lse[:, None])
+    q = p.clone()
+    q[rows, labels] -= 1
+    q /= B
+    e_p, u = 2 * e_lse + 16 * EPS, unit(dt)
+    e_q = p / B * (e_p + u + sums(6 * V))
+    e_q[rows, labels] = (p[rows, labels] * e_p + 32 * EPS) / B
+    dh, e_dh = torch.zeros_like(H), torch.zeros_like(H)
+    for c, qc, ec in zip(pts.split(50_000), q.split(50_000, 1), e_q.split(50_000, 1)):
+        C = c.double()
+        dh += torch.mm(qc.contiguous(), C)
+        e_dh += torch.mm((ec + sums(6 * V) * qc.abs()).contiguous(), C.abs())
+    assert ((r.dh.double() - scale * dh).abs() <= 1.02 * (scale * e_dh + u * (scale * dh).abs())).all()
+    at = torch.unique(torch.cat((labels, torch.randint(V, (3000,), device=dev, generator=gn))))
+    row = scale * torch.mm(q[:, at].t().contiguous(), H)
+    e = scale * torch.mm((e_q + sums(6 * B) * q.abs())[:, at].t().contiguous(), H.abs()) + u * row.abs()
+    assert ((r.drows[at].double() - row).abs() <= 1.02 * e + 1e-42).all()
+    e_b = p / B * (e_p + 8 * EPS)
+    e_b[rows, labels] = (p[rows, labels] * e_p + 8 * EPS) / B
+    assert ((r.dbias.double() - q.sum(0)).abs() <= 1.02 * (e_b.sum(0) + sums(B) * q.abs().sum(0)) + 1e-42).all()

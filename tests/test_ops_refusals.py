@@ -130,3 +130,18 @@ def test_binding_refuses_host_tensors():
 def test_unknown_attribute():
     with pytest.raises(AttributeError):
         boa.no_such_operator
+
+
+@pytest.mark.parametrize("grad", [0, 1])
+@pytest.mark.parametrize("dtype,B,V,d", [(1, 1, 4_000_000, 1001), (0, 40, 500_000, 4096), (0, 33, 3_000_000, 768),
+                                         (1, 20, 3_000_000, 2000)])
+def test_xent_workspace_copies_two_gigabytes_of_points_at_most(dtype, B, V, d, grad):
+    # points that are not read in place are copied in pieces; these are of odd widths or alignment, or float32
+    a = ops.Xent(dtype=dtype, d=d, B=B, V=V, h=P, h_stride=d, points=P + 8, points_stride=d, labels=P, bias=P, scale=1.0,
+                 reduction=2, loss=P)
+    if grad:
+        a.dh = a.dpoints = a.dbias = P
+    L = ops._lib()
+    # beside the copy: up to 256 MB of probabilities, shares of the queries' gradient, biases and first queries of the points
+    beside = (1 << 28) + 512 * 128 * (d + 16) * 4 + 8 * V if grad else 1 << 26
+    assert 0 < L.boa_softmax_xent_workspace(C.byref(a), grad) <= (1 << 31) + beside
