@@ -867,6 +867,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void dc_kernel(DcArgs a)
     }
 }
 
+constexpr int OWN_AHEAD = 8;   // rows of queries on their way at a time
+
 struct OwnArgs {
     const void *h;
     int64_t h_stride;
@@ -877,8 +879,13 @@ struct OwnArgs {
     float *own, *own_bias;   // own may be null
 };
 
+// The labels' own terms, sum of coef_b h_b over the queries of one point, kept
+// by the first of them. A block per query, which leaves unless its query is the
+// first: every block reads all labels, so this is for few queries (up to
+// SORT_FROM), where it shares a launch with other work; more are sorted. Of the
+// columns a block takes TH from c0.
 template <class T, int TH>
-__device__ inline void own_terms(const OwnArgs &a, int32_t b)
+__device__ inline void own_terms(const OwnArgs &a, int32_t b, int32_t c0)
 {
     const T *h = (const T *)a.h;
     const int64_t h_stride = a.h_stride;
@@ -888,6 +895,7 @@ __device__ inline void own_terms(const OwnArgs &a, int32_t b)
     float *own = a.own, *own_bias = a.own_bias;
     __shared__ int earlier;
     __shared__ int32_t list[TH];
+    __shared__ float by[TH];
     __shared__ int count;
     const int32_t y = label[b];
     if (y < 0) return;
@@ -897,10 +905,8 @@ __device__ inline void own_terms(const OwnArgs &a, int32_t b)
         if (label[i] == y) earlier = 1;
     __syncthreads();
     if (earlier) return;
-    float sb = 0.0f;
-    float acc[BOA_MAX_XENT_D / TH];
-#pragma unroll
-    for (int k = 0; k < BOA_MAX_XENT_D / TH; ++k) acc[k] = 0.0f;
+    const int32_t c = c0 + (int32_t)threadIdx.x;
+    float sb = 0.0f, acc = 0.0f;
     for (int32_t i0 = b; i0 < B; i0 += TH) {
         // the queries of this stretch that share the label, in order
         __syncthreads();
@@ -912,26 +918,28 @@ __device__ inline void own_terms(const OwnArgs &a, int32_t b)
         for (int w = 0; w < TH / 64; ++w) {
             if ((threadIdx.x >> 6) == w && in_wave) {
                 const int at = count + __popcll(in_wave & ((1ull << (threadIdx.x & 63)) - 1));
-                if (hit) list[at] = i;
+                if (hit) {
+                    list[at] = i;
+                    by[at] = coef[i];
+                }
                 __builtin_amdgcn_wave_barrier();
                 if ((threadIdx.x & 63) == 0) count += __popcll(in_wave);
             }
             __syncthreads();
         }
-        for (int j = 0; j < count; ++j) {
-            const int32_t q = list[j];
-            const float c = coef[q];
-            sb += c;
+        for (int j = 0; j < count; ++j) sb += by[j];
+        if (!own || c >= d) continue;
+        for (int j0 = 0; j0 < count; j0 += OWN_AHEAD) {
+            float v[OWN_AHEAD];
 #pragma unroll
-            for (int k = 0; k < BOA_MAX_XENT_D / TH; ++k)
-                if (k * TH + (int)threadIdx.x < d)
-                    acc[k] = fmaf(c, (float)h[(int64_t)q * h_stride + k * TH + threadIdx.x], acc[k]);
+            for (int u = 0; u < OWN_AHEAD; ++u) v[u] = (float)h[(int64_t)list[min(j0 + u, count - 1)] * h_stride + c];
+#pragma unroll
+            for (int u = 0; u < OWN_AHEAD; ++u)
+                if (j0 + u < count) acc = fmaf(by[j0 + u], v[u], acc);
         }
     }
-#pragma unroll
-    for (int k = 0; k < BOA_MAX_XENT_D / TH; ++k)
-        if (k * TH + (int)threadIdx.x < d && own) own[(int64_t)b * d + k * TH + threadIdx.x] = acc[k];
-    if (threadIdx.x == 0) {
+    if (own && c < d) own[(int64_t)b * d + c] = acc;
+    if (threadIdx.x == 0 && c0 == 0) {
         first[y] = b;
         own_bias[b] = sb;
     }
@@ -940,7 +948,309 @@ __device__ inline void own_terms(const OwnArgs &a, int32_t b)
 template <class T>
 __global__ __launch_bounds__(256) void own_kernel(OwnArgs a)
 {
-    own_terms<T, 256>(a, blockIdx.x);
+    own_terms<T, 256>(a, blockIdx.x, blockIdx.y * 256);
+}
+
+// ---------------------------------------------------------------------------
+// Many queries: the same terms in time that grows with them. The queries are
+// sorted by their label, stably, 8 bits a pass; a wave then adds up a stretch of
+// the sorted order (8 positions, or 64 of many queries), and what a point's
+// queries leave in later stretches than their first is joined to it. Every
+// order is fixed by the labels alone, so results do not depend on the schedule.
+constexpr int SORT_TILE = 2048, SORT_DIGITS = 256;   // queries a block sorts, 256 at a time
+// More queries than SORT_FROM are sorted (the whole call at 2,048 x 10,000 x 32
+// bfloat16: sorted 87 us whatever the labels; unsorted 81 with labels drawn at
+// random, 277 with equal ones), up to SORT_BLOCK by one block in LDS, which is
+// one launch in place of three a pass (8,192: 186 us in place of 217).
+constexpr int64_t SORT_FROM = 1024, SORT_BLOCK = 8192;
+
+struct SortArgs {
+    const int32_t *label;             // the first pass' keys: a label of -1 comes last, as key V
+    const uint32_t *key_in, *id_in;   // the later ones'
+    uint32_t *key_out, *id_out;
+    uint32_t *counts;                 // digits x tiles, then where each begins
+    int32_t B, V, tiles, shift;
+
+    __device__ uint32_t key(int32_t i) const
+    {
+        if (key_in) return key_in[i];
+        return (uint32_t)(label[i] < 0 ? V : label[i]);
+    }
+};
+
+__global__ __launch_bounds__(256) void sort_count_kernel(SortArgs a)
+{
+    __shared__ uint32_t count[SORT_DIGITS];
+    const int t = threadIdx.x;
+    count[t] = 0;
+    __syncthreads();
+    for (int r = 0; r < SORT_TILE; r += 256) {
+        const int32_t i = blockIdx.x * SORT_TILE + r + t;
+        if (i < a.B) atomicAdd(&count[a.key(i) >> a.shift & 255], 1u);
+    }
+    __syncthreads();
+    a.counts[(int64_t)t * a.tiles + blockIdx.x] = count[t];
+}
+
+// counts[i] = sum of counts before i, by one block: a stretch per thread
+__global__ __launch_bounds__(1024) void sort_scan_kernel(uint32_t *counts, int32_t n)
+{
+    __shared__ uint32_t waves[16];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int32_t per = (n + 1023) / 1024, from = min(n, t * per), to = min(n, from + per);
+    uint32_t sum = 0;
+    for (int32_t i = from; i < to; ++i) sum += counts[i];
+    uint32_t upto = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t v = __shfl_up(upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 63) waves[wave] = upto;
+    __syncthreads();
+    uint32_t at = upto - sum;
+    for (int w = 0; w < wave; ++w) at += waves[w];
+    for (int32_t i = from; i < to; ++i) {
+        const uint32_t c = counts[i];
+        counts[i] = at;
+        at += c;
+    }
+}
+
+// The wave's queries of a lane's digit: how many, and how many before it.
+struct SameDigit {
+    uint32_t count, rank;
+    __device__ SameDigit(bool live, uint32_t digit)
+    {
+        uint64_t same = __ballot(live);
+#pragma unroll
+        for (int b = 0; b < 8; ++b) {
+            const uint64_t set = __ballot(digit >> b & 1);
+            same &= digit >> b & 1 ? set : ~set;
+        }
+        count = __popcll(same);
+        rank = __popcll(same & ((1ull << (threadIdx.x & 63)) - 1));
+    }
+};
+
+__global__ __launch_bounds__(256) void sort_place_kernel(SortArgs a)
+{
+    __shared__ uint32_t base[SORT_DIGITS], mine[4][SORT_DIGITS];
+    const int t = threadIdx.x, wave = t >> 6;
+    base[t] = a.counts[(int64_t)t * a.tiles + blockIdx.x];
+    for (int r = 0; r < SORT_TILE; r += 256) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) mine[w][t] = 0;
+        __syncthreads();
+        const int32_t i = blockIdx.x * SORT_TILE + r + t;
+        const bool live = i < a.B;
+        const uint32_t key = live ? a.key(i) : 0, digit = key >> a.shift & 255;
+        const SameDigit same(live, digit);
+        if (live && same.rank == 0) mine[wave][digit] = same.count;
+        __syncthreads();
+        if (live) {
+            uint32_t at = base[digit] + same.rank;
+            for (int w = 0; w < wave; ++w) at += mine[w][digit];
+            a.key_out[at] = key;
+            a.id_out[at] = a.key_in ? a.id_in[i] : (uint32_t)i;
+        }
+        __syncthreads();
+        base[t] += mine[0][t] + mine[1][t] + mine[2][t] + mine[3][t];
+    }
+}
+
+// Up to SORT_BLOCK queries, all passes in LDS: keys and queries of before and
+// after a pass, 1024 queries at a time.
+__global__ __launch_bounds__(1024) void sort_block_kernel(SortArgs a)
+{
+    extern __shared__ uint32_t sort_lds[];   // 2 x B keys, the digits' counters, 2 x B ids of 16 bits
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int32_t B = a.B;
+    uint32_t *base = sort_lds + 2 * B, (*mine)[SORT_DIGITS] = (uint32_t(*)[SORT_DIGITS])(base + SORT_DIGITS);
+    uint16_t *ids = (uint16_t *)(base + 17 * SORT_DIGITS);
+    for (int32_t i = t; i < B; i += 1024) {
+        sort_lds[i] = a.key(i);
+        ids[i] = (uint16_t)i;
+    }
+    int from = 0;
+    for (int shift = 0; shift < 32 && ((uint32_t)a.V >> shift); shift += 8, from ^= 1) {
+        const uint32_t *key_in = sort_lds + from * B;
+        const uint16_t *id_in = ids + from * B;
+        uint32_t *key_out = sort_lds + (from ^ 1) * B;
+        uint16_t *id_out = ids + (from ^ 1) * B;
+        if (t < SORT_DIGITS) base[t] = 0;
+        __syncthreads();
+        for (int32_t i = t; i < B; i += 1024) atomicAdd(&base[key_in[i] >> shift & 255], 1u);
+        __syncthreads();
+        if (t < 64) {   // the first wave: where each digit begins, four digits a lane
+            uint32_t c[4], sum = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                c[k] = base[t * 4 + k];
+                sum += c[k];
+            }
+            uint32_t upto = sum;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const uint32_t v = __shfl_up(upto, o);
+                if (lane >= o) upto += v;
+            }
+            uint32_t at = upto - sum;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                base[t * 4 + k] = at;
+                at += c[k];
+            }
+        }
+        for (int32_t r = 0; r < B; r += 1024) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) mine[wave][w * 64 + lane] = 0;
+            __syncthreads();
+            const int32_t i = r + t;
+            const bool live = i < B;
+            const uint32_t key = live ? key_in[i] : 0, digit = key >> shift & 255;
+            const SameDigit same(live, digit);
+            if (live && same.rank == 0) mine[wave][digit] = same.count;
+            __syncthreads();
+            if (live) {
+                uint32_t at = base[digit] + same.rank;
+                for (int w = 0; w < wave; ++w) at += mine[w][digit];
+                key_out[at] = key;
+                id_out[at] = id_in[i];
+            }
+            __syncthreads();
+            if (t < SORT_DIGITS)
+#pragma unroll
+                for (int w = 0; w < 16; ++w) base[t] += mine[w][t];
+            __syncthreads();
+        }
+    }
+    for (int32_t i = t; i < B; i += 1024) {
+        a.key_out[i] = sort_lds[from * B + i];
+        a.id_out[i] = ids[from * B + i];
+    }
+}
+
+struct SegArgs {
+    OwnArgs o;
+    const uint32_t *key, *id;   // sorted
+    int32_t V, seg, segs;       // positions of a stretch, stretches
+    float *head, *head_bias;    // segs x d, segs: what continues from the stretch before
+};
+
+// 256 columns of a stretch a wave, four columns a lane
+template <class T>
+__device__ inline void seg_terms(const SegArgs &a, int32_t seg, int32_t col)
+{
+    const int lane = threadIdx.x & 63;
+    if (seg >= a.segs) return;
+    const int32_t d = a.o.d, pos = seg * a.seg + lane, c0 = col + lane;
+    const bool in = lane < a.seg && pos < a.o.B;
+    const uint32_t key = in ? a.key[pos] : (uint32_t)a.V;
+    const int n = __popcll(__ballot(key < (uint32_t)a.V));   // sorted: the live ones come first
+    if (n == 0) return;
+    const int32_t q = in ? (int32_t)a.id[pos] : 0;
+    const float coef = lane < n ? a.o.coef[q] : 0.0f;
+    uint32_t before = __shfl_up(key, 1);
+    if (lane == 0) before = pos ? a.key[pos - 1] : ~0u;
+    const uint64_t begins = __ballot(key != before);
+    const T *h = (const T *)a.o.h;
+    const bool rows = a.o.own != nullptr, first_cols = col == 0;
+    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f}, sb = 0.0f;
+    int32_t owner = -1;   // the query that keeps the sum, -1: it continues
+    auto flush = [&] {
+        if (rows) {
+            float *to = owner < 0 ? a.head + (int64_t)seg * d : a.o.own + (int64_t)owner * d;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c0 + 64 * j < d) to[c0 + 64 * j] = acc[j];
+        }
+        if (first_cols && lane == 0) {
+            if (owner < 0) a.head_bias[seg] = sb;
+            else a.o.own_bias[owner] = sb;
+        }
+    };
+    for (int i0 = 0; i0 < n; i0 += OWN_AHEAD) {
+        float v[OWN_AHEAD][4];
+        if (rows)
+#pragma unroll
+            for (int u = 0; u < OWN_AHEAD; ++u) {
+                const T *from = h + (int64_t)__builtin_amdgcn_readlane(q, min(i0 + u, n - 1)) * a.o.h_stride;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[u][j] = c0 + 64 * j < d ? (float)from[c0 + 64 * j] : 0.0f;
+            }
+#pragma unroll
+        for (int u = 0; u < OWN_AHEAD; ++u) {
+            const int i = i0 + u;
+            if (i >= n) break;
+            if (begins >> i & 1) {
+                if (i) flush();
+                owner = __builtin_amdgcn_readlane(q, i);
+                if (first_cols && lane == i) a.o.first[key] = q;
+                acc[0] = acc[1] = acc[2] = acc[3] = sb = 0.0f;
+            }
+            const float c = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(coef), i));
+            sb += c;
+            if (rows)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j] = fmaf(c, v[u][j], acc[j]);
+        }
+    }
+    flush();
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void seg_kernel(SegArgs a)
+{
+    seg_terms<T>(a, blockIdx.x * 4 + (threadIdx.x >> 6), blockIdx.y * 256);
+}
+
+// What a point's queries left in the stretches after their first, by the block
+// of the first of these: 16 waves take equal shares of them, added in order.
+__global__ __launch_bounds__(1024) void seg_join_kernel(SegArgs a)
+{
+    __shared__ float part[16][256], part_bias[16];
+    const int32_t seg = blockIdx.x + 1;
+    const uint32_t key = a.key[(int64_t)seg * a.seg];
+    if (key >= (uint32_t)a.V || a.key[(int64_t)seg * a.seg - 1] != key) return;        // nothing continues
+    if (seg > 1 && a.key[(int64_t)(seg - 1) * a.seg - 1] == key) return;               // an earlier block's
+    int32_t last = seg, end = a.segs;   // the last stretch that begins with the key: last <= it < end
+    while (end - last > 1) {
+        const int32_t mid = last + (end - last) / 2;
+        if (a.key[(int64_t)mid * a.seg] == key) last = mid;
+        else end = mid;
+    }
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int32_t d = a.o.d, c0 = blockIdx.y * 256, per = (end - seg + 15) / 16;
+    const int32_t from = min(end, seg + wave * per), to = min(end, from + per);
+    const bool rows = a.o.own != nullptr;
+    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f}, sb = 0.0f;
+    if (rows)
+#pragma unroll 4
+        for (int32_t k = from; k < to; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c0 + lane + 64 * j < d) acc[j] += a.head[(int64_t)k * d + c0 + lane + 64 * j];
+    if (lane == 0 && blockIdx.y == 0)
+#pragma unroll 4
+        for (int32_t k = from; k < to; ++k) sb += a.head_bias[k];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) part[wave][lane + 64 * j] = acc[j];
+    if (lane == 0) part_bias[wave] = sb;
+    __syncthreads();
+    const int32_t owner = a.o.first[key], c = c0 + threadIdx.x;
+    if (rows && threadIdx.x < 256 && c < d) {
+        float s = a.o.own[(int64_t)owner * d + c];
+#pragma unroll
+        for (int w = 0; w < 16; ++w) s += part[w][threadIdx.x];
+        a.o.own[(int64_t)owner * d + c] = s;
+    }
+    if (threadIdx.x == 0 && blockIdx.y == 0) {
+        float s = a.o.own_bias[owner];
+#pragma unroll
+        for (int w = 0; w < 16; ++w) s += part_bias[w];
+        a.o.own_bias[owner] = s;
+    }
 }
 
 __global__ __launch_bounds__(256) void dbias_kernel(const float *col, int32_t tiles_b, int32_t cols_pad, int32_t n,
@@ -1595,14 +1905,16 @@ __device__ inline void dh_of_shares(const DhShares &a, const OwnArgs &o, int32_t
     ((T *)a.dh)[(int64_t)b * o.d + c] = (T)(a.scale * *a.factor * sum);
 }
 
-// Between the sweeps: a block per query and task. TH: 1024 threads where there
-// are many shares to add, which are many where there are few queries.
+// Between the sweeps: the queries' gradients, a block each, and beside them the
+// labels' own terms. TH: 1024 threads where there are many shares to add, which
+// are many where there are few queries.
 template <class T, int TH>
-__global__ __launch_bounds__(TH) void between_kernel(OwnArgs o, DhShares s)
+__global__ __launch_bounds__(TH) void between_kernel(OwnArgs o, DhShares s, SegArgs g)
 {
-    const int32_t b = (int32_t)blockIdx.x >= o.B ? blockIdx.x - o.B : blockIdx.x;
-    if (s.dh && (int32_t)blockIdx.x < o.B) dh_of_shares<T, TH>(s, o, b);
-    else if (o.first) own_terms<T, TH>(o, b);
+    const int32_t dh = s.dh ? o.B : 0, b = (int32_t)blockIdx.x - dh;   // d is at most 128
+    if (b < 0) dh_of_shares<T, TH>(s, o, blockIdx.x);
+    else if (g.key) seg_terms<T>(g, b * (TH / 64) + (threadIdx.x >> 6), 0);
+    else own_terms<T, TH>(o, b, 0);
 }
 
 // ---------------------------------------------------------------------------
@@ -1622,7 +1934,10 @@ struct Plan {
     int64_t copied;            // points that are held as a copy at a time
     int32_t dh_splits, dh_k, tile_d, tiles_d;
     int64_t off_h, off_c, off_part, off_loss, off_top, off_rowf, off_coef, off_label, off_pick, off_factor, off_done;
+    bool sorted;               // the queries are sorted by label for the labels' own terms
+    int32_t sort_tiles, seg, segs;
     int64_t off_p, off_col, off_dh, off_first, off_own, off_ownb, off_bias, off_hz, off_dc, total;
+    int64_t off_keys, off_counts, off_head, off_headb;   // sorted only
 };
 
 // Whether the tiles can be read where the points are: bfloat16 rows of whole
@@ -1754,6 +2069,16 @@ Plan make_plan(const boa_xent *x, bool grad)
         p.off_first = take(x->V * 4);
         p.off_ownb = take(x->B * 4);
         if (dc) p.off_own = take(x->B * (int64_t)x->d * 4);
+        p.sorted = x->B > SORT_FROM;
+        if (p.sorted) {
+            p.sort_tiles = (int32_t)ceil_div(x->B, SORT_TILE);
+            p.seg = x->B <= SORT_BLOCK ? 8 : 64;   // 64 lanes know a stretch; few queries give more waves something to do
+            p.segs = (int32_t)ceil_div(x->B, p.seg);
+            p.off_keys = take(4 * x->B * 4);   // keys and queries, before and after a pass
+            p.off_counts = take((int64_t)SORT_DIGITS * p.sort_tiles * 4);
+            if (dc) p.off_head = take((int64_t)p.segs * x->d * 4);
+            p.off_headb = take((int64_t)p.segs * 4);
+        }
     }
     p.total = at;
     return p;
@@ -1870,6 +2195,54 @@ struct Work {
         }
         return o;
     }
+
+    // the queries sorted by label: what seg_kernel takes
+    SegArgs sort(const OwnArgs &o) const
+    {
+        const int32_t B = (int32_t)x->B;
+        uint32_t *keys[2] = {at<uint32_t>(p.off_keys), at<uint32_t>(p.off_keys) + 2 * x->B};
+        SortArgs s{};
+        s.label = o.label, s.counts = at<uint32_t>(p.off_counts);
+        s.B = B, s.V = (int32_t)x->V, s.tiles = p.sort_tiles;
+        s.key_out = keys[0], s.id_out = keys[0] + x->B;
+        if (B <= SORT_BLOCK) {
+            run(sort_block_kernel, 1, 1024, (size_t)B * 12 + 17 * SORT_DIGITS * 4, st, s);
+        } else {
+            const dim3 tiles((uint32_t)p.sort_tiles);
+            int to = 0;
+            for (s.shift = 0; s.shift < 32 && (x->V >> s.shift); s.shift += 8) {   // keys up to V
+                s.key_out = keys[to], s.id_out = keys[to] + x->B;
+                sort_count_kernel<<<tiles, 256, 0, st>>>(s);
+                sort_scan_kernel<<<dim3(1), 1024, 0, st>>>(s.counts, SORT_DIGITS * p.sort_tiles);
+                sort_place_kernel<<<tiles, 256, 0, st>>>(s);
+                s.key_in = s.key_out, s.id_in = s.id_out;
+                to ^= 1;
+            }
+        }
+        SegArgs a{};
+        a.o = o, a.key = s.key_out, a.id = s.id_out, a.V = s.V, a.seg = p.seg, a.segs = p.segs;
+        a.head = x->dpoints ? at<float>(p.off_head) : nullptr, a.head_bias = at<float>(p.off_headb);
+        return a;
+    }
+
+    void join_segs(const SegArgs &a) const
+    {
+        const uint32_t cols = a.o.own ? (uint32_t)ceil_div(x->d, 256) : 1;
+        if (p.segs > 1) seg_join_kernel<<<dim3((uint32_t)p.segs - 1, cols), 1024, 0, st>>>(a);
+    }
+
+    // the labels' own terms, in launches of their own
+    void own_terms(const OwnArgs &o) const
+    {
+        const uint32_t cols = o.own ? (uint32_t)ceil_div(x->d, 256) : 1;
+        if (!p.sorted) {
+            own_kernel<T><<<dim3((uint32_t)x->B, cols), 256, 0, st>>>(o);
+            return;
+        }
+        const SegArgs a = sort(o);
+        seg_kernel<T><<<dim3((uint32_t)ceil_div(p.segs, 4), cols), 256, 0, st>>>(a);
+        join_segs(a);
+    }
 };
 
 template <class S>
@@ -1959,11 +2332,15 @@ int run_sweeps(const Work<T> &w)
         shares.factor = factor, shares.points = x->points, shares.points_stride = x->points_stride;
         shares.scale = x->scale, shares.dh = x->dh;
     }
-    if (dh || w.want_c())
-    {
-        const dim3 grid((uint32_t)(dh && w.want_c() ? 2 * B : B));
-        if (p.shares > 64) between_kernel<T, 1024><<<grid, 1024, 0, st>>>(own, shares);
-        else between_kernel<T, 256><<<grid, 256, 0, st>>>(own, shares);
+    if (dh || w.want_c()) {
+        SegArgs g{};
+        if (w.want_c() && p.sorted) g = w.sort(own);
+        const int threads = p.shares > 64 ? 1024 : 256;
+        const int64_t terms = !w.want_c() ? 0 : p.sorted ? ceil_div(p.segs, threads / 64) : B;
+        const dim3 grid((uint32_t)((dh ? B : 0) + terms));
+        if (threads == 1024) between_kernel<T, 1024><<<grid, 1024, 0, st>>>(own, shares, g);
+        else between_kernel<T, 256><<<grid, 256, 0, st>>>(own, shares, g);
+        if (g.key) w.join_segs(g);
     }
     if (w.want_c()) {
         SweepArgs g = c;
@@ -2061,7 +2438,7 @@ int run_tiles(const Work<T> &w)
     const OwnArgs oa = w.own();
     const int32_t *first = oa.first;
     const float *own = oa.own, *own_bias = oa.own_bias;
-    if (w.want_c()) own_kernel<T><<<dim3((uint32_t)B), 256, 0, st>>>(oa);
+    if (w.want_c()) w.own_terms(oa);
     const int64_t p_part = (int64_t)p.rows_pad * p.cols_pad;
     for (int32_t i = 0; i < pieces; ++i) {
         const int32_t v0 = (int32_t)(i * p.Vc), n = (int32_t)std::min<int64_t>(p.Vc, V - v0);

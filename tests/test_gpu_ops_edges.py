@@ -9,7 +9,7 @@ import torch
 
 import paper_2609_16175_amd as boa
 
-from test_gpu_ops import BF16, EPS, F32, gen, sums, unit, xent_case
+from test_gpu_ops import BF16, EPS, F32, gen, sums, unit, xent_case, xent_check, xent_run
 
 pytestmark = pytest.mark.gpu
 
@@ -114,3 +114,78 @@ def test_softmax_xent_points_copied_in_pieces(dt, B, V, d):
     e_b = p / B * (e_p + 8 * EPS)
     e_b[rows, labels] = (p[rows, labels] * e_p + 8 * EPS) / B
     assert ((r.dbias.double() - q.sum(0)).abs() <= 1.02 * (e_b.sum(0) + sums(B) * q.abs().sum(0)) + 1e-42).all()
+
+
+def labels_of(kind, B, V, seed):
+    g = gen(seed)
+    if kind == "equal":
+        return torch.full((B,), V // 3)
+    if kind == "few":      # a popular point, some others, and many queries left out
+        lab = (V ** torch.rand(B, generator=g)).long() - 1
+        lab[torch.rand(B, generator=g) < 0.3] = -1
+        lab[: B // 4] = V - 1
+        return lab
+    if kind == "runs":     # sorted already, runs of every length
+        return (torch.arange(B).double() ** 0.7).long().clamp(max=V - 1)
+    return torch.randint(V, (B,), generator=g)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("kind", ["random", "equal", "few", "runs"])
+@pytest.mark.parametrize("B,V,d", [(700, 90, 40), (2048, 60, 300), (2049, 255, 33), (3000, 256, 300), (4100, 1000, 128),
+                                   (9000, 37, 8)])
+def test_softmax_xent_queries_of_one_point(B, V, d, dt, kind):
+    h, pts, _, bias = xent_case(B, V, d, dt, seed=B + d, out=0.0)
+    case = (h, pts, labels_of(kind, B, V, 5), bias)
+    got = xent_run(case, 6.0)
+    xent_check(case, got, dt, 6.0, "mean")
+    again = xent_run(case, 6.0)
+    assert all(torch.equal(getattr(got, k), getattr(again, k)) for k in ("loss", "dh", "drows", "dbias"))
+    for rows, b in ((True, False), (False, True)):
+        r = boa.softmax_xent_grad(*(t.cuda() for t in case), 6.0, h_grad=False, rows_grad=rows, bias_grad=b)
+        assert r.drows is None or torch.equal(r.drows, got.drows)
+        assert r.dbias is None or torch.equal(r.dbias, got.dbias)
+
+
+@pytest.mark.parametrize("B,V,d", [(3000, 70_000, 48), (2500, 70_000, 260)])
+def test_softmax_xent_queries_of_one_point_among_many_points(B, V, d):
+    # labels of three bytes, with equal low and middle ones
+    case = xent_case(B, V, d, F32, seed=3, out=0.0)
+    labels = torch.tensor([3, 3 + 256, 3 + 65536, 69_999, 69_999 - 256, 0])[torch.randint(6, (B,), generator=gen(4))]
+    labels[::7] = torch.randint(V, (labels[::7].numel(),), generator=gen(5))
+    h, pts, labels, bias = (t.cuda() for t in (case[0], case[1], labels, case[3]))
+    r = boa.softmax_xent_grad(h, pts, labels, bias, 6.0, bias_grad=True)
+    H, rows = h.double(), torch.arange(B, device="cuda")
+    l = 6.0 * torch.mm(H, pts.double().t().contiguous()) + bias.double()
+    mag = 6.0 * float(H.norm(dim=1).max()) * float(pts.double().norm(dim=1).max())
+    e_p = 4 * sums(6 * d) * mag + 16 * EPS * float(l.abs().max()) + 2 * sums(V) + 32 * EPS
+    q = torch.softmax(l, 1)
+    e_q = q / B * (e_p + unit(F32))
+    q[rows, labels] -= 1
+    q /= B
+    e_q[rows, labels] = (e_p + 32 * EPS) / B
+    want = 6.0 * torch.mm(q.t().contiguous(), H)
+    e = 6.0 * torch.mm((e_q + sums(6 * B) * q.abs()).t().contiguous(), H.abs()) + unit(F32) * want.abs()
+    assert ((r.drows.double() - want).abs() <= 1.02 * e + 1e-42).all()
+    assert ((r.dbias.double() - q.sum(0)).abs() <= 1.02 * (e_q.sum(0) + sums(B) * q.abs().sum(0)) + 1e-42).all()
+
+
+@pytest.mark.parametrize("kind", ["random", "equal"])
+def test_softmax_xent_time_of_label_terms_grows_with_the_queries(kind):
+    # the points' gradient adds one product of three and the labels' own terms: not a multiple of the queries' gradient alone
+    B, V, d = 1 << 18, 1000, 32
+    h, pts = (torch.randn(n, d, generator=gen(n)).to(BF16).cuda() for n in (B, V))
+    labels = labels_of(kind, B, V, 6).cuda()
+
+    def ms(**kw):
+        start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        times = []
+        for _ in range(4):
+            start.record()
+            boa.softmax_xent_grad(h, pts, labels, scale=0.1, **kw)
+            stop.record()
+            stop.synchronize()
+            times.append(start.elapsed_time(stop))
+        return min(times)
+
+    assert ms() < 6 * ms(rows_grad=False)
