@@ -69,10 +69,12 @@ __global__ __launch_bounds__(256) void rows4_any_kernel(VecArgs a)
 // Bound by reading the codes: at half a byte per weight even the few steps
 // that turn a code into a number count, so the products run on the 16x16x32
 // bf16 matrix instruction and a code becomes a bf16 number in two steps: its
-// four bits under the exponent of 16 are 16 + q. x is held exactly as
-// bf16 parts (1 of bfloat16, 2 of float16, 3 of float32), each a column of its
-// own, and sum (16 + q) x has 24 (or 16) times sum x taken off by starting
-// there, which leaves sum (q - 8) x (or sum q x).
+// four bits under an exponent are 16 + q times a power of two, DOWN. x is held
+// exactly as bf16 parts (1 of bfloat16, 2 of float16, 3 of float32), each a
+// column of its own, and sum (16 + q) x has 24 (or 16) times sum x taken off by
+// starting there, which leaves sum (q - 8) x (or sum q x). All of them are DOWN
+// times what they stand for until the result is written: so sums over a chunk's
+// 32 values, up to 31 times as large as them each, stay finite for any finite x.
 //
 // A lane holds one row's chunk: lane l has row l & 15 and chunk l >> 4 of four
 // in a step of 128 k, so a wave reads 64 bytes of 16 rows at once. Lanes of
@@ -94,6 +96,7 @@ constexpr int FAST_WAVES = 8;               // per block
 constexpr int AHEAD = 2;                    // units of loads a wave keeps in flight
 constexpr int ROWS_W = 32;                  // rows of a wave: two tiles of 16
 constexpr size_t FAST_LDS = 64 << 10;       // x of one stretch of k, at most
+constexpr float DOWN = 1.0f / 2048.0f;      // a power of two, 32 x (31 + 24) of which stay below 1
 
 template <class T>
 constexpr int parts_v = sizeof(T) == 4 ? 3 : std::is_same<T, bf16_t>::value ? 1 : 2;
@@ -177,7 +180,7 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void rows4_kernel(FastArgs f)
             for (int j = 0; j < 4; ++j) {
                 const bf16x8 v = xs[((step * 4 + j) * NC + set) * 16 + at];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) sum += (float)v[k];
+                for (int k = 0; k < 8; ++k) sum += DOWN * (float)v[k];
             }
             ((float *)sums)[(step * NC + set) * 16 + at] = sum;
         }
@@ -217,7 +220,7 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void rows4_kernel(FastArgs f)
     const bool mine = (r >> 2) == chunk;
     const int x_at = mine ? chunk * 4 + (r & 3) : zero_at, x_step = mine ? NC * 64 : 0;
     // in registers, so that masking and setting the exponent are one instruction
-    uint32_t four_bits = 0x00780078u, sixteen = 0x41804180u;
+    uint32_t four_bits = 0x00780078u, sixteen = 0x3C003C00u;   // 16 DOWN, twice
     asm volatile("" : "+v"(four_bits));
     asm volatile("" : "+s"(sixteen));
     float y[2][NC * 4];
@@ -287,7 +290,7 @@ __global__ __launch_bounds__(64 * FAST_WAVES) void rows4_kernel(FastArgs f)
 #pragma unroll
         for (int u = 0; u < OUT; ++u) {
             const int m = 2 * u + (chunk & 1);
-            if (m < VALS && m < f.vectors) ((T *)a.y)[(int64_t)(f.m0 + m) * a.y_stride + row] = (T)out[u];
+            if (m < VALS && m < f.vectors) ((T *)a.y)[(int64_t)(f.m0 + m) * a.y_stride + row] = (T)(out[u] / DOWN);
         }
     };
 

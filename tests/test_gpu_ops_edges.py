@@ -9,7 +9,7 @@ import torch
 
 import paper_2609_16175_amd as boa
 
-from test_gpu_ops import BF16, EPS, F32, gen, sums, unit, xent_case, xent_check, xent_run
+from test_gpu_ops import BF16, EPS, F32, gen, rows4_case, rows4_check, sums, unit, xent_case, xent_check, xent_run
 
 pytestmark = pytest.mark.gpu
 
@@ -189,3 +189,20 @@ def test_softmax_xent_time_of_label_terms_grows_with_the_queries(kind):
         return min(times)
 
     assert ms() < 6 * ms(rows_grad=False)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("offsets", [False, True])
+@pytest.mark.parametrize("N,K,group", [(60, 128, 32), (2000, 256, 64), (40, 8192, 128), (60, 100, 20)])
+def test_matvec_4bit_values_next_to_the_largest(N, K, group, offsets, dt):
+    # whole groups of 32 and others; products well in range of values that are not far below the type's largest
+    x, q, codes, s, o = rows4_case(5, N, K, group, dt, F32, offsets, seed=K)
+    s, o = s * 1e-3, None if o is None else o * 1e-3
+    x[0] = (2e37 * x[0].float()).to(dt)
+    x[1] = (x[1].float().sign() * 3.3e38).to(dt)
+    x[2], x[2, 3] = 0, 2e37
+    x[3] = (1e-33 * x[3].float()).to(dt)
+    q[0] = 8
+    codes[0] = 0x88
+    y = boa.matvec_4bit(x.cuda(), codes.cuda(), s.cuda(), None if o is None else o.cuda(), group=group)
+    rows4_check(y, x, q, s, o, group, dt)
