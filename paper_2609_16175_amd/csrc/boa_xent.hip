@@ -383,6 +383,7 @@ __device__ inline void make_parts(const PartsArgs &a, int64_t i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = r < a.R && c + e < a.C ? (float)from[e] : 0.0f;
     }
+    float first[8] = {};
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
         bf16x8 part, nil;
@@ -393,7 +394,11 @@ __device__ inline void make_parts(const PartsArgs &a, int64_t i)
                 part[e] = (bf16_t)v[e];
             } else {
                 const float top = __uint_as_float(__float_as_uint(v[e]) & 0xFFFF0000u);
-                part[e] = (bf16_t)top;
+                // A point's infinity times a query's part of 0 would be NaN: the part is the smallest normal number,
+                // which alters no sum of products that is not itself next to that.
+                part[e] = (bf16_t)(p && a.labels && top == 0.0f && fabsf(first[e]) >= 0x1p-100f
+                                       ? copysignf(0x1p-126f, first[e]) : top);
+                if (p == 0) first[e] = top;
                 v[e] = fabsf(top) < INFINITY ? v[e] - top : 0.0f;   // an infinity or NaN is its first part alone
             }
         }
@@ -1448,8 +1453,20 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
     // streamed rows: thread t's slots are rows t / CH + i * (256 / CH), stored chunk t % CH
     constexpr int PER = SWEEP_THREADS / S::CH, ITS = (S::SR + PER - 1) / PER;
     const int slot_row = t / S::CH, slot_chunk = (t % S::CH) ^ sweep_swap<S::CH>(slot_row);
-    // a chunk past the values present meets zeros on the other side: any finite value of the row will do
-    const int slot_at = slot_chunk * 8 < a.Kp ? slot_chunk * 8 : 0;
+    // Chunks past the values present are zeros: the other side has zeros there, and
+    // whatever else the row holds, an infinity among it, would not do.
+    const int slot_at = slot_chunk * 8;
+    const bool present = slot_at < a.Kp;
+    if (!S::STAGED && !present)
+#pragma unroll
+        for (int i = 0; i < 2 * PARTS * ITS; ++i) {
+            if (S::SR % PER && wave * 64 >= S::SR * S::CH) continue;
+            bf16x8 nil;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) nil[e] = (bf16_t)0.0f;
+            *(bf16x8 *)(smem + i / (PARTS * ITS) * S::STAGE + i / ITS % PARTS * S::PLANE
+                        + (i % ITS * SWEEP_THREADS + t) * 16) = nil;
+        }
     auto dma = [&](int buf, int32_t stage) {
         uint8_t *to = smem + buf * S::STAGE;
         uint32_t side_at = t * 4;
@@ -1476,7 +1493,7 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
                 for (int i = 0; i < ITS; ++i) {
                     if (S::SR % PER && wave * 64 >= S::SR * S::CH) continue;
                     const uint32_t at = ((uint32_t)min(i * PER + row0, last) * (uint32_t)a.m_ld + slot_at) * 2;
-                    __builtin_amdgcn_global_load_lds(
+                    if (present) __builtin_amdgcn_global_load_lds(
                         (const __attribute__((address_space(1))) void *)(first + p * a.m_part * 2 + at),
                         (__attribute__((address_space(3))) void *)(to + p * S::PLANE + (i * SWEEP_THREADS + wave * 64) * 16),
                         16, 0, 0);

@@ -206,3 +206,30 @@ def test_matvec_4bit_values_next_to_the_largest(N, K, group, offsets, dt):
     codes[0] = 0x88
     y = boa.matvec_4bit(x.cuda(), codes.cuda(), s.cuda(), None if o is None else o.cuda(), group=group)
     rows4_check(y, x, q, s, o, group, dt)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("B", [3, 40, 150, 300])
+@pytest.mark.parametrize("d", [16, 20, 48, 80, 112, 128, 200, 272])
+def test_softmax_xent_points_with_infinities(d, B, dt):
+    # a coordinate of -inf against positive ones: the point's logits are -inf, and it adds nothing
+    h, pts, labels, bias = xent_case(B, 200, d, dt, seed=B + d, ignored=0.0, out=0.0)
+    labels = labels % 150
+    h[:, 0], h[:, 1], h[:, d - 1] = 1.0, 0.375, 1.7 + torch.arange(B) * 1e-3
+    bad = pts.clone()
+    bad[160, 0] = bad[170, 1] = bad[199, d - 1] = -math.inf
+    l = 3.0 * (h.double() @ bad.double().t()) + bias.double()
+    assert torch.isneginf(l[:, [160, 170, 199]]).all()
+    lse = torch.logsumexp(l, 1)
+    want = lse - l[torch.arange(B), labels]
+    r = boa.softmax_xent_grad(h.cuda(), bad.cuda(), labels.cuda(), bias.cuda(), 3.0, "none", bias_grad=True)
+    mag = 3.0 * (h.double().norm(dim=1) * pts.double().norm(dim=1).max()).max()
+    e = 4 * sums(6 * d) * mag + 16 * EPS * l[torch.isfinite(l)].abs().max() + sums(200) + 16 * EPS
+    assert ((r.loss.double().cpu() - want).abs() <= e + 4 * EPS * want).all()
+    assert ((r.lse.double().cpu() - lse).abs() <= e + 4 * EPS * lse.abs()).all()
+    assert torch.equal(r.loss, boa.softmax_xent(h.cuda(), bad.cuda(), labels.cuda(), bias.cuda(), 3.0, "none"))
+    p = torch.exp(l - lse[:, None])
+    p[torch.arange(B), labels] -= 1
+    assert not r.dbias[[160, 170, 199]].any() and not r.drows[[160, 170, 199]].any()
+    assert ((r.dbias.double().cpu() - p.sum(0)).abs() <= 1.02 * ((p.abs() * (2 * e + 16 * EPS)).sum(0) + B * (2 * e + 32 * EPS)
+                                                                 * torch.bincount(labels, minlength=200)) + 1e-42).all()
