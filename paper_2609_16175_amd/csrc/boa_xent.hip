@@ -1566,7 +1566,7 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
         fetch(s_begin);
         put(0);
     }
-    __syncthreads();
+    wait_and_meet<0>();   // a barrier alone does not wait for loads to LDS
     for (int32_t stage = s_begin; stage < s_end; ++stage) {
         const int buf = (stage - s_begin) & 1;
         if (stage + 1 < s_end) {
@@ -1734,7 +1734,7 @@ __global__ __launch_bounds__(SWEEP_THREADS, 2) void sweep_kernel(SweepArgs a)
             }
         }
         if (stage + 1 < s_end) put(buf ^ 1);
-        __syncthreads();
+        wait_and_meet<0>();
     }
 
 #pragma unroll
