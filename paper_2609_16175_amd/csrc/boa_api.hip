@@ -86,6 +86,11 @@ struct PhasePlan {
 
 }  // namespace
 
+// the operators' messages (boa_ops.h) go to the same buffer
+namespace boa {
+int set_error(int code, const char *msg) { return fail(code, msg); }
+}  // namespace boa
+
 // Scratch of the allocation-free search (boa_search_noalloc): one array per
 // GPU the library runs on, held until the process ends. Host code never
 // names it directly (in host code the name is a stand-in, not a device

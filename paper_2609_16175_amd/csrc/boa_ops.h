@@ -9,14 +9,8 @@
 
 namespace boa {
 
-// Records the thread's error message and returns the code. boa_last_error()
-// gives the thread's buffer (boa_api.hip's g_err, 512 characters); nobody else
-// holds it while a call of this thread runs.
-inline int set_error(int code, const char *msg)
-{
-    __builtin_snprintf(const_cast<char *>(boa_last_error()), 512, "%s", msg);
-    return code;
-}
+// Records the thread's error message for boa_last_error() and returns the code (boa_api.hip).
+int set_error(int code, const char *msg);
 
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;

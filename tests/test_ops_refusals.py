@@ -145,3 +145,15 @@ def test_xent_workspace_copies_two_gigabytes_of_points_at_most(dtype, B, V, d, g
     # beside the copy: up to 256 MB of probabilities, shares of the queries' gradient, biases and first queries of the points
     beside = (1 << 28) + 512 * 128 * (d + 16) * 4 + 8 * V if grad else 1 << 26
     assert 0 < L.boa_softmax_xent_workspace(C.byref(a), grad) <= (1 << 31) + beside
+
+
+def test_error_buffer_is_written_in_one_place():
+    # the thread's buffer and its size belong to one source; the operators hand their messages over
+    import glob
+    import os
+    from paper_2609_16175_amd import build
+    sources = {os.path.basename(f): open(f).read() for f in glob.glob(os.path.join(build.PKG, "csrc", "*"))}
+    assert [f for f, s in sources.items() if "g_err" in s] == ["boa_api.hip"]
+    assert not [f for f, s in sources.items() if "boa_last_error()" in s.replace("for boa_last_error()", "")]
+    # a message longer than most arrives whole
+    assert _xent(dtype=2) == EUNSUPPORTED and _err().endswith("use bfloat16 or float32")
