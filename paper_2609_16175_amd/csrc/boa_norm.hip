@@ -417,9 +417,12 @@ int check_norm(const char *what, const void *x, int64_t rows, int32_t d, int64_t
 
 int64_t back_blocks(int64_t rows, int32_t d)
 {
-    // as many partial rows as blocks: at most 4 per CU, fewer where the partial
-    // rows would outweigh the input
-    return std::max<int64_t>(1, std::min<int64_t>(MAX_BLOCKS, ceil_div(rows, 8)));
+    // As many partial rows as blocks: at most 4 per CU; fewer of few rows, so that
+    // writing and adding them stays small beside reading the rows, and of rows
+    // above 16,384 values, which fill the GPU with blocks of columns: 128 MB of
+    // them at most.
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(MAX_BLOCKS, ((int64_t)1 << 24) / d));
+    return std::max<int64_t>(1, std::min(most, ceil_div(rows, 8)));
 }
 
 }  // namespace

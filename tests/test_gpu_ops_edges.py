@@ -233,3 +233,24 @@ def test_softmax_xent_points_with_infinities(d, B, dt):
     assert not r.dbias[[160, 170, 199]].any() and not r.drows[[160, 170, 199]].any()
     assert ((r.dbias.double().cpu() - p.sum(0)).abs() <= 1.02 * ((p.abs() * (2 * e + 16 * EPS)).sum(0) + B * (2 * e + 32 * EPS)
                                                                  * torch.bincount(labels, minlength=200)) + 1e-42).all()
+
+
+@pytest.mark.parametrize("rows,d", [(1200, 100_000), (700, 1 << 20)])
+def test_layer_norm_widest_rows(rows, d):
+    # fewer partial rows than the rows alone would take
+    gn = torch.Generator("cuda").manual_seed(rows)
+    x, dy = (torch.empty(rows, d, dtype=BF16, device="cuda").normal_(generator=gn) for _ in range(2))
+    w = 1 + 0.3 * torch.randn(d, device="cuda", generator=gn)
+    y, mean, rstd = boa.layer_norm_forward(x, w, eps=1e-5)
+    dx, dw, db = boa.layer_norm_backward(dy, x, w, mean, rstd)
+    assert dw.dtype == db.dtype == F32
+    for c in (slice(0, 1000), slice(d - 1000, d), slice(65_000, 66_000)):
+        xh = (x[:, c].double() - mean.double()[:, None]) * rstd.double()[:, None]
+        g = dy[:, c].double()
+        # one stripe's additions in a row, then the stripes'; the value and its product are off by four roundings
+        e = (rows / 16 + 24) * EPS
+        assert ((dw[c].double() - (g * xh).sum(0)).abs() <= e * (g * xh).abs().sum(0)).all()
+        assert ((db[c].double() - g.sum(0)).abs() <= e * g.abs().sum(0)).all()
+    few = boa.layer_norm_forward(x[-3:], w, eps=1e-5)
+    assert torch.equal(y[-3:], few[0])
+    assert torch.equal(dx[-3:], boa.layer_norm_backward(dy[-3:], x[-3:], w, few[1], few[2])[0])

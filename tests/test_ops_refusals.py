@@ -157,3 +157,11 @@ def test_error_buffer_is_written_in_one_place():
     assert not [f for f, s in sources.items() if "boa_last_error()" in s.replace("for boa_last_error()", "")]
     # a message longer than most arrives whole
     assert _xent(dtype=2) == EUNSUPPORTED and _err().endswith("use bfloat16 or float32")
+
+
+def test_layer_norm_backward_workspace_is_bounded():
+    ws = ops._lib().boa_layer_norm_backward_workspace
+    assert ws(8, 768) == 2 * 768 * 4 and ws(1 << 20, 8192) == 1024 * 2 * 8192 * 4
+    for d in (1, 4096, 16_384, 16_385, 100_000, 1 << 20):
+        for rows in (0, 1, 9, 1 << 13, (1 << 31) - 1):
+            assert 0 < ws(rows, d) <= max(2 * d * 4, 1 << 27)
