@@ -254,3 +254,18 @@ def test_layer_norm_widest_rows(rows, d):
     few = boa.layer_norm_forward(x[-3:], w, eps=1e-5)
     assert torch.equal(y[-3:], few[0])
     assert torch.equal(dx[-3:], boa.layer_norm_backward(dy[-3:], x[-3:], w, few[1], few[2])[0])
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("B,d", [(40, 64), (40, 272), (90, 100), (300, 160)])
+def test_softmax_xent_query_left_out_touches_nothing(B, d, dt):
+    # whatever its vector holds: losses, the other queries', the points' and the biases' gradients stay as they are
+    h, pts, labels, bias = xent_case(B, 300, d, dt, seed=B, ignored=0.0, out=0.0)
+    labels[5] = labels[B - 1] = -1
+    clean = xent_run((h, pts, labels, bias), 3.0, "sum")
+    for value in (math.nan, math.inf, -math.inf):
+        bad = h.clone()
+        bad[5, 3] = bad[B - 1, d - 1] = value
+        r = xent_run((bad, pts, labels, bias), 3.0, "sum")
+        assert torch.equal(r.loss, clean.loss) and torch.equal(r.dbias, clean.dbias)
+        assert torch.equal(r.dh, clean.dh) and torch.equal(r.drows, clean.drows)
