@@ -310,8 +310,9 @@ const char *boa_last_error(void);
  *     is the caller's (16-byte aligned, at least as large as the matching
  *     _workspace function says) and must not serve two calls at once.
  *   - Sums, statistics and logits are float32 whatever the element type, and
- *     results are rounded to it once. Nothing is added in an order that depends
- *     on the schedule: the same inputs give the same bits.
+ *     results are rounded to it once; what is rounded before (the cross
+ *     entropy's probabilities in bfloat16) is named below. Nothing is added in
+ *     an order that depends on the schedule: the same inputs give the same bits.
  */
 enum { BOA_T_F32 = 0, BOA_T_BF16 = 1, BOA_T_F16 = 2 };
 
@@ -343,7 +344,11 @@ enum { BOA_REDUCE_NONE = 0, BOA_REDUCE_SUM = 1, BOA_REDUCE_MEAN = 2 };
  * Softmax cross entropy of B queries over V points as classes:
  *   logit[b][v] = scale * (h[b] . points[v]) + bias[v]
  *   loss[b] = log(sum_v exp(logit[b][v])) - logit[b][labels[b]]
- * The logits are formed in tiles and never stored.
+ * The logits are formed in tiles and never stored. The gradients are sums of
+ * probability times point or query: in bfloat16 each probability is rounded to
+ * bfloat16 as the operand of such a product (in float32 it keeps its 24 bits).
+ * The label's own entry, probability - 1, stays float32 in both and keeps its
+ * digits next to 0. dbias adds unrounded probabilities.
  */
 typedef struct {
     int32_t dtype;          /* of h, points, dh and dpoints: BOA_T_F32 or BOA_T_BF16 */
@@ -356,9 +361,11 @@ typedef struct {
     const int64_t *labels;  /* B: the point each query belongs to. A negative label leaves its
                                query out (loss 0, gradients 0, not counted by the mean); one of V
                                or more gives loss NaN and gradients 0 */
-    const float *bias;      /* V, or NULL. -inf leaves a point out; with every point left out a
-                               query's loss is +inf and its gradients are 0. For squared L2 in
-                               place of the inner product: scale = 2 t, bias[v] = -t |points[v]|^2 */
+    const float *bias;      /* V, or NULL. -inf leaves a point out (its values have to be finite
+                               all the same: a NaN or infinity times its probability of 0 is NaN);
+                               with every point left out a query's loss is +inf and its gradients
+                               are 0. For squared L2 in place of the inner product: scale = 2 t,
+                               bias[v] = -t |points[v]|^2 */
     float scale;
     int32_t reduction;      /* of the loss. BOA_REDUCE_MEAN divides by the queries not left out
                                (0 where there is none) */
@@ -372,7 +379,11 @@ typedef struct {
 } boa_xent;
 
 /* Work memory in bytes of one call with these arguments (grad: of
- * boa_softmax_xent_grad); a negative BOA_E* code for invalid sizes. */
+ * boa_softmax_xent_grad); a negative BOA_E* code for invalid sizes. It holds a
+ * copy of points that are not read in place: bfloat16 rows that are not 16-byte
+ * aligned or no multiple of 16 wide (all of them up to 128 values a row; wider
+ * ones up to 2 GB at a time), and float32 rows of more than 128 values with more
+ * than 32 queries (6 bytes a value, up to 2 GB at a time). */
 int64_t boa_softmax_xent_workspace(const boa_xent *x, int32_t grad);
 
 /* The losses. Errors: BOA_EINVAL, BOA_EUNSUPPORTED (float16: probabilities of

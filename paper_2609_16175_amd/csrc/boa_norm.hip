@@ -5,9 +5,9 @@
 // and g = dy w: dx = r (g - mean(g) - xh mean(g xh)); dw = sum over rows of
 // dy xh, db = sum over rows of dy.
 //
-// Both are bound by memory (65,536 rows of 1,024 bfloat16 values: 48.6 us
-// forward, 5.5 TB/s; 84.5 us backward, 4.8 TB/s; a large copy reaches 5.2): a
-// row is read once into registers (TPR threads, NV loads of 16 bytes each), its
+// Both are bound by memory (65,536 rows of 1,024 bfloat16 values: 48.5 us
+// forward, 5.5 TB/s, some of it from the last-level cache; 84.2 us backward,
+// 4.8 TB/s; a large copy reaches 5.2): a row is read once into registers (TPR threads, NV loads of 16 bytes each), its
 // sums are taken in float32 over the values
 // held (the variance from x - mu, so that a large mean costs no digits), and
 // the result is written from the same registers. The backward pass keeps each

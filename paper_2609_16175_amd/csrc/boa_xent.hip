@@ -9,8 +9,8 @@
 // tile routine for all of them (tile_product). float32 inputs are split into
 // three bf16 parts whose sum is the value (8 + 8 + 8 bits), and the six
 // products of parts above 2^-24 of the result are added: float32's precision
-// for six bf16 products, which the matrix instructions do in three eighths of
-// the time of a float32 one.
+// for six bf16 products, which the matrix instructions do in two thirds of the
+// time of a float32 one (large products reach 1,387 and 154 TFLOP/s).
 //
 // The losses take one pass over the points: a block keeps, per query, the
 // running maximum and sum of exponentials of its share of the points; the
@@ -235,11 +235,12 @@ struct Side {
 
 // acc += A[row0a ..][k] * B[row0b ..][k], k in [from_k, from_k + K). Loads run
 // STAGES - 1 stages ahead of the matrix instructions (a stage of 256 x 256 is
-// 1000 cycles of them, 3000 with parts), which bound it: 1,070 TFLOP/s in the
-// losses of 777 queries x 100,003 points x 768 float32 values, 910 to 960 in the
-// gradients' products, whose tiles are shorter. Of parts, the six products above
-// 2^-24 of the result are added, smallest first. ACROSS_A, ACROSS_B: the
-// operand's rows are k; F32_A, F32_B: it is float32 in memory.
+// 1000 cycles of them, 3000 with parts), which bound it: the losses of 777
+// queries x 100,003 points x 768 float32 values take 0.80 ms, 1,030 TFLOP/s for
+// the 896 rows that are multiplied (890 for the 777), the gradients' products,
+// whose tiles are shorter, 0.90 to 0.95 ms each, 870 to 920 (755 to 800). Of
+// parts, the six products above 2^-24 of the result are added, smallest first.
+// ACROSS_A, ACROSS_B: the operand's rows are k; F32_A, F32_B: it is float32 in memory.
 template <class S, bool ACROSS_A, bool ACROSS_B, bool F32_A = false, bool F32_B = false>
 __device__ inline void tile_product(const Product &pr, int32_t row0a, int32_t row0b, bf16_t *lds,
                                     f32x16 (&acc)[S::TM][S::TN], int32_t from_k, int32_t K)
@@ -1323,10 +1324,12 @@ __global__ __launch_bounds__(256) void dh_join_kernel(const float *part, int32_t
 // by 2^8: the sums have room for that, and the output is scaled rarely.
 //
 // A tile of 32 x 32 logits is 512 cycles of matrix instructions at 128 values
-// and about 600 of vector instructions (16 cycles of them for each exponential),
-// which two waves per SIMD overlap in part: 2,048 queries x 1,000,000 points x
-// 128 values take 1.08 ms in SWEEP_H and 1.05 ms in SWEEP_C (970 and 1,000
-// TFLOP/s; a large library product reaches 1,387). Forming the logits again in
+// and some 750 of vector instructions (about 120 of them at 4 cycles, 16
+// exponentials at 16). 2,048 queries x 1,000,000 points x 128 values take
+// 1.11 ms in SWEEP_H and 1.09 ms in SWEEP_C (940 and 960 TFLOP/s; a large library
+// product reaches 1,387), which is some 1,300 cycles a tile: nearly the sum. Both
+// tiles of a wave pass each phase together, with scheduling barriers between the
+// phases, and the two waves of a SIMD hardly overlap. Forming the logits again in
 // SWEEP_C costs 2 d operations a logit; storing and reading them back would be
 // 6 bytes, more than twice the time at d = 128.
 enum { SWEEP_LOSS = 0, SWEEP_H = 1, SWEEP_C = 2 };
@@ -1348,7 +1351,9 @@ struct Sweep {
     static constexpr int OUT_LD = DT * 32 + 4;               // floats of a row of the output in LDS
     // The kept rows' last k steps lie in LDS where the registers do not hold
     // them all: a spilled one would be waited for together with the loads on
-    // their way to the next stage.
+    // their way to the next stage. SWEEP_H of 64 rows and 128 values a wave still
+    // spills 11 registers, addresses that are read back once a stage before its
+    // loads; with 32 rows shared by four waves 23, outside the loop.
     static constexpr int KS = 2 * DT, SHED = MODE != SWEEP_LOSS && PARTS * TN * DT >= 8 ? (MODE == SWEEP_H ? 2 : 1) : 0;
     static constexpr size_t lds()
     {
@@ -2025,8 +2030,9 @@ Plan make_plan(const boa_xent *x, bool grad)
         // columns of dh's product: 256, or 128 where that leaves 15% less past the end
         p.tile_d = round_up(x->d, 256) * 100 > round_up(x->d, 128) * 115 ? 128 : 256;
         p.tiles_d = (int32_t)ceil_div(x->d, p.tile_d);
-        // A piece's probabilities take up to 256 MB. Of the numbers of pieces
-        // that do, the one whose launches fill the GPU best: each launch takes
+        // A piece's probabilities take up to 256 MB, or four tiles of points where
+        // there are more than 131,072 queries (43,690 with parts). Of the numbers
+        // of pieces that do, the one whose launches fill the GPU best: each launch takes
         // whole rounds of resident blocks.
         // Points that cannot be read where they are get a copy: of all of them up
         // to 2 GB, so that it serves both passes, else a piece at a time, which

@@ -282,7 +282,9 @@ def softmax_xent_grad(h, rows, labels, bias=None, scale=1.0, reduction="mean", d
     logits = scale * h @ rows.T + bias, never stored. labels: int64 (B,), the
     point of each query; a negative one leaves its query out. bias: float32
     (V,), -inf leaves a point out. dloss: the gradient of the loss (default 1).
-    h_grad, rows_grad, bias_grad: which gradients to compute."""
+    h_grad, rows_grad, bias_grad: which gradients to compute. In bfloat16 the
+    probabilities, but for the labels' own, are rounded to bfloat16 as operands
+    of the gradients' products; the results are rounded once."""
     if bias_grad and bias is None:
         raise ValueError("softmax_xent: a gradient of bias without a bias")
     return _xent("softmax_xent", h, rows, labels, bias, scale, reduction, stream, True, dloss, h_grad, rows_grad, bias_grad)
@@ -290,7 +292,8 @@ def softmax_xent_grad(h, rows, labels, bias=None, scale=1.0, reduction="mean", d
 
 class _SoftmaxXent(torch.autograd.Function):
     # The gradients are formed in the forward pass, where the points pass by
-    # anyway; backward scales them. Unreduced losses have a gradient per
+    # anyway; backward scales them, which rounds bfloat16 gradients a second
+    # time where dloss is no power of two. Unreduced losses have a gradient per
     # query, which the points' gradient cannot be scaled by afterwards:
     # there, backward does the whole work.
     @staticmethod
@@ -321,7 +324,10 @@ class _SoftmaxXent(torch.autograd.Function):
 
 def softmax_xent(h, rows, labels, bias=None, scale=1.0, reduction="mean"):
     """The loss of softmax_xent_grad, for autograd; without gradients to
-    compute, the losses alone."""
+    compute, the losses alone. A reduced loss' gradients are formed with it and
+    multiplied by the gradient that arrives, in h's and rows' type: bfloat16
+    ones are rounded a second time then. softmax_xent_grad with dloss rounds
+    once."""
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (h, rows, bias)):
         return _SoftmaxXent.apply(h, rows, labels, bias, scale, reduction)
     return _xent("softmax_xent", h, rows, labels, bias, scale, reduction, None, False).loss
@@ -336,7 +342,8 @@ def matvec_4bit(x, codes, scales, offsets=None, group=None, stream=None):
 
     x: (M, K) or (K,), float32, bfloat16 or float16. codes: uint8 (N, K / 2),
     value 2j in the low nibble of byte j. scales, offsets: (N, groups) of one
-    floating type. group: values of k per scale (default K / groups)."""
+    floating type. group: values of k per scale (default K / groups). For
+    serving: autograd does not see it."""
     _device("matvec_4bit", x, codes, scales, offsets)
     dt = _dtype("matvec_4bit", x)
     sd = _dtype("matvec_4bit", scales)

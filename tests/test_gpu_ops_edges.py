@@ -269,3 +269,33 @@ def test_softmax_xent_query_left_out_touches_nothing(B, d, dt):
         r = xent_run((bad, pts, labels, bias), 3.0, "sum")
         assert torch.equal(r.loss, clean.loss) and torch.equal(r.dbias, clean.dbias)
         assert torch.equal(r.dh, clean.dh) and torch.equal(r.drows, clean.drows)
+
+
+@pytest.mark.parametrize("B,d", [(3000, 40), (9000, 40), (3000, 300)])
+def test_softmax_xent_many_queries_in_a_graph_and_on_another_stream(B, d):
+    h, pts, labels, bias = (t.cuda() for t in xent_case(B, 500, d, BF16, seed=B, out=0.0))
+    labels[: B // 3] = 7
+
+    def step(stream=None):
+        r = boa.softmax_xent_grad(h, pts, labels, bias, 4.0, bias_grad=True, stream=stream)
+        return [r.loss, r.lse, r.dh, r.drows, r.dbias]
+
+    want = step()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = step(side)
+    side.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in range(4):
+        for t in out:
+            t.fill_(float("nan"))
+        h.mul_(1.25)
+        labels.copy_(labels.roll(11))
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(out, want)), k
