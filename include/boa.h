@@ -409,6 +409,62 @@ int boa_matvec_fourbit(const void *x, int64_t M, int64_t x_stride, int32_t dtype
                        int32_t K, int64_t codes_stride, const void *scales, const void *offsets, int64_t scale_stride,
                        int32_t scale_dtype, int32_t group, void *y, int64_t y_stride, void *stream);
 
+#define BOA_MAX_LINEAR (1 << 17)
+#define BOA_LINEAR_FEW 64       /* rows up to which a 16-bit forward pass takes no work memory, */
+#define BOA_LINEAR_FEW_F32 16   /* and a float32 one */
+enum { BOA_ACT_NONE = 0, BOA_ACT_RELU = 1, BOA_ACT_SILU = 2, BOA_ACT_GELU = 3, BOA_ACT_GELU_TANH = 4 };
+/*
+ * A linear layer on M rows, with what follows it:
+ *   z = x w^T + bias        y = act(z) + residual
+ * act: max(z, 0); silu z / (1 + e^-z); gelu z (1 + erf(z / sqrt 2)) / 2;
+ * gelu_tanh z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2. And its gradients:
+ *   dz = dy act'(z)    dx = dz w    dw = dz^T x    dbias = sum over rows of dz
+ * (the residual's is dy). x, w, residual, y and their gradients have one type.
+ * Sums are float32. In bfloat16 and float16, z is kept in float16, clamped to its
+ * range (every act' is constant beyond it), and dz is rounded to the layer's type
+ * as an operand of the two products, not in dbias. In float32, with more than
+ * BOA_LINEAR_FEW_F32 rows or in the gradients, the products' operands are
+ * rounded to 22 bits (values far below the largest of their row, or of their
+ * column where the sum runs over rows, to 2^-40 of that). A non-finite value
+ * makes the results that it takes part in NaN or infinite.
+ */
+typedef struct {
+    int32_t dtype;          /* any of the three */
+    int32_t activation;     /* BOA_ACT_* */
+    int64_t M;              /* 0 .. 2^31 - 1 */
+    int32_t N, K;           /* 1 .. BOA_MAX_LINEAR */
+    const void *x;          /* M x K */
+    int64_t x_stride;
+    const void *w;          /* N x K */
+    int64_t w_stride;
+    const void *bias;       /* N, or NULL */
+    int32_t param_dtype;    /* of bias and dbias: dtype or BOA_T_F32 */
+    const void *residual;   /* M x N, or NULL */
+    int64_t residual_stride;
+    void *y;                /* M x N, dense */
+    void *pre;              /* z for the backward pass: M x N, dense, float16 (float32 where dtype is);
+                               NULL: not kept. The gradients read it unless the activation is BOA_ACT_NONE */
+    /* gradients (boa_linear_grad only); bias, residual and y are not read */
+    const void *dy;         /* M x N */
+    int64_t dy_stride;
+    void *dx;               /* M x K, dense, or NULL */
+    void *dw;               /* N x K, dense, or NULL */
+    void *dbias;            /* N, or NULL */
+} boa_dense;
+
+/* Work memory in bytes of one call with these arguments (grad: of
+ * boa_linear_grad); a negative BOA_E* code for invalid ones. It holds copies of
+ * operands that cannot be read in place (16-bit rows that are not 16-byte
+ * aligned or no multiple of 8 wide, float32 rows as parts), dz, and the shares
+ * of sums that are split. */
+int64_t boa_linear_workspace(const boa_dense *d, int32_t grad);
+
+/* The layer. Errors: BOA_EINVAL, BOA_EHIP. */
+int boa_linear(const boa_dense *d, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Its gradients. */
+int boa_linear_grad(const boa_dense *d, void *workspace, int64_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -276,7 +276,7 @@ class Index:
 
 # The query-tower operators (ops.py), loaded on first use: they import torch.
 _OPS = ("layer_norm", "layer_norm_forward", "layer_norm_backward", "softmax_xent", "softmax_xent_grad", "XentResult",
-        "matvec_4bit")
+        "matvec_4bit", "linear", "linear_forward", "linear_backward")
 
 
 def __getattr__(name):

@@ -1,0 +1,319 @@
+// Matrix products of the query tower's layers on the 16-bit matrix
+// instructions: out[p][q] = sum_k a(p, k) b(q, k), float32 sums.
+//
+// An operand's rows run along k, or "across": a row is then one k and runs
+// along the operand's own dimension. A linear layer's forward product has both
+// along k, its input's gradient the weights across, its weights' gradient both.
+// Float32 operands come as two f16 parts (parts below), and three products.
+#pragma once
+
+#include "boa_ops.h"
+
+namespace boa {
+
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+typedef bf16_t bf16x4 __attribute__((ext_vector_type(4)));
+typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
+typedef f16_t f16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+template <class T>
+struct Vec;
+template <>
+struct Vec<bf16_t> {
+    typedef bf16x8 v8;
+    typedef bf16x4 v4;
+};
+template <>
+struct Vec<f16_t> {
+    typedef f16x8 v8;
+    typedef f16x4 v4;
+};
+
+__device__ inline f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// One operand: rows `ld` values apart from a 16-byte aligned address, ld a
+// multiple of 8 and below 2^21, whole 16-byte chunks in every row. `own`: its extent in the
+// output. part: values from one part to the next. batch: from one product of a
+// batch to the next.
+struct Operand {
+    const void *p;
+    int64_t ld, part, batch;
+    int32_t own;
+};
+
+// The products that parts give: the ones above 2^-22 of the result, smallest first.
+struct Product {
+    Operand a, b;
+    int32_t K;         // of each part
+    int32_t terms;     // 1, or 3 of two parts: a1 b0, a0 b1, a0 b0
+    int32_t tiles_a, tiles_b, splits, batches;
+    int32_t steps;     // of k a split takes
+};
+
+// A block's tile: WA x WB waves of TA x TB tiles of 32 x 32, BK values of k a stage.
+template <class T_, int WA_, int WB_, int TA_, int TB_, int STAGES_>
+struct Tile {
+    typedef T_ T;
+    static constexpr int WA = WA_, WB = WB_, TA = TA_, TB = TB_, STAGES = STAGES_;
+    static constexpr int BA = WA * TA * 32, BB = WB * TB * 32, THREADS = 64 * WA * WB, BK = 64;
+    static constexpr int STAGE = (BA + BB) * BK;   // values
+    // columns that a wave turns over at a time at the end, and what that takes
+    static constexpr int TURN_COLS = TB % 2 ? 32 : 64, TURN_BYTES = TA * 32 * (TURN_COLS + 4) * 4;
+    static constexpr int LDS = STAGE * STAGES * 2 > WA * WB * TURN_BYTES ? STAGE * STAGES * 2 : WA * WB * TURN_BYTES;
+};
+
+constexpr uint32_t NOWHERE = 0x80000000u;   // an offset past every buffer: such loads give zeros
+
+// A buffer of 2^31 - 1 bytes from an address that all lanes share.
+__device__ inline words4 buffer_at(const void *p)
+{
+    const uint64_t a = (uint64_t)p;
+    words4 r;
+    r[0] = __builtin_amdgcn_readfirstlane((uint32_t)a);
+    r[1] = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+    r[2] = 0x7FFFFFFFu;
+    r[3] = 0x00027000u;
+    return r;
+}
+
+template <class T>
+__device__ inline uint32_t lds_address(const T *p)
+{
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const T *)p;
+}
+
+// 16 bytes a lane from the buffer to LDS, lane after lane from `to`; an offset
+// past the buffer's end gives zeros. Written out because the compiler waits for
+// all such loads that it knows of before any transposed read; here the kernel's
+// own waits count them.
+__device__ inline void load_to_lds(words4 buffer, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(buffer)
+                 : "memory");
+}
+
+// One operand's side of a stage: where this thread's loads come from, and where
+// its fragments lie.
+//
+// Along k, a stage holds ROWS rows of 64 values whose 16-byte chunks are stored
+// in the order chunk ^ (row & 7); across, 64 rows of ROWS values in the order
+// chunk ^ (row & 3) * 4, and fragments are read transposed, 64 bytes of four
+// rows by half a wave. Either way what lanes read together spreads over the
+// banks. The permutation is applied to the addresses loaded from, since a load
+// to LDS writes its lanes in order. Rows past the operand's end and k past K are
+// loaded as zeros (an offset that the buffer's bounds check refuses).
+template <class S, int ROWS, bool ACROSS>
+struct Side {
+    typedef typename S::T T;
+    static constexpr int CHUNKS = ACROSS ? ROWS / 8 : S::BK / 8;   // of an LDS row
+    static constexpr int N = ROWS * (S::BK / 8) / S::THREADS;     // loads of a stage
+    static constexpr int PER = S::THREADS / CHUNKS;               // LDS rows of one load of all threads
+    static_assert(N * S::THREADS == ROWS * (S::BK / 8) && PER * CHUNKS == S::THREADS, "whole loads");
+    static_assert(ACROSS ? PER % 4 == 0 || N == 1 : PER % 8 == 0, "one permutation for all of a thread's loads");
+    uint32_t at[N];   // byte offsets from the stage's base
+    int32_t k;        // of load 0 (across: + PER each)
+
+    __device__ static int swap(int row) { return ACROSS ? (ROWS >= 128 ? (row & 3) * 4 : (row & 1) * 4) : row & 7; }
+
+    __device__ Side(const Operand &o, int32_t own0)
+    {
+        const int t = threadIdx.x, row = t / CHUNKS, chunk = t % CHUNKS ^ swap(t / CHUNKS);
+        if constexpr (ACROSS) {
+            k = row;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                at[i] = own0 + chunk * 8 < o.own ? (uint32_t)(row + i * PER) * (uint32_t)o.ld * 2 + chunk * 16 : NOWHERE;
+        } else {
+            k = chunk * 8;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                at[i] = own0 + row + i * PER < o.own ? (uint32_t)(row + i * PER) * (uint32_t)o.ld * 2 + chunk * 16 : NOWHERE;
+        }
+    }
+    // loads a stage from `base`, of which the first k_left values of k count
+    __device__ void load(T *to, const T *base, int32_t k_left) const
+    {
+        const words4 rsrc = buffer_at(base);
+        const uint32_t lds = lds_address(to) + (threadIdx.x >> 6) * 1024;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t off = k + (ACROSS ? i * PER : 0) < k_left ? at[i] : NOWHERE;
+            load_to_lds(rsrc, off, __builtin_amdgcn_readfirstlane(lds + i * S::THREADS * 16));
+        }
+    }
+    // where this lane's fragments begin in a stage, in bytes; row0: the wave's first row of the tile
+    __device__ static uint32_t lane_at(int row0)
+    {
+        const int lane = threadIdx.x & 63, half = lane >> 5, r = lane & 31;
+        if constexpr (ACROSS) {
+            const int row = 8 * half + ((lane & 15) >> 2), chunk = row0 / 8 + ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
+            return row * ROWS * 2 + (chunk ^ swap(row)) * 16 + (lane & 1) * 8;
+        } else {
+            return (row0 + r) * S::BK * 2 + (half ^ swap(r)) * 16;
+        }
+    }
+    // The fragment of the wave's tile i and k step s. `at`: lane_at plus the
+    // stage; tiles and steps are exclusive ors on bits that nothing carries into.
+    __device__ static typename Vec<T>::v8 fragment(uint32_t at, int i, int s)
+    {
+        typedef typename Vec<T>::v8 v8;
+        typedef typename Vec<T>::v4 v4;
+        if constexpr (ACROSS) {
+            typedef __attribute__((address_space(3))) short4v Four;
+            v8 f;
+#pragma unroll
+            for (int jj = 0; jj < 2; ++jj) {
+                const uint32_t a = (at ^ (i * 64)) + (16 * s + 4 * jj) * ROWS * 2;
+                const v4 v = __builtin_bit_cast(v4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four *)(uintptr_t)a));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[4 * jj + e] = v[e];
+            }
+            return f;
+        } else {
+            typedef __attribute__((address_space(3))) v8 Row;
+            return *(const Row *)(uintptr_t)((at ^ (s * 32)) + i * 32 * S::BK * 2);
+        }
+    }
+};
+
+// Waits until at most LEFT of this wave's loads are on their way and its LDS
+// reads are done, then for the other waves.
+template <int LEFT>
+__device__ inline void wait_and_meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
+// What a block works on.
+struct Place {
+    int32_t ta, tb, split, batch;
+};
+
+// Work item of a block. Blocks go to the 8 XCDs in turn; each XCD takes a run of
+// tiles that share operand rows in its L2: bands of 8 tiles of a, one tile of b
+// after the other.
+__device__ inline Place place_of(const Product &pr)
+{
+    const uint32_t n = gridDim.x, id = blockIdx.x;
+    const uint32_t x = id & 7, per = n >> 3, extra = n & 7;
+    uint32_t t = x * per + min(x, extra) + (id >> 3);
+    const uint32_t tiles = (uint32_t)pr.tiles_a * pr.tiles_b;
+    Place w;
+    const uint32_t layer = t / tiles;
+    t -= layer * tiles;
+    w.batch = layer / pr.splits;
+    w.split = layer - w.batch * pr.splits;
+    const uint32_t band = t / (8 * pr.tiles_b), first = band * 8, rows = min(8u, pr.tiles_a - first);
+    t -= band * 8 * pr.tiles_b;
+    w.tb = t / rows;
+    w.ta = first + t - w.tb * rows;
+    return w;
+}
+
+// acc[i][j] += tile i of b times tile j of a: lane (l & 31) holds row j * 32 +
+// (l & 31) of a's side, its values e columns i * 32 + 8 (e / 4) + 4 (l / 32) +
+// e % 4 of b's side. Loads run STAGES - 1 stages ahead.
+template <class S, bool ACROSS_A, bool ACROSS_B>
+__device__ inline void tile_product(const Product &pr, const Place &w, typename S::T *lds, f32x16 (&acc)[S::TB][S::TA])
+{
+    typedef typename S::T T;
+    constexpr int STAGES = S::STAGES, BK = S::BK;
+    using A = Side<S, S::BA, ACROSS_A>;
+    using B = Side<S, S::BB, ACROSS_B>;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wa = wave % S::WA, wb = wave / S::WA;
+    const int32_t a0 = w.ta * S::BA, b0 = w.tb * S::BB;
+    const A a(pr.a, a0);
+    const B b(pr.b, b0);
+    const int32_t all = (pr.K + BK - 1) / BK;
+    const int32_t from = w.split * pr.steps, steps = min(pr.steps, all - from), total = steps * pr.terms;
+    const T *pa = (const T *)pr.a.p + w.batch * pr.a.batch + (ACROSS_A ? (int64_t)a0 : a0 * pr.a.ld);
+    const T *pb = (const T *)pr.b.p + w.batch * pr.b.batch + (ACROSS_B ? (int64_t)b0 : b0 * pr.b.ld);
+    int32_t term = pr.terms - 1, step = 0, stage = 0;   // of the next load; the last term is a0 b0
+    auto load = [&]() {
+        const int32_t k0 = (from + step) * BK;
+        const T *at_a = pa + (term == 2 ? pr.a.part : 0) + (ACROSS_A ? k0 * pr.a.ld : (int64_t)k0);
+        const T *at_b = pb + (term == 1 ? pr.b.part : 0) + (ACROSS_B ? k0 * pr.b.ld : (int64_t)k0);
+        const int32_t left = term < 0 ? 0 : pr.K - k0;   // past the end zeros, which nothing reads
+        T *to = lds + stage * S::STAGE;
+        a.load(to, at_a, left);
+        b.load(to + S::BA * BK, at_b, left);
+        if (++stage == STAGES) stage = 0;
+        if (++step == steps) step = 0, --term;
+    };
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) T *)lds;
+    const uint32_t lane_a = A::lane_at(wa * S::TA * 32), lane_b = B::lane_at(wb * S::TB * 32) + S::BA * BK * 2;
+    for (int i = 0; i < STAGES - 1; ++i) load();
+    int32_t cur = 0;
+    for (int32_t it = 0; it < total; ++it) {
+        wait_and_meet<(STAGES - 2) * (A::N + B::N)>();
+        load();
+        const uint32_t at_a = base + cur * S::STAGE * 2 + lane_a, at_b = base + cur * S::STAGE * 2 + lane_b;
+        if (++cur == STAGES) cur = 0;
+#pragma unroll
+        for (int s = 0; s < BK / 16; ++s) {
+            typename Vec<T>::v8 fa[S::TA], fb[S::TB];
+#pragma unroll
+            for (int j = 0; j < S::TA; ++j) fa[j] = A::fragment(at_a, j, s);
+#pragma unroll
+            for (int i = 0; i < S::TB; ++i) fb[i] = B::fragment(at_b, i, s);
+#pragma unroll
+            for (int i = 0; i < S::TB; ++i)
+#pragma unroll
+                for (int j = 0; j < S::TA; ++j) acc[i][j] = mfma32(fb[i], fa[j], acc[i][j]);
+        }
+    }
+    wait_and_meet<0>();
+}
+
+template <class S>
+__device__ inline void clear(f32x16 (&acc)[S::TB][S::TA])
+{
+#pragma unroll
+    for (int i = 0; i < S::TB; ++i)
+#pragma unroll
+        for (int j = 0; j < S::TA; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+}
+
+// Hands the sums out in runs of eight neighbouring columns: f(row of a's side,
+// first column of b's side, the eight sums in LDS). Each wave turns its tiles over
+// in its own piece of LDS, two columns of tiles at a time, so that what follows is written
+// once, and stores fill whole lines. The stages must no longer be in use.
+template <class S, class F>
+__device__ inline void each_run(const Place &w, const f32x16 (&acc)[S::TB][S::TA], char *lds, F f)
+{
+    constexpr int WIDE = S::TURN_COLS / 32, RUNS = S::TURN_COLS / 8, LD = S::TURN_COLS + 4;   // + 4: rows begin in other banks
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wa = wave % S::WA, wb = wave / S::WA;
+    const int lane = threadIdx.x & 63, half = lane >> 5, r = lane & 31;
+    float *mine = (float *)lds + wave * (S::TURN_BYTES / 4);
+    const int32_t p0 = w.ta * S::BA + wa * S::TA * 32, q0 = w.tb * S::BB + wb * S::TB * 32;
+#pragma unroll
+    for (int i0 = 0; i0 < S::TB; i0 += WIDE) {
+#pragma unroll
+        for (int i = 0; i < WIDE; ++i)
+#pragma unroll
+            for (int j = 0; j < S::TA; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x16 &v = acc[i0 + i][j];
+                    *(f32x4 *)(mine + (j * 32 + r) * LD + i * 32 + g * 8 + half * 4) =
+                        f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+                }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int k = lane; k < S::TA * 32 * RUNS; k += 64) {
+            const int row = k / RUNS, run = k % RUNS;
+            f(p0 + row, q0 + i0 * 32 + run * 8, (const float *)(mine + row * LD + run * 8));
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+}  // namespace boa

@@ -1,0 +1,885 @@
+// Linear layers with bias, activation and residual in the product's epilogue,
+// and their gradients.
+//
+//   z = x w^T + bias        y = act(z) + residual
+//   dz = dy act'(z)         dx = dz w         dw = dz^T x         dbias = sum over rows of dz
+//
+// A few rows (serving) read the weights once and are bound by that; more are
+// bound by the matrix instructions. 16-bit operands go there as they are, with
+// float32 sums; z is kept for the backward pass in f16 (11 bits, clamped to its
+// range, where every activation's slope is constant), and dz, an operand of two
+// products, is rounded to the layer's type. Float32 operands become two f16
+// parts of 11 bits each, scaled by a power of two per row (or per column, where
+// the sum runs over rows) so that the largest value lies below 2^15: three
+// products, each value exact to 2^-22 of itself or 2^-40 of its row's largest.
+// That is 3 / 16 of the time of float32 instructions; z stays float32.
+#include <algorithm>
+#include <type_traits>
+
+#include "boa_gemm.h"
+
+using namespace boa;
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// activations
+
+constexpr float SQRT_HALF = 0.70710678118654752f;
+constexpr float INV_SQRT_2PI = 0.39894228040143268f;
+constexpr float SQRT_2_PI = 0.79788456080286536f;
+constexpr float CUBE = 0.044715f;
+
+// FINE: float32 layers. The short exponential is off by some 2^-22 of its value
+// for arguments that matter, far below 16 bits' rounding.
+template <bool FINE>
+__device__ inline float exp_of(float v) { return FINE ? expf(v) : __expf(v); }
+
+template <bool FINE>
+__device__ inline float sigmoid(float z) { return 1.0f / (1.0f + exp_of<FINE>(-z)); }
+
+template <bool FINE>
+__device__ inline float act_of(float z, int32_t act)
+{
+    switch (act) {
+    case BOA_ACT_RELU: return z > 0.0f ? z : z != z ? z : 0.0f;
+    case BOA_ACT_SILU: return z == -INFINITY ? -0.0f : z * sigmoid<FINE>(z);
+    case BOA_ACT_GELU: return z == -INFINITY ? -0.0f : 0.5f * z * (1.0f + erff(z * SQRT_HALF));
+    // (1 + tanh u) / 2 = sigmoid(2 u)
+    case BOA_ACT_GELU_TANH: return z == -INFINITY ? -0.0f : z * sigmoid<FINE>(2.0f * SQRT_2_PI * (z + CUBE * z * z * z));
+    default: return z;
+    }
+}
+
+template <bool FINE>
+__device__ inline float slope_of(float z, int32_t act)
+{
+    switch (act) {
+    case BOA_ACT_RELU: return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
+    case BOA_ACT_SILU: {
+        const float s = sigmoid<FINE>(z);
+        return fabsf(z) > 100.0f ? (z > 0.0f ? 1.0f : 0.0f) : s * (1.0f + z * (1.0f - s));
+    }
+    case BOA_ACT_GELU: return fabsf(z) > 20.0f ? (z > 0.0f ? 1.0f : 0.0f)
+                              : 0.5f * (1.0f + erff(z * SQRT_HALF)) + z * INV_SQRT_2PI * exp_of<FINE>(-0.5f * z * z);
+    case BOA_ACT_GELU_TANH: {
+        const float s = sigmoid<FINE>(2.0f * SQRT_2_PI * (z + CUBE * z * z * z));
+        return fabsf(z) > 20.0f ? (z > 0.0f ? 1.0f : 0.0f)
+               : s + z * s * (1.0f - s) * 2.0f * SQRT_2_PI * (1.0f + 3.0f * CUBE * z * z);
+    }
+    default: return 1.0f;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// epilogue
+
+struct Epilogue {
+    void *out;
+    int64_t ld;
+    const void *bias;
+    int32_t bias_f32;
+    const void *residual;
+    int64_t residual_ld;
+    void *pre;
+    int32_t act;
+    int32_t rows, cols;
+    const float *max_a, *max_b;   // of scaled operands: the largest magnitudes
+    float *partial;               // of splits: rows x pad8(cols) sums each, in place of all that
+    int64_t partial_ld, partial_split;
+};
+
+// Power of two that brings magnitudes of up to m below 2^15.
+__device__ inline int up(float m) { return 15 - __builtin_amdgcn_frexp_expf(m); }
+
+__device__ inline f16_t kept(float z)
+{
+    return (f16_t)(z != z ? z : fminf(fmaxf(z, -65504.0f), 65504.0f));
+}
+
+// N neighbouring values of a row, at column q (the row has them all)
+template <class TO, int N>
+__device__ inline void finish(const Epilogue &e, int64_t p, int32_t q, float (&v)[N])
+{
+    constexpr bool WIDE = sizeof(TO) == 4;
+    if (e.bias) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += e.bias_f32 ? ((const float *)e.bias)[q + i] : (float)((const TO *)e.bias)[q + i];
+    }
+    if (e.pre) {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) ((float *)e.pre)[p * e.cols + q + i] = v[i];
+        } else if constexpr (N == 8) {
+            Pack<8, f16_t> k;
+#pragma unroll
+            for (int i = 0; i < N; ++i) k.v[i] = kept(v[i]);
+            *(loose4 *)((f16_t *)e.pre + p * e.cols + q) = __builtin_bit_cast(words4, k);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) ((f16_t *)e.pre)[p * e.cols + q + i] = kept(v[i]);
+        }
+    }
+    if (e.act != BOA_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = act_of<WIDE>(v[i], e.act);
+    }
+    TO *out = (TO *)e.out + p * e.ld + q;
+    if (e.residual) {
+        const TO *r = (const TO *)e.residual + p * e.residual_ld + q;
+        float t[N];
+        if constexpr (N == 8) {
+            load_loose<8, TO>(t, r);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) t[i] = (float)r[i];
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += t[i];
+    }
+    if constexpr (N == 8 && WIDE) {
+        store_loose<4, TO>(out, *(float(*)[4])v);
+        store_loose<4, TO>(out + 4, *(float(*)[4])(v + 4));
+    } else if constexpr (N == 8) {
+        store_loose<8, TO>(out, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) out[i] = (TO)v[i];
+    }
+}
+
+// Eight sums from column q on, of which the row may have fewer.
+template <class TO>
+__device__ inline void finish_run(const Epilogue &e, int64_t p, int32_t q, const float *sums)
+{
+    const int s = e.max_a ? up(e.max_a[p]) : 0;
+    if (q + 8 <= e.cols) {
+        float v[8];
+        load_f32<4, float>(*(float(*)[4])v, sums);
+        load_f32<4, float>(*(float(*)[4])(v + 4), sums + 4);
+        if (e.max_a) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = ldexpf(v[i], -(s + up(e.max_b[q + i])));
+        }
+        finish<TO, 8>(e, p, q, v);
+    } else {
+#pragma unroll 1
+        for (int i = 0; q + i < e.cols; ++i) {
+            float v[1] = {sums[i]};
+            if (e.max_a) v[0] = ldexpf(v[0], -(s + up(e.max_b[q + i])));
+            finish<TO, 1>(e, p, q + i, v);
+        }
+    }
+}
+
+template <class S, bool ACROSS_A, bool ACROSS_B, class TO>
+__global__ __launch_bounds__(S::THREADS) void product_kernel(Product pr, Epilogue e)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const Place w = place_of(pr);
+    f32x16 acc[S::TB][S::TA];
+    clear<S>(acc);
+    tile_product<S, ACROSS_A, ACROSS_B>(pr, w, (typename S::T *)lds, acc);
+    if (e.partial) {
+        float *out = e.partial + w.split * e.partial_split;
+        each_run<S>(w, acc, lds, [&](int32_t p, int32_t q, const float *v) {
+            if (p >= e.rows || q >= e.cols) return;
+            float *to = out + p * e.partial_ld + q;
+            *(f32x4 *)to = *(const f32x4 *)v;
+            *(f32x4 *)(to + 4) = *(const f32x4 *)(v + 4);
+        });
+        return;
+    }
+    each_run<S>(w, acc, lds, [&](int32_t p, int32_t q, const float *v) {
+        if (p < e.rows && q < e.cols) finish_run<TO>(e, p, q, v);
+    });
+}
+
+// The sum of the splits' shares, in their order.
+template <class TO>
+__global__ __launch_bounds__(256) void product_join_kernel(Epilogue e, int32_t splits)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, runs = e.partial_ld / 8;
+    const int64_t p = i / runs;
+    const int32_t q = (int32_t)(i % runs) * 8;
+    if (p >= e.rows) return;
+    f32x4 v0 = {0.0f, 0.0f, 0.0f, 0.0f}, v1 = v0;
+    const float *from = e.partial + p * e.partial_ld + q;
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+        v0 += *(const f32x4 *)(from + s * e.partial_split);
+        v1 += *(const f32x4 *)(from + s * e.partial_split + 4);
+    }
+    __shared__ __attribute__((aligned(16))) float sums[256 * 8];
+    float *mine = sums + threadIdx.x * 8;
+    *(f32x4 *)mine = v0;
+    *(f32x4 *)(mine + 4) = v1;
+    finish_run<TO>(e, p, q, mine);
+}
+
+// ---------------------------------------------------------------------------
+// operands that cannot be read in place
+
+// rows x cols, `ld` apart, to rows of pad8(cols) with zeros at the end
+struct CopyArgs {
+    const void *src;
+    void *dst;
+    int64_t ld, part, rows;
+    int32_t cols, pad;
+    float *most;   // of parts: the largest magnitude per row or column
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void pad_kernel(CopyArgs a)
+{
+    const int64_t chunks = a.pad / 8, n = a.rows * chunks;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / chunks;
+        const int32_t c = (int32_t)(i % chunks) * 8;
+        const T *from = (const T *)a.src + r * a.ld + c;
+        words4 w;
+        if (c + 8 <= a.cols) {
+            w = *(const loose4 *)from;
+        } else {
+            Pack<8, T> t;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t.v[e] = c + e < a.cols ? from[e] : (T)0.0f;
+            w = __builtin_bit_cast(words4, t);
+        }
+        *(words4 *)((T *)a.dst + r * a.pad + c) = w;
+    }
+}
+
+__device__ inline float finite_abs(float v) { return fabsf(v) < INFINITY ? fabsf(v) : 0.0f; }
+
+__device__ inline void read8(float (&v)[8], const float *from, int32_t c, int32_t cols)
+{
+    if (c + 8 <= cols) {
+        load_loose<8, float>(v, from + c);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? from[c + e] : 0.0f;
+    }
+}
+
+// eight values as two parts; s: their exponents' shifts
+__device__ inline void write_parts(const float (&v)[8], const int (&s)[8], f16_t *to, int64_t part)
+{
+    f16x8 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float t = ldexpf(v[e], s[e]);
+        hi[e] = (f16_t)t;
+        lo[e] = (f16_t)(fabsf(t) < INFINITY ? t - (float)hi[e] : 0.0f);
+    }
+    *(f16x8 *)to = hi;
+    *(f16x8 *)(to + part) = lo;
+}
+
+// Parts scaled by row: a wave per row, which it reads twice (the second time from the cache).
+__global__ __launch_bounds__(256) void row_parts_kernel(CopyArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows; r += (int64_t)gridDim.x * 4) {
+        const float *from = (const float *)a.src + r * a.ld;
+        float m = 0.0f;
+        for (int32_t c = lane * 8; c < a.cols; c += 512) {
+            float v[8];
+            read8(v, from, c, a.cols);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = fmaxf(m, finite_abs(v[e]));
+        }
+        m = wave_max(m);
+        if (lane == 0) a.most[r] = m;
+        const int u = up(m), s[8] = {u, u, u, u, u, u, u, u};
+        for (int32_t c = lane * 8; c < a.pad; c += 512) {
+            float v[8];
+            read8(v, from, c, a.cols);
+            write_parts(v, s, (f16_t *)a.dst + r * a.pad + c, a.part);
+        }
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void zero_kernel(T *p, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = (T)0.0f;
+}
+
+// Largest magnitudes per column: the maximum of bit patterns, whose order does not matter.
+__global__ __launch_bounds__(256) void col_max_kernel(CopyArgs a)
+{
+    const int32_t c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= a.cols) return;
+    float m = 0.0f;
+#pragma unroll 8
+    for (int64_t r = blockIdx.y; r < a.rows; r += gridDim.y) m = fmaxf(m, finite_abs(((const float *)a.src)[r * a.ld + c]));
+    atomicMax((uint32_t *)a.most + c, __float_as_uint(m));
+}
+
+__global__ __launch_bounds__(256) void col_parts_kernel(CopyArgs a)
+{
+    const int64_t chunks = a.pad / 8, n = a.rows * chunks;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / chunks;
+        const int32_t c = (int32_t)(i % chunks) * 8;
+        float v[8];
+        int s[8];
+        read8(v, (const float *)a.src + r * a.ld, c, a.cols);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = c + e < a.cols ? up(a.most[c + e]) : 0;
+        write_parts(v, s, (f16_t *)a.dst + r * a.pad + c, a.part);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// gradient of z
+
+struct SlopeArgs {
+    const void *dy, *pre;
+    void *dz;          // rows of `pad` values, or null
+    float *partial;    // stripes x N sums over rows, or null
+    int64_t M, ld;
+    int32_t N, pad, act;
+};
+
+// dz = dy act'(z), and its sums over the rows of a stripe. A thread has VEC
+// columns of every 8th row of its block's.
+template <class T>
+__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
+{
+    typedef std::conditional_t<sizeof(T) == 4, float, f16_t> Z;
+    constexpr int VEC = 8;
+    __shared__ float sums[8][32 * VEC];
+    const int col = threadIdx.x & 31, part = threadIdx.x >> 5;
+    const int32_t c = (blockIdx.x * 32 + col) * VEC;
+    float s[VEC] = {};
+    if (c < a.N) {
+        const bool whole = c + VEC <= a.N;
+        for (int64_t r = (int64_t)blockIdx.y * 8 + part; r < a.M; r += (int64_t)gridDim.y * 8) {
+            const T *dy = (const T *)a.dy + r * a.ld + c;
+            const Z *z = (const Z *)a.pre + r * a.N + c;
+            float g[VEC], x[VEC];
+            if (whole) {
+                load_loose<VEC, T>(g, dy);
+                if (a.act) load_loose<VEC, Z>(x, z);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    g[e] = c + e < a.N ? (float)dy[e] : 0.0f;
+                    x[e] = a.act && c + e < a.N ? (float)z[e] : 0.0f;
+                }
+            }
+            if (a.act) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) g[e] *= slope_of<sizeof(T) == 4>(x[e], a.act);
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s[e] += g[e];
+            if (a.dz) {   // rows have room for whole runs
+                T *to = (T *)a.dz + r * a.pad + c;
+                if constexpr (sizeof(T) == 4) {
+                    store_f32<4, T>(to, *(float(*)[4])g);
+                    store_f32<4, T>(to + 4, *(float(*)[4])(g + 4));
+                } else {
+                    store_f32<VEC, T>(to, g);
+                }
+            }
+        }
+    }
+    if (!a.partial) return;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) sums[part][e * 32 + col] = s[e];
+    __syncthreads();
+    const int32_t mine = blockIdx.x * 32 * VEC + threadIdx.x;
+    if (mine < a.N) {
+        const int at = (threadIdx.x % VEC) * 32 + threadIdx.x / VEC;
+        float t = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t += sums[k][at];
+        a.partial[(int64_t)blockIdx.y * a.N + mine] = t;
+    }
+}
+
+// Adds the stripes' sums: 16 columns a block and 16 slices of the stripes.
+template <class P>
+__global__ __launch_bounds__(256) void bias_join_kernel(const float *partial, int32_t stripes, int32_t N, P *db)
+{
+    __shared__ float part[16][17];
+    const int col = threadIdx.x & 15, slice = threadIdx.x >> 4;
+    const int32_t c = blockIdx.x * 16 + col;
+    float s = 0.0f;
+    if (c < N)
+#pragma unroll 4
+        for (int i = slice; i < stripes; i += 16) s += partial[(int64_t)i * N + c];
+    part[slice][col] = s;
+    __syncthreads();
+    if (slice == 0 && c < N) {
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += part[i][col];
+        db[c] = (P)s;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// a few rows
+
+struct FewArgs {
+    const void *x, *w;
+    int64_t x_ld, w_ld;
+    int32_t M, N, K;
+    Epilogue e;
+};
+
+// 16 rows of weights a block; its 16 waves share k and their sums are added
+// through LDS in order. Fragments come straight from memory: every weight is
+// read once, every state by each block from the cache. Rows past the end are
+// read as the last one, and what they give is dropped.
+template <class T, int MT>
+__global__ __launch_bounds__(1024) void few_kernel(FewArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    typedef typename Vec<T>::v8 v8;
+    constexpr int WAVES = 16;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4;
+    const int32_t n0 = blockIdx.x * 16;
+    const T *w = (const T *)a.w + (int64_t)min(n0 + r, a.N - 1) * a.w_ld;
+    const T *x[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) x[j] = (const T *)a.x + (int64_t)min(j * 16 + r, a.M - 1) * a.x_ld;
+    const int32_t whole = a.K / 32, each = (whole + WAVES - 1) / WAVES;
+    const int32_t end = min(whole, (wave + 1) * each);
+    auto eight = [](const T *p) { return __builtin_bit_cast(v8, (words4) * (const loose4 *)p); };
+    f32x4 acc[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int AHEAD = MT == 1 ? 8 : MT == 2 ? 4 : 2;   // steps whose loads are on their way together
+    for (int32_t s = wave * each; s < end; s += AHEAD) {
+        v8 fw[AHEAD], fx[AHEAD][MT];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (s + u < end) {
+                const int32_t k = (s + u) * 32 + part * 8;
+                fw[u] = eight(w + k);
+#pragma unroll
+                for (int j = 0; j < MT; ++j) fx[u][j] = eight(x[j] + k);
+            }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (s + u < end) {
+#pragma unroll
+                for (int j = 0; j < MT; ++j) acc[j] = mfma16(fw[u], fx[u][j], acc[j]);
+            }
+    }
+    if (a.K % 32 && wave == WAVES - 1) {   // the last values of k, zeros past them
+        auto some = [&](const T *p) {
+            v8 f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int32_t k = whole * 32 + part * 8 + e;
+                f[e] = k < a.K ? p[k] : (T)0.0f;
+            }
+            return f;
+        };
+        const v8 fw = some(w);
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[j] = mfma16(fw, some(x[j]), acc[j]);
+    }
+    float *sums = (float *)lds;   // [wave][row of x][row of w]
+#pragma unroll
+    for (int j = 0; j < MT; ++j) *(f32x4 *)(sums + ((wave * MT + j) * 16 + r) * 16 + part * 4) = acc[j];
+    __syncthreads();
+    if (threadIdx.x < MT * 256) {
+        float v[1] = {0.0f};
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) v[0] += sums[k * MT * 256 + threadIdx.x];
+        const int32_t m = threadIdx.x >> 4, n = n0 + (threadIdx.x & 15);
+        if (m < a.M && n < a.N) finish<T, 1>(a.e, m, n, v);
+    }
+}
+
+// The same in float32: four rows of weights a block, whose 8 waves share k.
+template <int MB>
+__global__ __launch_bounds__(512) void few_f32_kernel(FewArgs a)
+{
+    constexpr int WAVES = 8, ROWS = 4;
+    __shared__ float sums[WAVES][MB * ROWS];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int32_t n0 = blockIdx.x * ROWS;
+    float acc[MB][ROWS] = {};
+    const float *w[ROWS], *x[MB];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) w[i] = (const float *)a.w + (int64_t)min(n0 + i, a.N - 1) * a.w_ld;
+#pragma unroll
+    for (int m = 0; m < MB; ++m) x[m] = (const float *)a.x + (int64_t)min(m, a.M - 1) * a.x_ld;
+    const int32_t whole = a.K / 4 * 4;
+    for (int32_t k = threadIdx.x * 4; k < whole; k += WAVES * 256) {
+        float fw[ROWS][4];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) load_loose<4, float>(fw[i], w[i] + k);
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+            float fx[4];
+            load_loose<4, float>(fx, x[m] + k);
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[m][i] = fmaf(fx[e], fw[i][e], acc[m][i]);
+        }
+    }
+    if (const int32_t k = whole + (int32_t)threadIdx.x; k < a.K) {
+#pragma unroll
+        for (int m = 0; m < MB; ++m)
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) acc[m][i] = fmaf(x[m][k], w[i][k], acc[m][i]);
+    }
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const float s = wave_sum(acc[m][i]);
+            if (lane == 0) sums[wave][m * ROWS + i] = s;
+        }
+    __syncthreads();
+    if (threadIdx.x < MB * ROWS) {
+        float v[1] = {0.0f};
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) v[0] += sums[k][threadIdx.x];
+        const int32_t m = threadIdx.x / ROWS, n = n0 + threadIdx.x % ROWS;
+        if (m < a.M && n < a.N) finish<float, 1>(a.e, m, n, v);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host
+
+// Work memory handed out piece by piece; without a base it only counts.
+struct Arena {
+    char *base = nullptr;
+    int64_t used = 0;
+    void *take(int64_t bytes)
+    {
+        void *p = base ? base + used : nullptr;
+        used += ceil_div(bytes, 256) * 256;
+        return p;
+    }
+};
+
+int32_t pad8(int64_t n) { return (int32_t)(ceil_div(n, 8) * 8); }
+
+uint32_t spread(int64_t items) { return (uint32_t)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, 256), 1 << 14)); }
+
+bool in_place(const void *p, int64_t ld, int64_t rows, int64_t cols)
+{
+    return aligned(p, 16) && cols % 8 == 0 && (rows <= 1 || (ld % 8 == 0 && ld < 1 << 21));
+}
+
+template <class T>
+using Large = Tile<T, 4, 2, 2, 4, 2>;
+template <class T>
+using Middle = Tile<T, 2, 2, 2, 2, 2>;
+template <class T>
+using Small = Tile<T, 2, 2, 1, 1, 3>;
+
+// How a product is cut into blocks.
+struct Cut {
+    int shape, splits;
+};
+
+// The cheapest of three tiles and some numbers of splits by a model of the
+// time: rounds of blocks over the GPU's 256 CUs, each as long as its stages
+// and a beginning and end; splits also write and read their sums.
+Cut choose(int64_t A, int64_t B, int64_t K, int terms)
+{
+    struct Cost {
+        int side, at_once;
+        double stage, alone, ends;   // us a stage in a full CU and in a CU of its own, us of beginning and end
+    };
+    static const Cost costs[3] = {{256, 1, 1.85, 1.85, 5.0}, {128, 2, 1.07, 0.70, 3.0}, {64, 3, 0.65, 0.35, 2.0}};
+    static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    const int64_t steps = ceil_div(K, 64);
+    Cut best{0, 1};
+    double least = 1e30;
+    for (int s = 0; s < 3; ++s)
+        for (int n : counts) {
+            if (n > 1 && (n > steps || (double)n * A * B * 4 > 256e6)) break;
+            const Cost &c = costs[s];
+            const int64_t each = ceil_div(steps, n), splits = ceil_div(steps, each);
+            const double blocks = (double)ceil_div(A, c.side) * ceil_div(B, c.side) * splits, room = 256.0 * c.at_once;
+            const double full = (double)(int64_t)(blocks / room), rest = blocks - full * room;
+            double t = full * (each * terms * c.stage + c.ends);
+            if (rest > 0) t += each * terms * std::max(c.alone, c.stage * std::min(1.0, (double)ceil_div((int64_t)rest, 256) / c.at_once)) + c.ends;
+            if (splits > 1) t += 4.0 + (double)splits * A * B * 8 / 4e6;
+            if (t < least) least = t, best = {s, (int)splits};
+        }
+    return best;
+}
+
+template <class S, bool ACROSS_A, bool ACROSS_B, class TO>
+void launch(Product pr, const Epilogue &e, hipStream_t st)
+{
+    pr.tiles_a = (int32_t)ceil_div(pr.a.own, S::BA);
+    pr.tiles_b = (int32_t)ceil_div(pr.b.own, S::BB);
+    const auto kernel = product_kernel<S, ACROSS_A, ACROSS_B, TO>;
+    if (S::LDS > 64 << 10)   // has to be asked for
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+    kernel<<<dim3((uint32_t)((int64_t)pr.tiles_a * pr.tiles_b * pr.splits)), S::THREADS, S::LDS, st>>>(pr, e);
+}
+
+// out = a b^T with its epilogue; T: the operands' type in the product, TO: the layer's.
+template <class T, class TO, bool ACROSS_A, bool ACROSS_B>
+void product(Operand a, Operand b, int32_t K, int terms, Epilogue e, Arena &mem, bool run, hipStream_t st)
+{
+    const Cut cut = choose(a.own, b.own, K, terms);
+    Product pr{};
+    pr.a = a, pr.b = b, pr.K = K, pr.terms = terms, pr.batches = 1, pr.splits = cut.splits;
+    pr.steps = (int32_t)ceil_div(ceil_div(K, 64), cut.splits);
+    e.rows = a.own, e.cols = b.own;
+    if (cut.splits > 1) {
+        e.partial_ld = pad8(b.own);
+        e.partial_split = e.partial_ld * a.own;
+        e.partial = (float *)mem.take(e.partial_split * cut.splits * 4);
+    }
+    if (!run) return;
+    if (cut.shape == 0) launch<Large<T>, ACROSS_A, ACROSS_B, TO>(pr, e, st);
+    else if (cut.shape == 1) launch<Middle<T>, ACROSS_A, ACROSS_B, TO>(pr, e, st);
+    else launch<Small<T>, ACROSS_A, ACROSS_B, TO>(pr, e, st);
+    if (cut.splits > 1)
+        product_join_kernel<TO><<<dim3((uint32_t)ceil_div(e.partial_ld / 8 * a.own, 256)), 256, 0, st>>>(e, cut.splits);
+}
+
+// rows x cols at `src` as an operand, in place or copied.
+template <class T>
+Operand operand(const void *src, int64_t ld, int64_t rows, int32_t cols, bool across, Arena &mem, bool run, hipStream_t st)
+{
+    Operand o{};
+    o.own = (int32_t)(across ? cols : rows);
+    if (in_place(src, ld, rows, cols)) {
+        o.p = src, o.ld = rows > 1 ? ld : pad8(cols);
+        return o;
+    }
+    CopyArgs c{};
+    c.src = src, c.ld = ld, c.rows = rows, c.cols = cols, c.pad = pad8(cols);
+    c.dst = mem.take(rows * c.pad * 2);
+    o.p = c.dst, o.ld = c.pad;
+    if (run) pad_kernel<T><<<spread(rows * (c.pad / 8)), 256, 0, st>>>(c);
+    return o;
+}
+
+// float32 rows x cols at `src` as two parts, scaled per row, or per column where
+// the operand lies across; *most gets the magnitudes that the scales come from.
+Operand parts(const void *src, int64_t ld, int64_t rows, int32_t cols, bool across, bool by_column, const float **most, Arena &mem,
+              bool run, hipStream_t st)
+{
+    CopyArgs c{};
+    c.src = src, c.ld = ld, c.rows = rows, c.cols = cols, c.pad = pad8(cols), c.part = rows * c.pad;
+    c.dst = mem.take(2 * c.part * 2);
+    c.most = (float *)mem.take((by_column ? (int64_t)cols : rows) * 4);
+    *most = c.most;
+    Operand o{};
+    o.own = (int32_t)(across ? cols : rows), o.p = c.dst, o.ld = c.pad, o.part = c.part;
+    if (!run) return o;
+    if (!by_column) {
+        row_parts_kernel<<<dim3((uint32_t)std::min<int64_t>(ceil_div(rows, 4), 1 << 14)), 256, 0, st>>>(c);
+        return o;
+    }
+    zero_kernel<float><<<spread(cols), 256, 0, st>>>(c.most, cols);
+    const int64_t across_blocks = ceil_div(cols, 256), down = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 32), 2048 / across_blocks));
+    col_max_kernel<<<dim3((uint32_t)across_blocks, (uint32_t)down), 256, 0, st>>>(c);
+    col_parts_kernel<<<spread(rows * (c.pad / 8)), 256, 0, st>>>(c);
+    return o;
+}
+
+template <class F>
+int with_type(int32_t dtype, F f)
+{
+    if (dtype == BOA_T_F32) return f(0.0f);
+    return dtype == BOA_T_BF16 ? f(bf16_t{}) : f(f16_t{});
+}
+
+int few_rows(int32_t dtype) { return dtype == BOA_T_F32 ? BOA_LINEAR_FEW_F32 : BOA_LINEAR_FEW; }
+
+int check(const char *what, const boa_dense *d, bool grad)
+{
+    const char *why = nullptr;
+    if (!d) return set_error(BOA_EINVAL, "linear: NULL arguments");
+    const int32_t last = BOA_ACT_GELU_TANH;
+    if (!dtype_known(d->dtype)) why = "unknown dtype";
+    else if (d->activation < 0 || d->activation > last) why = "unknown activation";
+    else if (d->M < 0 || d->M >= (int64_t)1 << 31) why = "M out of range [0, 2^31)";
+    else if (d->N < 1 || d->N > BOA_MAX_LINEAR) why = "N out of range [1, 2^17]";
+    else if (d->K < 1 || d->K > BOA_MAX_LINEAR) why = "K out of range [1, 2^17]";
+    else if (d->M > 1 && d->x_stride < d->K) why = "x's row stride smaller than K";
+    else if (d->N > 1 && d->w_stride < d->K) why = "w's row stride smaller than K";
+    else if (d->param_dtype != d->dtype && d->param_dtype != BOA_T_F32) why = "the bias must have the layer's type or be float32";
+    else if (d->M && !d->x) why = "NULL x";
+    else if (!d->w) why = "NULL w";
+    else if (!grad && d->residual && d->M > 1 && d->residual_stride < d->N) why = "the residual's row stride smaller than N";
+    else if (!grad && d->M && !d->y) why = "NULL y";
+    else if (grad && d->M && !d->dy) why = "NULL dy";
+    else if (grad && d->M > 1 && d->dy_stride < d->N) why = "dy's row stride smaller than N";
+    else if (grad && d->M && d->activation != BOA_ACT_NONE && !d->pre) why = "NULL pre";
+    if (!why) return BOA_OK;
+    char msg[160];
+    __builtin_snprintf(msg, sizeof(msg), "%s: %s", what, why);
+    return set_error(BOA_EINVAL, msg);
+}
+
+template <class TO>
+void forward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
+{
+    constexpr bool WIDE = sizeof(TO) == 4;
+    typedef std::conditional_t<WIDE, f16_t, TO> T;
+    const int32_t M = (int32_t)d.M;
+    Epilogue e{};
+    e.out = d.y, e.ld = d.N, e.bias = d.bias, e.bias_f32 = d.param_dtype == BOA_T_F32;
+    e.residual = d.residual, e.residual_ld = d.residual_stride, e.pre = d.pre, e.act = d.activation;
+    e.rows = M, e.cols = d.N;
+    if (M <= few_rows(d.dtype)) {
+        if (!run) return;
+        FewArgs a{d.x, d.w, d.x_stride, d.w_stride, M, d.N, d.K, e};
+        if constexpr (WIDE) {
+            const dim3 grid((uint32_t)ceil_div(d.N, 4));
+            if (M <= 1) few_f32_kernel<1><<<grid, 512, 0, st>>>(a);
+            else if (M <= 2) few_f32_kernel<2><<<grid, 512, 0, st>>>(a);
+            else if (M <= 4) few_f32_kernel<4><<<grid, 512, 0, st>>>(a);
+            else if (M <= 8) few_f32_kernel<8><<<grid, 512, 0, st>>>(a);
+            else few_f32_kernel<16><<<grid, 512, 0, st>>>(a);
+        } else {
+            const dim3 grid((uint32_t)ceil_div(d.N, 16));
+            if (M <= 16) few_kernel<T, 1><<<grid, 1024, 16 << 10, st>>>(a);
+            else if (M <= 32) few_kernel<T, 2><<<grid, 1024, 32 << 10, st>>>(a);
+            else few_kernel<T, 4><<<grid, 1024, 64 << 10, st>>>(a);
+        }
+        return;
+    }
+    if constexpr (WIDE) {
+        const Operand x = parts(d.x, d.x_stride, M, d.K, false, false, &e.max_a, mem, run, st);
+        const Operand w = parts(d.w, d.w_stride, d.N, d.K, false, false, &e.max_b, mem, run, st);
+        product<T, TO, false, false>(x, w, d.K, 3, e, mem, run, st);
+    } else {
+        const Operand x = operand<T>(d.x, d.x_stride, M, d.K, false, mem, run, st);
+        const Operand w = operand<T>(d.w, d.w_stride, d.N, d.K, false, mem, run, st);
+        product<T, TO, false, false>(x, w, d.K, 1, e, mem, run, st);
+    }
+}
+
+template <class TO>
+void backward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
+{
+    constexpr bool WIDE = sizeof(TO) == 4;
+    typedef std::conditional_t<WIDE, f16_t, TO> T;
+    const int32_t M = (int32_t)d.M;
+    const bool act = d.activation != BOA_ACT_NONE;
+    // dz: dy itself where the activation has none and it can be read as it is
+    SlopeArgs s{};
+    s.dy = d.dy, s.ld = d.dy_stride, s.pre = d.pre, s.M = M, s.N = d.N, s.pad = pad8(d.N), s.act = d.activation;
+    const void *dz = d.dy;
+    int64_t dz_ld = d.dy_stride;
+    if ((d.dx || d.dw) && (act || (!WIDE && !in_place(d.dy, d.dy_stride, M, d.N)))) {
+        s.dz = mem.take((int64_t)M * s.pad * sizeof(TO));
+        dz = s.dz, dz_ld = s.pad;
+    }
+    const int64_t strips = ceil_div(d.N, 256);
+    const int32_t stripes = (int32_t)std::max<int64_t>(1, std::min<int64_t>(ceil_div(M, 64), std::max<int64_t>(1, 2048 / strips)));
+    if (d.dbias) s.partial = (float *)mem.take((int64_t)stripes * d.N * 4);
+    if (run && (s.dz || d.dbias)) slope_kernel<TO><<<dim3((uint32_t)strips, (uint32_t)stripes), 256, 0, st>>>(s);
+    if (run && d.dbias) {
+        const uint32_t grid = (uint32_t)ceil_div(d.N, 16);
+        if (d.param_dtype == BOA_T_F32) bias_join_kernel<float><<<grid, 256, 0, st>>>(s.partial, stripes, d.N, (float *)d.dbias);
+        else bias_join_kernel<TO><<<grid, 256, 0, st>>>(s.partial, stripes, d.N, (TO *)d.dbias);
+    }
+    Epilogue e{};
+    e.act = BOA_ACT_NONE;
+    const int64_t kept = mem.used;   // the two products' memory takes turns
+    int64_t most = kept;
+    if (d.dx && M) {
+        e.out = d.dx, e.ld = d.K;
+        if constexpr (WIDE) {
+            const Operand a = parts(dz, dz_ld, M, d.N, false, false, &e.max_a, mem, run, st);
+            const Operand b = parts(d.w, d.w_stride, d.N, d.K, true, true, &e.max_b, mem, run, st);
+            product<T, TO, false, true>(a, b, d.N, 3, e, mem, run, st);
+        } else {
+            Operand a{};
+            a.p = dz, a.ld = M > 1 || s.dz ? dz_ld : s.pad, a.own = M;
+            const Operand b = operand<T>(d.w, d.w_stride, d.N, d.K, true, mem, run, st);
+            product<T, TO, false, true>(a, b, d.N, 1, e, mem, run, st);
+        }
+        most = std::max(most, mem.used);
+        mem.used = kept;
+    }
+    if (d.dw) {
+        e.out = d.dw, e.ld = d.K;
+        if (M == 0) {
+            const int64_t n = (int64_t)d.N * d.K;
+            if (run) zero_kernel<TO><<<spread(n), 256, 0, st>>>((TO *)d.dw, n);
+        } else if constexpr (WIDE) {
+            const Operand a = parts(dz, dz_ld, M, d.N, true, true, &e.max_a, mem, run, st);
+            const Operand b = parts(d.x, d.x_stride, M, d.K, true, true, &e.max_b, mem, run, st);
+            product<T, TO, true, true>(a, b, M, 3, e, mem, run, st);
+        } else {
+            Operand a{};
+            a.p = dz, a.ld = M > 1 || s.dz ? dz_ld : s.pad, a.own = d.N;
+            const Operand b = operand<T>(d.x, d.x_stride, M, d.K, true, mem, run, st);
+            product<T, TO, true, true>(a, b, M, 1, e, mem, run, st);
+        }
+        most = std::max(most, mem.used);
+    }
+    mem.used = most;
+}
+
+int64_t measure(const boa_dense &d, bool grad)
+{
+    Arena mem;
+    with_type(d.dtype, [&](auto t) {
+        using TO = decltype(t);
+        if (grad) backward<TO>(d, mem, false, nullptr);
+        else forward<TO>(d, mem, false, nullptr);
+        return 0;
+    });
+    return mem.used;
+}
+
+int call(const char *what, const boa_dense *d, bool grad, void *workspace, int64_t bytes, void *stream)
+{
+    if (int rc = check(what, d, grad)) return rc;
+    if (!grad && d->M == 0) return BOA_OK;
+    if (grad && !d->dx && !d->dw && !d->dbias) return BOA_OK;
+    const int64_t need = measure(*d, grad);
+    if (need && (!workspace || !aligned(workspace, 16) || bytes < need)) {
+        char msg[96];
+        __builtin_snprintf(msg, sizeof(msg), "%s: workspace missing, unaligned or too small", what);
+        return set_error(BOA_EINVAL, msg);
+    }
+    Arena mem;
+    mem.base = (char *)workspace;
+    return with_type(d->dtype, [&](auto t) {
+        using TO = decltype(t);
+        if (grad) backward<TO>(*d, mem, true, (hipStream_t)stream);
+        else forward<TO>(*d, mem, true, (hipStream_t)stream);
+        return launch_status(what);
+    });
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t boa_linear_workspace(const boa_dense *d, int32_t grad)
+{
+    if (int rc = check("linear", d, grad != 0)) return rc;
+    return measure(*d, grad != 0);
+}
+
+int boa_linear(const boa_dense *d, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    return call("linear", d, false, workspace, workspace_bytes, stream);
+}
+
+int boa_linear_grad(const boa_dense *d, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    return call("linear_backward", d, true, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

@@ -1,5 +1,5 @@
-"""Operators of a query tower on device tensors: layer norm, softmax cross
-entropy over the points of an index, products with 4-bit rows.
+"""Operators of a query tower on device tensors: layer norm, linear layers,
+softmax cross entropy over the points of an index, products with 4-bit rows.
 
 Argument marshalling for libboa.so (include/boa.h); every computation runs in
 the library's HIP kernels. Tensors live on one GPU; calls are queued on its
@@ -30,6 +30,14 @@ class Xent(C.Structure):
                 ("dpoints", C.c_void_p), ("dbias", C.c_void_p)]
 
 
+class Dense(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("activation", C.c_int32), ("M", C.c_int64), ("N", C.c_int32), ("K", C.c_int32),
+                ("x", C.c_void_p), ("x_stride", C.c_int64), ("w", C.c_void_p), ("w_stride", C.c_int64),
+                ("bias", C.c_void_p), ("param_dtype", C.c_int32), ("residual", C.c_void_p), ("residual_stride", C.c_int64),
+                ("y", C.c_void_p), ("pre", C.c_void_p), ("dy", C.c_void_p), ("dy_stride", C.c_int64), ("dx", C.c_void_p),
+                ("dw", C.c_void_p), ("dbias", C.c_void_p)]
+
+
 _ready = None
 
 
@@ -47,6 +55,10 @@ def _lib():
         for f in (L.boa_softmax_xent, L.boa_softmax_xent_grad):
             f.argtypes = [C.POINTER(Xent), P, i64, P]
         L.boa_matvec_fourbit.argtypes = [P, i64, i64, i32, P, i64, i32, i64, P, P, i64, i32, i32, P, i64, P]
+        L.boa_linear_workspace.argtypes = [C.POINTER(Dense), i32]
+        L.boa_linear_workspace.restype = i64
+        for f in (L.boa_linear, L.boa_linear_grad):
+            f.argtypes = [C.POINTER(Dense), P, i64, P]
         _ready = L
     return _ready
 
@@ -377,3 +389,129 @@ def matvec_4bit(x, codes, scales, offsets=None, group=None, stream=None):
     _check(_lib().boa_matvec_fourbit(m.data_ptr(), M, _stride(m), dt, c.data_ptr(), N, K, _stride(c), s.data_ptr(), _ptr(o),
                                      _stride(s), sd, group, y.data_ptr(), N, _current_stream(x.get_device())))
     return y if x.dim() == 2 else y[0]
+
+
+# ---------------------------------------------------------------------------
+# linear layers
+
+_ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+LINEAR_FEW, LINEAR_FEW_F32 = 64, 16   # rows up to which a forward pass takes no work memory
+
+
+def _activation(name, activation):
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"{name}: activation must be one of {', '.join(_ACTIVATIONS)}")
+    return _ACTIVATIONS[activation]
+
+
+def _linear_shapes(name, x, weight, bias):
+    if weight.dim() != 2 or weight.dtype != x.dtype or x.dim() < 1 or x.shape[-1] != weight.shape[1]:
+        raise ValueError(f"{name}: x must be (..., K) and weight (N, K), of one type")
+    if weight.shape[0] < 1 or weight.shape[1] < 1:
+        raise ValueError(f"{name}: weight needs at least one row and one column")
+    if bias is not None and (bias.shape != weight.shape[:1] or bias.dtype not in (x.dtype, torch.float32)):
+        raise ValueError(f"{name}: bias must be ({weight.shape[0]},) of x's type or float32")
+
+
+def linear_forward(x, weight, bias=None, residual=None, activation="none", keep=False, stream=None):
+    """(y, pre) of a linear layer: y = activation(x @ weight.T + bias) + residual.
+
+    x: (..., K), float32, bfloat16 or float16; weight: (N, K) of x's type; bias:
+    (N,) of x's type or float32; residual: like y, (..., N). activation: "none",
+    "relu", "silu", "gelu" (the error function's) or "gelu_tanh". pre is what
+    linear_backward takes where there is an activation: x @ weight.T + bias in
+    float16, clamped to its range (float32 for float32 layers); None without
+    `keep` or without an activation."""
+    _device("linear", x, weight, bias, residual)
+    dt = _dtype("linear", x)
+    act = _activation("linear", activation)
+    _linear_shapes("linear", x, weight, bias)
+    N, K = weight.shape
+    shape = (*x.shape[:-1], N)
+    if residual is not None and (residual.shape != shape or residual.dtype != x.dtype):
+        raise ValueError(f"linear: residual must be {shape} of x's type")
+    other = _at(x, stream, x, weight, bias, residual)
+    if other is not None:
+        with other:
+            return linear_forward(x, weight, bias, residual, activation, keep)
+    m, w, b = _rows(x), _rows(weight), _dense(bias)
+    r = None if residual is None else _rows(residual)
+    M = m.shape[0]
+    y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    pre = torch.empty(shape, dtype=torch.float32 if dt == T_F32 else torch.float16, device=x.device) if keep and act else None
+    a = Dense(dt, act, M, N, K, m.data_ptr(), _stride(m), w.data_ptr(), _stride(w), _ptr(b), dt if b is None else _DTYPES[b.dtype],
+              _ptr(r), 0 if r is None else _stride(r), y.data_ptr(), _ptr(pre))
+    ws, n = _linear_workspace(x, a, M > (LINEAR_FEW_F32 if dt == T_F32 else LINEAR_FEW), 0)
+    _check(_lib().boa_linear(C.byref(a), _ptr(ws), n, _current_stream(x.get_device())))
+    return y, pre
+
+
+def _linear_workspace(x, a, needed, grad):
+    n = _lib().boa_linear_workspace(C.byref(a), grad) if needed else 0
+    if n < 0:
+        _check(n)
+    return (_workspace(x, n), n) if n else (None, 0)
+
+
+def linear_backward(dy, x, weight, pre=None, activation="none", need=(True, True, True), bias_dtype=None, stream=None):
+    """(dx, dweight, dbias) of linear_forward; the residual's gradient is dy.
+    pre: the forward pass's, where there is an activation. need: which of the
+    three to compute. dbias has bias_dtype: x's type (the default) or float32.
+    In bfloat16 and float16 the gradient before the activation is rounded to
+    x's type as an operand of the products, not in dbias; results are rounded
+    once."""
+    _device("linear_backward", dy, x, weight, pre)
+    dt = _dtype("linear_backward", x)
+    act = _activation("linear_backward", activation)
+    _linear_shapes("linear_backward", x, weight, None)
+    N, K = weight.shape
+    if tuple(dy.shape) != (*x.shape[:-1], N) or dy.dtype != x.dtype:
+        raise ValueError("linear_backward: dy must be (..., N) of x's type")
+    if act:
+        want = torch.float32 if dt == T_F32 else torch.float16
+        if pre is None or pre.shape != dy.shape or pre.dtype != want or not pre.is_contiguous():
+            raise ValueError("linear_backward: pre must be the tensor that linear_forward gave with keep")
+    ptype = x.dtype if bias_dtype is None else bias_dtype
+    if ptype not in (x.dtype, torch.float32):
+        raise ValueError("linear_backward: bias_dtype must be x's or float32")
+    other = _at(x, stream, dy, x, weight, pre)
+    if other is not None:
+        with other:
+            return linear_backward(dy, x, weight, pre, activation, need, bias_dtype)
+    m, w, g = _rows(x), _rows(weight), _rows(dy)
+    dev = x.device
+    dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if need[0] else None
+    dw = torch.empty((N, K), dtype=x.dtype, device=dev) if need[1] else None
+    db = torch.empty((N,), dtype=ptype, device=dev) if need[2] else None
+    a = Dense(dt, act, m.shape[0], N, K, m.data_ptr(), _stride(m), w.data_ptr(), _stride(w), None, _DTYPES[ptype], None, 0, None,
+              _ptr(pre) if act else None, g.data_ptr(), _stride(g), _ptr(dx), _ptr(dw), _ptr(db))
+    ws, n = _linear_workspace(x, a, True, 1)
+    _check(_lib().boa_linear_grad(C.byref(a), _ptr(ws), n, _current_stream(dev.index)))
+    return dx, dw, db
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, activation):
+        need = ctx.needs_input_grad
+        y, pre = linear_forward(x, weight, bias, residual, activation, keep=need[0] or need[1] or need[2])
+        ctx.save_for_backward(x, weight, pre)
+        ctx.activation, ctx.bias_dtype = activation, None if bias is None else bias.dtype
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, weight, pre = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx = dw = db = None
+        if any(need[:3]):
+            dx, dw, db = linear_backward(dy, x, weight, pre, ctx.activation, need[:3], ctx.bias_dtype)
+        return dx, dw, db, dy if need[3] else None, None
+
+
+def linear(x, weight, bias=None, residual=None, activation="none"):
+    """linear_forward's y, for autograd."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias, residual)):
+        return _Linear.apply(x, weight, bias, residual, activation)
+    return linear_forward(x, weight, bias, residual, activation)[0]
