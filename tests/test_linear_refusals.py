@@ -59,11 +59,11 @@ def test_workspace():
     size = lambda grad, **over: L.boa_linear_workspace(C.byref(_dense(**over)), grad)  # noqa: E731
     assert size(0, M=64) == 0 and size(0, M=16, dtype=0, param_dtype=0) == 0
     # rows read in place take none, others a copy each; float32 rows two parts of 16 bits and the largest magnitudes
-    assert size(0, M=8192, N=8192, K=8192, x_stride=8192, w_stride=8192) == 0
+    assert size(0, M=8192, N=8192, K=8192, x_stride=8192, w_stride=8192, residual=None) == 0
     copy = 8192 * 8192 * 2
-    assert size(0, M=8192, N=8192, K=8191, x_stride=8192, w_stride=8192) == 2 * copy
-    assert size(0, M=8192, N=8192, K=8192, x_stride=8192, w_stride=8192, x=P + 2) == copy
-    assert size(0, M=8192, N=8192, K=8192, x_stride=8192, w_stride=8192, dtype=0, param_dtype=0) == 2 * (2 * copy + 8192 * 4)
+    assert size(0, M=8192, N=8192, K=8191, x_stride=8192, w_stride=8192, residual=None) == 2 * copy
+    assert size(0, M=8192, N=8192, K=8192, x_stride=8192, w_stride=8192, residual=None, x=P + 2) == copy
+    assert size(0, M=8192, N=8192, K=8192, x_stride=8192, w_stride=8192, residual=None, dtype=0, param_dtype=0) == 2 * (2 * copy + 8192 * 4)
     assert _call(0, M=100, dtype=0, param_dtype=0, n=16) == EINVAL and "workspace" in _err()
     assert L.boa_linear_workspace(None, 0) == EINVAL and L.boa_linear(None, P, 0, None) == EINVAL
 
