@@ -465,6 +465,58 @@ int boa_linear(const boa_dense *d, void *workspace, int64_t workspace_bytes, voi
 /* Its gradients. */
 int boa_linear_grad(const boa_dense *d, void *workspace, int64_t workspace_bytes, void *stream);
 
+enum { BOA_NORM_LAYER = 0, BOA_NORM_RMS = 1 };
+/*
+ * What stands between two blocks of a residual tower, on rows of d values: the
+ * norm after a block (post), its gate, the residual sum, and the norm before the
+ * next block (pre).
+ *   u = post ? norm(f) * post_weight + post_bias : f
+ *   h = scale * x + gate * u
+ *   y = norm(h) * weight + bias
+ * norm(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps), or without the
+ * means (BOA_NORM_RMS). y is formed from h before h is rounded. Any of gate and
+ * the parameters may be NULL (ones, zeros).
+ */
+typedef struct {
+    int32_t dtype;          /* of x, f, h, y, their gradients, and a gate per value */
+    int32_t param_dtype;    /* of the parameters, their gradients, and a shared gate: dtype or BOA_T_F32 */
+    int64_t rows;           /* 0 .. 2^31 - 1 */
+    int32_t d;              /* 1 .. BOA_MAX_NORM_D */
+    int32_t norm;           /* BOA_NORM_* */
+    int32_t post, pre;      /* whether there is the first norm, and the second (without it no y) */
+    int32_t gate_rows;      /* 0: gate holds d values for all rows; 1: rows x d */
+    float scale, eps;
+    const void *x;          /* rows x d: the residual stream */
+    int64_t x_stride;
+    const void *f;          /* rows x d: the block's output */
+    int64_t f_stride;
+    const void *gate;
+    int64_t gate_stride;    /* of a gate per value */
+    const void *post_weight, *post_bias, *weight, *bias;   /* d each */
+    void *h, *y;            /* rows x d, dense */
+    float *stats;           /* 4 x rows, for the backward pass, or NULL: mean and 1 / deviation of f's
+                               rows (where post), then of h's (where pre) */
+    /* gradients (boa_block_norm_backward only, which reads h again from x and f;
+       y and h are not read, eps neither) */
+    const void *dh;         /* rows x d, or NULL (zeros) */
+    int64_t dh_stride;
+    const void *dy;         /* rows x d, or NULL (zeros) */
+    int64_t dy_stride;
+    void *dx, *df;          /* rows x d, dense, or NULL */
+    void *dgate;            /* like gate (dense), or NULL */
+    void *dpost_weight, *dpost_bias, *dweight, *dbias;   /* d each, or NULL; zeros without rows */
+    void *workspace;        /* where sums over rows are wanted (the last five, but for a gate per value) */
+    int64_t workspace_bytes;
+} boa_block;
+
+/* Errors of both: BOA_EINVAL, BOA_EHIP. */
+int boa_block_norm(const boa_block *b, void *stream);
+
+/* Work memory of boa_block_norm_backward in bytes. */
+int64_t boa_block_norm_backward_workspace(int64_t rows, int32_t d);
+
+int boa_block_norm_backward(const boa_block *b, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,13 +16,13 @@
 // no atomics, so results do not depend on the schedule.
 #include <algorithm>
 
-#include "boa_ops.h"
+#include "boa_rows.h"
 
 using namespace boa;
 
 namespace {
 
-constexpr int THREADS = 256;
+constexpr int THREADS = ROW_THREADS;
 constexpr int64_t MAX_BLOCKS = 1024;   // of the backward pass: 4 per CU, each with one partial row of dw and db
 
 struct NormArgs {
@@ -46,65 +46,6 @@ NormArgs rows_from(NormArgs a, int64_t row)
     if (a.rstd) a.rstd += row;
     a.rows = std::min(LAUNCH_ROWS, a.rows - row);
     return a;
-}
-
-// A thread's columns of load i of a row: [c, c + VEC), moved back to end with
-// the row where they would pass its end; the first `skip` of them are then
-// another thread's too, or all (skip >= VEC). Every load is whole and within the
-// row, with no branch around it. WHOLE: rows of whole loads, where skip is 0
-// or at least VEC.
-template <int VEC, int TPR>
-struct Cols {
-    int c, skip;
-    __device__ Cols(int i, int lane, int32_t d)
-    {
-        const int c0 = (i * TPR + lane) * VEC;
-        c = min(c0, d - VEC);
-        skip = c0 - c;
-    }
-    __device__ bool any() const { return skip < VEC; }
-    template <bool WHOLE>
-    __device__ bool mine(int j) const { return WHOLE ? skip == 0 : j >= skip; }
-};
-
-// Sum of a value over the TPR threads of a row (a wave, or the block).
-template <int TPR>
-__device__ inline float row_sum(float v, float *red)
-{
-    v = wave_sum(v);
-    if constexpr (TPR > 64) {
-        const int wave = threadIdx.x >> 6;
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) red[wave] = v;
-        __syncthreads();
-        v = 0.0f;
-#pragma unroll
-        for (int i = 0; i < TPR / 64; ++i) v += red[i];
-    }
-    return v;
-}
-
-// Two sums at once.
-template <int TPR>
-__device__ inline void row_sum2(float &a, float &b, float *red)
-{
-    a = wave_sum(a);
-    b = wave_sum(b);
-    if constexpr (TPR > 64) {
-        const int wave = threadIdx.x >> 6;
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) {
-            red[wave] = a;
-            red[4 + wave] = b;
-        }
-        __syncthreads();
-        a = b = 0.0f;
-#pragma unroll
-        for (int i = 0; i < TPR / 64; ++i) {
-            a += red[i];
-            b += red[4 + i];
-        }
-    }
 }
 
 template <class T, class P, int NV, int TPR, bool WHOLE>
@@ -366,24 +307,9 @@ __global__ __launch_bounds__(JOIN_COLS * JOIN_SLICES) void norm_join_kernel(cons
     }
 }
 
-// Calls f(T{}, P{}) for an element type and a parameter type: the parameters
-// have the rows' type or are float32.
-template <class F>
-int with_types(int32_t dtype, int32_t param, F f)
-{
-    if (dtype == BOA_T_F32) return f(0.0f, 0.0f);
-    if (dtype == BOA_T_BF16) return param == BOA_T_F32 ? f(bf16_t{}, 0.0f) : f(bf16_t{}, bf16_t{});
-    return param == BOA_T_F32 ? f(f16_t{}, 0.0f) : f(f16_t{}, f16_t{});
-}
-
 // The registers a row takes: f(NV, TPR, WHOLE) as compile-time constants. A
 // wave per row up to 4 loads a lane, then a block per row; false where a row
 // does not fit, or is shorter than a load.
-template <int V>
-struct Int {
-    static constexpr int value = V;
-};
-
 template <int VEC, class F>
 bool with_shape(int32_t d, F f)
 {

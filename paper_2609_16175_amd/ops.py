@@ -1,5 +1,6 @@
-"""Operators of a query tower on device tensors: layer norm, linear layers,
-softmax cross entropy over the points of an index, products with 4-bit rows.
+"""Operators of a query tower on device tensors: layer norm, linear layers, the
+norms around a residual block, softmax cross entropy over the points of an
+index, products with 4-bit rows.
 
 Argument marshalling for libboa.so (include/boa.h); every computation runs in
 the library's HIP kernels. Tensors live on one GPU; calls are queued on its
@@ -38,6 +39,17 @@ class Dense(C.Structure):
                 ("dw", C.c_void_p), ("dbias", C.c_void_p)]
 
 
+class Block(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("param_dtype", C.c_int32), ("rows", C.c_int64), ("d", C.c_int32), ("norm", C.c_int32),
+                ("post", C.c_int32), ("pre", C.c_int32), ("gate_rows", C.c_int32), ("scale", C.c_float), ("eps", C.c_float),
+                ("x", C.c_void_p), ("x_stride", C.c_int64), ("f", C.c_void_p), ("f_stride", C.c_int64), ("gate", C.c_void_p),
+                ("gate_stride", C.c_int64), ("post_weight", C.c_void_p), ("post_bias", C.c_void_p), ("weight", C.c_void_p),
+                ("bias", C.c_void_p), ("h", C.c_void_p), ("y", C.c_void_p), ("stats", C.c_void_p), ("dh", C.c_void_p),
+                ("dh_stride", C.c_int64), ("dy", C.c_void_p), ("dy_stride", C.c_int64), ("dx", C.c_void_p), ("df", C.c_void_p),
+                ("dgate", C.c_void_p), ("dpost_weight", C.c_void_p), ("dpost_bias", C.c_void_p), ("dweight", C.c_void_p),
+                ("dbias", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
 _ready = None
 
 
@@ -59,6 +71,10 @@ def _lib():
         L.boa_linear_workspace.restype = i64
         for f in (L.boa_linear, L.boa_linear_grad):
             f.argtypes = [C.POINTER(Dense), P, i64, P]
+        for f in (L.boa_block_norm, L.boa_block_norm_backward):
+            f.argtypes = [C.POINTER(Block), P]
+        L.boa_block_norm_backward_workspace.argtypes = [i64, i32]
+        L.boa_block_norm_backward_workspace.restype = i64
         _ready = L
     return _ready
 
@@ -515,3 +531,153 @@ def linear(x, weight, bias=None, residual=None, activation="none"):
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias, residual)):
         return _Linear.apply(x, weight, bias, residual, activation)
     return linear_forward(x, weight, bias, residual, activation)[0]
+
+
+# ---------------------------------------------------------------------------
+# the norms around a residual block
+
+_NORMS = {"layer": 0, "rms": 1}
+
+
+@dataclass
+class BlockNormGrads:
+    dx: "object"
+    df: "object"
+    dgate: "object" = None          # like gate
+    dpost_weight: "object" = None   # like the parameters, where there are some
+    dpost_bias: "object" = None
+    dweight: "object" = None
+    dbias: "object" = None
+
+
+def _block(name, x, f, gate, post, pre, post_weight, post_bias, weight, bias, norm, scale, eps):
+    """The arguments that both passes share, and the parameters' type."""
+    dt = _dtype(name, x)
+    d = x.shape[-1] if x.dim() else 0
+    if d < 1:
+        raise ValueError(f"{name}: x needs a last dimension of at least 1")
+    if f.shape != x.shape or f.dtype != x.dtype:
+        raise ValueError(f"{name}: f must have x's shape and type")
+    if norm not in _NORMS:
+        raise ValueError(f"{name}: norm must be one of {', '.join(_NORMS)}")
+    if not post and (post_weight is not None or post_bias is not None):
+        raise ValueError(f"{name}: post_weight and post_bias belong to the norm after the block: pass post=True")
+    if not pre and (weight is not None or bias is not None):
+        raise ValueError(f"{name}: weight and bias belong to the norm before the next block: pass pre=True")
+    gate_rows = gate is not None and x.dim() > 1 and gate.shape == x.shape
+    if gate_rows and gate.dtype != x.dtype:
+        raise ValueError(f"{name}: a gate of x's shape must have its type")
+    ptype = None
+    for p in (post_weight, post_bias, weight, bias, None if gate_rows else gate):
+        if p is None:
+            continue
+        if p.shape != x.shape[-1:] or p.dtype not in (x.dtype, torch.float32):
+            raise ValueError(f"{name}: parameters and a shared gate must be ({d},) of x's type or float32")
+        if ptype not in (None, p.dtype):
+            raise ValueError(f"{name}: parameters and a shared gate must have one type")
+        ptype = p.dtype
+    ptype = x.dtype if ptype is None else ptype
+    xm, fm = _rows(x), _rows(f)
+    gm = None if gate is None else _rows(gate) if gate_rows else _dense(gate)
+    keep = (xm, fm, gm, *(_dense(p) for p in (post_weight, post_bias, weight, bias)))
+    a = Block(dt, _DTYPES[ptype], xm.shape[0], d, _NORMS[norm], post, pre, gate_rows, scale, eps, xm.data_ptr(), _stride(xm),
+              fm.data_ptr(), _stride(fm), _ptr(gm), _stride(gm) if gate_rows else 0, *(_ptr(p) for p in keep[3:]))
+    return a, keep, ptype
+
+
+def block_norm_forward(x, f, gate=None, scale=1.0, post=False, post_weight=None, post_bias=None, pre=True, weight=None, bias=None,
+                       norm="layer", eps=1e-5, stream=None):
+    """(h, y, stats) of what stands between two blocks of a residual tower, for
+    the residual stream x and a block's output f:
+
+        u = norm(f) * post_weight + post_bias, or f without post
+        h = scale * x + gate * u
+        y = norm(h) * weight + bias, or None without pre
+
+    x, f: (..., d), float32, bfloat16 or float16. gate: (d,), or of x's shape and
+    type. post_weight, post_bias, weight, bias, a shared gate: (d,) of x's type
+    or float32, all of one; any may be None. norm: "layer" or "rms". stats
+    (float32, (4, rows)) is what block_norm_backward takes."""
+    _device("block_norm", x, f, gate, post_weight, post_bias, weight, bias)
+    other = _at(x, stream, x, f, gate, post_weight, post_bias, weight, bias)
+    if other is not None:
+        with other:
+            return block_norm_forward(x, f, gate, scale, post, post_weight, post_bias, pre, weight, bias, norm, eps)
+    a, keep, _ = _block("block_norm", x, f, gate, post, pre, post_weight, post_bias, weight, bias, norm, scale, eps)
+    h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if pre else None
+    stats = torch.empty((4, a.rows), dtype=torch.float32, device=x.device)
+    a.h, a.y, a.stats = h.data_ptr(), _ptr(y), stats.data_ptr()
+    _check(_lib().boa_block_norm(C.byref(a), _current_stream(x.get_device())))
+    return h, y, stats
+
+
+def block_norm_backward(dh, dy, x, f, stats, gate=None, scale=1.0, post=False, post_weight=None, post_bias=None, pre=True,
+                        weight=None, bias=None, norm="layer", need_gate=True, need_params=True, stream=None):
+    """Gradients of block_norm_forward from those of h and y (either may be
+    None): a BlockNormGrads with those of x and f, of the gate (need_gate) and of
+    the parameters that there are (need_params)."""
+    _device("block_norm_backward", x, f, stats, gate, post_weight, post_bias, weight, bias, dh, dy)
+    if dh is None and dy is None:
+        raise ValueError("block_norm_backward: neither dh nor dy")
+    if dy is not None and not pre:
+        raise ValueError("block_norm_backward: dy without pre")
+    for g in (dh, dy):
+        if g is not None and (g.shape != x.shape or g.dtype != x.dtype):
+            raise ValueError("block_norm_backward: dh and dy must have x's shape and type")
+    if stats.dtype != torch.float32 or stats.dim() != 2 or stats.shape[0] != 4 or not stats.is_contiguous() \
+            or x.dim() and stats.shape[1] * x.shape[-1] != x.numel():
+        raise ValueError("block_norm_backward: stats must be the tensor of the forward pass")
+    other = _at(x, stream, dh, dy, x, f, stats, gate, post_weight, post_bias, weight, bias)
+    if other is not None:
+        with other:
+            return block_norm_backward(dh, dy, x, f, stats, gate, scale, post, post_weight, post_bias, pre, weight, bias, norm,
+                                       need_gate, need_params)
+    a, keep, ptype = _block("block_norm_backward", x, f, gate, post, pre, post_weight, post_bias, weight, bias, norm, scale, 0.0)
+    dhm, dym = None if dh is None else _rows(dh), None if dy is None else _rows(dy)
+    dev, d = x.device, a.d
+    r = BlockNormGrads(torch.empty(x.shape, dtype=x.dtype, device=dev), torch.empty(x.shape, dtype=x.dtype, device=dev))
+    vector = lambda wanted: torch.empty((d,), dtype=ptype, device=dev) if wanted else None  # noqa: E731
+    if gate is not None and need_gate:
+        r.dgate = torch.empty(x.shape, dtype=x.dtype, device=dev) if a.gate_rows else vector(True)
+    r.dpost_weight, r.dpost_bias, r.dweight, r.dbias = (vector(need_params and p is not None)
+                                                        for p in (post_weight, post_bias, weight, bias))
+    ws = None
+    if any(t is not None for t in (r.dpost_weight, r.dpost_bias, r.dweight, r.dbias)) or r.dgate is not None and not a.gate_rows:
+        ws = _workspace(x, _lib().boa_block_norm_backward_workspace(a.rows, d))
+    a.stats = stats.data_ptr()
+    a.dh, a.dh_stride = _ptr(dhm), 0 if dhm is None else _stride(dhm)
+    a.dy, a.dy_stride = _ptr(dym), 0 if dym is None else _stride(dym)
+    a.dx, a.df, a.dgate = r.dx.data_ptr(), r.df.data_ptr(), _ptr(r.dgate)
+    a.dpost_weight, a.dpost_bias, a.dweight, a.dbias = _ptr(r.dpost_weight), _ptr(r.dpost_bias), _ptr(r.dweight), _ptr(r.dbias)
+    a.workspace, a.workspace_bytes = _ptr(ws), 0 if ws is None else ws.numel()
+    _check(_lib().boa_block_norm_backward(C.byref(a), _current_stream(dev.index)))
+    return r
+
+
+class _BlockNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, f, gate, post_weight, post_bias, weight, bias, scale, post, pre, norm, eps):
+        h, y, stats = block_norm_forward(x, f, gate, scale, post, post_weight, post_bias, pre, weight, bias, norm, eps)
+        ctx.save_for_backward(x, f, gate, post_weight, post_bias, weight, bias, stats)
+        ctx.args = scale, post, pre, norm
+        ctx.set_materialize_grads(False)
+        return h, y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dh, dy):
+        x, f, gate, post_weight, post_bias, weight, bias, stats = ctx.saved_tensors
+        scale, post, pre, norm = ctx.args
+        if dh is None and dy is None:
+            return (None,) * 12
+        need = ctx.needs_input_grad
+        r = block_norm_backward(dh, dy, x, f, stats, gate, scale, post, post_weight, post_bias, pre, weight, bias, norm, need[2],
+                                any(need[3:7]))
+        return r.dx, r.df, r.dgate, r.dpost_weight, r.dpost_bias, r.dweight, r.dbias, None, None, None, None, None
+
+
+def block_norm(x, f, gate=None, scale=1.0, post=False, post_weight=None, post_bias=None, pre=True, weight=None, bias=None,
+               norm="layer", eps=1e-5):
+    """(h, y) of block_norm_forward, for autograd."""
+    return _BlockNorm.apply(x, f, gate, post_weight, post_bias, weight, bias, scale, post, pre, norm, eps)
