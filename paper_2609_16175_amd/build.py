@@ -3,6 +3,8 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -12,7 +14,7 @@ SOURCES = [os.path.join(PKG, "csrc", f) for f in ("boa_kernels.hip", "boa_build.
 LIB = os.path.join(PKG, "libboa.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # distances rely on explicit fused multiply-adds and nothing else fused
     "-ffp-contract=off",
     # no packed-FP32 instructions in generated code
@@ -26,12 +28,20 @@ def build(verbose: bool = False, stage_profile: bool = False) -> str:
     variant that prints per-stage cycle counts of every phase to stderr."""
     lib = LIB if not stage_profile else os.path.join(PKG, "libboa_stageprof.so")
     tmp = lib + f".tmp{os.getpid()}"
-    cmd = ["hipcc", *HIPCC_FLAGS, *(["-DBOA_STAGE_PROFILE"] if stage_profile else []), *SOURCES, "-o", tmp]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + r.stdout + r.stderr)
+    flags = [*HIPCC_FLAGS, *(["-DBOA_STAGE_PROFILE"] if stage_profile else [])]
+
+    def run(cmd):
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + r.stdout + r.stderr)
+        return r.stderr
+
+    with tempfile.TemporaryDirectory() as d, ThreadPoolExecutor(len(SOURCES)) as pool:
+        objects = [os.path.join(d, os.path.basename(s) + ".o") for s in SOURCES]
+        said = list(pool.map(lambda s, o: run(["hipcc", *flags, "-c", s, "-o", o]), SOURCES, objects))
+        said.append(run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-o", tmp]))
     if verbose:
-        print(r.stderr)
+        print("".join(said))
     os.replace(tmp, lib)
     return lib
 
