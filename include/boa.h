@@ -517,6 +517,38 @@ int64_t boa_block_norm_backward_workspace(int64_t rows, int32_t d);
 
 int boa_block_norm_backward(const boa_block *b, void *stream);
 
+#define BOA_MAX_ORTH (1 << 15)
+#define BOA_MAX_ORTH_COUNT 65535
+#define BOA_MAX_ORTH_STEPS 32
+/*
+ * Orthogonalises updates of weight matrices (rows x cols each) by Newton-Schulz
+ * products: X = G / (|G| + eps), |G| the root of G's sum of squares, then
+ *   X <- a X + (b X X^T + c (X X^T)^2) X
+ * for each step's a, b, c: every singular value s of X becomes a s + b s^3 +
+ * c s^5, the singular vectors stay. A zero update stays zero. X is held in
+ * float32, and the results are rounded once; the products' operands are
+ * rounded to f16's 11 bits for bfloat16 updates whose rows and cols are 128 or
+ * more, to 22 bits for others. A value that is not finite makes its matrix NaN,
+ * and so may steps that let singular values grow beyond 8.
+ */
+typedef struct {
+    int32_t dtype;              /* of update and out: any of the three */
+    int32_t rows, cols;         /* 1 .. BOA_MAX_ORTH */
+    int64_t count;              /* matrices, 0 .. BOA_MAX_ORTH_COUNT */
+    const void *update;
+    int64_t update_stride, update_batch;   /* from row to row, from matrix to matrix */
+    int32_t steps;              /* 1 .. BOA_MAX_ORTH_STEPS */
+    const float *coefficients;  /* HOST, 3 per step; read before the call returns */
+    float eps;
+    void *out;                  /* count x rows x cols, dense */
+} boa_orth;
+
+/* Work memory of one call in bytes; a negative BOA_E* code for invalid arguments. */
+int64_t boa_orthogonalize_workspace(const boa_orth *d);
+
+/* Errors: BOA_EINVAL, BOA_EHIP. */
+int boa_orthogonalize(const boa_orth *d, void *workspace, int64_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

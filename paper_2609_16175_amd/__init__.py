@@ -277,7 +277,7 @@ class Index:
 # The query-tower operators (ops.py), loaded on first use: they import torch.
 _OPS = ("layer_norm", "layer_norm_forward", "layer_norm_backward", "softmax_xent", "softmax_xent_grad", "XentResult",
         "matvec_4bit", "linear", "linear_forward", "linear_backward", "block_norm", "block_norm_forward",
-        "block_norm_backward", "BlockNormGrads")
+        "block_norm_backward", "BlockNormGrads", "orthogonalize")
 
 
 def __getattr__(name):

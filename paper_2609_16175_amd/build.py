@@ -10,7 +10,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SOURCES = [os.path.join(PKG, "csrc", f) for f in ("boa_kernels.hip", "boa_build.hip", "boa_api.hip",
                                                    "boa_norm.hip", "boa_xent.hip", "boa_matvec.hip",
-                                                   "boa_linear.hip", "boa_block.hip")]
+                                                   "boa_linear.hip", "boa_block.hip", "boa_orth.hip")]
 LIB = os.path.join(PKG, "libboa.so")
 
 HIPCC_FLAGS = [

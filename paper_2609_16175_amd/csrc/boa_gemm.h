@@ -7,6 +7,8 @@
 // Float32 operands come as two f16 parts (parts below), and three products.
 #pragma once
 
+#include <algorithm>
+
 #include "boa_ops.h"
 
 namespace boa {
@@ -54,6 +56,7 @@ struct Product {
     int32_t terms;     // 1, or 3 of two parts: a1 b0, a0 b1, a0 b0
     int32_t tiles_a, tiles_b, splits, batches;
     int32_t steps;     // of k a split takes
+    int32_t symmetric; // the output is: tiles with ta <= tb only
 };
 
 // A block's tile: WA x WB waves of TA x TB tiles of 32 x 32, BK values of k a stage.
@@ -203,12 +206,20 @@ __device__ inline Place place_of(const Product &pr)
     const uint32_t n = gridDim.x, id = blockIdx.x;
     const uint32_t x = id & 7, per = n >> 3, extra = n & 7;
     uint32_t t = x * per + min(x, extra) + (id >> 3);
-    const uint32_t tiles = (uint32_t)pr.tiles_a * pr.tiles_b;
+    const uint32_t tiles = pr.symmetric ? (uint32_t)pr.tiles_b * (pr.tiles_b + 1) / 2 : (uint32_t)pr.tiles_a * pr.tiles_b;
     Place w;
     const uint32_t layer = t / tiles;
     t -= layer * tiles;
     w.batch = layer / pr.splits;
     w.split = layer - w.batch * pr.splits;
+    if (pr.symmetric) {   // columns of 1, 2, 3 ... tiles
+        uint32_t c = (uint32_t)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+        while (c * (c + 1) / 2 > t) --c;
+        while ((c + 1) * (c + 2) / 2 <= t) ++c;
+        w.tb = c;
+        w.ta = t - c * (c + 1) / 2;
+        return w;
+    }
     const uint32_t band = t / (8 * pr.tiles_b), first = band * 8, rows = min(8u, pr.tiles_a - first);
     t -= band * 8 * pr.tiles_b;
     w.tb = t / rows;
@@ -285,9 +296,11 @@ __device__ inline void clear(f32x16 (&acc)[S::TB][S::TA])
 // Hands the sums out in runs of eight neighbouring columns: f(row of a's side,
 // first column of b's side, the eight sums in LDS). Each wave turns its tiles over
 // in its own piece of LDS, two columns of tiles at a time, so that what follows is written
-// once, and stores fill whole lines. The stages must no longer be in use.
-template <class S, class F>
-__device__ inline void each_run(const Place &w, const f32x16 (&acc)[S::TB][S::TA], char *lds, F f)
+// once, and stores fill whole lines. `turned`: g(first row, column, eight sums
+// down that column) for all of them too, for a transposed output. The stages
+// must no longer be in use.
+template <class S, class F, class G>
+__device__ inline void each_run(const Place &w, const f32x16 (&acc)[S::TB][S::TA], char *lds, F f, bool turned, G g)
 {
     constexpr int WIDE = S::TURN_COLS / 32, RUNS = S::TURN_COLS / 8, LD = S::TURN_COLS + 4;   // + 4: rows begin in other banks
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wa = wave % S::WA, wb = wave / S::WA;
@@ -312,8 +325,86 @@ __device__ inline void each_run(const Place &w, const f32x16 (&acc)[S::TB][S::TA
             const int row = k / RUNS, run = k % RUNS;
             f(p0 + row, q0 + i0 * 32 + run * 8, (const float *)(mine + row * LD + run * 8));
         }
+        if (turned)
+#pragma unroll 1
+            for (int k = lane; k < S::TURN_COLS * S::TA * 4; k += 64) {
+                const int run = k % (S::TA * 4), col = k / (S::TA * 4);
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = mine[(run * 8 + e) * LD + col];
+                g(p0 + run * 8, q0 + i0 * 32 + col, v);
+            }
         __builtin_amdgcn_wave_barrier();
     }
+}
+
+template <class S, class F>
+__device__ inline void each_run(const Place &w, const f32x16 (&acc)[S::TB][S::TA], char *lds, F f)
+{
+    each_run<S>(w, acc, lds, f, false, [](int32_t, int32_t, const float (&)[8]) {});
+}
+
+// ---------------------------------------------------------------------------
+// host
+
+// Work memory handed out piece by piece; without a base it only counts.
+struct Arena {
+    char *base = nullptr;
+    int64_t used = 0;
+    void *take(int64_t bytes)
+    {
+        void *p = base ? base + used : nullptr;
+        used += ceil_div(bytes, 256) * 256;
+        return p;
+    }
+};
+
+inline int32_t pad8(int64_t n) { return (int32_t)(ceil_div(n, 8) * 8); }
+
+inline uint32_t spread(int64_t items) { return (uint32_t)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, 256), 1 << 14)); }
+
+template <class T>
+using Large = Tile<T, 4, 2, 2, 4, 2>;
+template <class T>
+using Middle = Tile<T, 2, 2, 2, 2, 2>;
+template <class T>
+using Small = Tile<T, 2, 2, 1, 1, 3>;
+
+// How a product is cut into blocks.
+struct Cut {
+    int shape, splits;
+};
+
+// The cheapest of three tiles and some numbers of splits by a model of the
+// time: rounds of blocks over the GPU's 256 CUs, each as long as its stages
+// and a beginning and end; splits also write and read their sums. symmetric:
+// only the tiles on one side of the diagonal.
+inline Cut choose(int64_t A, int64_t B, int64_t K, int terms, int64_t batches, bool symmetric, bool may_split)
+{
+    struct Cost {
+        int side, at_once;
+        double stage, alone, ends;   // us a stage in a full CU and in a CU of its own, us of beginning and end
+    };
+    static const Cost costs[3] = {{256, 1, 1.85, 1.85, 5.0}, {128, 2, 1.07, 0.70, 3.0}, {64, 3, 0.65, 0.35, 2.0}};
+    static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    const int64_t steps = ceil_div(K, 64);
+    Cut best{0, 1};
+    double least = 1e30;
+    for (int s = 0; s < 3; ++s)
+        for (int n : counts) {
+            if (n > 1 && (!may_split || n > steps || (double)n * A * B * 4 > 256e6)) break;
+            const Cost &c = costs[s];
+            const int64_t each = ceil_div(steps, n), splits = ceil_div(steps, each);
+            const double tiles_a = (double)ceil_div(A, c.side), tiles_b = (double)ceil_div(B, c.side);
+            const double blocks = (symmetric ? tiles_a * (tiles_a + 1) / 2 : tiles_a * tiles_b) * splits * batches;
+            const double room = 256.0 * c.at_once;
+            const double full = (double)(int64_t)(blocks / room), rest = blocks - full * room;
+            double t = full * (each * terms * c.stage + c.ends);
+            if (rest > 0) t += each * terms * std::max(c.alone, c.stage * std::min(1.0, (double)ceil_div((int64_t)rest, 256) / c.at_once)) + c.ends;
+            if (splits > 1) t += 4.0 + (double)splits * A * B * 8 / 4e6;
+            if (t < least) least = t, best = {s, (int)splits};
+        }
+    return best;
 }
 
 }  // namespace boa

@@ -554,66 +554,9 @@ __global__ __launch_bounds__(512) void few_f32_kernel(FewArgs a)
 // ---------------------------------------------------------------------------
 // host
 
-// Work memory handed out piece by piece; without a base it only counts.
-struct Arena {
-    char *base = nullptr;
-    int64_t used = 0;
-    void *take(int64_t bytes)
-    {
-        void *p = base ? base + used : nullptr;
-        used += ceil_div(bytes, 256) * 256;
-        return p;
-    }
-};
-
-int32_t pad8(int64_t n) { return (int32_t)(ceil_div(n, 8) * 8); }
-
-uint32_t spread(int64_t items) { return (uint32_t)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, 256), 1 << 14)); }
-
 bool in_place(const void *p, int64_t ld, int64_t rows, int64_t cols)
 {
     return aligned(p, 16) && cols % 8 == 0 && (rows <= 1 || (ld % 8 == 0 && ld < 1 << 21));
-}
-
-template <class T>
-using Large = Tile<T, 4, 2, 2, 4, 2>;
-template <class T>
-using Middle = Tile<T, 2, 2, 2, 2, 2>;
-template <class T>
-using Small = Tile<T, 2, 2, 1, 1, 3>;
-
-// How a product is cut into blocks.
-struct Cut {
-    int shape, splits;
-};
-
-// The cheapest of three tiles and some numbers of splits by a model of the
-// time: rounds of blocks over the GPU's 256 CUs, each as long as its stages
-// and a beginning and end; splits also write and read their sums.
-Cut choose(int64_t A, int64_t B, int64_t K, int terms)
-{
-    struct Cost {
-        int side, at_once;
-        double stage, alone, ends;   // us a stage in a full CU and in a CU of its own, us of beginning and end
-    };
-    static const Cost costs[3] = {{256, 1, 1.85, 1.85, 5.0}, {128, 2, 1.07, 0.70, 3.0}, {64, 3, 0.65, 0.35, 2.0}};
-    static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-    const int64_t steps = ceil_div(K, 64);
-    Cut best{0, 1};
-    double least = 1e30;
-    for (int s = 0; s < 3; ++s)
-        for (int n : counts) {
-            if (n > 1 && (n > steps || (double)n * A * B * 4 > 256e6)) break;
-            const Cost &c = costs[s];
-            const int64_t each = ceil_div(steps, n), splits = ceil_div(steps, each);
-            const double blocks = (double)ceil_div(A, c.side) * ceil_div(B, c.side) * splits, room = 256.0 * c.at_once;
-            const double full = (double)(int64_t)(blocks / room), rest = blocks - full * room;
-            double t = full * (each * terms * c.stage + c.ends);
-            if (rest > 0) t += each * terms * std::max(c.alone, c.stage * std::min(1.0, (double)ceil_div((int64_t)rest, 256) / c.at_once)) + c.ends;
-            if (splits > 1) t += 4.0 + (double)splits * A * B * 8 / 4e6;
-            if (t < least) least = t, best = {s, (int)splits};
-        }
-    return best;
 }
 
 template <class S, bool ACROSS_A, bool ACROSS_B, class TO>
@@ -631,7 +574,7 @@ void launch(Product pr, const Epilogue &e, hipStream_t st)
 template <class T, class TO, bool ACROSS_A, bool ACROSS_B>
 void product(Operand a, Operand b, int32_t K, int terms, Epilogue e, Arena &mem, bool run, hipStream_t st)
 {
-    const Cut cut = choose(a.own, b.own, K, terms);
+    const Cut cut = choose(a.own, b.own, K, terms, 1, false, true);
     Product pr{};
     pr.a = a, pr.b = b, pr.K = K, pr.terms = terms, pr.batches = 1, pr.splits = cut.splits;
     pr.steps = (int32_t)ceil_div(ceil_div(K, 64), cut.splits);

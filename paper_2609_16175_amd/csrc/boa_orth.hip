@@ -1,0 +1,352 @@
+// Orthogonalisation of a weight's update by Newton-Schulz products.
+//
+//   X = G / (|G| + eps), |G| the root of the sum of squares; then some times
+//   X <- a X + (b A + c A^2) X,   A = X X^T
+//
+// which takes every singular value s of X to a s + b s^3 + c s^5 and leaves the
+// singular vectors: towards 1 with the right coefficients. X lies so that A is
+// the smaller of the two Gram matrices (m x m, m <= n). A and A^2 are symmetric:
+// half of their tiles are computed, and written twice. What is left is
+// 3 m^2 n + m^3 multiply-adds a step, which bound it for all but small matrices.
+//
+// The products run on the f16 matrix instructions. X itself is kept in float32 beside
+// its f16 copy: values that have shrunk towards 0 are multiplied by a at every
+// step, and rounding X to 16 bits would put noise into directions that G does
+// not have and let it grow (a relative error of 0.04 for updates of rank 8 in
+// 512 x 512, 0.0004 so); rounding the products' operands only
+// turns the directions that are there. For bfloat16 updates of at least 128
+// rows and columns A, b A + c A^2 and X are rounded to f16 (11 bits) as operands,
+// which puts results off by less than their rounding to bfloat16 does; for
+// others every operand is two f16 parts (22 bits), and three products. G is
+// scaled by a power of two, which rounds nothing; the rest of 1 / |G| goes into the
+// first step's coefficients.
+#include "boa_gemm.h"
+
+using namespace boa;
+
+namespace {
+
+constexpr int SUM_BLOCKS = 64;   // per matrix, at most
+// f16 copies hold X 2^10, A 2^10, (b A + c A^2) 2^8: values from 2^-24 of that to 64, 64, 255
+constexpr float X_UP = 1024.0f, A_UP = 1024.0f, B_UP = 256.0f;
+
+struct Step {
+    float a, b, c;
+};
+
+struct PrepArgs {
+    const void *g;
+    int64_t ld, batch;          // of g
+    int32_t rows, cols, turned; // turned: X is g transposed
+    int32_t m, n, x_ld;         // of X
+    int64_t x_size, parts;      // values of one X; from part to part (0: one part)
+    float *x;
+    f16_t *x16;
+    double *sums;               // SUM_BLOCKS per matrix
+    int32_t sum_blocks;
+    float eps;
+    Step *first;                // per matrix: the first step's coefficients
+    Step step0;
+};
+
+// Sums of squares of a stripe of rows, in float64: float32's largest values square below its range.
+template <class T>
+__global__ __launch_bounds__(256) void square_kernel(PrepArgs a)
+{
+    __shared__ double part[4];
+    const T *g = (const T *)a.g + blockIdx.y * a.batch;
+    const int64_t n = (int64_t)a.rows * a.cols;
+    double s = 0.0;
+    // neighbouring threads take neighbouring columns
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const double v = (double)(float)g[i / a.cols * a.ld + i % a.cols];
+        s = fma(v, v, s);
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) a.sums[(int64_t)blockIdx.y * SUM_BLOCKS + blockIdx.x] = part[0] + part[1] + part[2] + part[3];
+}
+
+// eight values as an f16 copy, and what it leaves out as the second part
+__device__ inline void write16(f16_t *to, int64_t parts, const float (&v)[8])
+{
+    f16x8 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        hi[e] = (f16_t)v[e];
+        lo[e] = (f16_t)(v[e] - (float)hi[e]);
+    }
+    *(f16x8 *)to = hi;
+    if (parts) *(f16x8 *)(to + parts) = lo;
+}
+
+// X of the first step: G times the power of two that brings |G| into [1, 2), as
+// float32 and f16, in tiles of 64 x 64; and that step's coefficients.
+template <class T>
+__global__ __launch_bounds__(256) void prep_kernel(PrepArgs a)
+{
+    __shared__ float tile[64][65];
+    __shared__ double total;
+    const int32_t z = blockIdx.z;
+    if (threadIdx.x < 64) {
+        double s = (int32_t)threadIdx.x < a.sum_blocks ? a.sums[(int64_t)z * SUM_BLOCKS + threadIdx.x] : 0.0;
+#pragma unroll
+        for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+        if (threadIdx.x == 0) total = sqrt(s);
+    }
+    const T *g = (const T *)a.g + z * a.batch;
+    const int32_t r0 = (a.turned ? blockIdx.x : blockIdx.y) * 64, c0 = (a.turned ? blockIdx.y : blockIdx.x) * 64;
+    for (int i = threadIdx.x; i < 64 * 64; i += 256) {
+        const int r = i >> 6, c = i & 63;
+        const float v = r0 + r < a.rows && c0 + c < a.cols ? (float)g[(int64_t)(r0 + r) * a.ld + c0 + c] : 0.0f;
+        if (a.turned) tile[c][r] = v;
+        else tile[r][c] = v;
+    }
+    __syncthreads();
+    int up = 0;
+    if (total > 0.0 && total < INFINITY) up = 1 - __builtin_amdgcn_frexp_exp(total);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+        const double by = total < INFINITY ? 1.0 / ldexp(total + (double)a.eps, up) : NAN, b3 = by * by * by;
+        // |G| = 0 and eps = 0: X is 0, not NaN
+        const bool none = total == 0.0;
+        a.first[z] = none ? Step{0.0f, 0.0f, 0.0f} : Step{(float)(a.step0.a * by), (float)(a.step0.b * b3), (float)(a.step0.c * b3 * by * by)};
+    }
+    const int32_t p0 = blockIdx.y * 64, q0 = blockIdx.x * 64;
+    for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+        const int p = i >> 3, q = (i & 7) * 8;
+        if (p0 + p >= a.m || q0 + q >= a.x_ld) continue;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = ldexpf(tile[p][q + e], up);
+        const int64_t at = z * a.x_size + (int64_t)(p0 + p) * a.x_ld + q0 + q;
+        store_f32<4, float>(a.x + at, *(float(*)[4])v);
+        store_f32<4, float>(a.x + at + 4, *(float(*)[4])(v + 4));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= X_UP;
+        write16(a.x16 + at, a.parts, v);
+    }
+}
+
+enum Kind { GRAM, POLY, UPDATE, LAST };
+
+struct StepArgs {
+    Kind kind;
+    f16_t *to;               // GRAM: A; POLY: b A + c A^2; UPDATE: X
+    int64_t to_ld, to_size, to_parts;
+    const f16_t *a;          // POLY: A, laid out as `to`
+    float *x;                // UPDATE: X, in place; LAST: read only
+    void *out;               // LAST
+    int64_t out_ld, out_size;
+    int32_t rows, cols;      // that are written (columns of `to` up to its padding)
+    int32_t dtype, turned;
+    Step step;
+    const Step *first;       // per matrix, in place of `step`, or null
+};
+
+// tile_product and what becomes of it. B_ACROSS: X, whose rows are k.
+template <class S, bool B_ACROSS>
+__global__ __launch_bounds__(S::THREADS) void step_kernel(Product pr, StepArgs e)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const Place w = place_of(pr);
+    f32x16 acc[S::TB][S::TA];
+    clear<S>(acc);
+    tile_product<S, false, B_ACROSS>(pr, w, (f16_t *)lds, acc);
+    const Step k = e.first ? e.first[w.batch] : e.step;
+    const int64_t base = w.batch * e.to_size;
+    if constexpr (!B_ACROSS) {
+        auto value = [&](float v, int64_t at) {
+            if (e.kind == GRAM) return v * (A_UP / (X_UP * X_UP));
+            float was = (float)e.a[at];
+            if (e.to_parts) was += (float)e.a[at + e.to_parts];
+            return k.b * was * (B_UP / A_UP) + k.c * (v * (B_UP / (A_UP * A_UP)));
+        };
+        each_run<S>(w, acc, lds,
+            [&](int32_t p, int32_t q, const float *v) {
+                if (p >= e.rows || q >= e.to_ld) return;
+                const int64_t at = base + p * e.to_ld + q;
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = value(v[i], at + i);
+                write16(e.to + at, e.to_parts, o);
+            },
+            w.ta != w.tb,
+            [&](int32_t p, int32_t q, const float (&v)[8]) {   // the mirrored tile
+                if (q >= e.rows || p >= e.to_ld) return;
+                const int64_t at = base + q * e.to_ld + p;
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = value(v[i], at + i);
+                write16(e.to + at, e.to_parts, o);
+            });
+    } else {
+        const float *x = e.x + w.batch * e.to_size;
+        constexpr float BY = 1.0f / (B_UP * X_UP);
+        auto put = [&](int64_t at, float v) {
+            const int64_t i = w.batch * e.out_size + at;
+            if (e.dtype == BOA_T_F32) ((float *)e.out)[i] = v;
+            else if (e.dtype == BOA_T_BF16) ((bf16_t *)e.out)[i] = (bf16_t)v;
+            else ((f16_t *)e.out)[i] = (f16_t)v;
+        };
+        each_run<S>(w, acc, lds,
+            [&](int32_t p, int32_t q, const float *v) {
+                if (p >= e.rows || q >= e.to_ld) return;
+                const int64_t at = p * e.to_ld + q;
+                float was[8], o[8];
+                load_f32<4, float>(*(float(*)[4])was, x + at);
+                load_f32<4, float>(*(float(*)[4])(was + 4), x + at + 4);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = fmaf(k.a, was[i], v[i] * BY);
+                if (e.kind == UPDATE) {
+                    store_f32<4, float>(e.x + base + at, *(float(*)[4])o);
+                    store_f32<4, float>(e.x + base + at + 4, *(float(*)[4])(o + 4));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) o[i] *= X_UP;
+                    write16(e.to + base + at, e.to_parts, o);
+                } else if (!e.turned) {
+                    if (q + 8 <= e.cols && e.dtype != BOA_T_F32) {
+                        void *to = (char *)e.out + (w.batch * e.out_size + p * e.out_ld + q) * 2;
+                        if (e.dtype == BOA_T_BF16) store_loose<8, bf16_t>((bf16_t *)to, o);
+                        else store_loose<8, f16_t>((f16_t *)to, o);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (q + i < e.cols) put(p * e.out_ld + q + i, o[i]);
+                    }
+                }
+            },
+            e.kind == LAST && e.turned,
+            [&](int32_t p, int32_t q, const float (&v)[8]) {   // rows p of X are columns of the output
+                if (q >= e.cols) return;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (p + i < e.rows) put(q * e.out_ld + p + i, fmaf(k.a, x[(p + i) * e.to_ld + q], v[i] * BY));
+            });
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host
+
+template <class S, bool B_ACROSS>
+void launch(Product pr, const StepArgs &e, hipStream_t st)
+{
+    pr.tiles_a = (int32_t)ceil_div(pr.a.own, S::BA);
+    pr.tiles_b = (int32_t)ceil_div(pr.b.own, S::BB);
+    const int64_t tiles = pr.symmetric ? (int64_t)pr.tiles_b * (pr.tiles_b + 1) / 2 : (int64_t)pr.tiles_a * pr.tiles_b;
+    const auto kernel = step_kernel<S, B_ACROSS>;
+    if (S::LDS > 64 << 10)   // has to be asked for
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+    kernel<<<dim3((uint32_t)(tiles * pr.batches)), S::THREADS, S::LDS, st>>>(pr, e);
+}
+
+template <bool B_ACROSS>
+void step(const Operand &a, const Operand &b, int32_t K, int terms, int64_t batches, const StepArgs &e, hipStream_t st)
+{
+    Product pr{};
+    pr.a = a, pr.b = b, pr.K = K, pr.terms = terms, pr.splits = 1, pr.batches = (int32_t)batches;
+    pr.steps = (int32_t)ceil_div(K, 64), pr.symmetric = !B_ACROSS;
+    const Cut cut = choose(a.own, b.own, K, terms, batches, !B_ACROSS, false);
+    if (cut.shape == 0) launch<Large<f16_t>, B_ACROSS>(pr, e, st);
+    else if (cut.shape == 1) launch<Middle<f16_t>, B_ACROSS>(pr, e, st);
+    else launch<Small<f16_t>, B_ACROSS>(pr, e, st);
+}
+
+int check(const boa_orth *d)
+{
+    if (!d) return set_error(BOA_EINVAL, "orthogonalize: NULL arguments");
+    const char *why = nullptr;
+    if (!dtype_known(d->dtype)) why = "unknown dtype";
+    else if (d->count < 0 || d->count > BOA_MAX_ORTH_COUNT) why = "count out of range [0, 2^16)";
+    else if (d->rows < 1 || d->rows > BOA_MAX_ORTH || d->cols < 1 || d->cols > BOA_MAX_ORTH) why = "rows and cols out of range [1, 2^15]";
+    else if (d->steps < 1 || d->steps > BOA_MAX_ORTH_STEPS) why = "steps out of range [1, 32]";
+    else if (!d->coefficients) why = "NULL coefficients";
+    else if (!(d->eps >= 0.0f)) why = "eps must not be negative";
+    else if (d->rows > 1 && d->update_stride < d->cols) why = "row stride smaller than cols";
+    else if (d->count && (!d->update || !d->out)) why = "NULL matrices";
+    if (!why)
+        for (int i = 0; i < 3 * d->steps; ++i)
+            if (!(d->coefficients[i] - d->coefficients[i] == 0.0f)) why = "coefficients must be finite";
+    if (!why) return BOA_OK;
+    char msg[160];
+    __builtin_snprintf(msg, sizeof(msg), "orthogonalize: %s", why);
+    return set_error(BOA_EINVAL, msg);
+}
+
+void orthogonalize(const boa_orth &d, Arena &mem, bool run, hipStream_t st)
+{
+    const bool turned = d.rows > d.cols;
+    const int32_t m = turned ? d.cols : d.rows, n = turned ? d.rows : d.cols;
+    const int32_t parts = d.dtype == BOA_T_BF16 && m >= 128 ? 1 : 2, terms = parts == 1 ? 1 : 3;
+    const int32_t x_ld = pad8(n), a_ld = pad8(m);
+    const int64_t x_size = (int64_t)m * x_ld, a_size = (int64_t)m * a_ld, C = d.count;
+    float *x = (float *)mem.take(C * x_size * 4);
+    f16_t *x16[2];   // the update reads the one and writes the other
+    for (auto &p : x16) p = (f16_t *)mem.take(C * x_size * parts * 2);
+    f16_t *a16 = (f16_t *)mem.take(C * a_size * parts * 2), *b16 = (f16_t *)mem.take(C * a_size * parts * 2);
+    double *sums = (double *)mem.take(C * SUM_BLOCKS * 8);
+    Step *first = (Step *)mem.take(C * (int64_t)sizeof(Step));
+    if (!run) return;
+    auto coefficients = [&](int i) { return Step{d.coefficients[3 * i], d.coefficients[3 * i + 1], d.coefficients[3 * i + 2]}; };
+    PrepArgs p{};
+    p.g = d.update, p.ld = d.rows > 1 ? d.update_stride : d.cols, p.batch = d.update_batch, p.rows = d.rows, p.cols = d.cols;
+    p.turned = turned, p.m = m, p.n = n, p.x_ld = x_ld, p.x_size = x_size, p.parts = parts == 2 ? C * x_size : 0;
+    p.x = x, p.x16 = x16[0], p.sums = sums, p.eps = d.eps, p.first = first, p.step0 = coefficients(0);
+    p.sum_blocks = (int32_t)std::min<int64_t>(SUM_BLOCKS, ceil_div((int64_t)d.rows * d.cols, 4096));
+    const dim3 squares((uint32_t)p.sum_blocks, (uint32_t)C), tiles((uint32_t)ceil_div(x_ld, 64), (uint32_t)ceil_div(m, 64), (uint32_t)C);
+    auto prepare = [&](auto t) {
+        using T = decltype(t);
+        square_kernel<T><<<squares, 256, 0, st>>>(p);
+        prep_kernel<T><<<tiles, 256, 0, st>>>(p);
+    };
+    if (d.dtype == BOA_T_F32) prepare(0.0f);
+    else if (d.dtype == BOA_T_BF16) prepare(bf16_t{});
+    else prepare(f16_t{});
+
+    Operand A{}, B{};
+    A.p = a16, B.p = b16, A.ld = B.ld = a_ld, A.batch = B.batch = a_size, A.part = B.part = C * a_size, A.own = B.own = m;
+    for (int i = 0; i < d.steps; ++i) {
+        Operand X{};
+        X.p = x16[i & 1], X.ld = x_ld, X.batch = x_size, X.part = C * x_size, X.own = m;
+        StepArgs e{};
+        e.step = coefficients(i), e.first = i == 0 ? first : nullptr;
+        e.rows = m, e.to_ld = a_ld, e.to_size = a_size, e.to_parts = parts == 2 ? C * a_size : 0;
+        e.kind = GRAM, e.to = a16;
+        step<false>(X, X, n, terms, C, e, st);
+        e.kind = POLY, e.to = b16, e.a = a16;
+        step<false>(A, A, m, terms, C, e, st);
+        e.kind = i + 1 < d.steps ? UPDATE : LAST;
+        e.to = x16[(i + 1) & 1], e.to_ld = x_ld, e.to_size = x_size, e.to_parts = parts == 2 ? C * x_size : 0, e.x = x;
+        e.out = d.out, e.out_ld = d.cols, e.out_size = (int64_t)d.rows * d.cols, e.cols = n, e.dtype = d.dtype, e.turned = turned;
+        X.own = x_ld;
+        step<true>(B, X, m, terms, C, e, st);
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t boa_orthogonalize_workspace(const boa_orth *d)
+{
+    if (int rc = check(d)) return rc;
+    Arena mem;
+    orthogonalize(*d, mem, false, nullptr);
+    return mem.used;
+}
+
+int boa_orthogonalize(const boa_orth *d, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (int rc = check(d)) return rc;
+    if (d->count == 0) return BOA_OK;
+    if (!workspace || !aligned(workspace, 16) || workspace_bytes < boa_orthogonalize_workspace(d))
+        return set_error(BOA_EINVAL, "orthogonalize: workspace missing, unaligned or too small");
+    Arena mem;
+    mem.base = (char *)workspace;
+    orthogonalize(*d, mem, true, (hipStream_t)stream);
+    return launch_status("orthogonalize");
+}
+
+}  // extern "C"

@@ -1,6 +1,6 @@
 """Operators of a query tower on device tensors: layer norm, linear layers, the
 norms around a residual block, softmax cross entropy over the points of an
-index, products with 4-bit rows.
+index, products with 4-bit rows, orthogonalised updates of weights.
 
 Argument marshalling for libboa.so (include/boa.h); every computation runs in
 the library's HIP kernels. Tensors live on one GPU; calls are queued on its
@@ -50,6 +50,12 @@ class Block(C.Structure):
                 ("dbias", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
 
 
+class Orth(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("count", C.c_int64), ("update", C.c_void_p),
+                ("update_stride", C.c_int64), ("update_batch", C.c_int64), ("steps", C.c_int32), ("coefficients", C.c_void_p),
+                ("eps", C.c_float), ("out", C.c_void_p)]
+
+
 _ready = None
 
 
@@ -75,6 +81,9 @@ def _lib():
             f.argtypes = [C.POINTER(Block), P]
         L.boa_block_norm_backward_workspace.argtypes = [i64, i32]
         L.boa_block_norm_backward_workspace.restype = i64
+        L.boa_orthogonalize_workspace.argtypes = [C.POINTER(Orth)]
+        L.boa_orthogonalize_workspace.restype = i64
+        L.boa_orthogonalize.argtypes = [C.POINTER(Orth), P, i64, P]
         _ready = L
     return _ready
 
@@ -681,3 +690,47 @@ def block_norm(x, f, gate=None, scale=1.0, post=False, post_weight=None, post_bi
                norm="layer", eps=1e-5):
     """(h, y) of block_norm_forward, for autograd."""
     return _BlockNorm.apply(x, f, gate, post_weight, post_bias, weight, bias, scale, post, pre, norm, eps)
+
+
+# ---------------------------------------------------------------------------
+# orthogonalised updates
+
+def orthogonalize(update, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, stream=None):
+    """Newton-Schulz orthogonalisation of the last two dimensions of update, as
+    an optimiser of weight matrices applies it to a momentum: x = update /
+    (|update| + eps), then `steps` times x = a x + (b x x' + c (x x')^2) x, which
+    takes the singular values towards 1 and keeps the singular vectors.
+
+    update: (..., rows, cols), float32, bfloat16 or float16; the result has its
+    type. coefficients: (a, b, c) for every step, or one such triple a step
+    (`steps` of them). Updates of one shape are best passed together. Not seen by
+    autograd."""
+    _device("orthogonalize", update)
+    dt = _dtype("orthogonalize", update)
+    if update.dim() < 2 or update.shape[-1] < 1 or update.shape[-2] < 1:
+        raise ValueError("orthogonalize: update must be (..., rows, cols)")
+    if not 1 <= steps <= 32:
+        raise ValueError("orthogonalize: steps must be 1 to 32")
+    each = list(coefficients)
+    if len(each) == 3 and not any(hasattr(c, "__len__") for c in each):
+        each = [each] * steps
+    if len(each) != steps or any(len(c) != 3 for c in each):
+        raise ValueError("orthogonalize: coefficients must be (a, b, c), or one such triple a step")
+    other = _at(update, stream, update)
+    if other is not None:
+        with other:
+            return orthogonalize(update, steps, coefficients, eps)
+    rows, cols = update.shape[-2:]
+    u = update if update.dim() == 3 else update.reshape(-1, rows, cols)
+    if cols > 1 and u.stride(2) != 1 or rows > 1 and u.stride(1) < cols:
+        u = u.contiguous()
+    out = torch.empty(update.shape, dtype=update.dtype, device=update.device)
+    flat = (C.c_float * (3 * steps))(*(float(v) for c in each for v in c))
+    a = Orth(dt, rows, cols, u.shape[0], u.data_ptr(), u.stride(1) if rows > 1 else cols, u.stride(0), steps, C.addressof(flat), eps,
+             out.data_ptr())
+    n = _lib().boa_orthogonalize_workspace(C.byref(a))
+    if n < 0:
+        _check(n)
+    ws = _workspace(update, n)
+    _check(_lib().boa_orthogonalize(C.byref(a), ws.data_ptr(), ws.numel(), _current_stream(update.get_device())))
+    return out

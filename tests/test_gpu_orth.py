@@ -1,0 +1,240 @@
+"""Orthogonalised updates on the GPU against plain float64 computations.
+
+One step is held to a bound of every value: each operand's rounding (f16's 11
+bits, or 22 in two parts), sums of n terms off by (n / 16 + 32) roundings of
+their terms' magnitudes, the result's rounding. Several steps are held to a
+bound of the whole result: a step takes an error in X into one at most
+max |f'| times as large (f the step's polynomial: divided differences of f are
+means of f', and f(s) / s is one of them from 0), and its own roundings, of
+independent signs, add up by their squares; four deviations are allowed.
+"""
+import math
+
+import pytest
+import torch
+
+import paper_2609_16175_amd as boa
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+EPS = 2.0 ** -24
+CO = (3.4445, -4.7750, 2.0315)
+
+
+def unit(dt):
+    return {F32: 2.0 ** -24, BF16: 2.0 ** -8, F16: 2.0 ** -11}[dt]
+
+
+def tiny(dt):
+    return {F32: 0.0, BF16: 0.0, F16: 2.0 ** -25}[dt]
+
+
+def sums(n):
+    return (n / 16 + 32) * EPS
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def bits(dt, m):
+    """Largest relative error of an operand: the f16 copy's, or both parts' and the product left out of them."""
+    return 2.0 ** -11 if dt == BF16 and m >= 128 else 2.0 ** -21
+
+
+def wide(g):   # as the operator lays it out
+    x = g.double()
+    return (x, False) if x.shape[0] <= x.shape[1] else (x.T, True)
+
+
+def one_step(x, co, u, terms, rho):
+    """(the step, error bound) of an exact x; copies lose what is below 2^-25 of 2^-10, 2^-10, 2^-8.
+
+    The first step's products are of x rho, |G| 2^e / |G| of x's own size with e
+    such that 1 <= |G| 2^e < 2, rho = (|G| + eps) 2^e: the division is part of its
+    coefficients a / rho, b / rho^3, c / rho^5. So what the copy of b A + c A^2
+    loses, up to 2^-33 a value, meets x rho and not x; the losses of the other
+    copies are divided by rho and rho^2 on their way and stay below those of a
+    copy of x and A themselves."""
+    a, b, c = co
+    m, n = x.shape
+    ax = x.abs()
+    e_x = u * ax + 2.0 ** -35
+    A = x @ x.T
+    e = 2 * e_x @ ax.T
+    e = torch.maximum(e, e.T) + e_x @ e_x.T + sums(n * terms) * ax @ ax.T
+    e_A = e + u * (A.abs() + e) + 2.0 ** -35
+    P = A @ A
+    e_P = e_A @ A.abs() + A.abs() @ e_A + e_A @ e_A + sums(m * terms) * (A.abs() + e_A) @ (A.abs() + e_A)
+    B = b * A + c * P
+    e_B = abs(b) * e_A + abs(c) * e_P
+    e_B = e_B + (u + 4 * EPS) * (abs(b) * A.abs() + abs(c) * P.abs() + e_B) + 2.0 ** -33 * max(1.0, rho)
+    y = a * x + B @ x
+    e_y = e_B @ (ax + e_x) + B.abs() @ e_x + sums(m * terms) * (B.abs() + e_B) @ ax + 4 * EPS * (abs(a) * ax + (B @ x).abs())
+    return y, e_y
+
+
+def start(g, eps):
+    x, turned = wide(g)
+    return x / (torch.linalg.matrix_norm(x) + eps), turned
+
+
+def check_one(g, got, dt, co=CO, eps=1e-7):
+    x, turned = start(g, eps)
+    size = float(torch.linalg.matrix_norm(g.double()))
+    y, e = one_step(x, co, bits(dt, x.shape[0]), 1 if dt == BF16 and x.shape[0] >= 128 else 3,
+                    (size + eps) * 2.0 ** (1 - math.frexp(size)[1]))
+    if turned:
+        y, e = y.T, e.T
+    got = got.double().cpu()
+    assert torch.isfinite(got).all()
+    over = (got - y).abs() - 1.01 * (unit(dt) * (y.abs() + e) + e) - tiny(dt)
+    assert (over <= 0).all(), f"off by {float((got - y).abs().max()):.3g}, {float(over.max()):.3g} over"
+
+
+def check_all(g, got, dt, coefficients, eps=1e-7):
+    x, turned = start(g, eps)
+    m, n = x.shape
+    u = bits(dt, m) / math.sqrt(3) + 2 * EPS
+    var = 0.0
+    for a, b, c in coefficients:
+        s = torch.linalg.matrix_norm(x, 2).clamp(min=1e-3)
+        t = torch.linspace(0, 1.02 * float(s), 2000, dtype=torch.float64)
+        L = float((a + 3 * b * t ** 2 + 5 * c * t ** 4).abs().max())
+        A = x @ x.T
+        B = b * A + c * A @ A
+        # independent roundings of A's copy (twice in A^2, once in b A), of X's (twice in A, once in B X), of B's
+        nx, nA = float(torch.linalg.matrix_norm(x)), float(torch.linalg.matrix_norm(A))
+        sA, sB = float(s) ** 2, float(torch.linalg.matrix_norm(B, 2))
+        d_A = u * (2 * float(s) * nx + nA)
+        own = (abs(b) + 2 * abs(c) * sA) * float(s) * d_A + u * float(torch.linalg.matrix_norm(B)) * float(s) + sB * u * nx + 4 * EPS * nx * abs(a)
+        var = var * L * L + own * own
+        x = a * x + B @ x
+    y = x.T if turned else x
+    got = got.double().cpu()
+    assert torch.isfinite(got).all()
+    off, size = float(torch.linalg.matrix_norm(got - y)), float(torch.linalg.matrix_norm(y))
+    bound = 4 * math.sqrt(var) + 1.01 * unit(dt) * size + tiny(dt) * math.sqrt(m * n)
+    assert off <= bound, f"off by {off / size:.3g} of the result, {bound / size:.3g} allowed"
+    return off / size
+
+
+def update(rows, cols, dt, seed, rank=None):
+    g = gen(seed)
+    if rank is None:
+        return (1e-3 * torch.randn(rows, cols, generator=g)).to(dt)
+    return (1e-3 * torch.randn(rows, rank, generator=g) @ torch.randn(rank, cols, generator=g)).to(dt)
+
+
+SHAPES = [(1, 1), (1, 7), (9, 1), (2, 3), (8, 8), (17, 5), (31, 32), (32, 96), (64, 64), (65, 63), (96, 33), (100, 413), (127, 127),
+          (128, 128), (129, 127), (128, 300), (257, 129), (130, 1000), (300, 301), (520, 264), (264, 776)]
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_one_step(rows, cols, dt):
+    g = update(rows, cols, dt, rows * 31 + cols)
+    check_one(g, boa.orthogonalize(g.cuda(), steps=1), dt)
+    co = (1.5, -0.5, 0.0)
+    check_one(g, boa.orthogonalize(g.cuda(), steps=1, coefficients=[co], eps=0.5), dt, co, 0.5)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_five_steps(rows, cols, dt):
+    g = update(rows, cols, dt, rows * 37 + cols)
+    got = boa.orthogonalize(g.cuda())
+    assert got.dtype == dt and got.shape == g.shape
+    check_all(g, got, dt, [CO] * 5)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("rank", [1, 8])
+def test_updates_of_low_rank(rank, dt):
+    # directions that the update does not have stay small: they are multiplied by up to 3.4445^5 = 485
+    g = update(256, 200, F32, rank, rank)
+    g = (g.to(dt) if dt != BF16 else g)   # bfloat16's own rounding has full rank
+    got = boa.orthogonalize(g.to(dt).cuda())
+    off = check_all(g.to(dt), got, dt, [CO] * 5)
+    assert off <= 2.0 ** -8 + 2.0 ** -10
+
+
+def test_steps_of_their_own():
+    g = update(60, 90, F32, 3)
+    co = [(3.0, -3.5, 1.2), (2.5, -2.0, 0.6), (1.5, -0.5, 0.0)]
+    check_all(g, boa.orthogonalize(g.cuda(), steps=3, coefficients=co), F32, co)
+    # the classical cubic iteration converges: rows of the result are orthonormal
+    x = boa.orthogonalize(g.cuda(), steps=32, coefficients=(1.5, -0.5, 0.0)).double().cpu()
+    assert float((x @ x.T - torch.eye(60, dtype=torch.float64)).abs().max()) <= 60 * 2.0 ** -20
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_batches_strides_and_the_same_bits(dt):
+    w = torch.stack([update(140, 200 + 3, dt, k) for k in range(3)])
+    u = w.cuda()[:, :, :200]
+    got = boa.orthogonalize(u)
+    assert got.shape == (3, 140, 200) and torch.equal(got, boa.orthogonalize(u))
+    for k in range(3):
+        assert torch.equal(got[k], boa.orthogonalize(u[k].contiguous()))
+        assert torch.equal(got[k], boa.orthogonalize(u[k]))
+        check_all(w[k, :, :200], got[k], dt, [CO] * 5)
+    t = boa.orthogonalize(u.transpose(1, 2))
+    assert t.shape == (3, 200, 140)
+    check_all(w[1, :, :200].T, t[1], dt, [CO] * 5)
+    assert boa.orthogonalize(u.reshape(1, 3, 140, 200)).shape == (1, 3, 140, 200)
+
+
+def test_values_of_every_size():
+    for by in (1e-35, 1e30):
+        g = update(40, 70, F32, 4) * 1e3 * by
+        check_all(g, boa.orthogonalize(g.cuda(), eps=0.0), F32, [CO] * 5, 0.0)
+    g = update(33, 20, F32, 5) * 1e-27   # eps is most of the divisor: every step multiplies by a
+    want = g.double() / (torch.linalg.matrix_norm(g.double()) + 1e-7) * CO[0] ** 5
+    got = boa.orthogonalize(g.cuda()).double().cpu()
+    assert float((got - want).abs().max()) <= 2.0 ** -20 * float(want.abs().max())
+
+
+def test_nothing_zeros_and_nan():
+    z = torch.zeros(2, 30, 40, device="cuda")
+    assert torch.equal(boa.orthogonalize(z), z) and torch.equal(boa.orthogonalize(z, eps=0.0), z)
+    for bad in (math.nan, math.inf):
+        u = torch.randn(3, 150, 140, generator=gen(1)).bfloat16().cuda()
+        whole = boa.orthogonalize(u)
+        u[1, 5, 7] = bad
+        got = boa.orthogonalize(u)
+        assert torch.isnan(got[1]).all() and torch.equal(got[0], whole[0]) and torch.equal(got[2], whole[2])
+    assert boa.orthogonalize(torch.empty(0, 4, 5, device="cuda")).shape == (0, 4, 5)
+
+
+def test_another_stream_and_captured():
+    u = torch.randn(2, 150, 300, generator=gen(2)).cuda()
+    want = boa.orthogonalize(u)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = boa.orthogonalize(u, stream=s)
+    s.synchronize()
+    assert torch.equal(got, want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = boa.orthogonalize(u)
+    for k in range(3):
+        u.copy_(torch.randn(2, 150, 300, generator=gen(k + 3)))
+        g.replay()
+        mine = out.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(mine, boa.orthogonalize(u))
+
+
+def test_binding_refuses():
+    u = torch.zeros(4, 5, device="cuda")
+    for kw in (dict(steps=0), dict(steps=33), dict(coefficients=(1.0, 2.0)), dict(coefficients=[(1, 2, 3)] * 4),
+               dict(coefficients=[(1, 2)] * 5)):
+        with pytest.raises(ValueError):
+            boa.orthogonalize(u, **kw)
+    with pytest.raises(ValueError):
+        boa.orthogonalize(u[0])
+    with pytest.raises(TypeError):
+        boa.orthogonalize(u.double())
+    with pytest.raises(boa.BoaError, match="eps"):
+        boa.orthogonalize(u, eps=-1.0)
