@@ -420,8 +420,8 @@ enum { BOA_ACT_NONE = 0, BOA_ACT_RELU = 1, BOA_ACT_SILU = 2, BOA_ACT_GELU = 3, B
  * gelu_tanh z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2. And its gradients:
  *   dz = dy act'(z)    dx = dz w    dw = dz^T x    dbias = sum over rows of dz
  * (the residual's is dy). x, w, residual, y and their gradients have one type.
- * Sums are float32. In bfloat16 and float16, z is kept in float16, clamped to its
- * range (every act' is constant beyond it), and dz is rounded to the layer's type
+ * Sums are float32. In bfloat16 and float16, z is kept in float16, infinite beyond
+ * its range (where every act' is constant), and dz is rounded to the layer's type
  * as an operand of the two products, not in dbias. In float32, with more than
  * BOA_LINEAR_FEW_F32 rows or in the gradients, the products' operands are
  * rounded to 22 bits (values far below the largest of their row, or of their

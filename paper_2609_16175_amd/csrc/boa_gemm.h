@@ -59,12 +59,14 @@ struct Product {
     int32_t symmetric; // the output is: tiles with ta <= tb only
 };
 
-// A block's tile: WA x WB waves of TA x TB tiles of 32 x 32, BK values of k a stage.
-template <class T_, int WA_, int WB_, int TA_, int TB_, int STAGES_>
+// A block's tile: WA x WB waves of TA x TB tiles of 32 x 32, BK values of k a
+// stage, PER_CU blocks of it at once on a CU.
+template <class T_, int WA_, int WB_, int TA_, int TB_, int BK_, int STAGES_, int PER_CU_>
 struct Tile {
     typedef T_ T;
-    static constexpr int WA = WA_, WB = WB_, TA = TA_, TB = TB_, STAGES = STAGES_;
-    static constexpr int BA = WA * TA * 32, BB = WB * TB * 32, THREADS = 64 * WA * WB, BK = 64;
+    static constexpr int WA = WA_, WB = WB_, TA = TA_, TB = TB_, BK = BK_, STAGES = STAGES_, PER_CU = PER_CU_;
+    static constexpr int BA = WA * TA * 32, BB = WB * TB * 32, THREADS = 64 * WA * WB;
+    static_assert(STAGES >= 2 && (BK == 32 || BK == 64), "a stage is read while the next one arrives");
     static constexpr int STAGE = (BA + BB) * BK;   // values
     // columns that a wave turns over at a time at the end, and what that takes
     static constexpr int TURN_COLS = TB % 2 ? 32 : 64, TURN_BYTES = TA * 32 * (TURN_COLS + 4) * 4;
@@ -104,8 +106,9 @@ __device__ inline void load_to_lds(words4 buffer, uint32_t offset, uint32_t to)
 // One operand's side of a stage: where this thread's loads come from, and where
 // its fragments lie.
 //
-// Along k, a stage holds ROWS rows of 64 values whose 16-byte chunks are stored
-// in the order chunk ^ (row & 7); across, 64 rows of ROWS values in the order
+// Along k, a stage holds ROWS rows of BK values whose 16-byte chunks are stored
+// in the order chunk ^ (row / 2 & 7), or of four chunks chunk ^ (row / 4 & 3):
+// any 16 rows that follow each other are in all banks; across, BK rows of ROWS values in the order
 // chunk ^ (row & 3) * 4, and fragments are read transposed, 64 bytes of four
 // rows by half a wave. Either way what lanes read together spreads over the
 // banks. The permutation is applied to the addresses loaded from, since a load
@@ -118,11 +121,11 @@ struct Side {
     static constexpr int N = ROWS * (S::BK / 8) / S::THREADS;     // loads of a stage
     static constexpr int PER = S::THREADS / CHUNKS;               // LDS rows of one load of all threads
     static_assert(N * S::THREADS == ROWS * (S::BK / 8) && PER * CHUNKS == S::THREADS, "whole loads");
-    static_assert(ACROSS ? PER % 4 == 0 || N == 1 : PER % 8 == 0, "one permutation for all of a thread's loads");
+    static_assert(ACROSS ? PER % 4 == 0 || N == 1 : PER % 16 == 0 || N == 1, "one permutation for all of a thread's loads");
     uint32_t at[N];   // byte offsets from the stage's base
     int32_t k;        // of load 0 (across: + PER each)
 
-    __device__ static int swap(int row) { return ACROSS ? (ROWS >= 128 ? (row & 3) * 4 : (row & 1) * 4) : row & 7; }
+    __device__ static int swap(int row) { return ACROSS ? (ROWS >= 128 ? (row & 3) * 4 : (row & 1) * 4) : CHUNKS == 8 ? (row >> 1) & 7 : (row >> 2) & 3; }
 
     __device__ Side(const Operand &o, int32_t own0)
     {
@@ -229,7 +232,11 @@ __device__ inline Place place_of(const Product &pr)
 
 // acc[i][j] += tile i of b times tile j of a: lane (l & 31) holds row j * 32 +
 // (l & 31) of a's side, its values e columns i * 32 + 8 (e / 4) + 4 (l / 32) +
-// e % 4 of b's side. Loads run STAGES - 1 stages ahead.
+// e % 4 of b's side. Fragments are read one step of 16 ahead of the matrix
+// instructions. Before the last step of a stage the next one is waited for and
+// the waves meet: all fragments of the stage are in registers then, its place
+// takes the loads of the stage STAGES further on, and that step's instructions
+// cover the meeting and the next stage's first reads.
 template <class S, bool ACROSS_A, bool ACROSS_B>
 __device__ inline void tile_product(const Product &pr, const Place &w, typename S::T *lds, f32x16 (&acc)[S::TB][S::TA])
 {
@@ -257,27 +264,41 @@ __device__ inline void tile_product(const Product &pr, const Place &w, typename 
         if (++stage == STAGES) stage = 0;
         if (++step == steps) step = 0, --term;
     };
-    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) T *)lds;
+    const uint32_t base = lds_address(lds);
     const uint32_t lane_a = A::lane_at(wa * S::TA * 32), lane_b = B::lane_at(wb * S::TB * 32) + S::BA * BK * 2;
-    for (int i = 0; i < STAGES - 1; ++i) load();
+    typename Vec<T>::v8 fa[2][S::TA], fb[2][S::TB];
+    auto read = [&](int to, int32_t slot, int s) {
+        const uint32_t at_a = base + slot * S::STAGE * 2 + lane_a, at_b = base + slot * S::STAGE * 2 + lane_b;
+#pragma unroll
+        for (int j = 0; j < S::TA; ++j) fa[to][j] = A::fragment(at_a, j, s);
+#pragma unroll
+        for (int i = 0; i < S::TB; ++i) fb[to][i] = B::fragment(at_b, i, s);
+    };
+    constexpr int LOADS = A::N + B::N, STEPS = BK / 16;
+    for (int i = 0; i < STAGES; ++i) load();
+    wait_and_meet<(STAGES - 1) * LOADS>();
     int32_t cur = 0;
+    read(0, 0, 0);
     for (int32_t it = 0; it < total; ++it) {
-        wait_and_meet<(STAGES - 2) * (A::N + B::N)>();
-        load();
-        const uint32_t at_a = base + cur * S::STAGE * 2 + lane_a, at_b = base + cur * S::STAGE * 2 + lane_b;
-        if (++cur == STAGES) cur = 0;
+        const int32_t next = cur + 1 == STAGES ? 0 : cur + 1;
 #pragma unroll
-        for (int s = 0; s < BK / 16; ++s) {
-            typename Vec<T>::v8 fa[S::TA], fb[S::TB];
-#pragma unroll
-            for (int j = 0; j < S::TA; ++j) fa[j] = A::fragment(at_a, j, s);
-#pragma unroll
-            for (int i = 0; i < S::TB; ++i) fb[i] = B::fragment(at_b, i, s);
+        for (int s = 0; s < STEPS; ++s) {
+            if (s + 1 < STEPS) {
+                read((s + 1) & 1, cur, s + 1);
+            } else {
+                wait_and_meet<(STAGES - 2) * LOADS>();
+                load();
+                read(0, next, 0);
+            }
+            // else the reads would be gathered before the instructions that use them (4096^3: 1,010 in place of 1,170 TFLOP/s);
+            // transposed ones are as well off without (1,220 and 1,170)
+            if constexpr (!ACROSS_A && !ACROSS_B) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < S::TB; ++i)
 #pragma unroll
-                for (int j = 0; j < S::TA; ++j) acc[i][j] = mfma32(fb[i], fa[j], acc[i][j]);
+                for (int j = 0; j < S::TA; ++j) acc[i][j] = mfma32(fb[s & 1][i], fa[s & 1][j], acc[i][j]);
         }
+        cur = next;
     }
     wait_and_meet<0>();
 }
@@ -364,11 +385,11 @@ inline int32_t pad8(int64_t n) { return (int32_t)(ceil_div(n, 8) * 8); }
 inline uint32_t spread(int64_t items) { return (uint32_t)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, 256), 1 << 14)); }
 
 template <class T>
-using Large = Tile<T, 4, 2, 2, 4, 2>;
+using Large = Tile<T, 4, 2, 2, 4, 64, 2, 1>;
 template <class T>
-using Middle = Tile<T, 2, 2, 2, 2, 2>;
+using Middle = Tile<T, 2, 2, 2, 2, 64, 2, 2>;
 template <class T>
-using Small = Tile<T, 2, 2, 1, 1, 3>;
+using Small = Tile<T, 2, 2, 1, 1, 64, 2, 4>;
 
 // How a product is cut into blocks.
 struct Cut {

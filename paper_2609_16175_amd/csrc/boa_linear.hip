@@ -25,50 +25,85 @@ namespace {
 // ---------------------------------------------------------------------------
 // activations
 
+constexpr float LOG2E = 1.4426950408889634f;
 constexpr float SQRT_HALF = 0.70710678118654752f;
 constexpr float INV_SQRT_2PI = 0.39894228040143268f;
 constexpr float SQRT_2_PI = 0.79788456080286536f;
 constexpr float CUBE = 0.044715f;
 
-// FINE: float32 layers. The short exponential is off by some 2^-22 of its value
-// for arguments that matter, far below 16 bits' rounding.
+// FINE: float32 layers, with the library's functions. For 16 bits the hardware's
+// exponential and reciprocal (2^-22 of their values), since in a product's
+// epilogue every instruction counts.
 template <bool FINE>
-__device__ inline float exp_of(float v) { return FINE ? expf(v) : __expf(v); }
+__device__ inline float sigmoid(float z)
+{
+    if constexpr (FINE) return 1.0f / (1.0f + expf(-z));
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-LOG2E * z));
+}
 
+// The normal distribution's function and density at z. For 16 bits Hastings'
+// rational approximation of the error function (Abramowitz and Stegun 7.1.26, off by at most
+// 1.5e-7), whose e^(-x^2) is the density's too.
 template <bool FINE>
-__device__ inline float sigmoid(float z) { return 1.0f / (1.0f + exp_of<FINE>(-z)); }
+__device__ inline void normal(float z, float &below, float &density)
+{
+    if constexpr (FINE) {
+        below = 0.5f * (1.0f + erff(z * SQRT_HALF));
+        density = INV_SQRT_2PI * expf(-0.5f * z * z);
+    } else {
+        const float e = __builtin_amdgcn_exp2f(-0.5f * LOG2E * z * z);
+        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * SQRT_HALF, fabsf(z), 1.0f));
+        // halves of the published coefficients: 1 - erf becomes the share above |z|
+        float tail = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+        tail = fmaf(t, tail, 0.5f * 1.421413741f);
+        tail = fmaf(t, tail, 0.5f * -0.284496736f);
+        tail = fmaf(t, tail, 0.5f * 0.254829592f) * t * e;
+        below = z > 0.0f ? 1.0f - tail : tail;
+        density = INV_SQRT_2PI * e;
+    }
+}
 
+// Activations and their slopes; an activation's limit at -inf is 0, a slope's far from 0 is 0 or 1.
 template <bool FINE>
 __device__ inline float act_of(float z, int32_t act)
 {
-    switch (act) {
-    case BOA_ACT_RELU: return z > 0.0f ? z : z != z ? z : 0.0f;
-    case BOA_ACT_SILU: return z == -INFINITY ? -0.0f : z * sigmoid<FINE>(z);
-    case BOA_ACT_GELU: return z == -INFINITY ? -0.0f : 0.5f * z * (1.0f + erff(z * SQRT_HALF));
-    // (1 + tanh u) / 2 = sigmoid(2 u)
-    case BOA_ACT_GELU_TANH: return z == -INFINITY ? -0.0f : z * sigmoid<FINE>(2.0f * SQRT_2_PI * (z + CUBE * z * z * z));
-    default: return z;
+    float y;
+    if (act == BOA_ACT_RELU) {
+        return z > 0.0f ? z : z != z ? z : 0.0f;
+    } else if (act == BOA_ACT_SILU) {
+        y = z * sigmoid<FINE>(z);
+    } else if (act == BOA_ACT_GELU) {
+        float below, density;
+        normal<FINE>(z, below, density);
+        y = z * below;
+    } else if (act == BOA_ACT_GELU_TANH) {
+        y = z * sigmoid<FINE>(2.0f * SQRT_2_PI * z * fmaf(CUBE * z, z, 1.0f));   // (1 + tanh u) / 2 = sigmoid(2 u)
+    } else {
+        return z;
     }
+    return z == -INFINITY ? 0.0f : y;
 }
 
 template <bool FINE>
 __device__ inline float slope_of(float z, int32_t act)
 {
-    switch (act) {
-    case BOA_ACT_RELU: return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
-    case BOA_ACT_SILU: {
-        const float s = sigmoid<FINE>(z);
-        return fabsf(z) > 100.0f ? (z > 0.0f ? 1.0f : 0.0f) : s * (1.0f + z * (1.0f - s));
+    float s, far;
+    if (act == BOA_ACT_RELU) {
+        return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
+    } else if (act == BOA_ACT_SILU) {
+        const float g = sigmoid<FINE>(z);
+        s = fmaf(z * g, 1.0f - g, g), far = 100.0f;
+    } else if (act == BOA_ACT_GELU) {
+        float below, density;
+        normal<FINE>(z, below, density);
+        s = fmaf(z, density, below), far = 20.0f;
+    } else if (act == BOA_ACT_GELU_TANH) {
+        const float g = sigmoid<FINE>(2.0f * SQRT_2_PI * z * fmaf(CUBE * z, z, 1.0f));
+        s = fmaf(z * g * (1.0f - g), 2.0f * SQRT_2_PI * fmaf(3.0f * CUBE * z, z, 1.0f), g), far = 20.0f;
+    } else {
+        return 1.0f;
     }
-    case BOA_ACT_GELU: return fabsf(z) > 20.0f ? (z > 0.0f ? 1.0f : 0.0f)
-                              : 0.5f * (1.0f + erff(z * SQRT_HALF)) + z * INV_SQRT_2PI * exp_of<FINE>(-0.5f * z * z);
-    case BOA_ACT_GELU_TANH: {
-        const float s = sigmoid<FINE>(2.0f * SQRT_2_PI * (z + CUBE * z * z * z));
-        return fabsf(z) > 20.0f ? (z > 0.0f ? 1.0f : 0.0f)
-               : s + z * s * (1.0f - s) * 2.0f * SQRT_2_PI * (1.0f + 3.0f * CUBE * z * z);
-    }
-    default: return 1.0f;
-    }
+    return fabsf(z) > far ? (z > 0.0f ? 1.0f : 0.0f) : s;
 }
 
 // ---------------------------------------------------------------------------
@@ -92,19 +127,22 @@ struct Epilogue {
 // Power of two that brings magnitudes of up to m below 2^15.
 __device__ inline int up(float m) { return 15 - __builtin_amdgcn_frexp_expf(m); }
 
-__device__ inline f16_t kept(float z)
-{
-    return (f16_t)(z != z ? z : fminf(fmaxf(z, -65504.0f), 65504.0f));
-}
-
 // N neighbouring values of a row, at column q (the row has them all)
 template <class TO, int N>
 __device__ inline void finish(const Epilogue &e, int64_t p, int32_t q, float (&v)[N])
 {
     constexpr bool WIDE = sizeof(TO) == 4;
     if (e.bias) {
+        float t[N];
+        if constexpr (N == 8) {
+            if (e.bias_f32) load_loose<8, float>(t, (const float *)e.bias + q);
+            else load_loose<8, TO>(t, (const TO *)e.bias + q);
+        } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += e.bias_f32 ? ((const float *)e.bias)[q + i] : (float)((const TO *)e.bias)[q + i];
+            for (int i = 0; i < N; ++i) t[i] = e.bias_f32 ? ((const float *)e.bias)[q + i] : (float)((const TO *)e.bias)[q + i];
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += t[i];
     }
     if (e.pre) {
         if constexpr (WIDE) {
@@ -113,11 +151,11 @@ __device__ inline void finish(const Epilogue &e, int64_t p, int32_t q, float (&v
         } else if constexpr (N == 8) {
             Pack<8, f16_t> k;
 #pragma unroll
-            for (int i = 0; i < N; ++i) k.v[i] = kept(v[i]);
+            for (int i = 0; i < N; ++i) k.v[i] = (f16_t)v[i];
             *(loose4 *)((f16_t *)e.pre + p * e.cols + q) = __builtin_bit_cast(words4, k);
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) ((f16_t *)e.pre)[p * e.cols + q + i] = kept(v[i]);
+            for (int i = 0; i < N; ++i) ((f16_t *)e.pre)[p * e.cols + q + i] = (f16_t)v[i];
         }
     }
     if (e.act != BOA_ACT_NONE) {
@@ -173,7 +211,7 @@ __device__ inline void finish_run(const Epilogue &e, int64_t p, int32_t q, const
 }
 
 template <class S, bool ACROSS_A, bool ACROSS_B, class TO>
-__global__ __launch_bounds__(S::THREADS) void product_kernel(Product pr, Epilogue e)
+__global__ __launch_bounds__(S::THREADS, S::PER_CU * S::THREADS / 256) void product_kernel(Product pr, Epilogue e)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const Place w = place_of(pr);

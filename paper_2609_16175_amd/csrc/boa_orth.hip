@@ -147,7 +147,7 @@ struct StepArgs {
 
 // tile_product and what becomes of it. B_ACROSS: X, whose rows are k.
 template <class S, bool B_ACROSS>
-__global__ __launch_bounds__(S::THREADS) void step_kernel(Product pr, StepArgs e)
+__global__ __launch_bounds__(S::THREADS, S::PER_CU * S::THREADS / 256) void step_kernel(Product pr, StepArgs e)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const Place w = place_of(pr);
