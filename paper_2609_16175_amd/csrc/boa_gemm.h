@@ -315,13 +315,14 @@ __device__ inline void clear(f32x16 (&acc)[S::TB][S::TA])
 }
 
 // Hands the sums out in runs of eight neighbouring columns: f(row of a's side,
-// first column of b's side, the eight sums in LDS). Each wave turns its tiles over
-// in its own piece of LDS, two columns of tiles at a time, so that what follows is written
-// once, and stores fill whole lines. `turned`: g(first row, column, eight sums
-// down that column) for all of them too, for a transposed output. The stages
-// must no longer be in use.
-template <class S, class F, class G>
-__device__ inline void each_run(const Place &w, const f32x16 (&acc)[S::TB][S::TA], char *lds, F f, bool turned, G g)
+// first column of b's side, the eight sums in LDS, what(column)); a lane keeps
+// its columns over many rows, so that `what` (their bias, say) is asked for once.
+// Each wave turns its tiles over in its own piece of LDS, two columns of tiles at
+// a time, so that what follows is written once, and stores fill whole lines.
+// `turned`: g(first row, column, eight sums down that column) for all of them
+// too, for a transposed output. The stages must no longer be in use.
+template <class S, class W, class F, class G>
+__device__ inline void each_run(const Place &w, const f32x16 (&acc)[S::TB][S::TA], char *lds, W what, F f, bool turned, G g)
 {
     constexpr int WIDE = S::TURN_COLS / 32, RUNS = S::TURN_COLS / 8, LD = S::TURN_COLS + 4;   // + 4: rows begin in other banks
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wa = wave % S::WA, wb = wave / S::WA;
@@ -330,39 +331,38 @@ __device__ inline void each_run(const Place &w, const f32x16 (&acc)[S::TB][S::TA
     const int32_t p0 = w.ta * S::BA + wa * S::TA * 32, q0 = w.tb * S::BB + wb * S::TB * 32;
 #pragma unroll
     for (int i0 = 0; i0 < S::TB; i0 += WIDE) {
+        const int32_t col = lane % RUNS * 8, q = q0 + i0 * 32 + col;
+        const auto kept = what(q);
 #pragma unroll
         for (int i = 0; i < WIDE; ++i)
 #pragma unroll
             for (int j = 0; j < S::TA; ++j)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
+                for (int g4 = 0; g4 < 4; ++g4) {
                     const f32x16 &v = acc[i0 + i][j];
-                    *(f32x4 *)(mine + (j * 32 + r) * LD + i * 32 + g * 8 + half * 4) =
-                        f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+                    *(f32x4 *)(mine + (j * 32 + r) * LD + i * 32 + g4 * 8 + half * 4) =
+                        f32x4{v[4 * g4], v[4 * g4 + 1], v[4 * g4 + 2], v[4 * g4 + 3]};
                 }
         __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-        for (int k = lane; k < S::TA * 32 * RUNS; k += 64) {
-            const int row = k / RUNS, run = k % RUNS;
-            f(p0 + row, q0 + i0 * 32 + run * 8, (const float *)(mine + row * LD + run * 8));
-        }
+#pragma unroll 2
+        for (int row = lane / RUNS; row < S::TA * 32; row += 64 / RUNS) f(p0 + row, q, (const float *)(mine + row * LD + col), kept);
         if (turned)
 #pragma unroll 1
             for (int k = lane; k < S::TURN_COLS * S::TA * 4; k += 64) {
-                const int run = k % (S::TA * 4), col = k / (S::TA * 4);
+                const int run = k % (S::TA * 4), c = k / (S::TA * 4);
                 float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = mine[(run * 8 + e) * LD + col];
-                g(p0 + run * 8, q0 + i0 * 32 + col, v);
+                for (int e = 0; e < 8; ++e) v[e] = mine[(run * 8 + e) * LD + c];
+                g(p0 + run * 8, q0 + i0 * 32 + c, v);
             }
         __builtin_amdgcn_wave_barrier();
     }
 }
 
-template <class S, class F>
-__device__ inline void each_run(const Place &w, const f32x16 (&acc)[S::TB][S::TA], char *lds, F f)
+template <class S, class W, class F>
+__device__ inline void each_run(const Place &w, const f32x16 (&acc)[S::TB][S::TA], char *lds, W what, F f)
 {
-    each_run<S>(w, acc, lds, f, false, [](int32_t, int32_t, const float (&)[8]) {});
+    each_run<S>(w, acc, lds, what, f, false, [](int32_t, int32_t, const float (&)[8]) {});
 }
 
 // ---------------------------------------------------------------------------

@@ -64,19 +64,19 @@ __device__ inline void normal(float z, float &below, float &density)
 }
 
 // Activations and their slopes; an activation's limit at -inf is 0, a slope's far from 0 is 0 or 1.
-template <bool FINE>
-__device__ inline float act_of(float z, int32_t act)
+template <bool FINE, int ACT>
+__device__ inline float act_of(float z)
 {
     float y;
-    if (act == BOA_ACT_RELU) {
+    if constexpr (ACT == BOA_ACT_RELU) {
         return z > 0.0f ? z : z != z ? z : 0.0f;
-    } else if (act == BOA_ACT_SILU) {
+    } else if constexpr (ACT == BOA_ACT_SILU) {
         y = z * sigmoid<FINE>(z);
-    } else if (act == BOA_ACT_GELU) {
+    } else if constexpr (ACT == BOA_ACT_GELU) {
         float below, density;
         normal<FINE>(z, below, density);
         y = z * below;
-    } else if (act == BOA_ACT_GELU_TANH) {
+    } else if constexpr (ACT == BOA_ACT_GELU_TANH) {
         y = z * sigmoid<FINE>(2.0f * SQRT_2_PI * z * fmaf(CUBE * z, z, 1.0f));   // (1 + tanh u) / 2 = sigmoid(2 u)
     } else {
         return z;
@@ -84,26 +84,44 @@ __device__ inline float act_of(float z, int32_t act)
     return z == -INFINITY ? 0.0f : y;
 }
 
-template <bool FINE>
-__device__ inline float slope_of(float z, int32_t act)
+template <bool FINE, int ACT>
+__device__ inline float slope_of(float z)
 {
     float s, far;
-    if (act == BOA_ACT_RELU) {
+    if constexpr (ACT == BOA_ACT_RELU) {
         return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
-    } else if (act == BOA_ACT_SILU) {
+    } else if constexpr (ACT == BOA_ACT_SILU) {
         const float g = sigmoid<FINE>(z);
         s = fmaf(z * g, 1.0f - g, g), far = 100.0f;
-    } else if (act == BOA_ACT_GELU) {
+    } else if constexpr (ACT == BOA_ACT_GELU) {
         float below, density;
         normal<FINE>(z, below, density);
         s = fmaf(z, density, below), far = 20.0f;
-    } else if (act == BOA_ACT_GELU_TANH) {
+    } else if constexpr (ACT == BOA_ACT_GELU_TANH) {
         const float g = sigmoid<FINE>(2.0f * SQRT_2_PI * z * fmaf(CUBE * z, z, 1.0f));
         s = fmaf(z * g * (1.0f - g), 2.0f * SQRT_2_PI * fmaf(3.0f * CUBE * z, z, 1.0f), g), far = 20.0f;
     } else {
         return 1.0f;
     }
     return fabsf(z) > far ? (z > 0.0f ? 1.0f : 0.0f) : s;
+}
+
+// Calls f with the activation as a constant: one branch for many values.
+template <int N>
+struct Act {
+    static constexpr int value = N;
+};
+
+template <class F>
+__device__ inline void with_act(int32_t act, F f)
+{
+    switch (act) {
+    case BOA_ACT_RELU: f(Act<BOA_ACT_RELU>{}); break;
+    case BOA_ACT_SILU: f(Act<BOA_ACT_SILU>{}); break;
+    case BOA_ACT_GELU: f(Act<BOA_ACT_GELU>{}); break;
+    case BOA_ACT_GELU_TANH: f(Act<BOA_ACT_GELU_TANH>{}); break;
+    default: f(Act<BOA_ACT_NONE>{});
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -127,89 +145,97 @@ struct Epilogue {
 // Power of two that brings magnitudes of up to m below 2^15.
 __device__ inline int up(float m) { return 15 - __builtin_amdgcn_frexp_expf(m); }
 
-// N neighbouring values of a row, at column q (the row has them all)
-template <class TO, int N>
-__device__ inline void finish(const Epilogue &e, int64_t p, int32_t q, float (&v)[N])
+template <class TO>
+__device__ inline float bias_at(const Epilogue &e, int32_t q)
+{
+    return !e.bias ? 0.0f : e.bias_f32 ? ((const float *)e.bias)[q] : (float)((const TO *)e.bias)[q];
+}
+
+// What eight neighbouring columns have for all rows, where the rows have them all.
+template <class TO>
+struct Columns {
+    float bias[8];
+    int shift[sizeof(TO) == 4 ? 8 : 1];
+};
+
+template <class TO>
+__device__ inline Columns<TO> columns_at(const Epilogue &e, int32_t q)
 {
     constexpr bool WIDE = sizeof(TO) == 4;
-    if (e.bias) {
-        float t[N];
-        if constexpr (N == 8) {
-            if (e.bias_f32) load_loose<8, float>(t, (const float *)e.bias + q);
-            else load_loose<8, TO>(t, (const TO *)e.bias + q);
-        } else {
+    Columns<TO> c;
+    const bool whole = q + 8 <= e.cols;
+    if (!e.bias) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) t[i] = e.bias_f32 ? ((const float *)e.bias)[q + i] : (float)((const TO *)e.bias)[q + i];
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += t[i];
+        for (int i = 0; i < 8; ++i) c.bias[i] = 0.0f;
+    } else if (whole && (e.bias_f32 || WIDE)) {
+        load_loose<8, float>(c.bias, (const float *)e.bias + q);
+    } else if (whole) {
+        if constexpr (!WIDE) load_loose<8, TO>(c.bias, (const TO *)e.bias + q);
     }
-    if (e.pre) {
-        if constexpr (WIDE) {
+    if constexpr (WIDE) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) ((float *)e.pre)[p * e.cols + q + i] = v[i];
-        } else if constexpr (N == 8) {
-            Pack<8, f16_t> k;
-#pragma unroll
-            for (int i = 0; i < N; ++i) k.v[i] = (f16_t)v[i];
-            *(loose4 *)((f16_t *)e.pre + p * e.cols + q) = __builtin_bit_cast(words4, k);
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) ((f16_t *)e.pre)[p * e.cols + q + i] = (f16_t)v[i];
-        }
+        for (int i = 0; i < 8; ++i) c.shift[i] = e.max_b && q + i < e.cols ? up(e.max_b[q + i]) : 0;
     }
-    if (e.act != BOA_ACT_NONE) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = act_of<WIDE>(v[i], e.act);
-    }
-    TO *out = (TO *)e.out + p * e.ld + q;
-    if (e.residual) {
-        const TO *r = (const TO *)e.residual + p * e.residual_ld + q;
-        float t[N];
-        if constexpr (N == 8) {
-            load_loose<8, TO>(t, r);
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) t[i] = (float)r[i];
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += t[i];
-    }
-    if constexpr (N == 8 && WIDE) {
-        store_loose<4, TO>(out, *(float(*)[4])v);
-        store_loose<4, TO>(out + 4, *(float(*)[4])(v + 4));
-    } else if constexpr (N == 8) {
-        store_loose<8, TO>(out, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) out[i] = (TO)v[i];
-    }
+    return c;
+}
+
+// One value, at row p and column q.
+template <class TO, int ACT>
+__device__ inline void finish_one(const Epilogue &e, int64_t p, int32_t q, float v, float bias)
+{
+    typedef std::conditional_t<sizeof(TO) == 4, float, f16_t> Z;
+    v += bias;
+    if (e.pre) ((Z *)e.pre)[p * e.cols + q] = (Z)v;
+    v = act_of<sizeof(TO) == 4, ACT>(v);
+    if (e.residual) v += (float)((const TO *)e.residual)[p * e.residual_ld + q];
+    ((TO *)e.out)[p * e.ld + q] = (TO)v;
 }
 
 // Eight sums from column q on, of which the row may have fewer.
-template <class TO>
-__device__ inline void finish_run(const Epilogue &e, int64_t p, int32_t q, const float *sums)
+template <class TO, int ACT>
+__device__ inline void finish_run(const Epilogue &e, int64_t p, int32_t q, const float *sums, const Columns<TO> &c)
 {
-    const int s = e.max_a ? up(e.max_a[p]) : 0;
-    if (q + 8 <= e.cols) {
-        float v[8];
-        load_f32<4, float>(*(float(*)[4])v, sums);
-        load_f32<4, float>(*(float(*)[4])(v + 4), sums + 4);
-        if (e.max_a) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = ldexpf(v[i], -(s + up(e.max_b[q + i])));
-        }
-        finish<TO, 8>(e, p, q, v);
-    } else {
+    constexpr bool WIDE = sizeof(TO) == 4;
+    typedef std::conditional_t<WIDE, float, f16_t> Z;
+    const int s = WIDE && e.max_a ? up(e.max_a[p]) : 0;
+    if (q + 8 > e.cols) {
 #pragma unroll 1
         for (int i = 0; q + i < e.cols; ++i) {
-            float v[1] = {sums[i]};
-            if (e.max_a) v[0] = ldexpf(v[0], -(s + up(e.max_b[q + i])));
-            finish<TO, 1>(e, p, q + i, v);
+            float v = sums[i];
+            if constexpr (WIDE) v = ldexpf(v, e.max_a ? -(s + up(e.max_b[q + i])) : 0);
+            finish_one<TO, ACT>(e, p, q + i, v, bias_at<TO>(e, q + i));
         }
+        return;
     }
+    float v[8], r[8];
+    if (e.residual) load_loose<8, TO>(r, (const TO *)e.residual + p * e.residual_ld + q);
+    load_f32<4, float>(*(float(*)[4])v, sums);
+    load_f32<4, float>(*(float(*)[4])(v + 4), sums + 4);
+    auto store = [&](auto *to) {
+        typedef std::remove_reference_t<decltype(*to)> E;
+        if constexpr (WIDE) {
+            store_loose<4, E>(to, *(float(*)[4])v);
+            store_loose<4, E>(to + 4, *(float(*)[4])(v + 4));
+        } else {
+            store_loose<8, E>(to, v);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (WIDE) v[i] = ldexpf(v[i], -(s + c.shift[i]));
+        v[i] += c.bias[i];
+    }
+    if (e.pre) store((Z *)e.pre + p * e.cols + q);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = act_of<WIDE, ACT>(v[i]);
+    if (e.residual) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += r[i];
+    }
+    store((TO *)e.out + p * e.ld + q);
 }
 
+// A forward product (both operands along k) has the whole epilogue, the gradients' none.
 template <class S, bool ACROSS_A, bool ACROSS_B, class TO>
 __global__ __launch_bounds__(S::THREADS, S::PER_CU * S::THREADS / 256) void product_kernel(Product pr, Epilogue e)
 {
@@ -220,7 +246,7 @@ __global__ __launch_bounds__(S::THREADS, S::PER_CU * S::THREADS / 256) void prod
     tile_product<S, ACROSS_A, ACROSS_B>(pr, w, (typename S::T *)lds, acc);
     if (e.partial) {
         float *out = e.partial + w.split * e.partial_split;
-        each_run<S>(w, acc, lds, [&](int32_t p, int32_t q, const float *v) {
+        each_run<S>(w, acc, lds, [](int32_t) { return 0; }, [&](int32_t p, int32_t q, const float *v, int) {
             if (p >= e.rows || q >= e.cols) return;
             float *to = out + p * e.partial_ld + q;
             *(f32x4 *)to = *(const f32x4 *)v;
@@ -228,9 +254,14 @@ __global__ __launch_bounds__(S::THREADS, S::PER_CU * S::THREADS / 256) void prod
         });
         return;
     }
-    each_run<S>(w, acc, lds, [&](int32_t p, int32_t q, const float *v) {
-        if (p < e.rows && q < e.cols) finish_run<TO>(e, p, q, v);
-    });
+    auto all = [&](auto act) {
+        each_run<S>(w, acc, lds, [&](int32_t q) { return columns_at<TO>(e, q); },
+            [&](int32_t p, int32_t q, const float *v, const Columns<TO> &c) {
+                if (p < e.rows && q < e.cols) finish_run<TO, decltype(act)::value>(e, p, q, v, c);
+            });
+    };
+    if constexpr (ACROSS_A || ACROSS_B) all(Act<BOA_ACT_NONE>{});
+    else with_act(e.act, all);
 }
 
 // The sum of the splits' shares, in their order.
@@ -252,7 +283,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(Epilogue e, int32_t s
     float *mine = sums + threadIdx.x * 8;
     *(f32x4 *)mine = v0;
     *(f32x4 *)(mine + 4) = v1;
-    finish_run<TO>(e, p, q, mine);
+    with_act(e.act, [&](auto act) { finish_run<TO, decltype(act)::value>(e, p, q, mine, columns_at<TO>(e, q)); });
 }
 
 // ---------------------------------------------------------------------------
@@ -408,10 +439,11 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
                     x[e] = a.act && c + e < a.N ? (float)z[e] : 0.0f;
                 }
             }
-            if (a.act) {
+            if (a.act)
+                with_act(a.act, [&](auto act) {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) g[e] *= slope_of<sizeof(T) == 4>(x[e], a.act);
-            }
+                    for (int e = 0; e < VEC; ++e) g[e] *= slope_of<sizeof(T) == 4, decltype(act)::value>(x[e]);
+                });
 #pragma unroll
             for (int e = 0; e < VEC; ++e) s[e] += g[e];
             if (a.dz) {   // rows have room for whole runs
@@ -529,11 +561,14 @@ __global__ __launch_bounds__(1024) void few_kernel(FewArgs a)
     for (int j = 0; j < MT; ++j) *(f32x4 *)(sums + ((wave * MT + j) * 16 + r) * 16 + part * 4) = acc[j];
     __syncthreads();
     if (threadIdx.x < MT * 256) {
-        float v[1] = {0.0f};
+        float v = 0.0f;
 #pragma unroll
-        for (int k = 0; k < WAVES; ++k) v[0] += sums[k * MT * 256 + threadIdx.x];
+        for (int k = 0; k < WAVES; ++k) v += sums[k * MT * 256 + threadIdx.x];
         const int32_t m = threadIdx.x >> 4, n = n0 + (threadIdx.x & 15);
-        if (m < a.M && n < a.N) finish<T, 1>(a.e, m, n, v);
+        if (m < a.M && n < a.N) {
+            const float bias = bias_at<T>(a.e, n);
+            with_act(a.e.act, [&](auto act) { finish_one<T, decltype(act)::value>(a.e, m, n, v, bias); });
+        }
     }
 }
 
@@ -581,11 +616,14 @@ __global__ __launch_bounds__(512) void few_f32_kernel(FewArgs a)
         }
     __syncthreads();
     if (threadIdx.x < MB * ROWS) {
-        float v[1] = {0.0f};
+        float v = 0.0f;
 #pragma unroll
-        for (int k = 0; k < WAVES; ++k) v[0] += sums[k][threadIdx.x];
+        for (int k = 0; k < WAVES; ++k) v += sums[k][threadIdx.x];
         const int32_t m = threadIdx.x / ROWS, n = n0 + threadIdx.x % ROWS;
-        if (m < a.M && n < a.N) finish<float, 1>(a.e, m, n, v);
+        if (m < a.M && n < a.N) {
+            const float bias = bias_at<float>(a.e, n);
+            with_act(a.e.act, [&](auto act) { finish_one<float, decltype(act)::value>(a.e, m, n, v, bias); });
+        }
     }
 }
 
@@ -602,6 +640,7 @@ void launch(Product pr, const Epilogue &e, hipStream_t st)
 {
     pr.tiles_a = (int32_t)ceil_div(pr.a.own, S::BA);
     pr.tiles_b = (int32_t)ceil_div(pr.b.own, S::BB);
+    pr.steps = (int32_t)(ceil_div(ceil_div(pr.K, 64), pr.splits) * (64 / S::BK));
     const auto kernel = product_kernel<S, ACROSS_A, ACROSS_B, TO>;
     if (S::LDS > 64 << 10)   // has to be asked for
         (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
@@ -615,7 +654,6 @@ void product(Operand a, Operand b, int32_t K, int terms, Epilogue e, Arena &mem,
     const Cut cut = choose(a.own, b.own, K, terms, 1, false, true);
     Product pr{};
     pr.a = a, pr.b = b, pr.K = K, pr.terms = terms, pr.batches = 1, pr.splits = cut.splits;
-    pr.steps = (int32_t)ceil_div(ceil_div(K, 64), cut.splits);
     e.rows = a.own, e.cols = b.own;
     if (cut.splits > 1) {
         e.partial_ld = pad8(b.own);

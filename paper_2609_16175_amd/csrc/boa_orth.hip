@@ -163,8 +163,8 @@ __global__ __launch_bounds__(S::THREADS, S::PER_CU * S::THREADS / 256) void step
             if (e.to_parts) was += (float)e.a[at + e.to_parts];
             return k.b * was * (B_UP / A_UP) + k.c * (v * (B_UP / (A_UP * A_UP)));
         };
-        each_run<S>(w, acc, lds,
-            [&](int32_t p, int32_t q, const float *v) {
+        each_run<S>(w, acc, lds, [](int32_t) { return 0; },
+            [&](int32_t p, int32_t q, const float *v, int) {
                 if (p >= e.rows || q >= e.to_ld) return;
                 const int64_t at = base + p * e.to_ld + q;
                 float o[8];
@@ -190,8 +190,8 @@ __global__ __launch_bounds__(S::THREADS, S::PER_CU * S::THREADS / 256) void step
             else if (e.dtype == BOA_T_BF16) ((bf16_t *)e.out)[i] = (bf16_t)v;
             else ((f16_t *)e.out)[i] = (f16_t)v;
         };
-        each_run<S>(w, acc, lds,
-            [&](int32_t p, int32_t q, const float *v) {
+        each_run<S>(w, acc, lds, [](int32_t) { return 0; },
+            [&](int32_t p, int32_t q, const float *v, int) {
                 if (p >= e.rows || q >= e.to_ld) return;
                 const int64_t at = p * e.to_ld + q;
                 float was[8], o[8];
@@ -235,6 +235,7 @@ void launch(Product pr, const StepArgs &e, hipStream_t st)
 {
     pr.tiles_a = (int32_t)ceil_div(pr.a.own, S::BA);
     pr.tiles_b = (int32_t)ceil_div(pr.b.own, S::BB);
+    pr.steps = (int32_t)ceil_div(pr.K, S::BK);
     const int64_t tiles = pr.symmetric ? (int64_t)pr.tiles_b * (pr.tiles_b + 1) / 2 : (int64_t)pr.tiles_a * pr.tiles_b;
     const auto kernel = step_kernel<S, B_ACROSS>;
     if (S::LDS > 64 << 10)   // has to be asked for
@@ -247,7 +248,7 @@ void step(const Operand &a, const Operand &b, int32_t K, int terms, int64_t batc
 {
     Product pr{};
     pr.a = a, pr.b = b, pr.K = K, pr.terms = terms, pr.splits = 1, pr.batches = (int32_t)batches;
-    pr.steps = (int32_t)ceil_div(K, 64), pr.symmetric = !B_ACROSS;
+    pr.symmetric = !B_ACROSS;
     const Cut cut = choose(a.own, b.own, K, terms, batches, !B_ACROSS, false);
     if (cut.shape == 0) launch<Large<f16_t>, B_ACROSS>(pr, e, st);
     else if (cut.shape == 1) launch<Middle<f16_t>, B_ACROSS>(pr, e, st);
