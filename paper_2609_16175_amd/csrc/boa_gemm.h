@@ -59,18 +59,22 @@ struct Product {
     int32_t symmetric; // the output is: tiles with ta <= tb only
 };
 
-// A block's tile: WA x WB waves of TA x TB tiles of 32 x 32, BK values of k a
-// stage, PER_CU blocks of it at once on a CU.
-template <class T_, int WA_, int WB_, int TA_, int TB_, int BK_, int STAGES_, int PER_CU_>
+// A block's tile: WA x WB waves of TA x TB tiles of 32 x 32, 64 values of k a
+// stage; GROUPS such sets of waves, which share k and add their sums at the end;
+// PER_CU blocks of it at once on a CU.
+template <class T_, int WA_, int WB_, int TA_, int TB_, int GROUPS_, int STAGES_, int PER_CU_>
 struct Tile {
     typedef T_ T;
-    static constexpr int WA = WA_, WB = WB_, TA = TA_, TB = TB_, BK = BK_, STAGES = STAGES_, PER_CU = PER_CU_;
-    static constexpr int BA = WA * TA * 32, BB = WB * TB * 32, THREADS = 64 * WA * WB;
-    static_assert(STAGES >= 2 && (BK == 32 || BK == 64), "a stage is read while the next one arrives");
+    static constexpr int WA = WA_, WB = WB_, TA = TA_, TB = TB_, BK = 64, GROUPS = GROUPS_, STAGES = STAGES_, PER_CU = PER_CU_;
+    static constexpr int BA = WA * TA * 32, BB = WB * TB * 32, SET = 64 * WA * WB, THREADS = SET * GROUPS;
+    static constexpr int WAVES_PER_SIMD = PER_CU * THREADS / 256;
+    static_assert(STAGES >= 2, "a stage is read while the next one arrives");
     static constexpr int STAGE = (BA + BB) * BK;   // values
     // columns that a wave turns over at a time at the end, and what that takes
     static constexpr int TURN_COLS = TB % 2 ? 32 : 64, TURN_BYTES = TA * 32 * (TURN_COLS + 4) * 4;
-    static constexpr int LDS = STAGE * STAGES * 2 > WA * WB * TURN_BYTES ? STAGE * STAGES * 2 : WA * WB * TURN_BYTES;
+    static constexpr int ROOM = GROUPS * STAGES * STAGE * 2;
+    static constexpr int LDS = ROOM > WA * WB * TURN_BYTES ? ROOM : WA * WB * TURN_BYTES;
+    static_assert((GROUPS - 1) * BA * BB * 4 <= LDS && LDS * PER_CU <= 160 << 10, "LDS");
 };
 
 constexpr uint32_t NOWHERE = 0x80000000u;   // an offset past every buffer: such loads give zeros
@@ -106,9 +110,9 @@ __device__ inline void load_to_lds(words4 buffer, uint32_t offset, uint32_t to)
 // One operand's side of a stage: where this thread's loads come from, and where
 // its fragments lie.
 //
-// Along k, a stage holds ROWS rows of BK values whose 16-byte chunks are stored
-// in the order chunk ^ (row / 2 & 7), or of four chunks chunk ^ (row / 4 & 3):
-// any 16 rows that follow each other are in all banks; across, BK rows of ROWS values in the order
+// Along k, a stage holds ROWS rows of 64 values whose 16-byte chunks are stored
+// in the order chunk ^ (row / 2 & 7): the same chunk of any 16 rows that follow
+// each other lies in all banks; across, 64 rows of ROWS values in the order
 // chunk ^ (row & 3) * 4, and fragments are read transposed, 64 bytes of four
 // rows by half a wave. Either way what lanes read together spreads over the
 // banks. The permutation is applied to the addresses loaded from, since a load
@@ -118,18 +122,18 @@ template <class S, int ROWS, bool ACROSS>
 struct Side {
     typedef typename S::T T;
     static constexpr int CHUNKS = ACROSS ? ROWS / 8 : S::BK / 8;   // of an LDS row
-    static constexpr int N = ROWS * (S::BK / 8) / S::THREADS;     // loads of a stage
-    static constexpr int PER = S::THREADS / CHUNKS;               // LDS rows of one load of all threads
-    static_assert(N * S::THREADS == ROWS * (S::BK / 8) && PER * CHUNKS == S::THREADS, "whole loads");
-    static_assert(ACROSS ? PER % 4 == 0 || N == 1 : PER % 16 == 0 || N == 1, "one permutation for all of a thread's loads");
+    static constexpr int N = ROWS * (S::BK / 8) / S::SET;         // loads of a stage
+    static constexpr int PER = S::SET / CHUNKS;                   // LDS rows of one load of a set of waves
+    static_assert(N * S::SET == ROWS * (S::BK / 8) && PER * CHUNKS == S::SET, "whole loads");
+    static_assert(ACROSS ? PER % 4 == 0 || N == 1 : PER % 8 == 0, "across, one permutation for all of a thread's loads");
     uint32_t at[N];   // byte offsets from the stage's base
-    int32_t k;        // of load 0 (across: + PER each)
+    int32_t k;        // of load 0
 
-    __device__ static int swap(int row) { return ACROSS ? (ROWS >= 128 ? (row & 3) * 4 : (row & 1) * 4) : CHUNKS == 8 ? (row >> 1) & 7 : (row >> 2) & 3; }
+    __device__ static int swap(int row) { return ACROSS ? (ROWS >= 128 ? (row & 3) * 4 : (row & 1) * 4) : (row >> 1) & 7; }
 
     __device__ Side(const Operand &o, int32_t own0)
     {
-        const int t = threadIdx.x, row = t / CHUNKS, chunk = t % CHUNKS ^ swap(t / CHUNKS);
+        const int t = threadIdx.x % S::SET, row = t / CHUNKS, chunk = t % CHUNKS ^ swap(t / CHUNKS);
         if constexpr (ACROSS) {
             k = row;
 #pragma unroll
@@ -139,18 +143,20 @@ struct Side {
             k = chunk * 8;
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                at[i] = own0 + row + i * PER < o.own ? (uint32_t)(row + i * PER) * (uint32_t)o.ld * 2 + chunk * 16 : NOWHERE;
+                at[i] = own0 + row + i * PER < o.own ? (uint32_t)(row + i * PER) * (uint32_t)o.ld * 2 + k_of(i) * 2 : NOWHERE;
         }
     }
+    // the k of load i within a stage
+    __device__ int k_of(int i) const { return ACROSS ? k + i * PER : k ^ (i * PER / 2 & 7) * 8; }
     // loads a stage from `base`, of which the first k_left values of k count
     __device__ void load(T *to, const T *base, int32_t k_left) const
     {
         const words4 rsrc = buffer_at(base);
-        const uint32_t lds = lds_address(to) + (threadIdx.x >> 6) * 1024;
+        const uint32_t lds = lds_address(to) + (threadIdx.x % S::SET >> 6) * 1024;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const uint32_t off = k + (ACROSS ? i * PER : 0) < k_left ? at[i] : NOWHERE;
-            load_to_lds(rsrc, off, __builtin_amdgcn_readfirstlane(lds + i * S::THREADS * 16));
+            const uint32_t off = k_of(i) < k_left ? at[i] : NOWHERE;
+            load_to_lds(rsrc, off, __builtin_amdgcn_readfirstlane(lds + i * S::SET * 16));
         }
     }
     // where this lane's fragments begin in a stage, in bytes; row0: the wave's first row of the tile
@@ -236,32 +242,40 @@ __device__ inline Place place_of(const Product &pr)
 // instructions. Before the last step of a stage the next one is waited for and
 // the waves meet: all fragments of the stage are in registers then, its place
 // takes the loads of the stage STAGES further on, and that step's instructions
-// cover the meeting and the next stage's first reads.
+// cover the meeting and the next stage's first reads. True for the waves that
+// have the sums.
 template <class S, bool ACROSS_A, bool ACROSS_B>
-__device__ inline void tile_product(const Product &pr, const Place &w, typename S::T *lds, f32x16 (&acc)[S::TB][S::TA])
+__device__ inline bool tile_product(const Product &pr, const Place &w, typename S::T *lds, f32x16 (&acc)[S::TB][S::TA])
 {
     typedef typename S::T T;
     constexpr int STAGES = S::STAGES, BK = S::BK;
     using A = Side<S, S::BA, ACROSS_A>;
     using B = Side<S, S::BB, ACROSS_B>;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wa = wave % S::WA, wb = wave / S::WA;
+    const int set = S::GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / S::SET);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x % S::SET >> 6), wa = wave % S::WA, wb = wave / S::WA;
     const int32_t a0 = w.ta * S::BA, b0 = w.tb * S::BB;
     const A a(pr.a, a0);
     const B b(pr.b, b0);
     const int32_t all = (pr.K + BK - 1) / BK;
-    const int32_t from = w.split * pr.steps, steps = min(pr.steps, all - from), total = steps * pr.terms;
+    const int32_t from = w.split * pr.steps, steps = min(pr.steps, all - from);
+    // stages of this set of waves: [first, last) of all terms' one after the other
+    const int32_t each = (steps * pr.terms + S::GROUPS - 1) / S::GROUPS;
+    const int32_t first = set * each, last = min(steps * pr.terms, first + each);
     const T *pa = (const T *)pr.a.p + w.batch * pr.a.batch + (ACROSS_A ? (int64_t)a0 : a0 * pr.a.ld);
     const T *pb = (const T *)pr.b.p + w.batch * pr.b.batch + (ACROSS_B ? (int64_t)b0 : b0 * pr.b.ld);
-    int32_t term = pr.terms - 1, step = 0, stage = 0;   // of the next load; the last term is a0 b0
+    lds += set * STAGES * S::STAGE;
+    // of the next load; the last term is a0 b0
+    int32_t at = first, term = pr.terms - 1 - first / steps, step = first % steps, stage = 0;
     auto load = [&]() {
         const int32_t k0 = (from + step) * BK;
         const T *at_a = pa + (term == 2 ? pr.a.part : 0) + (ACROSS_A ? k0 * pr.a.ld : (int64_t)k0);
         const T *at_b = pb + (term == 1 ? pr.b.part : 0) + (ACROSS_B ? k0 * pr.b.ld : (int64_t)k0);
-        const int32_t left = term < 0 ? 0 : pr.K - k0;   // past the end zeros, which nothing reads
+        const int32_t left = at < last ? pr.K - k0 : 0;   // past the end zeros
         T *to = lds + stage * S::STAGE;
         a.load(to, at_a, left);
         b.load(to + S::BA * BK, at_b, left);
         if (++stage == STAGES) stage = 0;
+        ++at;
         if (++step == steps) step = 0, --term;
     };
     const uint32_t base = lds_address(lds);
@@ -279,7 +293,7 @@ __device__ inline void tile_product(const Product &pr, const Place &w, typename 
     wait_and_meet<(STAGES - 1) * LOADS>();
     int32_t cur = 0;
     read(0, 0, 0);
-    for (int32_t it = 0; it < total; ++it) {
+    for (int32_t it = 0; it < each; ++it) {
         const int32_t next = cur + 1 == STAGES ? 0 : cur + 1;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
@@ -301,6 +315,38 @@ __device__ inline void tile_product(const Product &pr, const Place &w, typename 
         cur = next;
     }
     wait_and_meet<0>();
+    if constexpr (S::GROUPS > 1) {   // the first set adds the others' sums, in their order
+        f32x4 *sums = (f32x4 *)(lds - set * STAGES * S::STAGE);
+        constexpr int PIECES = S::TA * S::TB * 4;
+        const int t = threadIdx.x % S::SET;
+        if (set) {
+#pragma unroll
+            for (int i = 0; i < S::TB; ++i)
+#pragma unroll
+                for (int j = 0; j < S::TA; ++j)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x16 &v = acc[i][j];
+                        sums[((set - 1) * PIECES + (i * S::TA + j) * 4 + g) * S::SET + t] =
+                            f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+                    }
+        }
+        __syncthreads();
+        if (!set)
+            for (int s = 0; s < S::GROUPS - 1; ++s)
+#pragma unroll
+                for (int i = 0; i < S::TB; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::TA; ++j)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const f32x4 v = sums[(s * PIECES + (i * S::TA + j) * 4 + g) * S::SET + t];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] += v[e];
+                        }
+        __syncthreads();
+    }
+    return set == 0;
 }
 
 template <class S>
@@ -384,44 +430,65 @@ inline int32_t pad8(int64_t n) { return (int32_t)(ceil_div(n, 8) * 8); }
 
 inline uint32_t spread(int64_t items) { return (uint32_t)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, 256), 1 << 14)); }
 
+// The tiles there are: 256 x 256 for large outputs; 128 x 128, two at once on a
+// CU, or one with its loads four stages ahead where a CU gets no second; 64 x 64
+// with two sets of waves, likewise. A smaller tile reads more of LDS for the same
+// products: 1,170, 980 and 620 TFLOP/s where there are tiles enough (k = 4,096).
 template <class T>
-using Large = Tile<T, 4, 2, 2, 4, 64, 2, 1>;
+using Large = Tile<T, 4, 2, 2, 4, 1, 2, 1>;
 template <class T>
-using Middle = Tile<T, 2, 2, 2, 2, 64, 2, 2>;
+using Middle = Tile<T, 2, 2, 2, 2, 1, 2, 2>;
 template <class T>
-using Small = Tile<T, 2, 2, 1, 1, 64, 2, 4>;
+using MiddleAlone = Tile<T, 2, 2, 2, 2, 1, 4, 1>;
+template <class T>
+using Small = Tile<T, 2, 2, 1, 1, 2, 2, 2>;
+template <class T>
+using SmallAlone = Tile<T, 2, 2, 1, 1, 2, 4, 1>;
 
 // How a product is cut into blocks.
 struct Cut {
     int shape, splits;
 };
 
-// The cheapest of three tiles and some numbers of splits by a model of the
+// f with the tile of a shape
+template <class T, class F>
+void with_tile(int shape, F f)
+{
+    if (shape == 0) f(Large<T>{});
+    else if (shape == 1) f(Middle<T>{});
+    else if (shape == 2) f(MiddleAlone<T>{});
+    else if (shape == 3) f(Small<T>{});
+    else f(SmallAlone<T>{});
+}
+
+// The cheapest of the tiles and some numbers of splits by a model of the
 // time: rounds of blocks over the GPU's 256 CUs, each as long as its stages
 // and a beginning and end; splits also write and read their sums. symmetric:
 // only the tiles on one side of the diagonal.
 inline Cut choose(int64_t A, int64_t B, int64_t K, int terms, int64_t batches, bool symmetric, bool may_split)
 {
     struct Cost {
-        int side, at_once;
+        int side, at_once, sets;
         double stage, alone, ends;   // us a stage in a full CU and in a CU of its own, us of beginning and end
     };
-    static const Cost costs[3] = {{256, 1, 1.85, 1.85, 5.0}, {128, 2, 1.07, 0.70, 3.0}, {64, 3, 0.65, 0.35, 2.0}};
+    // measured on outputs of 0.5 to 8 tiles a CU and k of 512 to 4,096
+    static const Cost costs[5] = {{256, 1, 1, 1.75, 1.40, 9.0}, {128, 2, 1, 0.98, 0.62, 6.5}, {128, 1, 1, 0.68, 0.60, 6.0},
+                                  {64, 2, 2, 0.75, 0.60, 5.0}, {64, 1, 2, 0.55, 0.50, 4.5}};
     static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
     const int64_t steps = ceil_div(K, 64);
     Cut best{0, 1};
     double least = 1e30;
-    for (int s = 0; s < 3; ++s)
+    for (int s = 0; s < 5; ++s)
         for (int n : counts) {
             if (n > 1 && (!may_split || n > steps || (double)n * A * B * 4 > 256e6)) break;
             const Cost &c = costs[s];
-            const int64_t each = ceil_div(steps, n), splits = ceil_div(steps, each);
+            const int64_t each = ceil_div(steps, n), splits = ceil_div(steps, each), turns = ceil_div(each * terms, c.sets);
             const double tiles_a = (double)ceil_div(A, c.side), tiles_b = (double)ceil_div(B, c.side);
             const double blocks = (symmetric ? tiles_a * (tiles_a + 1) / 2 : tiles_a * tiles_b) * splits * batches;
             const double room = 256.0 * c.at_once;
             const double full = (double)(int64_t)(blocks / room), rest = blocks - full * room;
-            double t = full * (each * terms * c.stage + c.ends);
-            if (rest > 0) t += each * terms * std::max(c.alone, c.stage * std::min(1.0, (double)ceil_div((int64_t)rest, 256) / c.at_once)) + c.ends;
+            double t = full * (turns * c.stage + c.ends);
+            if (rest > 0) t += turns * std::max(c.alone, c.stage * std::min(1.0, (double)ceil_div((int64_t)rest, 256) / c.at_once)) + c.ends;
             if (splits > 1) t += 4.0 + (double)splits * A * B * 8 / 4e6;
             if (t < least) least = t, best = {s, (int)splits};
         }

@@ -237,13 +237,13 @@ __device__ inline void finish_run(const Epilogue &e, int64_t p, int32_t q, const
 
 // A forward product (both operands along k) has the whole epilogue, the gradients' none.
 template <class S, bool ACROSS_A, bool ACROSS_B, class TO>
-__global__ __launch_bounds__(S::THREADS, S::PER_CU * S::THREADS / 256) void product_kernel(Product pr, Epilogue e)
+__global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void product_kernel(Product pr, Epilogue e)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const Place w = place_of(pr);
     f32x16 acc[S::TB][S::TA];
     clear<S>(acc);
-    tile_product<S, ACROSS_A, ACROSS_B>(pr, w, (typename S::T *)lds, acc);
+    if (!tile_product<S, ACROSS_A, ACROSS_B>(pr, w, (typename S::T *)lds, acc)) return;
     if (e.partial) {
         float *out = e.partial + w.split * e.partial_split;
         each_run<S>(w, acc, lds, [](int32_t) { return 0; }, [&](int32_t p, int32_t q, const float *v, int) {
@@ -640,7 +640,6 @@ void launch(Product pr, const Epilogue &e, hipStream_t st)
 {
     pr.tiles_a = (int32_t)ceil_div(pr.a.own, S::BA);
     pr.tiles_b = (int32_t)ceil_div(pr.b.own, S::BB);
-    pr.steps = (int32_t)(ceil_div(ceil_div(pr.K, 64), pr.splits) * (64 / S::BK));
     const auto kernel = product_kernel<S, ACROSS_A, ACROSS_B, TO>;
     if (S::LDS > 64 << 10)   // has to be asked for
         (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
@@ -654,6 +653,7 @@ void product(Operand a, Operand b, int32_t K, int terms, Epilogue e, Arena &mem,
     const Cut cut = choose(a.own, b.own, K, terms, 1, false, true);
     Product pr{};
     pr.a = a, pr.b = b, pr.K = K, pr.terms = terms, pr.batches = 1, pr.splits = cut.splits;
+    pr.steps = (int32_t)ceil_div(ceil_div(K, 64), cut.splits);
     e.rows = a.own, e.cols = b.own;
     if (cut.splits > 1) {
         e.partial_ld = pad8(b.own);
@@ -661,9 +661,7 @@ void product(Operand a, Operand b, int32_t K, int terms, Epilogue e, Arena &mem,
         e.partial = (float *)mem.take(e.partial_split * cut.splits * 4);
     }
     if (!run) return;
-    if (cut.shape == 0) launch<Large<T>, ACROSS_A, ACROSS_B, TO>(pr, e, st);
-    else if (cut.shape == 1) launch<Middle<T>, ACROSS_A, ACROSS_B, TO>(pr, e, st);
-    else launch<Small<T>, ACROSS_A, ACROSS_B, TO>(pr, e, st);
+    with_tile<T>(cut.shape, [&](auto tile) { launch<decltype(tile), ACROSS_A, ACROSS_B, TO>(pr, e, st); });
     if (cut.splits > 1)
         product_join_kernel<TO><<<dim3((uint32_t)ceil_div(e.partial_ld / 8 * a.own, 256)), 256, 0, st>>>(e, cut.splits);
 }

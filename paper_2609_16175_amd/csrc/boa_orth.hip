@@ -26,7 +26,7 @@ using namespace boa;
 
 namespace {
 
-constexpr int SUM_BLOCKS = 64;   // per matrix, at most
+constexpr int SUM_BLOCKS = 256;   // per matrix, at most
 // f16 copies hold X 2^10, A 2^10, (b A + c A^2) 2^8: values from 2^-24 of that to 64, 64, 255
 constexpr float X_UP = 1024.0f, A_UP = 1024.0f, B_UP = 256.0f;
 
@@ -55,13 +55,25 @@ __global__ __launch_bounds__(256) void square_kernel(PrepArgs a)
 {
     __shared__ double part[4];
     const T *g = (const T *)a.g + blockIdx.y * a.batch;
-    const int64_t n = (int64_t)a.rows * a.cols;
+    const int32_t runs = (a.cols + 7) / 8;
     double s = 0.0;
-    // neighbouring threads take neighbouring columns
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const double v = (double)(float)g[i / a.cols * a.ld + i % a.cols];
-        s = fma(v, v, s);
-    }
+    // a group of threads per row, as wide as the row has runs of eight, up to the block
+    int32_t wide = 256;
+    while (wide > 8 && wide / 2 >= runs) wide /= 2;
+    const int32_t mine = threadIdx.x % wide, group = threadIdx.x / wide, groups = 256 / wide;
+    for (int64_t r = (int64_t)blockIdx.x * groups + group; r < a.rows; r += (int64_t)gridDim.x * groups)
+        for (int32_t c = mine * 8; c < a.cols; c += wide * 8) {
+            const T *from = g + r * a.ld + c;
+            float v[8];
+            if (c + 8 <= a.cols) {
+                load_loose<8, T>(v, from);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = c + e < a.cols ? (float)from[e] : 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = fma((double)v[e], (double)v[e], s);
+        }
 #pragma unroll
     for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
@@ -91,7 +103,12 @@ __global__ __launch_bounds__(256) void prep_kernel(PrepArgs a)
     __shared__ double total;
     const int32_t z = blockIdx.z;
     if (threadIdx.x < 64) {
-        double s = (int32_t)threadIdx.x < a.sum_blocks ? a.sums[(int64_t)z * SUM_BLOCKS + threadIdx.x] : 0.0;
+        double s = 0.0;
+#pragma unroll
+        for (int k = 0; k < SUM_BLOCKS / 64; ++k) {
+            const int32_t i = k * 64 + (int32_t)threadIdx.x;
+            s += i < a.sum_blocks ? a.sums[(int64_t)z * SUM_BLOCKS + i] : 0.0;
+        }
 #pragma unroll
         for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
         if (threadIdx.x == 0) total = sqrt(s);
@@ -147,13 +164,13 @@ struct StepArgs {
 
 // tile_product and what becomes of it. B_ACROSS: X, whose rows are k.
 template <class S, bool B_ACROSS>
-__global__ __launch_bounds__(S::THREADS, S::PER_CU * S::THREADS / 256) void step_kernel(Product pr, StepArgs e)
+__global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Product pr, StepArgs e)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const Place w = place_of(pr);
     f32x16 acc[S::TB][S::TA];
     clear<S>(acc);
-    tile_product<S, false, B_ACROSS>(pr, w, (f16_t *)lds, acc);
+    if (!tile_product<S, false, B_ACROSS>(pr, w, (f16_t *)lds, acc)) return;
     const Step k = e.first ? e.first[w.batch] : e.step;
     const int64_t base = w.batch * e.to_size;
     if constexpr (!B_ACROSS) {
@@ -235,7 +252,6 @@ void launch(Product pr, const StepArgs &e, hipStream_t st)
 {
     pr.tiles_a = (int32_t)ceil_div(pr.a.own, S::BA);
     pr.tiles_b = (int32_t)ceil_div(pr.b.own, S::BB);
-    pr.steps = (int32_t)ceil_div(pr.K, S::BK);
     const int64_t tiles = pr.symmetric ? (int64_t)pr.tiles_b * (pr.tiles_b + 1) / 2 : (int64_t)pr.tiles_a * pr.tiles_b;
     const auto kernel = step_kernel<S, B_ACROSS>;
     if (S::LDS > 64 << 10)   // has to be asked for
@@ -248,11 +264,9 @@ void step(const Operand &a, const Operand &b, int32_t K, int terms, int64_t batc
 {
     Product pr{};
     pr.a = a, pr.b = b, pr.K = K, pr.terms = terms, pr.splits = 1, pr.batches = (int32_t)batches;
-    pr.symmetric = !B_ACROSS;
+    pr.steps = (int32_t)ceil_div(K, 64), pr.symmetric = !B_ACROSS;
     const Cut cut = choose(a.own, b.own, K, terms, batches, !B_ACROSS, false);
-    if (cut.shape == 0) launch<Large<f16_t>, B_ACROSS>(pr, e, st);
-    else if (cut.shape == 1) launch<Middle<f16_t>, B_ACROSS>(pr, e, st);
-    else launch<Small<f16_t>, B_ACROSS>(pr, e, st);
+    with_tile<f16_t>(cut.shape, [&](auto tile) { launch<decltype(tile), B_ACROSS>(pr, e, st); });
 }
 
 int check(const boa_orth *d)
@@ -295,7 +309,7 @@ void orthogonalize(const boa_orth &d, Arena &mem, bool run, hipStream_t st)
     p.g = d.update, p.ld = d.rows > 1 ? d.update_stride : d.cols, p.batch = d.update_batch, p.rows = d.rows, p.cols = d.cols;
     p.turned = turned, p.m = m, p.n = n, p.x_ld = x_ld, p.x_size = x_size, p.parts = parts == 2 ? C * x_size : 0;
     p.x = x, p.x16 = x16[0], p.sums = sums, p.eps = d.eps, p.first = first, p.step0 = coefficients(0);
-    p.sum_blocks = (int32_t)std::min<int64_t>(SUM_BLOCKS, ceil_div((int64_t)d.rows * d.cols, 4096));
+    p.sum_blocks = (int32_t)std::min<int64_t>(SUM_BLOCKS, ceil_div((int64_t)d.rows * d.cols, 8192));
     const dim3 squares((uint32_t)p.sum_blocks, (uint32_t)C), tiles((uint32_t)ceil_div(x_ld, 64), (uint32_t)ceil_div(m, 64), (uint32_t)C);
     auto prepare = [&](auto t) {
         using T = decltype(t);
