@@ -11,14 +11,15 @@
 //   dg = dH u    du = dH g    df = the same step back through the first norm
 //
 // and sums over rows: dw = dy hn, db = dy, dpw = du fn, dpb = du, dg of a shared
-// gate.
+// gate. With a shared gate the last three come of two: S = sum dH fn and
+// s = sum dH give dpw = g S, dpb = g s, dg = pw S + pb s.
 //
 // Both are bound by memory. Forward reads x and f (and a gate per value) and
 // writes h and y; backward reads x, f, dh and dy and writes dx and df: h is
 // formed again from x and f in float32, which costs what reading it would and
-// keeps the digits that its rounding loses. A row stays in registers, as in boa_norm.hip: a
-// wave holds up to 1,024 values, a block 4,096, and every thread at most 16
-// columns, so that the five column sums stay in registers too, over all rows
+// keeps the digits that its rounding loses. A row stays in registers, as in
+// boa_norm.hip: a wave holds up to 512 values, two waves 1,024, four 4,096, so that a
+// thread has 8 columns in most cases and 16 at most, so that the column sums stay in registers too, over all rows
 // of a block; they leave one partial row each per block, added in block order.
 #include <algorithm>
 
@@ -29,8 +30,11 @@ using namespace boa;
 namespace {
 
 constexpr int THREADS = ROW_THREADS;
-constexpr int SUMS = 5;   // over rows: dw, db, dpw, dpb, dg
-constexpr int64_t MAX_BLOCKS = 512;
+constexpr int SUMS = 4;   // over rows: dy hn, dy; t fn, t for t = dH, or du where every value has its gate
+constexpr int64_t MAX_BLOCKS = 1024;
+
+// Threads of a block whose rows take TPR of them each.
+constexpr int threads_of(int tpr) { return tpr < 128 ? THREADS : tpr; }
 
 struct BlockArgs {
     const void *x, *f, *gate, *pw, *pb, *w, *b, *dh, *dy;
@@ -104,13 +108,13 @@ __device__ inline void row_stats(float (&v)[NV][VEC], int lane, int32_t d, bool 
 }
 
 template <class T, class P, int NV, int TPR, bool WHOLE>
-__global__ __launch_bounds__(THREADS) void block_kernel(BlockArgs a)
+__global__ __launch_bounds__(threads_of(TPR)) void block_kernel(BlockArgs a)
 {
     constexpr int VEC = 16 / sizeof(T);
     __shared__ float red[8];
     const int lane = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
-    if (row >= a.rows) return;   // a whole wave (TPR 64) or block (TPR 256) leaves
+    const int64_t row = (int64_t)blockIdx.x * (threads_of(TPR) / TPR) + threadIdx.x / TPR;
+    if (row >= a.rows) return;   // a whole wave (TPR 64) or block leaves
     const int32_t d = a.d;
     const T *x = (const T *)a.x + row * a.x_ld, *f = (const T *)a.f + row * a.f_ld;
     float v[NV][VEC], h[NV][VEC];
@@ -183,15 +187,83 @@ __device__ inline void store_mine(T *row, const Cols<VEC, TPR> &at, const float 
     }
 }
 
-// DP: column sums are wanted.
-template <class T, class P, int NV, int TPR, bool WHOLE, bool DP>
-__global__ __launch_bounds__(THREADS) void block_back_kernel(BlockArgs a)
+// A row's values at a thread's columns, as they come from memory.
+template <class T, int NV>
+struct RawRow {
+    words4 f[NV], x[NV], dh[NV], dy[NV], gate[NV];
+    float stats[4];
+};
+
+template <class T, int VEC>
+__device__ inline void unpack(float (&to)[VEC], words4 w)
 {
-    constexpr int VEC = 16 / sizeof(T), GROUPS = THREADS / TPR;
+    typedef Pack<VEC, T> PV;
+    const PV p = __builtin_bit_cast(PV, w);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) to[j] = (float)p.v[j];
+}
+
+// DP: column sums are wanted. The next row is on its way while a row is worked
+// on, and the parameters of waves with a row each lie in LDS as float32: asked
+// for from memory they would wait for that row (65,536 rows of 1,024 bfloat16 values:
+// 419 us with the row and the parameters loaded where they are needed, and registers for one wave a SIMD).
+template <class T, int NV>
+constexpr bool ROW_AHEAD = NV * 16 / sizeof(T) <= 8;   // with more columns a thread it would not fit the registers
+
+// LDS that the four parameter vectors take, each thread's columns for itself.
+template <class T, int NV, int TPR>
+constexpr int PARAM_FLOATS = 4 * NV * 16 / (int)sizeof(T) * TPR;
+
+template <class T, class P, int NV, int TPR, bool WHOLE, bool DP>
+__global__ __launch_bounds__(threads_of(TPR), (ROW_AHEAD<T, NV> ? 2 : 1)) void block_back_kernel(BlockArgs a)
+{
+    constexpr int VEC = 16 / sizeof(T), BLOCK = threads_of(TPR), GROUPS = BLOCK / TPR;
+    constexpr bool AHEAD = ROW_AHEAD<T, NV>;
+    constexpr bool IN_LDS = PARAM_FLOATS<T, NV, TPR> <= 8192;
     __shared__ float red[8];
-    extern __shared__ float cols[];   // SUMS x d, where several rows share a block
+    extern __shared__ __attribute__((aligned(16))) float cols[];   // parameters; at the end, where rows share a block, SUMS x d sums
     const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const int32_t d = a.d;
+    if constexpr (IN_LDS) {
+        if (group == 0) {
+            const void *of[4] = {a.w, a.pw, a.pb, a.gate_rows ? nullptr : a.gate};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    float v[VEC];
+                    params<P, VEC>(v, of[k], Cols<VEC, TPR>(i, lane, d).c, k == 2 ? 0.0f : 1.0f);
+#pragma unroll
+                    for (int q = 0; q < VEC; q += 4)
+                        store_f32<4, float>(cols + (((k * NV + i) * VEC + q) * TPR + lane * 4), *(float(*)[4])(v + q));
+                }
+        }
+        __syncthreads();
+    }
+    enum { W, PW, PB, G };
+    auto param = [&](float (&to)[VEC], int which, int i, int c) {
+        if constexpr (IN_LDS) {   // a thread's own, 16 bytes a lane side by side
+#pragma unroll
+            for (int q = 0; q < VEC; q += 4)
+                load_f32<4, float>(*(float(*)[4])(to + q), cols + (((which * NV + i) * VEC + q) * TPR + lane * 4));
+        } else {
+            params<P, VEC>(to, which == W ? a.w : which == PW ? a.pw : which == PB ? a.pb : a.gate, c, which == PB ? 0.0f : 1.0f);
+        }
+    };
+    auto load = [&](RawRow<T, NV> &to, int64_t row) {
+        auto raw = [](const void *p, int64_t at) { return (words4) * (const loose4 *)((const T *)p + at); };
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = Cols<VEC, TPR>(i, lane, d).c;
+            to.f[i] = raw(a.f, row * a.f_ld + c);
+            to.x[i] = raw(a.x, row * a.x_ld + c);
+            to.dh[i] = a.dh ? raw(a.dh, row * a.dh_ld + c) : words4{0, 0, 0, 0};
+            to.dy[i] = a.dy ? raw(a.dy, row * a.dy_ld + c) : words4{0, 0, 0, 0};
+            if (a.gate_rows) to.gate[i] = raw(a.gate, row * a.gate_ld + c);
+        }
+        to.stats[0] = a.post ? a.stats[row] : 0.0f, to.stats[1] = a.post ? a.stats[a.stats_rows + row] : 1.0f;
+        to.stats[2] = a.dy ? a.stats[2 * a.stats_rows + row] : 0.0f, to.stats[3] = a.dy ? a.stats[3 * a.stats_rows + row] : 0.0f;
+    };
     float sums[SUMS][NV][VEC];
 #pragma unroll
     for (int k = 0; k < SUMS; ++k)
@@ -199,47 +271,69 @@ __global__ __launch_bounds__(THREADS) void block_back_kernel(BlockArgs a)
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) sums[k][i][j] = 0.0f;
-    for (int64_t row = (int64_t)blockIdx.x * GROUPS + group; row < a.rows; row += (int64_t)gridDim.x * GROUPS) {
-        float fn[NV][VEC], hn[NV][VEC], dH[NV][VEC], g1[NV][VEC];
+    const int64_t stride = (int64_t)gridDim.x * GROUPS;
+    int64_t row = (int64_t)blockIdx.x * GROUPS + group;
+    RawRow<T, NV> next;
+    if (AHEAD && row < a.rows) load(next, row);
+    for (; row < a.rows; row += stride) {
+        if (!AHEAD) load(next, row);
+        // what is needed later stays as it came: float32 would take twice the registers
+        words4 f[NV], dh[NV], dy[NV], gate[NV];
+        float v[NV][VEC];   // x, then hn, then dH, then the gradient of norm(f)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = Cols<VEC, TPR>(i, lane, d).c;
-            load_loose<VEC, T>(fn[i], (const T *)a.f + row * a.f_ld + c);
-            load_loose<VEC, T>(hn[i], (const T *)a.x + row * a.x_ld + c);
-            if (a.dh) load_loose<VEC, T>(dH[i], (const T *)a.dh + row * a.dh_ld + c);
-            if (a.dy) load_loose<VEC, T>(g1[i], (const T *)a.dy + row * a.dy_ld + c);
+            f[i] = next.f[i], dh[i] = next.dh[i], dy[i] = next.dy[i];
+            if (a.gate_rows) gate[i] = next.gate[i];
+            unpack<T, VEC>(v[i], next.x[i]);
         }
-        const float pm = a.post ? a.stats[row] : 0.0f, pr = a.post ? a.stats[a.stats_rows + row] : 1.0f;
-        const float hm = a.dy ? a.stats[2 * a.stats_rows + row] : 0.0f, hr = a.dy ? a.stats[3 * a.stats_rows + row] : 0.0f;
+        const float pm = next.stats[0], pr = next.stats[1], hm = next.stats[2], hr = next.stats[3];
+        // Between the steps nothing is kept that can be read or formed again: parameters from LDS, values as float32.
+        auto forget = [&] {
+            if constexpr (AHEAD) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(f[i]), "+v"(dy[i]) :: "memory");
+            }
+        };
+        forget();
+        if (AHEAD && row + stride < a.rows) load(next, row + stride);
+        auto gate_at = [&](float (&g)[VEC], int i, int c) {
+            if (a.gate_rows) unpack<T, VEC>(g, gate[i]);
+            else param(g, G, i, c);
+        };
+        auto fn_at = [&](float (&fn)[VEC], int i) {
+            unpack<T, VEC>(fn, f[i]);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) fn[j] = (fn[j] - pm) * pr;
+        };
+        // columns that are not this thread's count for nothing in the row's sums
+        auto g1_at = [&](float (&g1)[VEC], const Cols<VEC, TPR> &at, int i) {
+            float w[VEC];
+            param(w, W, i, at.c);
+            unpack<T, VEC>(g1, dy[i]);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) g1[j] = at.template mine<WHOLE>(j) ? g1[j] * w[j] : 0.0f;
+        };
         // h again, its norm, and the gradient through it
         float c1 = 0.0f, c2 = 0.0f;
-        auto gate_at = [&](float (&g)[VEC], int c) {
-            if (a.gate_rows) load_loose<VEC, T>(g, (const T *)a.gate + row * a.gate_ld + c);
-            else params<P, VEC>(g, a.gate, c, 1.0f);
-        };
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const Cols<VEC, TPR> at(i, lane, d);
-            float pw[VEC], pb[VEC], g[VEC], w[VEC];
-            params<P, VEC>(pw, a.pw, at.c, 1.0f);
-            params<P, VEC>(pb, a.pb, at.c, 0.0f);
-            gate_at(g, at.c);
-            params<P, VEC>(w, a.w, at.c, 1.0f);
+            float fn[VEC], pw[VEC], pb[VEC], g[VEC], g1[VEC], t[VEC];
+            fn_at(fn, i);
+            param(pw, PW, i, at.c);
+            param(pb, PB, i, at.c);
+            gate_at(g, i, at.c);
+            g1_at(g1, at, i);
+            unpack<T, VEC>(t, dy[i]);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                fn[i][j] = (fn[i][j] - pm) * pr;
-                const float u = fmaf(fn[i][j], pw[j], pb[j]);
-                hn[i][j] = (fmaf(a.scale, hn[i][j], g[j] * u) - hm) * hr;
-                if (!a.dh) dH[i][j] = 0.0f;
-                if (!a.dy) g1[i][j] = 0.0f;
+                v[i][j] = (fmaf(a.scale, v[i][j], g[j] * fmaf(fn[j], pw[j], pb[j])) - hm) * hr;
                 if (DP) {
-                    sums[0][i][j] = fmaf(g1[i][j], hn[i][j], sums[0][i][j]);
-                    sums[1][i][j] += g1[i][j];
+                    sums[0][i][j] = fmaf(t[j], v[i][j], sums[0][i][j]);
+                    sums[1][i][j] += t[j];
                 }
-                // columns that are not this thread's count for nothing in the row's sums
-                g1[i][j] = at.template mine<WHOLE>(j) ? g1[i][j] * w[j] : 0.0f;
-                c1 += g1[i][j];
-                c2 = fmaf(g1[i][j], hn[i][j], c2);
+                c1 += g1[j];
+                c2 = fmaf(g1[j], v[i][j], c2);
             }
         }
         if (a.dy) {
@@ -247,36 +341,44 @@ __global__ __launch_bounds__(THREADS) void block_back_kernel(BlockArgs a)
             c1 = a.layer ? c1 / (float)d : 0.0f;
             c2 /= (float)d;
         }
+        forget();
         float p1 = 0.0f, p2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const Cols<VEC, TPR> at(i, lane, d);
-            float pw[VEC], pb[VEC], g[VEC], o[VEC];
-            params<P, VEC>(pw, a.pw, at.c, 1.0f);
-            params<P, VEC>(pb, a.pb, at.c, 0.0f);
-            gate_at(g, at.c);
+            float fn[VEC], pw[VEC], g[VEC], g1[VEC], o[VEC];
+            fn_at(fn, i);
+            param(pw, PW, i, at.c);
+            gate_at(g, i, at.c);
+            g1_at(g1, at, i);
+            unpack<T, VEC>(o, dh[i]);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                dH[i][j] = fmaf(hr, g1[i][j] - c1 - hn[i][j] * c2, dH[i][j]);
-                o[j] = a.scale * dH[i][j];
+                v[i][j] = fmaf(hr, g1[j] - c1 - v[i][j] * c2, o[j]);
+                o[j] = a.scale * v[i][j];
             }
             if (a.dx) store_mine<T, VEC, TPR, WHOLE>((T *)a.dx + row * (int64_t)d, at, o);
+            if (a.dgate) {
+                float pb[VEC];
+                param(pb, PB, i, at.c);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) o[j] = v[i][j] * fmaf(fn[j], pw[j], pb[j]);
+                store_mine<T, VEC, TPR, WHOLE>((T *)a.dgate + row * (int64_t)d, at, o);
+            }
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                o[j] = dH[i][j] * fmaf(fn[i][j], pw[j], pb[j]);
-                if (DP) sums[4][i][j] += o[j];
-                dH[i][j] *= g[j];
+                const float du = v[i][j] * g[j], t = a.gate_rows ? du : v[i][j];
                 if (DP) {
-                    sums[2][i][j] = fmaf(dH[i][j], fn[i][j], sums[2][i][j]);
-                    sums[3][i][j] += dH[i][j];
+                    sums[2][i][j] = fmaf(t, fn[j], sums[2][i][j]);
+                    sums[3][i][j] += t;
                 }
-                dH[i][j] = at.template mine<WHOLE>(j) ? dH[i][j] * pw[j] : 0.0f;
-                p1 += dH[i][j];
-                p2 = fmaf(dH[i][j], fn[i][j], p2);
+                v[i][j] = at.template mine<WHOLE>(j) ? du * pw[j] : 0.0f;
+                p1 += v[i][j];
+                p2 = fmaf(v[i][j], fn[j], p2);
             }
-            if (a.dgate) store_mine<T, VEC, TPR, WHOLE>((T *)a.dgate + row * (int64_t)d, at, o);
         }
         if (!a.df) continue;
+        forget();
         if (a.post) {
             row_sum2<TPR>(p1, p2, red);
             p1 = a.layer ? p1 / (float)d : 0.0f;
@@ -287,14 +389,16 @@ __global__ __launch_bounds__(THREADS) void block_back_kernel(BlockArgs a)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const Cols<VEC, TPR> at(i, lane, d);
-            float o[VEC];
+            float fn[VEC];
+            fn_at(fn, i);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) o[j] = pr * (dH[i][j] - p1 - fn[i][j] * p2);
-            store_mine<T, VEC, TPR, WHOLE>((T *)a.df + row * (int64_t)d, at, o);
+            for (int j = 0; j < VEC; ++j) v[i][j] = pr * (v[i][j] - p1 - fn[j] * p2);
+            store_mine<T, VEC, TPR, WHOLE>((T *)a.df + row * (int64_t)d, at, v[i]);
         }
     }
     if constexpr (DP) {
         float *out = a.partial + (int64_t)blockIdx.x * SUMS * d;
+        if (GROUPS > 1) __syncthreads();   // the parameters have been read
         for (int k = 0; k < GROUPS; ++k) {   // the block's waves with a row each, added in order
             if (group == k) {
 #pragma unroll
@@ -314,7 +418,7 @@ __global__ __launch_bounds__(THREADS) void block_back_kernel(BlockArgs a)
             if (GROUPS > 1) __syncthreads();
         }
         if (GROUPS > 1)
-            for (int c = threadIdx.x; c < SUMS * d; c += THREADS) out[c] = cols[c];
+            for (int c = threadIdx.x; c < SUMS * d; c += BLOCK) out[c] = cols[c];
     }
 }
 
@@ -447,67 +551,92 @@ __global__ __launch_bounds__(THREADS) void block_cols_kernel(BlockArgs a)
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         Wide<T, P> w{a, row, 0.0f, 0.0f, 0.0f, 0.0f};
         w.read_stats();
-        const float dy = w.dy(c), dH = w.dH(c, a.back[2 * row], a.back[2 * row + 1]), du = dH * w.gate(c);
+        const float dy = w.dy(c), dH = w.dH(c, a.back[2 * row], a.back[2 * row + 1]), t = a.gate_rows ? dH * w.gate(c) : dH;
         s[0] = fmaf(dy, w.hn(c), s[0]);
         s[1] += dy;
-        s[2] = fmaf(du, w.fn(c), s[2]);
-        s[3] += du;
-        s[4] = fmaf(dH, w.u(c), s[4]);
+        s[2] = fmaf(t, w.fn(c), s[2]);
+        s[3] += t;
     }
 #pragma unroll
     for (int k = 0; k < SUMS; ++k) a.partial[((int64_t)blockIdx.x * SUMS + k) * d + c] = s[k];
 }
 
-// Adds the blocks' partial rows: 16 columns a block and 64 slices of the rows, then the slices in order.
+// Adds the blocks' partial rows: 16 columns a block and 64 slices of the rows,
+// then the slices in order; two of the four sums a block, and what comes of them.
 constexpr int JOIN_COLS = 16, JOIN_SLICES = 64;
 
 template <class P>
 struct JoinArgs {
     const float *partial;
-    P *to[SUMS];
+    const P *gate, *pw, *pb;    // of a shared gate; null: ones, ones, zeros
+    P *dw, *db, *dpw, *dpb, *dgate;
     int32_t blocks, d;
 };
 
 template <class P>
 __global__ __launch_bounds__(JOIN_COLS * JOIN_SLICES) void block_join_kernel(JoinArgs<P> a)
 {
-    __shared__ float part[JOIN_SLICES][JOIN_COLS + 1];
-    const int col = threadIdx.x % JOIN_COLS, slice = threadIdx.x / JOIN_COLS, which = blockIdx.y;
-    P *to = a.to[which];
-    if (!to) return;
+    __shared__ float part[2][JOIN_SLICES][JOIN_COLS + 1];
+    const int col = threadIdx.x % JOIN_COLS, slice = threadIdx.x / JOIN_COLS;
+    const bool first = blockIdx.y == 0;
+    if (first ? !a.dw && !a.db : !a.dpw && !a.dpb && !a.dgate) return;
     const int32_t c = blockIdx.x * JOIN_COLS + col;
-    const float *from = a.partial + (int64_t)which * a.d + c;
-    float s = 0.0f;
+    const float *from = a.partial + (first ? 0 : 2) * (int64_t)a.d + c;
+    float s0 = 0.0f, s1 = 0.0f;
     if (c < a.d)
 #pragma unroll 4
-        for (int i = slice; i < a.blocks; i += JOIN_SLICES) s += from[(int64_t)i * SUMS * a.d];
-    part[slice][col] = s;
+        for (int i = slice; i < a.blocks; i += JOIN_SLICES) {
+            s0 += from[(int64_t)i * SUMS * a.d];
+            s1 += from[(int64_t)i * SUMS * a.d + a.d];
+        }
+    part[0][slice][col] = s0;
+    part[1][slice][col] = s1;
     __syncthreads();
     if (slice == 0 && c < a.d) {
-        s = 0.0f;
+        s0 = s1 = 0.0f;
 #pragma unroll
-        for (int i = 0; i < JOIN_SLICES; ++i) s += part[i][col];
-        to[c] = (P)s;
+        for (int i = 0; i < JOIN_SLICES; ++i) {
+            s0 += part[0][i][col];
+            s1 += part[1][i][col];
+        }
+        if (first) {
+            if (a.dw) a.dw[c] = (P)s0;
+            if (a.db) a.db[c] = (P)s1;
+        } else {
+            const float g = a.gate ? (float)a.gate[c] : 1.0f;
+            if (a.dpw) a.dpw[c] = (P)(g * s0);
+            if (a.dpb) a.dpb[c] = (P)(g * s1);
+            if (a.dgate) a.dgate[c] = (P)fmaf(a.pw ? (float)a.pw[c] : 1.0f, s0, (a.pb ? (float)a.pb[c] : 0.0f) * s1);
+        }
     }
 }
 
-// The registers a row takes: f(NV, TPR, WHOLE) as compile-time constants, at
-// most 16 columns a thread; false where a row does not fit, or is shorter than a load.
-template <int VEC, class F>
+// The registers a row takes: f(NV, TPR, WHOLE) as compile-time constants; false
+// where a row does not fit, or is shorter than a load. Forward, a wave per row up
+// to 4 loads a lane (65,536 rows of 1,024 bfloat16 values: 98 us, two waves a row 117);
+// backward, at most 8 columns a thread up to 2,048 values, 16 beyond.
+template <int VEC, bool FORWARD, class F>
 bool with_shape(int32_t d, F f)
 {
     const int64_t n = ceil_div(d, VEC);
     if (d < VEC || n * VEC > 4096) return false;
     auto whole = [&](auto nv, auto tpr) { d % VEC ? f(nv, tpr, Int<0>{}) : f(nv, tpr, Int<1>{}); };
-    if (n <= 64) whole(Int<1>{}, Int<64>{});
-    else if (n <= 128) whole(Int<2>{}, Int<64>{});
-    else if constexpr (VEC == 4) {
-        if (n <= 192) whole(Int<3>{}, Int<64>{});
+    if constexpr (FORWARD) {
+        if (n <= 64) whole(Int<1>{}, Int<64>{});
+        else if (n <= 128) whole(Int<2>{}, Int<64>{});
         else if (n <= 256) whole(Int<4>{}, Int<64>{});
         else if (n <= 512) whole(Int<2>{}, Int<256>{});
         else whole(Int<4>{}, Int<256>{});
+    } else if constexpr (VEC == 4) {
+        if (n <= 64) whole(Int<1>{}, Int<64>{});
+        else if (n <= 128) whole(Int<2>{}, Int<64>{});
+        else if (n <= 256) whole(Int<2>{}, Int<128>{});
+        else if (n <= 512) whole(Int<2>{}, Int<256>{});
+        else whole(Int<4>{}, Int<256>{});
     } else {
-        if (n <= 256) whole(Int<1>{}, Int<256>{});
+        if (n <= 64) whole(Int<1>{}, Int<64>{});
+        else if (n <= 128) whole(Int<1>{}, Int<128>{});
+        else if (n <= 256) whole(Int<1>{}, Int<256>{});
         else whole(Int<2>{}, Int<256>{});
     }
     return true;
@@ -547,10 +676,10 @@ int check(const char *what, const boa_block *d, bool grad)
 
 int64_t back_blocks(int64_t rows, int32_t d)
 {
-    // As many partial rows as blocks: at most 2 per CU, what the registers let
+    // As many partial rows as blocks: at most 4 per CU, what the registers let
     // run at once; fewer of few rows, and of wide ones 128 MB of them at most.
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(MAX_BLOCKS, ((int64_t)1 << 25) / ((int64_t)SUMS * d)));
-    return std::max<int64_t>(1, std::min(most, ceil_div(rows, 8)));
+    return std::max<int64_t>(1, std::min(most, ceil_div(rows, d <= 512 ? 32 : 8)));   // 4 rows at a time, or one
 }
 
 BlockArgs args_of(const boa_block *b)
@@ -583,10 +712,11 @@ int boa_block_norm(const boa_block *b, void *stream)
         constexpr int VEC = 16 / sizeof(T);
         for (int64_t row = 0; row < b->rows; row += LAUNCH_ROWS) {
             const BlockArgs n = rows_from<T>(a, row);
-            const bool fits = with_shape<VEC>(b->d, [&](auto nv, auto tpr, auto whole) {
+            const bool fits = with_shape<VEC, true>(b->d, [&](auto nv, auto tpr, auto whole) {
                 constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value;
                 constexpr bool WHOLE = decltype(whole)::value;
-                block_kernel<T, P, NV, TPR, WHOLE><<<dim3((uint32_t)ceil_div(n.rows, THREADS / TPR)), THREADS, 0, st>>>(n);
+                block_kernel<T, P, NV, TPR, WHOLE>
+                    <<<dim3((uint32_t)ceil_div(n.rows, threads_of(TPR) / TPR)), threads_of(TPR), 0, st>>>(n);
             });
             if (!fits) block_wide_kernel<T, P><<<dim3((uint32_t)n.rows), THREADS, 0, st>>>(n);
         }
@@ -605,8 +735,7 @@ int boa_block_norm_backward(const boa_block *b, void *stream)
     if (int rc = check("block_norm_backward", b, true)) return rc;
     BlockArgs a = args_of(b);
     a.dx = b->dx, a.df = b->df, a.dgate = a.gate_rows ? b->dgate : nullptr;
-    void *to[SUMS] = {b->dweight, b->dbias, b->dpost_weight, b->dpost_bias, a.gate_rows ? nullptr : b->dgate};
-    const bool sums = std::any_of(to, to + SUMS, [](void *p) { return p != nullptr; });
+    const bool sums = b->dweight || b->dbias || b->dpost_weight || b->dpost_bias || (b->dgate && !a.gate_rows);
     if (!sums && (b->rows == 0 || (!a.dx && !a.df && !a.dgate))) return BOA_OK;
     const int64_t blocks = back_blocks(b->rows, b->d);
     if (sums) a.partial = (float *)b->workspace, a.back = a.partial + blocks * SUMS * b->d;
@@ -615,12 +744,14 @@ int boa_block_norm_backward(const boa_block *b, void *stream)
         using T = decltype(t);
         using P = decltype(p);
         constexpr int VEC = 16 / sizeof(T);
-        const bool fits = with_shape<VEC>(b->d, [&](auto nv, auto tpr, auto whole) {
+        const bool fits = with_shape<VEC, false>(b->d, [&](auto nv, auto tpr, auto whole) {
             constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value;
             constexpr bool WHOLE = decltype(whole)::value;
-            const size_t lds = sums && TPR < THREADS ? (size_t)SUMS * b->d * sizeof(float) : 0;
-            if (sums) block_back_kernel<T, P, NV, TPR, WHOLE, true><<<dim3((uint32_t)blocks), THREADS, lds, st>>>(a);
-            else block_back_kernel<T, P, NV, TPR, WHOLE, false><<<dim3((uint32_t)blocks), THREADS, 0, st>>>(a);
+            constexpr int own = PARAM_FLOATS<T, NV, TPR> <= 8192 ? PARAM_FLOATS<T, NV, TPR> : 0;
+            const size_t lds = sizeof(float) * std::max<size_t>(own, TPR < 128 ? (size_t)SUMS * b->d : 0);
+            const dim3 grid((uint32_t)blocks);
+            if (sums) block_back_kernel<T, P, NV, TPR, WHOLE, true><<<grid, threads_of(TPR), lds, st>>>(a);
+            else block_back_kernel<T, P, NV, TPR, WHOLE, false><<<grid, threads_of(TPR), lds, st>>>(a);
         });
         if (!fits) {
             for (int64_t row = 0; row < b->rows; row += LAUNCH_ROWS) {
@@ -632,8 +763,10 @@ int boa_block_norm_backward(const boa_block *b, void *stream)
         if (sums) {
             JoinArgs<P> j{};
             j.partial = a.partial, j.blocks = (int32_t)blocks, j.d = b->d;
-            for (int k = 0; k < SUMS; ++k) j.to[k] = (P *)to[k];
-            block_join_kernel<P><<<dim3((uint32_t)ceil_div(b->d, JOIN_COLS), SUMS), JOIN_COLS * JOIN_SLICES, 0, st>>>(j);
+            j.gate = a.gate_rows ? nullptr : (const P *)a.gate, j.pw = (const P *)a.pw, j.pb = (const P *)a.pb;
+            j.dw = (P *)b->dweight, j.db = (P *)b->dbias, j.dpw = (P *)b->dpost_weight, j.dpb = (P *)b->dpost_bias;
+            j.dgate = a.gate_rows ? nullptr : (P *)b->dgate;
+            block_join_kernel<P><<<dim3((uint32_t)ceil_div(b->d, JOIN_COLS), 2), JOIN_COLS * JOIN_SLICES, 0, st>>>(j);
         }
         return launch_status("block_norm_backward");
     });

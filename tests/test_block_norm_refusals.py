@@ -59,10 +59,10 @@ def test_nothing_to_do():
 
 def test_workspace_is_bounded():
     ws = ops._lib().boa_block_norm_backward_workspace
-    assert ws(8, 768) == (5 * 768 + 16) * 4 and ws(1 << 20, 1024) == (512 * 5 * 1024 + (2 << 20)) * 4
+    assert ws(8, 768) == (4 * 768 + 16) * 4 and ws(1 << 20, 1024) == (1024 * 4 * 1024 + (2 << 20)) * 4
     for d in (1, 4096, 16_384, 100_000, 1 << 20):
         for rows in (0, 1, 9, 1 << 13, (1 << 31) - 1):
-            assert 0 < ws(rows, d) <= max(5 * d * 4, 1 << 27) + 8 * rows
+            assert 0 < ws(rows, d) <= max(4 * d * 4, 1 << 27) + 8 * rows
 
 
 def test_binding_refuses_host_tensors():
