@@ -528,7 +528,7 @@ int boa_block_norm_backward(const boa_block *b, void *stream);
  * c s^5, the singular vectors stay. A zero update stays zero. X is held in
  * float32, and the results are rounded once; the products' operands are
  * rounded to f16's 11 bits for bfloat16 updates whose rows and cols are 128 or
- * more, to 22 bits for others. A value that is not finite makes its matrix NaN,
+ * more, to 22 bits for others, not at all for the smallest (up to 64 rows or cols). A value that is not finite makes its matrix NaN,
  * and so may steps that let singular values grow beyond 8.
  */
 typedef struct {
@@ -543,7 +543,7 @@ typedef struct {
     void *out;                  /* count x rows x cols, dense */
 } boa_orth;
 
-/* Work memory of one call in bytes; a negative BOA_E* code for invalid arguments. */
+/* Work memory of one call in bytes (none for the smallest); a negative BOA_E* code for invalid arguments. */
 int64_t boa_orthogonalize_workspace(const boa_orth *d);
 
 /* Errors: BOA_EINVAL, BOA_EHIP. */

@@ -94,6 +94,23 @@ __device__ inline void write16(f16_t *to, int64_t parts, const float (&v)[8])
     if (parts) *(f16x8 *)(to + parts) = lo;
 }
 
+// The power of two that brings |G| = total into [1, 2), and the first step's
+// coefficients for G times it in place of G / (|G| + eps).
+struct First {
+    int up;
+    Step step;
+};
+
+__device__ inline First first_step(double total, float eps, const Step &s)
+{
+    First f;
+    f.up = total > 0.0 && total < INFINITY ? 1 - __builtin_amdgcn_frexp_exp(total) : 0;
+    const double by = total < INFINITY ? 1.0 / ldexp(total + (double)eps, f.up) : NAN, b3 = by * by * by;
+    // |G| = 0 and eps = 0: X is 0, not NaN
+    f.step = total == 0.0 ? Step{0.0f, 0.0f, 0.0f} : Step{(float)(s.a * by), (float)(s.b * b3), (float)(s.c * b3 * by * by)};
+    return f;
+}
+
 // X of the first step: G times the power of two that brings |G| into [1, 2), as
 // float32 and f16, in tiles of 64 x 64; and that step's coefficients.
 template <class T>
@@ -122,14 +139,9 @@ __global__ __launch_bounds__(256) void prep_kernel(PrepArgs a)
         else tile[r][c] = v;
     }
     __syncthreads();
-    int up = 0;
-    if (total > 0.0 && total < INFINITY) up = 1 - __builtin_amdgcn_frexp_exp(total);
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
-        const double by = total < INFINITY ? 1.0 / ldexp(total + (double)a.eps, up) : NAN, b3 = by * by * by;
-        // |G| = 0 and eps = 0: X is 0, not NaN
-        const bool none = total == 0.0;
-        a.first[z] = none ? Step{0.0f, 0.0f, 0.0f} : Step{(float)(a.step0.a * by), (float)(a.step0.b * b3), (float)(a.step0.c * b3 * by * by)};
-    }
+    const First first = first_step(total, a.eps, a.step0);
+    const int up = first.up;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.first[z] = first.step;
     const int32_t p0 = blockIdx.y * 64, q0 = blockIdx.x * 64;
     for (int i = threadIdx.x; i < 64 * 8; i += 256) {
         const int p = i >> 3, q = (i & 7) * 8;
@@ -245,6 +257,113 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Pro
 }
 
 // ---------------------------------------------------------------------------
+// small matrices: a block does all steps on one, in LDS and in float32
+
+constexpr int SMALL_WAVES = 16, SMALL_TILES = 8;   // tiles of X a wave may have
+constexpr int SMALL_LDS = 150 << 10;
+
+struct SmallArgs {
+    const void *g;
+    int64_t ld, batch;
+    void *out;
+    int32_t rows, cols, turned, m, n, m_pad, n_pad, steps;   // pads: multiples of 16
+    float eps;
+    Step step[BOA_MAX_ORTH_STEPS];
+};
+
+// LDS rows are 4 values longer than their tiles, so that 16 rows x 4 values read together lie in all banks.
+inline int64_t small_bytes(int32_t m_pad, int32_t n_pad)
+{
+    return ((int64_t)m_pad * (n_pad + 4) + 2 * (int64_t)m_pad * (m_pad + 4)) * 4;
+}
+
+// Products by float32 matrix instructions, a 16 x 16 tile a wave at a time.
+// X (m x n), A and B = b A + c A^2 (m x m) stay in LDS; every wave holds its tiles of the new
+// X until all have read the old one. 32 x 96: 5 steps in 17 us, of which 15
+// launches of the large kernels took 90.
+template <class T>
+__global__ __launch_bounds__(64 * SMALL_WAVES) void small_kernel(SmallArgs s)
+{
+    extern __shared__ __attribute__((aligned(16))) float x[];
+    __shared__ double part[SMALL_WAVES];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+    const int xl = s.n_pad + 4, al = s.m_pad + 4, mt = s.m_pad / 16, nt = s.n_pad / 16;
+    float *a = x + s.m_pad * xl, *b = a + s.m_pad * al;
+    const T *g = (const T *)s.g + blockIdx.x * s.batch;
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < s.m_pad * s.n_pad; i += 64 * SMALL_WAVES) {
+        const int row = s.turned ? i % s.m_pad : i / s.n_pad, col = s.turned ? i / s.m_pad : i % s.n_pad;
+        const bool in = row < s.m && col < s.n;
+        const float v = !in ? 0.0f : (float)(s.turned ? g[col * s.ld + row] : g[row * s.ld + col]);
+        x[row * xl + col] = v;
+        sum = fma((double)v, (double)v, sum);
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < SMALL_WAVES; ++i) sum += part[i];
+    const First first = first_step(sqrt(sum), s.eps, s.step[0]);
+    for (int i = threadIdx.x; i < s.m_pad * s.n_pad; i += 64 * SMALL_WAVES) {
+        float *v = x + i / s.n_pad * xl + i % s.n_pad;
+        *v = ldexpf(*v, first.up);
+    }
+    __syncthreads();
+    // sum over k of a row of `u` times a row, or `down` a column, of `v`
+    auto product = [&](const float *u, int ul, int ti, const float *v, int vl, int tj, int K, bool down) {
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+        const float *pu = u + (ti * 16 + r) * ul + q, *pv = down ? v + q * vl + tj * 16 + r : v + (tj * 16 + r) * vl + q;
+        const int step = down ? 4 * vl : 4;
+#pragma unroll 4
+        for (int k = 0; k < K; k += 4) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(pu[k], pv[k / 4 * step], acc, 0, 0, 0);
+        return acc;
+    };
+    for (int it = 0; it < s.steps; ++it) {
+        const Step k = it ? s.step[it] : first.step;
+        for (int t = wave; t < mt * mt; t += SMALL_WAVES) {   // both of two mirrored tiles: their roundings are the same
+            const f32x4 v = product(x, xl, t / mt, x, xl, t % mt, s.n_pad, false);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[(t / mt * 16 + 4 * q + e) * al + t % mt * 16 + r] = v[e];
+        }
+        __syncthreads();
+        for (int t = wave; t < mt * mt; t += SMALL_WAVES) {
+            const f32x4 v = product(a, al, t / mt, a, al, t % mt, s.m_pad, false);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at = (t / mt * 16 + 4 * q + e) * al + t % mt * 16 + r;
+                b[at] = fmaf(k.b, a[at], k.c * v[e]);
+            }
+        }
+        __syncthreads();
+        f32x4 now[SMALL_TILES];
+#pragma unroll
+        for (int u = 0; u < SMALL_TILES; ++u) {
+            const int t = wave + u * SMALL_WAVES;
+            if (t < mt * nt) now[u] = product(b, al, t / nt, x, xl, t % nt, s.m_pad, true);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < SMALL_TILES; ++u) {
+            const int t = wave + u * SMALL_WAVES;
+            if (t < mt * nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float *v = x + (t / nt * 16 + 4 * q + e) * xl + t % nt * 16 + r;
+                    *v = fmaf(k.a, *v, now[u][e]);
+                }
+        }
+        __syncthreads();
+    }
+    T *out = (T *)s.out + (int64_t)blockIdx.x * s.rows * s.cols;
+    for (int i = threadIdx.x; i < s.rows * s.cols; i += 64 * SMALL_WAVES) {
+        const int row = i / s.cols, col = i % s.cols;
+        out[i] = (T)(s.turned ? x[col * xl + row] : x[row * xl + col]);
+    }
+}
+
+// ---------------------------------------------------------------------------
 // host
 
 template <class S, bool B_ACROSS>
@@ -294,6 +413,27 @@ void orthogonalize(const boa_orth &d, Arena &mem, bool run, hipStream_t st)
 {
     const bool turned = d.rows > d.cols;
     const int32_t m = turned ? d.cols : d.rows, n = turned ? d.rows : d.cols;
+    auto coefficients = [&](int i) { return Step{d.coefficients[3 * i], d.coefficients[3 * i + 1], d.coefficients[3 * i + 2]}; };
+    const int32_t m_pad = (m + 15) / 16 * 16, n_pad = (n + 15) / 16 * 16;
+    if (m_pad <= 64 && m_pad * n_pad <= 256 * SMALL_WAVES * SMALL_TILES && small_bytes(m_pad, n_pad) <= SMALL_LDS) {
+        if (!run) return;
+        SmallArgs s{};
+        s.g = d.update, s.ld = d.rows > 1 ? d.update_stride : d.cols, s.batch = d.update_batch, s.out = d.out;
+        s.rows = d.rows, s.cols = d.cols, s.turned = turned, s.m = m, s.n = n, s.m_pad = m_pad, s.n_pad = n_pad;
+        s.steps = d.steps, s.eps = d.eps;
+        for (int i = 0; i < d.steps; ++i) s.step[i] = coefficients(i);
+        const size_t lds = (size_t)small_bytes(m_pad, n_pad);
+        auto small = [&](auto t) {
+            const auto kernel = small_kernel<decltype(t)>;
+            if (lds > 60 << 10)   // has to be asked for
+                (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, SMALL_LDS);
+            kernel<<<dim3((uint32_t)d.count), 64 * SMALL_WAVES, lds, st>>>(s);
+        };
+        if (d.dtype == BOA_T_F32) small(0.0f);
+        else if (d.dtype == BOA_T_BF16) small(bf16_t{});
+        else small(f16_t{});
+        return;
+    }
     const int32_t parts = d.dtype == BOA_T_BF16 && m >= 128 ? 1 : 2, terms = parts == 1 ? 1 : 3;
     const int32_t x_ld = pad8(n), a_ld = pad8(m);
     const int64_t x_size = (int64_t)m * x_ld, a_size = (int64_t)m * a_ld, C = d.count;
@@ -304,7 +444,6 @@ void orthogonalize(const boa_orth &d, Arena &mem, bool run, hipStream_t st)
     double *sums = (double *)mem.take(C * SUM_BLOCKS * 8);
     Step *first = (Step *)mem.take(C * (int64_t)sizeof(Step));
     if (!run) return;
-    auto coefficients = [&](int i) { return Step{d.coefficients[3 * i], d.coefficients[3 * i + 1], d.coefficients[3 * i + 2]}; };
     PrepArgs p{};
     p.g = d.update, p.ld = d.rows > 1 ? d.update_stride : d.cols, p.batch = d.update_batch, p.rows = d.rows, p.cols = d.cols;
     p.turned = turned, p.m = m, p.n = n, p.x_ld = x_ld, p.x_size = x_size, p.parts = parts == 2 ? C * x_size : 0;
@@ -356,7 +495,8 @@ int boa_orthogonalize(const boa_orth *d, void *workspace, int64_t workspace_byte
 {
     if (int rc = check(d)) return rc;
     if (d->count == 0) return BOA_OK;
-    if (!workspace || !aligned(workspace, 16) || workspace_bytes < boa_orthogonalize_workspace(d))
+    const int64_t need = boa_orthogonalize_workspace(d);
+    if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
         return set_error(BOA_EINVAL, "orthogonalize: workspace missing, unaligned or too small");
     Arena mem;
     mem.base = (char *)workspace;

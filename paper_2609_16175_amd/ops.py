@@ -731,6 +731,6 @@ def orthogonalize(update, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1
     n = _lib().boa_orthogonalize_workspace(C.byref(a))
     if n < 0:
         _check(n)
-    ws = _workspace(update, n)
-    _check(_lib().boa_orthogonalize(C.byref(a), ws.data_ptr(), ws.numel(), _current_stream(update.get_device())))
+    ws = _workspace(update, n) if n else None
+    _check(_lib().boa_orthogonalize(C.byref(a), _ptr(ws), n, _current_stream(update.get_device())))
     return out

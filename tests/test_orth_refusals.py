@@ -49,7 +49,8 @@ def test_workspace():
     # X in float32 and twice in f16, A and b A + c A^2 in f16
     assert need >= 1024 * 4096 * 8 + 1024 * 1024 * 4 and need < 1024 * 4096 * 8 + 1024 * 1024 * 4 + 4096
     for ws, n in ((None, 1 << 40), (P + 8, 1 << 40), (P, 64)):
-        assert L.boa_orthogonalize(C.byref(_orth()), ws, n, None) == EINVAL and "workspace" in _err()
+        assert L.boa_orthogonalize(C.byref(_orth(rows=100, cols=90, update_stride=90)), ws, n, None) == EINVAL and "workspace" in _err()
+    assert L.boa_orthogonalize_workspace(C.byref(_orth())) == 0   # 20 x 30: in one block
     assert L.boa_orthogonalize(C.byref(_orth(count=0, update=None, out=None)), None, 0, None) == 0
     assert L.boa_orthogonalize(None, P, 1, None) == EINVAL
 
