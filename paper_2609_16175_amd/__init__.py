@@ -283,5 +283,6 @@ _OPS = ("layer_norm", "layer_norm_forward", "layer_norm_backward", "softmax_xent
 def __getattr__(name):
     if name in _OPS:
         from . import ops
-        return getattr(ops, name)
+        globals()[name] = getattr(ops, name)   # found here from now on
+        return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -11,6 +11,8 @@ caller's.
 from __future__ import annotations
 
 import ctypes as C
+import struct
+from array import array
 from dataclasses import dataclass
 
 import torch
@@ -56,6 +58,13 @@ class Orth(C.Structure):
                 ("eps", C.c_float), ("out", C.c_void_p)]
 
 
+def _packer(cls):
+    """pack() of a struct's values as bytes, in the order of its fields: a third of the time that filling the struct takes."""
+    code = {C.c_int32: "i", C.c_int64: "q", C.c_float: "f", C.c_void_p: "P"}
+    return struct.Struct("@" + "".join(code[kind] for _, kind in cls._fields_)).pack
+
+
+_pack_dense, _pack_block, _pack_orth = _packer(Dense), _packer(Block), _packer(Orth)
 _ready = None
 
 
@@ -73,17 +82,18 @@ def _lib():
         for f in (L.boa_softmax_xent, L.boa_softmax_xent_grad):
             f.argtypes = [C.POINTER(Xent), P, i64, P]
         L.boa_matvec_fourbit.argtypes = [P, i64, i64, i32, P, i64, i32, i64, P, P, i64, i32, i32, P, i64, P]
-        L.boa_linear_workspace.argtypes = [C.POINTER(Dense), i32]
+        # packed structs: bytes go as void pointers
+        L.boa_linear_workspace.argtypes = [P, i32]
         L.boa_linear_workspace.restype = i64
         for f in (L.boa_linear, L.boa_linear_grad):
-            f.argtypes = [C.POINTER(Dense), P, i64, P]
+            f.argtypes = [P, P, i64, P]
         for f in (L.boa_block_norm, L.boa_block_norm_backward):
-            f.argtypes = [C.POINTER(Block), P]
+            f.argtypes = [P, P]
         L.boa_block_norm_backward_workspace.argtypes = [i64, i32]
         L.boa_block_norm_backward_workspace.restype = i64
-        L.boa_orthogonalize_workspace.argtypes = [C.POINTER(Orth)]
+        L.boa_orthogonalize_workspace.argtypes = [P]
         L.boa_orthogonalize_workspace.restype = i64
-        L.boa_orthogonalize.argtypes = [C.POINTER(Orth), P, i64, P]
+        L.boa_orthogonalize.argtypes = [P, P, i64, P]
         _ready = L
     return _ready
 
@@ -116,12 +126,16 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _address(t):   # for packed structs
+    return 0 if t is None else t.data_ptr()
+
+
 def _device(name, *tensors):
     dev = None
     for t in tensors:
         if t is None:
             continue
-        at = t.get_device() if isinstance(t, torch.Tensor) and t.is_cuda else -1
+        at = t.get_device() if isinstance(t, torch.Tensor) else -1   # -1 for host tensors too
         if at < 0:
             raise ValueError(f"{name}: arguments must be device tensors")
         if dev is not None and at != dev:
@@ -464,15 +478,18 @@ def linear_forward(x, weight, bias=None, residual=None, activation="none", keep=
     M = m.shape[0]
     y = torch.empty(shape, dtype=x.dtype, device=x.device)
     pre = torch.empty(shape, dtype=torch.float32 if dt == T_F32 else torch.float16, device=x.device) if keep and act else None
-    a = Dense(dt, act, M, N, K, m.data_ptr(), _stride(m), w.data_ptr(), _stride(w), _ptr(b), dt if b is None else _DTYPES[b.dtype],
-              _ptr(r), 0 if r is None else _stride(r), y.data_ptr(), _ptr(pre))
-    ws, n = _linear_workspace(x, a, M > (LINEAR_FEW_F32 if dt == T_F32 else LINEAR_FEW), 0)
-    _check(_lib().boa_linear(C.byref(a), _ptr(ws), n, _current_stream(x.get_device())))
+    a = _pack_dense(dt, act, M, N, K, m.data_ptr(), _stride(m), w.data_ptr(), _stride(w), _address(b),
+                    dt if b is None else _DTYPES[b.dtype], _address(r), 0 if r is None else _stride(r), y.data_ptr(), _address(pre),
+                    0, 0, 0, 0, 0)
+    ws, n = _linear_workspace(x, a, 0) if M > (LINEAR_FEW_F32 if dt == T_F32 else LINEAR_FEW) else (None, 0)
+    rc = _lib().boa_linear(a, _ptr(ws), n, _current_stream(x.get_device()))
+    if rc:
+        _check(rc)
     return y, pre
 
 
-def _linear_workspace(x, a, needed, grad):
-    n = _lib().boa_linear_workspace(C.byref(a), grad) if needed else 0
+def _linear_workspace(x, a, grad):
+    n = _lib().boa_linear_workspace(a, grad)
     if n < 0:
         _check(n)
     return (_workspace(x, n), n) if n else (None, 0)
@@ -508,10 +525,10 @@ def linear_backward(dy, x, weight, pre=None, activation="none", need=(True, True
     dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if need[0] else None
     dw = torch.empty((N, K), dtype=x.dtype, device=dev) if need[1] else None
     db = torch.empty((N,), dtype=ptype, device=dev) if need[2] else None
-    a = Dense(dt, act, m.shape[0], N, K, m.data_ptr(), _stride(m), w.data_ptr(), _stride(w), None, _DTYPES[ptype], None, 0, None,
-              _ptr(pre) if act else None, g.data_ptr(), _stride(g), _ptr(dx), _ptr(dw), _ptr(db))
-    ws, n = _linear_workspace(x, a, True, 1)
-    _check(_lib().boa_linear_grad(C.byref(a), _ptr(ws), n, _current_stream(dev.index)))
+    a = _pack_dense(dt, act, m.shape[0], N, K, m.data_ptr(), _stride(m), w.data_ptr(), _stride(w), 0, _DTYPES[ptype], 0, 0, 0,
+                    _address(pre) if act else 0, g.data_ptr(), _stride(g), _address(dx), _address(dw), _address(db))
+    ws, n = _linear_workspace(x, a, 1)
+    _check(_lib().boa_linear_grad(a, _ptr(ws), n, _current_stream(dev.index)))
     return dx, dw, db
 
 
@@ -537,7 +554,8 @@ class _Linear(torch.autograd.Function):
 
 def linear(x, weight, bias=None, residual=None, activation="none"):
     """linear_forward's y, for autograd."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias, residual)):
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
+                                    or residual is not None and residual.requires_grad):
         return _Linear.apply(x, weight, bias, residual, activation)
     return linear_forward(x, weight, bias, residual, activation)[0]
 
@@ -546,6 +564,7 @@ def linear(x, weight, bias=None, residual=None, activation="none"):
 # the norms around a residual block
 
 _NORMS = {"layer": 0, "rms": 1}
+_NO_GRADIENTS = (0,) * 13   # the rest of a Block in the forward pass
 
 
 @dataclass
@@ -588,10 +607,11 @@ def _block(name, x, f, gate, post, pre, post_weight, post_bias, weight, bias, no
     ptype = x.dtype if ptype is None else ptype
     xm, fm = _rows(x), _rows(f)
     gm = None if gate is None else _rows(gate) if gate_rows else _dense(gate)
-    keep = (xm, fm, gm, *(_dense(p) for p in (post_weight, post_bias, weight, bias)))
-    a = Block(dt, _DTYPES[ptype], xm.shape[0], d, _NORMS[norm], post, pre, gate_rows, scale, eps, xm.data_ptr(), _stride(xm),
-              fm.data_ptr(), _stride(fm), _ptr(gm), _stride(gm) if gate_rows else 0, *(_ptr(p) for p in keep[3:]))
-    return a, keep, ptype
+    w = _dense(post_weight), _dense(post_bias), _dense(weight), _dense(bias)
+    head = (dt, _DTYPES[ptype], xm.shape[0], d, _NORMS[norm], post, pre, gate_rows, scale, eps, xm.data_ptr(), _stride(xm),
+            fm.data_ptr(), _stride(fm), _address(gm), _stride(gm) if gate_rows else 0, _address(w[0]), _address(w[1]), _address(w[2]),
+            _address(w[3]))
+    return head, (xm, fm, gm, w), ptype   # the tensors, which may be copies, have to live until the call
 
 
 def block_norm_forward(x, f, gate=None, scale=1.0, post=False, post_weight=None, post_bias=None, pre=True, weight=None, bias=None,
@@ -612,12 +632,14 @@ def block_norm_forward(x, f, gate=None, scale=1.0, post=False, post_weight=None,
     if other is not None:
         with other:
             return block_norm_forward(x, f, gate, scale, post, post_weight, post_bias, pre, weight, bias, norm, eps)
-    a, keep, _ = _block("block_norm", x, f, gate, post, pre, post_weight, post_bias, weight, bias, norm, scale, eps)
-    h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if pre else None
-    stats = torch.empty((4, a.rows), dtype=torch.float32, device=x.device)
-    a.h, a.y, a.stats = h.data_ptr(), _ptr(y), stats.data_ptr()
-    _check(_lib().boa_block_norm(C.byref(a), _current_stream(x.get_device())))
+    head, keep, _ = _block("block_norm", x, f, gate, post, pre, post_weight, post_bias, weight, bias, norm, scale, eps)
+    h = torch.empty_like(x, memory_format=torch.contiguous_format)
+    y = torch.empty_like(h) if pre else None
+    stats = torch.empty((4, head[2]), dtype=torch.float32, device=x.device)
+    rc = _lib().boa_block_norm(_pack_block(*head, h.data_ptr(), _address(y), stats.data_ptr(), *_NO_GRADIENTS),
+                               _current_stream(x.get_device()))
+    if rc:
+        _check(rc)
     return h, y, stats
 
 
@@ -642,25 +664,22 @@ def block_norm_backward(dh, dy, x, f, stats, gate=None, scale=1.0, post=False, p
         with other:
             return block_norm_backward(dh, dy, x, f, stats, gate, scale, post, post_weight, post_bias, pre, weight, bias, norm,
                                        need_gate, need_params)
-    a, keep, ptype = _block("block_norm_backward", x, f, gate, post, pre, post_weight, post_bias, weight, bias, norm, scale, 0.0)
+    head, keep, ptype = _block("block_norm_backward", x, f, gate, post, pre, post_weight, post_bias, weight, bias, norm, scale, 0.0)
     dhm, dym = None if dh is None else _rows(dh), None if dy is None else _rows(dy)
-    dev, d = x.device, a.d
+    dev, rows, d, gate_rows = x.device, head[2], head[3], head[7]
     r = BlockNormGrads(torch.empty(x.shape, dtype=x.dtype, device=dev), torch.empty(x.shape, dtype=x.dtype, device=dev))
     vector = lambda wanted: torch.empty((d,), dtype=ptype, device=dev) if wanted else None  # noqa: E731
     if gate is not None and need_gate:
-        r.dgate = torch.empty(x.shape, dtype=x.dtype, device=dev) if a.gate_rows else vector(True)
+        r.dgate = torch.empty(x.shape, dtype=x.dtype, device=dev) if gate_rows else vector(True)
     r.dpost_weight, r.dpost_bias, r.dweight, r.dbias = (vector(need_params and p is not None)
                                                         for p in (post_weight, post_bias, weight, bias))
     ws = None
-    if any(t is not None for t in (r.dpost_weight, r.dpost_bias, r.dweight, r.dbias)) or r.dgate is not None and not a.gate_rows:
-        ws = _workspace(x, _lib().boa_block_norm_backward_workspace(a.rows, d))
-    a.stats = stats.data_ptr()
-    a.dh, a.dh_stride = _ptr(dhm), 0 if dhm is None else _stride(dhm)
-    a.dy, a.dy_stride = _ptr(dym), 0 if dym is None else _stride(dym)
-    a.dx, a.df, a.dgate = r.dx.data_ptr(), r.df.data_ptr(), _ptr(r.dgate)
-    a.dpost_weight, a.dpost_bias, a.dweight, a.dbias = _ptr(r.dpost_weight), _ptr(r.dpost_bias), _ptr(r.dweight), _ptr(r.dbias)
-    a.workspace, a.workspace_bytes = _ptr(ws), 0 if ws is None else ws.numel()
-    _check(_lib().boa_block_norm_backward(C.byref(a), _current_stream(dev.index)))
+    if any(t is not None for t in (r.dpost_weight, r.dpost_bias, r.dweight, r.dbias)) or r.dgate is not None and not gate_rows:
+        ws = _workspace(x, _lib().boa_block_norm_backward_workspace(rows, d))
+    a = _pack_block(*head, 0, 0, stats.data_ptr(), _address(dhm), 0 if dhm is None else _stride(dhm), _address(dym),
+                    0 if dym is None else _stride(dym), r.dx.data_ptr(), r.df.data_ptr(), _address(r.dgate), _address(r.dpost_weight),
+                    _address(r.dpost_bias), _address(r.dweight), _address(r.dbias), _address(ws), 0 if ws is None else ws.numel())
+    _check(_lib().boa_block_norm_backward(a, _current_stream(dev.index)))
     return r
 
 
@@ -712,7 +731,7 @@ def orthogonalize(update, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1
     if not 1 <= steps <= 32:
         raise ValueError("orthogonalize: steps must be 1 to 32")
     each = list(coefficients)
-    if len(each) == 3 and not any(hasattr(c, "__len__") for c in each):
+    if len(each) == 3 and not hasattr(each[0], "__len__"):
         each = [each] * steps
     if len(each) != steps or any(len(c) != 3 for c in each):
         raise ValueError("orthogonalize: coefficients must be (a, b, c), or one such triple a step")
@@ -725,12 +744,12 @@ def orthogonalize(update, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1
     if cols > 1 and u.stride(2) != 1 or rows > 1 and u.stride(1) < cols:
         u = u.contiguous()
     out = torch.empty(update.shape, dtype=update.dtype, device=update.device)
-    flat = (C.c_float * (3 * steps))(*(float(v) for c in each for v in c))
-    a = Orth(dt, rows, cols, u.shape[0], u.data_ptr(), u.stride(1) if rows > 1 else cols, u.stride(0), steps, C.addressof(flat), eps,
-             out.data_ptr())
-    n = _lib().boa_orthogonalize_workspace(C.byref(a))
+    flat = array("f", [v for c in each for v in c])
+    a = _pack_orth(dt, rows, cols, u.shape[0], u.data_ptr(), u.stride(1) if rows > 1 else cols, u.stride(0), steps,
+                   flat.buffer_info()[0], eps, out.data_ptr())
+    n = _lib().boa_orthogonalize_workspace(a)
     if n < 0:
         _check(n)
     ws = _workspace(update, n) if n else None
-    _check(_lib().boa_orthogonalize(C.byref(a), _ptr(ws), n, _current_stream(update.get_device())))
+    _check(_lib().boa_orthogonalize(a, _ptr(ws), n, _current_stream(update.get_device())))
     return out
