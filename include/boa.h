@@ -517,7 +517,7 @@ int64_t boa_block_norm_backward_workspace(int64_t rows, int32_t d);
 
 int boa_block_norm_backward(const boa_block *b, void *stream);
 
-#define BOA_MAX_ORTH (1 << 15)
+#define BOA_MAX_ORTH (1 << 14)
 #define BOA_MAX_ORTH_COUNT 65535
 #define BOA_MAX_ORTH_STEPS 32
 /*

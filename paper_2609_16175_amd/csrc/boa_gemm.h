@@ -4,7 +4,8 @@
 // An operand's rows run along k, or "across": a row is then one k and runs
 // along the operand's own dimension. A linear layer's forward product has both
 // along k, its input's gradient the weights across, its weights' gradient both.
-// Float32 operands come as two f16 parts (parts below), and three products.
+// Float32 operands come as two f16 parts, a = a0 + a1, and the products of parts
+// above 2^-22 of the result are added: a1 b0 + a0 b1 + a0 b0.
 #pragma once
 
 #include <algorithm>
@@ -40,22 +41,21 @@ __device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_a
 __device__ inline f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 // One operand: rows `ld` values apart from a 16-byte aligned address, ld a
-// multiple of 8 and below 2^21, whole 16-byte chunks in every row. `own`: its extent in the
-// output. part: values from one part to the next. batch: from one product of a
-// batch to the next.
+// multiple of 8 and below 2^21, whole 16-byte chunks in every row. Of parts, the second lies `part` values
+// behind the first, and 32 values of k lie `block` values from the next 32 (along
+// k: 32 where the parts are two matrices, 64 where they alternate). own: the operand's extent in the output.
+// batch: from one product of a batch to the next.
 struct Operand {
     const void *p;
-    int64_t ld, part, batch;
+    int64_t ld, part, block, batch;
     int32_t own;
 };
 
-// The products that parts give: the ones above 2^-22 of the result, smallest first.
 struct Product {
     Operand a, b;
-    int32_t K;         // of each part
-    int32_t terms;     // 1, or 3 of two parts: a1 b0, a0 b1, a0 b0
+    int32_t K;
     int32_t tiles_a, tiles_b, splits, batches;
-    int32_t steps;     // of k a split takes
+    int32_t steps;     // stages of k a split takes
     int32_t symmetric; // the output is: tiles with ta <= tb only
 };
 
@@ -108,7 +108,8 @@ __device__ inline void load_to_lds(words4 buffer, uint32_t offset, uint32_t to)
 }
 
 // One operand's side of a stage: where this thread's loads come from, and where
-// its fragments lie.
+// its fragments lie. A stage is 64 values of k, or 32 of the first part and the
+// same 32 of the second behind them.
 //
 // Along k, a stage holds ROWS rows of 64 values whose 16-byte chunks are stored
 // in the order chunk ^ (row / 2 & 7): the same chunk of any 16 rows that follow
@@ -118,7 +119,7 @@ __device__ inline void load_to_lds(words4 buffer, uint32_t offset, uint32_t to)
 // banks. The permutation is applied to the addresses loaded from, since a load
 // to LDS writes its lanes in order. Rows past the operand's end and k past K are
 // loaded as zeros (an offset that the buffer's bounds check refuses).
-template <class S, int ROWS, bool ACROSS>
+template <class S, int ROWS, bool ACROSS, bool PARTS>
 struct Side {
     typedef typename S::T T;
     static constexpr int CHUNKS = ACROSS ? ROWS / 8 : S::BK / 8;   // of an LDS row
@@ -127,7 +128,7 @@ struct Side {
     static_assert(N * S::SET == ROWS * (S::BK / 8) && PER * CHUNKS == S::SET, "whole loads");
     static_assert(ACROSS ? PER % 4 == 0 || N == 1 : PER % 8 == 0, "across, one permutation for all of a thread's loads");
     uint32_t at[N];   // byte offsets from the stage's base
-    int32_t k;        // of load 0
+    int32_t k;        // place of load 0
 
     __device__ static int swap(int row) { return ACROSS ? (ROWS >= 128 ? (row & 3) * 4 : (row & 1) * 4) : (row >> 1) & 7; }
 
@@ -137,17 +138,23 @@ struct Side {
         if constexpr (ACROSS) {
             k = row;
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                at[i] = own0 + chunk * 8 < o.own ? (uint32_t)(row + i * PER) * (uint32_t)o.ld * 2 + chunk * 16 : NOWHERE;
+            for (int i = 0; i < N; ++i) {
+                const uint32_t from = (uint32_t)k_of(i) * (uint32_t)o.ld * 2 + (second(i) ? (uint32_t)o.part * 2 : 0);
+                at[i] = own0 + chunk * 8 < o.own ? from + chunk * 16 : NOWHERE;
+            }
         } else {
             k = chunk * 8;
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                at[i] = own0 + row + i * PER < o.own ? (uint32_t)(row + i * PER) * (uint32_t)o.ld * 2 + k_of(i) * 2 : NOWHERE;
+            for (int i = 0; i < N; ++i) {
+                const uint32_t from = (uint32_t)(row + i * PER) * (uint32_t)o.ld * 2 + (second(i) ? (uint32_t)o.part * 2 : 0);
+                at[i] = own0 + row + i * PER < o.own ? from + k_of(i) * 2 : NOWHERE;
+            }
         }
     }
-    // the k of load i within a stage
-    __device__ int k_of(int i) const { return ACROSS ? k + i * PER : k ^ (i * PER / 2 & 7) * 8; }
+    // the place of load i among a stage's 64 rows or values, its k, and whether it is of the second part
+    __device__ int place(int i) const { return ACROSS ? k + i * PER : k ^ (i * PER / 2 & 7) * 8; }
+    __device__ int k_of(int i) const { return PARTS ? place(i) & 31 : place(i); }
+    __device__ bool second(int i) const { return PARTS && place(i) >= 32; }
     // loads a stage from `base`, of which the first k_left values of k count
     __device__ void load(T *to, const T *base, int32_t k_left) const
     {
@@ -244,73 +251,83 @@ __device__ inline Place place_of(const Product &pr)
 // takes the loads of the stage STAGES further on, and that step's instructions
 // cover the meeting and the next stage's first reads. True for the waves that
 // have the sums.
-template <class S, bool ACROSS_A, bool ACROSS_B>
+template <class S, bool ACROSS_A, bool ACROSS_B, bool PARTS>
 __device__ inline bool tile_product(const Product &pr, const Place &w, typename S::T *lds, f32x16 (&acc)[S::TB][S::TA])
 {
     typedef typename S::T T;
     constexpr int STAGES = S::STAGES, BK = S::BK;
-    using A = Side<S, S::BA, ACROSS_A>;
-    using B = Side<S, S::BB, ACROSS_B>;
+    using A = Side<S, S::BA, ACROSS_A, PARTS>;
+    using B = Side<S, S::BB, ACROSS_B, PARTS>;
+    constexpr int DEEP = PARTS ? 32 : BK;   // k of a stage
     const int set = S::GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / S::SET);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x % S::SET >> 6), wa = wave % S::WA, wb = wave / S::WA;
     const int32_t a0 = w.ta * S::BA, b0 = w.tb * S::BB;
     const A a(pr.a, a0);
     const B b(pr.b, b0);
-    const int32_t all = (pr.K + BK - 1) / BK;
+    const int32_t all = (pr.K + DEEP - 1) / DEEP;
     const int32_t from = w.split * pr.steps, steps = min(pr.steps, all - from);
-    // stages of this set of waves: [first, last) of all terms' one after the other
-    const int32_t each = (steps * pr.terms + S::GROUPS - 1) / S::GROUPS;
-    const int32_t first = set * each, last = min(steps * pr.terms, first + each);
+    const int32_t each = (steps + S::GROUPS - 1) / S::GROUPS;   // stages of a set of waves
+    const int32_t last = from + min(steps, (set + 1) * each);
     const T *pa = (const T *)pr.a.p + w.batch * pr.a.batch + (ACROSS_A ? (int64_t)a0 : a0 * pr.a.ld);
     const T *pb = (const T *)pr.b.p + w.batch * pr.b.batch + (ACROSS_B ? (int64_t)b0 : b0 * pr.b.ld);
+    const int64_t next_a = PARTS ? pr.a.block : ACROSS_A ? BK * pr.a.ld : BK, next_b = PARTS ? pr.b.block : ACROSS_B ? BK * pr.b.ld : BK;
     lds += set * STAGES * S::STAGE;
-    // of the next load; the last term is a0 b0
-    int32_t at = first, term = pr.terms - 1 - first / steps, step = first % steps, stage = 0;
+    int32_t at = from + set * each, stage = 0;   // of the next load
     auto load = [&]() {
-        const int32_t k0 = (from + step) * BK;
-        const T *at_a = pa + (term == 2 ? pr.a.part : 0) + (ACROSS_A ? k0 * pr.a.ld : (int64_t)k0);
-        const T *at_b = pb + (term == 1 ? pr.b.part : 0) + (ACROSS_B ? k0 * pr.b.ld : (int64_t)k0);
-        const int32_t left = at < last ? pr.K - k0 : 0;   // past the end zeros
+        const int32_t left = at < last ? pr.K - at * DEEP : 0;   // past the end zeros
         T *to = lds + stage * S::STAGE;
-        a.load(to, at_a, left);
-        b.load(to + S::BA * BK, at_b, left);
+        a.load(to, pa + at * next_a, left);
+        b.load(to + S::BA * BK, pb + at * next_b, left);
         if (++stage == STAGES) stage = 0;
         ++at;
-        if (++step == steps) step = 0, --term;
     };
     const uint32_t base = lds_address(lds);
     const uint32_t lane_a = A::lane_at(wa * S::TA * 32), lane_b = B::lane_at(wb * S::TB * 32) + S::BA * BK * 2;
-    typename Vec<T>::v8 fa[2][S::TA], fb[2][S::TB];
+    // A step's fragments: of 16 values of k, or of 16 of both parts. Two steps'
+    // at a time, but for parts in a tile that has no registers left for that.
+    constexpr int P = PARTS ? 2 : 1, STEPS = BK / 16 / P, BUFFERS = PARTS && S::TA * S::TB > 4 ? 1 : 2;
+    typename Vec<T>::v8 fa[BUFFERS][P][S::TA], fb[BUFFERS][P][S::TB];
     auto read = [&](int to, int32_t slot, int s) {
         const uint32_t at_a = base + slot * S::STAGE * 2 + lane_a, at_b = base + slot * S::STAGE * 2 + lane_b;
 #pragma unroll
-        for (int j = 0; j < S::TA; ++j) fa[to][j] = A::fragment(at_a, j, s);
+        for (int q = 0; q < P; ++q) {
 #pragma unroll
-        for (int i = 0; i < S::TB; ++i) fb[to][i] = B::fragment(at_b, i, s);
+            for (int j = 0; j < S::TA; ++j) fa[to][q][j] = A::fragment(at_a, j, s + q * STEPS);
+#pragma unroll
+            for (int i = 0; i < S::TB; ++i) fb[to][q][i] = B::fragment(at_b, i, s + q * STEPS);
+        }
     };
-    constexpr int LOADS = A::N + B::N, STEPS = BK / 16;
+    auto multiply = [&](int from_buffer) {
+        const auto &u = fa[from_buffer];
+        const auto &v = fb[from_buffer];
+#pragma unroll
+        for (int q = P == 2 ? 0 : 2; q < 3; ++q)
+#pragma unroll
+            for (int i = 0; i < S::TB; ++i)
+#pragma unroll
+                for (int j = 0; j < S::TA; ++j) acc[i][j] = mfma32(v[q == 1 ? P - 1 : 0][i], u[q == 0 ? P - 1 : 0][j], acc[i][j]);
+    };
+    constexpr int LOADS = A::N + B::N;
     for (int i = 0; i < STAGES; ++i) load();
     wait_and_meet<(STAGES - 1) * LOADS>();
     int32_t cur = 0;
-    read(0, 0, 0);
+    if (BUFFERS == 2) read(0, 0, 0);
     for (int32_t it = 0; it < each; ++it) {
         const int32_t next = cur + 1 == STAGES ? 0 : cur + 1;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
+            if (BUFFERS == 1) read(0, cur, s);
             if (s + 1 < STEPS) {
-                read((s + 1) & 1, cur, s + 1);
+                if (BUFFERS == 2) read((s + 1) & 1, cur, s + 1);
             } else {
                 wait_and_meet<(STAGES - 2) * LOADS>();
                 load();
-                read(0, next, 0);
+                if (BUFFERS == 2) read(0, next, 0);
             }
             // else the reads would be gathered before the instructions that use them (4096^3: 1,010 in place of 1,170 TFLOP/s);
             // transposed ones are as well off without (1,220 and 1,170)
             if constexpr (!ACROSS_A && !ACROSS_B) __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < S::TB; ++i)
-#pragma unroll
-                for (int j = 0; j < S::TA; ++j) acc[i][j] = mfma32(fb[s & 1][i], fa[s & 1][j], acc[i][j]);
+            multiply(s & (BUFFERS - 1));
         }
         cur = next;
     }
@@ -448,6 +465,7 @@ using SmallAlone = Tile<T, 2, 2, 1, 1, 2, 4, 1>;
 // How a product is cut into blocks.
 struct Cut {
     int shape, splits;
+    int32_t steps;   // stages of k a split takes
 };
 
 // f with the tile of a shape
@@ -465,7 +483,7 @@ void with_tile(int shape, F f)
 // time: rounds of blocks over the GPU's 256 CUs, each as long as its stages
 // and a beginning and end; splits also write and read their sums. symmetric:
 // only the tiles on one side of the diagonal.
-inline Cut choose(int64_t A, int64_t B, int64_t K, int terms, int64_t batches, bool symmetric, bool may_split)
+inline Cut choose(int64_t A, int64_t B, int64_t K, bool parts, int64_t batches, bool symmetric, bool may_split)
 {
     struct Cost {
         int side, at_once, sets;
@@ -475,22 +493,24 @@ inline Cut choose(int64_t A, int64_t B, int64_t K, int terms, int64_t batches, b
     static const Cost costs[5] = {{256, 1, 1, 1.75, 1.40, 9.0}, {128, 2, 1, 0.98, 0.62, 6.5}, {128, 1, 1, 0.68, 0.60, 6.0},
                                   {64, 2, 2, 0.75, 0.60, 5.0}, {64, 1, 2, 0.55, 0.50, 4.5}};
     static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-    const int64_t steps = ceil_div(K, 64);
-    Cut best{0, 1};
+    const int64_t steps = ceil_div(K, parts ? 32 : 64);
+    const double longer = parts ? 1.25 : 1.0;   // a stage's time: three products of half its values
+    Cut best{0, 1, (int32_t)steps};
     double least = 1e30;
     for (int s = 0; s < 5; ++s)
         for (int n : counts) {
             if (n > 1 && (!may_split || n > steps || (double)n * A * B * 4 > 256e6)) break;
             const Cost &c = costs[s];
-            const int64_t each = ceil_div(steps, n), splits = ceil_div(steps, each), turns = ceil_div(each * terms, c.sets);
+            const int64_t each = ceil_div(steps, n), splits = ceil_div(steps, each), turns = ceil_div(each, c.sets);
             const double tiles_a = (double)ceil_div(A, c.side), tiles_b = (double)ceil_div(B, c.side);
             const double blocks = (symmetric ? tiles_a * (tiles_a + 1) / 2 : tiles_a * tiles_b) * splits * batches;
             const double room = 256.0 * c.at_once;
             const double full = (double)(int64_t)(blocks / room), rest = blocks - full * room;
-            double t = full * (turns * c.stage + c.ends);
-            if (rest > 0) t += turns * std::max(c.alone, c.stage * std::min(1.0, (double)ceil_div((int64_t)rest, 256) / c.at_once)) + c.ends;
+            double t = full * (turns * c.stage * longer + c.ends);
+            if (rest > 0)
+                t += turns * longer * std::max(c.alone, c.stage * std::min(1.0, (double)ceil_div((int64_t)rest, 256) / c.at_once)) + c.ends;
             if (splits > 1) t += 4.0 + (double)splits * A * B * 8 / 4e6;
-            if (t < least) least = t, best = {s, (int)splits};
+            if (t < least) least = t, best = {s, (int)splits, (int32_t)each};
         }
     return best;
 }

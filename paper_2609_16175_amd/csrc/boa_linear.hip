@@ -243,7 +243,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void product_kernel(
     const Place w = place_of(pr);
     f32x16 acc[S::TB][S::TA];
     clear<S>(acc);
-    if (!tile_product<S, ACROSS_A, ACROSS_B>(pr, w, (typename S::T *)lds, acc)) return;
+    if (!tile_product<S, ACROSS_A, ACROSS_B, sizeof(TO) == 4>(pr, w, (typename S::T *)lds, acc)) return;
     if (e.partial) {
         float *out = e.partial + w.split * e.partial_split;
         each_run<S>(w, acc, lds, [](int32_t) { return 0; }, [&](int32_t p, int32_t q, const float *v, int) {
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(Epilogue e, int32_t s
 struct CopyArgs {
     const void *src;
     void *dst;
-    int64_t ld, part, rows;
+    int64_t ld, rows;
     int32_t cols, pad;
     float *most;   // of parts: the largest magnitude per row or column
 };
@@ -345,7 +345,8 @@ __device__ inline void write_parts(const float (&v)[8], const int (&s)[8], f16_t
     *(f16x8 *)(to + part) = lo;
 }
 
-// Parts scaled by row: a wave per row, which it reads twice (the second time from the cache).
+// Parts scaled by row, whose 32 values of the first and of the second part
+// alternate, up to `pad` of each: a wave per row, which it reads twice (the second time from the cache).
 __global__ __launch_bounds__(256) void row_parts_kernel(CopyArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -364,7 +365,7 @@ __global__ __launch_bounds__(256) void row_parts_kernel(CopyArgs a)
         for (int32_t c = lane * 8; c < a.pad; c += 512) {
             float v[8];
             read8(v, from, c, a.cols);
-            write_parts(v, s, (f16_t *)a.dst + r * a.pad + c, a.part);
+            write_parts(v, s, (f16_t *)a.dst + r * 2 * a.pad + c / 32 * 64 + c % 32, 32);
         }
     }
 }
@@ -386,18 +387,19 @@ __global__ __launch_bounds__(256) void col_max_kernel(CopyArgs a)
     atomicMax((uint32_t *)a.most + c, __float_as_uint(m));
 }
 
+// Parts scaled by column: 32 rows of the first part and of the second alternate, with rows of zeros at the end.
 __global__ __launch_bounds__(256) void col_parts_kernel(CopyArgs a)
 {
-    const int64_t chunks = a.pad / 8, n = a.rows * chunks;
+    const int64_t chunks = a.pad / 8, n = (a.rows + 31) / 32 * 32 * chunks;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / chunks;
         const int32_t c = (int32_t)(i % chunks) * 8;
         float v[8];
         int s[8];
-        read8(v, (const float *)a.src + r * a.ld, c, a.cols);
+        read8(v, (const float *)a.src + min(r, a.rows - 1) * a.ld, c, r < a.rows ? a.cols : 0);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e] = c + e < a.cols ? up(a.most[c + e]) : 0;
-        write_parts(v, s, (f16_t *)a.dst + r * a.pad + c, a.part);
+        write_parts(v, s, (f16_t *)a.dst + (r / 32 * 64 + r % 32) * a.pad + c, 32 * (int64_t)a.pad);
     }
 }
 
@@ -648,12 +650,11 @@ void launch(Product pr, const Epilogue &e, hipStream_t st)
 
 // out = a b^T with its epilogue; T: the operands' type in the product, TO: the layer's.
 template <class T, class TO, bool ACROSS_A, bool ACROSS_B>
-void product(Operand a, Operand b, int32_t K, int terms, Epilogue e, Arena &mem, bool run, hipStream_t st)
+void product(Operand a, Operand b, int32_t K, Epilogue e, Arena &mem, bool run, hipStream_t st)
 {
-    const Cut cut = choose(a.own, b.own, K, terms, 1, false, true);
+    const Cut cut = choose(a.own, b.own, K, sizeof(TO) == 4, 1, false, true);
     Product pr{};
-    pr.a = a, pr.b = b, pr.K = K, pr.terms = terms, pr.batches = 1, pr.splits = cut.splits;
-    pr.steps = (int32_t)ceil_div(ceil_div(K, 64), cut.splits);
+    pr.a = a, pr.b = b, pr.K = K, pr.batches = 1, pr.splits = cut.splits, pr.steps = cut.steps;
     e.rows = a.own, e.cols = b.own;
     if (cut.splits > 1) {
         e.partial_ld = pad8(b.own);
@@ -684,27 +685,29 @@ Operand operand(const void *src, int64_t ld, int64_t rows, int32_t cols, bool ac
     return o;
 }
 
-// float32 rows x cols at `src` as two parts, scaled per row, or per column where
-// the operand lies across; *most gets the magnitudes that the scales come from.
-Operand parts(const void *src, int64_t ld, int64_t rows, int32_t cols, bool across, bool by_column, const float **most, Arena &mem,
-              bool run, hipStream_t st)
+// float32 rows x cols at `src` as two parts: along k scaled per row, across per
+// column; *most gets the magnitudes that the scales come from.
+Operand parts(const void *src, int64_t ld, int64_t rows, int32_t cols, bool across, const float **most, Arena &mem, bool run, hipStream_t st)
 {
     CopyArgs c{};
-    c.src = src, c.ld = ld, c.rows = rows, c.cols = cols, c.pad = pad8(cols), c.part = rows * c.pad;
-    c.dst = mem.take(2 * c.part * 2);
-    c.most = (float *)mem.take((by_column ? (int64_t)cols : rows) * 4);
+    c.src = src, c.ld = ld, c.rows = rows, c.cols = cols;
+    c.pad = across ? pad8(cols) : (int32_t)ceil_div(cols, 32) * 32;
+    c.dst = mem.take((across ? ceil_div(rows, 32) * 32 : rows) * 2 * (int64_t)c.pad * 2);
+    c.most = (float *)mem.take((across ? (int64_t)cols : rows) * 4);
     *most = c.most;
     Operand o{};
-    o.own = (int32_t)(across ? cols : rows), o.p = c.dst, o.ld = c.pad, o.part = c.part;
+    o.own = (int32_t)(across ? cols : rows), o.p = c.dst;
+    if (across) o.ld = c.pad, o.part = 32 * (int64_t)c.pad, o.block = 64 * (int64_t)c.pad;
+    else o.ld = 2 * (int64_t)c.pad, o.part = 32, o.block = 64;
     if (!run) return o;
-    if (!by_column) {
+    if (!across) {
         row_parts_kernel<<<dim3((uint32_t)std::min<int64_t>(ceil_div(rows, 4), 1 << 14)), 256, 0, st>>>(c);
         return o;
     }
     zero_kernel<float><<<spread(cols), 256, 0, st>>>(c.most, cols);
-    const int64_t across_blocks = ceil_div(cols, 256), down = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 32), 2048 / across_blocks));
-    col_max_kernel<<<dim3((uint32_t)across_blocks, (uint32_t)down), 256, 0, st>>>(c);
-    col_parts_kernel<<<spread(rows * (c.pad / 8)), 256, 0, st>>>(c);
+    const int64_t strips = ceil_div(cols, 256), down = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 32), 2048 / strips));
+    col_max_kernel<<<dim3((uint32_t)strips, (uint32_t)down), 256, 0, st>>>(c);
+    col_parts_kernel<<<spread(ceil_div(rows, 32) * 32 * (c.pad / 8)), 256, 0, st>>>(c);
     return o;
 }
 
@@ -772,13 +775,13 @@ void forward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
         return;
     }
     if constexpr (WIDE) {
-        const Operand x = parts(d.x, d.x_stride, M, d.K, false, false, &e.max_a, mem, run, st);
-        const Operand w = parts(d.w, d.w_stride, d.N, d.K, false, false, &e.max_b, mem, run, st);
-        product<T, TO, false, false>(x, w, d.K, 3, e, mem, run, st);
+        const Operand x = parts(d.x, d.x_stride, M, d.K, false, &e.max_a, mem, run, st);
+        const Operand w = parts(d.w, d.w_stride, d.N, d.K, false, &e.max_b, mem, run, st);
+        product<T, TO, false, false>(x, w, d.K, e, mem, run, st);
     } else {
         const Operand x = operand<T>(d.x, d.x_stride, M, d.K, false, mem, run, st);
         const Operand w = operand<T>(d.w, d.w_stride, d.N, d.K, false, mem, run, st);
-        product<T, TO, false, false>(x, w, d.K, 1, e, mem, run, st);
+        product<T, TO, false, false>(x, w, d.K, e, mem, run, st);
     }
 }
 
@@ -814,14 +817,14 @@ void backward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
     if (d.dx && M) {
         e.out = d.dx, e.ld = d.K;
         if constexpr (WIDE) {
-            const Operand a = parts(dz, dz_ld, M, d.N, false, false, &e.max_a, mem, run, st);
-            const Operand b = parts(d.w, d.w_stride, d.N, d.K, true, true, &e.max_b, mem, run, st);
-            product<T, TO, false, true>(a, b, d.N, 3, e, mem, run, st);
+            const Operand a = parts(dz, dz_ld, M, d.N, false, &e.max_a, mem, run, st);
+            const Operand b = parts(d.w, d.w_stride, d.N, d.K, true, &e.max_b, mem, run, st);
+            product<T, TO, false, true>(a, b, d.N, e, mem, run, st);
         } else {
             Operand a{};
             a.p = dz, a.ld = M > 1 || s.dz ? dz_ld : s.pad, a.own = M;
             const Operand b = operand<T>(d.w, d.w_stride, d.N, d.K, true, mem, run, st);
-            product<T, TO, false, true>(a, b, d.N, 1, e, mem, run, st);
+            product<T, TO, false, true>(a, b, d.N, e, mem, run, st);
         }
         most = std::max(most, mem.used);
         mem.used = kept;
@@ -832,14 +835,14 @@ void backward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
             const int64_t n = (int64_t)d.N * d.K;
             if (run) zero_kernel<TO><<<spread(n), 256, 0, st>>>((TO *)d.dw, n);
         } else if constexpr (WIDE) {
-            const Operand a = parts(dz, dz_ld, M, d.N, true, true, &e.max_a, mem, run, st);
-            const Operand b = parts(d.x, d.x_stride, M, d.K, true, true, &e.max_b, mem, run, st);
-            product<T, TO, true, true>(a, b, M, 3, e, mem, run, st);
+            const Operand a = parts(dz, dz_ld, M, d.N, true, &e.max_a, mem, run, st);
+            const Operand b = parts(d.x, d.x_stride, M, d.K, true, &e.max_b, mem, run, st);
+            product<T, TO, true, true>(a, b, M, e, mem, run, st);
         } else {
             Operand a{};
             a.p = dz, a.ld = M > 1 || s.dz ? dz_ld : s.pad, a.own = d.N;
             const Operand b = operand<T>(d.x, d.x_stride, M, d.K, true, mem, run, st);
-            product<T, TO, true, true>(a, b, M, 1, e, mem, run, st);
+            product<T, TO, true, true>(a, b, M, e, mem, run, st);
         }
         most = std::max(most, mem.used);
     }

@@ -39,7 +39,7 @@ struct PrepArgs {
     int64_t ld, batch;          // of g
     int32_t rows, cols, turned; // turned: X is g transposed
     int32_t m, n, x_ld;         // of X
-    int64_t x_size, parts;      // values of one X; from part to part (0: one part)
+    int64_t x_size, parts;      // values of one X; the same for copies of two parts (0: one part)
     float *x;
     f16_t *x16;
     double *sums;               // SUM_BLOCKS per matrix
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(256) void prep_kernel(PrepArgs a)
         store_f32<4, float>(a.x + at + 4, *(float(*)[4])(v + 4));
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= X_UP;
-        write16(a.x16 + at, a.parts, v);
+        write16(a.x16 + at + z * a.parts, a.parts, v);   // the parts of a matrix follow each other
     }
 }
 
@@ -163,9 +163,10 @@ enum Kind { GRAM, POLY, UPDATE, LAST };
 struct StepArgs {
     Kind kind;
     f16_t *to;               // GRAM: A; POLY: b A + c A^2; UPDATE: X
-    int64_t to_ld, to_size, to_parts;
+    int64_t to_ld, to_size, to_parts;   // to_size: from matrix to matrix
     const f16_t *a;          // POLY: A, laid out as `to`
     float *x;                // UPDATE: X, in place; LAST: read only
+    int64_t x_size;
     void *out;               // LAST
     int64_t out_ld, out_size;
     int32_t rows, cols;      // that are written (columns of `to` up to its padding)
@@ -175,14 +176,14 @@ struct StepArgs {
 };
 
 // tile_product and what becomes of it. B_ACROSS: X, whose rows are k.
-template <class S, bool B_ACROSS>
+template <class S, bool B_ACROSS, bool PARTS>
 __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Product pr, StepArgs e)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const Place w = place_of(pr);
     f32x16 acc[S::TB][S::TA];
     clear<S>(acc);
-    if (!tile_product<S, false, B_ACROSS>(pr, w, (f16_t *)lds, acc)) return;
+    if (!tile_product<S, false, B_ACROSS, PARTS>(pr, w, (f16_t *)lds, acc)) return;
     const Step k = e.first ? e.first[w.batch] : e.step;
     const int64_t base = w.batch * e.to_size;
     if constexpr (!B_ACROSS) {
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Pro
                 write16(e.to + at, e.to_parts, o);
             });
     } else {
-        const float *x = e.x + w.batch * e.to_size;
+        float *x = e.x + w.batch * e.x_size;
         constexpr float BY = 1.0f / (B_UP * X_UP);
         auto put = [&](int64_t at, float v) {
             const int64_t i = w.batch * e.out_size + at;
@@ -229,8 +230,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Pro
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[i] = fmaf(k.a, was[i], v[i] * BY);
                 if (e.kind == UPDATE) {
-                    store_f32<4, float>(e.x + base + at, *(float(*)[4])o);
-                    store_f32<4, float>(e.x + base + at + 4, *(float(*)[4])(o + 4));
+                    store_f32<4, float>(x + at, *(float(*)[4])o);
+                    store_f32<4, float>(x + at + 4, *(float(*)[4])(o + 4));
 #pragma unroll
                     for (int i = 0; i < 8; ++i) o[i] *= X_UP;
                     write16(e.to + base + at, e.to_parts, o);
@@ -366,26 +367,29 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void small_kernel(SmallArgs s)
 // ---------------------------------------------------------------------------
 // host
 
-template <class S, bool B_ACROSS>
+template <class S, bool B_ACROSS, bool PARTS>
 void launch(Product pr, const StepArgs &e, hipStream_t st)
 {
     pr.tiles_a = (int32_t)ceil_div(pr.a.own, S::BA);
     pr.tiles_b = (int32_t)ceil_div(pr.b.own, S::BB);
     const int64_t tiles = pr.symmetric ? (int64_t)pr.tiles_b * (pr.tiles_b + 1) / 2 : (int64_t)pr.tiles_a * pr.tiles_b;
-    const auto kernel = step_kernel<S, B_ACROSS>;
+    const auto kernel = step_kernel<S, B_ACROSS, PARTS>;
     if (S::LDS > 64 << 10)   // has to be asked for
         (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
     kernel<<<dim3((uint32_t)(tiles * pr.batches)), S::THREADS, S::LDS, st>>>(pr, e);
 }
 
 template <bool B_ACROSS>
-void step(const Operand &a, const Operand &b, int32_t K, int terms, int64_t batches, const StepArgs &e, hipStream_t st)
+void step(const Operand &a, const Operand &b, int32_t K, bool parts, int64_t batches, const StepArgs &e, hipStream_t st)
 {
     Product pr{};
-    pr.a = a, pr.b = b, pr.K = K, pr.terms = terms, pr.splits = 1, pr.batches = (int32_t)batches;
-    pr.steps = (int32_t)ceil_div(K, 64), pr.symmetric = !B_ACROSS;
-    const Cut cut = choose(a.own, b.own, K, terms, batches, !B_ACROSS, false);
-    with_tile<f16_t>(cut.shape, [&](auto tile) { launch<decltype(tile), B_ACROSS>(pr, e, st); });
+    const Cut cut = choose(a.own, b.own, K, parts, batches, !B_ACROSS, false);
+    pr.a = a, pr.b = b, pr.K = K, pr.splits = 1, pr.batches = (int32_t)batches;
+    pr.steps = cut.steps, pr.symmetric = !B_ACROSS;
+    with_tile<f16_t>(cut.shape, [&](auto tile) {
+        if (parts) launch<decltype(tile), B_ACROSS, true>(pr, e, st);
+        else launch<decltype(tile), B_ACROSS, false>(pr, e, st);
+    });
 }
 
 int check(const boa_orth *d)
@@ -394,7 +398,7 @@ int check(const boa_orth *d)
     const char *why = nullptr;
     if (!dtype_known(d->dtype)) why = "unknown dtype";
     else if (d->count < 0 || d->count > BOA_MAX_ORTH_COUNT) why = "count out of range [0, 2^16)";
-    else if (d->rows < 1 || d->rows > BOA_MAX_ORTH || d->cols < 1 || d->cols > BOA_MAX_ORTH) why = "rows and cols out of range [1, 2^15]";
+    else if (d->rows < 1 || d->rows > BOA_MAX_ORTH || d->cols < 1 || d->cols > BOA_MAX_ORTH) why = "rows and cols out of range [1, 2^14]";
     else if (d->steps < 1 || d->steps > BOA_MAX_ORTH_STEPS) why = "steps out of range [1, 32]";
     else if (!d->coefficients) why = "NULL coefficients";
     else if (!(d->eps >= 0.0f)) why = "eps must not be negative";
@@ -434,19 +438,19 @@ void orthogonalize(const boa_orth &d, Arena &mem, bool run, hipStream_t st)
         else small(f16_t{});
         return;
     }
-    const int32_t parts = d.dtype == BOA_T_BF16 && m >= 128 ? 1 : 2, terms = parts == 1 ? 1 : 3;
+    const bool parts = d.dtype != BOA_T_BF16 || m < 128;
     const int32_t x_ld = pad8(n), a_ld = pad8(m);
-    const int64_t x_size = (int64_t)m * x_ld, a_size = (int64_t)m * a_ld, C = d.count;
+    const int64_t x_size = (int64_t)m * x_ld, a_size = (int64_t)m * a_ld, C = d.count, copies = parts ? 2 : 1;
     float *x = (float *)mem.take(C * x_size * 4);
     f16_t *x16[2];   // the update reads the one and writes the other
-    for (auto &p : x16) p = (f16_t *)mem.take(C * x_size * parts * 2);
-    f16_t *a16 = (f16_t *)mem.take(C * a_size * parts * 2), *b16 = (f16_t *)mem.take(C * a_size * parts * 2);
+    for (auto &p : x16) p = (f16_t *)mem.take(C * x_size * copies * 2);
+    f16_t *a16 = (f16_t *)mem.take(C * a_size * copies * 2), *b16 = (f16_t *)mem.take(C * a_size * copies * 2);
     double *sums = (double *)mem.take(C * SUM_BLOCKS * 8);
     Step *first = (Step *)mem.take(C * (int64_t)sizeof(Step));
     if (!run) return;
     PrepArgs p{};
     p.g = d.update, p.ld = d.rows > 1 ? d.update_stride : d.cols, p.batch = d.update_batch, p.rows = d.rows, p.cols = d.cols;
-    p.turned = turned, p.m = m, p.n = n, p.x_ld = x_ld, p.x_size = x_size, p.parts = parts == 2 ? C * x_size : 0;
+    p.turned = turned, p.m = m, p.n = n, p.x_ld = x_ld, p.x_size = x_size, p.parts = parts ? x_size : 0;
     p.x = x, p.x16 = x16[0], p.sums = sums, p.eps = d.eps, p.first = first, p.step0 = coefficients(0);
     p.sum_blocks = (int32_t)std::min<int64_t>(SUM_BLOCKS, ceil_div((int64_t)d.rows * d.cols, 8192));
     const dim3 squares((uint32_t)p.sum_blocks, (uint32_t)C), tiles((uint32_t)ceil_div(x_ld, 64), (uint32_t)ceil_div(m, 64), (uint32_t)C);
@@ -459,23 +463,26 @@ void orthogonalize(const boa_orth &d, Arena &mem, bool run, hipStream_t st)
     else if (d.dtype == BOA_T_BF16) prepare(bf16_t{});
     else prepare(f16_t{});
 
-    Operand A{}, B{};
-    A.p = a16, B.p = b16, A.ld = B.ld = a_ld, A.batch = B.batch = a_size, A.part = B.part = C * a_size, A.own = B.own = m;
+    auto operand = [&](const f16_t *p, int64_t ld, int64_t size, int32_t own, bool across) {
+        Operand o{};
+        o.p = p, o.ld = ld, o.part = size, o.block = across ? 32 * ld : 32, o.batch = size * copies, o.own = own;
+        return o;
+    };
+    const Operand A = operand(a16, a_ld, a_size, m, false), B = operand(b16, a_ld, a_size, m, false);
     for (int i = 0; i < d.steps; ++i) {
-        Operand X{};
-        X.p = x16[i & 1], X.ld = x_ld, X.batch = x_size, X.part = C * x_size, X.own = m;
+        const Operand X = operand(x16[i & 1], x_ld, x_size, m, false), Xk = operand(x16[i & 1], x_ld, x_size, x_ld, true);
         StepArgs e{};
         e.step = coefficients(i), e.first = i == 0 ? first : nullptr;
-        e.rows = m, e.to_ld = a_ld, e.to_size = a_size, e.to_parts = parts == 2 ? C * a_size : 0;
+        e.rows = m, e.to_ld = a_ld, e.to_size = a_size * copies, e.to_parts = parts ? a_size : 0;
         e.kind = GRAM, e.to = a16;
-        step<false>(X, X, n, terms, C, e, st);
+        step<false>(X, X, n, parts, C, e, st);
         e.kind = POLY, e.to = b16, e.a = a16;
-        step<false>(A, A, m, terms, C, e, st);
+        step<false>(A, A, m, parts, C, e, st);
         e.kind = i + 1 < d.steps ? UPDATE : LAST;
-        e.to = x16[(i + 1) & 1], e.to_ld = x_ld, e.to_size = x_size, e.to_parts = parts == 2 ? C * x_size : 0, e.x = x;
+        e.to = x16[(i + 1) & 1], e.to_ld = x_ld, e.to_size = x_size * copies, e.to_parts = parts ? x_size : 0;
+        e.x = x, e.x_size = x_size;
         e.out = d.out, e.out_ld = d.cols, e.out_size = (int64_t)d.rows * d.cols, e.cols = n, e.dtype = d.dtype, e.turned = turned;
-        X.own = x_ld;
-        step<true>(B, X, m, terms, C, e, st);
+        step<true>(B, Xk, m, parts, C, e, st);
     }
 }
 

@@ -27,7 +27,7 @@ def _err():
 
 @pytest.mark.parametrize("over,needle", [
     (dict(dtype=4), "dtype"), (dict(count=-1), "count"), (dict(count=65536), "count"), (dict(rows=0), "rows and cols"),
-    (dict(cols=0), "rows and cols"), (dict(rows=(1 << 15) + 1), "rows and cols"), (dict(cols=(1 << 15) + 1), "rows and cols"),
+    (dict(cols=0), "rows and cols"), (dict(rows=(1 << 14) + 1), "rows and cols"), (dict(cols=(1 << 14) + 1), "rows and cols"),
     (dict(steps=0), "steps"), (dict(steps=33), "steps"), (dict(coefficients=None), "coefficients"), (dict(eps=-1.0), "eps"),
     (dict(eps=float("nan")), "eps"), (dict(update_stride=29), "stride"), (dict(update=None), "NULL"), (dict(out=None), "NULL"),
 ])
