@@ -214,6 +214,19 @@ struct Place {
     int32_t ta, tb, split, batch;
 };
 
+// Tiles a side of a symmetric output's squares.
+constexpr uint32_t SQUARE = 4;
+
+// Work items of an output.
+__host__ __device__ inline uint32_t tiles_of(const Product &pr)
+{
+    const uint32_t squares = (pr.tiles_b + SQUARE - 1) / SQUARE;
+    return pr.symmetric ? squares * (squares + 1) / 2 * SQUARE * SQUARE : (uint32_t)pr.tiles_a * pr.tiles_b;
+}
+
+// Whether a symmetric output's work item is a tile on or above the diagonal.
+__device__ inline bool is_needed(const Product &pr, const Place &w) { return !pr.symmetric || (w.ta <= w.tb && w.tb < pr.tiles_b); }
+
 // Work item of a block. Blocks go to the 8 XCDs in turn; each XCD takes a run of
 // tiles that share operand rows in its L2: bands of 8 tiles of a, one tile of b
 // after the other.
@@ -222,18 +235,19 @@ __device__ inline Place place_of(const Product &pr)
     const uint32_t n = gridDim.x, id = blockIdx.x;
     const uint32_t x = id & 7, per = n >> 3, extra = n & 7;
     uint32_t t = x * per + min(x, extra) + (id >> 3);
-    const uint32_t tiles = pr.symmetric ? (uint32_t)pr.tiles_b * (pr.tiles_b + 1) / 2 : (uint32_t)pr.tiles_a * pr.tiles_b;
+    const uint32_t tiles = tiles_of(pr);
     Place w;
     const uint32_t layer = t / tiles;
     t -= layer * tiles;
     w.batch = layer / pr.splits;
     w.split = layer - w.batch * pr.splits;
-    if (pr.symmetric) {   // columns of 1, 2, 3 ... tiles
-        uint32_t c = (uint32_t)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
-        while (c * (c + 1) / 2 > t) --c;
-        while ((c + 1) * (c + 2) / 2 <= t) ++c;
-        w.tb = c;
-        w.ta = t - c * (c + 1) / 2;
+    if (pr.symmetric) {   // squares of tiles, which share rows; a square's own diagonal has some that are not needed
+        const uint32_t square = t / (SQUARE * SQUARE), within = t - square * (SQUARE * SQUARE);
+        uint32_t c = (uint32_t)((sqrtf(8.0f * (float)square + 1.0f) - 1.0f) * 0.5f);
+        while (c * (c + 1) / 2 > square) --c;
+        while ((c + 1) * (c + 2) / 2 <= square) ++c;
+        w.tb = c * SQUARE + within / SQUARE;
+        w.ta = (square - c * (c + 1) / 2) * SQUARE + within % SQUARE;
         return w;
     }
     const uint32_t band = t / (8 * pr.tiles_b), first = band * 8, rows = min(8u, pr.tiles_a - first);
@@ -377,9 +391,15 @@ __device__ inline void clear(f32x16 (&acc)[S::TB][S::TA])
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
 }
 
+// Nothing to keep.
+struct Nothing {
+    __device__ void down() {}
+};
+
 // Hands the sums out in runs of eight neighbouring columns: f(row of a's side,
-// first column of b's side, the eight sums in LDS, what(column)); a lane keeps
-// its columns over many rows, so that `what` (their bias, say) is asked for once.
+// first column of b's side, the eight sums in LDS, kept). A lane keeps its columns
+// over every `step`th row: kept is what(first row, column, step), asked for once (addresses,
+// the columns' bias), and kept.down() takes it a step on.
 // Each wave turns its tiles over in its own piece of LDS, two columns of tiles at
 // a time, so that what follows is written once, and stores fill whole lines.
 // `turned`: g(first row, column, eight sums down that column) for all of them
@@ -394,8 +414,9 @@ __device__ inline void each_run(const Place &w, const f32x16 (&acc)[S::TB][S::TA
     const int32_t p0 = w.ta * S::BA + wa * S::TA * 32, q0 = w.tb * S::BB + wb * S::TB * 32;
 #pragma unroll
     for (int i0 = 0; i0 < S::TB; i0 += WIDE) {
+        constexpr int STEP = 64 / RUNS;
         const int32_t col = lane % RUNS * 8, q = q0 + i0 * 32 + col;
-        const auto kept = what(q);
+        auto kept = what(p0 + lane / RUNS, q, STEP);
 #pragma unroll
         for (int i = 0; i < WIDE; ++i)
 #pragma unroll
@@ -408,7 +429,10 @@ __device__ inline void each_run(const Place &w, const f32x16 (&acc)[S::TB][S::TA
                 }
         __builtin_amdgcn_wave_barrier();
 #pragma unroll 2
-        for (int row = lane / RUNS; row < S::TA * 32; row += 64 / RUNS) f(p0 + row, q, (const float *)(mine + row * LD + col), kept);
+        for (int row = lane / RUNS; row < S::TA * 32; row += STEP) {
+            f(p0 + row, q, (const float *)(mine + row * LD + col), kept);
+            kept.down();
+        }
         if (turned)
 #pragma unroll 1
             for (int k = lane; k < S::TURN_COLS * S::TA * 4; k += 64) {

@@ -41,9 +41,21 @@ __device__ inline float sigmoid(float z)
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-LOG2E * z));
 }
 
-// The normal distribution's function and density at z. For 16 bits Hastings'
-// rational approximation of the error function (Abramowitz and Stegun 7.1.26, off by at most
-// 1.5e-7), whose e^(-x^2) is the density's too.
+// The share of the normal distribution above m = |z|, and e = e^(-z^2 / 2):
+// Hastings' rational approximation of the error function (Abramowitz and Stegun
+// 7.1.26, off by at most 1.5e-7), for 16 bits.
+__device__ inline float share_above(float m, float z, float &e)
+{
+    e = __builtin_amdgcn_exp2f(-0.5f * LOG2E * z * z);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * SQRT_HALF, m, 1.0f));
+    // halves of the published coefficients
+    float s = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+    s = fmaf(t, s, 0.5f * 1.421413741f);
+    s = fmaf(t, s, 0.5f * -0.284496736f);
+    return fmaf(t, s, 0.5f * 0.254829592f) * t * e;
+}
+
+// The normal distribution's function and density at z.
 template <bool FINE>
 __device__ inline void normal(float z, float &below, float &density)
 {
@@ -51,15 +63,9 @@ __device__ inline void normal(float z, float &below, float &density)
         below = 0.5f * (1.0f + erff(z * SQRT_HALF));
         density = INV_SQRT_2PI * expf(-0.5f * z * z);
     } else {
-        const float e = __builtin_amdgcn_exp2f(-0.5f * LOG2E * z * z);
-        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * SQRT_HALF, fabsf(z), 1.0f));
-        // halves of the published coefficients: 1 - erf becomes the share above |z|
-        float tail = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
-        tail = fmaf(t, tail, 0.5f * 1.421413741f);
-        tail = fmaf(t, tail, 0.5f * -0.284496736f);
-        tail = fmaf(t, tail, 0.5f * 0.254829592f) * t * e;
-        below = z > 0.0f ? 1.0f - tail : tail;
-        density = INV_SQRT_2PI * e;
+        const float above = share_above(fabsf(z), z, density);
+        below = z > 0.0f ? 1.0f - above : above;
+        density *= INV_SQRT_2PI;
     }
 }
 
@@ -72,6 +78,11 @@ __device__ inline float act_of(float z)
         return z > 0.0f ? z : z != z ? z : 0.0f;
     } else if constexpr (ACT == BOA_ACT_SILU) {
         y = z * sigmoid<FINE>(z);
+    } else if constexpr (ACT == BOA_ACT_GELU && !FINE) {
+        // max(z, 0) - |z| (1 - erf(|z| / sqrt 2)) / 2; beyond 40 the share is 0, and |z| could be infinite
+        float e;
+        const float m = fminf(fabsf(z), 40.0f);
+        return fmaf(-m, share_above(m, z, e), fmaxf(z, 0.0f));
     } else if constexpr (ACT == BOA_ACT_GELU) {
         float below, density;
         normal<FINE>(z, below, density);
@@ -151,18 +162,28 @@ __device__ inline float bias_at(const Epilogue &e, int32_t q)
     return !e.bias ? 0.0f : e.bias_f32 ? ((const float *)e.bias)[q] : (float)((const TO *)e.bias)[q];
 }
 
-// What eight neighbouring columns have for all rows, where the rows have them all.
+// What eight neighbouring columns keep over the rows that a lane finishes: their
+// bias and scales (where the rows have all eight), and where the row's values are.
 template <class TO>
 struct Columns {
+    typedef std::conditional_t<sizeof(TO) == 4, float, f16_t> Z;
     float bias[8];
     int shift[sizeof(TO) == 4 ? 8 : 1];
+    TO *out;
+    const TO *residual;
+    Z *pre;
+    int64_t out_step, residual_step, pre_step;
+    __device__ void down() { out += out_step, residual += residual_step, pre += pre_step; }
 };
 
 template <class TO>
-__device__ inline Columns<TO> columns_at(const Epilogue &e, int32_t q)
+__device__ inline Columns<TO> columns_at(const Epilogue &e, int64_t p, int32_t q, int step)
 {
     constexpr bool WIDE = sizeof(TO) == 4;
     Columns<TO> c;
+    c.out = (TO *)e.out + p * e.ld + q, c.out_step = step * e.ld;
+    c.residual = (const TO *)e.residual + p * e.residual_ld + q, c.residual_step = step * e.residual_ld;
+    c.pre = (typename Columns<TO>::Z *)e.pre + p * e.cols + q, c.pre_step = (int64_t)step * e.cols;
     const bool whole = q + 8 <= e.cols;
     if (!e.bias) {
 #pragma unroll
@@ -191,12 +212,22 @@ __device__ inline void finish_one(const Epilogue &e, int64_t p, int32_t q, float
     ((TO *)e.out)[p * e.ld + q] = (TO)v;
 }
 
+template <class E>
+__device__ inline void store8(E *to, const float (&v)[8])
+{
+    if constexpr (sizeof(E) == 4) {
+        store_loose<4, E>(to, *(const float(*)[4])v);
+        store_loose<4, E>(to + 4, *(const float(*)[4])(v + 4));
+    } else {
+        store_loose<8, E>(to, v);
+    }
+}
+
 // Eight sums from column q on, of which the row may have fewer.
 template <class TO, int ACT>
 __device__ inline void finish_run(const Epilogue &e, int64_t p, int32_t q, const float *sums, const Columns<TO> &c)
 {
     constexpr bool WIDE = sizeof(TO) == 4;
-    typedef std::conditional_t<WIDE, float, f16_t> Z;
     const int s = WIDE && e.max_a ? up(e.max_a[p]) : 0;
     if (q + 8 > e.cols) {
 #pragma unroll 1
@@ -207,32 +238,34 @@ __device__ inline void finish_run(const Epilogue &e, int64_t p, int32_t q, const
         }
         return;
     }
-    float v[8], r[8];
-    if (e.residual) load_loose<8, TO>(r, (const TO *)e.residual + p * e.residual_ld + q);
+    words4 r[sizeof(TO) / 2];   // asked for before the sums are worked on
+    if (e.residual) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(TO) / 2; ++i) r[i] = ((const loose4 *)c.residual)[i];
+    }
+    float v[8];
     load_f32<4, float>(*(float(*)[4])v, sums);
     load_f32<4, float>(*(float(*)[4])(v + 4), sums + 4);
-    auto store = [&](auto *to) {
-        typedef std::remove_reference_t<decltype(*to)> E;
-        if constexpr (WIDE) {
-            store_loose<4, E>(to, *(float(*)[4])v);
-            store_loose<4, E>(to + 4, *(float(*)[4])(v + 4));
-        } else {
-            store_loose<8, E>(to, v);
-        }
-    };
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if constexpr (WIDE) v[i] = ldexpf(v[i], -(s + c.shift[i]));
         v[i] += c.bias[i];
     }
-    if (e.pre) store((Z *)e.pre + p * e.cols + q);
+    if (e.pre) store8(c.pre, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = act_of<WIDE, ACT>(v[i]);
     if (e.residual) {
+        typedef Pack<8, TO> P8;
+        struct Both {
+            words4 w[sizeof(TO) / 2];
+        } both;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += r[i];
+        for (int i = 0; i < (int)sizeof(TO) / 2; ++i) both.w[i] = r[i];
+        const P8 t = __builtin_bit_cast(P8, both);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += (float)t.v[i];
     }
-    store((TO *)e.out + p * e.ld + q);
+    store8(c.out, v);
 }
 
 // A forward product (both operands along k) has the whole epilogue, the gradients' none.
@@ -246,7 +279,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void product_kernel(
     if (!tile_product<S, ACROSS_A, ACROSS_B, sizeof(TO) == 4>(pr, w, (typename S::T *)lds, acc)) return;
     if (e.partial) {
         float *out = e.partial + w.split * e.partial_split;
-        each_run<S>(w, acc, lds, [](int32_t) { return 0; }, [&](int32_t p, int32_t q, const float *v, int) {
+        each_run<S>(w, acc, lds, [](int32_t, int32_t, int) { return Nothing{}; }, [&](int32_t p, int32_t q, const float *v, const Nothing &) {
             if (p >= e.rows || q >= e.cols) return;
             float *to = out + p * e.partial_ld + q;
             *(f32x4 *)to = *(const f32x4 *)v;
@@ -255,7 +288,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void product_kernel(
         return;
     }
     auto all = [&](auto act) {
-        each_run<S>(w, acc, lds, [&](int32_t q) { return columns_at<TO>(e, q); },
+        each_run<S>(w, acc, lds, [&](int32_t p, int32_t q, int step) { return columns_at<TO>(e, p, q, step); },
             [&](int32_t p, int32_t q, const float *v, const Columns<TO> &c) {
                 if (p < e.rows && q < e.cols) finish_run<TO, decltype(act)::value>(e, p, q, v, c);
             });
@@ -283,7 +316,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(Epilogue e, int32_t s
     float *mine = sums + threadIdx.x * 8;
     *(f32x4 *)mine = v0;
     *(f32x4 *)(mine + 4) = v1;
-    with_act(e.act, [&](auto act) { finish_run<TO, decltype(act)::value>(e, p, q, mine, columns_at<TO>(e, q)); });
+    with_act(e.act, [&](auto act) { finish_run<TO, decltype(act)::value>(e, p, q, mine, columns_at<TO>(e, p, q, 0)); });
 }
 
 // ---------------------------------------------------------------------------

@@ -181,6 +181,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Pro
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const Place w = place_of(pr);
+    if (!is_needed(pr, w)) return;
     f32x16 acc[S::TB][S::TA];
     clear<S>(acc);
     if (!tile_product<S, false, B_ACROSS, PARTS>(pr, w, (f16_t *)lds, acc)) return;
@@ -193,8 +194,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Pro
             if (e.to_parts) was += (float)e.a[at + e.to_parts];
             return k.b * was * (B_UP / A_UP) + k.c * (v * (B_UP / (A_UP * A_UP)));
         };
-        each_run<S>(w, acc, lds, [](int32_t) { return 0; },
-            [&](int32_t p, int32_t q, const float *v, int) {
+        each_run<S>(w, acc, lds, [](int32_t, int32_t, int) { return Nothing{}; },
+            [&](int32_t p, int32_t q, const float *v, const Nothing &) {
                 if (p >= e.rows || q >= e.to_ld) return;
                 const int64_t at = base + p * e.to_ld + q;
                 float o[8];
@@ -220,8 +221,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Pro
             else if (e.dtype == BOA_T_BF16) ((bf16_t *)e.out)[i] = (bf16_t)v;
             else ((f16_t *)e.out)[i] = (f16_t)v;
         };
-        each_run<S>(w, acc, lds, [](int32_t) { return 0; },
-            [&](int32_t p, int32_t q, const float *v, int) {
+        each_run<S>(w, acc, lds, [](int32_t, int32_t, int) { return Nothing{}; },
+            [&](int32_t p, int32_t q, const float *v, const Nothing &) {
                 if (p >= e.rows || q >= e.to_ld) return;
                 const int64_t at = p * e.to_ld + q;
                 float was[8], o[8];
@@ -372,7 +373,7 @@ void launch(Product pr, const StepArgs &e, hipStream_t st)
 {
     pr.tiles_a = (int32_t)ceil_div(pr.a.own, S::BA);
     pr.tiles_b = (int32_t)ceil_div(pr.b.own, S::BB);
-    const int64_t tiles = pr.symmetric ? (int64_t)pr.tiles_b * (pr.tiles_b + 1) / 2 : (int64_t)pr.tiles_a * pr.tiles_b;
+    const int64_t tiles = tiles_of(pr);
     const auto kernel = step_kernel<S, B_ACROSS, PARTS>;
     if (S::LDS > 64 << 10)   // has to be asked for
         (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
