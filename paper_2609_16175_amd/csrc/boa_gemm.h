@@ -472,9 +472,9 @@ inline int32_t pad8(int64_t n) { return (int32_t)(ceil_div(n, 8) * 8); }
 inline uint32_t spread(int64_t items) { return (uint32_t)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, 256), 1 << 14)); }
 
 // The tiles there are: 256 x 256 for large outputs; 128 x 128, two at once on a
-// CU, or one with its loads four stages ahead where a CU gets no second; 64 x 64
-// with two sets of waves, likewise. A smaller tile reads more of LDS for the same
-// products: 1,170, 980 and 620 TFLOP/s where there are tiles enough (k = 4,096).
+// CU, or one with its loads four stages ahead where a CU gets no second; 64 x 64,
+// four at once, or two with two sets of waves, or one of those with its loads four stages ahead. A smaller tile reads more of LDS for the same
+// products: 1,170, 980 and 630 TFLOP/s where there are tiles enough (k = 4,096).
 template <class T>
 using Large = Tile<T, 4, 2, 2, 4, 1, 2, 1>;
 template <class T>
@@ -482,7 +482,9 @@ using Middle = Tile<T, 2, 2, 2, 2, 1, 2, 2>;
 template <class T>
 using MiddleAlone = Tile<T, 2, 2, 2, 2, 1, 4, 1>;
 template <class T>
-using Small = Tile<T, 2, 2, 1, 1, 2, 2, 2>;
+using Small = Tile<T, 2, 2, 1, 1, 1, 2, 4>;
+template <class T>
+using SmallPair = Tile<T, 2, 2, 1, 1, 2, 2, 2>;
 template <class T>
 using SmallAlone = Tile<T, 2, 2, 1, 1, 2, 4, 1>;
 
@@ -500,6 +502,7 @@ void with_tile(int shape, F f)
     else if (shape == 1) f(Middle<T>{});
     else if (shape == 2) f(MiddleAlone<T>{});
     else if (shape == 3) f(Small<T>{});
+    else if (shape == 4) f(SmallPair<T>{});
     else f(SmallAlone<T>{});
 }
 
@@ -514,14 +517,14 @@ inline Cut choose(int64_t A, int64_t B, int64_t K, bool parts, int64_t batches, 
         double stage, alone, ends;   // us a stage in a full CU and in a CU of its own, us of beginning and end
     };
     // measured on outputs of 0.5 to 8 tiles a CU and k of 512 to 4,096
-    static const Cost costs[5] = {{256, 1, 1, 1.75, 1.40, 9.0}, {128, 2, 1, 0.98, 0.62, 6.5}, {128, 1, 1, 0.68, 0.60, 6.0},
-                                  {64, 2, 2, 0.75, 0.60, 5.0}, {64, 1, 2, 0.55, 0.50, 4.5}};
+    static const Cost costs[6] = {{256, 1, 1, 1.75, 1.40, 9.0}, {128, 2, 1, 0.98, 0.62, 6.5}, {128, 1, 1, 0.68, 0.60, 6.0},
+                                  {64, 4, 1, 0.72, 0.36, 4.5}, {64, 2, 2, 0.80, 0.62, 5.0}, {64, 1, 2, 0.55, 0.50, 4.5}};
     static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
     const int64_t steps = ceil_div(K, parts ? 32 : 64);
     const double longer = parts ? 1.25 : 1.0;   // a stage's time: three products of half its values
     Cut best{0, 1, (int32_t)steps};
     double least = 1e30;
-    for (int s = 0; s < 5; ++s)
+    for (int s = 0; s < 6; ++s)
         for (int n : counts) {
             if (n > 1 && (!may_split || n > steps || (double)n * A * B * 4 > 256e6)) break;
             const Cost &c = costs[s];
