@@ -443,6 +443,7 @@ struct SlopeArgs {
     const void *dy, *pre;
     void *dz;          // rows of `pad` values, or null
     float *partial;    // stripes x N sums over rows, or null
+    float *most;       // N: the columns' largest magnitudes (zeros at first), or null
     int64_t M, ld;
     int32_t N, pad, act;
 };
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
     __shared__ float sums[8][32 * VEC];
     const int col = threadIdx.x & 31, part = threadIdx.x >> 5;
     const int32_t c = (blockIdx.x * 32 + col) * VEC;
-    float s[VEC] = {};
+    float s[VEC] = {}, m[VEC] = {};
     if (c < a.N) {
         const bool whole = c + VEC <= a.N;
         for (int64_t r = (int64_t)blockIdx.y * 8 + part; r < a.M; r += (int64_t)gridDim.y * 8) {
@@ -480,7 +481,10 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
                     for (int e = 0; e < VEC; ++e) g[e] *= slope_of<sizeof(T) == 4, decltype(act)::value>(x[e]);
                 });
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) s[e] += g[e];
+            for (int e = 0; e < VEC; ++e) {
+                s[e] += g[e];
+                if (sizeof(T) == 4) m[e] = fmaxf(m[e], finite_abs(g[e]));
+            }
             if (a.dz) {   // rows have room for whole runs
                 T *to = (T *)a.dz + r * a.pad + c;
                 if constexpr (sizeof(T) == 4) {
@@ -492,17 +496,30 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
             }
         }
     }
-    if (!a.partial) return;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) sums[part][e * 32 + col] = s[e];
-    __syncthreads();
     const int32_t mine = blockIdx.x * 32 * VEC + threadIdx.x;
-    if (mine < a.N) {
-        const int at = (threadIdx.x % VEC) * 32 + threadIdx.x / VEC;
-        float t = 0.0f;
+    const int at = (threadIdx.x % VEC) * 32 + threadIdx.x / VEC;
+    if (a.partial) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t += sums[k][at];
-        a.partial[(int64_t)blockIdx.y * a.N + mine] = t;
+        for (int e = 0; e < VEC; ++e) sums[part][e * 32 + col] = s[e];
+        __syncthreads();
+        if (mine < a.N) {
+            float t = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t += sums[k][at];
+            a.partial[(int64_t)blockIdx.y * a.N + mine] = t;
+        }
+        __syncthreads();
+    }
+    if (sizeof(T) == 4 && a.most) {   // the maximum of bit patterns, whose order does not matter
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sums[part][e * 32 + col] = m[e];
+        __syncthreads();
+        if (mine < a.N) {
+            float t = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t = fmaxf(t, sums[k][at]);
+            atomicMax((uint32_t *)a.most + mine, __float_as_uint(t));
+        }
     }
 }
 
@@ -718,29 +735,36 @@ Operand operand(const void *src, int64_t ld, int64_t rows, int32_t cols, bool ac
     return o;
 }
 
-// float32 rows x cols at `src` as two parts: along k scaled per row, across per
-// column; *most gets the magnitudes that the scales come from.
-Operand parts(const void *src, int64_t ld, int64_t rows, int32_t cols, bool across, const float **most, Arena &mem, bool run, hipStream_t st)
+// float32 rows x cols at `src` as two parts: along k scaled per row ...
+Operand row_parts(const void *src, int64_t ld, int64_t rows, int32_t cols, const float **most, Arena &mem, bool run, hipStream_t st)
 {
     CopyArgs c{};
-    c.src = src, c.ld = ld, c.rows = rows, c.cols = cols;
-    c.pad = across ? pad8(cols) : (int32_t)ceil_div(cols, 32) * 32;
-    c.dst = mem.take((across ? ceil_div(rows, 32) * 32 : rows) * 2 * (int64_t)c.pad * 2);
-    c.most = (float *)mem.take((across ? (int64_t)cols : rows) * 4);
+    c.src = src, c.ld = ld, c.rows = rows, c.cols = cols, c.pad = (int32_t)ceil_div(cols, 32) * 32;
+    c.dst = mem.take(rows * 2 * (int64_t)c.pad * 2);
+    c.most = (float *)mem.take(rows * 4);
     *most = c.most;
     Operand o{};
-    o.own = (int32_t)(across ? cols : rows), o.p = c.dst;
-    if (across) o.ld = c.pad, o.part = 32 * (int64_t)c.pad, o.block = 64 * (int64_t)c.pad;
-    else o.ld = 2 * (int64_t)c.pad, o.part = 32, o.block = 64;
+    o.own = (int32_t)rows, o.p = c.dst, o.ld = 2 * (int64_t)c.pad, o.part = 32, o.block = 64;
+    if (run) row_parts_kernel<<<dim3((uint32_t)std::min<int64_t>(ceil_div(rows, 4), 1 << 14)), 256, 0, st>>>(c);
+    return o;
+}
+
+// ... and across scaled per column. most: the magnitudes that the scales come
+// from, zeros unless they are known.
+Operand col_parts(const void *src, int64_t ld, int64_t rows, int32_t cols, float *most, bool known, Arena &mem, bool run, hipStream_t st)
+{
+    CopyArgs c{};
+    c.src = src, c.ld = ld, c.rows = rows, c.cols = cols, c.pad = pad8(cols), c.most = most;
+    const int64_t deep = ceil_div(rows, 32) * 32;
+    c.dst = mem.take(deep * 2 * c.pad * 2);
+    Operand o{};
+    o.own = cols, o.p = c.dst, o.ld = c.pad, o.part = 32 * (int64_t)c.pad, o.block = 64 * (int64_t)c.pad;
     if (!run) return o;
-    if (!across) {
-        row_parts_kernel<<<dim3((uint32_t)std::min<int64_t>(ceil_div(rows, 4), 1 << 14)), 256, 0, st>>>(c);
-        return o;
+    if (!known) {
+        const int64_t strips = ceil_div(cols, 256), down = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 32), 2048 / strips));
+        col_max_kernel<<<dim3((uint32_t)strips, (uint32_t)down), 256, 0, st>>>(c);
     }
-    zero_kernel<float><<<spread(cols), 256, 0, st>>>(c.most, cols);
-    const int64_t strips = ceil_div(cols, 256), down = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 32), 2048 / strips));
-    col_max_kernel<<<dim3((uint32_t)strips, (uint32_t)down), 256, 0, st>>>(c);
-    col_parts_kernel<<<spread(ceil_div(rows, 32) * 32 * (c.pad / 8)), 256, 0, st>>>(c);
+    col_parts_kernel<<<spread(deep * (c.pad / 8)), 256, 0, st>>>(c);
     return o;
 }
 
@@ -808,8 +832,8 @@ void forward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
         return;
     }
     if constexpr (WIDE) {
-        const Operand x = parts(d.x, d.x_stride, M, d.K, false, &e.max_a, mem, run, st);
-        const Operand w = parts(d.w, d.w_stride, d.N, d.K, false, &e.max_b, mem, run, st);
+        const Operand x = row_parts(d.x, d.x_stride, M, d.K, &e.max_a, mem, run, st);
+        const Operand w = row_parts(d.w, d.w_stride, d.N, d.K, &e.max_b, mem, run, st);
         product<T, TO, false, false>(x, w, d.K, e, mem, run, st);
     } else {
         const Operand x = operand<T>(d.x, d.x_stride, M, d.K, false, mem, run, st);
@@ -834,6 +858,13 @@ void backward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
         s.dz = mem.take((int64_t)M * s.pad * sizeof(TO));
         dz = s.dz, dz_ld = s.pad;
     }
+    float *most_z = nullptr, *most_w = nullptr, *most_x = nullptr;
+    if (WIDE && M && (d.dx || d.dw)) {   // magnitudes of dz's, w's and x's columns
+        const int64_t n = d.N + 2 * (int64_t)d.K;
+        most_z = (float *)mem.take(n * 4), most_w = most_z + d.N, most_x = most_w + d.K;
+        if (run) zero_kernel<float><<<spread(n), 256, 0, st>>>(most_z, n);
+        if (d.dw && (s.dz || d.dbias)) s.most = most_z;   // the kernel runs anyway
+    }
     const int64_t strips = ceil_div(d.N, 256);
     const int32_t stripes = (int32_t)std::max<int64_t>(1, std::min<int64_t>(ceil_div(M, 64), std::max<int64_t>(1, 2048 / strips)));
     if (d.dbias) s.partial = (float *)mem.take((int64_t)stripes * d.N * 4);
@@ -850,8 +881,9 @@ void backward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
     if (d.dx && M) {
         e.out = d.dx, e.ld = d.K;
         if constexpr (WIDE) {
-            const Operand a = parts(dz, dz_ld, M, d.N, false, &e.max_a, mem, run, st);
-            const Operand b = parts(d.w, d.w_stride, d.N, d.K, true, &e.max_b, mem, run, st);
+            const Operand a = row_parts(dz, dz_ld, M, d.N, &e.max_a, mem, run, st);
+            const Operand b = col_parts(d.w, d.w_stride, d.N, d.K, most_w, false, mem, run, st);
+            e.max_b = most_w;
             product<T, TO, false, true>(a, b, d.N, e, mem, run, st);
         } else {
             Operand a{};
@@ -868,8 +900,9 @@ void backward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
             const int64_t n = (int64_t)d.N * d.K;
             if (run) zero_kernel<TO><<<spread(n), 256, 0, st>>>((TO *)d.dw, n);
         } else if constexpr (WIDE) {
-            const Operand a = parts(dz, dz_ld, M, d.N, true, &e.max_a, mem, run, st);
-            const Operand b = parts(d.x, d.x_stride, M, d.K, true, &e.max_b, mem, run, st);
+            const Operand a = col_parts(dz, dz_ld, M, d.N, most_z, s.most, mem, run, st);
+            const Operand b = col_parts(d.x, d.x_stride, M, d.K, most_x, false, mem, run, st);
+            e.max_a = most_z, e.max_b = most_x;
             product<T, TO, true, true>(a, b, M, e, mem, run, st);
         } else {
             Operand a{};
