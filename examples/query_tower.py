@@ -7,7 +7,11 @@ points as classes, with the negative squared distance of the search as logit
 (scale = 2 t, bias = -t |p|^2; t |h|^2 is the same for every class). Serving
 takes one state at a time: layer norm, then W in 4 bits, then the search.
 
-    python examples/query_tower.py [--steps 200]
+With --blocks the tower has residual blocks between the two: h <- h + gate V
+gelu(U y), y <- layer_norm(h). Their matrices learn from orthogonalised
+momenta, everything else from Adam.
+
+    python examples/query_tower.py [--steps 200] [--blocks 2]
 """
 import argparse
 import os
@@ -31,11 +35,54 @@ def found(index, queries, labels, wl):
     return float((ids == labels[:, None]).any(1).float().mean())
 
 
+class Tower:
+    """W of the last layer norm of a residual stream, which `blocks` blocks of `states` x 4 `states` weights add to."""
+
+    def __init__(self, states, d, blocks, g):
+        def leaf(t):
+            return t.requires_grad_()
+
+        def matrix(rows, cols):
+            return leaf(torch.randn(rows, cols, generator=g, device="cuda") / cols ** 0.5)
+
+        def vector(n, value):
+            return leaf(torch.full((n,), value, device="cuda"))
+
+        self.norm = vector(states, 1.0), vector(states, 0.0)
+        self.W = matrix(d, states)
+        self.blocks = [dict(up=matrix(4 * states, states), up_bias=vector(4 * states, 0.0), down=matrix(states, 4 * states),
+                            down_bias=vector(states, 0.0), gate=vector(states, 0.2), weight=vector(states, 1.0),
+                            bias=vector(states, 0.0)) for _ in range(blocks)]
+        self.hidden_matrices = [b[k] for b in self.blocks for k in ("up", "down")]
+        self.momenta = [torch.zeros_like(m) for m in self.hidden_matrices]
+        self.others = [*self.norm, self.W, *(v for b in self.blocks for k, v in b.items() if k not in ("up", "down"))]
+
+    def hidden(self, x):
+        """What W is applied to."""
+        h, y = x, boa.layer_norm(x, *self.norm)
+        for b in self.blocks:
+            f = boa.linear(boa.linear(y, b["up"], b["up_bias"], activation="gelu"), b["down"], b["down_bias"])
+            h, y = boa.block_norm(h, f, b["gate"], weight=b["weight"], bias=b["bias"])
+        return y
+
+    def __call__(self, x):
+        return self.hidden(x) @ self.W.t()
+
+    @torch.no_grad()
+    def step_hidden(self, lr=0.02, beta=0.9):
+        """Each hidden matrix a step against its orthogonalised momentum."""
+        for m, v in zip(self.hidden_matrices, self.momenta):
+            v.mul_(beta).add_(m.grad)
+            m.sub_(boa.orthogonalize(v), alpha=lr * max(1.0, m.shape[0] / m.shape[1]) ** 0.5)
+            m.grad = None
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--points", type=int, default=10_000)
     ap.add_argument("--states", type=int, default=96, help="width of the encoder's states")
+    ap.add_argument("--blocks", type=int, default=0, help="residual blocks of the tower")
     a = ap.parse_args(argv)
     wl = gen.TINY.scaled(a.points, nq=64)
     data = gen.generate(wl)
@@ -51,18 +98,13 @@ def main(argv=None):
     def states(labels):   # what an encoder gives for a text about each point
         return points[labels] @ mix + shift + 0.1 * torch.randn(len(labels), a.states, generator=g, device="cuda")
 
-    norm_w = torch.ones(a.states, device="cuda", requires_grad=True)
-    norm_b = torch.zeros(a.states, device="cuda", requires_grad=True)
-    W = (torch.randn(d, a.states, generator=g, device="cuda") / a.states ** 0.5).requires_grad_()
-    opt = torch.optim.Adam([norm_w, norm_b, W], lr=2e-2)
+    tower = Tower(a.states, d, a.blocks, g)
+    opt = torch.optim.Adam(tower.others, lr=2e-2)
     t = 2.0
     bias = -t * points.square().sum(1)
 
     held = torch.randint(n, (256,), generator=g, device="cuda")
     held_x = states(held)
-
-    def tower(x):
-        return boa.layer_norm(x, norm_w, norm_b) @ W.t()
 
     with torch.no_grad():
         first = float(boa.softmax_xent(tower(held_x), points, held, bias, 2 * t))
@@ -73,6 +115,7 @@ def main(argv=None):
         opt.zero_grad()
         loss.backward()
         opt.step()
+        tower.step_hidden()
         if (step + 1) % 50 == 0:
             print(f"step {step + 1}: loss {float(loss.detach()):.3f}", flush=True)
     with torch.no_grad():
@@ -80,14 +123,14 @@ def main(argv=None):
         last = float(boa.softmax_xent(h, points, held, bias, 2 * t))
         whole = found(index, h, held, wl)
         # serving: one state at a time through 4-bit weights
-        codes, scales, offsets = rows4.quantize(W, group=32)
-        one = [boa.matvec_4bit(boa.layer_norm_forward(x[None], norm_w, norm_b)[0], codes, scales, offsets) for x in held_x]
+        codes, scales, offsets = rows4.quantize(tower.W, group=32)
+        one = [boa.matvec_4bit(tower.hidden(x[None]), codes, scales, offsets) for x in held_x]
         served = torch.cat(one)
         in4 = found(index, served, held, wl)
     print(f"after: loss {last:.3f}, own point found {whole:.3f}, with 4-bit weights {in4:.3f}", flush=True)
     index.close()
-    return dict(first=first, last=last, found=whole, found_4bit=in4, h=h, served=served, W=W.detach(), norm=(norm_w, norm_b),
-                x=held_x)
+    return dict(first=first, last=last, found=whole, found_4bit=in4, h=h, served=served, W=tower.W.detach(), norm=tower.norm,
+                x=held_x, tower=tower)
 
 
 if __name__ == "__main__":
