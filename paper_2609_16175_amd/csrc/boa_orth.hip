@@ -262,7 +262,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Pro
 // small matrices: a block does all steps on one, in LDS and in float32
 
 constexpr int SMALL_WAVES = 16, SMALL_TILES = 8;   // tiles of X a wave may have
-constexpr int SMALL_LDS = 150 << 10;
+constexpr int SMALL_LDS = 158 << 10;
 
 struct SmallArgs {
     const void *g;
@@ -273,17 +273,28 @@ struct SmallArgs {
     Step step[BOA_MAX_ORTH_STEPS];
 };
 
-// LDS rows are 4 values longer than their tiles, so that 16 rows x 4 values read together lie in all banks.
+// Waves that share the sum of a tile of X X': 16 or 4 where it has 1 or 4 tiles, if the sum is long enough to pay for
+// the joining.
+__host__ __device__ inline int small_slices(int32_t m_pad, int32_t n_pad)
+{
+    return n_pad < 192 || m_pad > 32 ? 1 : m_pad <= 16 ? SMALL_WAVES : SMALL_WAVES / 4;
+}
+
+// LDS rows are 4 values longer than their tiles, so that 16 rows x 16 values read together lie in all banks.
 inline int64_t small_bytes(int32_t m_pad, int32_t n_pad)
 {
-    return ((int64_t)m_pad * (n_pad + 4) + 2 * (int64_t)m_pad * (m_pad + 4)) * 4;
+    return ((int64_t)m_pad * (n_pad + 4) + 2 * (int64_t)m_pad * (m_pad + 4) + (small_slices(m_pad, n_pad) > 1 ? SMALL_WAVES * 256 : 0)) * 4;
 }
 
 // Products by float32 matrix instructions, a 16 x 16 tile a wave at a time.
-// X (m x n), A and B = b A + c A^2 (m x m) stay in LDS; every wave holds its tiles of the new
-// X until all have read the old one. 32 x 96: 5 steps in 17 us, of which 15
-// launches of the large kernels took 90.
-template <class T>
+// X (m x n), A and B = b A + c A^2 (m x m) stay in LDS; every wave holds its
+// TILES tiles of the new X until all have read the old one. Bound by the
+// latencies of four short phases a step: 32 x 96, 5 steps, 17 us (82 in the 17
+// launches of the large kernels); 64 x 256 73 (109); 64 x 400 115 (123); 64 x
+// 480, the longest that fits, 134 (122), but 256 of them together 155 (508).
+// TILES = 8 for all would cost 32 x 96 3 us of instruction fetches; a sum of 16
+// x 1,024 split over 16 waves saves 24 us.
+template <class T, int TILES>
 __global__ __launch_bounds__(64 * SMALL_WAVES) void small_kernel(SmallArgs s)
 {
     extern __shared__ __attribute__((aligned(16))) float x[];
@@ -293,12 +304,24 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void small_kernel(SmallArgs s)
     float *a = x + s.m_pad * xl, *b = a + s.m_pad * al;
     const T *g = (const T *)s.g + blockIdx.x * s.batch;
     double sum = 0.0;
-    for (int i = threadIdx.x; i < s.m_pad * s.n_pad; i += 64 * SMALL_WAVES) {
-        const int row = s.turned ? i % s.m_pad : i / s.n_pad, col = s.turned ? i / s.m_pad : i % s.n_pad;
-        const bool in = row < s.m && col < s.n;
-        const float v = !in ? 0.0f : (float)(s.turned ? g[col * s.ld + row] : g[row * s.ld + col]);
-        x[row * xl + col] = v;
-        sum = fma((double)v, (double)v, sum);
+    for (int from = threadIdx.x; from < s.m_pad * s.n_pad; from += 4 * 64 * SMALL_WAVES) {   // four loads on their way
+        float v[4];
+        int at[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = from + e * 64 * SMALL_WAVES;
+            const int row = s.turned ? i % s.m_pad : i / s.n_pad, col = s.turned ? i / s.m_pad : i % s.n_pad;
+            const int64_t to = min(row, s.m - 1), along = min(col, s.n - 1);
+            v[e] = (float)(s.turned ? g[along * s.ld + to] : g[to * s.ld + along]);
+            if (row >= s.m || col >= s.n) v[e] = 0.0f;
+            at[e] = i < s.m_pad * s.n_pad ? row * xl + col : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (at[e] < 0) continue;
+            x[at[e]] = v[e];
+            sum = fma((double)v[e], (double)v[e], sum);
+        }
     }
 #pragma unroll
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
@@ -313,41 +336,66 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void small_kernel(SmallArgs s)
         *v = ldexpf(*v, first.up);
     }
     __syncthreads();
-    // sum over k of a row of `u` times a row, or `down` a column, of `v`
-    auto product = [&](const float *u, int ul, int ti, const float *v, int vl, int tj, int K, bool down) {
+    // sum over k in [from, to) of a row of `u` times a row, or `down` a column, of `v`; a lane's four k are next to each other
+    auto product = [&](const float *u, int ul, int ti, const float *v, int vl, int tj, int from, int to, auto down) {
         f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-        const float *pu = u + (ti * 16 + r) * ul + q, *pv = down ? v + q * vl + tj * 16 + r : v + (tj * 16 + r) * vl + q;
-        const int step = down ? 4 * vl : 4;
-#pragma unroll 4
-        for (int k = 0; k < K; k += 4) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(pu[k], pv[k / 4 * step], acc, 0, 0, 0);
+        const float *pu = u + (ti * 16 + r) * ul + 4 * q, *pv = down ? v + 4 * q * vl + tj * 16 + r : v + (tj * 16 + r) * vl + 4 * q;
+#pragma unroll 2
+        for (int k = from; k < to; k += 16) {
+            const f32x4 f = *(const f32x4 *)(pu + k);
+            f32x4 g;
+            if constexpr (down) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) g[e] = pv[(k + e) * vl];
+            } else {
+                g = *(const f32x4 *)(pv + k);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(f[e], g[e], acc, 0, 0, 0);
+        }
         return acc;
     };
-    for (int it = 0; it < s.steps; ++it) {
-        const Step k = it ? s.step[it] : first.step;
-        for (int t = wave; t < mt * mt; t += SMALL_WAVES) {   // both of two mirrored tiles: their roundings are the same
-            const f32x4 v = product(x, xl, t / mt, x, xl, t % mt, s.n_pad, false);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) a[(t / mt * 16 + 4 * q + e) * al + t % mt * 16 + r] = v[e];
-        }
-        __syncthreads();
-        for (int t = wave; t < mt * mt; t += SMALL_WAVES) {
-            const f32x4 v = product(a, al, t / mt, a, al, t % mt, s.m_pad, false);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int at = (t / mt * 16 + 4 * q + e) * al + t % mt * 16 + r;
-                b[at] = fmaf(k.b, a[at], k.c * v[e]);
+    // u u' for a symmetric result, its tiles to `to`; few tiles: each sum over several waves, joined in order
+    const int tiles = mt * mt;
+    f32x4 *joined = (f32x4 *)(b + s.m_pad * al);
+    auto square = [&](const float *u, int ul, int K, int slices, auto to) {
+        if (slices == 1) {
+            for (int t = wave; t < tiles; t += SMALL_WAVES)
+                to(t, product(u, ul, t / mt, u, ul, t % mt, 0, K, std::false_type{}));   // mirrored tiles: the same roundings
+        } else {
+            const int t = wave % tiles, at = wave / tiles, k = K / 16;
+            joined[threadIdx.x] = product(u, ul, t / mt, u, ul, t % mt, k * at / slices * 16, k * (at + 1) / slices * 16, std::false_type{});
+            __syncthreads();
+            if (wave < tiles) {
+                f32x4 v = joined[threadIdx.x];
+                for (int i = 1; i < slices; ++i) v += joined[threadIdx.x + i * tiles * 64];
+                to(wave, v);
             }
         }
         __syncthreads();
-        f32x4 now[SMALL_TILES];
+    };
+    for (int it = 0; it < s.steps; ++it) {
+        const Step k = it ? s.step[it] : first.step;
+        square(x, xl, s.n_pad, small_slices(s.m_pad, s.n_pad), [&](int tile, const f32x4 &v) {
 #pragma unroll
-        for (int u = 0; u < SMALL_TILES; ++u) {
+            for (int e = 0; e < 4; ++e) a[(tile / mt * 16 + 4 * q + e) * al + tile % mt * 16 + r] = v[e];
+        });
+        square(a, al, s.m_pad, 1, [&](int tile, const f32x4 &v) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at = (tile / mt * 16 + 4 * q + e) * al + tile % mt * 16 + r;
+                b[at] = fmaf(k.b, a[at], k.c * v[e]);
+            }
+        });
+        f32x4 now[TILES];
+#pragma unroll
+        for (int u = 0; u < TILES; ++u) {
             const int t = wave + u * SMALL_WAVES;
-            if (t < mt * nt) now[u] = product(b, al, t / nt, x, xl, t % nt, s.m_pad, true);
+            if (t < mt * nt) now[u] = product(b, al, t / nt, x, xl, t % nt, 0, s.m_pad, std::true_type{});
         }
         __syncthreads();
 #pragma unroll
-        for (int u = 0; u < SMALL_TILES; ++u) {
+        for (int u = 0; u < TILES; ++u) {
             const int t = wave + u * SMALL_WAVES;
             if (t < mt * nt)
 #pragma unroll
@@ -428,11 +476,16 @@ void orthogonalize(const boa_orth &d, Arena &mem, bool run, hipStream_t st)
         s.steps = d.steps, s.eps = d.eps;
         for (int i = 0; i < d.steps; ++i) s.step[i] = coefficients(i);
         const size_t lds = (size_t)small_bytes(m_pad, n_pad);
-        auto small = [&](auto t) {
-            const auto kernel = small_kernel<decltype(t)>;
+        auto launch = [&](auto kernel) {
             if (lds > 60 << 10)   // has to be asked for
                 (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, SMALL_LDS);
             kernel<<<dim3((uint32_t)d.count), 64 * SMALL_WAVES, lds, st>>>(s);
+        };
+        auto small = [&](auto t) {
+            const int32_t each = (int32_t)ceil_div(m_pad / 16 * (n_pad / 16), SMALL_WAVES);
+            if (each == 1) launch(small_kernel<decltype(t), 1>);
+            else if (each <= 4) launch(small_kernel<decltype(t), 4>);
+            else launch(small_kernel<decltype(t), SMALL_TILES>);
         };
         if (d.dtype == BOA_T_F32) small(0.0f);
         else if (d.dtype == BOA_T_BF16) small(bf16_t{});

@@ -128,7 +128,8 @@ def update(rows, cols, dt, seed, rank=None):
 
 
 SHAPES = [(1, 1), (1, 7), (9, 1), (2, 3), (8, 8), (17, 5), (31, 32), (32, 96), (64, 64), (65, 63), (96, 33), (100, 413), (127, 127),
-          (128, 128), (129, 127), (128, 300), (257, 129), (130, 1000), (300, 301), (520, 264), (264, 776)]
+          (128, 128), (129, 127), (128, 300), (257, 129), (130, 1000), (300, 301), (520, 264), (264, 776), (7, 200), (16, 1030), (513, 31),
+          (18, 191), (64, 480), (64, 481)]
 
 
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
