@@ -328,6 +328,7 @@ struct CopyArgs {
     void *dst;
     int64_t ld, rows;
     int32_t cols, pad;
+    int32_t across;   // of parts by column: log2 of the threads along a row
     float *most;   // of parts: the largest magnitude per row or column
 };
 
@@ -420,18 +421,24 @@ __global__ __launch_bounds__(256) void col_max_kernel(CopyArgs a)
     atomicMax((uint32_t *)a.most + c, __float_as_uint(m));
 }
 
-// Parts scaled by column: 32 rows of the first part and of the second alternate, with rows of zeros at the end.
+// Parts scaled by column: 32 rows of the first part and of the second
+// alternate, with rows of zeros at the end. A thread has 8 columns, whose scales
+// it works out once, of every few rows: of a block's threads 2^across lie side by side.
 __global__ __launch_bounds__(256) void col_parts_kernel(CopyArgs a)
 {
-    const int64_t chunks = a.pad / 8, n = (a.rows + 31) / 32 * 32 * chunks;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / chunks;
-        const int32_t c = (int32_t)(i % chunks) * 8;
-        float v[8];
-        int s[8];
-        read8(v, (const float *)a.src + min(r, a.rows - 1) * a.ld, c, r < a.rows ? a.cols : 0);
+    const int32_t c = ((int32_t)(blockIdx.x << a.across) + (threadIdx.x & ((1 << a.across) - 1))) * 8, step = 256 >> a.across;
+    if (c >= a.pad) return;
+    int s[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = c + e < a.cols ? up(a.most[c + e]) : 0;
+    for (int e = 0; e < 8; ++e) s[e] = c + e < a.cols ? up(a.most[c + e]) : 0;
+    const int64_t deep = (a.rows + 31) / 32 * 32;
+#pragma unroll 4
+    for (int64_t r = (int64_t)blockIdx.y * step + (threadIdx.x >> a.across); r < deep; r += (int64_t)gridDim.y * step) {
+        float v[8];
+        read8(v, (const float *)a.src + min(r, a.rows - 1) * a.ld, c, a.cols);
+        if (r >= a.rows)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = 0.0f;
         write_parts(v, s, (f16_t *)a.dst + (r / 32 * 64 + r % 32) * a.pad + c, 32 * (int64_t)a.pad);
     }
 }
@@ -764,7 +771,10 @@ Operand col_parts(const void *src, int64_t ld, int64_t rows, int32_t cols, float
         const int64_t strips = ceil_div(cols, 256), down = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 32), 2048 / strips));
         col_max_kernel<<<dim3((uint32_t)strips, (uint32_t)down), 256, 0, st>>>(c);
     }
-    col_parts_kernel<<<spread(deep * (c.pad / 8)), 256, 0, st>>>(c);
+    while (c.across < 5 && 8 << c.across < c.pad) ++c.across;
+    const int64_t wide = ceil_div(c.pad, 8 << c.across);
+    const int64_t down = std::max<int64_t>(1, std::min<int64_t>(ceil_div(deep, 256 >> c.across), 2048 / wide));
+    col_parts_kernel<<<dim3((uint32_t)wide, (uint32_t)down), 256, 0, st>>>(c);
     return o;
 }
 
@@ -866,7 +876,7 @@ void backward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
         if (d.dw && (s.dz || d.dbias)) s.most = most_z;   // the kernel runs anyway
     }
     const int64_t strips = ceil_div(d.N, 256);
-    const int32_t stripes = (int32_t)std::max<int64_t>(1, std::min<int64_t>(ceil_div(M, 64), std::max<int64_t>(1, 2048 / strips)));
+    const int32_t stripes = (int32_t)std::max<int64_t>(1, std::min<int64_t>(ceil_div(M, 16), std::max<int64_t>(1, 2048 / strips)));
     if (d.dbias) s.partial = (float *)mem.take((int64_t)stripes * d.N * 4);
     if (run && (s.dz || d.dbias)) slope_kernel<TO><<<dim3((uint32_t)strips, (uint32_t)stripes), 256, 0, st>>>(s);
     if (run && d.dbias) {
