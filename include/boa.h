@@ -410,6 +410,7 @@ int boa_matvec_fourbit(const void *x, int64_t M, int64_t x_stride, int32_t dtype
                        int32_t scale_dtype, int32_t group, void *y, int64_t y_stride, void *stream);
 
 #define BOA_MAX_LINEAR (1 << 17)
+#define BOA_MAX_LINEAR_ROWS 2147483392   /* 2^31 - 256 */
 #define BOA_LINEAR_FEW 64       /* rows up to which a 16-bit forward pass takes no work memory, */
 #define BOA_LINEAR_FEW_F32 16   /* and a float32 one */
 enum { BOA_ACT_NONE = 0, BOA_ACT_RELU = 1, BOA_ACT_SILU = 2, BOA_ACT_GELU = 3, BOA_ACT_GELU_TANH = 4 };
@@ -431,7 +432,7 @@ enum { BOA_ACT_NONE = 0, BOA_ACT_RELU = 1, BOA_ACT_SILU = 2, BOA_ACT_GELU = 3, B
 typedef struct {
     int32_t dtype;          /* any of the three */
     int32_t activation;     /* BOA_ACT_* */
-    int64_t M;              /* 0 .. 2^31 - 1 */
+    int64_t M;              /* 0 .. BOA_MAX_LINEAR_ROWS */
     int32_t N, K;           /* 1 .. BOA_MAX_LINEAR */
     const void *x;          /* M x K */
     int64_t x_stride;

@@ -41,10 +41,11 @@ __device__ inline f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_a
 __device__ inline f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 // One operand: rows `ld` values apart from a 16-byte aligned address, ld a
-// multiple of 8 and below 2^21, whole 16-byte chunks in every row. Of parts, the second lies `part` values
-// behind the first, and 32 values of k lie `block` values from the next 32 (along
-// k: 32 where the parts are two matrices, 64 where they alternate). own: the operand's extent in the output.
-// batch: from one product of a batch to the next.
+// multiple of 8 and below 2^21, whole 16-byte chunks in every row. Of parts, the
+// second lies `part` values behind the first, and 32 values of k lie `block`
+// values from the next 32 (along k: 32 where the parts are two matrices, 64 where
+// they alternate). own: the operand's extent in the output. batch: from one
+// product of a batch to the next.
 struct Operand {
     const void *p;
     int64_t ld, part, block, batch;
@@ -57,6 +58,7 @@ struct Product {
     int32_t tiles_a, tiles_b, splits, batches;
     int32_t steps;     // stages of k a split takes
     int32_t symmetric; // the output is: tiles with ta <= tb only
+    uint32_t first;    // work item of this launch's first block
 };
 
 // A block's tile: WA x WB waves of TA x TB tiles of 32 x 32, 64 values of k a
@@ -234,7 +236,7 @@ __device__ inline Place place_of(const Product &pr)
 {
     const uint32_t n = gridDim.x, id = blockIdx.x;
     const uint32_t x = id & 7, per = n >> 3, extra = n & 7;
-    uint32_t t = x * per + min(x, extra) + (id >> 3);
+    uint32_t t = pr.first + x * per + min(x, extra) + (id >> 3);
     const uint32_t tiles = tiles_of(pr);
     Place w;
     const uint32_t layer = t / tiles;
@@ -398,9 +400,8 @@ struct Nothing {
 
 // Hands the sums out in runs of eight neighbouring columns: f(row of a's side,
 // first column of b's side, the eight sums in LDS, kept). A lane keeps its columns
-// over every `step`th row: kept is what(first row, column, step), asked for once (addresses,
-// the columns' bias), and kept.down() takes it a step on.
-// Each wave turns its tiles over in its own piece of LDS, two columns of tiles at
+// over every `step`th row: kept is what(first row, column, step), asked for once
+// (addresses, the columns' bias), and kept.down() takes it a step on. Each wave turns its tiles over in its own piece of LDS, two columns of tiles at
 // a time, so that what follows is written once, and stores fill whole lines.
 // `turned`: g(first row, column, eight sums down that column) for all of them
 // too, for a transposed output. The stages must no longer be in use.
@@ -473,8 +474,10 @@ inline uint32_t spread(int64_t items) { return (uint32_t)std::max<int64_t>(1, st
 
 // The tiles there are: 256 x 256 for large outputs; 128 x 128, two at once on a
 // CU, or one with its loads four stages ahead where a CU gets no second; 64 x 64,
-// four at once, or two with two sets of waves, or one of those with its loads four stages ahead. A smaller tile reads more of LDS for the same
-// products: 1,170, 980 and 630 TFLOP/s where there are tiles enough (k = 4,096).
+// four at once, or two with two sets of waves, or one of those with its loads
+// four stages ahead. A smaller tile reads more of LDS for the same products:
+// 1,170, 980 and 630 TFLOP/s where there are tiles enough (k = 4,096); it is taken
+// where the larger would leave CUs without one.
 template <class T>
 using Large = Tile<T, 4, 2, 2, 4, 1, 2, 1>;
 template <class T>
@@ -493,6 +496,14 @@ struct Cut {
     int shape, splits;
     int32_t steps;   // stages of k a split takes
 };
+
+// f(first block, blocks) for the launches that a number of blocks takes: one may not have 2^32 threads.
+template <class F>
+void in_launches(int64_t blocks, int32_t threads, F f)
+{
+    const int64_t most = ((int64_t)1 << 31) / threads;
+    for (int64_t at = 0; at < blocks; at += most) f((uint32_t)at, (uint32_t)std::min(most, blocks - at));
+}
 
 // f with the tile of a shape
 template <class T, class F>

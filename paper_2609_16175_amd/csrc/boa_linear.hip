@@ -6,8 +6,8 @@
 //
 // A few rows (serving) read the weights once and are bound by that; more are
 // bound by the matrix instructions. 16-bit operands go there as they are, with
-// float32 sums; z is kept for the backward pass in f16 (11 bits, clamped to its
-// range, where every activation's slope is constant), and dz, an operand of two
+// float32 sums; z is kept for the backward pass in f16 (11 bits, infinite
+// beyond its range, where every activation's slope is constant), and dz, an operand of two
 // products, is rounded to the layer's type. Float32 operands become two f16
 // parts of 11 bits each, scaled by a power of two per row (or per column, where
 // the sum runs over rows) so that the largest value lies below 2^15: three
@@ -702,7 +702,10 @@ void launch(Product pr, const Epilogue &e, hipStream_t st)
     const auto kernel = product_kernel<S, ACROSS_A, ACROSS_B, TO>;
     if (S::LDS > 64 << 10)   // has to be asked for
         (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
-    kernel<<<dim3((uint32_t)((int64_t)pr.tiles_a * pr.tiles_b * pr.splits)), S::THREADS, S::LDS, st>>>(pr, e);
+    in_launches((int64_t)pr.tiles_a * pr.tiles_b * pr.splits, S::THREADS, [&](uint32_t first, uint32_t blocks) {
+        pr.first = first;
+        kernel<<<dim3(blocks), S::THREADS, S::LDS, st>>>(pr, e);
+    });
 }
 
 // out = a b^T with its epilogue; T: the operands' type in the product, TO: the layer's.
@@ -794,7 +797,7 @@ int check(const char *what, const boa_dense *d, bool grad)
     const int32_t last = BOA_ACT_GELU_TANH;
     if (!dtype_known(d->dtype)) why = "unknown dtype";
     else if (d->activation < 0 || d->activation > last) why = "unknown activation";
-    else if (d->M < 0 || d->M >= (int64_t)1 << 31) why = "M out of range [0, 2^31)";
+    else if (d->M < 0 || d->M > BOA_MAX_LINEAR_ROWS) why = "M out of range [0, 2^31 - 256]";
     else if (d->N < 1 || d->N > BOA_MAX_LINEAR) why = "N out of range [1, 2^17]";
     else if (d->K < 1 || d->K > BOA_MAX_LINEAR) why = "K out of range [1, 2^17]";
     else if (d->M > 1 && d->x_stride < d->K) why = "x's row stride smaller than K";

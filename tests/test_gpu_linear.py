@@ -350,3 +350,16 @@ def test_offsets_pass_32_bits():
     dx, dw, db = boa.linear_backward(y, x, w, pre, activation="relu", need=(True, False, False))
     at = slice(M - 100, M)
     check(x[at].cpu(), w.cpu(), None, None, "relu", BF16, None, y[at].cpu(), (dx[at], None, None), BF16)
+
+
+def test_more_tiles_than_a_launch_takes():
+    # 2^24 tiles of 64 rows and more, 2^23 a launch
+    M, N, K = (1 << 30) + 100, 1, 8
+    g = torch.Generator("cuda").manual_seed(2)
+    x = torch.empty(M, K, device="cuda", dtype=BF16).normal_(generator=g)
+    w = torch.randn(N, K, device="cuda", generator=g).bfloat16()
+    y, _ = boa.linear_forward(x, w)
+    dx, _, _ = boa.linear_backward(y, x, w, need=(True, False, False))
+    for at in (slice(0, 100), slice((1 << 29) - 50, (1 << 29) + 50), slice(M - 200, M)):
+        check(x[at].cpu(), w.cpu(), None, None, "none", BF16, y[at], y[at].cpu(), (dx[at], None, None), BF16)
+    torch.testing.assert_close(y[::1009, 0].float(), x[::1009].float() @ w[0].float(), rtol=2.0 ** -7, atol=2.0 ** -16)

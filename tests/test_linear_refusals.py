@@ -30,7 +30,7 @@ def _err():
 
 
 BOTH = [(dict(dtype=3), "dtype"), (dict(activation=5), "activation"), (dict(activation=-1), "activation"),
-        (dict(M=-1), "M out of range"), (dict(M=1 << 31), "M out of range"), (dict(N=0), "N out of range"),
+        (dict(M=-1), "M out of range"), (dict(M=1 << 31), "M out of range"), (dict(M=(1 << 31) - 255), "M out of range"), (dict(N=0), "N out of range"),
         (dict(N=(1 << 17) + 1), "N out of range"), (dict(K=0), "K out of range"), (dict(K=(1 << 17) + 1), "K out of range"),
         (dict(x_stride=23), "x's row stride"), (dict(w_stride=23), "w's row stride"), (dict(param_dtype=2), "bias"),
         (dict(x=None), "NULL x"), (dict(w=None), "NULL w")]
