@@ -411,8 +411,7 @@ int boa_matvec_fourbit(const void *x, int64_t M, int64_t x_stride, int32_t dtype
 
 #define BOA_MAX_LINEAR (1 << 17)
 #define BOA_MAX_LINEAR_ROWS 2147483392   /* 2^31 - 256 */
-#define BOA_LINEAR_FEW 64       /* rows up to which a 16-bit forward pass takes no work memory, */
-#define BOA_LINEAR_FEW_F32 16   /* and a float32 one */
+#define BOA_LINEAR_FEW 16   /* rows up to which a forward pass takes no work memory */
 enum { BOA_ACT_NONE = 0, BOA_ACT_RELU = 1, BOA_ACT_SILU = 2, BOA_ACT_GELU = 3, BOA_ACT_GELU_TANH = 4 };
 /*
  * A linear layer on M rows, with what follows it:
@@ -424,7 +423,7 @@ enum { BOA_ACT_NONE = 0, BOA_ACT_RELU = 1, BOA_ACT_SILU = 2, BOA_ACT_GELU = 3, B
  * Sums are float32. In bfloat16 and float16, z is kept in float16, infinite beyond
  * its range (where every act' is constant), and dz is rounded to the layer's type
  * as an operand of the two products, not in dbias. In float32, with more than
- * BOA_LINEAR_FEW_F32 rows or in the gradients, the products' operands are
+ * 16 to 128 rows (by N and K) and in the gradients, the products' operands are
  * rounded to 22 bits (values far below the largest of their row, or of their
  * column where the sum runs over rows, to 2^-40 of that). A non-finite value
  * makes the results that it takes part in NaN or infinite.

@@ -561,127 +561,99 @@ struct FewArgs {
     Epilogue e;
 };
 
-// 16 rows of weights a block; its 16 waves share k and their sums are added
-// through LDS in order. Fragments come straight from memory: every weight is
-// read once, every state by each block from the cache. Rows past the end are
-// read as the last one, and what they give is dropped.
+constexpr int FEW_WAVES = 16, FEW_MOST = 8;   // FEW_MOST x 16 rows of x at most
+
+// What a lane gives to the matrix instructions at a time: 16 bytes of a row, 8
+// values of 16 bits for one of them or 4 float32 values for four (whose k are
+// then not in their order, which the sum does not mind).
+template <class T>
+struct Few {
+    typedef typename Vec<T>::v8 V;
+    static constexpr int PER = 8;
+    static __device__ f32x4 times(V w, V x, f32x4 acc) { return mfma16(w, x, acc); }
+};
+template <>
+struct Few<float> {
+    typedef f32x4 V;
+    static constexpr int PER = 4;
+    static __device__ f32x4 times(V w, V x, f32x4 acc)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], x[e], acc, 0, 0, 0);
+        return acc;
+    }
+};
+
+// 16 rows of weights and 16 MT of x a block; its 16 waves share k and their sums
+// are added through LDS in order. Fragments come straight from memory: every weight
+// is read once, every state by each block from the cache. Rows past the end are
+// read as the last one, and what they give is dropped. Bound by memory where there
+// are blocks enough (1 x 4096 x 4096: 7.2 us in bfloat16, 15.5 in float32, 4.3 to
+// 4.7 TB/s), else by the latency of a block's k (1 x 768 x 768: 3.5 and 4.3 us; 1 x
+// 4096 x 1024: 6.7 and 11.8). Blocks of 8 or 4 rows of weights, of which there are
+// more, take as long or longer: a wave asks for as many lines.
 template <class T, int MT>
-__global__ __launch_bounds__(1024) void few_kernel(FewArgs a)
+__global__ __launch_bounds__(64 * FEW_WAVES) void few_kernel(FewArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    typedef typename Vec<T>::v8 v8;
-    constexpr int WAVES = 16;
+    typedef typename Few<T>::V V;
+    constexpr int PER = Few<T>::PER, STEP = 4 * PER;   // k of a step
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, part = lane >> 4;
     const int32_t n0 = blockIdx.x * 16;
     const T *w = (const T *)a.w + (int64_t)min(n0 + r, a.N - 1) * a.w_ld;
     const T *x[MT];
 #pragma unroll
     for (int j = 0; j < MT; ++j) x[j] = (const T *)a.x + (int64_t)min(j * 16 + r, a.M - 1) * a.x_ld;
-    const int32_t whole = a.K / 32, each = (whole + WAVES - 1) / WAVES;
+    const int32_t whole = a.K / STEP, each = (whole + FEW_WAVES - 1) / FEW_WAVES;
     const int32_t end = min(whole, (wave + 1) * each);
-    auto eight = [](const T *p) { return __builtin_bit_cast(v8, (words4) * (const loose4 *)p); };
+    auto get = [](const T *p) { return __builtin_bit_cast(V, (words4) * (const loose4 *)p); };
     f32x4 acc[MT];
 #pragma unroll
     for (int j = 0; j < MT; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int AHEAD = MT == 1 ? 8 : MT == 2 ? 4 : 2;   // steps whose loads are on their way together
+    constexpr int AHEAD = MT == 1 ? 8 : MT == 2 ? 4 : MT == 4 ? 2 : 1;   // steps whose loads are on their way together
     for (int32_t s = wave * each; s < end; s += AHEAD) {
-        v8 fw[AHEAD], fx[AHEAD][MT];
+        V fw[AHEAD], fx[AHEAD][MT];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
             if (s + u < end) {
-                const int32_t k = (s + u) * 32 + part * 8;
-                fw[u] = eight(w + k);
+                const int32_t k = (s + u) * STEP + part * PER;
+                fw[u] = get(w + k);
 #pragma unroll
-                for (int j = 0; j < MT; ++j) fx[u][j] = eight(x[j] + k);
+                for (int j = 0; j < MT; ++j) fx[u][j] = get(x[j] + k);
             }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
             if (s + u < end) {
 #pragma unroll
-                for (int j = 0; j < MT; ++j) acc[j] = mfma16(fw[u], fx[u][j], acc[j]);
+                for (int j = 0; j < MT; ++j) acc[j] = Few<T>::times(fw[u], fx[u][j], acc[j]);
             }
     }
-    if (a.K % 32 && wave == WAVES - 1) {   // the last values of k, zeros past them
+    if (a.K % STEP && wave == FEW_WAVES - 1) {   // the last values of k, zeros past them
         auto some = [&](const T *p) {
-            v8 f;
+            V f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int32_t k = whole * 32 + part * 8 + e;
+            for (int e = 0; e < PER; ++e) {
+                const int32_t k = whole * STEP + part * PER + e;
                 f[e] = k < a.K ? p[k] : (T)0.0f;
             }
             return f;
         };
-        const v8 fw = some(w);
+        const V fw = some(w);
 #pragma unroll
-        for (int j = 0; j < MT; ++j) acc[j] = mfma16(fw, some(x[j]), acc[j]);
+        for (int j = 0; j < MT; ++j) acc[j] = Few<T>::times(fw, some(x[j]), acc[j]);
     }
     float *sums = (float *)lds;   // [wave][row of x][row of w]
 #pragma unroll
     for (int j = 0; j < MT; ++j) *(f32x4 *)(sums + ((wave * MT + j) * 16 + r) * 16 + part * 4) = acc[j];
     __syncthreads();
-    if (threadIdx.x < MT * 256) {
+    for (int i = threadIdx.x; i < MT * 256; i += 64 * FEW_WAVES) {
         float v = 0.0f;
 #pragma unroll
-        for (int k = 0; k < WAVES; ++k) v += sums[k * MT * 256 + threadIdx.x];
-        const int32_t m = threadIdx.x >> 4, n = n0 + (threadIdx.x & 15);
+        for (int k = 0; k < FEW_WAVES; ++k) v += sums[k * MT * 256 + i];
+        const int32_t m = i >> 4, n = n0 + (i & 15);
         if (m < a.M && n < a.N) {
             const float bias = bias_at<T>(a.e, n);
             with_act(a.e.act, [&](auto act) { finish_one<T, decltype(act)::value>(a.e, m, n, v, bias); });
-        }
-    }
-}
-
-// The same in float32: four rows of weights a block, whose 8 waves share k.
-template <int MB>
-__global__ __launch_bounds__(512) void few_f32_kernel(FewArgs a)
-{
-    constexpr int WAVES = 8, ROWS = 4;
-    __shared__ float sums[WAVES][MB * ROWS];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int32_t n0 = blockIdx.x * ROWS;
-    float acc[MB][ROWS] = {};
-    const float *w[ROWS], *x[MB];
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) w[i] = (const float *)a.w + (int64_t)min(n0 + i, a.N - 1) * a.w_ld;
-#pragma unroll
-    for (int m = 0; m < MB; ++m) x[m] = (const float *)a.x + (int64_t)min(m, a.M - 1) * a.x_ld;
-    const int32_t whole = a.K / 4 * 4;
-    for (int32_t k = threadIdx.x * 4; k < whole; k += WAVES * 256) {
-        float fw[ROWS][4];
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) load_loose<4, float>(fw[i], w[i] + k);
-#pragma unroll
-        for (int m = 0; m < MB; ++m) {
-            float fx[4];
-            load_loose<4, float>(fx, x[m] + k);
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[m][i] = fmaf(fx[e], fw[i][e], acc[m][i]);
-        }
-    }
-    if (const int32_t k = whole + (int32_t)threadIdx.x; k < a.K) {
-#pragma unroll
-        for (int m = 0; m < MB; ++m)
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i) acc[m][i] = fmaf(x[m][k], w[i][k], acc[m][i]);
-    }
-#pragma unroll
-    for (int m = 0; m < MB; ++m)
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            const float s = wave_sum(acc[m][i]);
-            if (lane == 0) sums[wave][m * ROWS + i] = s;
-        }
-    __syncthreads();
-    if (threadIdx.x < MB * ROWS) {
-        float v = 0.0f;
-#pragma unroll
-        for (int k = 0; k < WAVES; ++k) v += sums[k][threadIdx.x];
-        const int32_t m = threadIdx.x / ROWS, n = n0 + threadIdx.x % ROWS;
-        if (m < a.M && n < a.N) {
-            const float bias = bias_at<float>(a.e, n);
-            with_act(a.e.act, [&](auto act) { finish_one<float, decltype(act)::value>(a.e, m, n, v, bias); });
         }
     }
 }
@@ -788,7 +760,17 @@ int with_type(int32_t dtype, F f)
     return dtype == BOA_T_BF16 ? f(bf16_t{}) : f(f16_t{});
 }
 
-int few_rows(int32_t dtype) { return dtype == BOA_T_F32 ? BOA_LINEAR_FEW_F32 : BOA_LINEAR_FEW; }
+// Whether a forward product is done by few_kernel. It takes a time for every row
+// of x and k, the tiles one for every weight in float32 (their parts) and nearly
+// the same whatever M: 32 x 1024 x 4096 in bfloat16 5.4 us (tiles 6.8), 64 x 1024
+// x 4096 7.4 (6.9), 32 x 4096 x 1024 13.0 (9.2); in float32 128 x 1024 x 4096 20
+// (27), 64 x 4096 x 4096 45 (59), 128 x 4096 x 4096 68 (66), 64 x 4096 x 1024 44 (32).
+bool is_few(int64_t M, int64_t N, int64_t K, int32_t dtype)
+{
+    if (M <= BOA_LINEAR_FEW) return true;
+    if (dtype != BOA_T_F32) return M <= 64 && M * K <= 49152;
+    return M <= 16 * FEW_MOST && ceil_div(M, 16) * 16 * K * ceil_div(N, 4096) <= 71000 + N * K / 64;
+}
 
 int check(const char *what, const boa_dense *d, bool grad)
 {
@@ -826,22 +808,19 @@ void forward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
     e.out = d.y, e.ld = d.N, e.bias = d.bias, e.bias_f32 = d.param_dtype == BOA_T_F32;
     e.residual = d.residual, e.residual_ld = d.residual_stride, e.pre = d.pre, e.act = d.activation;
     e.rows = M, e.cols = d.N;
-    if (M <= few_rows(d.dtype)) {
+    if (is_few(M, d.N, d.K, d.dtype)) {
         if (!run) return;
-        FewArgs a{d.x, d.w, d.x_stride, d.w_stride, M, d.N, d.K, e};
-        if constexpr (WIDE) {
-            const dim3 grid((uint32_t)ceil_div(d.N, 4));
-            if (M <= 1) few_f32_kernel<1><<<grid, 512, 0, st>>>(a);
-            else if (M <= 2) few_f32_kernel<2><<<grid, 512, 0, st>>>(a);
-            else if (M <= 4) few_f32_kernel<4><<<grid, 512, 0, st>>>(a);
-            else if (M <= 8) few_f32_kernel<8><<<grid, 512, 0, st>>>(a);
-            else few_f32_kernel<16><<<grid, 512, 0, st>>>(a);
-        } else {
-            const dim3 grid((uint32_t)ceil_div(d.N, 16));
-            if (M <= 16) few_kernel<T, 1><<<grid, 1024, 16 << 10, st>>>(a);
-            else if (M <= 32) few_kernel<T, 2><<<grid, 1024, 32 << 10, st>>>(a);
-            else few_kernel<T, 4><<<grid, 1024, 64 << 10, st>>>(a);
-        }
+        const FewArgs a{d.x, d.w, d.x_stride, d.w_stride, M, d.N, d.K, e};
+        auto launch = [&](auto kernel, int mt) {
+            const int lds = FEW_WAVES * mt * 1024;
+            if (lds > 64 << 10)   // has to be asked for
+                (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+            kernel<<<dim3((uint32_t)ceil_div(d.N, 16)), 64 * FEW_WAVES, lds, st>>>(a);
+        };
+        if (M <= 16) launch(few_kernel<TO, 1>, 1);
+        else if (M <= 32) launch(few_kernel<TO, 2>, 2);
+        else if (M <= 64) launch(few_kernel<TO, 4>, 4);
+        else if constexpr (WIDE) launch(few_kernel<TO, FEW_MOST>, FEW_MOST);
         return;
     }
     if constexpr (WIDE) {

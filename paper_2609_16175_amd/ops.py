@@ -434,7 +434,7 @@ def matvec_4bit(x, codes, scales, offsets=None, group=None, stream=None):
 # linear layers
 
 _ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
-LINEAR_FEW, LINEAR_FEW_F32 = 64, 16   # rows up to which a forward pass takes no work memory
+LINEAR_FEW = 16   # rows up to which a forward pass takes no work memory
 
 
 def _activation(name, activation):
@@ -481,7 +481,7 @@ def linear_forward(x, weight, bias=None, residual=None, activation="none", keep=
     a = _pack_dense(dt, act, M, N, K, m.data_ptr(), _stride(m), w.data_ptr(), _stride(w), _address(b),
                     dt if b is None else _DTYPES[b.dtype], _address(r), 0 if r is None else _stride(r), y.data_ptr(), _address(pre),
                     0, 0, 0, 0, 0)
-    ws, n = _linear_workspace(x, a, 0) if M > (LINEAR_FEW_F32 if dt == T_F32 else LINEAR_FEW) else (None, 0)
+    ws, n = _linear_workspace(x, a, 0) if M > LINEAR_FEW else (None, 0)
     rc = _lib().boa_linear(a, _ptr(ws), n, _current_stream(x.get_device()))
     if rc:
         _check(rc)

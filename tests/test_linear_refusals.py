@@ -64,7 +64,7 @@ def test_workspace():
     assert size(0, M=8192, N=8192, K=8191, x_stride=8192, w_stride=8192, residual=None) == 2 * copy
     assert size(0, M=8192, N=8192, K=8192, x_stride=8192, w_stride=8192, residual=None, x=P + 2) == copy
     assert size(0, M=8192, N=8192, K=8192, x_stride=8192, w_stride=8192, residual=None, dtype=0, param_dtype=0) == 2 * (2 * copy + 8192 * 4)
-    assert _call(0, M=100, dtype=0, param_dtype=0, n=16) == EINVAL and "workspace" in _err()
+    assert _call(0, M=129, dtype=0, param_dtype=0, n=16) == EINVAL and "workspace" in _err()
     assert L.boa_linear_workspace(None, 0) == EINVAL and L.boa_linear(None, P, 0, None) == EINVAL
 
 
