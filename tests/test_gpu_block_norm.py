@@ -178,7 +178,7 @@ TYPES = [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16), (F16, F32)]
 @pytest.mark.parametrize("dt,pt", TYPES)
 @pytest.mark.parametrize("rows,d", [(1, 1), (1, 768), (3, 2), (5, 7), (2, 8), (5, 63), (7, 64), (4, 65), (9, 96), (33, 128), (17, 255),
                                     (6, 256), (8, 257), (19, 413), (64, 512), (5, 520), (30, 768), (3, 1000), (12, 1024),
-                                    (5, 1025), (3, 1536), (4, 2048), (3, 2055), (3, 4095), (3, 4096), (2, 4097), (2, 9000)])
+                                    (5, 1025), (3, 1536), (4, 2048), (3, 2055), (3, 4095), (3, 4096), (2, 4097), (3, 8192), (5, 8191), (2, 8193), (2, 9000)])
 def test_block_norm(rows, d, dt, pt):
     n = rows + d
     both(rows, d, dt, pt, n, gate=("features", "rows", None)[n % 3], norm=("layer", "rms")[n % 2], post=n % 5 != 0)
@@ -188,14 +188,14 @@ def test_block_norm(rows, d, dt, pt):
 @pytest.mark.parametrize("kind", ["layer", "rms"])
 @pytest.mark.parametrize("gate", [None, "features", "rows"])
 @pytest.mark.parametrize("post,pre", [(True, True), (True, False), (False, True), (False, False)])
-@pytest.mark.parametrize("d", [200, 4500])
+@pytest.mark.parametrize("d", [200, 4500, 8200])
 def test_every_form(d, post, pre, gate, kind, dt, pt):
     both(13, d, dt, pt, 3, post=post, pre=pre, gate=gate, norm=kind)
     both(13, d, dt, pt, 4, post=post, pre=pre, gate=gate, norm=kind, params=False)
 
 
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
-@pytest.mark.parametrize("rows,d", [(9000, 96), (3001, 413), (4200, 1024), (1100, 2048)])
+@pytest.mark.parametrize("rows,d", [(9000, 96), (3001, 413), (4200, 1024), (1100, 2048), (600, 8192), (70, 8200)])
 def test_many_rows(rows, d, dt):
     c, got, r = both(rows, d, dt, dt, d)
     again, r2 = call(c)
@@ -211,7 +211,7 @@ def test_strided_rows(gap, gate, dt):
     both(37, 5, dt, dt, 6, gap=gap, gate=gate)
 
 
-@pytest.mark.parametrize("d", [96, 5000])
+@pytest.mark.parametrize("d", [96, 5000, 9000])
 def test_one_of_the_gradients(d):
     c = case(21, d, F32, F32, 8)
     check(c | {"dh": None}, None, F32, F32, call(c | {"dh": None})[1])
