@@ -19,9 +19,9 @@
 // formed again from x and f in float32, which costs what reading it would and
 // keeps the digits that its rounding loses. A row stays in registers, as in
 // boa_norm.hip: backward a wave holds up to 512 values, two waves 1,024, four
-// 4,096, eight 8,192, so that a thread has 8 columns in most cases and 16 at most and the column sums
-// stay in registers too, over all rows of a block; they leave one partial row each
-// per block, added in block order.
+// 4,096, eight 8,192, so that a thread has 8 columns in most cases and 16 at most
+// and the column sums stay in registers too, over all rows of a block; they leave
+// one partial row each per block, added in block order.
 #include <algorithm>
 
 #include "boa_rows.h"
