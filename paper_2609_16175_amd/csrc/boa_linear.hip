@@ -336,11 +336,25 @@ struct CopyArgs {
     float *most;   // of parts: the largest magnitude per row or column
 };
 
+// What one launch copies: a job for each blockIdx.z.
+struct CopyJobs {
+    CopyArgs job[3];
+    int32_t n;
+    uint32_t x, y;   // blocks that the largest of them takes
+    void add(const CopyArgs &c, int64_t nx, int64_t ny)
+    {
+        job[n++] = c;
+        x = std::max(x, (uint32_t)nx), y = std::max(y, (uint32_t)ny);
+    }
+    dim3 grid() const { return dim3(x, y, (uint32_t)n); }
+};
+
 // Bound by memory and, in most uses, by its launch: x and w of 9,973 x 413 x 777
 // take 4 us each on average.
 template <class T>
-__global__ __launch_bounds__(256) void pad_kernel(CopyArgs a)
+__global__ __launch_bounds__(256) void pad_kernel(CopyJobs jobs)
 {
+    const CopyArgs &a = jobs.job[blockIdx.z];
     const int64_t chunks = a.pad / 8, n = a.rows * chunks;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / chunks;
@@ -389,8 +403,9 @@ __device__ inline void write_parts(const float (&v)[8], const int (&s)[8], f16_t
 // alternate, up to `pad` of each: a wave per row, which it reads twice (the second
 // time from the cache). Bound by memory: x, w and dz of 10,000 x 768 x 1024 take 36
 // us, 4.2 TB/s.
-__global__ __launch_bounds__(256) void row_parts_kernel(CopyArgs a)
+__global__ __launch_bounds__(256) void row_parts_kernel(CopyJobs jobs)
 {
+    const CopyArgs &a = jobs.job[blockIdx.z];
     const int lane = threadIdx.x & 63;
     for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows; r += (int64_t)gridDim.x * 4) {
         const float *from = (const float *)a.src + r * a.ld;
@@ -420,14 +435,15 @@ __global__ __launch_bounds__(256) void zero_kernel(T *p, int64_t n)
 
 // Largest magnitudes per column: the maximum of bit patterns, whose order does not
 // matter. x and w of 10,000 x 768 x 1024: 9 us each, latency.
-__global__ __launch_bounds__(256) void col_max_kernel(CopyArgs a)
+__global__ __launch_bounds__(256) void col_max_kernel(CopyJobs jobs)
 {
+    const CopyArgs &a = jobs.job[blockIdx.z];
     const int32_t c = blockIdx.x * 256 + threadIdx.x;
     if (c >= a.cols) return;
     float m = 0.0f;
 #pragma unroll 8
     for (int64_t r = blockIdx.y; r < a.rows; r += gridDim.y) m = fmaxf(m, finite_abs(((const float *)a.src)[r * a.ld + c]));
-    atomicMax((uint32_t *)a.most + c, __float_as_uint(m));
+    if (m > 0.0f) atomicMax((uint32_t *)a.most + c, __float_as_uint(m));
 }
 
 // Parts scaled by column: 32 rows of the first part and of the second
@@ -435,8 +451,9 @@ __global__ __launch_bounds__(256) void col_max_kernel(CopyArgs a)
 // it works out once, of every few rows: of a block's threads 2^across lie side by
 // side. Bound by memory: x, w and dz of 10,000 x 768 x 1024 take 43 us, 3.5 TB/s
 // (62 with the scales worked out at every run).
-__global__ __launch_bounds__(256) void col_parts_kernel(CopyArgs a)
+__global__ __launch_bounds__(256) void col_parts_kernel(CopyJobs jobs)
 {
+    const CopyArgs &a = jobs.job[blockIdx.z];
     const int32_t c = ((int32_t)(blockIdx.x << a.across) + (threadIdx.x & ((1 << a.across) - 1))) * 8, step = 256 >> a.across;
     if (c >= a.pad) return;
     int s[8];
@@ -714,7 +731,7 @@ void product(Operand a, Operand b, int32_t K, Epilogue e, Arena &mem, bool run, 
 
 // rows x cols at `src` as an operand, in place or copied.
 template <class T>
-Operand operand(const void *src, int64_t ld, int64_t rows, int32_t cols, bool across, Arena &mem, bool run, hipStream_t st)
+Operand operand(const void *src, int64_t ld, int64_t rows, int32_t cols, bool across, Arena &mem, CopyJobs &pads)
 {
     Operand o{};
     o.own = (int32_t)(across ? cols : rows);
@@ -726,12 +743,12 @@ Operand operand(const void *src, int64_t ld, int64_t rows, int32_t cols, bool ac
     c.src = src, c.ld = ld, c.rows = rows, c.cols = cols, c.pad = pad8(cols);
     c.dst = mem.take(rows * c.pad * 2);
     o.p = c.dst, o.ld = c.pad;
-    if (run) pad_kernel<T><<<spread(rows * (c.pad / 8)), 256, 0, st>>>(c);
+    pads.add(c, spread(rows * (c.pad / 8)), 1);
     return o;
 }
 
 // float32 rows x cols at `src` as two parts: along k scaled per row ...
-Operand row_parts(const void *src, int64_t ld, int64_t rows, int32_t cols, const float **most, Arena &mem, bool run, hipStream_t st)
+Operand row_parts(const void *src, int64_t ld, int64_t rows, int32_t cols, const float **most, Arena &mem, CopyJobs &jobs)
 {
     CopyArgs c{};
     c.src = src, c.ld = ld, c.rows = rows, c.cols = cols, c.pad = (int32_t)ceil_div(cols, 32) * 32;
@@ -740,13 +757,13 @@ Operand row_parts(const void *src, int64_t ld, int64_t rows, int32_t cols, const
     *most = c.most;
     Operand o{};
     o.own = (int32_t)rows, o.p = c.dst, o.ld = 2 * (int64_t)c.pad, o.part = 32, o.block = 64;
-    if (run) row_parts_kernel<<<dim3((uint32_t)std::min<int64_t>(ceil_div(rows, 4), 1 << 14)), 256, 0, st>>>(c);
+    jobs.add(c, std::min<int64_t>(ceil_div(rows, 4), 1 << 14), 1);
     return o;
 }
 
 // ... and across scaled per column. most: the magnitudes that the scales come
-// from, zeros unless they are known.
-Operand col_parts(const void *src, int64_t ld, int64_t rows, int32_t cols, float *most, bool known, Arena &mem, bool run, hipStream_t st)
+// from, zeros that a job of `maxima` raises unless they are known.
+Operand col_parts(const void *src, int64_t ld, int64_t rows, int32_t cols, float *most, bool known, Arena &mem, CopyJobs &maxima, CopyJobs &jobs)
 {
     CopyArgs c{};
     c.src = src, c.ld = ld, c.rows = rows, c.cols = cols, c.pad = pad8(cols), c.most = most;
@@ -754,15 +771,13 @@ Operand col_parts(const void *src, int64_t ld, int64_t rows, int32_t cols, float
     c.dst = mem.take(deep * 2 * c.pad * 2);
     Operand o{};
     o.own = cols, o.p = c.dst, o.ld = c.pad, o.part = 32 * (int64_t)c.pad, o.block = 64 * (int64_t)c.pad;
-    if (!run) return o;
     if (!known) {
-        const int64_t strips = ceil_div(cols, 256), down = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 32), 2048 / strips));
-        col_max_kernel<<<dim3((uint32_t)strips, (uint32_t)down), 256, 0, st>>>(c);
+        const int64_t strips = ceil_div(cols, 256);
+        maxima.add(c, strips, std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 32), 2048 / strips)));
     }
     while (c.across < 5 && 8 << c.across < c.pad) ++c.across;
     const int64_t wide = ceil_div(c.pad, 8 << c.across);
-    const int64_t down = std::max<int64_t>(1, std::min<int64_t>(ceil_div(deep, 256 >> c.across), 2048 / wide));
-    col_parts_kernel<<<dim3((uint32_t)wide, (uint32_t)down), 256, 0, st>>>(c);
+    jobs.add(c, wide, std::max<int64_t>(1, std::min<int64_t>(ceil_div(deep, 256 >> c.across), 2048 / wide)));
     return o;
 }
 
@@ -836,15 +851,18 @@ void forward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
         else if constexpr (WIDE) launch(few_kernel<TO, FEW_MOST>, FEW_MOST);
         return;
     }
+    CopyJobs jobs{};
+    Operand x{}, w{};
     if constexpr (WIDE) {
-        const Operand x = row_parts(d.x, d.x_stride, M, d.K, &e.max_a, mem, run, st);
-        const Operand w = row_parts(d.w, d.w_stride, d.N, d.K, &e.max_b, mem, run, st);
-        product<T, TO, false, false>(x, w, d.K, e, mem, run, st);
+        x = row_parts(d.x, d.x_stride, M, d.K, &e.max_a, mem, jobs);
+        w = row_parts(d.w, d.w_stride, d.N, d.K, &e.max_b, mem, jobs);
+        if (run) row_parts_kernel<<<jobs.grid(), 256, 0, st>>>(jobs);
     } else {
-        const Operand x = operand<T>(d.x, d.x_stride, M, d.K, false, mem, run, st);
-        const Operand w = operand<T>(d.w, d.w_stride, d.N, d.K, false, mem, run, st);
-        product<T, TO, false, false>(x, w, d.K, e, mem, run, st);
+        x = operand<T>(d.x, d.x_stride, M, d.K, false, mem, jobs);
+        w = operand<T>(d.w, d.w_stride, d.N, d.K, false, mem, jobs);
+        if (run && jobs.n) pad_kernel<T><<<jobs.grid(), 256, 0, st>>>(jobs);
     }
+    product<T, TO, false, false>(x, w, d.K, e, mem, run, st);
 }
 
 template <class TO>
@@ -879,43 +897,48 @@ void backward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
         if (d.param_dtype == BOA_T_F32) bias_join_kernel<float><<<grid, 256, 0, st>>>(s.partial, stripes, d.N, (float *)d.dbias);
         else bias_join_kernel<TO><<<grid, 256, 0, st>>>(s.partial, stripes, d.N, (TO *)d.dbias);
     }
+    // dz along k and w across give dx, both across give dw; what they need is copied in few launches
+    const bool dx = d.dx && M, dw = d.dw && M;
+    const float *rows_z = nullptr;
+    Operand z_dx{}, w_dx{}, z_dw{}, x_dw{};
+    if constexpr (WIDE) {
+        CopyJobs along{}, maxima{}, across{};
+        if (dx) {
+            z_dx = row_parts(dz, dz_ld, M, d.N, &rows_z, mem, along);
+            w_dx = col_parts(d.w, d.w_stride, d.N, d.K, most_w, false, mem, maxima, across);
+        }
+        if (dw) {
+            z_dw = col_parts(dz, dz_ld, M, d.N, most_z, s.most, mem, maxima, across);
+            x_dw = col_parts(d.x, d.x_stride, M, d.K, most_x, false, mem, maxima, across);
+        }
+        if (run && along.n) row_parts_kernel<<<along.grid(), 256, 0, st>>>(along);
+        if (run && maxima.n) col_max_kernel<<<maxima.grid(), 256, 0, st>>>(maxima);
+        if (run && across.n) col_parts_kernel<<<across.grid(), 256, 0, st>>>(across);
+    } else {
+        CopyJobs pads{};
+        z_dx.p = dz, z_dx.ld = M > 1 || s.dz ? dz_ld : s.pad;
+        z_dw = z_dx, z_dx.own = M, z_dw.own = d.N;
+        if (dx) w_dx = operand<T>(d.w, d.w_stride, d.N, d.K, true, mem, pads);
+        if (dw) x_dw = operand<T>(d.x, d.x_stride, M, d.K, true, mem, pads);
+        if (run && pads.n) pad_kernel<T><<<pads.grid(), 256, 0, st>>>(pads);
+    }
     Epilogue e{};
     e.act = BOA_ACT_NONE;
-    const int64_t kept = mem.used;   // the two products' memory takes turns
+    const int64_t kept = mem.used;   // the two products' sums take turns
     int64_t most = kept;
-    if (d.dx && M) {
-        e.out = d.dx, e.ld = d.K;
-        if constexpr (WIDE) {
-            const Operand a = row_parts(dz, dz_ld, M, d.N, &e.max_a, mem, run, st);
-            const Operand b = col_parts(d.w, d.w_stride, d.N, d.K, most_w, false, mem, run, st);
-            e.max_b = most_w;
-            product<T, TO, false, true>(a, b, d.N, e, mem, run, st);
-        } else {
-            Operand a{};
-            a.p = dz, a.ld = M > 1 || s.dz ? dz_ld : s.pad, a.own = M;
-            const Operand b = operand<T>(d.w, d.w_stride, d.N, d.K, true, mem, run, st);
-            product<T, TO, false, true>(a, b, d.N, e, mem, run, st);
-        }
-        most = std::max(most, mem.used);
+    if (dx) {
+        e.out = d.dx, e.ld = d.K, e.max_a = rows_z, e.max_b = most_w;
+        product<T, TO, false, true>(z_dx, w_dx, d.N, e, mem, run, st);
+        most = mem.used;
         mem.used = kept;
     }
-    if (d.dw) {
-        e.out = d.dw, e.ld = d.K;
-        if (M == 0) {
-            const int64_t n = (int64_t)d.N * d.K;
-            if (run) zero_kernel<TO><<<spread(n), 256, 0, st>>>((TO *)d.dw, n);
-        } else if constexpr (WIDE) {
-            const Operand a = col_parts(dz, dz_ld, M, d.N, most_z, s.most, mem, run, st);
-            const Operand b = col_parts(d.x, d.x_stride, M, d.K, most_x, false, mem, run, st);
-            e.max_a = most_z, e.max_b = most_x;
-            product<T, TO, true, true>(a, b, M, e, mem, run, st);
-        } else {
-            Operand a{};
-            a.p = dz, a.ld = M > 1 || s.dz ? dz_ld : s.pad, a.own = d.N;
-            const Operand b = operand<T>(d.x, d.x_stride, M, d.K, true, mem, run, st);
-            product<T, TO, true, true>(a, b, M, e, mem, run, st);
-        }
+    if (dw) {
+        e.out = d.dw, e.ld = d.K, e.max_a = most_z, e.max_b = most_x;
+        product<T, TO, true, true>(z_dw, x_dw, M, e, mem, run, st);
         most = std::max(most, mem.used);
+    } else if (d.dw) {
+        const int64_t n = (int64_t)d.N * d.K;
+        if (run) zero_kernel<TO><<<spread(n), 256, 0, st>>>((TO *)d.dw, n);
     }
     mem.used = most;
 }
