@@ -229,12 +229,11 @@ __host__ __device__ inline uint32_t tiles_of(const Product &pr)
 // Whether a symmetric output's work item is a tile on or above the diagonal.
 __device__ inline bool is_needed(const Product &pr, const Place &w) { return !pr.symmetric || (w.ta <= w.tb && w.tb < pr.tiles_b); }
 
-// Work item of a block. Blocks go to the 8 XCDs in turn; each XCD takes a run of
+// Work item of block id of n. Blocks go to the 8 XCDs in turn; each XCD takes a run of
 // tiles that share operand rows in its L2: bands of 8 tiles of a, one tile of b
 // after the other.
-__device__ inline Place place_of(const Product &pr)
+__device__ inline Place place_of(const Product &pr, uint32_t id, uint32_t n)
 {
-    const uint32_t n = gridDim.x, id = blockIdx.x;
     const uint32_t x = id & 7, per = n >> 3, extra = n & 7;
     uint32_t t = pr.first + x * per + min(x, extra) + (id >> 3);
     const uint32_t tiles = tiles_of(pr);
@@ -496,6 +495,7 @@ struct Cut {
     int shape, splits;
     int32_t steps;   // stages of k a split takes
 };
+constexpr int SMALL = 3;   // Small's shape
 
 // f(first block, blocks) for the launches that a number of blocks takes: one may not have 2^32 threads.
 template <class F>
@@ -512,7 +512,7 @@ void with_tile(int shape, F f)
     if (shape == 0) f(Large<T>{});
     else if (shape == 1) f(Middle<T>{});
     else if (shape == 2) f(MiddleAlone<T>{});
-    else if (shape == 3) f(Small<T>{});
+    else if (shape == SMALL) f(Small<T>{});
     else if (shape == 4) f(SmallPair<T>{});
     else f(SmallAlone<T>{});
 }

@@ -273,10 +273,8 @@ __device__ inline void finish_run(const Epilogue &e, int64_t p, int32_t q, const
 // products and the rest the writing of y and z at the memory's rate; dx 265, dw
 // 263 (1,040 TFLOP/s). 10,000 x 768 x 1024 as parts: 76, 57, 63 (630 to 830).
 template <class S, bool ACROSS_A, bool ACROSS_B, class TO>
-__global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void product_kernel(Product pr, Epilogue e)
+__device__ inline void product_block(const Product &pr, const Epilogue &e, const Place &w, char *lds)
 {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const Place w = place_of(pr);
     f32x16 acc[S::TB][S::TA];
     clear<S>(acc);
     if (!tile_product<S, ACROSS_A, ACROSS_B, sizeof(TO) == 4>(pr, w, (typename S::T *)lds, acc)) return;
@@ -298,6 +296,30 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void product_kernel(
     };
     if constexpr (ACROSS_A || ACROSS_B) all(Act<BOA_ACT_NONE>{});
     else with_act(e.act, all);
+}
+
+template <class S, bool ACROSS_A, bool ACROSS_B, class TO>
+__global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void product_kernel(Product pr, Epilogue e)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    product_block<S, ACROSS_A, ACROSS_B, TO>(pr, e, place_of(pr, blockIdx.x, gridDim.x), lds);
+}
+
+// Both gradients' products in one launch, where their tiles fit on the GPU
+// together and neither sum is so long that splits of it would be faster: the first
+// `blocks` for dx, the others for dw. M x K x N in bfloat16, one launch and two: 200
+// x 768 x 768 7.0 and 11.3 us, 1000 x 2048 x 768 15.6 and 18.8, 2000 x 768 x 768
+// 18.3 and 20.1; beyond PAIR_STAGES 4000 x 512 x 512 32 and 19. float32, with its
+// copies: 200 x 768 x 768 32 and 34, 1000 x 1024 x 1024 46 and 51, 4000 x 512 x 512
+// 92 and 63.
+constexpr int PAIR_STAGES = 32;
+
+template <class S, class TO>
+__global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void pair_kernel(Product dx, Epilogue ex, Product dw, Epilogue ew, uint32_t blocks)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    if (blockIdx.x < blocks) product_block<S, false, true, TO>(dx, ex, place_of(dx, blockIdx.x, blocks), lds);
+    else product_block<S, true, true, TO>(dw, ew, place_of(dw, blockIdx.x - blocks, gridDim.x - blocks), lds);
 }
 
 // The sum of the splits' shares, in their order; bound by memory (4 splits of 4096
@@ -712,9 +734,9 @@ void launch(Product pr, const Epilogue &e, hipStream_t st)
 
 // out = a b^T with its epilogue; T: the operands' type in the product, TO: the layer's.
 template <class T, class TO, bool ACROSS_A, bool ACROSS_B>
-void product(Operand a, Operand b, int32_t K, Epilogue e, Arena &mem, bool run, hipStream_t st)
+void product(Operand a, Operand b, int32_t K, Epilogue e, Arena &mem, bool run, hipStream_t st, bool small = false)
 {
-    const Cut cut = choose(a.own, b.own, K, sizeof(TO) == 4, 1, false, true);
+    const Cut cut = small ? Cut{SMALL, 1, (int32_t)ceil_div(K, sizeof(TO) == 4 ? 32 : 64)} : choose(a.own, b.own, K, sizeof(TO) == 4, 1, false, true);
     Product pr{};
     pr.a = a, pr.b = b, pr.K = K, pr.batches = 1, pr.splits = cut.splits, pr.steps = cut.steps;
     e.rows = a.own, e.cols = b.own;
@@ -897,7 +919,7 @@ void backward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
         if (d.param_dtype == BOA_T_F32) bias_join_kernel<float><<<grid, 256, 0, st>>>(s.partial, stripes, d.N, (float *)d.dbias);
         else bias_join_kernel<TO><<<grid, 256, 0, st>>>(s.partial, stripes, d.N, (TO *)d.dbias);
     }
-    // dz along k and w across give dx, both across give dw; what they need is copied in few launches
+    // dz along k and w across give dx, both across give dw
     const bool dx = d.dx && M, dw = d.dw && M;
     const float *rows_z = nullptr;
     Operand z_dx{}, w_dx{}, z_dw{}, x_dw{};
@@ -926,15 +948,37 @@ void backward(const boa_dense &d, Arena &mem, bool run, hipStream_t st)
     e.act = BOA_ACT_NONE;
     const int64_t kept = mem.used;   // the two products' sums take turns
     int64_t most = kept;
+    using S = Small<T>;
+    auto tiles = [](int64_t a, int64_t b) { return ceil_div(a, S::BA) * ceil_div(b, S::BB); };
+    const int64_t blocks = tiles(M, d.K), others = tiles(d.N, d.K);
+    const int32_t deep = WIDE ? 32 : 64;   // k of a stage
+    // by sizes alone: a gradient is the same with the other one and without
+    const bool pair = blocks + others <= 256 * S::PER_CU && std::max(M, d.N) <= PAIR_STAGES * deep;
+    if (pair && dx && dw) {
+        if (run) {
+            Product px{}, pw{};
+            px.a = z_dx, px.b = w_dx, px.K = d.N, pw.a = z_dw, pw.b = x_dw, pw.K = M;
+            Epilogue ex = e, ew = e;
+            ex.out = d.dx, ex.ld = d.K, ex.max_a = rows_z, ex.max_b = most_w, ex.rows = M, ex.cols = d.K;
+            ew.out = d.dw, ew.ld = d.K, ew.max_a = most_z, ew.max_b = most_x, ew.rows = d.N, ew.cols = d.K;
+            for (Product *p : {&px, &pw}) {
+                p->batches = p->splits = 1, p->steps = (int32_t)ceil_div(p->K, deep);
+                p->tiles_a = (int32_t)ceil_div(p->a.own, S::BA), p->tiles_b = (int32_t)ceil_div(p->b.own, S::BB);
+            }
+            const auto kernel = pair_kernel<S, TO>;
+            kernel<<<dim3((uint32_t)(blocks + others)), S::THREADS, S::LDS, st>>>(px, ex, pw, ew, (uint32_t)blocks);
+        }
+        return;
+    }
     if (dx) {
         e.out = d.dx, e.ld = d.K, e.max_a = rows_z, e.max_b = most_w;
-        product<T, TO, false, true>(z_dx, w_dx, d.N, e, mem, run, st);
+        product<T, TO, false, true>(z_dx, w_dx, d.N, e, mem, run, st, pair);
         most = mem.used;
         mem.used = kept;
     }
     if (dw) {
         e.out = d.dw, e.ld = d.K, e.max_a = most_z, e.max_b = most_x;
-        product<T, TO, true, true>(z_dw, x_dw, M, e, mem, run, st);
+        product<T, TO, true, true>(z_dw, x_dw, M, e, mem, run, st, pair);
         most = std::max(most, mem.used);
     } else if (d.dw) {
         const int64_t n = (int64_t)d.N * d.K;

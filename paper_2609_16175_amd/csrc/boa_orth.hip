@@ -184,7 +184,7 @@ template <class S, bool B_ACROSS, bool PARTS>
 __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Product pr, StepArgs e)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const Place w = place_of(pr);
+    const Place w = place_of(pr, blockIdx.x, gridDim.x);
     if (!is_needed(pr, w)) return;
     f32x16 acc[S::TB][S::TA];
     clear<S>(acc);
