@@ -166,6 +166,15 @@ def test_linear(M, N, K, dt):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("M,N,K", [(1, 33, 4100), (16, 48, 4100), (17, 48, 4100), (33, 40, 1500), (48, 4100, 64), (64, 17, 777), (64, 24, 3),
+                                   (65, 33, 1024), (100, 40, 515), (128, 24, 520), (129, 24, 520), (2048, 64, 40), (2049, 64, 40),
+                                   (1024, 100, 72), (1025, 100, 72)])
+def test_where_the_kernels_change(M, N, K, dt):
+    # few rows and many (by rows, k and type), both gradients in one launch and in two
+    both(M, N, K, dt, M + N + K, "gelu_tanh", bias=dt, residual=True)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
 @pytest.mark.parametrize("kind", ACTS)
 @pytest.mark.parametrize("M", [4, 70, 300])
 def test_activations(M, kind, dt):
