@@ -421,9 +421,10 @@ enum { BOA_ACT_NONE = 0, BOA_ACT_RELU = 1, BOA_ACT_SILU = 2, BOA_ACT_GELU = 3, B
  *   dz = dy act'(z)    dx = dz w    dw = dz^T x    dbias = sum over rows of dz
  * (the residual's is dy). x, w, residual, y and their gradients have one type.
  * Sums are float32. In bfloat16 and float16, z is kept in float16, infinite beyond
- * its range (where every act' is constant), and dz is rounded to the layer's type
- * as an operand of the two products, not in dbias. In float32, with more than
- * 16 to 128 rows (by N and K) and in the gradients, the products' operands are
+ * its range (where every act' is constant) and with an absolute error of 2^-25
+ * below 2^-14 (relu: z above 0 stays above 0, so that its slope is 1), and dz is
+ * rounded to the layer's type as an operand of the two products, not in dbias. In
+ * float32, with more than 16 to 128 rows (by N and K) and in the gradients, the products' operands are
  * rounded to 22 bits (values far below the largest of their row, or of their
  * column where the sum runs over rows, to 2^-40 of that). A non-finite value
  * makes the results that it takes part in NaN or infinite.

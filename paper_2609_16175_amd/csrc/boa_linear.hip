@@ -7,8 +7,9 @@
 // A few rows (serving) read the weights once and are bound by that; more are
 // bound by the matrix instructions. 16-bit operands go there as they are, with
 // float32 sums; z is kept for the backward pass in f16 (11 bits, infinite
-// beyond its range, where every activation's slope is constant), and dz, an operand of two
-// products, is rounded to the layer's type. Float32 operands become two f16
+// beyond its range, where every activation's slope is constant, and for relu never 0
+// where z is above 0), and dz, an operand of two products, is rounded to the
+// layer's type. Float32 operands become two f16
 // parts of 11 bits each, scaled by a power of two per row (or per column, where
 // the sum runs over rows) so that the largest value lies below 2^15: three
 // products, each value exact to 2^-22 of itself or 2^-40 of its row's largest.
@@ -200,13 +201,23 @@ __device__ inline Columns<TO> columns_at(const Epilogue &e, int64_t p, int32_t q
     return c;
 }
 
+// z as it is kept. relu's slope is 1 above 0 however near, and a float16 that
+// rounded to 0 would not say so: such z are kept as its smallest value. The other
+// slopes are the same there and at 0 to 2^-24.
+template <class Z, int ACT>
+__device__ inline float to_keep(float z)
+{
+    if constexpr (sizeof(Z) == 2 && ACT == BOA_ACT_RELU) return z > 0.0f ? fmaxf(z, 0x1p-24f) : z;
+    return z;
+}
+
 // One value, at row p and column q.
 template <class TO, int ACT>
 __device__ inline void finish_one(const Epilogue &e, int64_t p, int32_t q, float v, float bias)
 {
     typedef std::conditional_t<sizeof(TO) == 4, float, f16_t> Z;
     v += bias;
-    if (e.pre) ((Z *)e.pre)[p * e.cols + q] = (Z)v;
+    if (e.pre) ((Z *)e.pre)[p * e.cols + q] = (Z)to_keep<Z, ACT>(v);
     v = act_of<sizeof(TO) == 4, ACT>(v);
     if (e.residual) v += (float)((const TO *)e.residual)[p * e.residual_ld + q];
     ((TO *)e.out)[p * e.ld + q] = (TO)v;
@@ -251,7 +262,12 @@ __device__ inline void finish_run(const Epilogue &e, int64_t p, int32_t q, const
         if constexpr (WIDE) v[i] = ldexpf(v[i], -(s + c.shift[i]));
         v[i] += c.bias[i];
     }
-    if (e.pre) store8(c.pre, v);
+    if (e.pre) {
+        float z[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = to_keep<typename Columns<TO>::Z, ACT>(v[i]);
+        store8(c.pre, z);
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = act_of<WIDE, ACT>(v[i]);
     if (e.residual) {

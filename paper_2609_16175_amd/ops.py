@@ -459,8 +459,8 @@ def linear_forward(x, weight, bias=None, residual=None, activation="none", keep=
     (N,) of x's type or float32; residual: like y, (..., N). activation: "none",
     "relu", "silu", "gelu" (the error function's) or "gelu_tanh". pre is what
     linear_backward takes where there is an activation: x @ weight.T + bias in
-    float16, infinite beyond its range (float32 for float32 layers); None
-    without `keep` or without an activation."""
+    float16, infinite beyond its range and for relu never 0 where it is above 0
+    (float32 for float32 layers); None without `keep` or without an activation."""
     _device("linear", x, weight, bias, residual)
     dt = _dtype("linear", x)
     act = _activation("linear", activation)
