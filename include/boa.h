@@ -501,7 +501,7 @@ typedef struct {
        y and h are not read, eps neither) */
     const void *dh;         /* rows x d, or NULL (zeros) */
     int64_t dh_stride;
-    const void *dy;         /* rows x d, or NULL (zeros) */
+    const void *dy;         /* rows x d, or NULL (nothing comes back through the second norm, whatever h is) */
     int64_t dy_stride;
     void *dx, *df;          /* rows x d, dense, or NULL */
     void *dgate;            /* like gate (dense), or NULL */

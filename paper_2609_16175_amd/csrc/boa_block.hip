@@ -317,30 +317,30 @@ __global__ __launch_bounds__(threads_of(TPR), (ROW_AHEAD<T, NV> ? 2 : 1)) void b
 #pragma unroll
             for (int j = 0; j < VEC; ++j) g1[j] = at.template mine<WHOLE>(j) ? g1[j] * w[j] : 0.0f;
         };
-        // h again, its norm, and the gradient through it
+        // h again, its norm, and the gradient through it; without dy nothing comes through it, whatever h is
         float c1 = 0.0f, c2 = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const Cols<VEC, TPR> at(i, lane, d);
-            float fn[VEC], pw[VEC], pb[VEC], g[VEC], g1[VEC], t[VEC];
-            fn_at(fn, i);
-            param(pw, PW, i, at.c);
-            param(pb, PB, i, at.c);
-            gate_at(g, i, at.c);
-            g1_at(g1, at, i);
-            unpack<T, VEC>(t, dy[i]);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                v[i][j] = (fmaf(a.scale, v[i][j], g[j] * fmaf(fn[j], pw[j], pb[j])) - hm) * hr;
-                if (DP) {
-                    sums[0][i][j] = fmaf(t[j], v[i][j], sums[0][i][j]);
-                    sums[1][i][j] += t[j];
-                }
-                c1 += g1[j];
-                c2 = fmaf(g1[j], v[i][j], c2);
-            }
-        }
         if (a.dy) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const Cols<VEC, TPR> at(i, lane, d);
+                float fn[VEC], pw[VEC], pb[VEC], g[VEC], g1[VEC], t[VEC];
+                fn_at(fn, i);
+                param(pw, PW, i, at.c);
+                param(pb, PB, i, at.c);
+                gate_at(g, i, at.c);
+                g1_at(g1, at, i);
+                unpack<T, VEC>(t, dy[i]);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    v[i][j] = (fmaf(a.scale, v[i][j], g[j] * fmaf(fn[j], pw[j], pb[j])) - hm) * hr;
+                    if (DP) {
+                        sums[0][i][j] = fmaf(t[j], v[i][j], sums[0][i][j]);
+                        sums[1][i][j] += t[j];
+                    }
+                    c1 += g1[j];
+                    c2 = fmaf(g1[j], v[i][j], c2);
+                }
+            }
             row_sum2<TPR>(c1, c2, red);
             c1 = a.layer ? c1 / (float)d : 0.0f;
             c2 /= (float)d;
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(threads_of(TPR), (ROW_AHEAD<T, NV> ? 2 : 1)) void b
             unpack<T, VEC>(o, dh[i]);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                v[i][j] = fmaf(hr, g1[j] - c1 - v[i][j] * c2, o[j]);
+                v[i][j] = a.dy ? fmaf(hr, g1[j] - c1 - v[i][j] * c2, o[j]) : o[j];
                 o[j] = a.scale * v[i][j];
             }
             if (a.dx) store_mine<T, VEC, TPR, WHOLE>((T *)a.dx + row * (int64_t)d, at, o);
@@ -387,16 +387,16 @@ __global__ __launch_bounds__(threads_of(TPR), (ROW_AHEAD<T, NV> ? 2 : 1)) void b
             row_sum2<TPR>(p1, p2, red);
             p1 = a.layer ? p1 / (float)d : 0.0f;
             p2 /= (float)d;
-        } else {
-            p1 = p2 = 0.0f;
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const Cols<VEC, TPR> at(i, lane, d);
-            float fn[VEC];
-            fn_at(fn, i);
+            if (a.post) {
+                float fn[VEC];
+                fn_at(fn, i);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) v[i][j] = pr * (v[i][j] - p1 - fn[j] * p2);
+                for (int j = 0; j < VEC; ++j) v[i][j] = pr * (v[i][j] - p1 - fn[j] * p2);
+            }
             store_mine<T, VEC, TPR, WHOLE>((T *)a.df + row * (int64_t)d, at, v[i]);
         }
     }
@@ -557,9 +557,12 @@ __global__ __launch_bounds__(THREADS) void block_cols_kernel(BlockArgs a)
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         Wide<T, P> w{a, row, 0.0f, 0.0f, 0.0f, 0.0f};
         w.read_stats();
-        const float dy = w.dy(c), dH = w.dH(c, a.back[2 * row], a.back[2 * row + 1]), t = a.gate_rows ? dH * w.gate(c) : dH;
-        s[0] = fmaf(dy, w.hn(c), s[0]);
-        s[1] += dy;
+        const float dH = w.dH(c, a.back[2 * row], a.back[2 * row + 1]), t = a.gate_rows ? dH * w.gate(c) : dH;
+        if (a.dy) {
+            const float dy = w.dy(c);
+            s[0] = fmaf(dy, w.hn(c), s[0]);
+            s[1] += dy;
+        }
         s[2] = fmaf(t, w.fn(c), s[2]);
         s[3] += t;
     }
