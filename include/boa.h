@@ -530,7 +530,7 @@ int boa_block_norm_backward(const boa_block *b, void *stream);
  * float32, and the results are rounded once; the products' operands are
  * rounded to f16's 11 bits for bfloat16 updates whose rows and cols are 128 or
  * more, to 22 bits for others, not at all for the smallest (up to 64 rows or cols). A value that is not finite makes its matrix NaN,
- * and so may steps that let singular values grow beyond 8.
+ * and so may steps that let singular values grow beyond 2^23.
  */
 typedef struct {
     int32_t dtype;              /* of update and out: any of the three */

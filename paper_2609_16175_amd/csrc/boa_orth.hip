@@ -20,6 +20,8 @@
 // others every operand is two f16 parts (22 bits), and three products. G is
 // scaled by a power of two, which rounds nothing; the rest of 1 / |G| goes into the
 // first step's coefficients.
+#include <cmath>
+
 #include "boa_gemm.h"
 
 using namespace boa;
@@ -27,8 +29,13 @@ using namespace boa;
 namespace {
 
 constexpr int SUM_BLOCKS = 256;   // per matrix, at most
-// f16 copies hold X 2^10, A 2^10, (b A + c A^2) 2^8: values from 2^-24 of that to 64, 64, 255
+// What f16 copies hold of X, A and b A + c A^2: values times 2^10, 2^10, 2^8, or
+// less in steps whose singular values could take them out of float16's range.
 constexpr float X_UP = 1024.0f, A_UP = 1024.0f, B_UP = 256.0f;
+
+struct Scales {
+    float x, a, b;
+};
 
 struct Step {
     float a, b, c;
@@ -175,6 +182,8 @@ struct StepArgs {
     int32_t dtype, turned;
     Step step;
     const Step *first;       // per matrix, in place of `step`, or null
+    Scales up;               // of this step's copies
+    float x_next;            // UPDATE: X's in the next one
 };
 
 // tile_product and what becomes of it. B_ACROSS: X, whose rows are k. 4096 x 2048 in
@@ -192,11 +201,13 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Pro
     const Step k = e.first ? e.first[w.batch] : e.step;
     const int64_t base = w.batch * e.to_size;
     if constexpr (!B_ACROSS) {
+        // powers of two, all of them
+        const float gram = e.up.a / (e.up.x * e.up.x), linear = e.up.b / e.up.a, quadratic = e.up.b / (e.up.a * e.up.a);
         auto value = [&](float v, int64_t at) {
-            if (e.kind == GRAM) return v * (A_UP / (X_UP * X_UP));
+            if (e.kind == GRAM) return v * gram;
             float was = (float)e.a[at];
             if (e.to_parts) was += (float)e.a[at + e.to_parts];
-            return k.b * was * (B_UP / A_UP) + k.c * (v * (B_UP / (A_UP * A_UP)));
+            return k.b * was * linear + k.c * (v * quadratic);
         };
         each_run<S>(w, acc, lds, [](int32_t, int32_t, int) { return Nothing{}; },
             [&](int32_t p, int32_t q, const float *v, const Nothing &) {
@@ -218,7 +229,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Pro
             });
     } else {
         float *x = e.x + w.batch * e.x_size;
-        constexpr float BY = 1.0f / (B_UP * X_UP);
+        const float by = 1.0f / (e.up.b * e.up.x);
         auto put = [&](int64_t at, float v) {
             const int64_t i = w.batch * e.out_size + at;
             if (e.dtype == BOA_T_F32) ((float *)e.out)[i] = v;
@@ -233,12 +244,12 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Pro
                 load_f32<4, float>(*(float(*)[4])was, x + at);
                 load_f32<4, float>(*(float(*)[4])(was + 4), x + at + 4);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = fmaf(k.a, was[i], v[i] * BY);
+                for (int i = 0; i < 8; ++i) o[i] = fmaf(k.a, was[i], v[i] * by);
                 if (e.kind == UPDATE) {
                     store_f32<4, float>(x + at, *(float(*)[4])o);
                     store_f32<4, float>(x + at + 4, *(float(*)[4])(o + 4));
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] *= X_UP;
+                    for (int i = 0; i < 8; ++i) o[i] *= e.x_next;
                     write16(e.to + base + at, e.to_parts, o);
                 } else if (!e.turned) {
                     if (q + 8 <= e.cols && e.dtype != BOA_T_F32) {
@@ -257,7 +268,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void step_kernel(Pro
                 if (q >= e.cols) return;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (p + i < e.rows) put(q * e.out_ld + p + i, fmaf(k.a, x[(p + i) * e.to_ld + q], v[i] * BY));
+                    if (p + i < e.rows) put(q * e.out_ld + p + i, fmaf(k.a, x[(p + i) * e.to_ld + q], v[i] * by));
             });
     }
 }
@@ -445,6 +456,40 @@ void step(const Operand &a, const Operand &b, int32_t K, bool parts, int64_t bat
     });
 }
 
+// The power of two, `most` at most, that keeps values of up to m below 2^13: an eighth of float16's range, which leaves
+// room for what the roundings of the copies add to singular values.
+float scale_for(double m, double most)
+{
+    int e = 0;
+    (void)std::frexp(m, &e);
+    return (float)std::min(most, std::ldexp(1.0, std::max(13 - e, -100)));
+}
+
+// The scales of each step. No value of a matrix is above its largest singular
+// value. That is below 2 for the first X (whose coefficients make a step of values
+// up to 1 of it), then at most the largest that a step makes of all values up to
+// the bound before it; beyond 2^30 it is not followed. Polynomials over [0, end]
+// have their extremes at its end or where their slopes are 0 (places that do not
+// exist are infinite or NaN, and not in there).
+void scales_of(const Step *step, int32_t steps, Scales *to)
+{
+    double s = 1.0;
+    for (int i = 0; i < steps; ++i) {
+        const double x = i ? s : 2.0, a = step[i].a, b = step[i].b, c = step[i].c, end = s * s;   // u = s^2 from here
+        auto largest = [&](auto f, std::initializer_list<double> flat) {
+            double m = std::fabs(f(end));
+            for (double u : flat)
+                if (u > 0.0 && u < end) m = std::max(m, std::fabs(f(u)));
+            return m;
+        };
+        const double poly = largest([&](double u) { return u * (b + u * c); }, {-b / (2 * c)});
+        to[i] = Scales{scale_for(x, X_UP), scale_for(x * x, A_UP), scale_for(poly, B_UP)};
+        const double root = std::sqrt(9 * b * b - 20 * a * c);
+        s = std::min(0x1p30, largest([&](double u) { return std::sqrt(u) * (a + u * (b + u * c)); },
+                                     {(-3 * b + root) / (10 * c), (-3 * b - root) / (10 * c), -a / (3 * b)}));   // the last where c is 0
+    }
+}
+
 int check(const boa_orth *d)
 {
     if (!d) return set_error(BOA_EINVAL, "orthogonalize: NULL arguments");
@@ -527,10 +572,14 @@ void orthogonalize(const boa_orth &d, Arena &mem, bool run, hipStream_t st)
         return o;
     };
     const Operand A = operand(a16, a_ld, a_size, m, false), B = operand(b16, a_ld, a_size, m, false);
+    Step each[BOA_MAX_ORTH_STEPS];
+    Scales up[BOA_MAX_ORTH_STEPS];
+    for (int i = 0; i < d.steps; ++i) each[i] = coefficients(i);
+    scales_of(each, d.steps, up);
     for (int i = 0; i < d.steps; ++i) {
         const Operand X = operand(x16[i & 1], x_ld, x_size, m, false), Xk = operand(x16[i & 1], x_ld, x_size, x_ld, true);
         StepArgs e{};
-        e.step = coefficients(i), e.first = i == 0 ? first : nullptr;
+        e.step = each[i], e.first = i == 0 ? first : nullptr, e.up = up[i];
         e.rows = m, e.to_ld = a_ld, e.to_size = a_size * copies, e.to_parts = parts ? a_size : 0;
         e.kind = GRAM, e.to = a16;
         step<false>(X, X, n, parts, C, e, st);
@@ -538,7 +587,7 @@ void orthogonalize(const boa_orth &d, Arena &mem, bool run, hipStream_t st)
         step<false>(A, A, m, parts, C, e, st);
         e.kind = i + 1 < d.steps ? UPDATE : LAST;
         e.to = x16[(i + 1) & 1], e.to_ld = x_ld, e.to_size = x_size * copies, e.to_parts = parts ? x_size : 0;
-        e.x = x, e.x_size = x_size;
+        e.x = x, e.x_size = x_size, e.x_next = i + 1 < d.steps ? up[i + 1].x : 0.0f;
         e.out = d.out, e.out_ld = d.cols, e.out_size = (int64_t)d.rows * d.cols, e.cols = n, e.dtype = d.dtype, e.turned = turned;
         step<true>(B, Xk, m, parts, C, e, st);
     }
