@@ -317,30 +317,30 @@ __global__ __launch_bounds__(threads_of(TPR), (ROW_AHEAD<T, NV> ? 2 : 1)) void b
 #pragma unroll
             for (int j = 0; j < VEC; ++j) g1[j] = at.template mine<WHOLE>(j) ? g1[j] * w[j] : 0.0f;
         };
-        // h again, its norm, and the gradient through it; without dy nothing comes through it, whatever h is
+        // h again, its norm, and the gradient through it (without dy none of that is used)
         float c1 = 0.0f, c2 = 0.0f;
-        if (a.dy) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const Cols<VEC, TPR> at(i, lane, d);
-                float fn[VEC], pw[VEC], pb[VEC], g[VEC], g1[VEC], t[VEC];
-                fn_at(fn, i);
-                param(pw, PW, i, at.c);
-                param(pb, PB, i, at.c);
-                gate_at(g, i, at.c);
-                g1_at(g1, at, i);
-                unpack<T, VEC>(t, dy[i]);
+        for (int i = 0; i < NV; ++i) {
+            const Cols<VEC, TPR> at(i, lane, d);
+            float fn[VEC], pw[VEC], pb[VEC], g[VEC], g1[VEC], t[VEC];
+            fn_at(fn, i);
+            param(pw, PW, i, at.c);
+            param(pb, PB, i, at.c);
+            gate_at(g, i, at.c);
+            g1_at(g1, at, i);
+            unpack<T, VEC>(t, dy[i]);
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    v[i][j] = (fmaf(a.scale, v[i][j], g[j] * fmaf(fn[j], pw[j], pb[j])) - hm) * hr;
-                    if (DP) {
-                        sums[0][i][j] = fmaf(t[j], v[i][j], sums[0][i][j]);
-                        sums[1][i][j] += t[j];
-                    }
-                    c1 += g1[j];
-                    c2 = fmaf(g1[j], v[i][j], c2);
+            for (int j = 0; j < VEC; ++j) {
+                v[i][j] = (fmaf(a.scale, v[i][j], g[j] * fmaf(fn[j], pw[j], pb[j])) - hm) * hr;
+                if (DP) {
+                    sums[0][i][j] = fmaf(t[j], v[i][j], sums[0][i][j]);
+                    sums[1][i][j] += t[j];
                 }
+                c1 += g1[j];
+                c2 = fmaf(g1[j], v[i][j], c2);
             }
+        }
+        if (a.dy) {
             row_sum2<TPR>(c1, c2, red);
             c1 = a.layer ? c1 / (float)d : 0.0f;
             c2 /= (float)d;
@@ -413,6 +413,7 @@ __global__ __launch_bounds__(threads_of(TPR), (ROW_AHEAD<T, NV> ? 2 : 1)) void b
                         if (!at.template mine<WHOLE>(j)) continue;
 #pragma unroll
                         for (int q = 0; q < SUMS; ++q) {
+                            if (q == 0 && !a.dy) sums[q][i][j] = 0.0f;   // 0 times a row that is not finite
                             float *to = (GROUPS == 1 ? out : cols) + (int64_t)q * d + at.c + j;
                             *to = k ? *to + sums[q][i][j] : sums[q][i][j];
                         }
