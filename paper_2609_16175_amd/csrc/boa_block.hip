@@ -53,9 +53,9 @@ const T *plus(const void *p, int64_t n) { return p ? (const T *)p + n : nullptr;
 template <class T>
 T *plus(void *p, int64_t n) { return p ? (T *)p + n : nullptr; }
 
-// The arguments of the rows from `row` on that one launch takes.
+// The arguments of the rows from `row` on, `most` at most.
 template <class T>
-BlockArgs rows_from(BlockArgs a, int64_t row)
+BlockArgs rows_from(BlockArgs a, int64_t row, int64_t most)
 {
     a.x = plus<T>(a.x, row * a.x_ld), a.f = plus<T>(a.f, row * a.f_ld);
     if (a.gate_rows) a.gate = plus<T>(a.gate, row * a.gate_ld);
@@ -63,8 +63,16 @@ BlockArgs rows_from(BlockArgs a, int64_t row)
     a.h = plus<T>(a.h, row * a.d), a.y = plus<T>(a.y, row * a.d), a.dx = plus<T>(a.dx, row * a.d);
     a.df = plus<T>(a.df, row * a.d), a.dgate = plus<T>(a.dgate, row * a.d);
     a.stats = plus<float>(a.stats, row), a.back = plus<float>(a.back, 2 * row);
-    a.rows = std::min(LAUNCH_ROWS, a.rows - row);
+    a.rows = std::min(most, a.rows - row);
     return a;
+}
+
+// f(arguments) for the rows of each launch of blocks of `threads` threads, which take `each` rows.
+template <class T, class F>
+void in_launches(const BlockArgs &a, int32_t threads, int32_t each, F f)
+{
+    const int64_t most = std::min(LAUNCH_ROWS, ((int64_t)1 << 31) / threads * each);   // 2^32 threads would be refused
+    for (int64_t row = 0; row < a.rows; row += most) f(rows_from<T>(a, row, most));
 }
 
 // A vector of parameters at a thread's columns, `or_else` where there is none.
@@ -726,16 +734,17 @@ int boa_block_norm(const boa_block *b, void *stream)
         using T = decltype(t);
         using P = decltype(p);
         constexpr int VEC = 16 / sizeof(T);
-        for (int64_t row = 0; row < b->rows; row += LAUNCH_ROWS) {
-            const BlockArgs n = rows_from<T>(a, row);
-            const bool fits = with_shape<VEC, true>(b->d, [&](auto nv, auto tpr, auto whole) {
-                constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value;
-                constexpr bool WHOLE = decltype(whole)::value;
-                block_kernel<T, P, NV, TPR, WHOLE>
-                    <<<dim3((uint32_t)ceil_div(n.rows, threads_of(TPR) / TPR)), threads_of(TPR), 0, st>>>(n);
+        const bool fits = with_shape<VEC, true>(b->d, [&](auto nv, auto tpr, auto whole) {
+            constexpr int NV = decltype(nv)::value, TPR = decltype(tpr)::value, BLOCK = threads_of(TPR), EACH = BLOCK / TPR;
+            constexpr bool WHOLE = decltype(whole)::value;
+            in_launches<T>(a, BLOCK, EACH, [&](const BlockArgs &n) {
+                block_kernel<T, P, NV, TPR, WHOLE><<<dim3((uint32_t)ceil_div(n.rows, EACH)), BLOCK, 0, st>>>(n);
             });
-            if (!fits) block_wide_kernel<T, P><<<dim3((uint32_t)n.rows), THREADS, 0, st>>>(n);
-        }
+        });
+        if (!fits)
+            in_launches<T>(a, THREADS, 1, [&](const BlockArgs &n) {
+                block_wide_kernel<T, P><<<dim3((uint32_t)n.rows), THREADS, 0, st>>>(n);
+            });
         return launch_status("block_norm");
     });
 }
@@ -770,10 +779,9 @@ int boa_block_norm_backward(const boa_block *b, void *stream)
             else block_back_kernel<T, P, NV, TPR, WHOLE, false><<<grid, threads_of(TPR), lds, st>>>(a);
         });
         if (!fits) {
-            for (int64_t row = 0; row < b->rows; row += LAUNCH_ROWS) {
-                const BlockArgs n = rows_from<T>(a, row);
+            in_launches<T>(a, THREADS, 1, [&](const BlockArgs &n) {
                 block_back_wide_kernel<T, P><<<dim3((uint32_t)n.rows), THREADS, 0, st>>>(n);
-            }
+            });
             if (sums) block_cols_kernel<T, P><<<dim3((uint32_t)blocks, (uint32_t)ceil_div(b->d, THREADS)), THREADS, 0, st>>>(a);
         }
         if (sums) {

@@ -1,4 +1,5 @@
-"""The norms around a residual block where values are not finite, on the GPU."""
+"""The norms around a residual block where values are not finite and where a
+launch ends, on the GPU."""
 import math
 
 import pytest
@@ -43,3 +44,20 @@ def test_values_that_are_not_finite_without_dy(d, post, pre, gate, dt):
         # a norm spreads them over its row
         spoilt = (~torch.isfinite(got.dgate)).cpu().nonzero().flatten().tolist()
         assert spoilt == (list(range(d)) if post else sorted({d // 3, 1}))
+
+
+@pytest.mark.parametrize("d", [4104, 8192])
+def test_more_rows_than_a_launch_with_512_threads_a_row_takes(d):
+    # a block of 512 threads a row: 2^22 rows a launch; only the residual sum, of x with itself
+    rows = (1 << 23) + 5 if d == 4104 else (1 << 22) + 5
+    x = torch.empty(rows, d, device="cuda", dtype=BF16)
+    x.view(torch.int16).fill_(0x3F80)   # ones
+    at = sorted({0, (1 << 22) - 1, 1 << 22, (1 << 22) + 4, rows - 1})
+    g = torch.Generator().manual_seed(1)
+    some = torch.randn(len(at), d, generator=g).bfloat16()
+    x[at] = some.cuda()
+    h, y, stats = boa.block_norm_forward(x, x, pre=False, scale=0.5)
+    assert y is None
+    assert torch.equal(h[at].cpu(), (some.float() * 1.5).bfloat16())
+    for lo in range(0, rows, 1 << 20):   # every other row was written, too
+        assert int((h[lo:lo + (1 << 20), ::512] == 1.5).sum(1).eq(h[:1, ::512].numel()).sum()) >= min(rows - lo, 1 << 20) - len(at)
