@@ -1,9 +1,11 @@
 """Linear layers at the ends of their ranges, on the GPU against plain float64
-computations: pre-activations next to 0.
+computations: pre-activations next to 0, gelu far below 0.
 
 `unit`, `tiny`, `within` and the bound of a product's sums are those of
 test_gpu_linear.py.
 """
+import math
+
 import pytest
 import torch
 
@@ -80,3 +82,25 @@ def test_activations_of_small_values(kind, dt, by_x, by_w):
         within(y, z / 2, 1.01 * (unit(dt) * z.abs() / 2 + e) + tiny(dt), kind)
         grads = boa.linear_backward(dy.cuda(), x.cuda(), w.cuda(), pre, activation=kind)
         linears.check(x, w, None, None, kind, dt, None, dy, grads, dt)
+
+
+@pytest.mark.parametrize("dt", [F32])
+@pytest.mark.parametrize("M", [16, 640])
+def test_gelu_far_below_zero(M, dt):
+    """Held relative to the values. z is exact: one product, with 1. The
+    distribution and its density are good to 2^-21 and some roundings of
+    themselves, 2^-20 in all. The slope is rounded to the layer's type as dz, and
+    dx, its product with 1, is the same value."""
+    values = (-torch.arange(2 * 64, 12 * 64, dtype=torch.float64) / 64).to(dt)
+    w = torch.ones(1, 1, dtype=dt)
+    for x in values[:, None].split(M):
+        z = x.double()
+        y, pre = boa.linear_forward(x.cuda(), w.cuda(), activation="gelu", keep=True)
+        off = 2.0 ** -20
+        below = 0.5 * torch.special.erfc(-z / math.sqrt(2))   # torch's ndtr is 1 + erf, which cancels
+        want = z * below
+        within(y, want, 1.01 * (unit(dt) + off) * want.abs() + tiny(dt), "y")
+        dx, _, _ = boa.linear_backward(torch.ones_like(y), x.cuda(), w.cuda(), pre, activation="gelu", need=(True, False, False))
+        other = z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+        want = below + other
+        within(dx, want, 1.01 * (unit(dt) * want.abs() + off * (below + other.abs())) + tiny(dt), "dx")
