@@ -16,6 +16,7 @@ from array import array
 from dataclasses import dataclass
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import _check, lib
@@ -553,9 +554,11 @@ class _Linear(torch.autograd.Function):
 
 
 def linear(x, weight, bias=None, residual=None, activation="none"):
-    """linear_forward's y, for autograd."""
-    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
-                                    or residual is not None and residual.requires_grad):
+    """linear_forward's y, for autograd. Forward-mode tangents raise."""
+    # past its function, which refuses them, a call would drop the tangents that there can be at a forward-mode level
+    if forward_ad._current_level >= 0 or torch.is_grad_enabled() and (
+            x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
+            or residual is not None and residual.requires_grad):
         return _Linear.apply(x, weight, bias, residual, activation)
     return linear_forward(x, weight, bias, residual, activation)[0]
 
