@@ -379,8 +379,10 @@ def softmax_xent(h, rows, labels, bias=None, scale=1.0, reduction="mean"):
     compute, the losses alone. A reduced loss' gradients are formed with it and
     multiplied by the gradient that arrives, in h's and rows' type: bfloat16
     ones are rounded a second time then. softmax_xent_grad with dloss rounds
-    once."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (h, rows, bias)):
+    once. Forward-mode tangents raise."""
+    # past its function, which refuses them, a call would drop the tangents that there can be at a forward-mode level
+    if forward_ad._current_level >= 0 or torch.is_grad_enabled() and any(
+            t is not None and t.requires_grad for t in (h, rows, bias)):
         return _SoftmaxXent.apply(h, rows, labels, bias, scale, reduction)
     return _xent("softmax_xent", h, rows, labels, bias, scale, reduction, None, False).loss
 

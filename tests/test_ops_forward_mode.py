@@ -15,7 +15,12 @@ def plain(monkeypatch):
         y = x @ weight.t()
         return y if bias is None else y + bias, None
 
+    def xent(name, h, rows, labels, bias, scale, reduction, stream, grad, *rest):
+        z = torch.zeros(())
+        return ops.XentResult(z, z, *(z,) * 3 if grad else ())
+
     monkeypatch.setattr(ops, "linear_forward", linear_forward)
+    monkeypatch.setattr(ops, "_xent", xent)
 
 
 def tensors():
@@ -30,6 +35,16 @@ def test_linear(plain, which, grad):
         t[which] = forward_ad.make_dual(t[which], torch.ones_like(t[which]))
         with pytest.raises(NotImplementedError, match="forward mode"):
             boa.linear(*t)
+
+
+@pytest.mark.parametrize("which", [0, 1, 3])
+def test_softmax_xent(plain, which):
+    t = [torch.ones(2, 3), torch.ones(4, 3), torch.zeros(2, dtype=torch.int64), torch.ones(4)]
+    with forward_ad.dual_level():
+        t[which] = forward_ad.make_dual(t[which], torch.ones_like(t[which]))
+        for reduction in ("mean", "none"):
+            with pytest.raises(NotImplementedError, match="forward mode"):
+                boa.softmax_xent(*t, reduction=reduction)
 
 
 def test_without_tangents(plain):
