@@ -527,10 +527,12 @@ int boa_block_norm_backward(const boa_block *b, void *stream);
  *   X <- a X + (b X X^T + c (X X^T)^2) X
  * for each step's a, b, c: every singular value s of X becomes a s + b s^3 +
  * c s^5, the singular vectors stay. A zero update stays zero. X is held in
- * float32, and the results are rounded once; the products' operands are
- * rounded to f16's 11 bits for bfloat16 updates whose rows and cols are 128 or
- * more, to 22 bits for others, not at all for the smallest (up to 64 rows or cols). A value that is not finite makes its matrix NaN,
- * and so may steps that let singular values grow beyond 2^23.
+ * float32, and the results are rounded once; the products' operands are rounded to
+ * f16's 11 bits for bfloat16 updates whose rows and cols are 128 or more, to 22 bits
+ * for others, and not at all for the smallest, which a CU's LDS holds: up to 16, 32,
+ * 48 or 64 rows (or cols) of up to 2,048, 1,024, 672 or 480 values. A value that is
+ * not finite makes its matrix NaN, and so may steps that let singular values grow
+ * beyond 2^23.
  */
 typedef struct {
     int32_t dtype;              /* of update and out: any of the three */
