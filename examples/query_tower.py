@@ -66,7 +66,7 @@ class Tower:
         return y
 
     def __call__(self, x):
-        return self.hidden(x) @ self.W.t()
+        return boa.linear(self.hidden(x), self.W)
 
     @torch.no_grad()
     def step_hidden(self, lr=0.02, beta=0.9):
