@@ -423,11 +423,12 @@ enum { BOA_ACT_NONE = 0, BOA_ACT_RELU = 1, BOA_ACT_SILU = 2, BOA_ACT_GELU = 3, B
  * Sums are float32. In bfloat16 and float16, z is kept in float16, infinite beyond
  * its range (where every act' is constant) and with an absolute error of 2^-25
  * below 2^-14 (relu: z above 0 stays above 0, so that its slope is 1), and dz is
- * rounded to the layer's type as an operand of the two products, not in dbias. In
- * float32, with more than 16 to 128 rows (by N and K) and in the gradients, the products' operands are
- * rounded to 22 bits (values far below the largest of their row, or of their
- * column where the sum runs over rows, to 2^-40 of that). A non-finite value
- * makes the results that it takes part in NaN or infinite.
+ * rounded to the layer's type as an operand of the two products, not in dbias
+ * (float16's is infinite beyond its range, and its steps are 2^-24 below 2^-14). In
+ * float32, with more than 16 to 128 rows (by N and K) and in the gradients, the
+ * products' operands are rounded to 22 bits (values far below the largest of their
+ * row, or of their column where the sum runs over rows, to 2^-40 of that). A
+ * non-finite value makes the results that it takes part in NaN or infinite.
  */
 typedef struct {
     int32_t dtype;          /* any of the three */
@@ -529,8 +530,9 @@ int boa_block_norm_backward(const boa_block *b, void *stream);
  * c s^5, the singular vectors stay. A zero update stays zero. X is held in
  * float32, and the results are rounded once; the products' operands are rounded to
  * f16's 11 bits for bfloat16 updates whose rows and cols are 128 or more, to 22 bits
- * for others, and not at all for the smallest, which a CU's LDS holds: up to 16, 32,
- * 48 or 64 rows (or cols) of up to 2,048, 1,024, 672 or 480 values. A value that is
+ * for others (f16's smallest value ends that at 2^-33 where singular values stay
+ * around 1), and not at all for the smallest, which a CU's LDS holds: up to 16, 32, 48
+ * or 64 rows (or cols) of up to 2,048, 1,024, 672 or 480 values. A value that is
  * not finite makes its matrix NaN, and so may steps that let singular values grow
  * beyond 2^23.
  */

@@ -312,7 +312,7 @@ __device__ inline void finish_run(const Epilogue &e, int64_t p, int32_t q, const
 }
 
 // A forward product (both operands along k) has the whole epilogue, the
-// gradients' none. 32,768 x 1024 x 4096 in bfloat16: forward 391 us, 230 of them
+// gradients' none. 32,768 x 1024 x 4096 in bfloat16: forward 398 us, 230 of them
 // products and the rest the writing of y and z at the memory's rate; dx 265, dw
 // 263 (1,040 TFLOP/s). 10,000 x 768 x 1024 as parts: 76, 57, 63 (630 to 830).
 template <class S, bool ACROSS_A, bool ACROSS_B, class TO>
